@@ -27,7 +27,7 @@
  *   q = j / 4; element j of a worker's vector uses output word j mod 4, low 23 bits.
  *   domain 0: C_nat, 1: D_nat rounding, 2: sparsifier selection, 3: low bits of binary64
  *   thresholds, 4: byte-wide draws of nc_compress_bf16_r8, 5: half-word draws of
- *   nc_compress_f16_r16.
+ *   nc_compress_f16_r16, 6: byte-wide draws of the 8-bit activation checkpoints.
  * The stream depends on (seed, worker, j) only, so outputs are reproducible and
  * independent of launch geometry.
  *
@@ -433,6 +433,73 @@ nc_status nc_topk_compress(const float* x, size_t d, uint64_t K, uint64_t seed, 
  * >= d are skipped.  Indices of one list are distinct, so no atomics are needed. */
 nc_status nc_topk_decode_accumulate(const uint32_t* idx, const uint8_t* exp, const uint32_t* sign,
                                     size_t count, size_t d, float* acc, cudaStream_t stream);
+
+/* ---- training operators around 8-bit activation checkpoints (no counterpart in the paper) ------
+ * The other side of a training step whose gradients the calls above exchange: activations kept in
+ * 8 bits between the forward and the backward pass, layer norm with its gradients, and the weight
+ * gradient of a linear layer whose input was kept.
+ *
+ * Checkpoint of a rows x cols matrix: every row is cut into blocks of 32 neighbouring values (the
+ * last one is filled up with zeros; pitch = cols rounded up to 32).  A block's unit is 2^e, the
+ * smallest power of two with max|x| <= 127 * 2^e, e >= -118.
+ *   codes[row * pitch + col]        (sign << 7) | m, the value +-m * 2^e, 0 <= m <= 127
+ *   scales[row * pitch / 32 + b]    e + 127 of block b of the row; 255: the block holds an inf or a
+ *                                   NaN, its codes are 0 and it decodes to NaN
+ *   NC_ROUND_NEAREST  m = |x| / 2^e rounded to nearest, ties to even: off by half a unit at most
+ *   NC_ROUND_RANDOM   m = floor((Y + r) / 256), Y = 256 |x| / 2^e rounded to nearest, ties to even,
+ *                     r = byte (j mod 4) of stream word j / 4 of (seed, worker, domain 6),
+ *                     j = row * pitch + col: the expectation of m is Y / 256
+ * A value has 7 significant bits, so it is exact in bfloat16 (a magnitude above 127.5 * 2^121
+ * may round up to inf, and in binary16 one above 65,024, as in any rounding to fewer bits).
+ *
+ * Matrices are row-major with a row stride ld* >= cols in elements and any alignment of whole
+ * elements (rows on 16-byte boundaries are read and written in vectors); dtype is one of
+ * NC_DTYPE_*.  codes, scales and workspace are 16-byte aligned, fp32 vectors 4-byte.  Sums and
+ * statistics are binary32.  An output may not overlap an input, except that dx may be dres.  Calls
+ * with rows == 0 or cols == 0 write nothing, except that sums over no rows are 0 (rows == 0 clears
+ * dgamma, dbeta, dw and db unless `accumulate`).  No call holds state; every result is the same
+ * from run to run on one device. */
+enum { NC_ROUND_NEAREST = 0, NC_ROUND_RANDOM = 1 };
+size_t nc_act8_code_bytes(size_t rows, size_t cols);    /* rows * pitch */
+size_t nc_act8_scale_bytes(size_t rows, size_t cols);   /* rows * pitch / 32, rounded up to 16
+                                                           (the filling is not written) */
+/* At most 2^36 - 32 codes in one call (NC_ERR_TOO_LARGE). */
+nc_status nc_act8_compress(const void* x, int dtype, size_t rows, size_t cols, size_t ldx,
+                           int rounding, uint64_t seed, uint32_t worker, uint8_t* codes,
+                           uint8_t* scales, cudaStream_t stream);
+nc_status nc_act8_decompress(const uint8_t* codes, const uint8_t* scales, size_t rows, size_t cols,
+                             void* out, int dtype, size_t ldo, cudaStream_t stream);
+
+/* y = gamma * xh + beta, xh = (x - mean) * rstd by rows; mean and 1 / sqrt(variance + eps) of a
+ * row in binary32, the variance from the centred values.  x and y: dtype.  gamma, beta: param_dtype,
+ * cols entries each; NULL: 1, 0.  mean, rstd: fp32[rows], each may be NULL.  codes and scales (both
+ * or neither NULL): checkpoint of xh, rounded from its binary32 values; rounding, seed and worker
+ * concern it alone.  1 <= cols <= 32768 and rows < 2^31, else NC_ERR_TOO_LARGE. */
+nc_status nc_layer_norm_forward(const void* x, int dtype, size_t rows, size_t cols, size_t ldx,
+                                const void* gamma, const void* beta, int param_dtype, float eps,
+                                void* y, size_t ldy, float* mean, float* rstd, uint8_t* codes,
+                                uint8_t* scales, int rounding, uint64_t seed, uint32_t worker,
+                                cudaStream_t stream);
+
+/* With g = gamma * dy:  dx = rstd * (g - mean(g) - xh * mean(g * xh)) + dres,  dgamma = sum over the
+ * rows of dy * xh,  dbeta = sum over the rows of dy (added to what they hold if accumulate != 0).
+ * The first call takes xh = (x - mean) * rstd from the saved input, the second from the checkpoint.
+ * dy, x, dres, dx: dtype.  dres (the gradient that reaches x past the norm) and gamma may be NULL.
+ * dgamma, dbeta: fp32[cols].  workspace: nc_layer_norm_workspace_bytes(rows, cols).  Limits as for
+ * the forward call. */
+size_t nc_layer_norm_workspace_bytes(size_t rows, size_t cols);
+nc_status nc_layer_norm_backward(const void* dy, int dtype, size_t rows, size_t cols, size_t lddy,
+                                 const void* x, size_t ldx, const float* mean, const float* rstd,
+                                 const void* gamma, int param_dtype, const void* dres,
+                                 size_t lddres, void* dx, size_t lddx, float* dgamma, float* dbeta,
+                                 int accumulate, void* workspace, size_t workspace_bytes,
+                                 cudaStream_t stream);
+nc_status nc_act8_layer_norm_backward(const void* dy, int dtype, size_t rows, size_t cols,
+                                      size_t lddy, const uint8_t* codes, const uint8_t* scales,
+                                      const float* rstd, const void* gamma, int param_dtype,
+                                      const void* dres, size_t lddres, void* dx, size_t lddx,
+                                      float* dgamma, float* dbeta, int accumulate, void* workspace,
+                                      size_t workspace_bytes, cudaStream_t stream);
 
 /* ---- debug build (no counterpart in the paper) ------------------------------------------------
  * `python paper_1905_10988_b200/build.py --bounds` builds libnatcomp_bounds.so with -DNC_BOUNDS:

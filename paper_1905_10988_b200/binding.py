@@ -44,7 +44,9 @@ EXPORTS = (
     "nd_sparse_compact_aggregate", "nc_aggregate_compress_shard", "nc_compress_bf16_r8",
     "nc_compress_bf16_r8_batch", "nc_compress_f16_r16", "nc_compress_f16_r16_batch",
     "nd_norm_status", "nd_norms_batch", "nd_round_batch", "nc_debug_bounds_status",
-    "nc_debug_bounds_selftest",
+    "nc_debug_bounds_selftest", "nc_act8_code_bytes", "nc_act8_scale_bytes", "nc_act8_compress",
+    "nc_act8_decompress", "nc_layer_norm_forward", "nc_layer_norm_workspace_bytes",
+    "nc_layer_norm_backward", "nc_act8_layer_norm_backward",
 )
 
 
@@ -578,3 +580,79 @@ def nd_sparse_compact_aggregate(idxs, planes, counts, norms, n, s, d, cap, out,
     _check("nd_sparse_compact_aggregate",
            _nd_sparse_compact_aggregate(_ptrs(idxs), _ptrs(planes), _ptrs(counts), _ptrs(norms),
                                         n, s, d, cap, _ptr(out), _stream(stream)))
+
+
+# ---- training operators around 8-bit activation checkpoints ------------------------------------
+ROUND_NEAREST, ROUND_RANDOM = 0, 1
+_nc_act8_code_bytes = _sig("nc_act8_code_bytes", _sz, _sz, _sz)
+_nc_act8_scale_bytes = _sig("nc_act8_scale_bytes", _sz, _sz, _sz)
+_nc_act8_compress = _sig("nc_act8_compress", C.c_int, _vp, C.c_int, _sz, _sz, _sz, C.c_int,
+                         C.c_uint64, C.c_uint32, _vp, _vp, _vp)
+_nc_act8_decompress = _sig("nc_act8_decompress", C.c_int, _vp, _vp, _sz, _sz, _vp, C.c_int, _sz,
+                           _vp)
+_nc_layer_norm_forward = _sig("nc_layer_norm_forward", C.c_int, _vp, C.c_int, _sz, _sz, _sz, _vp,
+                              _vp, C.c_int, C.c_float, _vp, _sz, _vp, _vp, _vp, _vp, C.c_int,
+                              C.c_uint64, C.c_uint32, _vp)
+_nc_layer_norm_workspace_bytes = _sig("nc_layer_norm_workspace_bytes", _sz, _sz, _sz)
+_nc_layer_norm_backward = _sig("nc_layer_norm_backward", C.c_int, _vp, C.c_int, _sz, _sz, _sz, _vp,
+                               _sz, _vp, _vp, _vp, C.c_int, _vp, _sz, _vp, _sz, _vp, _vp, C.c_int,
+                               _vp, _sz, _vp)
+_nc_act8_layer_norm_backward = _sig("nc_act8_layer_norm_backward", C.c_int, _vp, C.c_int, _sz,
+                                    _sz, _sz, _vp, _vp, _vp, _vp, C.c_int, _vp, _sz, _vp, _sz,
+                                    _vp, _vp, C.c_int, _vp, _sz, _vp)
+
+
+def nc_act8_code_bytes(rows: int, cols: int) -> int:
+    return int(_nc_act8_code_bytes(rows, cols))
+
+
+def nc_act8_scale_bytes(rows: int, cols: int) -> int:
+    return int(_nc_act8_scale_bytes(rows, cols))
+
+
+def nc_act8_compress(x, dtype, rows, cols, ldx, rounding, seed, worker, codes, scales,
+                     stream=None) -> None:
+    _check("nc_act8_compress",
+           _nc_act8_compress(_ptr(x), dtype, rows, cols, ldx, rounding, seed, worker, _ptr(codes),
+                             _ptr(scales), _stream(stream)))
+
+
+def nc_act8_decompress(codes, scales, rows, cols, out, dtype, ldo, stream=None) -> None:
+    _check("nc_act8_decompress",
+           _nc_act8_decompress(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), dtype, ldo,
+                               _stream(stream)))
+
+
+def nc_layer_norm_forward(x, dtype, rows, cols, ldx, gamma, beta, param_dtype, eps, y, ldy, mean,
+                          rstd, codes, scales, rounding, seed, worker, stream=None) -> None:
+    """codes and scales None: no checkpoint.  gamma, beta, mean, rstd may be None."""
+    _check("nc_layer_norm_forward",
+           _nc_layer_norm_forward(_ptr(x), dtype, rows, cols, ldx, _ptr(gamma), _ptr(beta),
+                                  param_dtype, eps, _ptr(y), ldy, _ptr(mean), _ptr(rstd),
+                                  _ptr(codes), _ptr(scales), rounding, seed, worker,
+                                  _stream(stream)))
+
+
+def nc_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_nc_layer_norm_workspace_bytes(rows, cols))
+
+
+def nc_layer_norm_backward(dy, dtype, rows, cols, lddy, x, ldx, mean, rstd, gamma, param_dtype,
+                           dres, lddres, dx, lddx, dgamma, dbeta, accumulate, workspace,
+                           workspace_bytes, stream=None) -> None:
+    _check("nc_layer_norm_backward",
+           _nc_layer_norm_backward(_ptr(dy), dtype, rows, cols, lddy, _ptr(x), ldx, _ptr(mean),
+                                   _ptr(rstd), _ptr(gamma), param_dtype, _ptr(dres), lddres,
+                                   _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), int(accumulate),
+                                   _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def nc_act8_layer_norm_backward(dy, dtype, rows, cols, lddy, codes, scales, rstd, gamma,
+                                param_dtype, dres, lddres, dx, lddx, dgamma, dbeta, accumulate,
+                                workspace, workspace_bytes, stream=None) -> None:
+    _check("nc_act8_layer_norm_backward",
+           _nc_act8_layer_norm_backward(_ptr(dy), dtype, rows, cols, lddy, _ptr(codes),
+                                        _ptr(scales), _ptr(rstd), _ptr(gamma), param_dtype,
+                                        _ptr(dres), lddres, _ptr(dx), lddx, _ptr(dgamma),
+                                        _ptr(dbeta), int(accumulate), _ptr(workspace),
+                                        workspace_bytes, _stream(stream)))
