@@ -501,6 +501,22 @@ nc_status nc_act8_layer_norm_backward(const void* dy, int dtype, size_t rows, si
                                       float* dgamma, float* dbeta, int accumulate, void* workspace,
                                       size_t workspace_bytes, cudaStream_t stream);
 
+/* Weight gradient of a linear layer y = W a whose input a = gamma * xh + beta was kept as the
+ * checkpoint of xh (rows x k):  dw[n][k] = sum over the rows of dy[row][n] * a[row][k],
+ * db[n] = sum over the rows of dy[row][n].  gamma and beta NULL: a is what the checkpoint holds.
+ * dy: bfloat16, rows x n.  dw: n x k, dw_dtype NC_DTYPE_F32 or NC_DTYPE_BF16.  db: fp32[n], may be
+ * NULL.  accumulate != 0: both are added to what they hold.  The product runs in bfloat16 (the
+ * decoded values are exact in it; other types of dy are refused for that reason) with binary32
+ * accumulation on the tensor cores, which truncate: the relative error grows with the rows, about
+ * 1e-5 at 16384.  workspace: nc_act8_weight_grad_workspace_bytes(rows, n, k).
+ * rows, n < 2^31 and k < 2^23, else NC_ERR_TOO_LARGE. */
+size_t nc_act8_weight_grad_workspace_bytes(size_t rows, size_t n, size_t k);
+nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy,
+                              const uint8_t* codes, const uint8_t* scales, size_t k,
+                              const void* gamma, const void* beta, int param_dtype, void* dw,
+                              int dw_dtype, size_t lddw, float* db, int accumulate,
+                              void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
 /* ---- debug build (no counterpart in the paper) ------------------------------------------------
  * `python paper_1905_10988_b200/build.py --bounds` builds libnatcomp_bounds.so with -DNC_BOUNDS:
  * the same entry points, but every global store of the C_nat and D_nat kernels (nc_compress*,

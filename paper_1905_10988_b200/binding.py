@@ -47,6 +47,7 @@ EXPORTS = (
     "nc_debug_bounds_selftest", "nc_act8_code_bytes", "nc_act8_scale_bytes", "nc_act8_compress",
     "nc_act8_decompress", "nc_layer_norm_forward", "nc_layer_norm_workspace_bytes",
     "nc_layer_norm_backward", "nc_act8_layer_norm_backward",
+    "nc_act8_weight_grad_workspace_bytes", "nc_act8_weight_grad",
 )
 
 
@@ -656,3 +657,24 @@ def nc_act8_layer_norm_backward(dy, dtype, rows, cols, lddy, codes, scales, rstd
                                         _ptr(dres), lddres, _ptr(dx), lddx, _ptr(dgamma),
                                         _ptr(dbeta), int(accumulate), _ptr(workspace),
                                         workspace_bytes, _stream(stream)))
+
+
+_nc_act8_weight_grad_workspace_bytes = _sig("nc_act8_weight_grad_workspace_bytes", _sz, _sz, _sz,
+                                            _sz)
+_nc_act8_weight_grad = _sig("nc_act8_weight_grad", C.c_int, _vp, _sz, _sz, _sz, _vp, _vp, _sz, _vp,
+                            _vp, C.c_int, _vp, C.c_int, _sz, _vp, C.c_int, _vp, _sz, _vp)
+
+
+def nc_act8_weight_grad_workspace_bytes(rows: int, n: int, k: int) -> int:
+    return int(_nc_act8_weight_grad_workspace_bytes(rows, n, k))
+
+
+def nc_act8_weight_grad(dy, rows, n, lddy, codes, scales, k, gamma, beta, param_dtype, dw,
+                        dw_dtype, lddw, db, accumulate, workspace, workspace_bytes,
+                        stream=None) -> None:
+    """gamma and beta (None: 1, 0) are those of the norm whose output the layer reads."""
+    _check("nc_act8_weight_grad",
+           _nc_act8_weight_grad(_ptr(dy), rows, n, lddy, _ptr(codes), _ptr(scales), k,
+                                _ptr(gamma), _ptr(beta), param_dtype, _ptr(dw), dw_dtype, lddw,
+                                _ptr(db), int(accumulate), _ptr(workspace), workspace_bytes,
+                                _stream(stream)))
