@@ -509,7 +509,7 @@ nc_status nc_act8_layer_norm_backward(const void* dy, int dtype, size_t rows, si
  * decoded values are exact in it; other types of dy are refused for that reason) with binary32
  * accumulation on the tensor cores, which truncate: the relative error grows with the rows, about
  * 1e-5 at 16384.  workspace: nc_act8_weight_grad_workspace_bytes(rows, n, k).
- * rows, n < 2^31 and k < 2^23, else NC_ERR_TOO_LARGE. */
+ * rows, n, k < 2^31 and n * k below about 2^40, else NC_ERR_TOO_LARGE. */
 size_t nc_act8_weight_grad_workspace_bytes(size_t rows, size_t n, size_t k);
 nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy,
                               const uint8_t* codes, const uint8_t* scales, size_t k,

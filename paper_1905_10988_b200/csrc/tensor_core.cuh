@@ -39,12 +39,15 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
                  : "memory");
 }
 
-// arrive at the barrier that lies at the same place in block `rank` of the cluster
+// Arrive at the barrier that lies at the same place in block `rank` of the cluster.  What the
+// arrival announces was made visible by a proxy fence or a tcgen05 fence before it; a release at
+// cluster scope on top would wait for every access of the thread, global loads included (measured:
+// the weight gradient at 16384 x 4096 x 4096 took 810 us instead of 516).
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank) {
     asm volatile("{\n\t"
                  ".reg .b32 remote;\n\t"
                  "mapa.shared::cluster.u32 remote, %0, %1;\n\t"
-                 "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [remote];\n\t"
+                 "mbarrier.arrive.shared::cluster.b64 _, [remote];\n\t"
                  "}" ::"r"(bar), "r"(rank)
                  : "memory");
 }
@@ -53,7 +56,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n\t"
                  ".reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t"
                  "}"
                  : "=r"(done)

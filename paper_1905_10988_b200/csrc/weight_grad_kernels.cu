@@ -8,16 +8,18 @@
 // binary32 accumulation; a checkpoint's values are exact in bfloat16, so nothing is rounded on the
 // way.  They exist as bfloat16 in shared memory only.
 //
-// A pair of blocks (cta_group::2) computes 256 x 256 values of dW; block r of it brings 128 of the
-// n and 128 of the k.  Both operands have the tokens as their strided dimension, as they lie in
-// memory.  A step is 64 tokens:
-//   - warp 8 copies the dY tile by tensor copies (rows on 16-byte boundaries), or warps 10 to 17
+// A pair of blocks (cta_group::2) computes tiles of 256 x 256 values of dW one after another; block
+// r of it brings 128 of the n and 128 of the k.  Both operands have the tokens as their strided
+// dimension, as they lie in memory.  A step is 64 tokens, and its operands pass through a ring in
+// shared memory:
+//   - one thread copies the dY tile by tensor copies (rows on 16-byte boundaries), or four warps
 //     gather it with plain loads (rows at any element);
-//   - warps 0 to 7 hold the codes of the next four steps in registers, decode them and store them
-//     in the swizzled operand layout;
-//   - one thread of warp 9 of the pair's first block issues the matrix instructions.
-// Few tiles: the tokens are split over several pairs, whose binary32 parts a second kernel adds in
-// order.
+//   - sixteen warps decode, in four groups that take every fourth step: a group holds the codes of
+//     its next step in registers while the other three work, which covers the loads' latency;
+//   - one thread of the pair's first block issues the matrix instructions; TMEM holds two tiles, so
+//     four more warps write one out while the next is computed.
+// The tiles are dealt out evenly to the chip's 74 pairs.  What is left over, fewer tiles than
+// pairs, is split along the tokens, and a second kernel adds its binary32 parts in order.
 #include "act8_common.cuh"
 #include "tensor_core.cuh"
 
@@ -27,14 +29,17 @@ constexpr int kWgTile = 256;             // n and k of a pair's tile
 constexpr int kWgHalf = 128;             // of a block
 constexpr int kWgStep = 64;              // tokens
 constexpr int kWgStages = 6;
-constexpr int kWgAhead = 4;              // steps whose codes are in flight
-constexpr int kWgDecoders = 8, kWgLoaders = 8;       // warps
+constexpr int kWgGroups = 4, kWgGroupWarps = 4;      // decoders
+constexpr int kWgWriters = 4, kWgLoaders = 4;        // warps
+constexpr int kWgCopyWarp = kWgWriters, kWgMmaWarp = kWgWriters + 1;
+constexpr int kWgDecodeWarp = kWgWriters + 2;        // the first of them
+constexpr int kWgLoadWarp = kWgDecodeWarp + kWgGroups * kWgGroupWarps;
 constexpr uint32_t kWgPanel = kWgStep * 128;         // bytes of 64 values x 64 tokens
 constexpr uint32_t kWgOperand = 2 * kWgPanel;        // of a block's half
 constexpr uint32_t kWgStageBytes = 2 * kWgOperand;
 constexpr uint32_t kWgSmem = kWgStages * kWgStageBytes + 1024 + 256 + 2 * kWgTile * 4;
 constexpr int kWgPairs = 74;             // pairs of blocks that the chip holds at a time
-constexpr int kWgMinSteps = 8;           // of a split
+constexpr int kWgMinSteps = 4;           // of a part
 
 struct WgArgs {
     const __nv_bfloat16* dy;
@@ -46,10 +51,12 @@ struct WgArgs {
     void* dw;
     int dw_f32;
     uint64_t lddw;
-    const float* db;                     // complete when the product's epilogue reads it
-    int accumulate, splits;
+    const float* db;                     // complete when dW is written
+    int accumulate;
     bool vector;                         // dw rows may be written 16 bytes at a time
-    float* parts;                        // [splits][n, rounded up to tiles][k, likewise]
+    uint32_t tiles_n, tiles;             // tile i: n tile i % tiles_n, k tile i / tiles_n
+    uint32_t whole, splits;              // tiles from `whole` on are computed in `splits` parts
+    float* parts;                        // [tile - whole][part][256][256]
 };
 
 __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) {
@@ -58,29 +65,88 @@ __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) 
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// what a decoder thread reads of one step: 16 codes in each of the two panels and their scales
-struct WgCodes {
-    uint4 c[2];
-    uint32_t scale[2];
+// the u-th piece of work of a pair: a tile's steps, or a part of them
+struct WgUnit {
+    uint32_t tile, part, first, steps;   // steps == 0: no more work
+    uint64_t n0, k0;                     // of the tile
 };
 
-__device__ __forceinline__ void wg_load_codes(const WgArgs& a, uint64_t t, uint64_t k, WgCodes& r) {
+__device__ __forceinline__ WgUnit wg_unit(const WgArgs& a, uint32_t pair, uint32_t u) {
+    const uint32_t all = (uint32_t)((a.rows + kWgStep - 1) / kWgStep);
+    const uint32_t pairs = gridDim.x >> 1, rounds = a.whole / pairs;
+    WgUnit w = {};
+    if (u < rounds) {
+        w.tile = u * pairs + pair;
+        w.steps = all;
+    } else if (u == rounds && pair < (a.tiles - a.whole) * a.splits) {
+        w.tile = a.whole + pair / a.splits;
+        w.part = pair % a.splits;
+        w.first = (uint32_t)((uint64_t)all * w.part / a.splits);
+        w.steps = (uint32_t)((uint64_t)all * (w.part + 1) / a.splits) - w.first;
+    }
+    w.n0 = (uint64_t)(w.tile % a.tiles_n) * kWgTile;
+    w.k0 = (uint64_t)(w.tile / a.tiles_n) * kWgTile;
+    return w;
+}
+
+// a place in a pair's sequence of steps
+struct WgWalk {
+    WgUnit unit;
+    uint32_t u, step;
+    __device__ __forceinline__ void begin(const WgArgs& a, uint32_t pair) {
+        u = 0;
+        step = 0;
+        unit = wg_unit(a, pair, 0);
+    }
+    __device__ __forceinline__ bool more() const { return unit.steps != 0; }
+    __device__ __forceinline__ void advance(const WgArgs& a, uint32_t pair, uint32_t by) {
+        step += by;
+        while (unit.steps != 0 && step >= unit.steps) {
+            step -= unit.steps;
+            unit = wg_unit(a, pair, ++u);
+        }
+    }
+    __device__ __forceinline__ uint64_t token() const {
+        return (uint64_t)(unit.first + step) * kWgStep;
+    }
+};
+
+// a place in the ring of stages
+struct WgRing {
+    uint32_t stage, parity;
+    __device__ __forceinline__ void advance(uint32_t by) {
+        stage += by;
+        if (stage >= kWgStages) {
+            stage -= kWgStages;
+            parity ^= 1;
+        }
+    }
+};
+
+// what a decoder thread holds of one step: 16 codes of each of four tokens
+struct WgCodes {
+    uint4 c[4];
+    uint32_t scale[4];
+};
+
+__device__ __forceinline__ void wg_load_codes(const WgArgs& a, uint64_t t, uint64_t col, WgCodes& r) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-        const uint64_t col = k + 64 * p;
-        r.c[p] = make_uint4(0u, 0u, 0u, 0u);
-        r.scale[p] = 127u;
-        if (t < a.rows && col < a.pitch) {
-            r.c[p] = __ldg(reinterpret_cast<const uint4*>(a.codes + t * a.pitch + col));
-            r.scale[p] = __ldg(a.scales + ((t * a.pitch + col) >> 5));
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t row = t + 16 * i;
+        r.c[i] = make_uint4(0u, 0u, 0u, 0u);
+        r.scale[i] = 127u;
+        if (row < a.rows && col < a.pitch) {
+            const uint64_t at = row * a.pitch + col;
+            r.c[i] = __ldg(reinterpret_cast<const uint4*>(a.codes + at));
+            r.scale[i] = __ldg(a.scales + (at >> 5));
         }
     }
 }
 
-// sixteen codes -> two swizzled 16-byte chunks of the thread's line
-__device__ __forceinline__ void wg_decode(const uint4& c, uint32_t scale, uint32_t line,
-                                          uint32_t chunk, uint32_t flip) {
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+// sixteen codes -> the two 16-byte chunks at `first` and `second`, of the words' first and second
+// half
+__device__ __forceinline__ void wg_decode(const uint32_t (&w)[4], uint32_t scale, uint32_t first,
+                                          uint32_t second) {
     uint32_t v[8];
     if (scale <= kAct8MaxFast) {
         const uint32_t fields = act8_fields(scale);
@@ -96,8 +162,7 @@ __device__ __forceinline__ void wg_decode(const uint4& c, uint32_t scale, uint32
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                         line + (((chunk + h) ^ flip) << 4)),
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(h ? second : first),
                      "r"(v[4 * h]), "r"(v[4 * h + 1]), "r"(v[4 * h + 2]), "r"(v[4 * h + 3])
                      : "memory");
 }
@@ -115,40 +180,78 @@ __device__ __forceinline__ uint4 wg_load_dy8(const WgArgs& a, uint64_t t, uint64
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// four neighbouring values of dW, `add` = beta's part
+__device__ __forceinline__ void wg_store4(const WgArgs& a, uint64_t n, uint64_t k, float (&v)[4]) {
+    if (a.dw_f32) {
+        float* p = static_cast<float*>(a.dw) + n * a.lddw + k;
+        if (a.vector && k + 4 <= a.k) {
+            float4 o = make_float4(v[0], v[1], v[2], v[3]);
+            if (a.accumulate) {
+                const float4 old = *reinterpret_cast<const float4*>(p);
+                o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+            }
+            *reinterpret_cast<float4*>(p) = o;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k + i < a.k) p[i] = a.accumulate ? p[i] + v[i] : v[i];
+        }
+    } else {
+        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + n * a.lddw + k;
+        if (a.vector && k + 4 <= a.k) {
+            if (a.accumulate) {
+                const uint2 old = *reinterpret_cast<const uint2*>(p);
+                float e, f;
+                unpack2<__nv_bfloat16>(old.x, e, f);
+                v[0] += e;
+                v[1] += f;
+                unpack2<__nv_bfloat16>(old.y, e, f);
+                v[2] += e;
+                v[3] += f;
+            }
+            *reinterpret_cast<uint2*>(p) = make_uint2(pack2<__nv_bfloat16>(v[0], v[1]),
+                                                      pack2<__nv_bfloat16>(v[2], v[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k + i < a.k)
+                    p[i] = __float2bfloat16_rn(a.accumulate ? __bfloat162float(p[i]) + v[i] : v[i]);
+        }
+    }
+}
+
 template <bool COPY>
 __global__ void __cluster_dims__(2, 1, 1)
-__launch_bounds__(32 * (kWgDecoders + 2 + (COPY ? 0 : kWgLoaders)), 1)
+__launch_bounds__(32 * (kWgLoadWarp + (COPY ? 0 : kWgLoaders)), 1)
 wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ uint8_t raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const uint32_t tiles = smem_u32(base);
     uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgStages * kWgStageBytes);
-    const uint32_t empty = smem_u32(bars);                       // [stages] operands consumed
-    const uint32_t copied = empty + 8 * kWgStages;               // [stages] dY tile arrived
-    const uint32_t ready = copied + 8 * kWgStages;               // [stages] both blocks' operands
-    const uint32_t done = ready + 8 * kWgStages;                 // the tile's product
-    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 3 * kWgStages + 1);
+    const uint32_t empty = smem_u32(bars);             // [stages] operands consumed
+    const uint32_t copied = empty + 8 * kWgStages;     // [stages] the block's dY tile arrived
+    const uint32_t ready = copied + 8 * kWgStages;     // [stages] of the first block: the others' share
+    const uint32_t full = ready + 8 * kWgStages;       // [2] a tile's product is complete
+    const uint32_t drained = full + 16;                // [2] of the first block: TMEM read out
+    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 3 * kWgStages + 4);
     volatile uint32_t* gave_up = words + 1;
     float* affine = reinterpret_cast<float*>(base + kWgStages * kWgStageBytes + 256);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
-    const uint64_t n0 = (uint64_t)(blockIdx.x >> 1) * kWgTile + rank * kWgHalf;   // of A and D rows
-    const uint64_t k0 = (uint64_t)blockIdx.y * kWgTile;
-    const uint64_t all = (a.rows + kWgStep - 1) / kWgStep;
-    const int first = (int)(all * blockIdx.z / a.splits);
-    const int steps = (int)(all * (blockIdx.z + 1) / a.splits) - first;
-    const uint64_t t0 = (uint64_t)first * kWgStep;
+    const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1;
 
-    if (warp == kWgDecoders + 1) tmem_alloc_pair(smem_u32(words), kWgTile);
+    if (warp == kWgMmaWarp) tmem_alloc_pair(smem_u32(words), 2 * kWgTile);
     if (threadIdx.x == 0) {
         words[1] = 0;
         for (int s = 0; s < kWgStages; ++s) {
             mbar_init(empty + 8 * s, 1);
             mbar_init(copied + 8 * s, 1);
-            mbar_init(ready + 8 * s, 2 * (kWgDecoders + (COPY ? 0 : kWgLoaders)));
+            mbar_init(ready + 8 * s, 2 * kWgGroupWarps + (COPY ? 1 : 2 * kWgLoaders));
         }
-        mbar_init(done, 1);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(full + 8 * b, 1);
+            mbar_init(drained + 8 * b, 2 * kWgWriters);
+        }
         mbar_init_fence();
     }
     tc_fence_before();
@@ -156,215 +259,190 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     tc_fence_after();
     const uint32_t tmem = words[0];
 
-    if (warp < kWgDecoders) {
-        // ---- decode: the thread's token and its sixteen values of each panel.  Four lanes cover
-        // half a line and eight lanes two lines, whose swizzles differ: no bank is hit twice.
-        const uint32_t token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
-        const uint64_t k = k0 + rank * kWgHalf + 16 * quarter;
-        WgCodes r[kWgAhead];
+    if (warp >= kWgDecodeWarp && warp < kWgLoadWarp) {
+        // ---- decode.  Eight lanes read the 128 codes of a token, a whole line of memory.  Four of
+        // them write the even chunks of a line of the first panel while the other four write the
+        // odd chunks of the same line of the second, so no bank is hit twice.
+        const uint32_t group = (warp - kWgDecodeWarp) / kWgGroupWarps;
+        const uint32_t i0 = (threadIdx.x - 32 * kWgDecodeWarp) & (32 * kWgGroupWarps - 1);
+        const uint32_t token = i0 >> 3, eighth = i0 & 7;
+        const uint64_t column = rank * kWgHalf + 16 * eighth;
+        const bool odd = eighth >= 4;
+        const uint32_t place = kWgOperand + (odd ? kWgPanel : 0u) + token * 128;
+        const uint32_t chunk = (2 * (eighth & 3) + odd) ^ (token & 7);
+        WgWalk walk;
+        walk.begin(a, pair);
+        walk.advance(a, pair, group);
+        WgRing ring = {group, 1};
+        WgCodes r;
+        if (walk.more()) wg_load_codes(a, walk.token() + token, walk.unit.k0 + column, r);
+        while (walk.more()) {
+            walk.advance(a, pair, kWgGroups);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
+                break;
+            const uint32_t line = tiles + ring.stage * kWgStageBytes + place;
 #pragma unroll
-        for (int u = 0; u < kWgAhead; ++u)
-            if (u < steps) wg_load_codes(a, t0 + u * kWgStep + token, k, r[u]);
-        uint32_t stage = 0, parity = 1;
-        bool ok = true;
-        for (int s0 = 0; s0 < steps && ok; s0 += kWgAhead) {
-#pragma unroll
-            for (int u = 0; u < kWgAhead; ++u) {
-                const int s = s0 + u;
-                if (s < steps && ok) {
-                    ok = mbar_wait(empty + 8 * stage, parity, gave_up);
-                    const uint32_t line =
-                        tiles + stage * kWgStageBytes + kWgOperand + token * 128;
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-                        wg_decode(r[u].c[p], r[u].scale[p], line + p * kWgPanel, 2 * quarter,
-                                  token & 7);
-                    if (s + kWgAhead < steps)
-                        wg_load_codes(a, t0 + (uint64_t)(s + kWgAhead) * kWgStep + token, k, r[u]);
-                    fence_async_proxy();
-                    __syncwarp();
-                    if (lane == 0) {
-                        // the pair's first block hears of the dY tile through the decoders
-                        if (COPY && ok) ok = mbar_wait(copied + 8 * stage, parity ^ 1, gave_up);
-                        mbar_arrive_at(ready + 8 * stage, 0);
-                    }
-                    ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-                    if (++stage == kWgStages) {
-                        stage = 0;
-                        parity ^= 1;
-                    }
+            for (int i = 0; i < 4; ++i) {
+                const uint4 c = r.c[i];
+                const uint32_t w[4] = {odd ? c.z : c.x, odd ? c.w : c.y, odd ? c.x : c.z,
+                                       odd ? c.y : c.w};
+                const uint32_t at = line + i * (16 * 128);
+                wg_decode(w, r.scale[i], at + (chunk << 4), at + ((chunk ^ 1) << 4));
+            }
+            if (walk.more()) wg_load_codes(a, walk.token() + token, walk.unit.k0 + column, r);
+            fence_async_proxy();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(ready + 8 * ring.stage, 0);
+            ring.advance(kWgGroups);
+        }
+    } else if (warp < kWgWriters) {
+        // ---- write a tile out: lane = row
+        uint32_t u = 0;
+        for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) {
+            const uint64_t n = w.n0 + rank * kWgHalf + 32 * warp + lane, k0 = w.k0;
+            const bool part = w.tile >= a.whole && a.splits > 1;
+            float add = 0.0f;
+            if (!part) {
+                asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgWriters) : "memory");
+                for (int i = threadIdx.x; i < kWgTile; i += 32 * kWgWriters) {
+                    const bool in = k0 + i < a.k;
+                    affine[i] = a.gamma && in ? wg_param(a.gamma, a.param_dtype, k0 + i) : 1.0f;
+                    affine[kWgTile + i] =
+                        a.beta && in ? wg_param(a.beta, a.param_dtype, k0 + i) : 0.0f;
                 }
+                asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgWriters) : "memory");
+                if (a.beta && n < a.n) add = a.db[n];
             }
-        }
-        // ---- epilogue: lane = row of D, a warp takes half of the columns
-        for (int i = threadIdx.x; i < kWgTile; i += 32 * kWgDecoders) {
-            const bool in = k0 + i < a.k;
-            affine[i] = a.gamma && in ? wg_param(a.gamma, a.param_dtype, k0 + i) : 1.0f;
-            affine[kWgTile + i] = a.beta && in ? wg_param(a.beta, a.param_dtype, k0 + i) : 0.0f;
-        }
-        asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgDecoders) : "memory");
-        ok = mbar_wait(done, 0, gave_up) && ok && !*gave_up;
-        tc_fence_after();
-        const uint64_t n = n0 + 32 * (warp & 3) + lane;
-        const int half = (warp >> 2) * kWgHalf;
-        const uint64_t padded_n = (uint64_t)(gridDim.x >> 1) * kWgTile;
-        const uint64_t padded_k = (uint64_t)gridDim.y * kWgTile;
-        const float add = a.splits == 1 && a.beta && n < a.n ? a.db[n] : 0.0f;
+            bool ok = mbar_wait(full + 8 * (u & 1), (u >> 1) & 1, gave_up);
+            ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
+            tc_fence_after();
+            const uint32_t from = tmem + (u & 1) * kWgTile + ((uint32_t)(32 * warp) << 16);
+            float* parts = a.parts + (((uint64_t)(w.tile - a.whole) * a.splits + w.part) * kWgTile +
+                                      rank * kWgHalf + 32 * warp + lane) * kWgTile;
 #pragma unroll 1
-        for (int c = 0; c < kWgHalf; c += 32) {
-            float v[32];
-            tmem_load32(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + half + c, v);
-            if (!ok) {               // a wait ran out: the result must not pass for one
+            for (int c = 0; c < kWgTile; c += 32) {
+                float v[32];
+                tmem_load32(from + c, v);
+                if (!ok) {           // a wait ran out: the result must not pass for one
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
-            }
-            const uint64_t k = k0 + half + c;
-            if (a.splits > 1) {
-                float4* p = reinterpret_cast<float4*>(
-                    a.parts + (blockIdx.z * padded_n + n) * padded_k + k);
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
+                }
+                if (part) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                continue;
-            }
-            if (n >= a.n || k >= a.k) continue;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                v[i] = fmaf(v[i], affine[half + c + i], add * affine[kWgTile + half + c + i]);
-            if (a.dw_f32) {
-                float* p = static_cast<float*>(a.dw) + n * a.lddw + k;
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<float4*>(parts + c + i) =
+                            make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    continue;
+                }
+                if (n >= a.n || k0 + c >= a.k) continue;
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
-                    if (a.vector && k + i + 4 <= a.k) {
-                        float4 o = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                        if (a.accumulate) {
-                            const float4 old = *reinterpret_cast<const float4*>(p + i);
-                            o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
-                        }
-                        *reinterpret_cast<float4*>(p + i) = o;
-                    } else {
+                    float o[4];
 #pragma unroll
-                        for (int j = i; j < i + 4; ++j)
-                            if (k + j < a.k) p[j] = a.accumulate ? p[j] + v[j] : v[j];
-                    }
-                }
-            } else {
-                __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + n * a.lddw + k;
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    if (a.vector && k + i + 8 <= a.k) {
-                        uint4* q = reinterpret_cast<uint4*>(p + i);
-                        uint32_t o[4];
-                        if (a.accumulate) {
-                            const uint4 old = *q;
-                            const uint32_t w[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                float e, f;
-                                unpack2<__nv_bfloat16>(w[j], e, f);
-                                v[i + 2 * j] += e;
-                                v[i + 2 * j + 1] += f;
-                            }
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            o[j] = pack2<__nv_bfloat16>(v[i + 2 * j], v[i + 2 * j + 1]);
-                        *q = make_uint4(o[0], o[1], o[2], o[3]);
-                    } else {
-#pragma unroll
-                        for (int j = i; j < i + 8; ++j)
-                            if (k + j < a.k)
-                                p[j] = __float2bfloat16_rn(
-                                    a.accumulate ? __bfloat162float(p[j]) + v[j] : v[j]);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        o[j] = fmaf(v[i + j], affine[c + i + j],
+                                    add * affine[kWgTile + c + i + j]);
+                    wg_store4(a, n, k0 + c + i, o);
                 }
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(drained + 8 * (u & 1), 0);
         }
-        tc_fence_before();
-    } else if (warp == kWgDecoders) {
+    } else if (warp == kWgCopyWarp) {
         // ---- copies of the dY tile: two panels of 64 n
         if (COPY && lane == 0) {
-            uint32_t stage = 0, parity = 1;
-            int s = 0;
-            for (; s < steps; ++s) {
-                if (!mbar_wait(empty + 8 * stage, parity, gave_up)) break;
-                const uint32_t dst = tiles + stage * kWgStageBytes;
-                mbar_expect(copied + 8 * stage, kWgOperand);
+            WgRing ring = {0, 1};
+            WgWalk walk;
+            uint32_t issued = 0;
+            for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1)) {
+                if (!mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)) break;
+                const uint32_t dst = tiles + ring.stage * kWgStageBytes;
+                mbar_expect(copied + 8 * ring.stage, kWgOperand);
                 for (int p = 0; p < 2; ++p)
-                    tma_load_2d(dst + p * kWgPanel, &map, (int)(n0 + 64 * p),
-                                (int)(t0 + (uint64_t)s * kWgStep), copied + 8 * stage);
-                if (++stage == kWgStages) {
-                    stage = 0;
-                    parity ^= 1;
-                }
+                    tma_load_2d(dst + p * kWgPanel, &map,
+                                (int)(walk.unit.n0 + rank * kWgHalf + 64 * p), (int)walk.token(),
+                                copied + 8 * ring.stage);
+                ring.advance(1);
+                ++issued;
             }
-            // given up: the copies in flight still land before the block may end
-            if (s < steps) {
-                const long long begin = clock64();
-                for (int back = 1; back <= kWgStages && back <= s; ++back) {
-                    const int i = s - back;
-                    while (!mbar_try(copied + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
-                           clock64() - begin < 4000000000ll) {}
-                }
-            }
+            // the copies in flight land before the block may end
+            const long long begin = clock64();
+            for (uint32_t i = issued < kWgStages ? 0 : issued - kWgStages; i < issued; ++i)
+                while (!mbar_try(copied + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
+                       clock64() - begin < 4000000000ll) {}
         }
-    } else if (warp == kWgDecoders + 1) {
-        // ---- matrix instructions
-        if (rank == 0 && lane == 0) {
-            uint32_t stage = 0, parity = 0;
+    } else if (warp == kWgMmaWarp) {
+        if (lane == 0 && rank == 0) {
+            // ---- matrix instructions
             const uint32_t shape = mma_shape(kWgTile, kWgTile);
-            for (int s = 0; s < steps; ++s) {
-                if (!mbar_wait(ready + 8 * stage, parity, gave_up)) break;
+            WgRing ring = {0, 0};
+            bool ok = true;
+            uint32_t u = 0;
+            for (WgUnit w = wg_unit(a, pair, 0); w.steps && ok; w = wg_unit(a, pair, ++u)) {
+                const uint32_t to = tmem + (u & 1) * kWgTile;
+                ok = mbar_wait(drained + 8 * (u & 1), ((u >> 1) & 1) ^ 1, gave_up);
                 tc_fence_after();
-                const uint32_t at = tiles + stage * kWgStageBytes;
+                for (uint32_t s = 0; s < w.steps && ok; ++s) {
+                    ok = (!COPY || mbar_wait(copied + 8 * ring.stage, ring.parity, gave_up)) &&
+                         mbar_wait(ready + 8 * ring.stage, ring.parity, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = tiles + ring.stage * kWgStageBytes;
 #pragma unroll
-                for (int i = 0; i < kWgStep / 16; ++i)      // 16 tokens are two groups of lines
-                    mma_pair(tmem, mma_operand(at + 2048 * i, kWgPanel),
-                             mma_operand(at + kWgOperand + 2048 * i, kWgPanel), shape,
-                             s > 0 || i > 0);
-                mma_commit_pair(empty + 8 * stage);
-                if (++stage == kWgStages) {
-                    stage = 0;
-                    parity ^= 1;
+                    for (int i = 0; i < kWgStep / 16; ++i)      // 16 tokens: two groups of lines
+                        mma_pair(to, mma_operand(at + 2048 * i, kWgPanel),
+                                 mma_operand(at + kWgOperand + 2048 * i, kWgPanel), shape,
+                                 s > 0 || i > 0);
+                    mma_commit_pair(empty + 8 * ring.stage);
+                    ring.advance(1);
                 }
+                mma_commit_pair(full + 8 * (u & 1));
             }
-            mma_commit_pair(done);
+        } else if (COPY && lane == 0) {
+            // ---- the other block: pass on that its dY tile has arrived
+            WgRing ring = {0, 0};
+            WgWalk walk;
+            for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1)) {
+                if (!mbar_wait(copied + 8 * ring.stage, ring.parity, gave_up)) break;
+                mbar_arrive_at(ready + 8 * ring.stage, 0);
+                ring.advance(1);
+            }
         }
     } else if (!COPY) {
         // ---- plain loads of the dY tile, a step ahead: 16 lanes cover the 128 n of a token
-        const int i0 = threadIdx.x - 32 * (kWgDecoders + 2);
-        const uint32_t chunk = i0 & 15, token0 = i0 >> 4;          // tokens token0 + 16 j
-        const uint64_t n = n0 + 8 * chunk;
-        uint4 v[4];
+        const int i0 = threadIdx.x - 32 * kWgLoadWarp;
+        const uint32_t chunk = i0 & 15, token0 = i0 >> 4;          // tokens token0 + 8 j
+        WgWalk walk;
+        walk.begin(a, pair);
+        WgRing ring = {0, 1};
+        uint4 v[8];
+        if (walk.more()) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = wg_load_dy8(a, t0 + token0 + 16 * j, n);
-        uint32_t stage = 0, parity = 1;
-        for (int s = 0; s < steps; ++s) {
-            bool ok = mbar_wait(empty + 8 * stage, parity, gave_up);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            const uint32_t dst = tiles + stage * kWgStageBytes + (chunk >> 3) * kWgPanel;
+            for (int j = 0; j < 8; ++j)
+                v[j] = wg_load_dy8(a, walk.token() + token0 + 8 * j,
+                                   walk.unit.n0 + rank * kWgHalf + 8 * chunk);
+        }
+        while (walk.more()) {
+            walk.advance(a, pair, 1);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
+                break;
+            const uint32_t dst = tiles + ring.stage * kWgStageBytes + (chunk >> 3) * kWgPanel;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t token = token0 + 16 * j;
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t token = token0 + 8 * j;
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
                                  dst + token * 128 + (((chunk & 7) ^ (token & 7)) << 4)),
                              "r"(v[j].x), "r"(v[j].y), "r"(v[j].z), "r"(v[j].w)
                              : "memory");
-            }
-            if (s + 1 < steps) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    v[j] = wg_load_dy8(a, t0 + (uint64_t)(s + 1) * kWgStep + token0 + 16 * j, n);
+                if (walk.more())
+                    v[j] = wg_load_dy8(a, walk.token() + token,
+                                       walk.unit.n0 + rank * kWgHalf + 8 * chunk);
             }
             fence_async_proxy();
             __syncwarp();
-            if (lane == 0) mbar_arrive_at(ready + 8 * stage, 0);
-            if (++stage == kWgStages) {
-                stage = 0;
-                parity ^= 1;
-            }
+            if (lane == 0) mbar_arrive_at(ready + 8 * ring.stage, 0);
+            ring.advance(1);
         }
     }
     // the pair stays until both blocks are done with each other's barriers and with TMEM
@@ -372,59 +450,82 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     tc_fence_before();
     cluster_sync();
     tc_fence_after();
-    if (warp == kWgDecoders + 1) tmem_free_pair(tmem, kWgTile);
+    if (warp == kWgMmaWarp) tmem_free_pair(tmem, 2 * kWgTile);
 }
 
-// dw <- [dw +] gamma * (sum of the parts, in order) + beta * db; no parts: the sum over no tokens
-__global__ void __launch_bounds__(256)
-wg_join_kernel(const __grid_constant__ WgArgs a, const uint64_t padded_n, const uint64_t padded_k) {
-    const uint64_t k = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (k >= a.k) return;
-    for (uint64_t n = blockIdx.y; n < a.n; n += gridDim.y) {
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int z = 0; z < a.splits; ++z) {
-            const float4 p = __ldcs(
-                reinterpret_cast<const float4*>(a.parts + (z * padded_n + n) * padded_k + k));
-            s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
-        }
-        float v[4] = {s.x, s.y, s.z, s.w};
-        const float add = a.beta ? a.db[n] : 0.0f;
+// the tiles that were computed in parts: dw <- [dw +] gamma * (sum of the parts, in order) +
+// beta * db; no parts: the sum over no tokens.  A block takes 4 rows of a tile.
+__global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a) {
+    const uint32_t tile = a.whole + blockIdx.x / 64, row = blockIdx.x % 64 * 4 + (threadIdx.x >> 6);
+    const uint32_t column = (threadIdx.x & 63) * 4;
+    const uint64_t n = (uint64_t)(tile % a.tiles_n) * kWgTile + row;
+    const uint64_t k = (uint64_t)(tile / a.tiles_n) * kWgTile + column;
+    if (n >= a.n || k >= a.k) return;
+    const float* p = a.parts + ((uint64_t)(tile - a.whole) * a.splits * kWgTile + row) * kWgTile + column;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (uint32_t z = 0; z < a.splits; ++z) {
+        const float4 q =
+            __ldcs(reinterpret_cast<const float4*>(p + (uint64_t)z * kWgTile * kWgTile));
+        v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+    }
+    const float add = a.beta ? a.db[n] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (k + i >= a.k) break;
+    for (int i = 0; i < 4; ++i)
+        if (k + i < a.k) {
             if (a.gamma) v[i] *= wg_param(a.gamma, a.param_dtype, k + i);
             if (a.beta) v[i] = fmaf(add, wg_param(a.beta, a.param_dtype, k + i), v[i]);
-            if (a.dw_f32) {
-                float* p = static_cast<float*>(a.dw) + n * a.lddw + k + i;
-                *p = a.accumulate ? *p + v[i] : v[i];
-            } else {
-                __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + n * a.lddw + k + i;
-                *p = __float2bfloat16_rn(a.accumulate ? __bfloat162float(*p) + v[i] : v[i]);
-            }
         }
-    }
+    wg_store4(a, n, k, v);
 }
 
-// ---- column sums of dY: parts of kWgSumRows rows, then their sum ----------------------------------
-constexpr int kWgSumBlocks = 256;
+// ---- column sums of dY: a block adds up a range of rows, a thread eight columns, or one where the
+// rows are not on 16-byte boundaries
+constexpr int kWgSumBlocks = 256;        // ranges at most
 
+template <bool VECTOR>
 __global__ void __launch_bounds__(256)
 wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
                const uint64_t lddy, float* __restrict__ parts) {
-    __shared__ float sums[8][33];
+    constexpr int W = VECTOR ? 8 : 1;
+    __shared__ float sums[8][32 * W + 1];
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
-    const uint64_t col = (uint64_t)blockIdx.x * 32 + lane;
+    const uint64_t col = ((uint64_t)blockIdx.x * 32 + lane) * W;
     const uint64_t begin = rows * blockIdx.y / gridDim.y, end = rows * (blockIdx.y + 1) / gridDim.y;
-    float s = 0.0f;
-    if (col < n)
-        for (uint64_t t = begin + group; t < end; t += 8) s += __bfloat162float(dy[t * lddy + col]);
-    sums[group][lane] = s;
-    __syncthreads();
-    if (group == 0 && col < n) {
-        s = sums[0][lane];
+    float s[W];
 #pragma unroll
-        for (int g = 1; g < 8; ++g) s += sums[g][lane];
-        parts[blockIdx.y * n + col] = s;
+    for (int i = 0; i < W; ++i) s[i] = 0.0f;
+    if (col < n) {
+        const __nv_bfloat16* p = dy + col;
+        if constexpr (VECTOR) {
+#pragma unroll 8
+            for (uint64_t t = begin + group; t < end; t += 8) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + t * lddy));
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float e, f;
+                    unpack2<__nv_bfloat16>(w[i], e, f);
+                    s[2 * i] += e;
+                    s[2 * i + 1] += f;
+                }
+            }
+        } else {
+#pragma unroll 8
+            for (uint64_t t = begin + group; t < end; t += 8)
+                s[0] += __bfloat162float(__ldg(p + t * lddy));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) sums[group][lane * W + i] = s[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * W; c += 256) {
+        const uint64_t at = (uint64_t)blockIdx.x * 32 * W + c;
+        if (at >= n) continue;
+        float v = sums[0][c];
+#pragma unroll
+        for (int g = 1; g < 8; ++g) v += sums[g][c];
+        parts[blockIdx.y * n + at] = v;
     }
 }
 
@@ -441,25 +542,28 @@ wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uin
 }
 
 struct WgPlan {
-    uint64_t tiles_n, tiles_k;
-    int splits, sum_blocks;
+    uint64_t tiles_n, tiles, whole;
+    uint32_t splits;
+    int sum_blocks;
     size_t sum_offset, fresh_offset, bytes;
 };
 
 static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k) {
     WgPlan p = {};
     p.tiles_n = (n + kWgTile - 1) / kWgTile;
-    p.tiles_k = (k + kWgTile - 1) / kWgTile;
-    const uint64_t tiles = p.tiles_n * p.tiles_k, steps = (rows + kWgStep - 1) / kWgStep;
-    uint64_t splits = tiles ? kWgPairs / tiles : 1;
+    p.tiles = p.tiles_n * ((k + kWgTile - 1) / kWgTile);
+    const uint64_t steps = (rows + kWgStep - 1) / kWgStep, left = p.tiles % kWgPairs;
+    uint64_t splits = left ? kWgPairs / left : 1;
     if (splits > steps / kWgMinSteps) splits = steps / kWgMinSteps;
-    p.splits = (int)(splits < 1 ? 1 : splits);
-    const uint64_t sum_tiles = (n + 31) / 32;
-    uint64_t blocks = sum_tiles ? 8 * 148 / sum_tiles : 1;
+    p.whole = p.tiles - left;
+    p.splits = splits < 1 ? 1 : (uint32_t)splits;
+    // eight blocks for every SM in the column sums
+    const uint64_t across = (n + 255) / 256;
+    uint64_t blocks = across ? 8 * 148 / across : 1;
     if (blocks > (rows + 63) / 64) blocks = (rows + 63) / 64;
     if (blocks > kWgSumBlocks) blocks = kWgSumBlocks;
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
-    p.sum_offset = p.splits > 1 ? p.splits * tiles * kWgTile * kWgTile * 4 : 0;
+    p.sum_offset = p.splits > 1 ? left * p.splits * kWgTile * kWgTile * 4 : 0;
     p.fresh_offset = p.sum_offset + round_up16(p.sum_blocks * n * 4);
     p.bytes = p.fresh_offset + round_up16(n * 4);
     return p;
@@ -488,8 +592,8 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     if (k && (!dw || lddw < k)) return NC_ERR_INVALID;
     if (rows && (!dy || lddy < n || !workspace || (k && (!codes || !scales))))
         return NC_ERR_INVALID;
-    if (rows >= ((size_t)1 << 31) || n >= ((size_t)1 << 31) || k >= ((size_t)1 << 23) ||
-        !act8_fits(rows, k))
+    if (rows >= ((size_t)1 << 31) || n >= ((size_t)1 << 31) || k >= ((size_t)1 << 31) ||
+        !act8_fits(rows, k) || ((n + 255) / 256) * ((k + 255) / 256) >= ((size_t)1 << 24))
         return NC_ERR_TOO_LARGE;
     const int wbytes = dw_dtype == NC_DTYPE_F32 ? 4 : 2;
     if (!element_aligned(dy, 2) || !element_aligned(gamma, pbytes) ||
@@ -504,8 +608,11 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     const bool with_beta = beta && k && rows;
     if (db || with_beta) {
         float* sums = reinterpret_cast<float*>(ws + p.sum_offset);
+        const bool vector = n % 8 == 0 && row_access(dy, lddy, 2, rows) != kRowElement;
+        auto kernel = vector ? wg_sums_kernel<true> : wg_sums_kernel<false>;
         if (rows)
-            wg_sums_kernel<<<dim3((unsigned)((n + 31) / 32), p.sum_blocks), 256, 0, stream>>>(
+            kernel<<<dim3((unsigned)((n + (vector ? 255 : 31)) / (vector ? 256 : 32)),
+                          p.sum_blocks), 256, 0, stream>>>(
                 static_cast<const __nv_bfloat16*>(dy), rows, n, lddy, sums);
         wg_sums_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(
             sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
@@ -517,8 +624,12 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     a.rows = rows; a.n = n; a.lddy = lddy; a.codes = codes; a.scales = scales; a.k = k;
     a.pitch = act8_pitch(k); a.gamma = gamma; a.beta = with_beta ? beta : nullptr;
     a.param_dtype = param_dtype; a.dw = dw; a.dw_f32 = dw_dtype == NC_DTYPE_F32; a.lddw = lddw;
-    a.db = fresh; a.accumulate = accumulate; a.splits = rows ? p.splits : 0;
+    a.db = fresh; a.accumulate = accumulate;
     a.vector = row_access(dw, lddw, wbytes, n) != kRowElement;
+    a.tiles_n = (uint32_t)p.tiles_n;
+    a.tiles = (uint32_t)p.tiles;
+    a.whole = rows ? (uint32_t)p.whole : 0;
+    a.splits = rows ? p.splits : 0;
     a.parts = reinterpret_cast<float*>(ws);
     if (rows) {
         const bool copy = row_access(dy, lddy, 2, rows) != kRowElement;
@@ -530,15 +641,12 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmem) !=
             cudaSuccess)
             return NC_ERR_CUDA;
-        const dim3 grid((unsigned)(2 * p.tiles_n), (unsigned)p.tiles_k, (unsigned)p.splits);
-        kernel<<<grid, 32 * (kWgDecoders + 2 + (copy ? 0 : kWgLoaders)), kWgSmem, stream>>>(a, map);
+        const uint64_t pairs = p.whole ? kWgPairs : (p.tiles - p.whole) * p.splits;
+        kernel<<<(unsigned)(2 * pairs), 32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders)), kWgSmem,
+                 stream>>>(a, map);
     }
-    if (a.splits != 1) {
-        const unsigned across = (unsigned)((k + 1023) / 1024);
-        const unsigned down = (unsigned)(n < 4096 ? n : 4096);
-        wg_join_kernel<<<dim3(across, down), 256, 0, stream>>>(a, p.tiles_n * kWgTile,
-                                                               p.tiles_k * kWgTile);
-    }
+    if (a.splits != 1 && a.whole < a.tiles)
+        wg_join_kernel<<<(a.tiles - a.whole) * 64, 256, 0, stream>>>(a);
     return launch_status();
 }
 

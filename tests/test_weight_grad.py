@@ -67,7 +67,8 @@ def test_refusals_need_no_gpu():
     assert _status(lambda: f(ws_bytes=16)) == "NC_ERR_WORKSPACE"
     assert _status(lambda: f(t=1 << 31)) == "NC_ERR_TOO_LARGE"
     assert _status(lambda: f(n=1 << 31, lddy=1 << 31)) == "NC_ERR_TOO_LARGE"
-    assert _status(lambda: f(k=1 << 23, lddw=1 << 23)) == "NC_ERR_TOO_LARGE"
+    assert _status(lambda: f(k=1 << 31, lddw=1 << 31)) == "NC_ERR_TOO_LARGE"
+    assert _status(lambda: f(n=1 << 21, lddy=1 << 21, k=1 << 21, lddw=1 << 21)) == "NC_ERR_TOO_LARGE"
     f(n=0)
     del keep
 
