@@ -375,8 +375,14 @@ def _ptrs(ts: Sequence):
     return (_vp * len(ts))(*[_ptr(t) for t in ts])
 
 
+# the current stream's handle without the torch.cuda.Stream object around it (3 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream

@@ -20,16 +20,16 @@
 
 namespace natcomp {
 
-constexpr int kLnWarps = 4;             // rows of a forward block where a warp owns a row
 constexpr int kLnMaxCols = 32768;
 constexpr int kLnBackThreads = 512;     // most threads of a backward block; a cluster of 2 or 4
                                         // blocks shares a row of more than 16 * 512 columns
 constexpr int kLnMaxParts = 592;        // blocks that write partial parameter gradients
 
 struct LnParams {
-    const void *gamma, *beta;
+    const void *gamma, *beta;           // where absent, the address of some other input
     int dtype;
     bool vector;                        // both may be read 16 bytes at a time
+    bool has_gamma, has_beta;
 };
 
 // ---- a thread's values of a row ------------------------------------------------------------
@@ -96,9 +96,10 @@ __device__ __forceinline__ float ln_param(const void* p, int dtype, uint32_t col
 
 // sixteen parameters in float; absent ones are `none`
 template <bool ELEMENT>
-__device__ __forceinline__ void ln_params(const void* p, int dtype, bool vector, int c, int G,
-                                          int tid, uint32_t cols, float none, float (&v)[16]) {
-    if (!p) {
+__device__ __forceinline__ void ln_params(const void* p, bool has, int dtype, bool vector, int c,
+                                          int G, int tid, uint32_t cols, float none,
+                                          float (&v)[16]) {
+    if (!has) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = none;
         return;
@@ -127,128 +128,171 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// sum over the threads of a row; `part` holds a slot for every warp and is not reused without a
-// barrier in between
-template <bool BLOCK>
-__device__ __forceinline__ float row_sum(float v, float* part) {
-    v = warp_sum(v);
-    if (BLOCK) {
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-        __syncthreads();
-        const int warps = blockDim.x >> 5;
-        v = 0.0f;
-        for (int w = 0; w < warps; ++w) v += part[w];
-    }
-    return v;
+// the threads of group `group` of a block, G of them
+__device__ __forceinline__ void group_sync(int group, int G) {
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(G) : "memory");
 }
 
 // ---- forward -------------------------------------------------------------------------------
 
 enum LnKeep { kKeepNone = 0, kKeepNearest = 1, kKeepRandom = 2 };
 
-template <typename T, int C, bool BLOCK, bool ELEMENT, int KEEP>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 32 * kLnWarps)
+// A block holds blockDim / G groups of G threads; a group takes a row at a time and reads a row
+// ahead.  Every warp sums up its own values and their squared distances from its own mean; one
+// barrier later the group's mean and variance follow from these (the squared distances about the
+// common mean are the warps' own plus n_w (mean_w - mean)^2).
+template <typename T, int C, int THREADS, bool ELEMENT, int KEEP>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 ln_forward_kernel(const T* __restrict__ x, const uint64_t rows, const uint32_t cols,
                   const uint64_t ldx, const LnParams params, const float eps, T* __restrict__ y,
                   const uint64_t ldy, const bool wide, float* __restrict__ mean_out,
                   float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
-                  uint8_t* __restrict__ scales, const uint32_t worker,
+                  uint8_t* __restrict__ scales, const uint32_t worker, const int G,
                   const __grid_constant__ PhiloxKeys keys) {
-    __shared__ float part[2][32];
-    const int G = BLOCK ? blockDim.x : 32;
-    const int tid = BLOCK ? threadIdx.x : threadIdx.x & 31;
-    const int lane = threadIdx.x & 31;
-    const uint64_t row = BLOCK ? blockIdx.x
-                               : (uint64_t)blockIdx.x * kLnWarps + (threadIdx.x >> 5);
-    if (row >= rows) return;            // whole warps; BLOCK launches one block per row
+    __shared__ float2 part[2][32];       // sum and squared distances of a warp, two rows in turn
+    __shared__ float count[32];          // values of a warp
+    const int groups = blockDim.x / G, group = threadIdx.x / G, tid = threadIdx.x - group * G;
+    const int warps = G >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    const float inverse_cols = 1.0f / (float)cols;
 
-    float v[C][16];
-    float sum = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        Raw16<T> r;
-        ln_load<T, ELEMENT>(x + row * ldx, c, G, tid, cols, wide, r);
-        unpack16<T>(r, v[c]);
-    }
+    int mine = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += v[c][i];
-    const float mean = row_sum<BLOCK>(sum, part[0]) / (float)cols;
-    float square = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[c][i] -= mean;
-            if (ln_col<ELEMENT>(c, i, G, tid) < cols) square = fmaf(v[c][i], v[c][i], square);
-        }
-    const float rstd = 1.0f / sqrtf(row_sum<BLOCK>(square, part[1]) / (float)cols + eps);
-    if (tid == 0) {
-        if (mean_out) mean_out[row] = mean;
-        if (rstd_out) rstd_out[row] = rstd;
-    }
+        for (int i = 0; i < 16; ++i) mine += ln_col<ELEMENT>(c, i, G, tid) < cols;
+    const bool whole = mine == 16 * C;
+    const float n_warp = warp_sum((float)mine), inverse_n = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
+    if (lane == 0) count[warp] = n_warp;
+    __syncthreads();
 
-    const uint32_t pitch = (cols + 31) & ~31u;
-    const uint64_t plane = row * pitch;              // the row's first code
+    uint64_t row = (uint64_t)blockIdx.x * groups + group;
+    Raw16<T> next[C];
+    if (row < rows) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+        for (int c = 0; c < C; ++c) ln_load<T, ELEMENT>(x + row * ldx, c, G, tid, cols, wide, next[c]);
+    }
+    for (int turn = 0; row < rows; row += step, turn ^= 1) {
+        float v[C][16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            v[c][i] = ln_col<ELEMENT>(c, i, G, tid) < cols ? v[c][i] * rstd : 0.0f;
-        if (KEEP != kKeepNone && !ELEMENT) {
-            uint32_t top = max_bits16(v[c]);
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            const uint32_t scale = act8_scale(top);
-            const uint32_t col = ln_col<false>(c, 0, G, tid);
-            if (col < pitch) {
-                const uint64_t q = (plane + col) >> 4;
-                __stcs(reinterpret_cast<uint4*>(codes) + q,
-                       act8_sixteen<KEEP == kKeepRandom>(v[c], scale, q, worker, keys));
-                if (!(tid & 1)) scales[q >> 1] = (uint8_t)scale;
-            }
+        for (int c = 0; c < C; ++c) unpack16<T>(next[c], v[c]);
+        if (row + step < rows) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                ln_load<T, ELEMENT>(x + (row + step) * ldx, c, G, tid, cols, wide, next[c]);
         }
-        if (KEEP != kKeepNone && ELEMENT) {
-            // step i of the warp is the block of 32 columns that starts at ln_col of lane 0
-            uint32_t r[4] = {0u, 0u, 0u, 0u};
-            if (KEEP == kKeepRandom) {
-                const uint32_t col = ln_col<true>(c, lane >> 1, G, tid - lane) + 16 * (lane & 1);
-                stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
-            }
+        float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t first = ln_col<true>(c, i, G, tid - lane);
-                const uint32_t top =
-                    __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[c][i]) & 0x7FFFFFFFu);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += v[c][i];
+        sum = warp_sum(sum);
+        float mean = sum * inverse_n, square = 0.0f;
+        if (whole) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float d = v[c][i] - mean;
+                    square = fmaf(d, d, square);
+                }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float d = v[c][i] - mean;
+                    if (ln_col<ELEMENT>(c, i, G, tid) < cols) square = fmaf(d, d, square);
+                }
+        }
+        square = warp_sum(square);
+        if (warps > 1) {
+            // a slot is written again only after the barrier of the row in between, which its
+            // readers have passed
+            if (lane == 0) part[turn][warp] = make_float2(sum, square);
+            group_sync(group, G);
+            const bool has = lane < warps;
+            const float2 p = has ? part[turn][group * warps + lane] : make_float2(0.0f, 0.0f);
+            const float n = has ? count[group * warps + lane] : 0.0f;
+            mean = warp_sum(p.x) * inverse_cols;
+            const float d = n > 0.0f ? p.x / n - mean : 0.0f;
+            square = warp_sum(fmaf(n * d, d, p.y));
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(square, inverse_cols, eps));
+        if (tid == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+
+        const uint32_t pitch = (cols + 31) & ~31u;
+        const uint64_t plane = row * pitch;              // the row's first code
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[c][i] = (v[c][i] - mean) * rstd;
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (ln_col<ELEMENT>(c, i, G, tid) >= cols) v[c][i] = 0.0f;
+            }
+            if (KEEP != kKeepNone && !ELEMENT) {
+                uint32_t top = max_bits16(v[c]);
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 const uint32_t scale = act8_scale(top);
-                uint32_t draw = 0;
-                if (KEEP == kKeepRandom) {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t t =
-                            __shfl_sync(0xFFFFFFFFu, r[k], 2 * i + (lane >> 4));
-                        if (((lane >> 2) & 3) == k) word = t;
-                    }
-                    draw = (word >> (8 * (lane & 3))) & 0xFFu;
-                }
-                if (first < pitch) {
-                    codes[plane + first + lane] = (uint8_t)(
-                        scale == kAct8Nan
-                            ? 0u
-                            : act8_one(v[c][i], act8_inverse(scale, KEEP == kKeepRandom),
-                                       KEEP == kKeepRandom, draw));
-                    if (lane == 0) scales[(plane + first) >> 5] = (uint8_t)scale;
+                const uint32_t col = ln_col<false>(c, 0, G, tid);
+                if (col < pitch) {
+                    const uint64_t q = (plane + col) >> 4;
+                    __stcs(reinterpret_cast<uint4*>(codes) + q,
+                           act8_sixteen<KEEP == kKeepRandom>(v[c], scale, q, worker, keys));
+                    if (!(tid & 1)) scales[q >> 1] = (uint8_t)scale;
                 }
             }
-        }
-        float gamma[16], beta[16];
-        ln_params<ELEMENT>(params.gamma, params.dtype, params.vector, c, G, tid, cols, 1.0f,
-                           gamma);
-        ln_params<ELEMENT>(params.beta, params.dtype, params.vector, c, G, tid, cols, 0.0f, beta);
+            if (KEEP != kKeepNone && ELEMENT) {
+                // step i of the warp is the block of 32 columns that starts at ln_col of lane 0
+                uint32_t r[4] = {0u, 0u, 0u, 0u};
+                if (KEEP == kKeepRandom) {
+                    const uint32_t col =
+                        ln_col<true>(c, lane >> 1, G, tid - lane) + 16 * (lane & 1);
+                    stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
+                }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[c][i] = fmaf(v[c][i], gamma[i], beta[i]);
-        ln_store<T, ELEMENT>(y + row * ldy, c, G, tid, cols, wide, v[c]);
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t first = ln_col<true>(c, i, G, tid - lane);
+                    const uint32_t top =
+                        __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[c][i]) & 0x7FFFFFFFu);
+                    const uint32_t scale = act8_scale(top);
+                    uint32_t draw = 0;
+                    if (KEEP == kKeepRandom) {
+                        uint32_t word = 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t t =
+                                __shfl_sync(0xFFFFFFFFu, r[k], 2 * i + (lane >> 4));
+                            if (((lane >> 2) & 3) == k) word = t;
+                        }
+                        draw = (word >> (8 * (lane & 3))) & 0xFFu;
+                    }
+                    if (first < pitch) {
+                        codes[plane + first + lane] = (uint8_t)(
+                            scale == kAct8Nan
+                                ? 0u
+                                : act8_one(v[c][i], act8_inverse(scale, KEEP == kKeepRandom),
+                                           KEEP == kKeepRandom, draw));
+                        if (lane == 0) scales[(plane + first) >> 5] = (uint8_t)scale;
+                    }
+                }
+            }
+            float p[16];
+            ln_params<ELEMENT>(params.gamma, params.has_gamma, params.dtype, params.vector, c, G,
+                               tid, cols, 1.0f, p);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[c][i] *= p[i];
+            ln_params<ELEMENT>(params.beta, params.has_beta, params.dtype, params.vector, c, G, tid,
+                               cols, 0.0f, p);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[c][i] += p[i];
+            ln_store<T, ELEMENT>(y + row * ldy, c, G, tid, cols, wide, v[c]);
+        }
     }
 }
 
@@ -269,39 +313,40 @@ struct LnForward {
     uint32_t worker;
 };
 
-template <typename T, int C, bool BLOCK, bool ELEMENT, int KEEP>
-static void ln_forward_go(const LnForward& a, unsigned grid, unsigned threads,
-                          cudaStream_t stream) {
-    ln_forward_kernel<T, C, BLOCK, ELEMENT, KEEP><<<grid, threads, 0, stream>>>(
-        static_cast<const T*>(a.x), a.rows, a.cols, a.ldx, a.params, a.eps, static_cast<T*>(a.y),
-        a.ldy, a.access == kRowWide, a.mean, a.rstd, a.codes, a.scales, a.worker,
-        make_philox_keys(a.seed));
+template <typename T, int C, int THREADS, bool ELEMENT, int KEEP>
+static void ln_forward_go(const LnForward& a, int G, cudaStream_t stream) {
+    const int groups = G < THREADS ? THREADS / G : 1;
+    const uint64_t want = (a.rows + groups - 1) / groups;
+    const uint64_t fit = (uint64_t)device_sm_count() * (1024 / (G * groups));
+    ln_forward_kernel<T, C, THREADS, ELEMENT, KEEP>
+        <<<(unsigned)(want < fit ? want : fit), G * groups, 0, stream>>>(
+            static_cast<const T*>(a.x), a.rows, a.cols, a.ldx, a.params, a.eps,
+            static_cast<T*>(a.y), a.ldy, a.access == kRowWide, a.mean, a.rstd, a.codes, a.scales,
+            a.worker, G, make_philox_keys(a.seed));
 }
 
-template <typename T, int C, bool BLOCK>
-static void ln_forward_rows(const LnForward& a, unsigned grid, unsigned threads,
-                            cudaStream_t stream) {
+template <typename T, int C, int THREADS>
+static void ln_forward_rows(const LnForward& a, int G, cudaStream_t stream) {
     const bool element = a.access == kRowElement;
     auto go = a.keep == kKeepNone
-                  ? (element ? ln_forward_go<T, C, BLOCK, true, kKeepNone>
-                             : ln_forward_go<T, C, BLOCK, false, kKeepNone>)
+                  ? (element ? ln_forward_go<T, C, THREADS, true, kKeepNone>
+                             : ln_forward_go<T, C, THREADS, false, kKeepNone>)
               : a.keep == kKeepNearest
-                  ? (element ? ln_forward_go<T, C, BLOCK, true, kKeepNearest>
-                             : ln_forward_go<T, C, BLOCK, false, kKeepNearest>)
-                  : (element ? ln_forward_go<T, C, BLOCK, true, kKeepRandom>
-                             : ln_forward_go<T, C, BLOCK, false, kKeepRandom>);
-    go(a, grid, threads, stream);
+                  ? (element ? ln_forward_go<T, C, THREADS, true, kKeepNearest>
+                             : ln_forward_go<T, C, THREADS, false, kKeepNearest>)
+                  : (element ? ln_forward_go<T, C, THREADS, true, kKeepRandom>
+                             : ln_forward_go<T, C, THREADS, false, kKeepRandom>);
+    go(a, G, stream);
 }
 
 template <typename T>
 static void ln_forward_launch(const LnForward& a, cudaStream_t stream) {
-    const unsigned warp_grid = (unsigned)((a.rows + kLnWarps - 1) / kLnWarps);
-    if (a.cols <= 512)
-        ln_forward_rows<T, 1, false>(a, warp_grid, 32 * kLnWarps, stream);
+    if (a.cols <= 4096)
+        ln_forward_rows<T, 1, 256>(a, (int)((a.cols + 511) / 512 * 32), stream);
     else if (a.cols <= 16384)
-        ln_forward_rows<T, 1, true>(a, (unsigned)a.rows, (a.cols + 511) / 512 * 32, stream);
+        ln_forward_rows<T, 1, 1024>(a, (int)((a.cols + 511) / 512 * 32), stream);
     else
-        ln_forward_rows<T, 2, true>(a, (unsigned)a.rows, (a.cols + 1023) / 1024 * 32, stream);
+        ln_forward_rows<T, 2, 1024>(a, (int)((a.cols + 1023) / 1024 * 32), stream);
 }
 
 // ---- backward ------------------------------------------------------------------------------
@@ -383,7 +428,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int G) {
     {
         const int bytes = a.params.dtype == NC_DTYPE_F32 ? 4 : 2;
         const char* p = static_cast<const char*>(a.params.gamma);
-        ln_params<ELEMENT>(p ? p + (size_t)origin * bytes : nullptr, a.params.dtype,
+        ln_params<ELEMENT>(p + (size_t)origin * bytes, a.params.has_gamma, a.params.dtype,
                            a.params.vector, 0, G, tid, cols, 1.0f, gamma);
     }
 #pragma unroll
@@ -445,7 +490,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int G) {
                 cluster.sync();
             } else {
                 if (lane == 0) part[turn][warp] = make_float2(s1, s2);
-                asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(G) : "memory");
+                group_sync(group, G);
             }
             s1 = s2 = 0.0f;
             for (int k = 0; k < CLUSTER; ++k)
@@ -620,9 +665,10 @@ static nc_status ln_backward_call(LnBackward a, int dtype, size_t cols, int para
     a.parts_pitch = (uint32_t)act8_pitch(cols);
     if (a.rows && workspace_bytes < nc_layer_norm_workspace_bytes(a.rows, cols))
         return NC_ERR_WORKSPACE;
-    a.params.beta = nullptr;
     a.params.dtype = param_dtype;
     a.params.vector = aligned16(a.params.gamma);
+    a.params.has_gamma = a.params.gamma != nullptr;
+    if (!a.params.has_gamma) a.params.gamma = a.dy;
     int access = row_access(a.dy, a.lddy, bytes, a.rows);
     const int others[3] = {row_access(a.dx, a.lddx, bytes, a.rows),
                            a.dres ? row_access(a.dres, a.lddres, bytes, a.rows) : kRowWide,
@@ -665,9 +711,11 @@ nc_status nc_layer_norm_forward(const void* x, int dtype, size_t rows, size_t co
         !element_aligned(gamma, pbytes) || !element_aligned(beta, pbytes) || !aligned4(mean) ||
         !aligned4(rstd) || !aligned16(codes) || !aligned16(scales))
         return NC_ERR_ALIGN;
-    LnForward a = {x, rows, (uint32_t)cols, ldx, {gamma, beta, param_dtype, false}, eps, y, ldy,
-                   0, mean, rstd, codes, scales, kKeepNone, seed, worker};
-    a.params.vector = aligned16(gamma) && aligned16(beta);
+    const LnParams params = {gamma ? gamma : x, beta ? beta : x, param_dtype,
+                             aligned16(gamma) && aligned16(beta), gamma != nullptr,
+                             beta != nullptr};
+    LnForward a = {x, rows, (uint32_t)cols, ldx, params, eps, y, ldy, 0, mean, rstd, codes, scales,
+                   kKeepNone, seed, worker};
     const int ax = row_access(x, ldx, bytes, rows), ay = row_access(y, ldy, bytes, rows);
     a.access = ax > ay ? ax : ay;
     if (codes) a.keep = rounding == NC_ROUND_RANDOM ? kKeepRandom : kKeepNearest;
