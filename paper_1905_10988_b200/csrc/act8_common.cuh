@@ -171,6 +171,153 @@ __device__ __forceinline__ void st_part16(T* p, const float (&v)[16], int count)
         if (i < count) p[i] = from_f32<T>(v[i]);
 }
 
+// ---- pairs of binary32 values: one instruction for two additions, products or both --------------
+typedef unsigned long long f32x2;
+
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void of_pair(f32x2 v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack16(const Raw16<T>& r, f32x2 (&v)[8]) {
+    float f[16];
+    unpack16<T>(r, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
+}
+
+// ---- a thread's sixteen values of a row, two assignments --------------------------------------
+// G threads share a row, 16 values each.  Value i of thread `tid` is column
+//   16 * tid + i                                rows on 16-byte boundaries: vector accesses
+//   SPREAD, 4-byte types: i * G + tid           any rows: neighbouring lanes, neighbouring values
+//   SPREAD, 2-byte types: 2 * ((i / 2) * G + tid) + i % 2     the same by pairs of values, so that
+//                                               a row on a 4-byte boundary moves a pair at a time
+template <typename T, bool SPREAD>
+__device__ __forceinline__ uint32_t row_col(int i, int G, int tid) {
+    if (!SPREAD) return 16u * tid + i;
+    if (sizeof(T) == 4) return (uint32_t)i * G + tid;
+    return 2u * ((uint32_t)(i >> 1) * G + tid) + (i & 1);
+}
+
+// values from `cols` on read as 0
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int tid, uint32_t cols,
+                                         bool wide, Raw16<T>& r) {
+    if constexpr (!SPREAD) {
+        const uint32_t col = 16u * tid;
+        if (col + 16 <= cols)
+            r = ld_raw16<T>(row + col, wide);
+        else
+            r = ld_raw16_part<T>(row + col, col < cols ? (int)(cols - col) : 0);
+    } else if constexpr (sizeof(T) == 4) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(row);
+        if (row_col<T, true>(15, G, tid) < cols) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                r.b[i >> 3].v[i & 7] = __ldg(p + row_col<T, true>(i, G, tid));
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t col = row_col<T, true>(i, G, tid);
+            r.b[i >> 3].v[i & 7] = col < cols ? __ldg(p + col) : 0u;
+        }
+    } else {
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(row);
+        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;     // the same for all lanes
+        if (row_col<T, true>(15, G, tid) < cols) {
+            if (!odd) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    r.b[0].v[i] = __ldg(
+                        reinterpret_cast<const uint32_t*>(p + row_col<T, true>(2 * i, G, tid)));
+            } else {
+                // two words hold a pair's halves; the row's first and last value have no
+                // neighbour to share a word with
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t col = row_col<T, true>(2 * i, G, tid);
+                    const uint32_t* q = reinterpret_cast<const uint32_t*>(p + col - 1);
+                    const uint32_t lo = i > 0 || tid > 0 ? __ldg(q) : (uint32_t)__ldg(p) << 16;
+                    const uint32_t hi =
+                        i < 7 || col + 2 < cols ? __ldg(q + 1) : (uint32_t)__ldg(p + col + 1);
+                    r.b[0].v[i] = __funnelshift_r(lo, hi, 16);
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            uint32_t w = 0;
+            if (col < cols) w = __ldg(p + col);
+            if (col + 1 < cols) w |= (uint32_t)__ldg(p + col + 1) << 16;
+            r.b[0].v[i] = w;
+        }
+    }
+}
+
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void row_store(T* __restrict__ row, int G, int tid, uint32_t cols,
+                                          bool wide, const float (&v)[16]) {
+    if constexpr (!SPREAD) {
+        const uint32_t col = 16u * tid;
+        if (col + 16 <= cols)
+            st_raw16<T>(row + col, pack16<T>(v), wide);
+        else if (col < cols)
+            st_part16<T>(row + col, v, (int)(cols - col));
+    } else if constexpr (sizeof(T) == 4) {
+        if (row_col<T, true>(15, G, tid) < cols) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) row[row_col<T, true>(i, G, tid)] = v[i];
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t col = row_col<T, true>(i, G, tid);
+            if (col < cols) row[col] = v[i];
+        }
+    } else {
+        unsigned short* p = reinterpret_cast<unsigned short*>(row);
+        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;
+        const bool whole = row_col<T, true>(15, G, tid) < cols;
+        if (whole && !odd) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<uint32_t*>(p + row_col<T, true>(2 * i, G, tid)) =
+                    pack2<T>(v[2 * i], v[2 * i + 1]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            const uint32_t w = pack2<T>(v[2 * i], v[2 * i + 1]);
+            if (whole || col < cols) p[col] = (unsigned short)w;
+            if (whole || col + 1 < cols) p[col + 1] = (unsigned short)(w >> 16);
+        }
+    }
+}
+
 // ---- encoder ---------------------------------------------------------------------------------
 
 // scale byte of a block from the largest |x| bit pattern.  The patterns order as the magnitudes
@@ -216,11 +363,18 @@ __device__ __forceinline__ uint32_t act8_four(const float* x, float inverse, uin
     return (m & 0x7F7F7F7Fu) | (s & 0x80808080u);
 }
 
+// the largest magnitude of three, NaN if one of them is
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
+
 __device__ __forceinline__ uint32_t max_bits16(const float (&v)[16]) {
-    uint32_t a = 0;
+    float a = max3_abs(v[0], v[1], v[2]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a = max(a, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return a;
+    for (int i = 3; i < 15; i += 2) a = max3_abs(a, v[i], v[i + 1]);
+    return __float_as_uint(max3_abs(a, v[15], v[15]));
 }
 
 // codes of sixteen neighbouring values, one half of the block whose scale byte is `scale`;
@@ -235,6 +389,66 @@ __device__ __forceinline__ uint4 act8_sixteen(const float (&v)[16], uint32_t sca
     return make_uint4(act8_four<RANDOM>(v, inverse, r[0]), act8_four<RANDOM>(v + 4, inverse, r[1]),
                       act8_four<RANDOM>(v + 8, inverse, r[2]),
                       act8_four<RANDOM>(v + 12, inverse, r[3]));
+}
+
+// Codes of a thread's spread values (row_col<T, true>).  `plane`: place of the row's first code,
+// `first` = tid - lane, `pitch`: codes of the row.  A step of the warp covers one block (4-byte
+// types) or two, of 16 lanes each.  The warp's 32 generator blocks of 16 draws are computed one
+// a lane.
+template <typename T, bool RANDOM>
+__device__ __forceinline__ void act8_encode_spread(const float (&v)[16], uint64_t plane,
+                                                   uint32_t pitch, int G, int first,
+                                                   uint32_t worker, const PhiloxKeys& keys,
+                                                   uint8_t* __restrict__ codes,
+                                                   uint8_t* __restrict__ scales) {
+    constexpr int PER = sizeof(T) == 4 ? 1 : 2;      // values of a lane in a step
+    const int lane = threadIdx.x & 31;
+    uint32_t r[4] = {0u, 0u, 0u, 0u};
+    if (RANDOM) {
+        const int step = lane / (2 * PER), part = lane % (2 * PER);
+        const uint32_t col = row_col<T, true>(step * PER, G, first) + 16 * part;
+        stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
+    }
+#pragma unroll
+    for (int s = 0; s < 16 / PER; ++s) {
+        const uint32_t begin = row_col<T, true>(s * PER, G, first);
+        uint32_t top;
+        if (PER == 1) {
+            top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[s]) & 0x7FFFFFFFu);
+        } else {
+            const float m = max3_abs(v[PER * s], v[PER * s + PER - 1], 0.0f);
+            top = __float_as_uint(m);
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        }
+        const uint32_t scale = act8_scale(top);
+        uint32_t word = 0;
+        if (RANDOM) {          // the lane's draws: bytes of word (column / 4) mod 4 of its chunk
+            const int source = s * 2 * PER + lane * PER / 16, which = (lane * PER >> 2) & 3;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t t = __shfl_sync(0xFFFFFFFFu, r[k], source);
+                if (which == k) word = t;
+            }
+            word >>= 8 * (lane * PER & 3);
+        }
+        const uint32_t col = begin + lane * PER;
+        if (col < pitch) {
+            const float inverse = act8_inverse(scale, RANDOM);
+            uint32_t code = 0;
+            if (scale != kAct8Nan) {
+                code = act8_one(v[PER * s], inverse, RANDOM, word & 0xFFu);
+                if (PER == 2)
+                    code |= act8_one(v[PER * s + PER - 1], inverse, RANDOM, (word >> 8) & 0xFFu)
+                            << 8;
+            }
+            if (PER == 1)
+                codes[plane + col] = (uint8_t)code;
+            else
+                *reinterpret_cast<unsigned short*>(codes + plane + col) = (unsigned short)code;
+            if ((col & 31) == 0) scales[(plane + col) >> 5] = (uint8_t)scale;
+        }
+    }
 }
 
 // ---- decoder ---------------------------------------------------------------------------------
@@ -275,6 +489,42 @@ __device__ __forceinline__ void act8_decode16(const uint4& c, uint32_t scale, fl
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = act8_value(w[i >> 2] >> (8 * (i & 3)) & 0xFFu, scale);
+    }
+}
+
+// a thread's spread values of a row of codes; those from `cols` on are 0
+template <typename T>
+__device__ __forceinline__ void act8_decode_spread(const uint8_t* __restrict__ codes,
+                                                   const uint8_t* __restrict__ scales,
+                                                   uint64_t plane, int G, int tid, uint32_t cols,
+                                                   float (&v)[16]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t col = row_col<T, true>(i, G, tid);
+            v[i] = col < cols ? act8_value(__ldg(codes + plane + col),
+                                           __ldg(scales + ((plane + col) >> 5)))
+                              : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            v[2 * i] = v[2 * i + 1] = 0.0f;
+            if (col < cols) {
+                const uint32_t c =
+                    __ldg(reinterpret_cast<const unsigned short*>(codes + plane + col));
+                const uint32_t scale = __ldg(scales + ((plane + col) >> 5));
+                if (scale <= kAct8MaxFast) {
+                    unpack2<__nv_bfloat16>(act8_pair_bf16(c, 0, act8_fields(scale)), v[2 * i],
+                                           v[2 * i + 1]);
+                } else {
+                    v[2 * i] = act8_value(c & 0xFFu, scale);
+                    v[2 * i + 1] = act8_value(c >> 8, scale);
+                }
+                if (col + 1 >= cols) v[2 * i + 1] = 0.0f;
+            }
+        }
     }
 }
 

@@ -3,8 +3,8 @@
 // Bound by memory: 2 + 33/32 bytes per bfloat16 value in either direction.  A thread takes 16
 // neighbouring values, half a block: two lanes agree on the block's largest magnitude with one
 // shuffle, a 16-byte store takes the codes, and one generator block serves the 16 draws of random
-// rounding.  Rows that are not 16-byte aligned are read one element per lane, 32 neighbours (one
-// block) per step, the largest magnitude by one warp-wide reduction.
+// rounding.  Rows that are not 16-byte aligned are spread over the lanes, an element or a pair of
+// two-byte elements per access.
 #include "act8_common.cuh"
 
 namespace natcomp {
@@ -43,50 +43,26 @@ act8_compress_kernel(const T* __restrict__ x, const Act8Rows g, const uint32_t w
     if (!(i & 1)) scales[i >> 1] = (uint8_t)scale;
 }
 
-// rows at any element: a warp takes 512 neighbouring values of a row, 32 a step
+// rows at any element: a warp takes 512 neighbouring values of a row
 template <typename T, bool RANDOM>
 __global__ void __launch_bounds__(kBlockThreads)
-act8_compress_element_kernel(const T* __restrict__ x, const Act8Rows g, const uint32_t worker,
-                             uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                             const __grid_constant__ PhiloxKeys keys) {
+act8_compress_spread_kernel(const T* __restrict__ x, const Act8Rows g, const uint32_t worker,
+                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                            const __grid_constant__ PhiloxKeys keys) {
     const int lane = threadIdx.x & 31;
     const uint32_t segments = (g.per_row + 31) / 32;
-    const uint64_t w = (uint64_t)blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
-    const uint64_t row = w / segments;
+    const uint32_t w = blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
+    const uint32_t row = w / segments;
     if (row >= g.rows) return;
-    const uint32_t first = (uint32_t)(w - row * segments) * 32;       // chunk within the row
-    const T* p = x + row * g.ld;
-    const uint64_t chunk = row * g.per_row + first;
-    uint32_t r[4] = {0u, 0u, 0u, 0u};
-    if (RANDOM) stream_words4(chunk + lane, worker, kDomainAct8, keys, r);
+    const uint64_t first = 512ull * (w - row * segments);
+    Raw16<T> r;
     float v[16];
-#pragma unroll
-    for (int s = 0; s < 16; ++s) {
-        const uint64_t col = 16ull * first + 32 * s + lane;
-        v[s] = col < g.cols ? to_f32<T>(p[col]) : 0.0f;
-    }
-#pragma unroll
-    for (int s = 0; s < 16; ++s) {
-        if (first + 2 * s >= g.per_row) break;
-        const uint32_t top =
-            __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[s]) & 0x7FFFFFFFu);
-        const uint32_t scale = act8_scale(top);
-        uint32_t draw = 0;
-        if (RANDOM) {          // chunk 2s + lane / 16 holds this lane's byte, in its word lane / 4
-            uint32_t word = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t t = __shfl_sync(0xFFFFFFFFu, r[k], 2 * s + (lane >> 4));
-                if (((lane >> 2) & 3) == k) word = t;
-            }
-            draw = (word >> (8 * (lane & 3))) & 0xFFu;
-        }
-        const uint32_t code =
-            scale == kAct8Nan ? 0u : act8_one(v[s], act8_inverse(scale, RANDOM), RANDOM, draw);
-        const uint64_t at = 16 * chunk + 32 * s;
-        codes[at + lane] = (uint8_t)code;
-        if (lane == 0) scales[at >> 5] = (uint8_t)scale;
-    }
+    row_load<T, true>(x + row * g.ld + first, 32, lane,
+                      g.cols > first ? (uint32_t)min(g.cols - first, (uint64_t)512) : 0u, false, r);
+    unpack16<T>(r, v);
+    act8_encode_spread<T, RANDOM>(v, 16ull * row * g.per_row + first,
+                                  (uint32_t)min(16ull * g.per_row - first, 512ull), 32, 0, worker,
+                                  keys, codes, scales);
 }
 
 template <typename T>
@@ -109,23 +85,19 @@ act8_decompress_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restr
 
 template <typename T>
 __global__ void __launch_bounds__(kBlockThreads)
-act8_decompress_element_kernel(const uint8_t* __restrict__ codes,
-                               const uint8_t* __restrict__ scales, const Act8Rows g,
-                               T* __restrict__ out) {
+act8_decompress_spread_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                              const Act8Rows g, T* __restrict__ out) {
     const int lane = threadIdx.x & 31;
     const uint32_t segments = (g.per_row + 31) / 32;
-    const uint64_t w = (uint64_t)blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
-    const uint64_t row = w / segments;
+    const uint32_t w = blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
+    const uint32_t row = w / segments;
     if (row >= g.rows) return;
-    const uint32_t first = (uint32_t)(w - row * segments) * 32;
-    const uint64_t at = 16 * (row * g.per_row + first);
-#pragma unroll
-    for (int s = 0; s < 16; ++s) {
-        const uint64_t col = 16ull * first + 32 * s + lane;
-        if (col < g.cols)
-            out[row * g.ld + col] = from_f32<T>(
-                act8_value(__ldg(codes + at + 32 * s + lane), __ldg(scales + (at >> 5) + s)));
-    }
+    const uint64_t first = 512ull * (w - row * segments);
+    if (first >= g.cols) return;
+    const uint32_t cols = (uint32_t)min(g.cols - first, (uint64_t)512);
+    float v[16];
+    act8_decode_spread<T>(codes, scales, 16ull * row * g.per_row + first, 32, lane, cols, v);
+    row_store<T, true>(out + row * g.ld + first, 32, lane, cols, false, v);
 }
 
 // the plane of a matrix: one long row where the matrix has no gaps and whole blocks
@@ -157,8 +129,8 @@ static void act8_compress_launch(const void* x, const Act8Rows& g, bool random, 
                                  cudaStream_t stream) {
     const PhiloxKeys keys = make_philox_keys(seed);
     auto kernel = g.access == kRowElement
-                      ? (random ? act8_compress_element_kernel<T, true>
-                                : act8_compress_element_kernel<T, false>)
+                      ? (random ? act8_compress_spread_kernel<T, true>
+                                : act8_compress_spread_kernel<T, false>)
                       : (random ? act8_compress_kernel<T, true> : act8_compress_kernel<T, false>);
     kernel<<<act8_grid(g), kBlockThreads, 0, stream>>>(static_cast<const T*>(x), g, worker, codes,
                                                        scales, keys);
@@ -167,7 +139,7 @@ static void act8_compress_launch(const void* x, const Act8Rows& g, bool random, 
 template <typename T>
 static void act8_decompress_launch(const uint8_t* codes, const uint8_t* scales, const Act8Rows& g,
                                    void* out, cudaStream_t stream) {
-    auto kernel = g.access == kRowElement ? act8_decompress_element_kernel<T>
+    auto kernel = g.access == kRowElement ? act8_decompress_spread_kernel<T>
                                           : act8_decompress_kernel<T>;
     kernel<<<act8_grid(g), kBlockThreads, 0, stream>>>(codes, scales, g, static_cast<T*>(out));
 }

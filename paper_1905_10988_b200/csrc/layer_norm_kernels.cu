@@ -10,82 +10,21 @@
 // backward kernel is persistent: a thread keeps the sums of its own columns over all its rows in
 // registers and reads a row ahead, the blocks' sums go to the workspace once, and a second kernel
 // adds them in a fixed order, so no atomics decide the order of any sum.
-//
-// Two assignments of a row's values to threads, one code: rows that start on multiples of 16
-// bytes give a thread 16 neighbouring values at a time; other rows give neighbouring values to
-// neighbouring lanes, one element per access.
-#include <cooperative_groups.h>
-
 #include "act8_common.cuh"
+#include "tensor_core.cuh"
 
 namespace natcomp {
 
 constexpr int kLnMaxCols = 32768;
-constexpr int kLnBackThreads = 512;     // most threads of a backward block; a cluster of 2 or 4
-                                        // blocks shares a row of more than 16 * 512 columns
+constexpr int kLnThreads = 256;         // most threads of a row in one block; a cluster of 2, 4 or 8
+                                        // blocks shares a row of more than 16 * 256 columns
 constexpr int kLnMaxParts = 592;        // blocks that write partial parameter gradients
 
 struct LnParams {
     const void *gamma, *beta;           // where absent, the address of some other input
     int dtype;
-    bool vector;                        // both may be read 16 bytes at a time
     bool has_gamma, has_beta;
 };
-
-// ---- a thread's values of a row ------------------------------------------------------------
-// value (c, i) of thread `tid` of G: column 16 * (c * G + tid) + i, or, ELEMENT,
-// (16 * c + i) * G + tid
-template <bool ELEMENT>
-__device__ __forceinline__ uint32_t ln_col(int c, int i, int G, int tid) {
-    return ELEMENT ? (uint32_t)(16 * c + i) * G + tid : 16u * (c * G + tid) + i;
-}
-
-template <typename T, bool ELEMENT>
-__device__ __forceinline__ void ln_load(const T* __restrict__ row, int c, int G, int tid,
-                                        uint32_t cols, bool wide, Raw16<T>& r) {
-    if (ELEMENT) {
-#pragma unroll
-        for (int b = 0; b < (int)sizeof(T) / 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r.b[b].v[i] = 0u;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = ln_col<true>(c, i, G, tid);
-            if (col < cols) {
-                if constexpr (sizeof(T) == 4)
-                    r.b[i >> 3].v[i & 7] = __ldg(reinterpret_cast<const uint32_t*>(row) + col);
-                else
-                    r.b[0].v[i >> 1] |=
-                        (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row) + col)
-                        << (16 * (i & 1));
-            }
-        }
-        return;
-    }
-    const uint32_t col = ln_col<false>(c, 0, G, tid);
-    if (col + 16 <= cols)
-        r = ld_raw16<T>(row + col, wide);
-    else
-        r = ld_raw16_part<T>(row + col, col < cols ? (int)(cols - col) : 0);
-}
-
-template <typename T, bool ELEMENT>
-__device__ __forceinline__ void ln_store(T* __restrict__ row, int c, int G, int tid, uint32_t cols,
-                                         bool wide, const float (&v)[16]) {
-    if (ELEMENT) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = ln_col<true>(c, i, G, tid);
-            if (col < cols) row[col] = from_f32<T>(v[i]);
-        }
-        return;
-    }
-    const uint32_t col = ln_col<false>(c, 0, G, tid);
-    if (col + 16 <= cols)
-        st_raw16<T>(row + col, pack16<T>(v), wide);
-    else if (col < cols)
-        st_part16<T>(row + col, v, (int)(cols - col));
-}
 
 __device__ __forceinline__ float ln_param(const void* p, int dtype, uint32_t col) {
     if (dtype == NC_DTYPE_F32) return __ldg(static_cast<const float*>(p) + col);
@@ -94,32 +33,41 @@ __device__ __forceinline__ float ln_param(const void* p, int dtype, uint32_t col
     return __half2float(__ldg(static_cast<const __half*>(p) + col));
 }
 
-// sixteen parameters in float; absent ones are `none`
-template <bool ELEMENT>
-__device__ __forceinline__ void ln_params(const void* p, bool has, int dtype, bool vector, int c,
-                                          int G, int tid, uint32_t cols, float none,
-                                          float (&v)[16]) {
-    if (!has) {
+// A vector of parameters as the threads of a group read it: four values of thread `tid` at
+// table[q * G + tid], q = 0..3, in the order of the thread's columns.  Absent ones are `none`.
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void ln_table(float4* table, const void* p, bool has, int dtype, int G,
+                                         uint32_t origin, uint32_t cols, float none) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < 4 * G; i += blockDim.x) {
+        const int q = i / G, tid = i - q * G;
+        float f[4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = none;
-        return;
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t at = row_col<T, SPREAD>(4 * q + k, G, tid);
+            f[k] = none;
+            if (has && at < cols) f[k] = ln_param(p, dtype, origin + at);
+        }
+        table[i] = make_float4(f[0], f[1], f[2], f[3]);
     }
-    const uint32_t col = ln_col<false>(c, 0, G, tid);
-    if (!ELEMENT && vector && col + 16 <= cols) {
-        if (dtype == NC_DTYPE_F32)
-            unpack16<float>(ld_raw16<float>(static_cast<const float*>(p) + col, false), v);
-        else if (dtype == NC_DTYPE_BF16)
-            unpack16<__nv_bfloat16>(
-                ld_raw16<__nv_bfloat16>(static_cast<const __nv_bfloat16*>(p) + col, false), v);
-        else
-            unpack16<__half>(ld_raw16<__half>(static_cast<const __half*>(p) + col, false), v);
-        return;
-    }
+}
+
+__device__ __forceinline__ void ln_params(const float4* table, int G, int tid, f32x2 (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t at = ln_col<ELEMENT>(c, i, G, tid);
-        v[i] = at < cols ? ln_param(p, dtype, at) : 0.0f;
+    for (int q = 0; q < 4; ++q) {
+        const float4 f = table[q * G + tid];
+        v[2 * q] = pair_of(f.x, f.y);
+        v[2 * q + 1] = pair_of(f.z, f.w);
     }
+}
+
+// (The empty statement keeps this a branch: few threads need it.)
+template <typename T, bool SPREAD>
+__device__ __forceinline__ void clear_beyond(float (&v)[16], int G, int tid, uint32_t cols) {
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (row_col<T, SPREAD>(i, G, tid) >= cols) v[i] = 0.0f;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -128,173 +76,127 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// the threads of group `group` of a block, G of them
-__device__ __forceinline__ void group_sync(int group, int G) {
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(G) : "memory");
+__device__ __forceinline__ float sum_of(const f32x2 (&v)[8]) {
+    const f32x2 s = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])),
+                         add2(add2(v[4], v[5]), add2(v[6], v[7])));
+    float a, b;
+    of_pair(s, a, b);
+    return a + b;
 }
+
+// values of warp `w` of the row's block `rank`
+template <typename T, bool SPREAD>
+__device__ __forceinline__ uint32_t ln_warp_values(int rank, int w, int G, uint32_t all_cols) {
+    uint32_t n = 0;
+    const uint32_t origin = rank * 16 * G;
+    if (!SPREAD) {
+        const uint32_t first = origin + 512u * w;
+        n = all_cols > first ? min(all_cols - first, 512u) : 0u;
+    } else {
+        const uint32_t run = sizeof(T) == 4 ? 32u : 64u;       // neighbours that a step covers
+        for (uint32_t i = 0; i < 512u / run; ++i) {
+            const uint32_t first = origin + i * (run / 32u) * G + w * run;
+            n += all_cols > first ? min(all_cols - first, run) : 0u;
+        }
+    }
+    return n;
+}
+
+// Where a thread stands: a block holds blockDim / G groups of G threads, and a group owns a row at
+// a time.  CLUSTER > 1: one group a block, and the blocks of a cluster share a row, block r of it
+// owning the columns from r * 16 * G on.
+template <int CLUSTER>
+struct LnPlace {
+    int G, groups, group, tid, warps, warp, lane;
+    uint32_t rank, origin, cols;         // the block's first column and how many there are from it
+    uint64_t first, step;                // rows
+    __device__ __forceinline__ LnPlace(int g, uint32_t all_cols) {
+        G = g;
+        groups = blockDim.x / G;
+        group = threadIdx.x / G;
+        tid = threadIdx.x - group * G;
+        warps = G >> 5;
+        warp = tid >> 5;
+        lane = threadIdx.x & 31;
+        rank = CLUSTER > 1 ? blockIdx.x % CLUSTER : 0;
+        origin = rank * 16 * G;
+        cols = all_cols > origin ? all_cols - origin : 0;
+        step = (uint64_t)(gridDim.x / CLUSTER) * groups;
+        first = (uint64_t)(blockIdx.x / CLUSTER) * groups + group;
+    }
+};
+
+// Two numbers of every warp of a row for all of them.  A row has up to 8 warps, or up to 64 in a
+// cluster; slots without a warp stay 0.  Two rows use two sets in turn, so that a slot is written
+// again only after the readers of the row before have passed the row in between.
+//
+// One block: a barrier of the group's threads.  Cluster: asynchronous stores to all its blocks, of
+// which every block's own barrier counts the bytes; a cluster-wide barrier would wait for the loads
+// and stores of global memory in flight as well.
+template <int CLUSTER>
+struct LnExchange {
+    static constexpr int kSlots = CLUSTER > 1 ? 8 * CLUSTER : 8;      // of a row
+    float2* set[2];
+    uint32_t bars, bytes, parity;
+    // `slots`: [2][kSlots * groups], `words`: two barriers; all threads of the cluster call
+    __device__ __forceinline__ void begin(float2* slots, uint64_t* words,
+                                          const LnPlace<CLUSTER>& p) {
+        const int all = kSlots * p.groups;
+        for (int i = threadIdx.x; i < 2 * all; i += blockDim.x) slots[i] = make_float2(0.0f, 0.0f);
+        set[0] = slots + kSlots * p.group;
+        set[1] = set[0] + all;
+        bars = smem_u32(words);
+        bytes = 8 * CLUSTER * p.warps;
+        parity = 0;
+        if (CLUSTER > 1 && threadIdx.x == 0) {
+            mbar_init(bars, 1);
+            mbar_init(bars + 8, 1);
+            mbar_expect(bars, bytes);
+            mbar_expect(bars + 8, bytes);
+            mbar_init_fence();
+        }
+        __syncthreads();
+        if (CLUSTER > 1) cluster_sync();
+    }
+    // row number `turn` of the group (0, 1, 2, ...)
+    __device__ __forceinline__ const float2* send(float2 mine, uint32_t turn,
+                                                  const LnPlace<CLUSTER>& p) {
+        float2* slots = set[turn & 1];
+        if constexpr (CLUSTER > 1) {
+            const uint32_t bar = bars + 8 * (turn & 1);
+            if (p.lane < CLUSTER)
+                st_async_pair(smem_u32(&slots[p.rank * p.warps + p.warp]), bar, p.lane, mine);
+            const long long begin = clock64();
+            bool done = mbar_try(bar, (turn >> 1) & 1);
+            while (!done && clock64() - begin < 4000000000ll) done = mbar_try(bar, (turn >> 1) & 1);
+            if (!done) {             // given up: the row must not pass for a result
+                const float nan = __uint_as_float(0x7FC00000u);
+                slots[p.lane & (kSlots - 1)] = make_float2(nan, nan);
+            }
+            // armed for the row after next: nothing of it arrives before this block has sent
+            // its part of the next row
+            if (threadIdx.x == 0) mbar_expect(bar, bytes);
+        } else {
+            if (p.lane == 0) slots[p.warp] = mine;
+            asm volatile("bar.sync %0, %1;" ::"r"(p.group + 1), "r"(p.G) : "memory");
+        }
+        return slots;
+    }
+    // f(slot) summed over the row's slots, the same in every lane
+    template <typename F>
+    __device__ __forceinline__ float sum(const float2* slots, int lane, F f) const {
+        constexpr int kLanes = kSlots < 32 ? kSlots : 32;
+        float s = f(slots, lane & (kLanes - 1));
+        if (kSlots > 32) s += f(slots, lane + 32);
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        return s;
+    }
+};
 
 // ---- forward -------------------------------------------------------------------------------
 
 enum LnKeep { kKeepNone = 0, kKeepNearest = 1, kKeepRandom = 2 };
-
-// A block holds blockDim / G groups of G threads; a group takes a row at a time and reads a row
-// ahead.  Every warp sums up its own values and their squared distances from its own mean; one
-// barrier later the group's mean and variance follow from these (the squared distances about the
-// common mean are the warps' own plus n_w (mean_w - mean)^2).
-template <typename T, int C, int THREADS, bool ELEMENT, int KEEP>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
-ln_forward_kernel(const T* __restrict__ x, const uint64_t rows, const uint32_t cols,
-                  const uint64_t ldx, const LnParams params, const float eps, T* __restrict__ y,
-                  const uint64_t ldy, const bool wide, float* __restrict__ mean_out,
-                  float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
-                  uint8_t* __restrict__ scales, const uint32_t worker, const int G,
-                  const __grid_constant__ PhiloxKeys keys) {
-    __shared__ float2 part[2][32];       // sum and squared distances of a warp, two rows in turn
-    __shared__ float count[32];          // values of a warp
-    const int groups = blockDim.x / G, group = threadIdx.x / G, tid = threadIdx.x - group * G;
-    const int warps = G >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint64_t step = (uint64_t)gridDim.x * groups;
-    const float inverse_cols = 1.0f / (float)cols;
-
-    int mine = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mine += ln_col<ELEMENT>(c, i, G, tid) < cols;
-    const bool whole = mine == 16 * C;
-    const float n_warp = warp_sum((float)mine), inverse_n = n_warp > 0.0f ? 1.0f / n_warp : 0.0f;
-    if (lane == 0) count[warp] = n_warp;
-    __syncthreads();
-
-    uint64_t row = (uint64_t)blockIdx.x * groups + group;
-    Raw16<T> next[C];
-    if (row < rows) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) ln_load<T, ELEMENT>(x + row * ldx, c, G, tid, cols, wide, next[c]);
-    }
-    for (int turn = 0; row < rows; row += step, turn ^= 1) {
-        float v[C][16];
-#pragma unroll
-        for (int c = 0; c < C; ++c) unpack16<T>(next[c], v[c]);
-        if (row + step < rows) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                ln_load<T, ELEMENT>(x + (row + step) * ldx, c, G, tid, cols, wide, next[c]);
-        }
-        float sum = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum += v[c][i];
-        sum = warp_sum(sum);
-        float mean = sum * inverse_n, square = 0.0f;
-        if (whole) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float d = v[c][i] - mean;
-                    square = fmaf(d, d, square);
-                }
-        } else {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float d = v[c][i] - mean;
-                    if (ln_col<ELEMENT>(c, i, G, tid) < cols) square = fmaf(d, d, square);
-                }
-        }
-        square = warp_sum(square);
-        if (warps > 1) {
-            // a slot is written again only after the barrier of the row in between, which its
-            // readers have passed
-            if (lane == 0) part[turn][warp] = make_float2(sum, square);
-            group_sync(group, G);
-            const bool has = lane < warps;
-            const float2 p = has ? part[turn][group * warps + lane] : make_float2(0.0f, 0.0f);
-            const float n = has ? count[group * warps + lane] : 0.0f;
-            mean = warp_sum(p.x) * inverse_cols;
-            const float d = n > 0.0f ? p.x / n - mean : 0.0f;
-            square = warp_sum(fmaf(n * d, d, p.y));
-        }
-        const float rstd = 1.0f / sqrtf(fmaf(square, inverse_cols, eps));
-        if (tid == 0) {
-            if (mean_out) mean_out[row] = mean;
-            if (rstd_out) rstd_out[row] = rstd;
-        }
-
-        const uint32_t pitch = (cols + 31) & ~31u;
-        const uint64_t plane = row * pitch;              // the row's first code
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[c][i] = (v[c][i] - mean) * rstd;
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (ln_col<ELEMENT>(c, i, G, tid) >= cols) v[c][i] = 0.0f;
-            }
-            if (KEEP != kKeepNone && !ELEMENT) {
-                uint32_t top = max_bits16(v[c]);
-                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                const uint32_t scale = act8_scale(top);
-                const uint32_t col = ln_col<false>(c, 0, G, tid);
-                if (col < pitch) {
-                    const uint64_t q = (plane + col) >> 4;
-                    __stcs(reinterpret_cast<uint4*>(codes) + q,
-                           act8_sixteen<KEEP == kKeepRandom>(v[c], scale, q, worker, keys));
-                    if (!(tid & 1)) scales[q >> 1] = (uint8_t)scale;
-                }
-            }
-            if (KEEP != kKeepNone && ELEMENT) {
-                // step i of the warp is the block of 32 columns that starts at ln_col of lane 0
-                uint32_t r[4] = {0u, 0u, 0u, 0u};
-                if (KEEP == kKeepRandom) {
-                    const uint32_t col =
-                        ln_col<true>(c, lane >> 1, G, tid - lane) + 16 * (lane & 1);
-                    stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t first = ln_col<true>(c, i, G, tid - lane);
-                    const uint32_t top =
-                        __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[c][i]) & 0x7FFFFFFFu);
-                    const uint32_t scale = act8_scale(top);
-                    uint32_t draw = 0;
-                    if (KEEP == kKeepRandom) {
-                        uint32_t word = 0;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t t =
-                                __shfl_sync(0xFFFFFFFFu, r[k], 2 * i + (lane >> 4));
-                            if (((lane >> 2) & 3) == k) word = t;
-                        }
-                        draw = (word >> (8 * (lane & 3))) & 0xFFu;
-                    }
-                    if (first < pitch) {
-                        codes[plane + first + lane] = (uint8_t)(
-                            scale == kAct8Nan
-                                ? 0u
-                                : act8_one(v[c][i], act8_inverse(scale, KEEP == kKeepRandom),
-                                           KEEP == kKeepRandom, draw));
-                        if (lane == 0) scales[(plane + first) >> 5] = (uint8_t)scale;
-                    }
-                }
-            }
-            float p[16];
-            ln_params<ELEMENT>(params.gamma, params.has_gamma, params.dtype, params.vector, c, G,
-                               tid, cols, 1.0f, p);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[c][i] *= p[i];
-            ln_params<ELEMENT>(params.beta, params.has_beta, params.dtype, params.vector, c, G, tid,
-                               cols, 0.0f, p);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[c][i] += p[i];
-            ln_store<T, ELEMENT>(y + row * ldy, c, G, tid, cols, wide, v[c]);
-        }
-    }
-}
 
 struct LnForward {
     const void* x;
@@ -313,40 +215,186 @@ struct LnForward {
     uint32_t worker;
 };
 
-template <typename T, int C, int THREADS, bool ELEMENT, int KEEP>
-static void ln_forward_go(const LnForward& a, int G, cudaStream_t stream) {
-    const int groups = G < THREADS ? THREADS / G : 1;
-    const uint64_t want = (a.rows + groups - 1) / groups;
-    const uint64_t fit = (uint64_t)device_sm_count() * (1024 / (G * groups));
-    ln_forward_kernel<T, C, THREADS, ELEMENT, KEEP>
-        <<<(unsigned)(want < fit ? want : fit), G * groups, 0, stream>>>(
-            static_cast<const T*>(a.x), a.rows, a.cols, a.ldx, a.params, a.eps,
-            static_cast<T*>(a.y), a.ldy, a.access == kRowWide, a.mean, a.rstd, a.codes, a.scales,
-            a.worker, G, make_philox_keys(a.seed));
+// Every warp sums up its own values and their squared distances from its own mean; one exchange
+// later the row's mean and variance follow from these (the squared distances about the common
+// mean are the warps' own plus n_w (mean_w - mean)^2).  A row is read ahead.
+template <typename T, bool SPREAD, int KEEP, int CLUSTER>
+__global__ void __launch_bounds__(kLnThreads, 4)
+ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
+                  const __grid_constant__ PhiloxKeys keys) {
+    __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
+    __shared__ float2 counts[LnExchange<CLUSTER>::kSlots];
+    __shared__ uint64_t bars[2];
+    extern __shared__ float4 tables[];   // gamma, beta
+    const LnPlace<CLUSTER> p(threads, a.cols);
+    const int row_warps = CLUSTER * p.warps;
+    const float inverse_cols = 1.0f / (float)a.cols;
+    const bool wide = a.access == kRowWide;
+    const T* x = static_cast<const T*>(a.x) + p.origin;
+    T* y = static_cast<T*>(a.y) + p.origin;
+    const uint32_t pitch = (a.cols + 31) & ~31u;
+    const uint32_t own = pitch > p.origin ? pitch - p.origin : 0;    // codes of a row from here on
+
+    Raw16<T> next;
+    if (p.first < a.rows) row_load<T, SPREAD>(x + p.first * a.ldx, p.G, p.tid, p.cols, wide, next);
+    ln_table<T, SPREAD>(tables, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+                        p.cols, 1.0f);
+    ln_table<T, SPREAD>(tables + 4 * p.G, a.params.beta, a.params.has_beta, a.params.dtype, p.G,
+                        p.origin, p.cols, 0.0f);
+    // values of each warp of the row and their reciprocal
+    for (int w = threadIdx.x; w < LnExchange<CLUSTER>::kSlots; w += blockDim.x) {
+        const float n = (float)ln_warp_values<T, SPREAD>(w / p.warps, w % p.warps, p.G, a.cols);
+        counts[w] = make_float2(n, n > 0.0f ? 1.0f / n : 0.0f);
+    }
+    LnExchange<CLUSTER> others;
+    others.begin(slots, bars, p);
+    const bool whole = row_col<T, SPREAD>(15, p.G, p.tid) < p.cols;
+    const float inverse_n = counts[p.rank * p.warps + p.warp].y;
+
+    uint32_t turn = 0;
+    for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
+        f32x2 v[8];
+        unpack16<T>(next, v);
+        if (row + p.step < a.rows)
+            row_load<T, SPREAD>(x + (row + p.step) * a.ldx, p.G, p.tid, p.cols, wide, next);
+        const float sum = warp_sum(sum_of(v));
+        float mean = sum * inverse_n;
+        float f[16];
+        {
+            const f32x2 m = pair_of(-mean, -mean);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const f32x2 d = add2(v[i], m);
+                of_pair(d, f[2 * i], f[2 * i + 1]);
+            }
+        }
+        if (!whole) clear_beyond<T, SPREAD>(f, p.G, p.tid, p.cols);
+        f32x2 q = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f32x2 d = pair_of(f[2 * i], f[2 * i + 1]);
+            q = fma2(d, d, q);
+        }
+        float square, odd;
+        of_pair(q, square, odd);
+        square = warp_sum(square + odd);
+        if (row_warps > 1) {
+            const float2* got = others.send(make_float2(sum, square), turn, p);
+            mean = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; }) *
+                   inverse_cols;
+            square = others.sum(got, p.lane, [&](const float2* s, int w) {
+                const float d = fmaf(s[w].x, counts[w].y, -mean);
+                return fmaf(counts[w].x * d, d, s[w].y);
+            });
+        }
+        const float rstd = rsqrtf(fmaf(square, inverse_cols, a.eps));
+        if (p.tid == 0 && p.rank == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        {
+            const f32x2 m = pair_of(-mean, -mean), s = pair_of(rstd, rstd);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = mul2(add2(v[i], m), s);
+                of_pair(v[i], f[2 * i], f[2 * i + 1]);
+            }
+        }
+        if constexpr (KEEP != kKeepNone) {
+            float kept[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) kept[i] = f[i];
+            if (!whole) clear_beyond<T, SPREAD>(kept, p.G, p.tid, p.cols);
+            const uint64_t plane = row * pitch + p.origin;
+            if constexpr (SPREAD) {
+                act8_encode_spread<T, KEEP == kKeepRandom>(kept, plane, own, p.G, p.tid - p.lane,
+                                                           a.worker, keys, a.codes, a.scales);
+            } else {
+                uint32_t top = max_bits16(kept);
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                const uint32_t scale = act8_scale(top);
+                if (16u * p.tid < own) {
+                    const uint64_t at = (plane >> 4) + p.tid;
+                    __stcs(reinterpret_cast<uint4*>(a.codes) + at,
+                           act8_sixteen<KEEP == kKeepRandom>(kept, scale, at, a.worker, keys));
+                    if (!(p.tid & 1)) a.scales[at >> 1] = (uint8_t)scale;
+                }
+            }
+        }
+        f32x2 gamma[8], beta[8];
+        ln_params(tables, p.G, p.tid, gamma);
+        ln_params(tables + 4 * p.G, p.G, p.tid, beta);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) of_pair(fma2(v[i], gamma[i], beta[i]), f[2 * i], f[2 * i + 1]);
+        row_store<T, SPREAD>(y + row * a.ldy, p.G, p.tid, p.cols, wide, f);
+    }
+    // no block leaves while another may still write to its slots
+    if (CLUSTER > 1) cluster_sync();
 }
 
-template <typename T, int C, int THREADS>
-static void ln_forward_rows(const LnForward& a, int G, cudaStream_t stream) {
-    const bool element = a.access == kRowElement;
-    auto go = a.keep == kKeepNone
-                  ? (element ? ln_forward_go<T, C, THREADS, true, kKeepNone>
-                             : ln_forward_go<T, C, THREADS, false, kKeepNone>)
-              : a.keep == kKeepNearest
-                  ? (element ? ln_forward_go<T, C, THREADS, true, kKeepNearest>
-                             : ln_forward_go<T, C, THREADS, false, kKeepNearest>)
-                  : (element ? ln_forward_go<T, C, THREADS, true, kKeepRandom>
-                             : ln_forward_go<T, C, THREADS, false, kKeepRandom>);
-    go(a, G, stream);
+// how the rows are dealt out
+struct LnDeal {
+    int cluster, G, groups;              // blocks of a row, threads of a group, groups of a block
+    uint64_t owners;                     // blocks (clusters) that have a row
+};
+
+static LnDeal ln_deal(uint64_t rows, uint64_t cols) {
+    LnDeal d;
+    d.cluster = 1;
+    while (cols > 16u * kLnThreads * d.cluster) d.cluster *= 2;
+    const uint64_t share = (cols + d.cluster - 1) / d.cluster;
+    d.G = (int)((share + 511) / 512 * 32);
+    d.groups = d.cluster == 1 ? kLnThreads / d.G : 1;
+    d.owners = (rows + d.groups - 1) / d.groups;
+    return d;
+}
+
+// launches `kernel` on as many blocks as have rows, at most `threads` threads for every SM
+template <typename Kernel, typename... Args>
+static nc_status ln_launch(Kernel kernel, const LnDeal& d, int threads, uint64_t most, size_t smem,
+                           uint64_t* blocks, cudaStream_t stream, const Args&... args) {
+    const int per_sm = threads / (d.G * d.groups);
+    uint64_t n = (uint64_t)device_sm_count() * (per_sm < 1 ? 1 : per_sm) / d.cluster;
+    if (n > most) n = most;
+    if (n > d.owners) n = d.owners;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n * d.cluster);
+    cfg.blockDim = dim3(d.G * d.groups);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = d.cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = d.cluster > 1 ? 1 : 0;
+    if (blocks) *blocks = n;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? NC_OK : NC_ERR_CUDA;
+}
+
+template <typename T, bool SPREAD, int KEEP>
+static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
+    const LnDeal d = ln_deal(a.rows, a.cols);
+    auto kernel = d.cluster == 1   ? ln_forward_kernel<T, SPREAD, KEEP, 1>
+                  : d.cluster == 2 ? ln_forward_kernel<T, SPREAD, KEEP, 2>
+                  : d.cluster == 4 ? ln_forward_kernel<T, SPREAD, KEEP, 4>
+                                   : ln_forward_kernel<T, SPREAD, KEEP, 8>;
+    return ln_launch(kernel, d, 1024, (uint64_t)1 << 30, 2 * 16 * d.G * sizeof(float), nullptr,
+                     stream, a, d.G, make_philox_keys(a.seed));
 }
 
 template <typename T>
-static void ln_forward_launch(const LnForward& a, cudaStream_t stream) {
-    if (a.cols <= 4096)
-        ln_forward_rows<T, 1, 256>(a, (int)((a.cols + 511) / 512 * 32), stream);
-    else if (a.cols <= 16384)
-        ln_forward_rows<T, 1, 1024>(a, (int)((a.cols + 511) / 512 * 32), stream);
-    else
-        ln_forward_rows<T, 2, 1024>(a, (int)((a.cols + 1023) / 1024 * 32), stream);
+static nc_status ln_forward_launch(const LnForward& a, cudaStream_t stream) {
+    const bool spread = a.access == kRowElement;
+    auto go = a.keep == kKeepNone
+                  ? (spread ? ln_forward_go<T, true, kKeepNone> : ln_forward_go<T, false, kKeepNone>)
+              : a.keep == kKeepNearest
+                  ? (spread ? ln_forward_go<T, true, kKeepNearest>
+                            : ln_forward_go<T, false, kKeepNearest>)
+                  : (spread ? ln_forward_go<T, true, kKeepRandom>
+                            : ln_forward_go<T, false, kKeepRandom>);
+    return go(a, stream);
 }
 
 // ---- backward ------------------------------------------------------------------------------
@@ -381,168 +429,174 @@ struct LnRow {
     float mean, rstd;
 };
 
-// A block holds blockDim / G groups of G threads, a group owns a row at a time, 16 values a
-// thread.  CLUSTER > 1: one group a block, and the blocks of a cluster share a row, block r of it
-// owning the columns from r * 16 * G on.
-template <typename T, bool ELEMENT, bool SAVED8, bool RES, int CLUSTER>
-__global__ void __launch_bounds__(kLnBackThreads)
-ln_backward_kernel(const __grid_constant__ LnBackward a, const int G) {
-    __shared__ float2 part[2][CLUSTER * 16];
-    extern __shared__ float columns[];   // several groups: their sums
-    const int groups = blockDim.x / G, group = threadIdx.x / G, tid = threadIdx.x - group * G;
-    const int warps = G >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CLUSTER > 1 ? blockIdx.x % CLUSTER : 0;
-    const uint32_t origin = rank * 16 * G;                          // the block's first column
-    const uint32_t cols = a.cols > origin ? a.cols - origin : 0;    // from there on
-    const uint64_t step = (uint64_t)(gridDim.x / CLUSTER) * groups;
-    const uint64_t begin = (uint64_t)(blockIdx.x / CLUSTER) * groups + group;
+template <typename T, bool SPREAD, bool SAVED8, bool RES, int CLUSTER>
+__global__ void __launch_bounds__(kLnThreads, 2)
+ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
+    __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
+    __shared__ uint64_t bars[2];
+    extern __shared__ float4 table[];    // gamma; several groups: their sums behind it
+    const LnPlace<CLUSTER> p(threads, a.cols);
+    float* columns = reinterpret_cast<float*>(table + 4 * p.G);
+    const int row_warps = CLUSTER * p.warps;
+    const float inverse_cols = 1.0f / (float)a.cols;
 
-    const T* dy = static_cast<const T*>(a.dy) + origin;
-    const T* x = static_cast<const T*>(a.x) + (SAVED8 ? 0 : origin);
-    const T* dres = static_cast<const T*>(a.dres) + (RES ? origin : 0);
-    T* dx = static_cast<T*>(a.dx) + origin;
+    const T* dy = static_cast<const T*>(a.dy) + p.origin;
+    const T* x = static_cast<const T*>(a.x) + (SAVED8 ? 0 : p.origin);
+    const T* dres = static_cast<const T*>(a.dres) + (RES ? p.origin : 0);
+    T* dx = static_cast<T*>(a.dx) + p.origin;
     const uint32_t pitch = (a.cols + 31) & ~31u;
-    const uint32_t own = pitch > origin ? pitch - origin : 0;       // codes from there on
-    const uint32_t col0 = ln_col<false>(0, 0, G, tid);
+    const uint32_t own = pitch > p.origin ? pitch - p.origin : 0;    // codes of a row from here on
 
     auto load = [&](uint64_t row, LnRow<T, SAVED8, RES>& r) {
         r.rstd = __ldg(a.rstd + row);
-        ln_load<T, ELEMENT>(dy + row * a.lddy, 0, G, tid, cols, a.wide, r.dy);
-        if constexpr (SAVED8) {
-            const uint64_t plane = row * pitch + origin;
+        row_load<T, SPREAD>(dy + row * a.lddy, p.G, p.tid, p.cols, a.wide, r.dy);
+        if constexpr (SAVED8 && !SPREAD) {
+            const uint64_t plane = row * pitch + p.origin;
             r.codes = make_uint4(0u, 0u, 0u, 0u);
             r.scale = kAct8MinScale;
-            if (!ELEMENT && col0 < own) {
-                r.codes = ld_stream_u4(a.codes + plane + col0);
-                r.scale = __ldg(a.scales + ((plane + col0) >> 5));
+            if (16u * p.tid < own) {
+                r.codes = ld_stream_u4(a.codes + plane + 16u * p.tid);
+                r.scale = __ldg(a.scales + ((plane + 16u * p.tid) >> 5));
             }
-        } else {
+        } else if constexpr (!SAVED8) {
             r.mean = __ldg(a.mean + row);
-            ln_load<T, ELEMENT>(x + row * a.ldx, 0, G, tid, cols, a.wide, r.x);
+            row_load<T, SPREAD>(x + row * a.ldx, p.G, p.tid, p.cols, a.wide, r.x);
         }
         if constexpr (RES)
-            ln_load<T, ELEMENT>(dres + row * a.lddres, 0, G, tid, cols, a.wide, r.dres);
+            row_load<T, SPREAD>(dres + row * a.lddres, p.G, p.tid, p.cols, a.wide, r.dres);
     };
 
-    float gamma[16], dgamma[16], dbeta[16];
-    {
-        const int bytes = a.params.dtype == NC_DTYPE_F32 ? 4 : 2;
-        const char* p = static_cast<const char*>(a.params.gamma);
-        ln_params<ELEMENT>(p + (size_t)origin * bytes, a.params.has_gamma, a.params.dtype,
-                           a.params.vector, 0, G, tid, cols, 1.0f, gamma);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dgamma[i] = dbeta[i] = 0.0f;
-
-    // the other blocks' slots exist once all blocks of the cluster run
-    if (CLUSTER > 1) cooperative_groups::this_cluster().sync();
     LnRow<T, SAVED8, RES> next;
-    if (begin < a.rows) load(begin, next);
-    int turn = 0;
-    for (uint64_t row = begin; row < a.rows; row += step, turn ^= 1) {
-        const LnRow<T, SAVED8, RES> r = next;
-        if (row + step < a.rows) load(row + step, next);
-        float g[16], xh[16];
-        unpack16<T>(r.dy, g);
-        if constexpr (SAVED8) {
-            if (ELEMENT) {
-                const uint64_t plane = row * pitch + origin;
+    if (p.first < a.rows) load(p.first, next);
+    f32x2 dgamma[8], dbeta[8];
+    ln_table<T, SPREAD>(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+                        p.cols, 1.0f);
+    LnExchange<CLUSTER> others;
+    others.begin(slots, bars, p);
+    const bool whole = row_col<T, SPREAD>(15, p.G, p.tid) < p.cols;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = ln_col<true>(0, i, G, tid);
-                    xh[i] = col < cols ? act8_value(__ldg(a.codes + plane + col),
-                                                    __ldg(a.scales + ((plane + col) >> 5)))
-                                       : 0.0f;
-                }
+    for (int i = 0; i < 8; ++i) dgamma[i] = dbeta[i] = 0;
+
+    uint32_t turn = 0;
+    for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
+        f32x2 g[8], xh[8];
+        const float rstd = next.rstd;
+        unpack16<T>(next.dy, g);
+        {
+            float f[16];
+            if constexpr (SAVED8) {
+                if constexpr (SPREAD)
+                    act8_decode_spread<T>(a.codes, a.scales, row * pitch + p.origin, p.G, p.tid,
+                                          p.cols, f);
+                else
+                    act8_decode16(next.codes, next.scale, f);
             } else {
-                act8_decode16(r.codes, r.scale, xh);
-                if (col0 + 16 > cols) {
+                unpack16<T>(next.x, f);
+                const float mean = next.mean;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (col0 + i >= cols) xh[i] = 0.0f;      // of a block that is not finite
-                }
+                for (int i = 0; i < 16; ++i) f[i] = (f[i] - mean) * rstd;
             }
-        } else {
-            unpack16<T>(r.x, xh);
+            if (!whole) clear_beyond<T, SPREAD>(f, p.G, p.tid, p.cols);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                xh[i] = ln_col<ELEMENT>(0, i, G, tid) < cols ? (xh[i] - r.mean) * r.rstd : 0.0f;
+            for (int i = 0; i < 8; ++i) xh[i] = pair_of(f[2 * i], f[2 * i + 1]);
         }
-        float s1 = 0.0f, s2 = 0.0f;
+        Raw16<T> late;
+        if constexpr (RES) late = next.dres;
+        if (row + p.step < a.rows) load(row + p.step, next);
+        f32x2 s1 = 0, s2 = 0, gamma[8];
+        ln_params(table, p.G, p.tid, gamma);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            dbeta[i] += g[i];
-            dgamma[i] = fmaf(g[i], xh[i], dgamma[i]);
-            g[i] *= gamma[i];
-            s1 += g[i];
-            s2 = fmaf(g[i], xh[i], s2);
+        for (int i = 0; i < 8; ++i) {
+            dbeta[i] = add2(dbeta[i], g[i]);
+            dgamma[i] = fma2(g[i], xh[i], dgamma[i]);
+            g[i] = mul2(g[i], gamma[i]);
+            s1 = add2(s1, g[i]);
+            s2 = fma2(g[i], xh[i], s2);
         }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if (CLUSTER > 1 || warps > 1) {
-            // two sets of slots in turn: a slot is written again only after the barrier of the
-            // row in between, which its readers have passed
-            if constexpr (CLUSTER > 1) {
-                cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
-                if (lane < CLUSTER)
-                    *cluster.map_shared_rank(&part[turn][rank * 16 + warp], lane) =
-                        make_float2(s1, s2);
-                cluster.sync();
-            } else {
-                if (lane == 0) part[turn][warp] = make_float2(s1, s2);
-                group_sync(group, G);
-            }
-            s1 = s2 = 0.0f;
-            for (int k = 0; k < CLUSTER; ++k)
-                for (int w = 0; w < warps; ++w) {
-                    const float2 p = part[turn][k * 16 + group * warps + w];
-                    s1 += p.x;
-                    s2 += p.y;
-                }
+        float m1, m2, odd;
+        of_pair(s1, m1, odd);
+        m1 = warp_sum(m1 + odd);
+        of_pair(s2, m2, odd);
+        m2 = warp_sum(m2 + odd);
+        if (row_warps > 1) {
+            const float2* got = others.send(make_float2(m1, m2), turn, p);
+            m1 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; });
+            m2 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].y; });
         }
-        const float m1 = s1 / (float)a.cols, m2 = s2 / (float)a.cols;
+        m1 *= inverse_cols;
+        m2 *= inverse_cols;
+        // rstd * (g - m1 - xh * m2) + dres
+        float out[16];
+        const f32x2 n1 = pair_of(-m1, -m1), n2 = pair_of(-m2, -m2), s = pair_of(rstd, rstd);
+        f32x2 d[8];
+        if constexpr (RES) unpack16<T>(late, d);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) g[i] = r.rstd * fmaf(-xh[i], m2, g[i] - m1);
-        if constexpr (RES) {
-            float d[16];
-            unpack16<T>(r.dres, d);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) g[i] += d[i];
+        for (int i = 0; i < 8; ++i) {
+            const f32x2 inner = fma2(xh[i], n2, add2(g[i], n1));
+            of_pair(RES ? fma2(inner, s, d[i]) : mul2(inner, s), out[2 * i], out[2 * i + 1]);
         }
-        ln_store<T, ELEMENT>(dx + row * a.lddx, 0, G, tid, cols, a.wide, g);
+        row_store<T, SPREAD>(dx + row * a.lddx, p.G, p.tid, p.cols, a.wide, out);
     }
 
-    float* out = a.parts + (uint64_t)(blockIdx.x / CLUSTER) * 2 * a.parts_pitch + origin;
-    if (groups == 1) {
+    float dg[16], db[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = ln_col<ELEMENT>(0, i, G, tid);
-            if (col < cols) {
-                out[col] = dgamma[i];
-                out[a.parts_pitch + col] = dbeta[i];
-            }
-        }
-        // no block leaves while another may still write to its slots
-        if (CLUSTER > 1) cooperative_groups::this_cluster().sync();
-    } else {
-        for (int k = 0; k < groups; ++k) {           // the groups in order
-            if (group == k) {
+    for (int i = 0; i < 8; ++i) {
+        of_pair(dgamma[i], dg[2 * i], dg[2 * i + 1]);
+        of_pair(dbeta[i], db[2 * i], db[2 * i + 1]);
+    }
+    float* out = a.parts + (uint64_t)(blockIdx.x / CLUSTER) * 2 * a.parts_pitch + p.origin;
+    float* out2 = out + a.parts_pitch;
+    if (p.groups > 1) {                  // the groups add up in order
+        out = columns;
+        out2 = columns + pitch;
+        for (int k = 0; k < p.groups; ++k) {
+            if (p.group == k && k > 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = ln_col<ELEMENT>(0, i, G, tid);
-                    if (col < cols) {
-                        columns[col] = dgamma[i] + (k ? columns[col] : 0.0f);
-                        columns[pitch + col] = dbeta[i] + (k ? columns[pitch + col] : 0.0f);
+                    const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                    if (col < p.cols) {
+                        dg[i] += out[col];
+                        db[i] += out2[col];
+                    }
+                }
+            }
+            if (p.group == k && k + 1 < p.groups) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                    if (col < p.cols) {
+                        out[col] = dg[i];
+                        out2[col] = db[i];
                     }
                 }
             }
             __syncthreads();
         }
-        for (uint32_t col = threadIdx.x; col < cols; col += blockDim.x) {
-            out[col] = columns[col];
-            out[a.parts_pitch + col] = columns[pitch + col];
+        out = a.parts + (uint64_t)blockIdx.x * 2 * a.parts_pitch;
+        out2 = out + a.parts_pitch;
+    }
+    if (p.group == p.groups - 1) {
+        if (!SPREAD && whole) {          // the workspace's rows start on 16 bytes
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                *reinterpret_cast<float4*>(out + 16 * p.tid + i) =
+                    make_float4(dg[i], dg[i + 1], dg[i + 2], dg[i + 3]);
+                *reinterpret_cast<float4*>(out2 + 16 * p.tid + i) =
+                    make_float4(db[i], db[i + 1], db[i + 2], db[i + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                if (col < p.cols) {
+                    out[col] = dg[i];
+                    out2[col] = db[i];
+                }
+            }
         }
     }
+    // no block leaves while another may still write to its slots
+    if (CLUSTER > 1) cluster_sync();
 }
 
 // dgamma, dbeta <- [their values +] the sum of the blocks' parts, in the order of the blocks
@@ -556,8 +610,10 @@ ln_parts_kernel(const float* __restrict__ parts, const int blocks, const uint32_
     const uint32_t col = blockIdx.x * 32 + lane;
     const float* p = parts + (blockIdx.y ? pitch : 0) + col;
     float s = 0.0f;
-    if (col < cols)
-        for (int b = group; b < blocks; b += 8) s += p[(uint64_t)b * 2 * pitch];
+    if (col < cols) {
+#pragma unroll 8
+        for (int b = group; b < blocks; b += 8) s += __ldg(p + (uint64_t)b * 2 * pitch);
+    }
     sums[group][lane] = s;
     __syncthreads();
     if (group == 0 && col < cols) {
@@ -569,69 +625,34 @@ ln_parts_kernel(const float* __restrict__ parts, const int blocks, const uint32_
     }
 }
 
-// how the rows are dealt out
-struct LnDeal {
-    int cluster, G, groups;              // blocks of a row, threads of a group, groups of a block
-    uint64_t owners;                     // blocks (clusters) that are wanted at most
-};
-
-static LnDeal ln_deal(uint64_t rows, uint64_t cols) {
-    LnDeal d;
-    d.cluster = 1;
-    while (cols > 16u * kLnBackThreads * d.cluster) d.cluster *= 2;
-    const uint64_t share = (cols + d.cluster - 1) / d.cluster;
-    d.G = (int)((share + 511) / 512 * 32);
-    d.groups = d.G <= 128 ? 256 / d.G : 1;
-    const uint64_t owners = (rows + d.groups - 1) / d.groups;
-    d.owners = owners < (uint64_t)kLnMaxParts ? owners : (uint64_t)kLnMaxParts;
-    return d;
+template <typename T, bool SPREAD, bool SAVED8, bool RES>
+static nc_status ln_backward_go(const LnBackward& a, uint64_t* blocks, cudaStream_t stream) {
+    const LnDeal d = ln_deal(a.rows, a.cols);
+    auto kernel = d.cluster == 1   ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 1>
+                  : d.cluster == 2 ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 2>
+                  : d.cluster == 4 ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 4>
+                                   : ln_backward_kernel<T, SPREAD, SAVED8, RES, 8>;
+    const size_t smem =
+        16 * d.G * sizeof(float) + (d.groups > 1 ? 2 * act8_pitch(a.cols) * sizeof(float) : 0);
+    return ln_launch(kernel, d, 512, kLnMaxParts, smem, blocks, stream, a, d.G);
 }
 
-template <typename T, bool ELEMENT, bool SAVED8, int CLUSTER>
-static nc_status ln_backward_go(const LnBackward& a, const LnDeal& d, uint64_t blocks,
-                                cudaStream_t stream) {
-    auto kernel = a.dres ? ln_backward_kernel<T, ELEMENT, SAVED8, true, CLUSTER>
-                         : ln_backward_kernel<T, ELEMENT, SAVED8, false, CLUSTER>;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks * CLUSTER);
-    cfg.blockDim = dim3(d.G * d.groups);
-    cfg.dynamicSmemBytes = d.groups > 1 ? 2 * act8_pitch(a.cols) * sizeof(float) : 0;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    if (CLUSTER > 1) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = CLUSTER;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-    }
-    return cudaLaunchKernelEx(&cfg, kernel, a, d.G) == cudaSuccess ? NC_OK : NC_ERR_CUDA;
-}
-
-template <typename T, int CLUSTER>
-static nc_status ln_backward_rows(const LnBackward& a, bool element, const LnDeal& d,
-                                  uint64_t blocks, cudaStream_t stream) {
-    auto go = element ? (a.codes ? ln_backward_go<T, true, true, CLUSTER>
-                                 : ln_backward_go<T, true, false, CLUSTER>)
-                      : (a.codes ? ln_backward_go<T, false, true, CLUSTER>
-                                 : ln_backward_go<T, false, false, CLUSTER>);
-    return go(a, d, blocks, stream);
+template <typename T, bool SPREAD>
+static nc_status ln_backward_rows(const LnBackward& a, uint64_t* blocks, cudaStream_t stream) {
+    auto go = a.codes ? (a.dres ? ln_backward_go<T, SPREAD, true, true>
+                                : ln_backward_go<T, SPREAD, true, false>)
+                      : (a.dres ? ln_backward_go<T, SPREAD, false, true>
+                                : ln_backward_go<T, SPREAD, false, false>);
+    return go(a, blocks, stream);
 }
 
 template <typename T>
-static nc_status ln_backward_launch(LnBackward a, bool element, float* dgamma, float* dbeta,
+static nc_status ln_backward_launch(const LnBackward& a, bool spread, float* dgamma, float* dbeta,
                                     bool accumulate, cudaStream_t stream) {
     uint64_t blocks = 0;
     if (a.rows) {
-        // as many blocks as have the 512 threads that an SM's registers hold
-        const LnDeal d = ln_deal(a.rows, a.cols);
-        const uint64_t fit =
-            (uint64_t)device_sm_count() * (kLnBackThreads / (d.G * d.groups)) / d.cluster;
-        blocks = d.owners < fit ? d.owners : fit;
-        const nc_status st = d.cluster == 1   ? ln_backward_rows<T, 1>(a, element, d, blocks, stream)
-                             : d.cluster == 2 ? ln_backward_rows<T, 2>(a, element, d, blocks, stream)
-                                              : ln_backward_rows<T, 4>(a, element, d, blocks, stream);
+        const nc_status st = spread ? ln_backward_rows<T, true>(a, &blocks, stream)
+                                    : ln_backward_rows<T, false>(a, &blocks, stream);
         if (st != NC_OK) return st;
     }
     ln_parts_kernel<<<dim3((a.cols + 31) / 32, 2), 256, 0, stream>>>(
@@ -666,7 +687,6 @@ static nc_status ln_backward_call(LnBackward a, int dtype, size_t cols, int para
     if (a.rows && workspace_bytes < nc_layer_norm_workspace_bytes(a.rows, cols))
         return NC_ERR_WORKSPACE;
     a.params.dtype = param_dtype;
-    a.params.vector = aligned16(a.params.gamma);
     a.params.has_gamma = a.params.gamma != nullptr;
     if (!a.params.has_gamma) a.params.gamma = a.dy;
     int access = row_access(a.dy, a.lddy, bytes, a.rows);
@@ -675,13 +695,13 @@ static nc_status ln_backward_call(LnBackward a, int dtype, size_t cols, int para
                            a.codes ? kRowWide : row_access(a.x, a.ldx, bytes, a.rows)};
     for (int o : others) access = o > access ? o : access;
     a.wide = access == kRowWide;
-    const bool element = access == kRowElement;
+    const bool spread = access == kRowElement;
     if (dtype == NC_DTYPE_F32)
-        return ln_backward_launch<float>(a, element, dgamma, dbeta, accumulate != 0, stream);
+        return ln_backward_launch<float>(a, spread, dgamma, dbeta, accumulate != 0, stream);
     if (dtype == NC_DTYPE_BF16)
-        return ln_backward_launch<__nv_bfloat16>(a, element, dgamma, dbeta, accumulate != 0,
+        return ln_backward_launch<__nv_bfloat16>(a, spread, dgamma, dbeta, accumulate != 0,
                                                  stream);
-    return ln_backward_launch<__half>(a, element, dgamma, dbeta, accumulate != 0, stream);
+    return ln_backward_launch<__half>(a, spread, dgamma, dbeta, accumulate != 0, stream);
 }
 
 }  // namespace natcomp
@@ -692,7 +712,9 @@ extern "C" {
 
 size_t nc_layer_norm_workspace_bytes(size_t rows, size_t cols) {
     if (cols > kLnMaxCols) return 0;                 // refused by the calls
-    return ln_deal(rows, cols).owners * 2 * act8_pitch(cols) * sizeof(float);
+    const uint64_t owners = ln_deal(rows, cols).owners;
+    return (owners < (uint64_t)kLnMaxParts ? owners : (uint64_t)kLnMaxParts) * 2 *
+           act8_pitch(cols) * sizeof(float);
 }
 
 nc_status nc_layer_norm_forward(const void* x, int dtype, size_t rows, size_t cols, size_t ldx,
@@ -711,8 +733,7 @@ nc_status nc_layer_norm_forward(const void* x, int dtype, size_t rows, size_t co
         !element_aligned(gamma, pbytes) || !element_aligned(beta, pbytes) || !aligned4(mean) ||
         !aligned4(rstd) || !aligned16(codes) || !aligned16(scales))
         return NC_ERR_ALIGN;
-    const LnParams params = {gamma ? gamma : x, beta ? beta : x, param_dtype,
-                             aligned16(gamma) && aligned16(beta), gamma != nullptr,
+    const LnParams params = {gamma ? gamma : x, beta ? beta : x, param_dtype, gamma != nullptr,
                              beta != nullptr};
     LnForward a = {x, rows, (uint32_t)cols, ldx, params, eps, y, ldy, 0, mean, rstd, codes, scales,
                    kKeepNone, seed, worker};
@@ -720,12 +741,9 @@ nc_status nc_layer_norm_forward(const void* x, int dtype, size_t rows, size_t co
     a.access = ax > ay ? ax : ay;
     if (codes) a.keep = rounding == NC_ROUND_RANDOM ? kKeepRandom : kKeepNearest;
     if (dtype == NC_DTYPE_F32)
-        ln_forward_launch<float>(a, stream);
-    else if (dtype == NC_DTYPE_BF16)
-        ln_forward_launch<__nv_bfloat16>(a, stream);
-    else
-        ln_forward_launch<__half>(a, stream);
-    return launch_status();
+        return ln_forward_launch<float>(a, stream);
+    if (dtype == NC_DTYPE_BF16) return ln_forward_launch<__nv_bfloat16>(a, stream);
+    return ln_forward_launch<__half>(a, stream);
 }
 
 nc_status nc_layer_norm_backward(const void* dy, int dtype, size_t rows, size_t cols, size_t lddy,

@@ -52,6 +52,17 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank) {
                  : "memory");
 }
 
+// eight bytes to the same place in block `rank` of the cluster, counted by its barrier `bar`
+__device__ __forceinline__ void st_async_pair(uint32_t dst, uint32_t bar, uint32_t rank, float2 v) {
+    asm volatile("{\n\t"
+                 ".reg .b32 to, at;\n\t"
+                 "mapa.shared::cluster.u32 to, %0, %2;\n\t"
+                 "mapa.shared::cluster.u32 at, %1, %2;\n\t"
+                 "st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [to], {%3, %4}, [at];"
+                 "\n\t}" ::"r"(dst), "r"(bar), "r"(rank), "f"(v.x), "f"(v.y)
+                 : "memory");
+}
+
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n\t"
