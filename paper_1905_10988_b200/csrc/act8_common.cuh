@@ -206,24 +206,29 @@ __device__ __forceinline__ void unpack16(const Raw16<T>& r, f32x2 (&v)[8]) {
     for (int i = 0; i < 8; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
 }
 
-// ---- a thread's sixteen values of a row, two assignments --------------------------------------
+// ---- a thread's sixteen values of a row ---------------------------------------------------------
 // G threads share a row, 16 values each.  Value i of thread `tid` is column
 //   16 * tid + i                                rows on 16-byte boundaries: vector accesses
-//   SPREAD, 4-byte types: i * G + tid           any rows: neighbouring lanes, neighbouring values
-//   SPREAD, 2-byte types: 2 * ((i / 2) * G + tid) + i % 2     the same by pairs of values, so that
+//   kSpread, 4-byte types: i * G + tid          any rows: neighbouring lanes, neighbouring values
+//   kSpread, 2-byte types: 2 * ((i / 2) * G + tid) + i % 2    the same by pairs of values, so that
 //                                               a row on a 4-byte boundary moves a pair at a time
-template <typename T, bool SPREAD>
+// kRegular: rows on 32-byte boundaries, and every thread has sixteen values; no branches.
+enum RowMode { kRegular = 0, kVector = 1, kSpread = 2 };
+
+template <typename T, int MODE>
 __device__ __forceinline__ uint32_t row_col(int i, int G, int tid) {
-    if (!SPREAD) return 16u * tid + i;
+    if (MODE != kSpread) return 16u * tid + i;
     if (sizeof(T) == 4) return (uint32_t)i * G + tid;
     return 2u * ((uint32_t)(i >> 1) * G + tid) + (i & 1);
 }
 
 // values from `cols` on read as 0
-template <typename T, bool SPREAD>
+template <typename T, int MODE>
 __device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int tid, uint32_t cols,
                                          bool wide, Raw16<T>& r) {
-    if constexpr (!SPREAD) {
+    if constexpr (MODE == kRegular) {
+        r = ld_raw16<T>(row + 16u * tid, true);
+    } else if constexpr (MODE == kVector) {
         const uint32_t col = 16u * tid;
         if (col + 16 <= cols)
             r = ld_raw16<T>(row + col, wide);
@@ -231,32 +236,32 @@ __device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int t
             r = ld_raw16_part<T>(row + col, col < cols ? (int)(cols - col) : 0);
     } else if constexpr (sizeof(T) == 4) {
         const uint32_t* p = reinterpret_cast<const uint32_t*>(row);
-        if (row_col<T, true>(15, G, tid) < cols) {
+        if (row_col<T, kSpread>(15, G, tid) < cols) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                r.b[i >> 3].v[i & 7] = __ldg(p + row_col<T, true>(i, G, tid));
+                r.b[i >> 3].v[i & 7] = __ldg(p + row_col<T, kSpread>(i, G, tid));
             return;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, true>(i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(i, G, tid);
             r.b[i >> 3].v[i & 7] = col < cols ? __ldg(p + col) : 0u;
         }
     } else {
         const unsigned short* p = reinterpret_cast<const unsigned short*>(row);
         const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;     // the same for all lanes
-        if (row_col<T, true>(15, G, tid) < cols) {
+        if (row_col<T, kSpread>(15, G, tid) < cols) {
             if (!odd) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     r.b[0].v[i] = __ldg(
-                        reinterpret_cast<const uint32_t*>(p + row_col<T, true>(2 * i, G, tid)));
+                        reinterpret_cast<const uint32_t*>(p + row_col<T, kSpread>(2 * i, G, tid)));
             } else {
                 // two words hold a pair's halves; the row's first and last value have no
                 // neighbour to share a word with
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t col = row_col<T, true>(2 * i, G, tid);
+                    const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
                     const uint32_t* q = reinterpret_cast<const uint32_t*>(p + col - 1);
                     const uint32_t lo = i > 0 || tid > 0 ? __ldg(q) : (uint32_t)__ldg(p) << 16;
                     const uint32_t hi =
@@ -268,7 +273,7 @@ __device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int t
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
             uint32_t w = 0;
             if (col < cols) w = __ldg(p + col);
             if (col + 1 < cols) w |= (uint32_t)__ldg(p + col + 1) << 16;
@@ -277,40 +282,42 @@ __device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int t
     }
 }
 
-template <typename T, bool SPREAD>
+template <typename T, int MODE>
 __device__ __forceinline__ void row_store(T* __restrict__ row, int G, int tid, uint32_t cols,
                                           bool wide, const float (&v)[16]) {
-    if constexpr (!SPREAD) {
+    if constexpr (MODE == kRegular) {
+        st_raw16<T>(row + 16u * tid, pack16<T>(v), true);
+    } else if constexpr (MODE == kVector) {
         const uint32_t col = 16u * tid;
         if (col + 16 <= cols)
             st_raw16<T>(row + col, pack16<T>(v), wide);
         else if (col < cols)
             st_part16<T>(row + col, v, (int)(cols - col));
     } else if constexpr (sizeof(T) == 4) {
-        if (row_col<T, true>(15, G, tid) < cols) {
+        if (row_col<T, kSpread>(15, G, tid) < cols) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) row[row_col<T, true>(i, G, tid)] = v[i];
+            for (int i = 0; i < 16; ++i) row[row_col<T, kSpread>(i, G, tid)] = v[i];
             return;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, true>(i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(i, G, tid);
             if (col < cols) row[col] = v[i];
         }
     } else {
         unsigned short* p = reinterpret_cast<unsigned short*>(row);
         const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;
-        const bool whole = row_col<T, true>(15, G, tid) < cols;
+        const bool whole = row_col<T, kSpread>(15, G, tid) < cols;
         if (whole && !odd) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<uint32_t*>(p + row_col<T, true>(2 * i, G, tid)) =
+                *reinterpret_cast<uint32_t*>(p + row_col<T, kSpread>(2 * i, G, tid)) =
                     pack2<T>(v[2 * i], v[2 * i + 1]);
             return;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
             const uint32_t w = pack2<T>(v[2 * i], v[2 * i + 1]);
             if (whole || col < cols) p[col] = (unsigned short)w;
             if (whole || col + 1 < cols) p[col + 1] = (unsigned short)(w >> 16);
@@ -391,7 +398,7 @@ __device__ __forceinline__ uint4 act8_sixteen(const float (&v)[16], uint32_t sca
                       act8_four<RANDOM>(v + 12, inverse, r[3]));
 }
 
-// Codes of a thread's spread values (row_col<T, true>).  `plane`: place of the row's first code,
+// Codes of a thread's spread values (row_col<T, kSpread>).  `plane`: place of the row's first code,
 // `first` = tid - lane, `pitch`: codes of the row.  A step of the warp covers one block (4-byte
 // types) or two, of 16 lanes each.  The warp's 32 generator blocks of 16 draws are computed one
 // a lane.
@@ -406,12 +413,12 @@ __device__ __forceinline__ void act8_encode_spread(const float (&v)[16], uint64_
     uint32_t r[4] = {0u, 0u, 0u, 0u};
     if (RANDOM) {
         const int step = lane / (2 * PER), part = lane % (2 * PER);
-        const uint32_t col = row_col<T, true>(step * PER, G, first) + 16 * part;
+        const uint32_t col = row_col<T, kSpread>(step * PER, G, first) + 16 * part;
         stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
     }
 #pragma unroll
     for (int s = 0; s < 16 / PER; ++s) {
-        const uint32_t begin = row_col<T, true>(s * PER, G, first);
+        const uint32_t begin = row_col<T, kSpread>(s * PER, G, first);
         uint32_t top;
         if (PER == 1) {
             top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[s]) & 0x7FFFFFFFu);
@@ -501,7 +508,7 @@ __device__ __forceinline__ void act8_decode_spread(const uint8_t* __restrict__ c
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, true>(i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(i, G, tid);
             v[i] = col < cols ? act8_value(__ldg(codes + plane + col),
                                            __ldg(scales + ((plane + col) >> 5)))
                               : 0.0f;
@@ -509,7 +516,7 @@ __device__ __forceinline__ void act8_decode_spread(const uint8_t* __restrict__ c
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, true>(2 * i, G, tid);
+            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
             v[2 * i] = v[2 * i + 1] = 0.0f;
             if (col < cols) {
                 const uint32_t c =

@@ -57,7 +57,7 @@ act8_compress_spread_kernel(const T* __restrict__ x, const Act8Rows g, const uin
     const uint64_t first = 512ull * (w - row * segments);
     Raw16<T> r;
     float v[16];
-    row_load<T, true>(x + row * g.ld + first, 32, lane,
+    row_load<T, kSpread>(x + row * g.ld + first, 32, lane,
                       g.cols > first ? (uint32_t)min(g.cols - first, (uint64_t)512) : 0u, false, r);
     unpack16<T>(r, v);
     act8_encode_spread<T, RANDOM>(v, 16ull * row * g.per_row + first,
@@ -97,7 +97,7 @@ act8_decompress_spread_kernel(const uint8_t* __restrict__ codes, const uint8_t* 
     const uint32_t cols = (uint32_t)min(g.cols - first, (uint64_t)512);
     float v[16];
     act8_decode_spread<T>(codes, scales, 16ull * row * g.per_row + first, 32, lane, cols, v);
-    row_store<T, true>(out + row * g.ld + first, 32, lane, cols, false, v);
+    row_store<T, kSpread>(out + row * g.ld + first, 32, lane, cols, false, v);
 }
 
 // the plane of a matrix: one long row where the matrix has no gaps and whole blocks

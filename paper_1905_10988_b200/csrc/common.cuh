@@ -53,6 +53,20 @@ inline int device_sm_count() {
     return cached[dev];
 }
 
+// lets `kernel` use `bytes` of dynamic shared memory; `allowed` is a table of its own for each kernel,
+// so that a device is asked once
+inline bool allow_dynamic_smem(const void* kernel, int bytes, bool (&allowed)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const bool keep = dev >= 0 && dev < 64;
+    if (keep && allowed[dev]) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) !=
+        cudaSuccess)
+        return false;
+    if (keep) allowed[dev] = true;
+    return true;
+}
+
 inline nc_status launch_status() {
     return cudaPeekAtLastError() == cudaSuccess ? NC_OK : NC_ERR_CUDA;
 }

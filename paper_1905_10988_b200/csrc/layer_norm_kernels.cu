@@ -35,7 +35,7 @@ __device__ __forceinline__ float ln_param(const void* p, int dtype, uint32_t col
 
 // A vector of parameters as the threads of a group read it: four values of thread `tid` at
 // table[q * G + tid], q = 0..3, in the order of the thread's columns.  Absent ones are `none`.
-template <typename T, bool SPREAD>
+template <typename T, int MODE>
 __device__ __forceinline__ void ln_table(float4* table, const void* p, bool has, int dtype, int G,
                                          uint32_t origin, uint32_t cols, float none) {
 #pragma unroll 4
@@ -44,7 +44,7 @@ __device__ __forceinline__ void ln_table(float4* table, const void* p, bool has,
         float f[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t at = row_col<T, SPREAD>(4 * q + k, G, tid);
+            const uint32_t at = row_col<T, MODE>(4 * q + k, G, tid);
             f[k] = none;
             if (has && at < cols) f[k] = ln_param(p, dtype, origin + at);
         }
@@ -62,12 +62,12 @@ __device__ __forceinline__ void ln_params(const float4* table, int G, int tid, f
 }
 
 // (The empty statement keeps this a branch: few threads need it.)
-template <typename T, bool SPREAD>
+template <typename T, int MODE>
 __device__ __forceinline__ void clear_beyond(float (&v)[16], int G, int tid, uint32_t cols) {
     asm volatile("");
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-        if (row_col<T, SPREAD>(i, G, tid) >= cols) v[i] = 0.0f;
+        if (row_col<T, MODE>(i, G, tid) >= cols) v[i] = 0.0f;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -85,11 +85,11 @@ __device__ __forceinline__ float sum_of(const f32x2 (&v)[8]) {
 }
 
 // values of warp `w` of the row's block `rank`
-template <typename T, bool SPREAD>
+template <typename T, int MODE>
 __device__ __forceinline__ uint32_t ln_warp_values(int rank, int w, int G, uint32_t all_cols) {
     uint32_t n = 0;
     const uint32_t origin = rank * 16 * G;
-    if (!SPREAD) {
+    if (MODE != kSpread) {
         const uint32_t first = origin + 512u * w;
         n = all_cols > first ? min(all_cols - first, 512u) : 0u;
     } else {
@@ -218,7 +218,7 @@ struct LnForward {
 // Every warp sums up its own values and their squared distances from its own mean; one exchange
 // later the row's mean and variance follow from these (the squared distances about the common
 // mean are the warps' own plus n_w (mean_w - mean)^2).  A row is read ahead.
-template <typename T, bool SPREAD, int KEEP, int CLUSTER>
+template <typename T, int MODE, int KEEP, int CLUSTER>
 __global__ void __launch_bounds__(kLnThreads, 4)
 ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
                   const __grid_constant__ PhiloxKeys keys) {
@@ -236,19 +236,19 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
     const uint32_t own = pitch > p.origin ? pitch - p.origin : 0;    // codes of a row from here on
 
     Raw16<T> next;
-    if (p.first < a.rows) row_load<T, SPREAD>(x + p.first * a.ldx, p.G, p.tid, p.cols, wide, next);
-    ln_table<T, SPREAD>(tables, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+    if (p.first < a.rows) row_load<T, MODE>(x + p.first * a.ldx, p.G, p.tid, p.cols, wide, next);
+    ln_table<T, MODE>(tables, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
                         p.cols, 1.0f);
-    ln_table<T, SPREAD>(tables + 4 * p.G, a.params.beta, a.params.has_beta, a.params.dtype, p.G,
+    ln_table<T, MODE>(tables + 4 * p.G, a.params.beta, a.params.has_beta, a.params.dtype, p.G,
                         p.origin, p.cols, 0.0f);
     // values of each warp of the row and their reciprocal
     for (int w = threadIdx.x; w < LnExchange<CLUSTER>::kSlots; w += blockDim.x) {
-        const float n = (float)ln_warp_values<T, SPREAD>(w / p.warps, w % p.warps, p.G, a.cols);
+        const float n = (float)ln_warp_values<T, MODE>(w / p.warps, w % p.warps, p.G, a.cols);
         counts[w] = make_float2(n, n > 0.0f ? 1.0f / n : 0.0f);
     }
     LnExchange<CLUSTER> others;
     others.begin(slots, bars, p);
-    const bool whole = row_col<T, SPREAD>(15, p.G, p.tid) < p.cols;
+    const bool whole = MODE == kRegular || row_col<T, MODE>(15, p.G, p.tid) < p.cols;
     const float inverse_n = counts[p.rank * p.warps + p.warp].y;
 
     uint32_t turn = 0;
@@ -256,7 +256,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         f32x2 v[8];
         unpack16<T>(next, v);
         if (row + p.step < a.rows)
-            row_load<T, SPREAD>(x + (row + p.step) * a.ldx, p.G, p.tid, p.cols, wide, next);
+            row_load<T, MODE>(x + (row + p.step) * a.ldx, p.G, p.tid, p.cols, wide, next);
         const float sum = warp_sum(sum_of(v));
         float mean = sum * inverse_n;
         float f[16];
@@ -268,7 +268,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
                 of_pair(d, f[2 * i], f[2 * i + 1]);
             }
         }
-        if (!whole) clear_beyond<T, SPREAD>(f, p.G, p.tid, p.cols);
+        if (!whole) clear_beyond<T, MODE>(f, p.G, p.tid, p.cols);
         f32x2 q = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -304,16 +304,16 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
             float kept[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) kept[i] = f[i];
-            if (!whole) clear_beyond<T, SPREAD>(kept, p.G, p.tid, p.cols);
+            if (!whole) clear_beyond<T, MODE>(kept, p.G, p.tid, p.cols);
             const uint64_t plane = row * pitch + p.origin;
-            if constexpr (SPREAD) {
+            if constexpr (MODE == kSpread) {
                 act8_encode_spread<T, KEEP == kKeepRandom>(kept, plane, own, p.G, p.tid - p.lane,
                                                            a.worker, keys, a.codes, a.scales);
             } else {
                 uint32_t top = max_bits16(kept);
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 const uint32_t scale = act8_scale(top);
-                if (16u * p.tid < own) {
+                if (MODE == kRegular || 16u * p.tid < own) {
                     const uint64_t at = (plane >> 4) + p.tid;
                     __stcs(reinterpret_cast<uint4*>(a.codes) + at,
                            act8_sixteen<KEEP == kKeepRandom>(kept, scale, at, a.worker, keys));
@@ -326,7 +326,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         ln_params(tables + 4 * p.G, p.G, p.tid, beta);
 #pragma unroll
         for (int i = 0; i < 8; ++i) of_pair(fma2(v[i], gamma[i], beta[i]), f[2 * i], f[2 * i + 1]);
-        row_store<T, SPREAD>(y + row * a.ldy, p.G, p.tid, p.cols, wide, f);
+        row_store<T, MODE>(y + row * a.ldy, p.G, p.tid, p.cols, wide, f);
     }
     // no block leaves while another may still write to its slots
     if (CLUSTER > 1) cluster_sync();
@@ -373,27 +373,148 @@ static nc_status ln_launch(Kernel kernel, const LnDeal& d, int threads, uint64_t
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? NC_OK : NC_ERR_CUDA;
 }
 
-template <typename T, bool SPREAD, int KEEP>
+// Rows of a multiple of 1024 columns up to 8192 on 32-byte boundaries: 32 values a thread, half
+// the reductions a value, and no case to tell apart.
+template <typename T, int KEEP>
+__global__ void __launch_bounds__(kLnThreads, sizeof(T) == 4 ? 2 : 3)
+ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads,
+                          const __grid_constant__ PhiloxKeys keys) {
+    __shared__ float2 slots[2 * 8 * 8];
+    __shared__ uint64_t bars[2];
+    extern __shared__ float4 tables[];   // gamma, beta of the first and of the second half
+    const LnPlace<1> p(threads, a.cols);
+    const int G = p.G;
+    const float inverse_cols = 1.0f / (float)a.cols;
+    const T* x = static_cast<const T*>(a.x) + 16 * p.tid;
+    T* y = static_cast<T*>(a.y) + 16 * p.tid;
+
+    Raw16<T> next[2];
+    if (p.first < a.rows) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) next[c] = ld_raw16<T>(x + p.first * a.ldx + c * 16 * G, true);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const uint32_t origin = c * 16 * G;
+        ln_table<T, kRegular>(tables + 8 * G * c, a.params.gamma, a.params.has_gamma,
+                              a.params.dtype, G, origin, a.cols - origin, 1.0f);
+        ln_table<T, kRegular>(tables + 8 * G * c + 4 * G, a.params.beta, a.params.has_beta,
+                              a.params.dtype, G, origin, a.cols - origin, 0.0f);
+    }
+    LnExchange<1> others;
+    others.begin(slots, bars, p);
+
+    uint32_t turn = 0;
+    for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
+        f32x2 v[2][8];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) unpack16<T>(next[c], v[c]);
+        if (row + p.step < a.rows) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                next[c] = ld_raw16<T>(x + (row + p.step) * a.ldx + c * 16 * G, true);
+        }
+        const float sum = warp_sum(sum_of(v[0]) + sum_of(v[1]));
+        float mean = sum * (1.0f / 1024.0f);
+        f32x2 q = 0;
+        f32x2 m = pair_of(-mean, -mean);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const f32x2 d = add2(v[c][i], m);
+                q = fma2(d, d, q);
+            }
+        float square, odd;
+        of_pair(q, square, odd);
+        square = warp_sum(square + odd);
+        if (p.warps > 1) {
+            const float2* got = others.send(make_float2(sum, square), turn, p);
+            mean = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; }) *
+                   inverse_cols;
+            square = others.sum(got, p.lane, [&](const float2* s, int w) {
+                const float d = fmaf(s[w].x, 1.0f / 1024.0f, -mean);
+                return w < p.warps ? fmaf(1024.0f * d, d, s[w].y) : 0.0f;
+            });
+        }
+        const float rstd = rsqrtf(fmaf(square, inverse_cols, a.eps));
+        if (p.tid == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        m = pair_of(-mean, -mean);
+        const f32x2 s = pair_of(rstd, rstd);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] = mul2(add2(v[c][i], m), s);
+                of_pair(v[c][i], f[2 * i], f[2 * i + 1]);
+            }
+            if constexpr (KEEP != kKeepNone) {
+                uint32_t top = max_bits16(f);
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                const uint32_t scale = act8_scale(top);
+                const uint64_t at = ((row * a.cols) >> 4) + c * G + p.tid;
+                __stcs(reinterpret_cast<uint4*>(a.codes) + at,
+                       act8_sixteen<KEEP == kKeepRandom>(f, scale, at, a.worker, keys));
+                if (!(p.tid & 1)) a.scales[at >> 1] = (uint8_t)scale;
+            }
+            f32x2 gamma[8], beta[8];
+            ln_params(tables + 8 * G * c, G, p.tid, gamma);
+            ln_params(tables + 8 * G * c + 4 * G, G, p.tid, beta);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                of_pair(fma2(v[c][i], gamma[i], beta[i]), f[2 * i], f[2 * i + 1]);
+            st_raw16<T>(y + row * a.ldy + c * 16 * G, pack16<T>(f), true);
+        }
+    }
+}
+
+// rows on 32-byte boundaries whose values fill every thread of every block
+static bool ln_regular(const LnDeal& d, uint64_t cols, int access) {
+    return access == kRowWide && d.cluster <= 2 && cols == 16ull * d.G * d.cluster;
+}
+
+template <typename T, int KEEP>
 static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
+    if (a.access == kRowWide && a.cols % 1024 == 0 && a.cols <= 8192) {
+        LnDeal d;
+        d.cluster = 1;
+        d.G = (int)(a.cols / 32);
+        d.groups = kLnThreads / d.G;
+        d.owners = (a.rows + d.groups - 1) / d.groups;
+        const size_t smem = 4 * 16 * d.G * sizeof(float);
+        static bool allowed[64];
+        if (!allow_dynamic_smem((const void*)ln_forward_regular_kernel<T, KEEP>,
+                                4 * 16 * kLnThreads * sizeof(float), allowed))
+            return NC_ERR_CUDA;
+        return ln_launch(ln_forward_regular_kernel<T, KEEP>, d, sizeof(T) == 4 ? 512 : 768,
+                         (uint64_t)1 << 30, smem, nullptr, stream, a, d.G,
+                         make_philox_keys(a.seed));
+    }
     const LnDeal d = ln_deal(a.rows, a.cols);
-    auto kernel = d.cluster == 1   ? ln_forward_kernel<T, SPREAD, KEEP, 1>
-                  : d.cluster == 2 ? ln_forward_kernel<T, SPREAD, KEEP, 2>
-                  : d.cluster == 4 ? ln_forward_kernel<T, SPREAD, KEEP, 4>
-                                   : ln_forward_kernel<T, SPREAD, KEEP, 8>;
-    return ln_launch(kernel, d, 1024, (uint64_t)1 << 30, 2 * 16 * d.G * sizeof(float), nullptr,
+    auto pick = [&]() {
+        if (a.access != kRowElement)
+            return d.cluster == 1   ? ln_forward_kernel<T, kVector, KEEP, 1>
+                   : d.cluster == 2 ? ln_forward_kernel<T, kVector, KEEP, 2>
+                   : d.cluster == 4 ? ln_forward_kernel<T, kVector, KEEP, 4>
+                                    : ln_forward_kernel<T, kVector, KEEP, 8>;
+        return d.cluster == 1   ? ln_forward_kernel<T, kSpread, KEEP, 1>
+               : d.cluster == 2 ? ln_forward_kernel<T, kSpread, KEEP, 2>
+               : d.cluster == 4 ? ln_forward_kernel<T, kSpread, KEEP, 4>
+                                : ln_forward_kernel<T, kSpread, KEEP, 8>;
+    };
+    return ln_launch(pick(), d, 1024, (uint64_t)1 << 30, 2 * 16 * d.G * sizeof(float), nullptr,
                      stream, a, d.G, make_philox_keys(a.seed));
 }
 
 template <typename T>
 static nc_status ln_forward_launch(const LnForward& a, cudaStream_t stream) {
-    const bool spread = a.access == kRowElement;
-    auto go = a.keep == kKeepNone
-                  ? (spread ? ln_forward_go<T, true, kKeepNone> : ln_forward_go<T, false, kKeepNone>)
-              : a.keep == kKeepNearest
-                  ? (spread ? ln_forward_go<T, true, kKeepNearest>
-                            : ln_forward_go<T, false, kKeepNearest>)
-                  : (spread ? ln_forward_go<T, true, kKeepRandom>
-                            : ln_forward_go<T, false, kKeepRandom>);
+    auto go = a.keep == kKeepNone      ? ln_forward_go<T, kKeepNone>
+              : a.keep == kKeepNearest ? ln_forward_go<T, kKeepNearest>
+                                       : ln_forward_go<T, kKeepRandom>;
     return go(a, stream);
 }
 
@@ -429,7 +550,7 @@ struct LnRow {
     float mean, rstd;
 };
 
-template <typename T, bool SPREAD, bool SAVED8, bool RES, int CLUSTER>
+template <typename T, int MODE, bool SAVED8, bool RES, int CLUSTER>
 __global__ void __launch_bounds__(kLnThreads, 2)
 ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
@@ -449,31 +570,31 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
 
     auto load = [&](uint64_t row, LnRow<T, SAVED8, RES>& r) {
         r.rstd = __ldg(a.rstd + row);
-        row_load<T, SPREAD>(dy + row * a.lddy, p.G, p.tid, p.cols, a.wide, r.dy);
-        if constexpr (SAVED8 && !SPREAD) {
+        row_load<T, MODE>(dy + row * a.lddy, p.G, p.tid, p.cols, a.wide, r.dy);
+        if constexpr (SAVED8 && MODE != kSpread) {
             const uint64_t plane = row * pitch + p.origin;
             r.codes = make_uint4(0u, 0u, 0u, 0u);
             r.scale = kAct8MinScale;
-            if (16u * p.tid < own) {
+            if (MODE == kRegular || 16u * p.tid < own) {
                 r.codes = ld_stream_u4(a.codes + plane + 16u * p.tid);
                 r.scale = __ldg(a.scales + ((plane + 16u * p.tid) >> 5));
             }
         } else if constexpr (!SAVED8) {
             r.mean = __ldg(a.mean + row);
-            row_load<T, SPREAD>(x + row * a.ldx, p.G, p.tid, p.cols, a.wide, r.x);
+            row_load<T, MODE>(x + row * a.ldx, p.G, p.tid, p.cols, a.wide, r.x);
         }
         if constexpr (RES)
-            row_load<T, SPREAD>(dres + row * a.lddres, p.G, p.tid, p.cols, a.wide, r.dres);
+            row_load<T, MODE>(dres + row * a.lddres, p.G, p.tid, p.cols, a.wide, r.dres);
     };
 
     LnRow<T, SAVED8, RES> next;
     if (p.first < a.rows) load(p.first, next);
     f32x2 dgamma[8], dbeta[8];
-    ln_table<T, SPREAD>(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+    ln_table<T, MODE>(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
                         p.cols, 1.0f);
     LnExchange<CLUSTER> others;
     others.begin(slots, bars, p);
-    const bool whole = row_col<T, SPREAD>(15, p.G, p.tid) < p.cols;
+    const bool whole = MODE == kRegular || row_col<T, MODE>(15, p.G, p.tid) < p.cols;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgamma[i] = dbeta[i] = 0;
 
@@ -485,7 +606,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         {
             float f[16];
             if constexpr (SAVED8) {
-                if constexpr (SPREAD)
+                if constexpr (MODE == kSpread)
                     act8_decode_spread<T>(a.codes, a.scales, row * pitch + p.origin, p.G, p.tid,
                                           p.cols, f);
                 else
@@ -496,7 +617,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) f[i] = (f[i] - mean) * rstd;
             }
-            if (!whole) clear_beyond<T, SPREAD>(f, p.G, p.tid, p.cols);
+            if (!whole) clear_beyond<T, MODE>(f, p.G, p.tid, p.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) xh[i] = pair_of(f[2 * i], f[2 * i + 1]);
         }
@@ -535,7 +656,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             const f32x2 inner = fma2(xh[i], n2, add2(g[i], n1));
             of_pair(RES ? fma2(inner, s, d[i]) : mul2(inner, s), out[2 * i], out[2 * i + 1]);
         }
-        row_store<T, SPREAD>(dx + row * a.lddx, p.G, p.tid, p.cols, a.wide, out);
+        row_store<T, MODE>(dx + row * a.lddx, p.G, p.tid, p.cols, a.wide, out);
     }
 
     float dg[16], db[16];
@@ -553,7 +674,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             if (p.group == k && k > 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                    const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
                     if (col < p.cols) {
                         dg[i] += out[col];
                         db[i] += out2[col];
@@ -563,7 +684,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             if (p.group == k && k + 1 < p.groups) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                    const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
                     if (col < p.cols) {
                         out[col] = dg[i];
                         out2[col] = db[i];
@@ -576,7 +697,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         out2 = out + a.parts_pitch;
     }
     if (p.group == p.groups - 1) {
-        if (!SPREAD && whole) {          // the workspace's rows start on 16 bytes
+        if (MODE != kSpread && whole) {  // the workspace's rows start on 16 bytes
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 *reinterpret_cast<float4*>(out + 16 * p.tid + i) =
@@ -587,7 +708,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const uint32_t col = row_col<T, SPREAD>(i, p.G, p.tid);
+                const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
                 if (col < p.cols) {
                     out[col] = dg[i];
                     out2[col] = db[i];
@@ -625,34 +746,38 @@ ln_parts_kernel(const float* __restrict__ parts, const int blocks, const uint32_
     }
 }
 
-template <typename T, bool SPREAD, bool SAVED8, bool RES>
-static nc_status ln_backward_go(const LnBackward& a, uint64_t* blocks, cudaStream_t stream) {
+template <typename T, bool SAVED8, bool RES>
+static nc_status ln_backward_go(const LnBackward& a, int access, uint64_t* blocks,
+                                cudaStream_t stream) {
     const LnDeal d = ln_deal(a.rows, a.cols);
-    auto kernel = d.cluster == 1   ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 1>
-                  : d.cluster == 2 ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 2>
-                  : d.cluster == 4 ? ln_backward_kernel<T, SPREAD, SAVED8, RES, 4>
-                                   : ln_backward_kernel<T, SPREAD, SAVED8, RES, 8>;
+    auto pick = [&]() {
+        if (ln_regular(d, a.cols, access))
+            return d.cluster == 1 ? ln_backward_kernel<T, kRegular, SAVED8, RES, 1>
+                                  : ln_backward_kernel<T, kRegular, SAVED8, RES, 2>;
+        if (access != kRowElement)
+            return d.cluster == 1   ? ln_backward_kernel<T, kVector, SAVED8, RES, 1>
+                   : d.cluster == 2 ? ln_backward_kernel<T, kVector, SAVED8, RES, 2>
+                   : d.cluster == 4 ? ln_backward_kernel<T, kVector, SAVED8, RES, 4>
+                                    : ln_backward_kernel<T, kVector, SAVED8, RES, 8>;
+        return d.cluster == 1   ? ln_backward_kernel<T, kSpread, SAVED8, RES, 1>
+               : d.cluster == 2 ? ln_backward_kernel<T, kSpread, SAVED8, RES, 2>
+               : d.cluster == 4 ? ln_backward_kernel<T, kSpread, SAVED8, RES, 4>
+                                : ln_backward_kernel<T, kSpread, SAVED8, RES, 8>;
+    };
     const size_t smem =
         16 * d.G * sizeof(float) + (d.groups > 1 ? 2 * act8_pitch(a.cols) * sizeof(float) : 0);
-    return ln_launch(kernel, d, 512, kLnMaxParts, smem, blocks, stream, a, d.G);
-}
-
-template <typename T, bool SPREAD>
-static nc_status ln_backward_rows(const LnBackward& a, uint64_t* blocks, cudaStream_t stream) {
-    auto go = a.codes ? (a.dres ? ln_backward_go<T, SPREAD, true, true>
-                                : ln_backward_go<T, SPREAD, true, false>)
-                      : (a.dres ? ln_backward_go<T, SPREAD, false, true>
-                                : ln_backward_go<T, SPREAD, false, false>);
-    return go(a, blocks, stream);
+    return ln_launch(pick(), d, 512, kLnMaxParts, smem, blocks, stream, a, d.G);
 }
 
 template <typename T>
-static nc_status ln_backward_launch(const LnBackward& a, bool spread, float* dgamma, float* dbeta,
+static nc_status ln_backward_launch(const LnBackward& a, int access, float* dgamma, float* dbeta,
                                     bool accumulate, cudaStream_t stream) {
     uint64_t blocks = 0;
     if (a.rows) {
-        const nc_status st = spread ? ln_backward_rows<T, true>(a, &blocks, stream)
-                                    : ln_backward_rows<T, false>(a, &blocks, stream);
+        auto go = a.codes ? (a.dres ? ln_backward_go<T, true, true> : ln_backward_go<T, true, false>)
+                          : (a.dres ? ln_backward_go<T, false, true>
+                                    : ln_backward_go<T, false, false>);
+        const nc_status st = go(a, access, &blocks, stream);
         if (st != NC_OK) return st;
     }
     ln_parts_kernel<<<dim3((a.cols + 31) / 32, 2), 256, 0, stream>>>(
@@ -695,13 +820,12 @@ static nc_status ln_backward_call(LnBackward a, int dtype, size_t cols, int para
                            a.codes ? kRowWide : row_access(a.x, a.ldx, bytes, a.rows)};
     for (int o : others) access = o > access ? o : access;
     a.wide = access == kRowWide;
-    const bool spread = access == kRowElement;
     if (dtype == NC_DTYPE_F32)
-        return ln_backward_launch<float>(a, spread, dgamma, dbeta, accumulate != 0, stream);
+        return ln_backward_launch<float>(a, access, dgamma, dbeta, accumulate != 0, stream);
     if (dtype == NC_DTYPE_BF16)
-        return ln_backward_launch<__nv_bfloat16>(a, spread, dgamma, dbeta, accumulate != 0,
+        return ln_backward_launch<__nv_bfloat16>(a, access, dgamma, dbeta, accumulate != 0,
                                                  stream);
-    return ln_backward_launch<__half>(a, spread, dgamma, dbeta, accumulate != 0, stream);
+    return ln_backward_launch<__half>(a, access, dgamma, dbeta, accumulate != 0, stream);
 }
 
 }  // namespace natcomp

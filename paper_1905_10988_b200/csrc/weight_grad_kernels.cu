@@ -569,21 +569,6 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k) {
     return p;
 }
 
-// lets the product's kernels use their shared memory, once per device
-static bool wg_allow_smem(bool copy) {
-    static bool allowed[2][64];
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return false;
-    const bool keep = device >= 0 && device < 64;
-    if (keep && allowed[copy][device]) return true;
-    auto kernel = copy ? wg_product_kernel<true> : wg_product_kernel<false>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmem) !=
-        cudaSuccess)
-        return false;
-    if (keep) allowed[copy][device] = true;
-    return true;
-}
-
 }  // namespace natcomp
 
 using namespace natcomp;
@@ -653,7 +638,8 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
                                      kWgStep))
             return NC_ERR_CUDA;
         auto kernel = copy ? wg_product_kernel<true> : wg_product_kernel<false>;
-        if (!wg_allow_smem(copy)) return NC_ERR_CUDA;
+        static bool allowed[2][64];
+        if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[copy])) return NC_ERR_CUDA;
         const uint64_t pairs = p.whole ? kWgPairs : (p.tiles - p.whole) * p.splits;
         kernel<<<(unsigned)(2 * pairs), 32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders)), kWgSmem,
                  stream>>>(a, map);
