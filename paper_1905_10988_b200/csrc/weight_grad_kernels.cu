@@ -8,18 +8,21 @@
 // binary32 accumulation; a checkpoint's values are exact in bfloat16, so nothing is rounded on the
 // way.  They exist as bfloat16 in shared memory only.
 //
-// A pair of blocks (cta_group::2) computes tiles of 256 x 256 values of dW one after another; block
-// r of it brings 128 of the n and 128 of the k.  Both operands have the tokens as their strided
-// dimension, as they lie in memory.  A step is 64 tokens, and its operands pass through a ring in
-// shared memory:
+// A pair of blocks (cta_group::2) computes tiles of dW one after another: 256 x 256 values, or two
+// neighbours along n at a time, 512 x 256; block r of the pair brings 128 of each 256 n and 128 of
+// the k.  What bounds a step is shared memory: it takes the dY tile, the decoded tile and the
+// codes, and the tensor cores read both tiles.  Two tiles at a time share the decoded one.  Both
+// operands have the tokens as their strided dimension, as they lie in memory.  A step is 64 tokens,
+// and its operands pass through a ring in shared memory:
 //   - one thread copies the dY tile by tensor copies (rows on 16-byte boundaries), or four warps
 //     gather it with plain loads (rows at any element);
 //   - sixteen warps decode, in four groups that take every fourth step: a group holds the codes of
 //     its next step in registers while the other three work, which covers the loads' latency;
 //   - one thread of the pair's first block issues the matrix instructions; TMEM holds two tiles, so
 //     four more warps write one out while the next is computed.
-// The tiles are dealt out evenly to the chip's 74 pairs.  What is left over, fewer tiles than
-// pairs, is split along the tokens, and a second kernel adds its binary32 parts in order.
+// The tiles are dealt out evenly to the chip's 74 pairs, double ones while there are rounds of
+// them, then single ones.  What is left over, fewer tiles than pairs, is split along the tokens,
+// and a second kernel adds its binary32 parts in order.
 #include "act8_common.cuh"
 #include "tensor_core.cuh"
 
@@ -28,7 +31,7 @@ namespace natcomp {
 constexpr int kWgTile = 256;             // n and k of a pair's tile
 constexpr int kWgHalf = 128;             // of a block
 constexpr int kWgStep = 64;              // tokens
-constexpr int kWgStages = 6;
+constexpr int kWgStages = 6;             // of the ring of decoded tiles and of the ring of dY tiles
 constexpr int kWgGroups = 4, kWgGroupWarps = 4;      // decoders
 constexpr int kWgWriters = 4, kWgLoaders = 4;        // warps
 constexpr int kWgCopyWarp = kWgWriters, kWgMmaWarp = kWgWriters + 1;
@@ -36,8 +39,9 @@ constexpr int kWgDecodeWarp = kWgWriters + 2;        // the first of them
 constexpr int kWgLoadWarp = kWgDecodeWarp + kWgGroups * kWgGroupWarps;
 constexpr uint32_t kWgPanel = kWgStep * 128;         // bytes of 64 values x 64 tokens
 constexpr uint32_t kWgOperand = 2 * kWgPanel;        // of a block's half
-constexpr uint32_t kWgStageBytes = 2 * kWgOperand;
-constexpr uint32_t kWgSmem = kWgStages * kWgStageBytes + 1024 + 256 + 2 * kWgTile * 4;
+constexpr uint32_t kWgDecoded = kWgStages * kWgOperand;   // the decoded tiles follow the dY tiles
+constexpr uint32_t kWgTiles = 2 * kWgStages * kWgOperand;
+constexpr uint32_t kWgSmem = kWgTiles + 1024 + 512 + 2 * kWgTile * 4;
 constexpr int kWgPairs = 74;             // pairs of blocks that the chip holds at a time
 constexpr int kWgMinSteps = 4;           // of a part
 
@@ -54,8 +58,11 @@ struct WgArgs {
     const float* db;                     // complete when dW is written
     int accumulate;
     bool vector;                         // dw rows may be written 16 bytes at a time
-    uint32_t tiles_n, tiles;             // tile i: n tile i % tiles_n, k tile i / tiles_n
-    uint32_t whole, splits;              // tiles from `whole` on are computed in `splits` parts
+    uint32_t tiles_n, tiles_k;           // of 256 x 256
+    uint32_t rounds;                     // of double tiles; double tile i: n tiles 2 (i % m) and
+                                         // one more, m = tiles_n / 2, k tile i / m
+    uint32_t tiles;                      // single ones after that
+    uint32_t whole, splits;              // those from `whole` on are computed in `splits` parts
     float* parts;                        // [tile - whole][part][256][256]
 };
 
@@ -65,16 +72,41 @@ __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) 
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// the u-th piece of work of a pair: a tile's steps, or a part of them
+// the u-th piece of work of a pair: the steps of a double tile, of a single one, or a part of them
 struct WgUnit {
     uint32_t tile, part, first, steps;   // steps == 0: no more work
-    uint64_t n0, k0;                     // of the tile
+    uint32_t halves;                     // tiles of 256 n
+    uint64_t n0, k0;
 };
+
+// place of the single tile `i`: first the halves of the double tiles that no round has taken, then
+// the last column of an odd number
+__device__ __forceinline__ void wg_single(const WgArgs& a, uint32_t i, uint64_t& n0, uint64_t& k0) {
+    const uint32_t m = a.tiles_n / 2, taken = a.rounds * kWgPairs, left = 2 * (m * a.tiles_k - taken);
+    if (i < left) {
+        const uint32_t d = taken + i / 2;
+        n0 = (uint64_t)(2 * (d % m) + (i & 1)) * kWgTile;
+        k0 = (uint64_t)(d / m) * kWgTile;
+    } else {
+        n0 = (uint64_t)(a.tiles_n - 1) * kWgTile;
+        k0 = (uint64_t)(i - left) * kWgTile;
+    }
+}
 
 __device__ __forceinline__ WgUnit wg_unit(const WgArgs& a, uint32_t pair, uint32_t u) {
     const uint32_t all = (uint32_t)((a.rows + kWgStep - 1) / kWgStep);
     const uint32_t pairs = gridDim.x >> 1, rounds = a.whole / pairs;
     WgUnit w = {};
+    w.halves = 1;
+    if (u < a.rounds) {
+        const uint32_t m = a.tiles_n / 2, d = u * pairs + pair;
+        w.halves = 2;
+        w.steps = all;
+        w.n0 = (uint64_t)(d % m) * (2 * kWgTile);
+        w.k0 = (uint64_t)(d / m) * kWgTile;
+        return w;
+    }
+    u -= a.rounds;
     if (u < rounds) {
         w.tile = u * pairs + pair;
         w.steps = all;
@@ -84,10 +116,30 @@ __device__ __forceinline__ WgUnit wg_unit(const WgArgs& a, uint32_t pair, uint32
         w.first = (uint32_t)((uint64_t)all * w.part / a.splits);
         w.steps = (uint32_t)((uint64_t)all * (w.part + 1) / a.splits) - w.first;
     }
-    w.n0 = (uint64_t)(w.tile % a.tiles_n) * kWgTile;
-    w.k0 = (uint64_t)(w.tile / a.tiles_n) * kWgTile;
+    if (w.steps) wg_single(a, w.tile, w.n0, w.k0);
     return w;
 }
+
+// which of the two accumulators in TMEM a unit's tiles use, and how often each was used before
+struct WgTurns {
+    uint32_t uses[2], next;
+    __device__ __forceinline__ WgTurns() : uses{0u, 0u}, next(0u) {}
+    __device__ __forceinline__ uint32_t of(const WgUnit& w, uint32_t half) const {
+        return w.halves == 2 ? half : next;
+    }
+    __device__ __forceinline__ void done(const WgUnit& w) {
+        if (w.halves == 2) {
+            ++uses[0];
+            ++uses[1];
+        } else {
+            if (next) ++uses[1]; else ++uses[0];
+            next ^= 1;
+        }
+    }
+    __device__ __forceinline__ uint32_t parity(uint32_t b) const {
+        return (b ? uses[1] : uses[0]) & 1;
+    }
+};
 
 // a place in a pair's sequence of steps
 struct WgWalk {
@@ -227,15 +279,17 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     extern __shared__ uint8_t raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const uint32_t tiles = smem_u32(base);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgStages * kWgStageBytes);
-    const uint32_t empty = smem_u32(bars);             // [stages] operands consumed
-    const uint32_t copied = empty + 8 * kWgStages;     // [stages] the block's dY tile arrived
-    const uint32_t ready = copied + 8 * kWgStages;     // [stages] of the first block: the others' share
-    const uint32_t full = ready + 8 * kWgStages;       // [2] a tile's product is complete
-    const uint32_t drained = full + 16;                // [2] of the first block: TMEM read out
+    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgTiles);
+    // Barriers by step (step % stages).  The thread that issues the matrix instructions waits for
+    // one of them and commits to one a step: every further wait would leave the tensor cores idle.
+    const uint32_t empty = smem_u32(bars);             // operands consumed
+    const uint32_t ready = empty + 8 * kWgStages;      // first block's: both blocks' operands are there
+    const uint32_t copied = ready + 8 * kWgStages;     // second block's: its dY tiles arrived
+    const uint32_t full = copied + 8 * kWgStages;      // [2] a tile's product is complete
+    const uint32_t drained = full + 16;                // [2] first block's: TMEM read out
     uint32_t* words = reinterpret_cast<uint32_t*>(bars + 3 * kWgStages + 4);
     volatile uint32_t* gave_up = words + 1;
-    float* affine = reinterpret_cast<float*>(base + kWgStages * kWgStageBytes + 256);
+    float* affine = reinterpret_cast<float*>(base + kWgTiles + 512);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1;
@@ -245,8 +299,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         words[1] = 0;
         for (int s = 0; s < kWgStages; ++s) {
             mbar_init(empty + 8 * s, 1);
+            mbar_init(ready + 8 * s, 2 * (kWgGroupWarps + (COPY ? 1 : kWgLoaders)));
             mbar_init(copied + 8 * s, 1);
-            mbar_init(ready + 8 * s, 2 * kWgGroupWarps + (COPY ? 1 : 2 * kWgLoaders));
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(full + 8 * b, 1);
@@ -268,7 +322,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         const uint32_t token = i0 >> 3, eighth = i0 & 7;
         const uint64_t column = rank * kWgHalf + 16 * eighth;
         const bool odd = eighth >= 4;
-        const uint32_t place = kWgOperand + (odd ? kWgPanel : 0u) + token * 128;
+        const uint32_t place = kWgDecoded + (odd ? kWgPanel : 0u) + token * 128;
         const uint32_t chunk = (2 * (eighth & 3) + odd) ^ (token & 7);
         WgWalk walk;
         walk.begin(a, pair);
@@ -280,7 +334,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             walk.advance(a, pair, kWgGroups);
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
                 break;
-            const uint32_t line = tiles + ring.stage * kWgStageBytes + place;
+            const uint32_t line = tiles + ring.stage * kWgOperand + place;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint4 c = r.c[i];
@@ -298,10 +352,10 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     } else if (warp < kWgWriters) {
         // ---- write a tile out: lane = row
         uint32_t u = 0;
+        WgTurns turns;
         for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) {
-            const uint64_t n = w.n0 + rank * kWgHalf + 32 * warp + lane, k0 = w.k0;
-            const bool part = w.tile >= a.whole && a.splits > 1;
-            float add = 0.0f;
+            const uint64_t k0 = w.k0;
+            const bool part = w.halves == 1 && w.tile >= a.whole && a.splits > 1;
             if (!part) {
                 asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgWriters) : "memory");
                 for (int i = threadIdx.x; i < kWgTile; i += 32 * kWgWriters) {
@@ -311,65 +365,85 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                         a.beta && in ? wg_param(a.beta, a.param_dtype, k0 + i) : 0.0f;
                 }
                 asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgWriters) : "memory");
-                if (a.beta && n < a.n) add = a.db[n];
             }
-            bool ok = mbar_wait(full + 8 * (u & 1), (u >> 1) & 1, gave_up);
-            ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
-            tc_fence_after();
-            const uint32_t from = tmem + (u & 1) * kWgTile + ((uint32_t)(32 * warp) << 16);
-            float* parts = a.parts + (((uint64_t)(w.tile - a.whole) * a.splits + w.part) * kWgTile +
-                                      rank * kWgHalf + 32 * warp + lane) * kWgTile;
 #pragma unroll 1
-            for (int c = 0; c < kWgTile; c += 32) {
-                float v[32];
-                tmem_load32(from + c, v);
-                if (!ok) {           // a wait ran out: the result must not pass for one
+            for (uint32_t h = 0; h < w.halves; ++h) {
+                const uint32_t b = turns.of(w, h);
+                const uint64_t n = w.n0 + h * kWgTile + rank * kWgHalf + 32 * warp + lane;
+                const float add = !part && a.beta && n < a.n ? a.db[n] : 0.0f;
+                bool ok = mbar_wait(full + 8 * b, turns.parity(b), gave_up);
+                ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
+                tc_fence_after();
+                const uint32_t from = tmem + b * kWgTile + ((uint32_t)(32 * warp) << 16);
+                float* parts = a.parts + (((uint64_t)(w.tile - a.whole) * a.splits + w.part) *
+                                              kWgTile + rank * kWgHalf + 32 * warp + lane) * kWgTile;
+#pragma unroll 1
+                for (int c = 0; c < kWgTile; c += 32) {
+                    float v[32];
+                    tmem_load32(from + c, v);
+                    if (!ok) {       // a wait ran out: the result must not pass for one
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
+                    }
+                    if (part) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4*>(parts + c + i) =
+                                make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        continue;
+                    }
+                    if (n >= a.n || k0 + c >= a.k) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        float o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[j] = fmaf(v[i + j], affine[c + i + j],
+                                        add * affine[kWgTile + c + i + j]);
+                        wg_store4(a, n, k0 + c + i, o);
+                    }
                 }
-                if (part) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<float4*>(parts + c + i) =
-                            make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                    continue;
-                }
-                if (n >= a.n || k0 + c >= a.k) continue;
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float o[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        o[j] = fmaf(v[i + j], affine[c + i + j],
-                                    add * affine[kWgTile + c + i + j]);
-                    wg_store4(a, n, k0 + c + i, o);
-                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(drained + 8 * b, 0);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_at(drained + 8 * (u & 1), 0);
+            turns.done(w);
         }
     } else if (warp == kWgCopyWarp) {
-        // ---- copies of the dY tile: two panels of 64 n
+        // ---- copies of the dY tiles: two panels of 64 n each.  A place of their ring is free when
+        // the step that used it last is done.
         if (COPY && lane == 0) {
-            WgRing ring = {0, 1};
             WgWalk walk;
-            uint32_t issued = 0;
-            for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1)) {
-                if (!mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)) break;
-                const uint32_t dst = tiles + ring.stage * kWgStageBytes;
-                mbar_expect(copied + 8 * ring.stage, kWgOperand);
-                for (int p = 0; p < 2; ++p)
-                    tma_load_2d(dst + p * kWgPanel, &map,
-                                (int)(walk.unit.n0 + rank * kWgHalf + 64 * p), (int)walk.token(),
-                                copied + 8 * ring.stage);
-                ring.advance(1);
-                ++issued;
+            const uint32_t arrived = rank ? copied : ready;
+            uint32_t place = 0, step = 0, last[kWgStages];        // last: step + 1, 0: unused
+            for (int s = 0; s < kWgStages; ++s) last[s] = 0;
+            bool ok = true;
+            for (walk.begin(a, pair); walk.more() && ok; walk.advance(a, pair, 1), ++step) {
+                const uint32_t bar = arrived + 8 * (step % kWgStages);
+                for (uint32_t h = 0; h < walk.unit.halves; ++h) {
+                    uint32_t before = 0;
+#pragma unroll
+                    for (int s = 0; s < kWgStages; ++s)
+                        if (s == (int)place) {
+                            before = last[s];
+                            last[s] = step + 1;
+                        }
+                    if (before)
+                        ok = mbar_wait(empty + 8 * ((before - 1) % kWgStages),
+                                       ((before - 1) / kWgStages) & 1, gave_up);
+                    if (!ok) break;
+                    if (h == 0) mbar_expect(bar, walk.unit.halves * kWgOperand);
+                    for (int p = 0; p < 2; ++p)
+                        tma_load_2d(tiles + place * kWgOperand + p * kWgPanel, &map,
+                                    (int)(walk.unit.n0 + h * kWgTile + rank * kWgHalf + 64 * p),
+                                    (int)walk.token(), bar);
+                    place = place + 1 == kWgStages ? 0 : place + 1;
+                }
             }
             // the copies in flight land before the block may end
             const long long begin = clock64();
-            for (uint32_t i = issued < kWgStages ? 0 : issued - kWgStages; i < issued; ++i)
-                while (!mbar_try(copied + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
+            for (uint32_t i = step < kWgStages ? 0 : step - kWgStages; i < step; ++i)
+                while (!mbar_try(arrived + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
                        clock64() - begin < 4000000000ll) {}
         }
     } else if (warp == kWgMmaWarp) {
@@ -377,30 +451,43 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             // ---- matrix instructions
             const uint32_t shape = mma_shape(kWgTile, kWgTile);
             WgRing ring = {0, 0};
-            bool ok = true;
-            uint32_t u = 0;
+            bool ok = true, here = false;            // here: the next step was seen to be ready
+            uint32_t u = 0, place = 0;
+            WgTurns turns;
             for (WgUnit w = wg_unit(a, pair, 0); w.steps && ok; w = wg_unit(a, pair, ++u)) {
-                const uint32_t to = tmem + (u & 1) * kWgTile;
-                ok = mbar_wait(drained + 8 * (u & 1), ((u >> 1) & 1) ^ 1, gave_up);
-                tc_fence_after();
+                for (uint32_t h = 0; h < w.halves && ok; ++h) {
+                    const uint32_t b = turns.of(w, h);
+                    ok = mbar_wait(drained + 8 * b, turns.parity(b) ^ 1, gave_up);
+                }
+                const uint32_t to[2] = {tmem + turns.of(w, 0) * kWgTile, tmem + kWgTile};
                 for (uint32_t s = 0; s < w.steps && ok; ++s) {
-                    ok = (!COPY || mbar_wait(copied + 8 * ring.stage, ring.parity, gave_up)) &&
-                         mbar_wait(ready + 8 * ring.stage, ring.parity, gave_up);
+                    if (!here) ok = mbar_wait(ready + 8 * ring.stage, ring.parity, gave_up);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t at = tiles + ring.stage * kWgStageBytes;
-#pragma unroll
-                    for (int i = 0; i < kWgStep / 16; ++i)      // 16 tokens: two groups of lines
-                        mma_pair(to, mma_operand(at + 2048 * i, kWgPanel),
-                                 mma_operand(at + kWgOperand + 2048 * i, kWgPanel), shape,
-                                 s > 0 || i > 0);
-                    mma_commit_pair(empty + 8 * ring.stage);
+                    const uint32_t decoded = tiles + kWgDecoded + ring.stage * kWgOperand;
+                    const uint32_t empty_bar = empty + 8 * ring.stage;
                     ring.advance(1);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1 && w.halves == 1) break;
+                        const uint32_t at = tiles + place * kWgOperand;
+                        place = place + 1 == kWgStages ? 0 : place + 1;
+#pragma unroll
+                        for (int i = 0; i < kWgStep / 16; ++i) {  // 16 tokens: two groups of lines
+                            mma_pair(to[h], mma_operand(at + 2048 * i, kWgPanel),
+                                     mma_operand(decoded + 2048 * i, kWgPanel), shape,
+                                     s > 0 || i > 0);
+                            if (i == 1 && h + 1 == (int)w.halves)
+                                here = mbar_try(ready + 8 * ring.stage, ring.parity);
+                        }
+                    }
+                    mma_commit_pair(empty_bar);
                 }
-                mma_commit_pair(full + 8 * (u & 1));
+                for (uint32_t h = 0; h < w.halves; ++h) mma_commit_pair(full + 8 * turns.of(w, h));
+                turns.done(w);
             }
         } else if (COPY && lane == 0) {
-            // ---- the other block: pass on that its dY tile has arrived
+            // ---- the other block: pass on that its dY tiles have arrived
             WgRing ring = {0, 0};
             WgWalk walk;
             for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1)) {
@@ -427,7 +514,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             walk.advance(a, pair, 1);
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
                 break;
-            const uint32_t dst = tiles + ring.stage * kWgStageBytes + (chunk >> 3) * kWgPanel;
+            const uint32_t dst = tiles + ring.stage * kWgOperand + (chunk >> 3) * kWgPanel;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t token = token0 + 8 * j;
@@ -458,8 +545,10 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
 __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a) {
     const uint32_t tile = a.whole + blockIdx.x / 64, row = blockIdx.x % 64 * 4 + (threadIdx.x >> 6);
     const uint32_t column = (threadIdx.x & 63) * 4;
-    const uint64_t n = (uint64_t)(tile % a.tiles_n) * kWgTile + row;
-    const uint64_t k = (uint64_t)(tile / a.tiles_n) * kWgTile + column;
+    uint64_t n, k;
+    wg_single(a, tile, n, k);
+    n += row;
+    k += column;
     if (n >= a.n || k >= a.k) return;
     const float* p = a.parts + ((uint64_t)(tile - a.whole) * a.splits * kWgTile + row) * kWgTile + column;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -529,6 +618,46 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
     }
 }
 
+// the same for rows that are not on 16-byte boundaries, and a copy of dY whose rows are: a warp
+// takes 512 columns of every eighth row
+__global__ void __launch_bounds__(256)
+wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
+                const uint64_t lddy, __nv_bfloat16* __restrict__ copy, const uint64_t ldc,
+                float* __restrict__ parts) {
+    __shared__ float sums[512];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t first = (uint64_t)blockIdx.x * 512;
+    const uint32_t cols = (uint32_t)min(n - first, (uint64_t)512);
+    const uint64_t begin = rows * blockIdx.y / gridDim.y, end = rows * (blockIdx.y + 1) / gridDim.y;
+    float s[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    for (uint64_t t = begin + warp; t < end; t += 8) {
+        Raw16<__nv_bfloat16> r;
+        row_load<__nv_bfloat16, kSpread>(dy + t * lddy + first, 32, lane, cols, false, r);
+        uint32_t* out = reinterpret_cast<uint32_t*>(copy + t * ldc + first);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)      // rows of the copy hold whole pairs
+            if (row_col<__nv_bfloat16, kSpread>(2 * i, 32, lane) < cols)
+                out[32 * i + lane] = r.b[0].v[i];
+        float v[16];
+        unpack16<__nv_bfloat16>(r, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] += v[i];
+    }
+    for (int w = 0; w < 8; ++w) {        // the warps in order
+        if (warp == w) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t c = row_col<__nv_bfloat16, kSpread>(i, 32, lane);
+                sums[c] = w ? sums[c] + s[i] : s[i];
+            }
+        }
+        __syncthreads();
+    }
+    for (uint32_t c = threadIdx.x; c < cols; c += 256) parts[blockIdx.y * n + first + c] = sums[c];
+}
+
 // db <- [db +] the parts' sum; `fresh` (may be db) gets the sum alone
 __global__ void __launch_bounds__(256)
 wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uint64_t n,
@@ -542,16 +671,20 @@ wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uin
 }
 
 struct WgPlan {
-    uint64_t tiles_n, tiles, whole;
+    uint64_t tiles_n, tiles_k, rounds, tiles, whole;
     uint32_t splits;
     int sum_blocks;
-    size_t sum_offset, fresh_offset, bytes;
+    uint64_t ldc;                        // row stride of the aligned copy of dY
+    size_t sum_offset, fresh_offset, copy_offset, bytes;
 };
 
-static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k) {
+// `doubles`: double tiles may be used
+static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     WgPlan p = {};
     p.tiles_n = (n + kWgTile - 1) / kWgTile;
-    p.tiles = p.tiles_n * ((k + kWgTile - 1) / kWgTile);
+    p.tiles_k = (k + kWgTile - 1) / kWgTile;
+    p.rounds = doubles ? p.tiles_n / 2 * p.tiles_k / kWgPairs : 0;
+    p.tiles = p.tiles_n * p.tiles_k - 2 * kWgPairs * p.rounds;
     const uint64_t steps = (rows + kWgStep - 1) / kWgStep, left = p.tiles % kWgPairs;
     uint64_t splits = left ? kWgPairs / left : 1;
     if (splits > steps / kWgMinSteps) splits = steps / kWgMinSteps;
@@ -565,7 +698,10 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k) {
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
     p.sum_offset = p.splits > 1 ? left * p.splits * kWgTile * kWgTile * 4 : 0;
     p.fresh_offset = p.sum_offset + round_up16(p.sum_blocks * n * 4);
-    p.bytes = p.fresh_offset + round_up16(n * 4);
+    p.copy_offset = p.fresh_offset + round_up16(n * 4);
+    p.ldc = (n + 7) / 8 * 8;
+    // a copy is made where the width itself keeps rows off the boundaries
+    p.bytes = p.copy_offset + (n % 8 ? rows * p.ldc * 2 : 0);
     return p;
 }
 
@@ -577,7 +713,7 @@ extern "C" {
 
 size_t nc_act8_weight_grad_workspace_bytes(size_t rows, size_t n, size_t k) {
     if (n > ((size_t)1 << 31) || k > ((size_t)1 << 31) || rows > ((size_t)1 << 31)) return 0;
-    return wg_plan(rows, n, k).bytes;
+    return wg_plan(rows, n, k, true).bytes;
 }
 
 nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy,
@@ -600,22 +736,32 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         !element_aligned(beta, pbytes) || !element_aligned(dw, wbytes) || !aligned4(db) ||
         !aligned16(codes) || !aligned16(scales) || !aligned16(workspace))
         return NC_ERR_ALIGN;
-    const WgPlan p = wg_plan(rows, n, k);
+    const bool aligned = row_access(dy, lddy, 2, rows) != kRowElement;
+    const bool copied = !aligned && n % 8 != 0;          // through a copy that is
+    const WgPlan p = wg_plan(rows, n, k, rows && (aligned || copied));
     if (rows && workspace_bytes < p.bytes) return NC_ERR_WORKSPACE;
 
     char* ws = static_cast<char*>(workspace);
     float* fresh = reinterpret_cast<float*>(ws + p.fresh_offset);
     const bool with_beta = beta && k && rows;
-    if (db || with_beta) {
+    if (db || with_beta || copied) {
         float* sums = reinterpret_cast<float*>(ws + p.sum_offset);
-        const bool vector = n % 8 == 0 && row_access(dy, lddy, 2, rows) != kRowElement;
-        auto kernel = vector ? wg_sums_kernel<true> : wg_sums_kernel<false>;
-        if (rows)
+        const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(dy);
+        if (copied) {
+            __nv_bfloat16* copy = reinterpret_cast<__nv_bfloat16*>(ws + p.copy_offset);
+            wg_align_kernel<<<dim3((unsigned)((n + 511) / 512), p.sum_blocks), 256, 0, stream>>>(
+                in, rows, n, lddy, copy, p.ldc, sums);
+            dy = copy;
+            lddy = p.ldc;
+        } else if (rows) {
+            const bool vector = aligned && n % 8 == 0;
+            auto kernel = vector ? wg_sums_kernel<true> : wg_sums_kernel<false>;
             kernel<<<dim3((unsigned)((n + (vector ? 255 : 31)) / (vector ? 256 : 32)),
-                          p.sum_blocks), 256, 0, stream>>>(
-                static_cast<const __nv_bfloat16*>(dy), rows, n, lddy, sums);
-        wg_sums_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(
-            sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
+                          p.sum_blocks), 256, 0, stream>>>(in, rows, n, lddy, sums);
+        }
+        if (db || with_beta)
+            wg_sums_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(
+                sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
     }
     if (k == 0) return launch_status();
 
@@ -627,20 +773,21 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     a.db = fresh; a.accumulate = accumulate;
     a.vector = row_access(dw, lddw, wbytes, n) != kRowElement;
     a.tiles_n = (uint32_t)p.tiles_n;
+    a.tiles_k = (uint32_t)p.tiles_k;
+    a.rounds = (uint32_t)p.rounds;
     a.tiles = (uint32_t)p.tiles;
     a.whole = rows ? (uint32_t)p.whole : 0;
     a.splits = rows ? p.splits : 0;
     a.parts = reinterpret_cast<float*>(ws);
     if (rows) {
-        const bool copy = row_access(dy, lddy, 2, rows) != kRowElement;
+        const bool copy = aligned || copied;             // by tensor copies
         CUtensorMap map = {};
-        if (copy && !make_tensor_map(&map, dy, rows, n, rows > 1 ? lddy : (n + 7) / 8 * 8, 64,
-                                     kWgStep))
+        if (copy && !make_tensor_map(&map, dy, rows, n, rows > 1 ? lddy : p.ldc, 64, kWgStep))
             return NC_ERR_CUDA;
         auto kernel = copy ? wg_product_kernel<true> : wg_product_kernel<false>;
         static bool allowed[2][64];
         if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[copy])) return NC_ERR_CUDA;
-        const uint64_t pairs = p.whole ? kWgPairs : (p.tiles - p.whole) * p.splits;
+        const uint64_t pairs = p.whole || p.rounds ? kWgPairs : (p.tiles - p.whole) * p.splits;
         kernel<<<(unsigned)(2 * pairs), 32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders)), kWgSmem,
                  stream>>>(a, map);
     }

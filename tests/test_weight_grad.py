@@ -153,6 +153,16 @@ def test_gpu_weight_gradient(t, n, k, dy_layout, dw_layout, affine, wkind, accum
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,n,k,dy_layout", [(130, 5128, 2100, "whole"), (70, 5299, 2050, "any"),
+                                             (200, 9000, 2304, "gap"), (65, 5128, 2100, "any")])
+def test_gpu_more_tiles_than_pairs(t, n, k, dy_layout):
+    # rounds of double tiles, then single ones, then a rest; an odd number of tiles along n
+    got, want, tol, gotb, wantb, tolb = run(t, n, k, "bf16", "bf16", False, dy_layout, "whole")
+    assert np.all(np.abs(got - want) <= tol)
+    assert np.all(np.abs(gotb - wantb) <= tolb)
+
+
+@pytest.mark.gpu
 def test_gpu_long_contraction():
     got, want, tol, gotb, wantb, tolb = run(20_000, 300, 700, "bf16", "f32", False, "whole",
                                             "whole")
