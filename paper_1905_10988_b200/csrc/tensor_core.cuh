@@ -101,6 +101,14 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
                  : "memory");
 }
 
+// `bytes` (a multiple of 16) neighbouring bytes; both addresses are multiples of 16
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
+                                          uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes"
+                 " [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
 // ordinary stores to shared memory become visible to tensor copies and tensor-core reads
 __device__ __forceinline__ void fence_async_proxy() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -185,8 +193,9 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
 
 // ---- host ------------------------------------------------------------------------------------
 
-// map of a row-major matrix of bfloat16 for boxes of box_cols x box_rows with 128-byte swizzle
-inline bool make_tensor_map(CUtensorMap* map, const void* p, uint64_t rows, uint64_t cols,
+// map of a row-major matrix of bfloat16 for boxes of box_cols x box_rows with 128-byte swizzle, or
+// of bytes without
+inline bool make_tensor_map(CUtensorMap* map, const void* p, bool bf16, uint64_t rows, uint64_t cols,
                             uint64_t ld, uint32_t box_cols, uint32_t box_rows) {
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -202,10 +211,11 @@ inline bool make_tensor_map(CUtensorMap* map, const void* p, uint64_t rows, uint
             return false;
         encode = (Encode)f;
     }
-    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {2 * ld};
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {(bf16 ? 2 : 1) * ld};
     const cuuint32_t box[2] = {box_cols, box_rows}, steps[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides,
-                  box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
+                  const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  bf16 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -16,8 +16,10 @@
 // and its operands pass through a ring in shared memory:
 //   - one thread copies the dY tile by tensor copies (rows on 16-byte boundaries), or four warps
 //     gather it with plain loads (rows at any element);
-//   - sixteen warps decode, in four groups that take every fourth step: a group holds the codes of
-//     its next step in registers while the other three work, which covers the loads' latency;
+//   - another thread copies the codes and their scale bytes, which a small kernel has laid out by
+//     columns of 128 beforehand, so that a step's are 256 neighbouring bytes and not a byte or four
+//     of each of 64 lines;
+//   - sixteen warps decode, in four groups that take every fourth step;
 //   - one thread of the pair's first block issues the matrix instructions; TMEM holds two tiles, so
 //     four more warps write one out while the next is computed.
 // The tiles are dealt out evenly to the chip's 74 pairs, double ones while there are rounds of
@@ -31,25 +33,31 @@ namespace natcomp {
 constexpr int kWgTile = 256;             // n and k of a pair's tile
 constexpr int kWgHalf = 128;             // of a block
 constexpr int kWgStep = 64;              // tokens
-constexpr int kWgStages = 6;             // of the ring of decoded tiles and of the ring of dY tiles
+constexpr int kWgStages = 6;             // steps that barriers tell apart, places of dY tiles
+constexpr int kWgSlots = 5;              // places of codes and of decoded tiles
 constexpr int kWgGroups = 4, kWgGroupWarps = 4;      // decoders
 constexpr int kWgWriters = 4, kWgLoaders = 4;        // warps
-constexpr int kWgCopyWarp = kWgWriters, kWgMmaWarp = kWgWriters + 1;
-constexpr int kWgDecodeWarp = kWgWriters + 2;        // the first of them
+constexpr int kWgCopyWarp = kWgWriters, kWgCodeWarp = kWgWriters + 1, kWgMmaWarp = kWgWriters + 2;
+constexpr int kWgDecodeWarp = kWgWriters + 4;        // the first of them, a multiple of four
 constexpr int kWgLoadWarp = kWgDecodeWarp + kWgGroups * kWgGroupWarps;
 constexpr uint32_t kWgPanel = kWgStep * 128;         // bytes of 64 values x 64 tokens
 constexpr uint32_t kWgOperand = 2 * kWgPanel;        // of a block's half
-constexpr uint32_t kWgDecoded = kWgStages * kWgOperand;   // the decoded tiles follow the dY tiles
-constexpr uint32_t kWgTiles = 2 * kWgStages * kWgOperand;
-constexpr uint32_t kWgSmem = kWgTiles + 1024 + 512 + 2 * kWgTile * 4;
+constexpr uint32_t kWgCodeBytes = kWgStep * 128, kWgScaleBytes = kWgStep * 4;
+// shared memory: dY tiles, decoded tiles, codes, scales, barriers, gamma and beta
+constexpr uint32_t kWgDecoded = kWgStages * kWgOperand;
+constexpr uint32_t kWgCodes = kWgDecoded + kWgSlots * kWgOperand;
+constexpr uint32_t kWgScales = kWgCodes + kWgSlots * kWgCodeBytes;
+constexpr uint32_t kWgBars = kWgScales + kWgSlots * kWgScaleBytes;
+constexpr uint32_t kWgSmem = kWgBars + 512 + 2 * kWgTile * 4 + 1024;
 constexpr int kWgPairs = 74;             // pairs of blocks that the chip holds at a time
 constexpr int kWgMinSteps = 4;           // of a part
 
 struct WgArgs {
     const __nv_bfloat16* dy;
     uint64_t rows, n, lddy;
-    const uint8_t *codes, *scales;
-    uint64_t k, pitch;
+    uint64_t k;
+    const uint32_t* scales;              // [columns of 128][token_pitch]: four scale bytes each
+    uint64_t token_pitch;
     const void *gamma, *beta;
     int param_dtype;
     void* dw;
@@ -175,26 +183,6 @@ struct WgRing {
     }
 };
 
-// what a decoder thread holds of one step: 16 codes of each of four tokens
-struct WgCodes {
-    uint4 c[4];
-    uint32_t scale[4];
-};
-
-__device__ __forceinline__ void wg_load_codes(const WgArgs& a, uint64_t t, uint64_t col, WgCodes& r) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint64_t row = t + 16 * i;
-        r.c[i] = make_uint4(0u, 0u, 0u, 0u);
-        r.scale[i] = 127u;
-        if (row < a.rows && col < a.pitch) {
-            const uint64_t at = row * a.pitch + col;
-            r.c[i] = __ldg(reinterpret_cast<const uint4*>(a.codes + at));
-            r.scale[i] = __ldg(a.scales + (at >> 5));
-        }
-    }
-}
-
 // sixteen codes -> the two 16-byte chunks at `first` and `second`, of the words' first and second
 // half
 __device__ __forceinline__ void wg_decode(const uint32_t (&w)[4], uint32_t scale, uint32_t first,
@@ -272,24 +260,32 @@ __device__ __forceinline__ void wg_store4(const WgArgs& a, uint64_t n, uint64_t 
     }
 }
 
+// waits until step number `step` of the pair is done
+__device__ __forceinline__ bool wg_wait_step(uint32_t empty, uint32_t step,
+                                             volatile uint32_t* gave_up) {
+    return mbar_wait(empty + 8 * (step % kWgStages), (step / kWgStages) & 1, gave_up);
+}
+
 template <bool COPY>
 __global__ void __cluster_dims__(2, 1, 1)
 __launch_bounds__(32 * (kWgLoadWarp + (COPY ? 0 : kWgLoaders)), 1)
-wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorMap map) {
+wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorMap map,
+                  const __grid_constant__ CUtensorMap code_map) {
     extern __shared__ uint8_t raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const uint32_t tiles = smem_u32(base);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgTiles);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgBars);
     // Barriers by step (step % stages).  The thread that issues the matrix instructions waits for
     // one of them and commits to one a step: every further wait would leave the tensor cores idle.
     const uint32_t empty = smem_u32(bars);             // operands consumed
     const uint32_t ready = empty + 8 * kWgStages;      // first block's: both blocks' operands are there
     const uint32_t copied = ready + 8 * kWgStages;     // second block's: its dY tiles arrived
-    const uint32_t full = copied + 8 * kWgStages;      // [2] a tile's product is complete
+    const uint32_t coded = copied + 8 * kWgStages;     // the block's codes arrived
+    const uint32_t full = coded + 8 * kWgStages;       // [2] a tile's product is complete
     const uint32_t drained = full + 16;                // [2] first block's: TMEM read out
-    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 3 * kWgStages + 4);
+    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 4 * kWgStages + 4);
     volatile uint32_t* gave_up = words + 1;
-    float* affine = reinterpret_cast<float*>(base + kWgTiles + 512);
+    float* affine = reinterpret_cast<float*>(base + kWgBars + 512);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1;
@@ -301,6 +297,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             mbar_init(empty + 8 * s, 1);
             mbar_init(ready + 8 * s, 2 * (kWgGroupWarps + (COPY ? 1 : kWgLoaders)));
             mbar_init(copied + 8 * s, 1);
+            mbar_init(coded + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(full + 8 * b, 1);
@@ -314,40 +311,36 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     const uint32_t tmem = words[0];
 
     if (warp >= kWgDecodeWarp && warp < kWgLoadWarp) {
-        // ---- decode.  Eight lanes read the 128 codes of a token, a whole line of memory.  Four of
-        // them write the even chunks of a line of the first panel while the other four write the
-        // odd chunks of the same line of the second, so no bank is hit twice.
+        // ---- decode.  Eight lanes read the 128 codes of a token.  Four of them write the even
+        // chunks of a line of the first panel while the other four write the odd chunks of the same
+        // line of the second, so no bank is hit twice.
         const uint32_t group = (warp - kWgDecodeWarp) / kWgGroupWarps;
         const uint32_t i0 = (threadIdx.x - 32 * kWgDecodeWarp) & (32 * kWgGroupWarps - 1);
         const uint32_t token = i0 >> 3, eighth = i0 & 7;
-        const uint64_t column = rank * kWgHalf + 16 * eighth;
         const bool odd = eighth >= 4;
         const uint32_t place = kWgDecoded + (odd ? kWgPanel : 0u) + token * 128;
         const uint32_t chunk = (2 * (eighth & 3) + odd) ^ (token & 7);
-        WgWalk walk;
-        walk.begin(a, pair);
-        walk.advance(a, pair, group);
-        WgRing ring = {group, 1};
-        WgCodes r;
-        if (walk.more()) wg_load_codes(a, walk.token() + token, walk.unit.k0 + column, r);
-        while (walk.more()) {
-            walk.advance(a, pair, kWgGroups);
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
-                break;
-            const uint32_t line = tiles + ring.stage * kWgOperand + place;
+        uint32_t total = 0, u = 0;
+        for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) total += w.steps;
+        for (uint32_t step = group; step < total; step += kWgGroups) {
+            const uint32_t stage = step % kWgStages, slot = step % kWgSlots;
+            bool ok = step < kWgSlots || wg_wait_step(empty, step - kWgSlots, gave_up);
+            ok = ok && mbar_wait(coded + 8 * stage, (step / kWgStages) & 1, gave_up);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            const uint32_t line = tiles + slot * kWgOperand + place;
+            const uint8_t* from = base + kWgCodes + slot * kWgCodeBytes + token * 128 + eighth * 16;
+            const uint8_t* scale = base + kWgScales + slot * kWgScaleBytes + token * 4 + (eighth >> 1);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint4 c = r.c[i];
+                const uint4 c = *reinterpret_cast<const uint4*>(from + i * (16 * 128));
                 const uint32_t w[4] = {odd ? c.z : c.x, odd ? c.w : c.y, odd ? c.x : c.z,
                                        odd ? c.y : c.w};
                 const uint32_t at = line + i * (16 * 128);
-                wg_decode(w, r.scale[i], at + (chunk << 4), at + ((chunk ^ 1) << 4));
+                wg_decode(w, scale[i * 64], at + (chunk << 4), at + ((chunk ^ 1) << 4));
             }
-            if (walk.more()) wg_load_codes(a, walk.token() + token, walk.unit.k0 + column, r);
             fence_async_proxy();
             __syncwarp();
-            if (lane == 0) mbar_arrive_at(ready + 8 * ring.stage, 0);
-            ring.advance(kWgGroups);
+            if (lane == 0) mbar_arrive_at(ready + 8 * stage, 0);
         }
     } else if (warp < kWgWriters) {
         // ---- write a tile out: lane = row
@@ -428,9 +421,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                             before = last[s];
                             last[s] = step + 1;
                         }
-                    if (before)
-                        ok = mbar_wait(empty + 8 * ((before - 1) % kWgStages),
-                                       ((before - 1) / kWgStages) & 1, gave_up);
+                    if (before) ok = wg_wait_step(empty, before - 1, gave_up);
                     if (!ok) break;
                     if (h == 0) mbar_expect(bar, walk.unit.halves * kWgOperand);
                     for (int p = 0; p < 2; ++p)
@@ -446,13 +437,34 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                 while (!mbar_try(arrived + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
                        clock64() - begin < 4000000000ll) {}
         }
+    } else if (warp == kWgCodeWarp) {
+        // ---- copies of the codes and of their scales
+        if (lane == 0) {
+            WgWalk walk;
+            uint32_t step = 0;
+            for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1), ++step) {
+                const uint32_t slot = step % kWgSlots, bar = coded + 8 * (step % kWgStages);
+                if (step >= kWgSlots && !wg_wait_step(empty, step - kWgSlots, gave_up)) break;
+                const uint64_t column = walk.unit.k0 + rank * kWgHalf;
+                mbar_expect(bar, kWgCodeBytes + kWgScaleBytes);
+                tma_load_2d(tiles + kWgCodes + slot * kWgCodeBytes, &code_map, (int)column,
+                            (int)walk.token(), bar);
+                bulk_load(tiles + kWgScales + slot * kWgScaleBytes,
+                          a.scales + (column / 128) * a.token_pitch + walk.token(), kWgScaleBytes,
+                          bar);
+            }
+            const long long begin = clock64();
+            for (uint32_t i = step < kWgStages ? 0 : step - kWgStages; i < step; ++i)
+                while (!mbar_try(coded + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
+                       clock64() - begin < 4000000000ll) {}
+        }
     } else if (warp == kWgMmaWarp) {
         if (lane == 0 && rank == 0) {
             // ---- matrix instructions
             const uint32_t shape = mma_shape(kWgTile, kWgTile);
             WgRing ring = {0, 0};
             bool ok = true, here = false;            // here: the next step was seen to be ready
-            uint32_t u = 0, place = 0;
+            uint32_t u = 0, place = 0, slot = 0;
             WgTurns turns;
             for (WgUnit w = wg_unit(a, pair, 0); w.steps && ok; w = wg_unit(a, pair, ++u)) {
                 for (uint32_t h = 0; h < w.halves && ok; ++h) {
@@ -464,7 +476,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                     if (!here) ok = mbar_wait(ready + 8 * ring.stage, ring.parity, gave_up);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t decoded = tiles + kWgDecoded + ring.stage * kWgOperand;
+                    const uint32_t decoded = tiles + kWgDecoded + slot * kWgOperand;
+                    slot = slot + 1 == kWgSlots ? 0 : slot + 1;
                     const uint32_t empty_bar = empty + 8 * ring.stage;
                     ring.advance(1);
 #pragma unroll
@@ -496,7 +509,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                 ring.advance(1);
             }
         }
-    } else if (!COPY) {
+    } else if (!COPY && warp >= kWgLoadWarp) {
         // ---- plain loads of the dY tile, a step ahead: 16 lanes cover the 128 n of a token
         const int i0 = threadIdx.x - 32 * kWgLoadWarp;
         const uint32_t chunk = i0 & 15, token0 = i0 >> 4;          // tokens token0 + 8 j
@@ -568,19 +581,62 @@ __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ Wg
     wg_store4(a, n, k, v);
 }
 
+// ---- scale bytes by columns of 128: word [c][t] holds the four bytes of token t and of the columns
+// from 128 c on; those beyond the checkpoint are a unit of 1.  A block moves 64 tokens x 32 words.
+struct WgScales {
+    const uint8_t* in;
+    uint64_t rows, row_bytes;            // of the checkpoint
+    uint32_t* out;
+    uint64_t token_pitch, columns;       // of 128, even
+    uint32_t across;                     // pieces of 32 columns
+    uint64_t pieces;                     // of 64 tokens x 32 columns
+};
+
+// blocks from row `first` of the grid on take the pieces in turn
+__device__ __forceinline__ void wg_lay_scales(const WgScales& g, int first) {
+    __shared__ uint32_t words[32][65];
+    for (uint64_t piece = (uint64_t)(blockIdx.y - first) * gridDim.x + blockIdx.x; piece < g.pieces;
+         piece += (uint64_t)(gridDim.y - first) * gridDim.x) {
+        const uint64_t t0 = piece / g.across * 64, c0 = piece % g.across * 32;
+        for (int i = threadIdx.x; i < 64 * 32; i += 256) {
+            const uint64_t t = t0 + i / 32, c = c0 + i % 32;
+            uint32_t w = 0x7F7F7F7Fu;
+            if (t < g.rows) {
+    #pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (4 * c + b < g.row_bytes)
+                        w = (w & ~(0xFFu << (8 * b))) |
+                            (uint32_t)__ldg(g.in + t * g.row_bytes + 4 * c + b) << (8 * b);
+            }
+            words[i % 32][i / 32] = w;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 64 * 32; i += 256) {
+            const uint64_t t = t0 + i % 64, c = c0 + i / 64;
+            if (c < g.columns) g.out[c * g.token_pitch + t] = words[i / 64][i % 64];
+        }
+        __syncthreads();
+    }
+}
+
 // ---- column sums of dY: a block adds up a range of rows, a thread eight columns, or one where the
-// rows are not on 16-byte boundaries
+// rows are not on 16-byte boundaries.  Blocks beyond the last range lay out the scales.
 constexpr int kWgSumBlocks = 256;        // ranges at most
 
 template <bool VECTOR>
 __global__ void __launch_bounds__(256)
 wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
-               const uint64_t lddy, float* __restrict__ parts) {
+               const uint64_t lddy, float* __restrict__ parts, const int ranges,
+               const __grid_constant__ WgScales scales) {
+    if ((int)blockIdx.y >= ranges) {
+        wg_lay_scales(scales, ranges);
+        return;
+    }
     constexpr int W = VECTOR ? 8 : 1;
     __shared__ float sums[8][32 * W + 1];
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const uint64_t col = ((uint64_t)blockIdx.x * 32 + lane) * W;
-    const uint64_t begin = rows * blockIdx.y / gridDim.y, end = rows * (blockIdx.y + 1) / gridDim.y;
+    const uint64_t begin = rows * blockIdx.y / ranges, end = rows * (blockIdx.y + 1) / ranges;
     float s[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) s[i] = 0.0f;
@@ -623,12 +679,17 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
 __global__ void __launch_bounds__(256)
 wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
                 const uint64_t lddy, __nv_bfloat16* __restrict__ copy, const uint64_t ldc,
-                float* __restrict__ parts) {
+                float* __restrict__ parts, const int ranges,
+                const __grid_constant__ WgScales scales) {
+    if ((int)blockIdx.y >= ranges) {
+        wg_lay_scales(scales, ranges);
+        return;
+    }
     __shared__ float sums[512];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint64_t first = (uint64_t)blockIdx.x * 512;
     const uint32_t cols = (uint32_t)min(n - first, (uint64_t)512);
-    const uint64_t begin = rows * blockIdx.y / gridDim.y, end = rows * (blockIdx.y + 1) / gridDim.y;
+    const uint64_t begin = rows * blockIdx.y / ranges, end = rows * (blockIdx.y + 1) / ranges;
     float s[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
@@ -658,16 +719,28 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
     for (uint32_t c = threadIdx.x; c < cols; c += 256) parts[blockIdx.y * n + first + c] = sums[c];
 }
 
-// db <- [db +] the parts' sum; `fresh` (may be db) gets the sum alone
+// db <- [db +] the parts' sum, in the order of the parts within each of 8 interleaved groups, then of
+// the groups; `fresh`, where wanted, gets the sum alone
 __global__ void __launch_bounds__(256)
 wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uint64_t n,
                     float* fresh, float* db, const bool accumulate) {
-    const uint64_t col = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= n) return;
+    __shared__ float sums[8][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const uint64_t col = (uint64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    for (int b = 0; b < blocks; ++b) s += parts[b * n + col];
-    if (fresh) fresh[col] = s;
-    if (db) db[col] = accumulate ? db[col] + s : s;
+    if (col < n) {
+#pragma unroll 8
+        for (int b = group; b < blocks; b += 8) s += __ldg(parts + b * n + col);
+    }
+    sums[group][lane] = s;
+    __syncthreads();
+    if (group == 0 && col < n) {
+        s = sums[0][lane];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s += sums[k][lane];
+        if (fresh) fresh[col] = s;
+        if (db) db[col] = accumulate ? db[col] + s : s;
+    }
 }
 
 struct WgPlan {
@@ -675,7 +748,8 @@ struct WgPlan {
     uint32_t splits;
     int sum_blocks;
     uint64_t ldc;                        // row stride of the aligned copy of dY
-    size_t sum_offset, fresh_offset, copy_offset, bytes;
+    uint64_t token_pitch;                // tokens of a column of laid out scales
+    size_t sum_offset, fresh_offset, scale_offset, copy_offset, bytes;
 };
 
 // `doubles`: double tiles may be used
@@ -698,7 +772,9 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
     p.sum_offset = p.splits > 1 ? left * p.splits * kWgTile * kWgTile * 4 : 0;
     p.fresh_offset = p.sum_offset + round_up16(p.sum_blocks * n * 4);
-    p.copy_offset = p.fresh_offset + round_up16(n * 4);
+    p.scale_offset = p.fresh_offset + round_up16(n * 4);
+    p.token_pitch = steps * kWgStep;
+    p.copy_offset = p.scale_offset + 2 * p.tiles_k * p.token_pitch * 4;
     p.ldc = (n + 7) / 8 * 8;
     // a copy is made where the width itself keeps rows off the boundaries
     p.bytes = p.copy_offset + (n % 8 ? rows * p.ldc * 2 : 0);
@@ -744,31 +820,45 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     char* ws = static_cast<char*>(workspace);
     float* fresh = reinterpret_cast<float*>(ws + p.fresh_offset);
     const bool with_beta = beta && k && rows;
-    if (db || with_beta || copied) {
-        float* sums = reinterpret_cast<float*>(ws + p.sum_offset);
+    float* sums = reinterpret_cast<float*>(ws + p.sum_offset);
+    WgScales g = {};
+    g.in = scales;
+    g.rows = rows;
+    g.row_bytes = act8_pitch(k) / 32;
+    g.out = reinterpret_cast<uint32_t*>(ws + p.scale_offset);
+    g.token_pitch = k ? p.token_pitch : 0;
+    g.columns = 2 * p.tiles_k;
+    g.across = (uint32_t)((g.columns + 31) / 32);
+    g.pieces = g.token_pitch / 64 * g.across;
+    const int ranges = db || with_beta || copied ? p.sum_blocks : 0;
+    if (rows) {
         const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(dy);
+        const bool vector = aligned && n % 8 == 0;
+        const uint64_t across = (n + (copied ? 511 : vector ? 255 : 31)) /
+                                (copied ? 512 : vector ? 256 : 32);
+        const uint64_t lay = (g.pieces + across - 1) / across;       // rows of blocks for them
+        const unsigned down = ranges + (unsigned)(lay < 4096 ? lay : 4096);
+        const dim3 grid((unsigned)across, down);
         if (copied) {
             __nv_bfloat16* copy = reinterpret_cast<__nv_bfloat16*>(ws + p.copy_offset);
-            wg_align_kernel<<<dim3((unsigned)((n + 511) / 512), p.sum_blocks), 256, 0, stream>>>(
-                in, rows, n, lddy, copy, p.ldc, sums);
+            wg_align_kernel<<<grid, 256, 0, stream>>>(in, rows, n, lddy, copy, p.ldc, sums, ranges,
+                                                      g);
             dy = copy;
             lddy = p.ldc;
-        } else if (rows) {
-            const bool vector = aligned && n % 8 == 0;
+        } else if (down) {
             auto kernel = vector ? wg_sums_kernel<true> : wg_sums_kernel<false>;
-            kernel<<<dim3((unsigned)((n + (vector ? 255 : 31)) / (vector ? 256 : 32)),
-                          p.sum_blocks), 256, 0, stream>>>(in, rows, n, lddy, sums);
+            kernel<<<grid, 256, 0, stream>>>(in, rows, n, lddy, sums, ranges, g);
         }
-        if (db || with_beta)
-            wg_sums_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(
-                sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
     }
+    if (db || with_beta)
+        wg_sums_join_kernel<<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(
+            sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
     if (k == 0) return launch_status();
 
     WgArgs a = {};
     a.dy = static_cast<const __nv_bfloat16*>(dy);
-    a.rows = rows; a.n = n; a.lddy = lddy; a.codes = codes; a.scales = scales; a.k = k;
-    a.pitch = act8_pitch(k); a.gamma = gamma; a.beta = with_beta ? beta : nullptr;
+    a.rows = rows; a.n = n; a.lddy = lddy; a.k = k; a.scales = g.out;
+    a.token_pitch = p.token_pitch; a.gamma = gamma; a.beta = with_beta ? beta : nullptr;
     a.param_dtype = param_dtype; a.dw = dw; a.dw_f32 = dw_dtype == NC_DTYPE_F32; a.lddw = lddw;
     a.db = fresh; a.accumulate = accumulate;
     a.vector = row_access(dw, lddw, wbytes, n) != kRowElement;
@@ -781,15 +871,18 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     a.parts = reinterpret_cast<float*>(ws);
     if (rows) {
         const bool copy = aligned || copied;             // by tensor copies
-        CUtensorMap map = {};
-        if (copy && !make_tensor_map(&map, dy, rows, n, rows > 1 ? lddy : p.ldc, 64, kWgStep))
+        CUtensorMap map = {}, code_map = {};
+        if (copy && !make_tensor_map(&map, dy, true, rows, n, rows > 1 ? lddy : p.ldc, 64, kWgStep))
+            return NC_ERR_CUDA;
+        if (!make_tensor_map(&code_map, codes, false, rows, act8_pitch(k), act8_pitch(k), 128,
+                             kWgStep))
             return NC_ERR_CUDA;
         auto kernel = copy ? wg_product_kernel<true> : wg_product_kernel<false>;
         static bool allowed[2][64];
         if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[copy])) return NC_ERR_CUDA;
         const uint64_t pairs = p.whole || p.rounds ? kWgPairs : (p.tiles - p.whole) * p.splits;
         kernel<<<(unsigned)(2 * pairs), 32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders)), kWgSmem,
-                 stream>>>(a, map);
+                 stream>>>(a, map, code_map);
     }
     if (a.splits != 1 && a.whole < a.tiles)
         wg_join_kernel<<<(a.tiles - a.whole) * 64, 256, 0, stream>>>(a);
