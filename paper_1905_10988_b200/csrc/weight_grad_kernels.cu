@@ -183,28 +183,25 @@ struct WgRing {
     }
 };
 
-// sixteen codes -> the two 16-byte chunks at `first` and `second`, of the words' first and second
-// half
-__device__ __forceinline__ void wg_decode(const uint32_t (&w)[4], uint32_t scale, uint32_t first,
-                                          uint32_t second) {
-    uint32_t v[8];
-    if (scale <= kAct8MaxFast) {
-        const uint32_t fields = act8_fields(scale);
+// sixteen codes -> eight pairs of bfloat16; FAST: the scale byte is at most kAct8MaxFast
+template <bool FAST>
+__device__ __forceinline__ void wg_decode(const uint32_t (&w)[4], uint32_t scale, uint32_t (&v)[8]) {
+    const uint32_t fields = act8_fields(scale);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act8_pair_bf16(w[i >> 1], i & 1, fields);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {
+        if (FAST) {
+            v[i] = act8_pair_bf16(w[i >> 1], i & 1, fields);
+        } else {
             const uint32_t two = w[i >> 1] >> (16 * (i & 1));
             v[i] = pack2<__nv_bfloat16>(act8_value(two & 0xFFu, scale),
                                         act8_value((two >> 8) & 0xFFu, scale));
         }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(h ? second : first),
-                     "r"(v[4 * h]), "r"(v[4 * h + 1]), "r"(v[4 * h + 2]), "r"(v[4 * h + 3])
-                     : "memory");
+}
+
+__device__ __forceinline__ void wg_put(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
 }
 
 // eight values of a dY row at any element
@@ -260,10 +257,10 @@ __device__ __forceinline__ void wg_store4(const WgArgs& a, uint64_t n, uint64_t 
     }
 }
 
-// waits until step number `step` of the pair is done
-__device__ __forceinline__ bool wg_wait_step(uint32_t empty, uint32_t step,
+// waits until the barrier of step number `step` among `bars` is over
+__device__ __forceinline__ bool wg_wait_step(uint32_t bars, uint32_t step,
                                              volatile uint32_t* gave_up) {
-    return mbar_wait(empty + 8 * (step % kWgStages), (step / kWgStages) & 1, gave_up);
+    return mbar_wait(bars + 8 * (step % kWgStages), (step / kWgStages) & 1, gave_up);
 }
 
 template <bool COPY>
@@ -281,9 +278,10 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     const uint32_t ready = empty + 8 * kWgStages;      // first block's: both blocks' operands are there
     const uint32_t copied = ready + 8 * kWgStages;     // second block's: its dY tiles arrived
     const uint32_t coded = copied + 8 * kWgStages;     // the block's codes arrived
-    const uint32_t full = coded + 8 * kWgStages;       // [2] a tile's product is complete
+    const uint32_t taken = coded + 8 * kWgStages;      // they were read
+    const uint32_t full = taken + 8 * kWgStages;       // [2] a tile's product is complete
     const uint32_t drained = full + 16;                // [2] first block's: TMEM read out
-    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 4 * kWgStages + 4);
+    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 5 * kWgStages + 4);
     volatile uint32_t* gave_up = words + 1;
     float* affine = reinterpret_cast<float*>(base + kWgBars + 512);
 
@@ -298,6 +296,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             mbar_init(ready + 8 * s, 2 * (kWgGroupWarps + (COPY ? 1 : kWgLoaders)));
             mbar_init(copied + 8 * s, 1);
             mbar_init(coded + 8 * s, 1);
+            mbar_init(taken + 8 * s, kWgGroupWarps);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(full + 8 * b, 1);
@@ -324,19 +323,39 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) total += w.steps;
         for (uint32_t step = group; step < total; step += kWgGroups) {
             const uint32_t stage = step % kWgStages, slot = step % kWgSlots;
-            bool ok = step < kWgSlots || wg_wait_step(empty, step - kWgSlots, gave_up);
-            ok = ok && mbar_wait(coded + 8 * stage, (step / kWgStages) & 1, gave_up);
+            bool ok = mbar_wait(coded + 8 * stage, (step / kWgStages) & 1, gave_up);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
-            const uint32_t line = tiles + slot * kWgOperand + place;
             const uint8_t* from = base + kWgCodes + slot * kWgCodeBytes + token * 128 + eighth * 16;
-            const uint8_t* scale = base + kWgScales + slot * kWgScaleBytes + token * 4 + (eighth >> 1);
+            const uint8_t* scales = base + kWgScales + slot * kWgScaleBytes + token * 4 + (eighth >> 1);
+            uint32_t w[4][4], scale[4], most = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint4 c = *reinterpret_cast<const uint4*>(from + i * (16 * 128));
-                const uint32_t w[4] = {odd ? c.z : c.x, odd ? c.w : c.y, odd ? c.x : c.z,
-                                       odd ? c.y : c.w};
+                w[i][0] = odd ? c.z : c.x;
+                w[i][1] = odd ? c.w : c.y;
+                w[i][2] = odd ? c.x : c.z;
+                w[i][3] = odd ? c.y : c.w;
+                scale[i] = scales[i * 64];
+                most = max(most, scale[i]);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken + 8 * stage);
+            uint32_t v[4][8];
+            if (most <= kAct8MaxFast) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wg_decode<true>(w[i], scale[i], v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wg_decode<false>(w[i], scale[i], v[i]);
+            }
+            ok = step < kWgSlots || wg_wait_step(empty, step - kWgSlots, gave_up);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            const uint32_t line = tiles + slot * kWgOperand + place;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
                 const uint32_t at = line + i * (16 * 128);
-                wg_decode(w, scale[i * 64], at + (chunk << 4), at + ((chunk ^ 1) << 4));
+                wg_put(at + (chunk << 4), v[i][0], v[i][1], v[i][2], v[i][3]);
+                wg_put(at + ((chunk ^ 1) << 4), v[i][4], v[i][5], v[i][6], v[i][7]);
             }
             fence_async_proxy();
             __syncwarp();
@@ -444,7 +463,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             uint32_t step = 0;
             for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1), ++step) {
                 const uint32_t slot = step % kWgSlots, bar = coded + 8 * (step % kWgStages);
-                if (step >= kWgSlots && !wg_wait_step(empty, step - kWgSlots, gave_up)) break;
+                if (step >= kWgSlots && !wg_wait_step(taken, step - kWgSlots, gave_up)) break;
                 const uint64_t column = walk.unit.k0 + rank * kWgHalf;
                 mbar_expect(bar, kWgCodeBytes + kWgScaleBytes);
                 tma_load_2d(tiles + kWgCodes + slot * kWgCodeBytes, &code_map, (int)column,
@@ -491,7 +510,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                                      mma_operand(decoded + 2048 * i, kWgPanel), shape,
                                      s > 0 || i > 0);
                             if (i == 1 && h + 1 == (int)w.halves)
-                                here = mbar_try(ready + 8 * ring.stage, ring.parity);
+                                here = mbar_test(ready + 8 * ring.stage, ring.parity);
                         }
                     }
                     mma_commit_pair(empty_bar);
