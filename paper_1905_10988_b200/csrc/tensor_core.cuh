@@ -13,12 +13,6 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return (uint32_t)__cvta_generic_to_shared(p);
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
                  "barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -191,21 +185,41 @@ __host__ __device__ constexpr uint32_t mma_shape(uint32_t m, uint32_t n) {
            ((m >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_pair(uint32_t tmem, uint64_t a, uint64_t b, uint32_t shape,
-                                         bool add) {
+// One thread of a warp issues.  All of its lanes come here, with the same operands, so that these
+// stay in uniform registers: with a branch around the instruction its operands were moved there one
+// by one, and issuing took longer than the tensor cores did.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
     asm volatile("{\n\t"
                  ".reg .pred p;\n\t"
+                 "elect.sync _|p, 0xFFFFFFFF;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t"
+                 "}"
+                 : "=r"(one));
+    return one != 0;
+}
+
+__device__ __forceinline__ void mma_pair(uint32_t tmem, uint64_t a, uint64_t b, uint32_t shape,
+                                         bool add, bool elected) {
+    asm volatile("{\n\t"
+                 ".reg .pred p, q;\n\t"
                  "setp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
-                 "}" ::"r"(tmem), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+                 "setp.ne.u32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+                 "}" ::"r"(tmem), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add),
+                 "r"((uint32_t)elected)
                  : "memory");
 }
 
 // the barrier at this place in both blocks of the pair is arrived at once when the matrix
 // instructions issued so far are done
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster"
-                 ".multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar, bool elected) {
+    asm volatile("{\n\t"
+                 ".reg .pred q;\n\t"
+                 "setp.ne.u32 q, %2, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster"
+                 ".multicast::cluster.b64 [%0], %1;\n\t"
+                 "}" ::"r"(bar), "h"((uint16_t)3), "r"((uint32_t)elected)
                  : "memory");
 }
 

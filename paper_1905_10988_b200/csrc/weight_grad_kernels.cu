@@ -285,8 +285,9 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     volatile uint32_t* gave_up = words + 1;
     float* affine = reinterpret_cast<float*>(base + kWgBars + 512);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank(), pair = blockIdx.x >> 1;
+    // (the shuffle tells the compiler that a warp has one number)
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1;     // of the cluster of two
 
     if (warp == kWgMmaWarp) tmem_alloc_pair(smem_u32(words), 2 * kWgTile);
     if (threadIdx.x == 0) {
@@ -307,7 +308,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     tc_fence_before();
     cluster_sync();
     tc_fence_after();
-    const uint32_t tmem = words[0];
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, words[0], 0);
 
     if (warp >= kWgDecodeWarp && warp < kWgLoadWarp) {
         // ---- decode.  Eight lanes read the 128 codes of a token.  Four of them write the even
@@ -478,44 +479,50 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                        clock64() - begin < 4000000000ll) {}
         }
     } else if (warp == kWgMmaWarp) {
-        if (lane == 0 && rank == 0) {
-            // ---- matrix instructions
+        if (rank == 0) {
+            // ---- matrix instructions: the whole warp, of which one thread issues
             const uint32_t shape = mma_shape(kWgTile, kWgTile);
-            WgRing ring = {0, 0};
+            const bool elected = elect_one();
+            const uint64_t operand = mma_operand(tiles, kWgPanel);   // + bytes / 16: further on
             bool ok = true, here = false;            // here: the next step was seen to be ready
-            uint32_t u = 0, place = 0, slot = 0;
+            uint32_t u = 0, place = 0, slot = 0, stage = 0, parity = 0;
             WgTurns turns;
             for (WgUnit w = wg_unit(a, pair, 0); w.steps && ok; w = wg_unit(a, pair, ++u)) {
                 for (uint32_t h = 0; h < w.halves && ok; ++h) {
                     const uint32_t b = turns.of(w, h);
                     ok = mbar_wait(drained + 8 * b, turns.parity(b) ^ 1, gave_up);
                 }
-                const uint32_t to[2] = {tmem + turns.of(w, 0) * kWgTile, tmem + kWgTile};
+                const uint32_t to = tmem + turns.of(w, 0) * kWgTile;
+                const bool twice = w.halves == 2;
                 for (uint32_t s = 0; s < w.steps && ok; ++s) {
-                    if (!here) ok = mbar_wait(ready + 8 * ring.stage, ring.parity, gave_up);
+                    if (!here) ok = mbar_wait(ready + 8 * stage, parity, gave_up);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t decoded = tiles + kWgDecoded + slot * kWgOperand;
+                    const uint64_t right = operand + (kWgDecoded + slot * kWgOperand) / 16;
                     slot = slot + 1 == kWgSlots ? 0 : slot + 1;
-                    const uint32_t empty_bar = empty + 8 * ring.stage;
-                    ring.advance(1);
+                    const uint32_t done = empty + 8 * stage;
+                    stage = stage + 1 == kWgStages ? 0 : stage + 1;
+                    parity ^= stage == 0;
+                    uint64_t left = operand + place * (kWgOperand / 16);
+                    place = place + 1 == kWgStages ? 0 : place + 1;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (h == 1 && w.halves == 1) break;
-                        const uint32_t at = tiles + place * kWgOperand;
+                    for (int i = 0; i < kWgStep / 16; ++i)   // 16 tokens: two groups of lines
+                        mma_pair(to, left + 128 * i, right + 128 * i, shape, s > 0 || i > 0,
+                                 elected);
+                    if (twice) {
+                        left = operand + place * (kWgOperand / 16);
                         place = place + 1 == kWgStages ? 0 : place + 1;
 #pragma unroll
-                        for (int i = 0; i < kWgStep / 16; ++i) {  // 16 tokens: two groups of lines
-                            mma_pair(to[h], mma_operand(at + 2048 * i, kWgPanel),
-                                     mma_operand(decoded + 2048 * i, kWgPanel), shape,
-                                     s > 0 || i > 0);
-                            if (i == 1 && h + 1 == (int)w.halves)
-                                here = mbar_test(ready + 8 * ring.stage, ring.parity);
-                        }
+                        for (int i = 0; i < kWgStep / 16; ++i)
+                            mma_pair(to + kWgTile, left + 128 * i, right + 128 * i, shape,
+                                     s > 0 || i > 0, elected);
                     }
-                    mma_commit_pair(empty_bar);
+                    mma_commit_pair(done, elected);
+                    here = __all_sync(0xFFFFFFFFu, mbar_test(ready + 8 * stage, parity));
                 }
-                for (uint32_t h = 0; h < w.halves; ++h) mma_commit_pair(full + 8 * turns.of(w, h));
+                for (uint32_t h = 0; h < w.halves; ++h)
+                    mma_commit_pair(full + 8 * turns.of(w, h), elected);
                 turns.done(w);
             }
         } else if (COPY && lane == 0) {
