@@ -67,6 +67,33 @@ inline bool allow_dynamic_smem(const void* kernel, int bytes, bool (&allowed)[64
     return true;
 }
 
+// Launches `kernel` so that it may begin while the kernel before it in the stream ends
+// (programmatic dependent launch).  It must call after_previous() before it touches what that kernel
+// or any earlier one wrote or reads, and the kernel before it may call let_next_begin() early.
+template <typename Kernel, typename... Args>
+inline cudaError_t launch_overlapping(Kernel kernel, dim3 grid, dim3 block, size_t smem,
+                                      cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+__device__ __forceinline__ void after_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+__device__ __forceinline__ void let_next_begin() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 inline nc_status launch_status() {
     return cudaPeekAtLastError() == cudaSuccess ? NC_OK : NC_ERR_CUDA;
 }

@@ -659,6 +659,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         row_store<T, MODE>(dx + row * a.lddx, p.G, p.tid, p.cols, a.wide, out);
     }
 
+    let_next_begin();
     float dg[16], db[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -727,13 +728,14 @@ ln_parts_kernel(const float* __restrict__ parts, const int blocks, const uint32_
                 const uint32_t cols, float* __restrict__ dgamma, float* __restrict__ dbeta,
                 const bool accumulate) {
     __shared__ float sums[8][33];
+    after_previous();
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const uint32_t col = blockIdx.x * 32 + lane;
     const float* p = parts + (blockIdx.y ? pitch : 0) + col;
     float s = 0.0f;
     if (col < cols) {
 #pragma unroll 8
-        for (int b = group; b < blocks; b += 8) s += __ldg(p + (uint64_t)b * 2 * pitch);
+        for (int b = group; b < blocks; b += 8) s += __ldcg(p + (uint64_t)b * 2 * pitch);
     }
     sums[group][lane] = s;
     __syncthreads();
@@ -780,9 +782,11 @@ static nc_status ln_backward_launch(const LnBackward& a, int access, float* dgam
         const nc_status st = go(a, access, &blocks, stream);
         if (st != NC_OK) return st;
     }
-    ln_parts_kernel<<<dim3((a.cols + 31) / 32, 2), 256, 0, stream>>>(
-        a.parts, (int)blocks, a.parts_pitch, a.cols, dgamma, dbeta, accumulate);
-    return launch_status();
+    return launch_overlapping(ln_parts_kernel, dim3((a.cols + 31) / 32, 2), dim3(256), 0, stream,
+                              (const float*)a.parts, (int)blocks, a.parts_pitch, a.cols, dgamma,
+                              dbeta, accumulate) == cudaSuccess
+               ? NC_OK
+               : NC_ERR_CUDA;
 }
 
 static nc_status ln_backward_call(LnBackward a, int dtype, size_t cols, int param_dtype,

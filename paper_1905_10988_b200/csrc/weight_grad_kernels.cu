@@ -308,6 +308,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     tc_fence_before();
     cluster_sync();
     tc_fence_after();
+    after_previous();
+    let_next_begin();
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, words[0], 0);
 
     if (warp >= kWgDecodeWarp && warp < kWgLoadWarp) {
@@ -582,6 +584,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
 // the tiles that were computed in parts: dw <- [dw +] gamma * (sum of the parts, in order) +
 // beta * db; no parts: the sum over no tokens.  A block takes 4 rows of a tile.
 __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a) {
+    after_previous();
     const uint32_t tile = a.whole + blockIdx.x / 64, row = blockIdx.x % 64 * 4 + (threadIdx.x >> 6);
     const uint32_t column = (threadIdx.x & 63) * 4;
     uint64_t n, k;
@@ -654,6 +657,7 @@ __global__ void __launch_bounds__(256)
 wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
                const uint64_t lddy, float* __restrict__ parts, const int ranges,
                const __grid_constant__ WgScales scales) {
+    let_next_begin();
     if ((int)blockIdx.y >= ranges) {
         wg_lay_scales(scales, ranges);
         return;
@@ -707,6 +711,7 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
                 const uint64_t lddy, __nv_bfloat16* __restrict__ copy, const uint64_t ldc,
                 float* __restrict__ parts, const int ranges,
                 const __grid_constant__ WgScales scales) {
+    let_next_begin();
     if ((int)blockIdx.y >= ranges) {
         wg_lay_scales(scales, ranges);
         return;
@@ -751,12 +756,14 @@ __global__ void __launch_bounds__(256)
 wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uint64_t n,
                     float* fresh, float* db, const bool accumulate) {
     __shared__ float sums[8][33];
+    let_next_begin();
+    after_previous();
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const uint64_t col = (uint64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (col < n) {
 #pragma unroll 8
-        for (int b = group; b < blocks; b += 8) s += __ldg(parts + b * n + col);
+        for (int b = group; b < blocks; b += 8) s += __ldcg(parts + b * n + col);
     }
     sums[group][lane] = s;
     __syncthreads();
@@ -877,8 +884,9 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         }
     }
     if (db || with_beta)
-        wg_sums_join_kernel<<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(
-            sums, rows ? p.sum_blocks : 0, n, with_beta ? fresh : nullptr, db, accumulate != 0);
+        launch_overlapping(wg_sums_join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(256), 0,
+                           stream, (const float*)sums, rows ? p.sum_blocks : 0, (uint64_t)n,
+                           with_beta ? fresh : (float*)nullptr, db, accumulate != 0);
     if (k == 0) return launch_status();
 
     WgArgs a = {};
@@ -907,11 +915,12 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         static bool allowed[2][64];
         if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[copy])) return NC_ERR_CUDA;
         const uint64_t pairs = p.whole || p.rounds ? kWgPairs : (p.tiles - p.whole) * p.splits;
-        kernel<<<(unsigned)(2 * pairs), 32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders)), kWgSmem,
-                 stream>>>(a, map, code_map);
+        launch_overlapping(kernel, dim3((unsigned)(2 * pairs)),
+                           dim3(32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders))), kWgSmem, stream, a,
+                           map, code_map);
     }
     if (a.splits != 1 && a.whole < a.tiles)
-        wg_join_kernel<<<(a.tiles - a.whole) * 64, 256, 0, stream>>>(a);
+        launch_overlapping(wg_join_kernel, dim3((a.tiles - a.whole) * 64), dim3(256), 0, stream, a);
     return launch_status();
 }
 
