@@ -207,24 +207,34 @@ __device__ __forceinline__ void unpack16(const Raw16<T>& r, f32x2 (&v)[8]) {
 }
 
 // ---- a thread's sixteen values of a row ---------------------------------------------------------
-// G threads share a row, 16 values each.  Value i of thread `tid` is column
-//   16 * tid + i                                rows on 16-byte boundaries: vector accesses
-//   kSpread, 4-byte types: i * G + tid          any rows: neighbouring lanes, neighbouring values
-//   kSpread, 2-byte types: 2 * ((i / 2) * G + tid) + i % 2    the same by pairs of values, so that
-//                                               a row on a 4-byte boundary moves a pair at a time
-// kRegular: rows on 32-byte boundaries, and every thread has sixteen values; no branches.
+// Threads share a row, 16 neighbouring values each: thread `tid` has the columns from 16 * tid on.
+//   kRegular  rows on 32-byte boundaries, and every thread has sixteen values: no branches
+//   kVector   rows on 16-byte boundaries: vector accesses
+//   kSpread   rows at any element: neighbouring lanes access neighbouring values (pairs of two-byte
+//             ones), and a warp's 512 values change places in shared memory afterwards or before
 enum RowMode { kRegular = 0, kVector = 1, kSpread = 2 };
 
-template <typename T, int MODE>
-__device__ __forceinline__ uint32_t row_col(int i, int G, int tid) {
-    if (MODE != kSpread) return 16u * tid + i;
-    if (sizeof(T) == 4) return (uint32_t)i * G + tid;
-    return 2u * ((uint32_t)(i >> 1) * G + tid) + (i & 1);
+// the warp's i-th spread access: which of its 512 columns lane `lane` has (2-byte types: the first
+// of a pair)
+template <typename T>
+__device__ __forceinline__ uint32_t spread_col(int i, int lane) {
+    return sizeof(T) == 4 ? 32u * i + lane : 64u * i + 2 * lane;
 }
 
-// values from `cols` on read as 0
+// where that word lies in shared memory: sixteen values of a lane follow each other, and the lanes
+// are four words further apart, so that a lane reads its values by 16 bytes
+template <typename T> constexpr int kSpreadPitch = sizeof(T) == 4 ? 20 : 12;
+template <typename T> constexpr int kSpreadWords = 32 * kSpreadPitch<T>;      // of a warp
+
+template <typename T>
+__device__ __forceinline__ uint32_t spread_place(int i, int lane) {
+    return sizeof(T) == 4 ? (2 * i + (lane >> 4)) * 20 + (lane & 15)
+                          : (4 * i + (lane >> 3)) * 12 + (lane & 7);
+}
+
+// values from `cols` on read as 0; kSpread: still spread, row_arrange() follows
 template <typename T, int MODE>
-__device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int tid, uint32_t cols,
+__device__ __forceinline__ void row_load(const T* __restrict__ row, int tid, uint32_t cols,
                                          bool wide, Raw16<T>& r) {
     if constexpr (MODE == kRegular) {
         r = ld_raw16<T>(row + 16u * tid, true);
@@ -235,56 +245,72 @@ __device__ __forceinline__ void row_load(const T* __restrict__ row, int G, int t
         else
             r = ld_raw16_part<T>(row + col, col < cols ? (int)(cols - col) : 0);
     } else if constexpr (sizeof(T) == 4) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(row);
-        if (row_col<T, kSpread>(15, G, tid) < cols) {
+        const uint32_t first = 16u * (tid & ~31);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + first;
+        const int lane = tid & 31;
+        if (first + 512 <= cols) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r.b[i >> 3].v[i & 7] = __ldg(p + spread_col<T>(i, lane));
+        } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                r.b[i >> 3].v[i & 7] = __ldg(p + row_col<T, kSpread>(i, G, tid));
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, kSpread>(i, G, tid);
-            r.b[i >> 3].v[i & 7] = col < cols ? __ldg(p + col) : 0u;
+                r.b[i >> 3].v[i & 7] =
+                    first + spread_col<T>(i, lane) < cols ? __ldg(p + spread_col<T>(i, lane)) : 0u;
         }
     } else {
-        const unsigned short* p = reinterpret_cast<const unsigned short*>(row);
-        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;     // the same for all lanes
-        if (row_col<T, kSpread>(15, G, tid) < cols) {
-            if (!odd) {
+        const uint32_t first = 16u * (tid & ~31);
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + first;
+        const int lane = tid & 31;
+        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;
+        if (!odd && first + 512 <= cols) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    r.b[0].v[i] = __ldg(
-                        reinterpret_cast<const uint32_t*>(p + row_col<T, kSpread>(2 * i, G, tid)));
-            } else {
-                // two words hold a pair's halves; the row's first and last value have no
-                // neighbour to share a word with
+            for (int i = 0; i < 8; ++i)
+                r.b[0].v[i] = __ldg(reinterpret_cast<const uint32_t*>(p + spread_col<T>(i, lane)));
+        } else if (odd && first + 512 < cols) {
+            // two words hold a pair's halves; the row's first value has no neighbour to share one
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
-                    const uint32_t* q = reinterpret_cast<const uint32_t*>(p + col - 1);
-                    const uint32_t lo = i > 0 || tid > 0 ? __ldg(q) : (uint32_t)__ldg(p) << 16;
-                    const uint32_t hi =
-                        i < 7 || col + 2 < cols ? __ldg(q + 1) : (uint32_t)__ldg(p + col + 1);
-                    r.b[0].v[i] = __funnelshift_r(lo, hi, 16);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t* q =
+                    reinterpret_cast<const uint32_t*>(p + (int)spread_col<T>(i, lane) - 1);
+                const uint32_t lo = i > 0 || tid > 0 ? __ldg(q) : (uint32_t)__ldg(p) << 16;
+                r.b[0].v[i] = __funnelshift_r(lo, __ldg(q + 1), 16);
             }
-            return;
-        }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
-            uint32_t w = 0;
-            if (col < cols) w = __ldg(p + col);
-            if (col + 1 < cols) w |= (uint32_t)__ldg(p + col + 1) << 16;
-            r.b[0].v[i] = w;
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t c = spread_col<T>(i, lane);
+                uint32_t w = 0;
+                if (first + c < cols) w = __ldg(p + c);
+                if (first + c + 1 < cols) w |= (uint32_t)__ldg(p + c + 1) << 16;
+                r.b[0].v[i] = w;
+            }
+        }
+    }
+}
+
+// kSpread: the lanes' words change places; `scratch` is the warp's own, kSpreadWords<T> words on a
+// 16-byte boundary
+template <typename T, int MODE>
+__device__ __forceinline__ void row_arrange(Raw16<T>& r, uint32_t* scratch) {
+    if constexpr (MODE == kSpread) {
+        const int lane = threadIdx.x & 31;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) * 4; ++i)
+            scratch[spread_place<T>(i, lane)] = r.b[i >> 3].v[i & 7];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) {
+            const uint4 q = reinterpret_cast<const uint4*>(scratch + lane * kSpreadPitch<T>)[i];
+            uint32_t* v = r.b[i >> 1].v + 4 * (i & 1);
+            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
         }
     }
 }
 
 template <typename T, int MODE>
-__device__ __forceinline__ void row_store(T* __restrict__ row, int G, int tid, uint32_t cols,
-                                          bool wide, const float (&v)[16]) {
+__device__ __forceinline__ void row_store(T* __restrict__ row, int tid, uint32_t cols, bool wide,
+                                          const float (&v)[16], uint32_t* scratch) {
     if constexpr (MODE == kRegular) {
         st_raw16<T>(row + 16u * tid, pack16<T>(v), true);
     } else if constexpr (MODE == kVector) {
@@ -293,34 +319,44 @@ __device__ __forceinline__ void row_store(T* __restrict__ row, int G, int tid, u
             st_raw16<T>(row + col, pack16<T>(v), wide);
         else if (col < cols)
             st_part16<T>(row + col, v, (int)(cols - col));
-    } else if constexpr (sizeof(T) == 4) {
-        if (row_col<T, kSpread>(15, G, tid) < cols) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) row[row_col<T, kSpread>(i, G, tid)] = v[i];
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, kSpread>(i, G, tid);
-            if (col < cols) row[col] = v[i];
-        }
     } else {
-        unsigned short* p = reinterpret_cast<unsigned short*>(row);
-        const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;
-        const bool whole = row_col<T, kSpread>(15, G, tid) < cols;
-        if (whole && !odd) {
+        const int lane = tid & 31;
+        const uint32_t first = 16u * (tid & ~31);
+        const Raw16<T> r = pack16<T>(v);
+        __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<uint32_t*>(p + row_col<T, kSpread>(2 * i, G, tid)) =
-                    pack2<T>(v[2 * i], v[2 * i + 1]);
-            return;
+        for (int i = 0; i < (int)sizeof(T); ++i) {
+            const uint32_t* w = r.b[i >> 1].v + 4 * (i & 1);
+            reinterpret_cast<uint4*>(scratch + lane * kSpreadPitch<T>)[i] =
+                make_uint4(w[0], w[1], w[2], w[3]);
         }
+        __syncwarp();
+        if constexpr (sizeof(T) == 4) {
+            uint32_t* p = reinterpret_cast<uint32_t*>(row) + first;
+            const bool whole = first + 512 <= cols;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
-            const uint32_t w = pack2<T>(v[2 * i], v[2 * i + 1]);
-            if (whole || col < cols) p[col] = (unsigned short)w;
-            if (whole || col + 1 < cols) p[col + 1] = (unsigned short)(w >> 16);
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t c = spread_col<T>(i, lane), w = scratch[spread_place<T>(i, lane)];
+                if (whole || first + c < cols) p[c] = w;
+            }
+        } else {
+            unsigned short* p = reinterpret_cast<unsigned short*>(row) + first;
+            const bool odd = (reinterpret_cast<uintptr_t>(row) & 2) != 0;
+            const bool whole = first + 512 <= cols;
+            if (whole && !odd) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<uint32_t*>(p + spread_col<T>(i, lane)) =
+                        scratch[spread_place<T>(i, lane)];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t c = spread_col<T>(i, lane);
+                    const uint32_t w = scratch[spread_place<T>(i, lane)];
+                    if (whole || first + c < cols) p[c] = (unsigned short)w;
+                    if (whole || first + c + 1 < cols) p[c + 1] = (unsigned short)(w >> 16);
+                }
+            }
         }
     }
 }
@@ -341,15 +377,9 @@ __device__ __forceinline__ float act8_inverse(uint32_t scale, bool random) {
     return __uint_as_float(((random ? 262u : 254u) - (scale == kAct8Nan ? 128u : scale)) << 23);
 }
 
-// magnitude of one value: adding 2^23 leaves rint(|x| * inverse) in the low bits.  Random
-// rounding keeps eight more bits, adds the draw to them and drops them: up with probability
-// (their value) / 256, so the expectation is |x| rounded to 1/256 unit.
-__device__ __forceinline__ uint32_t act8_one(float x, float inverse, bool random, uint32_t draw) {
-    const uint32_t f = __float_as_uint(fmaf(fabsf(x), inverse, 8388608.0f));
-    const uint32_t m = random ? ((f & 0xFFFFu) + draw) >> 8 : f & 0x7Fu;
-    return m | ((__float_as_uint(x) >> 24) & 0x80u);
-}
-
+// Magnitudes: adding 2^23 leaves rint(|x| * inverse) in the low bits.  Random rounding keeps eight
+// more bits, adds the draw to them and drops them: up with probability (their value) / 256, so the
+// expectation is |x| rounded to 1/256 unit.
 // codes of four neighbouring values; `draws`: their four stream bytes
 template <bool RANDOM>
 __device__ __forceinline__ uint32_t act8_four(const float* x, float inverse, uint32_t draws) {
@@ -398,66 +428,6 @@ __device__ __forceinline__ uint4 act8_sixteen(const float (&v)[16], uint32_t sca
                       act8_four<RANDOM>(v + 12, inverse, r[3]));
 }
 
-// Codes of a thread's spread values (row_col<T, kSpread>).  `plane`: place of the row's first code,
-// `first` = tid - lane, `pitch`: codes of the row.  A step of the warp covers one block (4-byte
-// types) or two, of 16 lanes each.  The warp's 32 generator blocks of 16 draws are computed one
-// a lane.
-template <typename T, bool RANDOM>
-__device__ __forceinline__ void act8_encode_spread(const float (&v)[16], uint64_t plane,
-                                                   uint32_t pitch, int G, int first,
-                                                   uint32_t worker, const PhiloxKeys& keys,
-                                                   uint8_t* __restrict__ codes,
-                                                   uint8_t* __restrict__ scales) {
-    constexpr int PER = sizeof(T) == 4 ? 1 : 2;      // values of a lane in a step
-    const int lane = threadIdx.x & 31;
-    uint32_t r[4] = {0u, 0u, 0u, 0u};
-    if (RANDOM) {
-        const int step = lane / (2 * PER), part = lane % (2 * PER);
-        const uint32_t col = row_col<T, kSpread>(step * PER, G, first) + 16 * part;
-        stream_words4((plane + col) >> 4, worker, kDomainAct8, keys, r);
-    }
-#pragma unroll
-    for (int s = 0; s < 16 / PER; ++s) {
-        const uint32_t begin = row_col<T, kSpread>(s * PER, G, first);
-        uint32_t top;
-        if (PER == 1) {
-            top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v[s]) & 0x7FFFFFFFu);
-        } else {
-            const float m = max3_abs(v[PER * s], v[PER * s + PER - 1], 0.0f);
-            top = __float_as_uint(m);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        }
-        const uint32_t scale = act8_scale(top);
-        uint32_t word = 0;
-        if (RANDOM) {          // the lane's draws: bytes of word (column / 4) mod 4 of its chunk
-            const int source = s * 2 * PER + lane * PER / 16, which = (lane * PER >> 2) & 3;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t t = __shfl_sync(0xFFFFFFFFu, r[k], source);
-                if (which == k) word = t;
-            }
-            word >>= 8 * (lane * PER & 3);
-        }
-        const uint32_t col = begin + lane * PER;
-        if (col < pitch) {
-            const float inverse = act8_inverse(scale, RANDOM);
-            uint32_t code = 0;
-            if (scale != kAct8Nan) {
-                code = act8_one(v[PER * s], inverse, RANDOM, word & 0xFFu);
-                if (PER == 2)
-                    code |= act8_one(v[PER * s + PER - 1], inverse, RANDOM, (word >> 8) & 0xFFu)
-                            << 8;
-            }
-            if (PER == 1)
-                codes[plane + col] = (uint8_t)code;
-            else
-                *reinterpret_cast<unsigned short*>(codes + plane + col) = (unsigned short)code;
-            if ((col & 31) == 0) scales[(plane + col) >> 5] = (uint8_t)scale;
-        }
-    }
-}
-
 // ---- decoder ---------------------------------------------------------------------------------
 
 // any scale byte, one code at a time
@@ -496,42 +466,6 @@ __device__ __forceinline__ void act8_decode16(const uint4& c, uint32_t scale, fl
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = act8_value(w[i >> 2] >> (8 * (i & 3)) & 0xFFu, scale);
-    }
-}
-
-// a thread's spread values of a row of codes; those from `cols` on are 0
-template <typename T>
-__device__ __forceinline__ void act8_decode_spread(const uint8_t* __restrict__ codes,
-                                                   const uint8_t* __restrict__ scales,
-                                                   uint64_t plane, int G, int tid, uint32_t cols,
-                                                   float (&v)[16]) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t col = row_col<T, kSpread>(i, G, tid);
-            v[i] = col < cols ? act8_value(__ldg(codes + plane + col),
-                                           __ldg(scales + ((plane + col) >> 5)))
-                              : 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t col = row_col<T, kSpread>(2 * i, G, tid);
-            v[2 * i] = v[2 * i + 1] = 0.0f;
-            if (col < cols) {
-                const uint32_t c =
-                    __ldg(reinterpret_cast<const unsigned short*>(codes + plane + col));
-                const uint32_t scale = __ldg(scales + ((plane + col) >> 5));
-                if (scale <= kAct8MaxFast) {
-                    unpack2<__nv_bfloat16>(act8_pair_bf16(c, 0, act8_fields(scale)), v[2 * i],
-                                           v[2 * i + 1]);
-                } else {
-                    v[2 * i] = act8_value(c & 0xFFu, scale);
-                    v[2 * i + 1] = act8_value(c >> 8, scale);
-                }
-                if (col + 1 >= cols) v[2 * i + 1] = 0.0f;
-            }
-        }
     }
 }
 

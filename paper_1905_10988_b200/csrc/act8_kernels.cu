@@ -4,7 +4,7 @@
 // neighbouring values, half a block: two lanes agree on the block's largest magnitude with one
 // shuffle, a 16-byte store takes the codes, and one generator block serves the 16 draws of random
 // rounding.  Rows that are not 16-byte aligned are spread over the lanes, an element or a pair of
-// two-byte elements per access.
+// two-byte elements an access, and a warp puts them in order in shared memory.
 #include "act8_common.cuh"
 
 namespace natcomp {
@@ -49,20 +49,28 @@ __global__ void __launch_bounds__(kBlockThreads)
 act8_compress_spread_kernel(const T* __restrict__ x, const Act8Rows g, const uint32_t worker,
                             uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                             const __grid_constant__ PhiloxKeys keys) {
-    const int lane = threadIdx.x & 31;
+    __shared__ __align__(16) uint32_t scratch[kWarpsPerBlock][kSpreadWords<T>];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t segments = (g.per_row + 31) / 32;
-    const uint32_t w = blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
+    const uint32_t w = blockIdx.x * kWarpsPerBlock + warp;
     const uint32_t row = w / segments;
     if (row >= g.rows) return;
-    const uint64_t first = 512ull * (w - row * segments);
+    const uint32_t segment = w - row * segments;
+    const uint64_t first = 512ull * segment;
     Raw16<T> r;
     float v[16];
-    row_load<T, kSpread>(x + row * g.ld + first, 32, lane,
-                      g.cols > first ? (uint32_t)min(g.cols - first, (uint64_t)512) : 0u, false, r);
+    row_load<T, kSpread>(x + row * g.ld + first, lane,
+                         g.cols > first ? (uint32_t)min(g.cols - first, (uint64_t)1024) : 0u, false,
+                         r);
+    row_arrange<T, kSpread>(r, scratch[warp]);
     unpack16<T>(r, v);
-    act8_encode_spread<T, RANDOM>(v, 16ull * row * g.per_row + first,
-                                  (uint32_t)min(16ull * g.per_row - first, 512ull), 32, 0, worker,
-                                  keys, codes, scales);
+    uint32_t top = max_bits16(v);
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    const uint32_t scale = act8_scale(top), chunk = 32 * segment + lane;
+    if (chunk >= g.per_row) return;
+    const uint64_t i = (uint64_t)row * g.per_row + chunk;
+    __stcs(reinterpret_cast<uint4*>(codes) + i, act8_sixteen<RANDOM>(v, scale, i, worker, keys));
+    if (!(i & 1)) scales[i >> 1] = (uint8_t)scale;
 }
 
 template <typename T>
@@ -87,17 +95,22 @@ template <typename T>
 __global__ void __launch_bounds__(kBlockThreads)
 act8_decompress_spread_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                               const Act8Rows g, T* __restrict__ out) {
-    const int lane = threadIdx.x & 31;
+    __shared__ __align__(16) uint32_t scratch[kWarpsPerBlock][kSpreadWords<T>];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t segments = (g.per_row + 31) / 32;
-    const uint32_t w = blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
+    const uint32_t w = blockIdx.x * kWarpsPerBlock + warp;
     const uint32_t row = w / segments;
     if (row >= g.rows) return;
-    const uint64_t first = 512ull * (w - row * segments);
+    const uint32_t segment = w - row * segments, chunk = 32 * segment + lane;
+    const uint64_t first = 512ull * segment, i = (uint64_t)row * g.per_row + chunk;
     if (first >= g.cols) return;
-    const uint32_t cols = (uint32_t)min(g.cols - first, (uint64_t)512);
     float v[16];
-    act8_decode_spread<T>(codes, scales, 16ull * row * g.per_row + first, 32, lane, cols, v);
-    row_store<T, kSpread>(out + row * g.ld + first, 32, lane, cols, false, v);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = 0.0f;
+    if (chunk < g.per_row)
+        act8_decode16(ld_stream_u4(codes + 16 * i), __ldg(scales + (i >> 1)), v);
+    row_store<T, kSpread>(out + row * g.ld + first, lane,
+                          (uint32_t)min(g.cols - first, (uint64_t)1024), false, v, scratch[warp]);
 }
 
 // the plane of a matrix: one long row where the matrix has no gaps and whole blocks

@@ -33,22 +33,39 @@ __device__ __forceinline__ float ln_param(const void* p, int dtype, uint32_t col
     return __half2float(__ldg(static_cast<const __half*>(p) + col));
 }
 
-// A vector of parameters as the threads of a group read it: four values of thread `tid` at
-// table[q * G + tid], q = 0..3, in the order of the thread's columns.  Absent ones are `none`.
-template <typename T, int MODE>
+// A vector of parameters as the threads of a group read it: columns 16 * tid + 4 * q .. + 3 at
+// table[q * G + tid].  Absent ones are `none`.
 __device__ __forceinline__ void ln_table(float4* table, const void* p, bool has, int dtype, int G,
                                          uint32_t origin, uint32_t cols, float none) {
+    const bool vector = (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < 4 * G; i += blockDim.x) {
-        const int q = i / G, tid = i - q * G;
-        float f[4];
+    for (int i = threadIdx.x; i < 4 * G; i += blockDim.x) {      // i: four columns
+        const uint32_t col = 4 * i;
+        float f[4] = {none, none, none, none};
+        if (has) {
+            if (vector && col + 4 <= cols) {
+                if (dtype == NC_DTYPE_F32) {
+                    const float4 v = __ldg(reinterpret_cast<const float4*>(
+                        static_cast<const float*>(p) + origin + col));
+                    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+                } else {
+                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(
+                        static_cast<const unsigned short*>(p) + origin + col));
+                    if (dtype == NC_DTYPE_BF16) {
+                        unpack2<__nv_bfloat16>(v.x, f[0], f[1]);
+                        unpack2<__nv_bfloat16>(v.y, f[2], f[3]);
+                    } else {
+                        unpack2<__half>(v.x, f[0], f[1]);
+                        unpack2<__half>(v.y, f[2], f[3]);
+                    }
+                }
+            } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t at = row_col<T, MODE>(4 * q + k, G, tid);
-            f[k] = none;
-            if (has && at < cols) f[k] = ln_param(p, dtype, origin + at);
+                for (int k = 0; k < 4; ++k)
+                    if (col + k < cols) f[k] = ln_param(p, dtype, origin + col + k);
+            }
         }
-        table[i] = make_float4(f[0], f[1], f[2], f[3]);
+        table[(i & 3) * G + (i >> 2)] = make_float4(f[0], f[1], f[2], f[3]);
     }
 }
 
@@ -61,13 +78,12 @@ __device__ __forceinline__ void ln_params(const float4* table, int G, int tid, f
     }
 }
 
-// (The empty statement keeps this a branch: few threads need it.)
-template <typename T, int MODE>
-__device__ __forceinline__ void clear_beyond(float (&v)[16], int G, int tid, uint32_t cols) {
+// (The empty statement keeps the caller's condition a branch: few threads need it.)
+__device__ __forceinline__ void clear_beyond(float (&v)[16], int tid, uint32_t cols) {
     asm volatile("");
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-        if (row_col<T, MODE>(i, G, tid) >= cols) v[i] = 0.0f;
+        if (16u * tid + i >= cols) v[i] = 0.0f;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -85,21 +101,9 @@ __device__ __forceinline__ float sum_of(const f32x2 (&v)[8]) {
 }
 
 // values of warp `w` of the row's block `rank`
-template <typename T, int MODE>
 __device__ __forceinline__ uint32_t ln_warp_values(int rank, int w, int G, uint32_t all_cols) {
-    uint32_t n = 0;
-    const uint32_t origin = rank * 16 * G;
-    if (MODE != kSpread) {
-        const uint32_t first = origin + 512u * w;
-        n = all_cols > first ? min(all_cols - first, 512u) : 0u;
-    } else {
-        const uint32_t run = sizeof(T) == 4 ? 32u : 64u;       // neighbours that a step covers
-        for (uint32_t i = 0; i < 512u / run; ++i) {
-            const uint32_t first = origin + i * (run / 32u) * G + w * run;
-            n += all_cols > first ? min(all_cols - first, run) : 0u;
-        }
-    }
-    return n;
+    const uint32_t first = rank * 16 * G + 512u * w;
+    return all_cols > first ? min(all_cols - first, 512u) : 0u;
 }
 
 // Where a thread stands: a block holds blockDim / G groups of G threads, and a group owns a row at
@@ -224,6 +228,9 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
                   const __grid_constant__ PhiloxKeys keys) {
     __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
     __shared__ float2 counts[LnExchange<CLUSTER>::kSlots];
+    __shared__ __align__(16) uint32_t
+        scratches[MODE == kSpread ? kLnThreads / 32 : 1][MODE == kSpread ? kSpreadWords<T> : 4];
+    uint32_t* scratch = scratches[MODE == kSpread ? threadIdx.x >> 5 : 0];
     __shared__ uint64_t bars[2];
     extern __shared__ float4 tables[];   // gamma, beta
     const LnPlace<CLUSTER> p(threads, a.cols);
@@ -236,27 +243,28 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
     const uint32_t own = pitch > p.origin ? pitch - p.origin : 0;    // codes of a row from here on
 
     Raw16<T> next;
-    if (p.first < a.rows) row_load<T, MODE>(x + p.first * a.ldx, p.G, p.tid, p.cols, wide, next);
-    ln_table<T, MODE>(tables, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+    if (p.first < a.rows) row_load<T, MODE>(x + p.first * a.ldx, p.tid, p.cols, wide, next);
+    ln_table(tables, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
                         p.cols, 1.0f);
-    ln_table<T, MODE>(tables + 4 * p.G, a.params.beta, a.params.has_beta, a.params.dtype, p.G,
+    ln_table(tables + 4 * p.G, a.params.beta, a.params.has_beta, a.params.dtype, p.G,
                         p.origin, p.cols, 0.0f);
     // values of each warp of the row and their reciprocal
     for (int w = threadIdx.x; w < LnExchange<CLUSTER>::kSlots; w += blockDim.x) {
-        const float n = (float)ln_warp_values<T, MODE>(w / p.warps, w % p.warps, p.G, a.cols);
+        const float n = (float)ln_warp_values(w / p.warps, w % p.warps, p.G, a.cols);
         counts[w] = make_float2(n, n > 0.0f ? 1.0f / n : 0.0f);
     }
     LnExchange<CLUSTER> others;
     others.begin(slots, bars, p);
-    const bool whole = MODE == kRegular || row_col<T, MODE>(15, p.G, p.tid) < p.cols;
+    const bool whole = MODE == kRegular || 16u * p.tid + 15 < p.cols;
     const float inverse_n = counts[p.rank * p.warps + p.warp].y;
 
     uint32_t turn = 0;
     for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
         f32x2 v[8];
+        row_arrange<T, MODE>(next, scratch);
         unpack16<T>(next, v);
         if (row + p.step < a.rows)
-            row_load<T, MODE>(x + (row + p.step) * a.ldx, p.G, p.tid, p.cols, wide, next);
+            row_load<T, MODE>(x + (row + p.step) * a.ldx, p.tid, p.cols, wide, next);
         const float sum = warp_sum(sum_of(v));
         float mean = sum * inverse_n;
         float f[16];
@@ -268,7 +276,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
                 of_pair(d, f[2 * i], f[2 * i + 1]);
             }
         }
-        if (!whole) clear_beyond<T, MODE>(f, p.G, p.tid, p.cols);
+        if (!whole) clear_beyond(f, p.tid, p.cols);
         f32x2 q = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -304,21 +312,16 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
             float kept[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) kept[i] = f[i];
-            if (!whole) clear_beyond<T, MODE>(kept, p.G, p.tid, p.cols);
+            if (!whole) clear_beyond(kept, p.tid, p.cols);
             const uint64_t plane = row * pitch + p.origin;
-            if constexpr (MODE == kSpread) {
-                act8_encode_spread<T, KEEP == kKeepRandom>(kept, plane, own, p.G, p.tid - p.lane,
-                                                           a.worker, keys, a.codes, a.scales);
-            } else {
-                uint32_t top = max_bits16(kept);
-                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                const uint32_t scale = act8_scale(top);
-                if (MODE == kRegular || 16u * p.tid < own) {
-                    const uint64_t at = (plane >> 4) + p.tid;
-                    __stcs(reinterpret_cast<uint4*>(a.codes) + at,
-                           act8_sixteen<KEEP == kKeepRandom>(kept, scale, at, a.worker, keys));
-                    if (!(p.tid & 1)) a.scales[at >> 1] = (uint8_t)scale;
-                }
+            uint32_t top = max_bits16(kept);
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            const uint32_t scale = act8_scale(top);
+            if (16u * p.tid < own) {
+                const uint64_t at = (plane >> 4) + p.tid;
+                __stcs(reinterpret_cast<uint4*>(a.codes) + at,
+                       act8_sixteen<KEEP == kKeepRandom>(kept, scale, at, a.worker, keys));
+                if (!(p.tid & 1)) a.scales[at >> 1] = (uint8_t)scale;
             }
         }
         f32x2 gamma[8], beta[8];
@@ -326,7 +329,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         ln_params(tables + 4 * p.G, p.G, p.tid, beta);
 #pragma unroll
         for (int i = 0; i < 8; ++i) of_pair(fma2(v[i], gamma[i], beta[i]), f[2 * i], f[2 * i + 1]);
-        row_store<T, MODE>(y + row * a.ldy, p.G, p.tid, p.cols, wide, f);
+        row_store<T, MODE>(y + row * a.ldy, p.tid, p.cols, wide, f, scratch);
     }
     // no block leaves while another may still write to its slots
     if (CLUSTER > 1) cluster_sync();
@@ -396,9 +399,9 @@ ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const uint32_t origin = c * 16 * G;
-        ln_table<T, kRegular>(tables + 8 * G * c, a.params.gamma, a.params.has_gamma,
+        ln_table(tables + 8 * G * c, a.params.gamma, a.params.has_gamma,
                               a.params.dtype, G, origin, a.cols - origin, 1.0f);
-        ln_table<T, kRegular>(tables + 8 * G * c + 4 * G, a.params.beta, a.params.has_beta,
+        ln_table(tables + 8 * G * c + 4 * G, a.params.beta, a.params.has_beta,
                               a.params.dtype, G, origin, a.cols - origin, 0.0f);
     }
     LnExchange<1> others;
@@ -479,7 +482,8 @@ static bool ln_regular(const LnDeal& d, uint64_t cols, int access) {
 
 template <typename T, int KEEP>
 static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
-    if (a.access == kRowWide && a.cols % 1024 == 0 && a.cols <= 8192) {
+    // (few rows: with half the threads a row, one row of 4096 took 8.2 us instead of 6.5)
+    if (a.access == kRowWide && a.cols % 1024 == 0 && a.cols <= 8192 && a.rows >= 512) {
         LnDeal d;
         d.cluster = 1;
         d.G = (int)(a.cols / 32);
@@ -496,6 +500,9 @@ static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
     }
     const LnDeal d = ln_deal(a.rows, a.cols);
     auto pick = [&]() {
+        if (ln_regular(d, a.cols, a.access))
+            return d.cluster == 1 ? ln_forward_kernel<T, kRegular, KEEP, 1>
+                                  : ln_forward_kernel<T, kRegular, KEEP, 2>;
         if (a.access != kRowElement)
             return d.cluster == 1   ? ln_forward_kernel<T, kVector, KEEP, 1>
                    : d.cluster == 2 ? ln_forward_kernel<T, kVector, KEEP, 2>
@@ -506,8 +513,16 @@ static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
                : d.cluster == 4 ? ln_forward_kernel<T, kSpread, KEEP, 4>
                                 : ln_forward_kernel<T, kSpread, KEEP, 8>;
     };
-    return ln_launch(pick(), d, 1024, (uint64_t)1 << 30, 2 * 16 * d.G * sizeof(float), nullptr,
-                     stream, a, d.G, make_philox_keys(a.seed));
+    const auto kernel = pick();
+    const size_t smem = 2 * 16 * d.G * sizeof(float);
+    // spread rows of four-byte values need more than the 48 KB that come without asking
+    static bool allowed[4][64];
+    if (a.access == kRowElement && sizeof(T) == 4 &&
+        !allow_dynamic_smem((const void*)kernel, 2 * 16 * kLnThreads * sizeof(float),
+                            allowed[31 - __builtin_clz((unsigned)d.cluster)]))
+        return NC_ERR_CUDA;
+    return ln_launch(kernel, d, 1024, (uint64_t)1 << 30, smem, nullptr, stream, a, d.G,
+                     make_philox_keys(a.seed));
 }
 
 template <typename T>
@@ -554,6 +569,9 @@ template <typename T, int MODE, bool SAVED8, bool RES, int CLUSTER>
 __global__ void __launch_bounds__(kLnThreads, 2)
 ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
+    __shared__ __align__(16) uint32_t
+        scratches[MODE == kSpread ? kLnThreads / 32 : 1][MODE == kSpread ? kSpreadWords<T> : 4];
+    uint32_t* scratch = scratches[MODE == kSpread ? threadIdx.x >> 5 : 0];
     __shared__ uint64_t bars[2];
     extern __shared__ float4 table[];    // gamma; several groups: their sums behind it
     const LnPlace<CLUSTER> p(threads, a.cols);
@@ -570,8 +588,8 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
 
     auto load = [&](uint64_t row, LnRow<T, SAVED8, RES>& r) {
         r.rstd = __ldg(a.rstd + row);
-        row_load<T, MODE>(dy + row * a.lddy, p.G, p.tid, p.cols, a.wide, r.dy);
-        if constexpr (SAVED8 && MODE != kSpread) {
+        row_load<T, MODE>(dy + row * a.lddy, p.tid, p.cols, a.wide, r.dy);
+        if constexpr (SAVED8) {
             const uint64_t plane = row * pitch + p.origin;
             r.codes = make_uint4(0u, 0u, 0u, 0u);
             r.scale = kAct8MinScale;
@@ -579,22 +597,22 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
                 r.codes = ld_stream_u4(a.codes + plane + 16u * p.tid);
                 r.scale = __ldg(a.scales + ((plane + 16u * p.tid) >> 5));
             }
-        } else if constexpr (!SAVED8) {
+        } else {
             r.mean = __ldg(a.mean + row);
-            row_load<T, MODE>(x + row * a.ldx, p.G, p.tid, p.cols, a.wide, r.x);
+            row_load<T, MODE>(x + row * a.ldx, p.tid, p.cols, a.wide, r.x);
         }
         if constexpr (RES)
-            row_load<T, MODE>(dres + row * a.lddres, p.G, p.tid, p.cols, a.wide, r.dres);
+            row_load<T, MODE>(dres + row * a.lddres, p.tid, p.cols, a.wide, r.dres);
     };
 
     LnRow<T, SAVED8, RES> next;
     if (p.first < a.rows) load(p.first, next);
     f32x2 dgamma[8], dbeta[8];
-    ln_table<T, MODE>(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
+    ln_table(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
                         p.cols, 1.0f);
     LnExchange<CLUSTER> others;
     others.begin(slots, bars, p);
-    const bool whole = MODE == kRegular || row_col<T, MODE>(15, p.G, p.tid) < p.cols;
+    const bool whole = MODE == kRegular || 16u * p.tid + 15 < p.cols;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgamma[i] = dbeta[i] = 0;
 
@@ -602,22 +620,20 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
         f32x2 g[8], xh[8];
         const float rstd = next.rstd;
+        row_arrange<T, MODE>(next.dy, scratch);
         unpack16<T>(next.dy, g);
         {
             float f[16];
             if constexpr (SAVED8) {
-                if constexpr (MODE == kSpread)
-                    act8_decode_spread<T>(a.codes, a.scales, row * pitch + p.origin, p.G, p.tid,
-                                          p.cols, f);
-                else
-                    act8_decode16(next.codes, next.scale, f);
+                act8_decode16(next.codes, next.scale, f);
             } else {
+                row_arrange<T, MODE>(next.x, scratch);
                 unpack16<T>(next.x, f);
                 const float mean = next.mean;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) f[i] = (f[i] - mean) * rstd;
             }
-            if (!whole) clear_beyond<T, MODE>(f, p.G, p.tid, p.cols);
+            if (!whole) clear_beyond(f, p.tid, p.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) xh[i] = pair_of(f[2 * i], f[2 * i + 1]);
         }
@@ -650,13 +666,16 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         float out[16];
         const f32x2 n1 = pair_of(-m1, -m1), n2 = pair_of(-m2, -m2), s = pair_of(rstd, rstd);
         f32x2 d[8];
-        if constexpr (RES) unpack16<T>(late, d);
+        if constexpr (RES) {
+            row_arrange<T, MODE>(late, scratch);
+            unpack16<T>(late, d);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const f32x2 inner = fma2(xh[i], n2, add2(g[i], n1));
             of_pair(RES ? fma2(inner, s, d[i]) : mul2(inner, s), out[2 * i], out[2 * i + 1]);
         }
-        row_store<T, MODE>(dx + row * a.lddx, p.G, p.tid, p.cols, a.wide, out);
+        row_store<T, MODE>(dx + row * a.lddx, p.tid, p.cols, a.wide, out, scratch);
     }
 
     let_next_begin();
@@ -675,7 +694,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             if (p.group == k && k > 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
+                    const uint32_t col = 16u * p.tid + i;
                     if (col < p.cols) {
                         dg[i] += out[col];
                         db[i] += out2[col];
@@ -685,7 +704,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             if (p.group == k && k + 1 < p.groups) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
+                    const uint32_t col = 16u * p.tid + i;
                     if (col < p.cols) {
                         out[col] = dg[i];
                         out2[col] = db[i];
@@ -698,7 +717,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         out2 = out + a.parts_pitch;
     }
     if (p.group == p.groups - 1) {
-        if (MODE != kSpread && whole) {  // the workspace's rows start on 16 bytes
+        if (whole) {                     // the workspace's rows start on 16 bytes
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 *reinterpret_cast<float4*>(out + 16 * p.tid + i) =
@@ -709,7 +728,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const uint32_t col = row_col<T, MODE>(i, p.G, p.tid);
+                const uint32_t col = 16u * p.tid + i;
                 if (col < p.cols) {
                     out[col] = dg[i];
                     out2[col] = db[i];

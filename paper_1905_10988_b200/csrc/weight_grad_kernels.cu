@@ -719,18 +719,18 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
     __shared__ float sums[512];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint64_t first = (uint64_t)blockIdx.x * 512;
-    const uint32_t cols = (uint32_t)min(n - first, (uint64_t)512);
+    const uint32_t cols = (uint32_t)min(n - first, (uint64_t)1024);
     const uint64_t begin = rows * blockIdx.y / ranges, end = rows * (blockIdx.y + 1) / ranges;
     float s[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
     for (uint64_t t = begin + warp; t < end; t += 8) {
         Raw16<__nv_bfloat16> r;
-        row_load<__nv_bfloat16, kSpread>(dy + t * lddy + first, 32, lane, cols, false, r);
+        row_load<__nv_bfloat16, kSpread>(dy + t * lddy + first, lane, cols, false, r);
         uint32_t* out = reinterpret_cast<uint32_t*>(copy + t * ldc + first);
 #pragma unroll
         for (int i = 0; i < 8; ++i)      // rows of the copy hold whole pairs
-            if (row_col<__nv_bfloat16, kSpread>(2 * i, 32, lane) < cols)
+            if (spread_col<__nv_bfloat16>(i, lane) < cols)
                 out[32 * i + lane] = r.b[0].v[i];
         float v[16];
         unpack16<__nv_bfloat16>(r, v);
@@ -741,13 +741,13 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
         if (warp == w) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const uint32_t c = row_col<__nv_bfloat16, kSpread>(i, 32, lane);
+                const uint32_t c = spread_col<__nv_bfloat16>(i >> 1, lane) + (i & 1);
                 sums[c] = w ? sums[c] + s[i] : s[i];
             }
         }
         __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < cols; c += 256) parts[blockIdx.y * n + first + c] = sums[c];
+    for (uint32_t c = threadIdx.x; c < min(cols, 512u); c += 256) parts[blockIdx.y * n + first + c] = sums[c];
 }
 
 // db <- [db +] the parts' sum, in the order of the parts within each of 8 interleaved groups, then of
