@@ -554,7 +554,33 @@ struct LnBackward {
     bool wide;
 };
 
-// what a thread holds of a row before it is unpacked: loaded one row ahead
+// kRegular rows pass through a ring in shared memory, filled by bulk copies that one thread of a group
+// issues two or three rows ahead (with the rows ahead held in registers instead, 2051 x 8192 took 31 us
+// and 16384 x 4096 from the checkpoint 92).  Places of a row's pieces in a stage, for G threads:
+template <typename T, bool SAVED8, bool RES>
+struct LnStage {
+    static constexpr int kStages = sizeof(T) == 4 ? 2 : 3;
+    static constexpr uint32_t kValues = 16 * sizeof(T);              // bytes of a thread
+    static constexpr uint32_t kSaved = SAVED8 ? 16 : kValues;
+    __host__ __device__ static uint32_t saved(int G) { return kValues * G; }
+    __host__ __device__ static uint32_t scales(int G) { return saved(G) + kSaved * G; }
+    __host__ __device__ static uint32_t dres(int G) { return scales(G) + (SAVED8 ? G / 2 : 0); }
+    __host__ __device__ static uint32_t bytes(int G) { return dres(G) + (RES ? kValues * G : 0); }
+};
+
+template <typename T>
+__device__ __forceinline__ Raw16<T> ld_shared16(const uint8_t* p) {
+    Raw16<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+        const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+        uint32_t* v = r.b[i >> 1].v + 4 * (i & 1);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    }
+    return r;
+}
+
+// what a thread holds of a row before it is unpacked; other rows: loaded one row ahead
 template <typename T, bool SAVED8, bool RES>
 struct LnRow {
     Raw16<T> dy;
@@ -572,8 +598,8 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     __shared__ __align__(16) uint32_t
         scratches[MODE == kSpread ? kLnThreads / 32 : 1][MODE == kSpread ? kSpreadWords<T> : 4];
     uint32_t* scratch = scratches[MODE == kSpread ? threadIdx.x >> 5 : 0];
-    __shared__ uint64_t bars[2];
-    extern __shared__ float4 table[];    // gamma; several groups: their sums behind it
+    __shared__ uint64_t bars[2], ringbars[MODE == kRegular ? 8 : 1][3];
+    extern __shared__ float4 table[];    // gamma; several groups: their sums; the ring
     const LnPlace<CLUSTER> p(threads, a.cols);
     float* columns = reinterpret_cast<float*>(table + 4 * p.G);
     const int row_warps = CLUSTER * p.warps;
@@ -586,40 +612,85 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     const uint32_t pitch = (a.cols + 31) & ~31u;
     const uint32_t own = pitch > p.origin ? pitch - p.origin : 0;    // codes of a row from here on
 
+    using Stage = LnStage<T, SAVED8, RES>;
+    constexpr bool kRing = MODE == kRegular;
+    uint8_t* ring = reinterpret_cast<uint8_t*>(columns + (p.groups > 1 ? 2 * pitch : 0)) +
+                    p.group * Stage::kStages * Stage::bytes(p.G);
+    const uint32_t arrived = smem_u32(ringbars[p.group]);
+
     auto load = [&](uint64_t row, LnRow<T, SAVED8, RES>& r) {
         r.rstd = __ldg(a.rstd + row);
-        row_load<T, MODE>(dy + row * a.lddy, p.tid, p.cols, a.wide, r.dy);
+        if constexpr (!SAVED8) r.mean = __ldg(a.mean + row);
+        if constexpr (!kRing) {
+            row_load<T, MODE>(dy + row * a.lddy, p.tid, p.cols, a.wide, r.dy);
+            if constexpr (SAVED8) {
+                const uint64_t plane = row * pitch + p.origin;
+                r.codes = make_uint4(0u, 0u, 0u, 0u);
+                r.scale = kAct8MinScale;
+                if (16u * p.tid < own) {
+                    r.codes = ld_stream_u4(a.codes + plane + 16u * p.tid);
+                    r.scale = __ldg(a.scales + ((plane + 16u * p.tid) >> 5));
+                }
+            } else {
+                row_load<T, MODE>(x + row * a.ldx, p.tid, p.cols, a.wide, r.x);
+            }
+            if constexpr (RES)
+                row_load<T, MODE>(dres + row * a.lddres, p.tid, p.cols, a.wide, r.dres);
+        }
+    };
+    // one thread: the group's part of a row into stage `s`
+    auto fetch = [&](uint64_t row, uint32_t s) {
+        const uint32_t bar = arrived + 8 * s, at = smem_u32(ring + s * Stage::bytes(p.G));
+        const uint32_t values = Stage::kValues * p.G;
+        mbar_expect(bar, Stage::bytes(p.G));
+        bulk_load(at, dy + row * a.lddy, values, bar);
         if constexpr (SAVED8) {
             const uint64_t plane = row * pitch + p.origin;
-            r.codes = make_uint4(0u, 0u, 0u, 0u);
-            r.scale = kAct8MinScale;
-            if (MODE == kRegular || 16u * p.tid < own) {
-                r.codes = ld_stream_u4(a.codes + plane + 16u * p.tid);
-                r.scale = __ldg(a.scales + ((plane + 16u * p.tid) >> 5));
-            }
+            bulk_load(at + Stage::saved(p.G), a.codes + plane, 16 * p.G, bar);
+            bulk_load(at + Stage::scales(p.G), a.scales + (plane >> 5), p.G / 2, bar);
         } else {
-            r.mean = __ldg(a.mean + row);
-            row_load<T, MODE>(x + row * a.ldx, p.tid, p.cols, a.wide, r.x);
+            bulk_load(at + Stage::saved(p.G), x + row * a.ldx, values, bar);
         }
-        if constexpr (RES)
-            row_load<T, MODE>(dres + row * a.lddres, p.tid, p.cols, a.wide, r.dres);
+        if constexpr (RES) bulk_load(at + Stage::dres(p.G), dres + row * a.lddres, values, bar);
     };
 
     LnRow<T, SAVED8, RES> next;
     if (p.first < a.rows) load(p.first, next);
+    if (kRing && p.tid == 0) {
+        for (int s = 0; s < Stage::kStages; ++s) mbar_init(arrived + 8 * s, 1);
+        mbar_init_fence();
+        for (int s = 0; s < Stage::kStages; ++s)
+            if (p.first + s * p.step < a.rows) fetch(p.first + s * p.step, s);
+    }
     f32x2 dgamma[8], dbeta[8];
-    ln_table(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin,
-                        p.cols, 1.0f);
+    ln_table(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin, p.cols, 1.0f);
     LnExchange<CLUSTER> others;
     others.begin(slots, bars, p);
     const bool whole = MODE == kRegular || 16u * p.tid + 15 < p.cols;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgamma[i] = dbeta[i] = 0;
 
-    uint32_t turn = 0;
+    uint32_t turn = 0, stage = 0, parity = 0;
     for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
         f32x2 g[8], xh[8];
-        const float rstd = next.rstd;
+        float rstd = next.rstd;
+        const float mean = SAVED8 ? 0.0f : next.mean;
+        const uint8_t* here = ring + stage * Stage::bytes(p.G);
+        if constexpr (kRing) {
+            const long long begin = clock64();
+            bool done = mbar_try(arrived + 8 * stage, parity);
+            while (!done && clock64() - begin < 4000000000ll)
+                done = mbar_try(arrived + 8 * stage, parity);
+            if (!done) rstd = __uint_as_float(0x7FC00000u);   // must not pass for a result
+            next.dy = ld_shared16<T>(here + Stage::kValues * p.tid);
+            if constexpr (SAVED8) {
+                next.codes =
+                    *reinterpret_cast<const uint4*>(here + Stage::saved(p.G) + 16 * p.tid);
+                next.scale = here[Stage::scales(p.G) + (p.tid >> 1)];
+            } else {
+                next.x = ld_shared16<T>(here + Stage::saved(p.G) + Stage::kValues * p.tid);
+            }
+        }
         row_arrange<T, MODE>(next.dy, scratch);
         unpack16<T>(next.dy, g);
         {
@@ -629,7 +700,6 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             } else {
                 row_arrange<T, MODE>(next.x, scratch);
                 unpack16<T>(next.x, f);
-                const float mean = next.mean;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) f[i] = (f[i] - mean) * rstd;
             }
@@ -638,7 +708,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             for (int i = 0; i < 8; ++i) xh[i] = pair_of(f[2 * i], f[2 * i + 1]);
         }
         Raw16<T> late;
-        if constexpr (RES) late = next.dres;
+        if constexpr (RES && !kRing) late = next.dres;
         if (row + p.step < a.rows) load(row + p.step, next);
         f32x2 s1 = 0, s2 = 0, gamma[8];
         ln_params(table, p.G, p.tid, gamma);
@@ -659,6 +729,19 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             const float2* got = others.send(make_float2(m1, m2), turn, p);
             m1 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; });
             m2 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].y; });
+        } else if (kRing) {
+            __syncwarp();
+        }
+        if constexpr (kRing) {
+            // the whole group has come by, so it is done with the stage of the row before
+            const uint32_t before = stage ? stage - 1 : Stage::kStages - 1;
+            const uint64_t ahead = row + (Stage::kStages - 1) * p.step;
+            if (p.tid == 0 && turn > 0 && ahead < a.rows) fetch(ahead, before);
+            if constexpr (RES) late = ld_shared16<T>(here + Stage::dres(p.G) + Stage::kValues * p.tid);
+            if (++stage == Stage::kStages) {
+                stage = 0;
+                parity ^= 1;
+            }
         }
         m1 *= inverse_cols;
         m2 *= inverse_cols;
@@ -785,9 +868,21 @@ static nc_status ln_backward_go(const LnBackward& a, int access, uint64_t* block
                : d.cluster == 4 ? ln_backward_kernel<T, kSpread, SAVED8, RES, 4>
                                 : ln_backward_kernel<T, kSpread, SAVED8, RES, 8>;
     };
-    const size_t smem =
+    size_t smem =
         16 * d.G * sizeof(float) + (d.groups > 1 ? 2 * act8_pitch(a.cols) * sizeof(float) : 0);
-    return ln_launch(pick(), d, 512, kLnMaxParts, smem, blocks, stream, a, d.G);
+    const auto kernel = pick();
+    if (ln_regular(d, a.cols, access)) {
+        using Stage = LnStage<T, SAVED8, RES>;
+        constexpr size_t kGroups = kLnThreads / 32;      // the most that any G takes
+        static bool allowed[2][64];
+        if (!allow_dynamic_smem((const void*)kernel,
+                                16 * kLnThreads * sizeof(float) + 2 * 4096 * sizeof(float) +
+                                    Stage::kStages * kGroups * Stage::bytes(32),
+                                allowed[d.cluster - 1]))
+            return NC_ERR_CUDA;
+        smem += d.groups * Stage::kStages * Stage::bytes(d.G);
+    }
+    return ln_launch(kernel, d, 512, kLnMaxParts, smem, blocks, stream, a, d.G);
 }
 
 template <typename T>
