@@ -48,7 +48,8 @@ constexpr uint32_t kWgDecoded = kWgStages * kWgOperand;
 constexpr uint32_t kWgCodes = kWgDecoded + kWgSlots * kWgOperand;
 constexpr uint32_t kWgScales = kWgCodes + kWgSlots * kWgCodeBytes;
 constexpr uint32_t kWgBars = kWgScales + kWgSlots * kWgScaleBytes;
-constexpr uint32_t kWgSmem = kWgBars + 512 + 2 * kWgTile * 4 + 1024;
+constexpr uint32_t kWgRows = 32 * 9 * 4;             // a writer warp's rows in passing
+constexpr uint32_t kWgSmem = kWgBars + 512 + 2 * kWgTile * 4 + kWgWriters * kWgRows + 1024;
 constexpr int kWgPairs = 74;             // pairs of blocks that the chip holds at a time
 constexpr int kWgMinSteps = 4;           // of a part
 
@@ -71,7 +72,7 @@ struct WgArgs {
                                          // one more, m = tiles_n / 2, k tile i / m
     uint32_t tiles;                      // single ones after that
     uint32_t whole, splits;              // those from `whole` on are computed in `splits` parts
-    float* parts;                        // [tile - whole][part][256][256]
+    float* parts;                        // [tile - whole][part][k / 4][256 n][4]
 };
 
 __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) {
@@ -217,42 +218,81 @@ __device__ __forceinline__ uint4 wg_load_dy8(const WgArgs& a, uint64_t t, uint64
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// four neighbouring values of dW, `add` = beta's part
-__device__ __forceinline__ void wg_store4(const WgArgs& a, uint64_t n, uint64_t k, float (&v)[4]) {
+// eight neighbouring values of dW
+__device__ __forceinline__ void wg_store8(const WgArgs& a, uint64_t n, uint64_t k, float (&v)[8]) {
+    const bool vector = a.vector && k + 8 <= a.k;
     if (a.dw_f32) {
         float* p = static_cast<float*>(a.dw) + n * a.lddw + k;
-        if (a.vector && k + 4 <= a.k) {
-            float4 o = make_float4(v[0], v[1], v[2], v[3]);
-            if (a.accumulate) {
-                const float4 old = *reinterpret_cast<const float4*>(p);
-                o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+        if (vector) {
+            float4* q = reinterpret_cast<float4*>(p);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 o = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+                if (a.accumulate) {
+                    const float4 old = q[h];
+                    o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+                }
+                q[h] = o;
             }
-            *reinterpret_cast<float4*>(p) = o;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i)
                 if (k + i < a.k) p[i] = a.accumulate ? p[i] + v[i] : v[i];
         }
     } else {
         __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + n * a.lddw + k;
-        if (a.vector && k + 4 <= a.k) {
+        if (vector) {
+            uint4* q = reinterpret_cast<uint4*>(p);
             if (a.accumulate) {
-                const uint2 old = *reinterpret_cast<const uint2*>(p);
-                float e, f;
-                unpack2<__nv_bfloat16>(old.x, e, f);
-                v[0] += e;
-                v[1] += f;
-                unpack2<__nv_bfloat16>(old.y, e, f);
-                v[2] += e;
-                v[3] += f;
+                const uint4 old = *q;
+                const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float e, f;
+                    unpack2<__nv_bfloat16>(w[i], e, f);
+                    v[2 * i] += e;
+                    v[2 * i + 1] += f;
+                }
             }
-            *reinterpret_cast<uint2*>(p) = make_uint2(pack2<__nv_bfloat16>(v[0], v[1]),
-                                                      pack2<__nv_bfloat16>(v[2], v[3]));
+            *q = make_uint4(pack2<__nv_bfloat16>(v[0], v[1]), pack2<__nv_bfloat16>(v[2], v[3]),
+                            pack2<__nv_bfloat16>(v[4], v[5]), pack2<__nv_bfloat16>(v[6], v[7]));
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i)
                 if (k + i < a.k)
                     p[i] = __float2bfloat16_rn(a.accumulate ? __bfloat162float(p[i]) + v[i] : v[i]);
+        }
+    }
+}
+
+// eight neighbouring values of the 32 rows of a warp, a row a lane, where rows cannot be written by 16
+// bytes: they change places in shared memory, so that the lanes write neighbouring values
+__device__ __forceinline__ void wg_store_rows(const WgArgs& a, uint64_t n0, uint64_t k,
+                                              const float (&v)[8], uint32_t* rows) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rows[lane * 9 + i] = __float_as_uint(v[i]);
+    __syncwarp();
+    const uint64_t col = k + (lane & 7);
+    const uint32_t row = lane >> 3;
+    const uint64_t at = (n0 + row) * a.lddw + col, step = 4 * a.lddw;
+    const int count = col >= a.k || n0 + row >= a.n ? 0 : (int)min((a.n - n0 - row + 3) / 4, (uint64_t)8);
+    if (a.dw_f32) {
+        float* p = static_cast<float*>(a.dw) + at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float o = __uint_as_float(rows[(4 * i + row) * 9 + (lane & 7)]);
+            if (i < count) p[i * step] = a.accumulate ? p[i * step] + o : o;
+        }
+    } else {
+        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float o = __uint_as_float(rows[(4 * i + row) * 9 + (lane & 7)]);
+            if (i < count)
+                p[i * step] = __float2bfloat16_rn(
+                    a.accumulate ? __bfloat162float(p[i * step]) + o : o);
         }
     }
 }
@@ -366,6 +406,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         }
     } else if (warp < kWgWriters) {
         // ---- write a tile out: lane = row
+        uint32_t* rows = reinterpret_cast<uint32_t*>(affine + 2 * kWgTile) + warp * (kWgRows / 4);
         uint32_t u = 0;
         WgTurns turns;
         for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) {
@@ -390,33 +431,34 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                 ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
                 tc_fence_after();
                 const uint32_t from = tmem + b * kWgTile + ((uint32_t)(32 * warp) << 16);
-                float* parts = a.parts + (((uint64_t)(w.tile - a.whole) * a.splits + w.part) *
-                                              kWgTile + rank * kWgHalf + 32 * warp + lane) * kWgTile;
+                float4* parts = reinterpret_cast<float4*>(a.parts) +
+                                ((uint64_t)(w.tile - a.whole) * a.splits + w.part) *
+                                    (kWgTile / 4 * kWgTile) +
+                                rank * kWgHalf + 32 * warp + lane;
+                // (a loop of few instructions: in a short call they are all fetched for the first time)
+                const int end = part || k0 + kWgTile <= a.k ? kWgTile : (int)((a.k - k0 + 7) & ~7ull);
+                uint32_t next[8];
+                tmem_load8(from, next);
 #pragma unroll 1
-                for (int c = 0; c < kWgTile; c += 32) {
-                    float v[32];
-                    tmem_load32(from + c, v);
-                    if (!ok) {       // a wait ran out: the result must not pass for one
+                for (int c = 0; c < end; c += 8) {
+                    float v[8];
+                    tmem_wait8(next);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FC00000u);
-                    }
-                    if (part) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4*>(parts + c + i) =
-                                make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    for (int i = 0; i < 8; ++i)      // NaN: a wait ran out, no result
+                        v[i] = ok ? __uint_as_float(next[i]) : __uint_as_float(0x7FC00000u);
+                    if (c + 8 < end) tmem_load8(from + c + 8, next);
+                    if (part) {      // four columns of all rows follow each other
+                        parts[c / 4 * kWgTile] = make_float4(v[0], v[1], v[2], v[3]);
+                        parts[(c / 4 + 1) * kWgTile] = make_float4(v[4], v[5], v[6], v[7]);
                         continue;
                     }
-                    if (n >= a.n || k0 + c >= a.k) continue;
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        float o[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            o[j] = fmaf(v[i + j], affine[c + i + j],
-                                        add * affine[kWgTile + c + i + j]);
-                        wg_store4(a, n, k0 + c + i, o);
-                    }
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = fmaf(v[i], affine[c + i], add * affine[kWgTile + c + i]);
+                    if (!a.vector || k0 + c + 8 > a.k)
+                        wg_store_rows(a, n - lane, k0 + c, v, rows);
+                    else if (n < a.n)
+                        wg_store8(a, n, k0 + c, v);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -582,32 +624,65 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
 }
 
 // the tiles that were computed in parts: dw <- [dw +] gamma * (sum of the parts, in order) +
-// beta * db; no parts: the sum over no tokens.  A block takes 4 rows of a tile.
+// beta * db; no parts: the sum over no tokens.  A block takes 32 rows x 32 columns of a tile; the
+// parts hold rows side by side, dw columns, so they change places in shared memory.
 __global__ void __launch_bounds__(256) wg_join_kernel(const __grid_constant__ WgArgs a) {
+    __shared__ float4 sums[8][33];
     after_previous();
-    const uint32_t tile = a.whole + blockIdx.x / 64, row = blockIdx.x % 64 * 4 + (threadIdx.x >> 6);
-    const uint32_t column = (threadIdx.x & 63) * 4;
+    const uint32_t tile = a.whole + blockIdx.x / 64, piece = blockIdx.x % 64;
     uint64_t n, k;
     wg_single(a, tile, n, k);
-    n += row;
-    k += column;
+    n += piece / 8 * 32;
+    k += piece % 8 * 32;
     if (n >= a.n || k >= a.k) return;
-    const float* p = a.parts + ((uint64_t)(tile - a.whole) * a.splits * kWgTile + row) * kWgTile + column;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    {
+        const uint32_t row = threadIdx.x & 31, four = threadIdx.x >> 5;
+        const float4* p = reinterpret_cast<const float4*>(a.parts) +
+                          (uint64_t)(tile - a.whole) * a.splits * (kWgTile / 4 * kWgTile) +
+                          (piece % 8 * 8 + four) * kWgTile + piece / 8 * 32 + row;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-    for (uint32_t z = 0; z < a.splits; ++z) {
-        const float4 q =
-            __ldcs(reinterpret_cast<const float4*>(p + (uint64_t)z * kWgTile * kWgTile));
-        v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+        for (uint32_t z = 0; z < a.splits; ++z) {
+            const float4 q = __ldcs(p + (uint64_t)z * (kWgTile / 4 * kWgTile));
+            s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+        }
+        sums[four][row] = s;
     }
+    __syncthreads();
+    if (!a.vector) {                     // a value at a time, neighbours side by side
+        const uint32_t column = threadIdx.x & 31;
+        if (k + column >= a.k) return;
+        const float gamma = a.gamma ? wg_param(a.gamma, a.param_dtype, k + column) : 1.0f;
+        const float beta = a.beta ? wg_param(a.beta, a.param_dtype, k + column) : 0.0f;
+        for (uint32_t row = threadIdx.x >> 5; row < 32 && n + row < a.n; row += 8) {
+            const float s = reinterpret_cast<const float*>(&sums[column >> 2][row])[column & 3];
+            const float v = a.beta ? fmaf(a.db[n + row], beta, s * gamma) : s * gamma;
+            const uint64_t at = (n + row) * a.lddw + k + column;
+            if (a.dw_f32) {
+                float* p = static_cast<float*>(a.dw) + at;
+                *p = a.accumulate ? *p + v : v;
+            } else {
+                __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw) + at;
+                *p = __float2bfloat16_rn(a.accumulate ? __bfloat162float(*p) + v : v);
+            }
+        }
+        return;
+    }
+    if (threadIdx.x >= 128) return;
+    const uint32_t row = threadIdx.x >> 2, eight = threadIdx.x & 3;
+    n += row;
+    k += 8 * eight;
+    if (n >= a.n || k >= a.k) return;
+    const float4 lo = sums[2 * eight][row], hi = sums[2 * eight + 1][row];
+    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     const float add = a.beta ? a.db[n] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
         if (k + i < a.k) {
             if (a.gamma) v[i] *= wg_param(a.gamma, a.param_dtype, k + i);
             if (a.beta) v[i] = fmaf(add, wg_param(a.beta, a.param_dtype, k + i), v[i]);
         }
-    wg_store4(a, n, k, v);
+    wg_store8(a, n, k, v);
 }
 
 // ---- scale bytes by columns of 128: word [c][t] holds the four bytes of token t and of the columns
@@ -631,7 +706,7 @@ __device__ __forceinline__ void wg_lay_scales(const WgScales& g, int first) {
             const uint64_t t = t0 + i / 32, c = c0 + i % 32;
             uint32_t w = 0x7F7F7F7Fu;
             if (t < g.rows) {
-    #pragma unroll
+#pragma unroll
                 for (int b = 0; b < 4; ++b)
                     if (4 * c + b < g.row_bytes)
                         w = (w & ~(0xFFu << (8 * b))) |
@@ -648,6 +723,16 @@ __device__ __forceinline__ void wg_lay_scales(const WgScales& g, int first) {
     }
 }
 
+// where the columns' sums go when there is one range of rows only: `fresh` gets the sum, db <- [db +] it
+struct WgDb {
+    float *fresh, *db;
+    bool accumulate;
+    __device__ __forceinline__ void store(uint64_t n, float s) const {
+        if (fresh) fresh[n] = s;
+        if (db) db[n] = accumulate ? db[n] + s : s;
+    }
+};
+
 // ---- column sums of dY: a block adds up a range of rows, a thread eight columns, or one where the
 // rows are not on 16-byte boundaries.  Blocks beyond the last range lay out the scales.
 constexpr int kWgSumBlocks = 256;        // ranges at most
@@ -655,7 +740,7 @@ constexpr int kWgSumBlocks = 256;        // ranges at most
 template <bool VECTOR>
 __global__ void __launch_bounds__(256)
 wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
-               const uint64_t lddy, float* __restrict__ parts, const int ranges,
+               const uint64_t lddy, float* __restrict__ parts, const int ranges, const WgDb last,
                const __grid_constant__ WgScales scales) {
     let_next_begin();
     if ((int)blockIdx.y >= ranges) {
@@ -700,7 +785,10 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
         float v = sums[0][c];
 #pragma unroll
         for (int g = 1; g < 8; ++g) v += sums[g][c];
-        parts[blockIdx.y * n + at] = v;
+        if (ranges == 1)
+            last.store(at, v);
+        else
+            parts[blockIdx.y * n + at] = v;
     }
 }
 
@@ -709,7 +797,7 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
 __global__ void __launch_bounds__(256)
 wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const uint64_t n,
                 const uint64_t lddy, __nv_bfloat16* __restrict__ copy, const uint64_t ldc,
-                float* __restrict__ parts, const int ranges,
+                float* __restrict__ parts, const int ranges, const WgDb last,
                 const __grid_constant__ WgScales scales) {
     let_next_begin();
     if ((int)blockIdx.y >= ranges) {
@@ -747,14 +835,19 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
         }
         __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < min(cols, 512u); c += 256) parts[blockIdx.y * n + first + c] = sums[c];
+    for (uint32_t c = threadIdx.x; c < min(cols, 512u); c += 256) {
+        if (ranges == 1)
+            last.store(first + c, sums[c]);
+        else
+            parts[blockIdx.y * n + first + c] = sums[c];
+    }
 }
 
 // db <- [db +] the parts' sum, in the order of the parts within each of 8 interleaved groups, then of
 // the groups; `fresh`, where wanted, gets the sum alone
 __global__ void __launch_bounds__(256)
 wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uint64_t n,
-                    float* fresh, float* db, const bool accumulate) {
+                    const WgDb last) {
     __shared__ float sums[8][33];
     let_next_begin();
     after_previous();
@@ -771,8 +864,7 @@ wg_sums_join_kernel(const float* __restrict__ parts, const int blocks, const uin
         s = sums[0][lane];
 #pragma unroll
         for (int k = 1; k < 8; ++k) s += sums[k][lane];
-        if (fresh) fresh[col] = s;
-        if (db) db[col] = accumulate ? db[col] + s : s;
+        last.store(col, s);
     }
 }
 
@@ -798,9 +890,11 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     p.whole = p.tiles - left;
     p.splits = splits < 1 ? 1 : (uint32_t)splits;
     // eight blocks for every SM in the column sums
-    const uint64_t across = (n + 255) / 256;
+    // (unaligned widths are copied as well: four rows a warp at least)
+    const uint64_t across = n % 8 ? (n + 511) / 512 : (n + 255) / 256, least = n % 8 && rows <= 1024 ? 32 : 64;
     uint64_t blocks = across ? 8 * 148 / across : 1;
-    if (blocks > (rows + 63) / 64) blocks = (rows + 63) / 64;
+    if (blocks > (rows + least - 1) / least) blocks = (rows + least - 1) / least;
+    if (n % 8 == 0 && rows <= 256) blocks = 1;       // no kernel to join ranges
     if (blocks > kWgSumBlocks) blocks = kWgSumBlocks;
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
     p.sum_offset = p.splits > 1 ? left * p.splits * kWgTile * kWgTile * 4 : 0;
@@ -863,7 +957,8 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     g.columns = 2 * p.tiles_k;
     g.across = (uint32_t)((g.columns + 31) / 32);
     g.pieces = g.token_pitch / 64 * g.across;
-    const int ranges = db || with_beta || copied ? p.sum_blocks : 0;
+    const int ranges = rows && (db || with_beta || copied) ? p.sum_blocks : 0;
+    const WgDb last = {with_beta ? fresh : nullptr, db, accumulate != 0};
     if (rows) {
         const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(dy);
         const bool vector = aligned && n % 8 == 0;
@@ -875,18 +970,17 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         if (copied) {
             __nv_bfloat16* copy = reinterpret_cast<__nv_bfloat16*>(ws + p.copy_offset);
             wg_align_kernel<<<grid, 256, 0, stream>>>(in, rows, n, lddy, copy, p.ldc, sums, ranges,
-                                                      g);
+                                                      last, g);
             dy = copy;
             lddy = p.ldc;
         } else if (down) {
             auto kernel = vector ? wg_sums_kernel<true> : wg_sums_kernel<false>;
-            kernel<<<grid, 256, 0, stream>>>(in, rows, n, lddy, sums, ranges, g);
+            kernel<<<grid, 256, 0, stream>>>(in, rows, n, lddy, sums, ranges, last, g);
         }
     }
-    if (db || with_beta)
+    if ((db || with_beta) && ranges != 1)
         launch_overlapping(wg_sums_join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(256), 0,
-                           stream, (const float*)sums, rows ? p.sum_blocks : 0, (uint64_t)n,
-                           with_beta ? fresh : (float*)nullptr, db, accumulate != 0);
+                           stream, (const float*)sums, rows ? p.sum_blocks : 0, (uint64_t)n, last);
     if (k == 0) return launch_status();
 
     WgArgs a = {};
