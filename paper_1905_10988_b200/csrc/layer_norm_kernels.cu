@@ -140,18 +140,17 @@ struct LnPlace {
 template <int CLUSTER>
 struct LnExchange {
     static constexpr int kSlots = CLUSTER > 1 ? 8 * CLUSTER : 8;      // of a row
-    float2* set[2];
-    uint32_t bars, bytes, parity;
+    float2* set;                         // of even rows; the other one lies `other` further on
+    uint32_t other, bars, bytes;
     // `slots`: [2][kSlots * groups], `words`: two barriers; all threads of the cluster call
     __device__ __forceinline__ void begin(float2* slots, uint64_t* words,
                                           const LnPlace<CLUSTER>& p) {
         const int all = kSlots * p.groups;
         for (int i = threadIdx.x; i < 2 * all; i += blockDim.x) slots[i] = make_float2(0.0f, 0.0f);
-        set[0] = slots + kSlots * p.group;
-        set[1] = set[0] + all;
+        set = slots + kSlots * p.group;
+        other = all;
         bars = smem_u32(words);
         bytes = 8 * CLUSTER * p.warps;
-        parity = 0;
         if (CLUSTER > 1 && threadIdx.x == 0) {
             mbar_init(bars, 1);
             mbar_init(bars + 8, 1);
@@ -165,7 +164,7 @@ struct LnExchange {
     // row number `turn` of the group (0, 1, 2, ...)
     __device__ __forceinline__ const float2* send(float2 mine, uint32_t turn,
                                                   const LnPlace<CLUSTER>& p) {
-        float2* slots = set[turn & 1];
+        float2* slots = set + (turn & 1 ? other : 0u);
         if constexpr (CLUSTER > 1) {
             const uint32_t bar = bars + 8 * (turn & 1);
             if (p.lane < CLUSTER)
@@ -379,7 +378,7 @@ static nc_status ln_launch(Kernel kernel, const LnDeal& d, int threads, uint64_t
 // Rows of a multiple of 1024 columns up to 8192 on 32-byte boundaries: 32 values a thread, half
 // the reductions a value, and no case to tell apart.
 template <typename T, int KEEP>
-__global__ void __launch_bounds__(kLnThreads, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kLnThreads, 2)
 ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads,
                           const __grid_constant__ PhiloxKeys keys) {
     __shared__ float2 slots[2 * 8 * 8];
@@ -487,14 +486,18 @@ static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
         LnDeal d;
         d.cluster = 1;
         d.G = (int)(a.cols / 32);
-        d.groups = kLnThreads / d.G;
+        // blocks of 128 threads where rows allow it: four of them leave the registers that a thread
+        // needs (three blocks of 256 with 80 registers: 70 instead of 63 us for 16384 x 4096; four-byte
+        // values, twice the registers ahead: 55 with blocks of 256, 59 with blocks of 128)
+        const int block = sizeof(T) == 4 ? kLnThreads : 128;
+        d.groups = d.G < block ? block / d.G : 1;
         d.owners = (a.rows + d.groups - 1) / d.groups;
         const size_t smem = 4 * 16 * d.G * sizeof(float);
         static bool allowed[64];
         if (!allow_dynamic_smem((const void*)ln_forward_regular_kernel<T, KEEP>,
                                 4 * 16 * kLnThreads * sizeof(float), allowed))
             return NC_ERR_CUDA;
-        return ln_launch(ln_forward_regular_kernel<T, KEEP>, d, sizeof(T) == 4 ? 512 : 768,
+        return ln_launch(ln_forward_regular_kernel<T, KEEP>, d, 512,
                          (uint64_t)1 << 30, smem, nullptr, stream, a, d.G,
                          make_philox_keys(a.seed));
     }
