@@ -221,8 +221,14 @@ struct LnForward {
 // Every warp sums up its own values and their squared distances from its own mean; one exchange
 // later the row's mean and variance follow from these (the squared distances about the common
 // mean are the warps' own plus n_w (mean_w - mean)^2).  A row is read ahead.
+// Four-byte values that are not kRegular do not fit 64 registers a thread with a row ahead, so they
+// get 80 and three blocks an SM (binary32 with checkpoint, 4097 x 4099: 78 -> 47 us, 40000 x 1001:
+// 80 -> 74); two-byte values fit (bfloat16 30000 x 1001: 52 us with four blocks, 58 with three).
+template <typename T, int MODE>
+constexpr int kLnForwardBlocks = sizeof(T) == 4 && MODE != kRegular ? 3 : 4;
+
 template <typename T, int MODE, int KEEP, int CLUSTER>
-__global__ void __launch_bounds__(kLnThreads, 4)
+__global__ void __launch_bounds__(kLnThreads, kLnForwardBlocks<T, MODE>)
 ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
                   const __grid_constant__ PhiloxKeys keys) {
     __shared__ float2 slots[2 * LnExchange<CLUSTER>::kSlots * (CLUSTER > 1 ? 1 : 8)];
@@ -524,7 +530,9 @@ static nc_status ln_forward_go(const LnForward& a, cudaStream_t stream) {
         !allow_dynamic_smem((const void*)kernel, 2 * 16 * kLnThreads * sizeof(float),
                             allowed[31 - __builtin_clz((unsigned)d.cluster)]))
         return NC_ERR_CUDA;
-    return ln_launch(kernel, d, 1024, (uint64_t)1 << 30, smem, nullptr, stream, a, d.G,
+    const int most = ln_regular(d, a.cols, a.access) ? kLnForwardBlocks<T, kRegular>
+                                                     : kLnForwardBlocks<T, kVector>;
+    return ln_launch(kernel, d, kLnThreads * most, (uint64_t)1 << 30, smem, nullptr, stream, a, d.G,
                      make_philox_keys(a.seed));
 }
 
@@ -590,7 +598,6 @@ struct LnRow {
     Raw16<T> x;                          // !SAVED8
     uint4 codes;                         // SAVED8
     uint32_t scale;
-    Raw16<T> dres;                       // RES
     float mean, rstd;
 };
 
@@ -637,8 +644,6 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             } else {
                 row_load<T, MODE>(x + row * a.ldx, p.tid, p.cols, a.wide, r.x);
             }
-            if constexpr (RES)
-                row_load<T, MODE>(dres + row * a.lddres, p.tid, p.cols, a.wide, r.dres);
         }
     };
     // one thread: the group's part of a row into stage `s`
@@ -711,7 +716,10 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             for (int i = 0; i < 8; ++i) xh[i] = pair_of(f[2 * i], f[2 * i + 1]);
         }
         Raw16<T> late;
-        if constexpr (RES && !kRing) late = next.dres;
+        // issued here, not with the row ahead: the registers it would hold meanwhile cost more than its
+        // latency (binary32 40000 x 1001: 207 -> 150 us, bfloat16 30000 x 1001: 119 -> 97)
+        if constexpr (RES && !kRing)
+            row_load<T, MODE>(dres + row * a.lddres, p.tid, p.cols, a.wide, late);
         if (row + p.step < a.rows) load(row + p.step, next);
         f32x2 s1 = 0, s2 = 0, gamma[8];
         ln_params(table, p.G, p.tid, gamma);
