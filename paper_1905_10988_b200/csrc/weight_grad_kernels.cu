@@ -696,16 +696,21 @@ struct WgScales {
     uint64_t pieces;                     // of 64 tokens x 32 columns
 };
 
-// blocks from row `first` of the grid on take the pieces in turn
-__device__ __forceinline__ void wg_lay_scales(const WgScales& g, int first) {
+// the blocks of `down` rows of the grid, this one in row `y` of them, take the pieces in turn
+__device__ __forceinline__ void wg_lay_scales(const WgScales& g, int y, int down) {
     __shared__ uint32_t words[32][65];
-    for (uint64_t piece = (uint64_t)(blockIdx.y - first) * gridDim.x + blockIdx.x; piece < g.pieces;
-         piece += (uint64_t)(gridDim.y - first) * gridDim.x) {
+    const bool whole = g.row_bytes % 4 == 0;                         // words of a row: one access
+    for (uint64_t piece = (uint64_t)y * gridDim.x + blockIdx.x; piece < g.pieces;
+         piece += (uint64_t)down * gridDim.x) {
         const uint64_t t0 = piece / g.across * 64, c0 = piece % g.across * 32;
+#pragma unroll 4
         for (int i = threadIdx.x; i < 64 * 32; i += 256) {
             const uint64_t t = t0 + i / 32, c = c0 + i % 32;
             uint32_t w = 0x7F7F7F7Fu;
-            if (t < g.rows) {
+            if (whole) {
+                if (t < g.rows && 4 * c < g.row_bytes)
+                    w = __ldg(reinterpret_cast<const uint32_t*>(g.in + t * g.row_bytes + 4 * c));
+            } else if (t < g.rows) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     if (4 * c + b < g.row_bytes)
@@ -734,7 +739,8 @@ struct WgDb {
 };
 
 // ---- column sums of dY: a block adds up a range of rows, a thread eight columns, or one where the
-// rows are not on 16-byte boundaries.  Blocks beyond the last range lay out the scales.
+// rows are not on 16-byte boundaries.  The blocks of the grid's first rows lay out the scales (as its
+// last blocks they came after a full wave: 8192 x 4096 x 1024 took 111 instead of 107 us).
 constexpr int kWgSumBlocks = 256;        // ranges at most
 
 template <bool VECTOR>
@@ -743,31 +749,40 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
                const uint64_t lddy, float* __restrict__ parts, const int ranges, const WgDb last,
                const __grid_constant__ WgScales scales) {
     let_next_begin();
-    if ((int)blockIdx.y >= ranges) {
-        wg_lay_scales(scales, ranges);
+    const int down = gridDim.y - ranges, range = (int)blockIdx.y - down;
+    if (range < 0) {
+        wg_lay_scales(scales, blockIdx.y, down);
         return;
     }
     constexpr int W = VECTOR ? 8 : 1;
     __shared__ float sums[8][32 * W + 1];
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const uint64_t col = ((uint64_t)blockIdx.x * 32 + lane) * W;
-    const uint64_t begin = rows * blockIdx.y / ranges, end = rows * (blockIdx.y + 1) / ranges;
+    const uint64_t begin = rows * range / ranges, end = rows * (range + 1) / ranges;
     float s[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) s[i] = 0.0f;
     if (col < n) {
         const __nv_bfloat16* p = dy + col;
         if constexpr (VECTOR) {
-#pragma unroll 8
-            for (uint64_t t = begin + group; t < end; t += 8) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + t * lddy));
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (uint64_t t = begin + group; t < end; t += 32) {     // four loads in flight
+                uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float e, f;
-                    unpack2<__nv_bfloat16>(w[i], e, f);
-                    s[2 * i] += e;
-                    s[2 * i + 1] += f;
+                for (int u = 0; u < 4; ++u) {
+                    v[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (t + 8 * u < end)
+                        v[u] = __ldg(reinterpret_cast<const uint4*>(p + (t + 8 * u) * lddy));
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float e, f;
+                        unpack2<__nv_bfloat16>(w[i], e, f);
+                        s[2 * i] += e;
+                        s[2 * i + 1] += f;
+                    }
                 }
             }
         } else {
@@ -788,7 +803,7 @@ wg_sums_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const 
         if (ranges == 1)
             last.store(at, v);
         else
-            parts[blockIdx.y * n + at] = v;
+            parts[range * n + at] = v;
     }
 }
 
@@ -800,15 +815,16 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
                 float* __restrict__ parts, const int ranges, const WgDb last,
                 const __grid_constant__ WgScales scales) {
     let_next_begin();
-    if ((int)blockIdx.y >= ranges) {
-        wg_lay_scales(scales, ranges);
+    const int range = blockIdx.y;        // the scales last here, in the shadow of the longer copies
+    if (range >= ranges) {
+        wg_lay_scales(scales, range - ranges, gridDim.y - ranges);
         return;
     }
     __shared__ float sums[512];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint64_t first = (uint64_t)blockIdx.x * 512;
     const uint32_t cols = (uint32_t)min(n - first, (uint64_t)1024);
-    const uint64_t begin = rows * blockIdx.y / ranges, end = rows * (blockIdx.y + 1) / ranges;
+    const uint64_t begin = rows * range / ranges, end = rows * (range + 1) / ranges;
     float s[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
@@ -839,7 +855,7 @@ wg_align_kernel(const __nv_bfloat16* __restrict__ dy, const uint64_t rows, const
         if (ranges == 1)
             last.store(first + c, sums[c]);
         else
-            parts[blockIdx.y * n + first + c] = sums[c];
+            parts[range * n + first + c] = sums[c];
     }
 }
 
