@@ -414,18 +414,24 @@ __device__ __forceinline__ uint32_t max_bits16(const float (&v)[16]) {
     return __float_as_uint(max3_abs(a, v[15], v[15]));
 }
 
-// codes of sixteen neighbouring values, one half of the block whose scale byte is `scale`;
-// `q` is the index of these sixteen codes in the code plane, which is also their generator block
+// the sixteen stream bytes of the sixteen codes with index q of the code plane, q < 2^32
 template <bool RANDOM>
-__device__ __forceinline__ uint4 act8_sixteen(const float (&v)[16], uint32_t scale, uint64_t q,
-                                              uint32_t worker, const PhiloxKeys& keys) {
+__device__ __forceinline__ uint4 act8_draws(uint32_t q, uint32_t worker, const PhiloxKeys& keys) {
+    uint32_t r[4] = {0u, 0u, 0u, 0u};
+    if (RANDOM) philox4x32_10(q, 0u, worker, kDomainAct8, keys, r);
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// codes of sixteen neighbouring values, one half of the block whose scale byte is `scale`
+template <bool RANDOM>
+__device__ __forceinline__ uint4 act8_sixteen(const float (&v)[16], uint32_t scale,
+                                              const uint4& draws) {
     if (scale == kAct8Nan) return make_uint4(0u, 0u, 0u, 0u);
     const float inverse = act8_inverse(scale, RANDOM);
-    uint32_t r[4] = {0u, 0u, 0u, 0u};
-    if (RANDOM) stream_words4(q, worker, kDomainAct8, keys, r);
-    return make_uint4(act8_four<RANDOM>(v, inverse, r[0]), act8_four<RANDOM>(v + 4, inverse, r[1]),
-                      act8_four<RANDOM>(v + 8, inverse, r[2]),
-                      act8_four<RANDOM>(v + 12, inverse, r[3]));
+    return make_uint4(act8_four<RANDOM>(v, inverse, draws.x),
+                      act8_four<RANDOM>(v + 4, inverse, draws.y),
+                      act8_four<RANDOM>(v + 8, inverse, draws.z),
+                      act8_four<RANDOM>(v + 12, inverse, draws.w));
 }
 
 // ---- decoder ---------------------------------------------------------------------------------

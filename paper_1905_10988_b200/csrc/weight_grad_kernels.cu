@@ -25,6 +25,9 @@
 // The tiles are dealt out evenly to the chip's 74 pairs, double ones while there are rounds of
 // them, then single ones.  What is left over, fewer tiles than pairs, is split along the tokens,
 // and a second kernel adds its binary32 parts in order.
+//
+// 16384 x 4096 x 4096: the product 390 us (1.41 PFLOP/s, the tensor pipe active 77 % of the cycles;
+// 400 to 445 us back to back, where the power cap lowers the clock), all kernels 440 to 490 us.
 #include "act8_common.cuh"
 #include "tensor_core.cuh"
 
