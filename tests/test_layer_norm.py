@@ -140,6 +140,8 @@ def layout(name, cols, size):
         return cols, 0
     if name == "gap16":                       # rows on 16-byte boundaries, some not on 32
         return -(-cols // 8) * 8 + 16 // size + (8 if size == 2 else 4), 16 // size
+    if name == "gap32":                       # rows on 32-byte boundaries
+        return cols + 32 // size, 32 // size
     return cols + 1, 1
 
 
@@ -278,6 +280,29 @@ def test_gpu_backward(kind, pkind, where, rows, cols, saved8):
         tb = (chain + 1) * U * ady.sum(0) + U * np.abs(base + wdb)
         assert np.all(np.abs(dgamma.numpy(np.float32) - (base + wdg)) <= tg + 1e-45)
         assert np.all(np.abs(dbeta.numpy(np.float32) - (base + wdb)) <= tb + 1e-45)
+
+
+# several rows an owner: rows whose values fill every thread (32 a thread forward; backward through
+# the ring, which comes round), of a warp, a block or a cluster, and such that do not
+MANY = [(5000, 512), (2500, 1024), (520, 2048), (1300, 4096), (600, 5120), (700, 7168), (700, 8192),
+        (513, 8200), (1500, 1001), (700, 4099)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,pkind,where", [("f32", "f32", "gap32"), ("bf16", "bf16", "whole"),
+                                              ("f16", "f32", "gap32")])
+@pytest.mark.parametrize("rows,cols", MANY)
+def test_gpu_forward_many_rows(kind, pkind, where, rows, cols):
+    test_gpu_forward(kind, pkind, where, rows, cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,pkind,where", [("f32", "f32", "gap32"), ("bf16", "bf16", "whole"),
+                                              ("f16", "f32", "gap32")])
+@pytest.mark.parametrize("rows,cols", MANY)
+@pytest.mark.parametrize("saved8", [False, True])
+def test_gpu_backward_many_rows(kind, pkind, where, rows, cols, saved8):
+    test_gpu_backward(kind, pkind, where, rows, cols, saved8)
 
 
 @pytest.mark.gpu
