@@ -971,7 +971,7 @@ using namespace natcomp;
 extern "C" {
 
 size_t nc_layer_norm_workspace_bytes(size_t rows, size_t cols) {
-    if (cols > kLnMaxCols) return 0;                 // refused by the calls
+    if (cols == 0 || cols > kLnMaxCols) return 0;    // nothing to do; refused by the calls
     const uint64_t owners = ln_deal(rows, cols).owners;
     return (owners < (uint64_t)kLnMaxParts ? owners : (uint64_t)kLnMaxParts) * 2 *
            act8_pitch(cols) * sizeof(float);

@@ -6,6 +6,10 @@ kernels is a serial chain of at most 32 terms a thread, 5 shuffle steps and at m
 it is off by at most 101 u times the sum of the terms' magnitudes; parameter gradients have a
 chain of the rows of an owner and of the owners' parts instead.  Every other operation adds one u
 of its result."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -113,6 +117,16 @@ def test_workspace_size():
     assert nc.nc_layer_norm_workspace_bytes(0, 64) == 0
     assert nc.nc_layer_norm_workspace_bytes(1, 33) == 2 * 64 * 4
     assert nc.nc_layer_norm_workspace_bytes(10 ** 6, 4096) <= 592 * 2 * 4096 * 4
+
+
+def test_workspace_of_no_columns():
+    # asked for before a call that has nothing to do; in a process of its own, which a division by
+    # zero in the library would end
+    code = ("import paper_1905_10988_b200 as nc\n"
+            "assert nc.nc_layer_norm_workspace_bytes(4, 0) == 0\n"
+            "assert nc.nc_layer_norm_workspace_bytes(0, 0) == 0\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert subprocess.run([sys.executable, "-c", code], cwd=root).returncode == 0
 
 
 # ---- GPU ------------------------------------------------------------------------------------
