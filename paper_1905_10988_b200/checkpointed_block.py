@@ -37,14 +37,37 @@ class Checkpoint:
         return self.codes.numel() + self.scales.numel()
 
     def keep(self, x, rounding, seed, worker) -> None:
-        nc.nc_act8_compress(x, nc.DTYPE_BF16, self.rows, self.cols, x.stride(0), rounding, seed,
-                            worker, self.codes, self.scales)
+        """x: bfloat16 rows x cols."""
+        ldx = _row_stride("x", x, self.rows, self.cols, torch.bfloat16, self.codes.device)
+        nc.nc_act8_compress(x, nc.DTYPE_BF16, self.rows, self.cols, ldx, rounding, seed, worker,
+                            self.codes, self.scales)
 
     def read(self):
         out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16, device=self.codes.device)
         nc.nc_act8_decompress(self.codes, self.scales, self.rows, self.cols, out, nc.DTYPE_BF16,
                               self.cols)
         return out
+
+
+def _row_stride(name: str, x, rows: int, cols: int, dtype, device) -> int:
+    """The row stride of a matrix that the kernels may read as rows x cols of `dtype` on `device`;
+    ValueError for any other.  The library sees an address and a stride only."""
+    if x.dtype != dtype:
+        raise ValueError("%s is %s, not %s" % (name, x.dtype, dtype))
+    if tuple(x.shape) != (rows, cols):
+        raise ValueError("%s has shape %s, not %s" % (name, tuple(x.shape), (rows, cols)))
+    if (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
+        raise ValueError("%s has strides %s: rows of neighbouring values, one behind the other, are "
+                         "needed" % (name, tuple(x.stride())))
+    _on_device(name, x, device)
+    return x.stride(0) if rows > 1 else cols
+
+
+def _on_device(name: str, x, device) -> None:
+    if x.device.type != "cuda" or x.device != device:
+        raise ValueError("%s is on %s, not on the block's GPU (%s)" % (name, x.device, device))
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, which is not the current device" % (name, x.device))
 
 
 def _gelu_and_slope(h):
@@ -72,6 +95,7 @@ class CheckpointedBlock:
         self.before = Checkpoint(tokens, hidden, device)      # the activation function's inputs
         self.after = Checkpoint(tokens, hidden, device)       # and outputs
         self.rstd = torch.empty(tokens, dtype=torch.float32, device=device)
+        self.kept = False                                     # the checkpoints hold a forward pass
         # one fp32 vector for all gradients, every piece on a 32-byte boundary
         self.slices, at = {}, 0
         for name in self.NAMES:
@@ -91,23 +115,29 @@ class CheckpointedBlock:
     def forward(self, x, seed: int = 0, worker: int = 0):
         """x: bfloat16 tokens x width.  seed and worker draw the checkpoints' rounding."""
         t, w = self.tokens, self.width
+        ldx = _row_stride("x", x, t, w, torch.bfloat16, self.rstd.device)
         a = torch.empty(t, w, dtype=torch.bfloat16, device=x.device)
-        nc.nc_layer_norm_forward(x, nc.DTYPE_BF16, t, w, x.stride(0), self.gamma, self.beta,
-                                 nc.DTYPE_BF16, EPS, a, w, None, self.rstd, self.normed.codes,
-                                 self.normed.scales, self.rounding, seed, 3 * worker)
+        nc.nc_layer_norm_forward(x, nc.DTYPE_BF16, t, w, ldx, self.gamma, self.beta, nc.DTYPE_BF16,
+                                 EPS, a, w, None, self.rstd, self.normed.codes, self.normed.scales,
+                                 self.rounding, seed, 3 * worker)
         h = torch.addmm(self.b1, a, self.w1.t())
         self.before.keep(h, self.rounding, seed, 3 * worker + 1)
         u = _gelu_and_slope(h)[0].bfloat16()
         self.after.keep(u, self.rounding, seed, 3 * worker + 2)
+        self.kept = True
         return x + torch.addmm(self.b2, u, self.w2.t())
 
     def backward(self, dy, gradient, accumulate: bool = False):
         """dy: bfloat16 tokens x width.  Writes all parameters' gradients into the fp32 vector
         `gradient` (gradient_size entries) and returns the gradient of x."""
         t, w, k = self.tokens, self.width, self.hidden
+        lddy = _row_stride("dy", dy, t, w, torch.bfloat16, self.rstd.device)
+        self._check_gradient(gradient)
+        if not self.kept:
+            raise RuntimeError("no forward pass has kept activations for this one")
         piece = {name: gradient[at:at + n] for name, (at, n) in self.slices.items()}
         f32, bf16 = nc.DTYPE_F32, nc.DTYPE_BF16
-        nc.nc_act8_weight_grad(dy, t, w, dy.stride(0), self.after.codes, self.after.scales, k, None,
+        nc.nc_act8_weight_grad(dy, t, w, lddy, self.after.codes, self.after.scales, k, None,
                                None, bf16, piece["w2"], f32, k, piece["b2"], accumulate,
                                self.workspace, self.ws_bytes)
         slope = _gelu_and_slope(self.before.read())[1]
@@ -118,10 +148,18 @@ class CheckpointedBlock:
         da = torch.mm(dh, self.w1)
         dx = torch.empty(t, w, dtype=torch.bfloat16, device=dy.device)
         nc.nc_act8_layer_norm_backward(da, bf16, t, w, w, self.normed.codes, self.normed.scales,
-                                       self.rstd, self.gamma, bf16, dy, dy.stride(0), dx, w,
-                                       piece["gamma"], piece["beta"], accumulate, self.workspace,
-                                       self.ws_bytes)
+                                       self.rstd, self.gamma, bf16, dy, lddy, dx, w, piece["gamma"],
+                                       piece["beta"], accumulate, self.workspace, self.ws_bytes)
         return dx
+
+    def _check_gradient(self, gradient) -> None:
+        size = self.gradient_size
+        if gradient.dtype != torch.float32 or gradient.dim() != 1 or gradient.numel() < size:
+            raise ValueError("gradient is %s %s, not a torch.float32 vector of %d entries"
+                             % (gradient.dtype, tuple(gradient.shape), size))
+        if gradient.stride(0) != 1:
+            raise ValueError("gradient has a stride of %d" % gradient.stride(0))
+        _on_device("gradient", gradient, self.rstd.device)
 
     def apply(self, gradient, rate: float) -> None:
         """Plain gradient descent with the (aggregated) fp32 gradient vector."""
