@@ -103,6 +103,8 @@ class CheckpointedBlock:
             self.slices[name] = (at, n)
             at += -(-n // 8) * 8
         self.gradient_size = at
+        # what lies between the pieces: (begin, end)
+        self.gaps = [(at + n, at + -(-n // 8) * 8) for at, n in self.slices.values() if n % 8]
         self.ws_bytes = max(nc.nc_layer_norm_workspace_bytes(tokens, width),
                             nc.nc_act8_weight_grad_workspace_bytes(tokens, hidden, width),
                             nc.nc_act8_weight_grad_workspace_bytes(tokens, width, hidden))
@@ -129,12 +131,14 @@ class CheckpointedBlock:
 
     def backward(self, dy, gradient, accumulate: bool = False):
         """dy: bfloat16 tokens x width.  Writes all parameters' gradients into the fp32 vector
-        `gradient` (gradient_size entries) and returns the gradient of x."""
+        `gradient` (gradient_size entries; 0 between the pieces) and returns the gradient of x."""
         t, w, k = self.tokens, self.width, self.hidden
         lddy = _row_stride("dy", dy, t, w, torch.bfloat16, self.rstd.device)
         self._check_gradient(gradient)
         if not self.kept:
             raise RuntimeError("no forward pass has kept activations for this one")
+        for begin, end in self.gaps:         # the compressors read them, and norms count them
+            gradient[begin:end].zero_()
         piece = {name: gradient[at:at + n] for name, (at, n) in self.slices.items()}
         f32, bf16 = nc.DTYPE_F32, nc.DTYPE_BF16
         nc.nc_act8_weight_grad(dy, t, w, lddy, self.after.codes, self.after.scales, k, None,

@@ -81,3 +81,25 @@ def test_gpu_views_and_single_tokens_give_what_whole_rows_give():
             grad = torch.zeros(b.gradient_size, device="cuda")
             outs.append((b.forward(u), b.backward(v, grad), grad))
         assert all(torch.equal(p, q) for p, q in zip(*outs))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width,hidden", [(100, 50), (20, 13), (64, 64)])
+def test_gpu_every_entry_of_the_gradient_vector_is_written(width, hidden):
+    # what lies between the pieces goes to the compressors as well: an inf or NaN there would set
+    # the norm of a whole bucket
+    b = CheckpointedBlock(T, width, hidden)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(T, width, generator=g, device="cuda").bfloat16()
+    b.forward(x)
+    between = torch.ones(b.gradient_size, dtype=torch.bool, device="cuda")
+    for at, n in b.slices.values():
+        between[at:at + n] = False
+    for accumulate in (False, True):
+        grad = torch.full((b.gradient_size + 3,), float("nan"), device="cuda")
+        if accumulate:
+            grad[:b.gradient_size][~between] = 0.0
+        b.backward(x, grad, accumulate)
+        assert bool(torch.isfinite(grad[:b.gradient_size]).all())
+        assert not bool(grad[:b.gradient_size][between].any())
+        assert bool(torch.isnan(grad[b.gradient_size:]).all())
