@@ -1005,7 +1005,9 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     WgArgs a = {};
     a.dy = static_cast<const __nv_bfloat16*>(dy);
     a.rows = rows; a.n = n; a.lddy = lddy; a.k = k; a.scales = g.out;
-    a.token_pitch = p.token_pitch; a.gamma = gamma; a.beta = with_beta ? beta : nullptr;
+    a.token_pitch = p.token_pitch;
+    a.gamma = rows ? gamma : nullptr;        // no tokens: 0, not 0 * gamma
+    a.beta = with_beta ? beta : nullptr;
     a.param_dtype = param_dtype; a.dw = dw; a.dw_f32 = dw_dtype == NC_DTYPE_F32; a.lddw = lddw;
     a.db = fresh; a.accumulate = accumulate;
     a.vector = row_access(dw, lddw, wbytes, n) != kRowElement;

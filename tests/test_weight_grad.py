@@ -242,3 +242,17 @@ def test_gpu_repeatable_and_on_another_stream():
         outs.append((dw, db))
     for o in outs[1:]:
         assert all(torch.equal(p, q) for p, q in zip(o, outs[0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gpu_no_tokens_give_zero_whatever_the_parameters_are(accumulate):
+    # a sum over no tokens has no term that an inf or NaN parameter could reach
+    dw = torch.full((3, 40), 2.0, device="cuda")
+    db = torch.full((3,), 4.0, device="cuda")
+    gamma = torch.full((40,), float("inf"), device="cuda")
+    beta = torch.full((40,), float("nan"), device="cuda")
+    F = nc.DTYPE_F32
+    nc.nc_act8_weight_grad(None, 0, 3, 3, None, None, 40, gamma, beta, F, dw, F, 40, db, accumulate,
+                           None, 0)
+    assert bool((dw == (2 if accumulate else 0)).all()) and bool((db == (4 if accumulate else 0)).all())
