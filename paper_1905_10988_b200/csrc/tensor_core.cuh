@@ -57,6 +57,19 @@ __device__ __forceinline__ void st_async_pair(uint32_t dst, uint32_t bar, uint32
                  : "memory");
 }
 
+// a word at the same place in block `rank` of the cluster
+__device__ __forceinline__ void shared_store_at(uint32_t at, uint32_t rank, uint32_t v) {
+    asm volatile("{\n\t"
+                 ".reg .b32 remote;\n\t"
+                 "mapa.shared::cluster.u32 remote, %0, %1;\n\t"
+                 "st.shared::cluster.u32 [remote], %2;\n\t"
+                 "}" ::"r"(at), "r"(rank), "r"(v)
+                 : "memory");
+}
+
+// the stores of this thread are visible in the cluster before what it does next
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n\t"
@@ -118,6 +131,12 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                                           uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes"
                  " [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void shared_store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
+                                               uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
                  : "memory");
 }
 

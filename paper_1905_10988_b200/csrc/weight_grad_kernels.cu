@@ -203,11 +203,6 @@ __device__ __forceinline__ void wg_decode(const uint32_t (&w)[4], uint32_t scale
     }
 }
 
-__device__ __forceinline__ void wg_put(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
-                 : "memory");
-}
-
 // eight values of a dY row at any element
 __device__ __forceinline__ uint4 wg_load_dy8(const WgArgs& a, uint64_t t, uint64_t n) {
     uint32_t v[4] = {0u, 0u, 0u, 0u};
@@ -400,8 +395,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t at = line + i * (16 * 128);
-                wg_put(at + (chunk << 4), v[i][0], v[i][1], v[i][2], v[i][3]);
-                wg_put(at + ((chunk ^ 1) << 4), v[i][4], v[i][5], v[i][6], v[i][7]);
+                shared_store16(at + (chunk << 4), v[i][0], v[i][1], v[i][2], v[i][3]);
+                shared_store16(at + ((chunk ^ 1) << 4), v[i][4], v[i][5], v[i][6], v[i][7]);
             }
             fence_async_proxy();
             __syncwarp();
@@ -568,6 +563,14 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                     mma_commit_pair(done, elected);
                     here = __all_sync(0xFFFFFFFFu, mbar_test(ready + 8 * stage, parity));
                 }
+                // given up: both blocks know before their writers hear that the tile is complete, for
+                // what stands in TMEM is the sum of some of the steps
+                if (!ok && elected) {
+                    shared_store_at(smem_u32(words + 1), 0, 1);
+                    shared_store_at(smem_u32(words + 1), 1, 1);
+                    fence_cluster();
+                }
+                __syncwarp();
                 for (uint32_t h = 0; h < w.halves; ++h)
                     mma_commit_pair(full + 8 * turns.of(w, h), elected);
                 turns.done(w);
@@ -604,10 +607,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t token = token0 + 8 * j;
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                 dst + token * 128 + (((chunk & 7) ^ (token & 7)) << 4)),
-                             "r"(v[j].x), "r"(v[j].y), "r"(v[j].z), "r"(v[j].w)
-                             : "memory");
+                shared_store16(dst + token * 128 + (((chunk & 7) ^ (token & 7)) << 4), v[j].x, v[j].y,
+                               v[j].z, v[j].w);
                 if (walk.more())
                     v[j] = wg_load_dy8(a, walk.token() + token,
                                        walk.unit.n0 + rank * kWgHalf + 8 * chunk);

@@ -1,0 +1,84 @@
+"""The weight gradient's kernels thread by thread on the host (tests/device_model): their schedule with
+few pairs of blocks, the bounds of every access, and waits that run out of time.  The values are
+compared with a product in 64 bits; the address sanitizer checks global and shared memory; copies and
+matrix instructions take effect late and in changing order; a wait that nothing ends, a barrier that
+gets too many arrivals or a copy in flight at a block's end is an error."""
+import os
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+MODEL = os.path.join(HERE, "device_model")
+sys.path.insert(0, MODEL)
+
+import translate  # noqa: E402
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no C++ compiler")
+
+
+def build(folder, name, pairs=2, change=None):
+    source, program = str(folder / (name + ".cpp")), str(folder / name)
+    with open(os.path.join(MODEL, name + ".cpp")) as f:
+        main = f.read()
+    with open(source, "w") as f:
+        f.write(translate.translate([name + "_kernels.cu"], pairs, change) + main)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.run(["g++", "-std=c++20", "-O1", "-g1", "-w", "-ffp-contract=off", "-fsanitize=address",
+                    "-I" + MODEL, "-I" + os.path.join(translate.ROOT, "include"),
+                    "-I" + os.path.join(cuda, "include"), "-o", program, source], check=True)
+    return program
+
+
+def run(program, *args):
+    got = subprocess.run([program] + [str(a) for a in args], capture_output=True, text=True,
+                         timeout=300)
+    assert got.returncode == 0 and got.stdout.startswith("ok"), got.stdout + got.stderr[-2000:]
+    return got.stdout
+
+
+@pytest.fixture(scope="module")
+def weight_grad(tmp_path_factory):
+    return build(tmp_path_factory.mktemp("model"), "weight_grad")
+
+
+# rows, n, k, layout of dY, type of dW, affine, accumulate: less than a step and a ragged one; single
+# tiles, split ones, double ones, double then single, an odd number of tiles along n; rows of dY on
+# 16-byte boundaries, beside them, and through the aligned copy; no tokens
+CASES = [(1, 1, 1, "whole", "f32", 0, 0), (70, 40, 33, "whole", "f32", 1, 0),
+         (300, 260, 300, "gap", "bf16", 1, 1), (130, 512, 520, "whole", "f32", 1, 0),
+         (130, 601, 520, "any", "f32", 1, 1), (65, 600, 300, "any", "bf16", 0, 0),
+         (700, 256, 256, "whole", "bf16", 1, 0), (200, 1300, 520, "any", "f32", 1, 0),
+         (520, 1032, 300, "gap", "f32", 0, 1), (0, 5, 40, "whole", "f32", 1, 1),
+         (700, 300, 1030, "whole", "f32", 1, 0)]
+
+
+@pytest.mark.parametrize("case", CASES, ids=["-".join(map(str, c)) for c in CASES])
+def test_values_and_bounds(weight_grad, case):
+    run(weight_grad, *case, 1)
+
+
+@pytest.mark.parametrize("seed", [1, 2])
+@pytest.mark.parametrize("hold", [None, 0, 1])
+@pytest.mark.parametrize("rank", [0, 1])
+def test_a_wait_that_runs_out_leaves_nan_and_no_partial_sums(weight_grad, rank, hold, seed):
+    # a copy of one block's second tile never arrives.  Whichever block's wait ends first, and also
+    # where the other block's writers begin to wait late: a value is complete or NaN, and the kernel ends
+    args = ["drop_rank=%d" % rank, "drop_nth=4"]
+    if hold is not None:
+        args += ["hold_rank=%d" % hold, "hold_after=100", "hold_until=3500000000"]
+    run(weight_grad, 192, 256, 1024, "whole", "f32", 1, 0, seed, *args)
+
+
+@pytest.mark.parametrize("old,new", [
+    ("step < kWgSlots || wg_wait_step(empty, step - kWgSlots, gave_up)", "true"),
+    ("if (before) ok = wg_wait_step(empty, before - 1, gave_up);", "")])
+def test_the_model_sees_a_wait_that_is_missing(tmp_path, old, new):
+    def without(name, text):
+        assert name != "weight_grad_kernels.cu" or text.count(old) == 1
+        return text.replace(old, new)
+    program = build(tmp_path, "weight_grad", change=without)
+    with pytest.raises(AssertionError):
+        run(program, 700, 300, 300, "whole", "f32", 1, 0, 1)
