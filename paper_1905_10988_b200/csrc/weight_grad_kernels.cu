@@ -36,9 +36,15 @@ namespace natcomp {
 constexpr int kWgTile = 256;             // n and k of a pair's tile
 constexpr int kWgHalf = 128;             // of a block
 constexpr int kWgStep = 64;              // tokens
-constexpr int kWgStages = 6;             // steps that barriers tell apart, places of dY tiles
+constexpr int kWgPlaces = 6;             // places of dY tiles
 constexpr int kWgSlots = 5;              // places of codes and of decoded tiles
 constexpr int kWgGroups = 4, kWgGroupWarps = 4;      // decoders
+// Steps that barriers tell apart.  A wait by parity cannot tell a phase from the one before the last,
+// so whoever waits for a step must know that the step which used the barrier before is over: a
+// decoding group has waited for that one itself, because it takes every fourth step and the barrier
+// comes round after a multiple of four.
+constexpr int kWgRing = 8;
+static_assert(kWgRing % kWgGroups == 0 && kWgRing >= kWgPlaces && kWgRing >= kWgSlots, "");
 constexpr int kWgWriters = 4, kWgLoaders = 4;        // warps
 constexpr int kWgCopyWarp = kWgWriters, kWgCodeWarp = kWgWriters + 1, kWgMmaWarp = kWgWriters + 2;
 constexpr int kWgDecodeWarp = kWgWriters + 4;        // the first of them, a multiple of four
@@ -47,7 +53,7 @@ constexpr uint32_t kWgPanel = kWgStep * 128;         // bytes of 64 values x 64 
 constexpr uint32_t kWgOperand = 2 * kWgPanel;        // of a block's half
 constexpr uint32_t kWgCodeBytes = kWgStep * 128, kWgScaleBytes = kWgStep * 4;
 // shared memory: dY tiles, decoded tiles, codes, scales, barriers, gamma and beta
-constexpr uint32_t kWgDecoded = kWgStages * kWgOperand;
+constexpr uint32_t kWgDecoded = kWgPlaces * kWgOperand;
 constexpr uint32_t kWgCodes = kWgDecoded + kWgSlots * kWgOperand;
 constexpr uint32_t kWgScales = kWgCodes + kWgSlots * kWgCodeBytes;
 constexpr uint32_t kWgBars = kWgScales + kWgSlots * kWgScaleBytes;
@@ -180,8 +186,8 @@ struct WgRing {
     uint32_t stage, parity;
     __device__ __forceinline__ void advance(uint32_t by) {
         stage += by;
-        if (stage >= kWgStages) {
-            stage -= kWgStages;
+        if (stage >= kWgRing) {
+            stage -= kWgRing;
             parity ^= 1;
         }
     }
@@ -298,7 +304,7 @@ __device__ __forceinline__ void wg_store_rows(const WgArgs& a, uint64_t n0, uint
 // waits until the barrier of step number `step` among `bars` is over
 __device__ __forceinline__ bool wg_wait_step(uint32_t bars, uint32_t step,
                                              volatile uint32_t* gave_up) {
-    return mbar_wait(bars + 8 * (step % kWgStages), (step / kWgStages) & 1, gave_up);
+    return mbar_wait(bars + 8 * (step % kWgRing), (step / kWgRing) & 1, gave_up);
 }
 
 template <bool COPY>
@@ -310,16 +316,16 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const uint32_t tiles = smem_u32(base);
     uint64_t* bars = reinterpret_cast<uint64_t*>(base + kWgBars);
-    // Barriers by step (step % stages).  The thread that issues the matrix instructions waits for
+    // Barriers by step (step % kWgRing).  The thread that issues the matrix instructions waits for
     // one of them and commits to one a step: every further wait would leave the tensor cores idle.
     const uint32_t empty = smem_u32(bars);             // operands consumed
-    const uint32_t ready = empty + 8 * kWgStages;      // first block's: both blocks' operands are there
-    const uint32_t copied = ready + 8 * kWgStages;     // second block's: its dY tiles arrived
-    const uint32_t coded = copied + 8 * kWgStages;     // the block's codes arrived
-    const uint32_t taken = coded + 8 * kWgStages;      // they were read
-    const uint32_t full = taken + 8 * kWgStages;       // [2] a tile's product is complete
+    const uint32_t ready = empty + 8 * kWgRing;      // first block's: both blocks' operands are there
+    const uint32_t copied = ready + 8 * kWgRing;     // second block's: its dY tiles arrived
+    const uint32_t coded = copied + 8 * kWgRing;     // the block's codes arrived
+    const uint32_t taken = coded + 8 * kWgRing;      // they were read
+    const uint32_t full = taken + 8 * kWgRing;       // [2] a tile's product is complete
     const uint32_t drained = full + 16;                // [2] first block's: TMEM read out
-    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 5 * kWgStages + 4);
+    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 5 * kWgRing + 4);
     volatile uint32_t* gave_up = words + 1;
     float* affine = reinterpret_cast<float*>(base + kWgBars + 512);
 
@@ -330,7 +336,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     if (warp == kWgMmaWarp) tmem_alloc_pair(smem_u32(words), 2 * kWgTile);
     if (threadIdx.x == 0) {
         words[1] = 0;
-        for (int s = 0; s < kWgStages; ++s) {
+        for (int s = 0; s < kWgRing; ++s) {
             mbar_init(empty + 8 * s, 1);
             mbar_init(ready + 8 * s, 2 * (kWgGroupWarps + (COPY ? 1 : kWgLoaders)));
             mbar_init(copied + 8 * s, 1);
@@ -363,8 +369,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         uint32_t total = 0, u = 0;
         for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) total += w.steps;
         for (uint32_t step = group; step < total; step += kWgGroups) {
-            const uint32_t stage = step % kWgStages, slot = step % kWgSlots;
-            bool ok = mbar_wait(coded + 8 * stage, (step / kWgStages) & 1, gave_up);
+            const uint32_t stage = step % kWgRing, slot = step % kWgSlots;
+            bool ok = wg_wait_step(coded, step, gave_up);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             const uint8_t* from = base + kWgCodes + slot * kWgCodeBytes + token * 128 + eighth * 16;
             const uint8_t* scales = base + kWgScales + slot * kWgScaleBytes + token * 4 + (eighth >> 1);
@@ -470,15 +476,15 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         if (COPY && lane == 0) {
             WgWalk walk;
             const uint32_t arrived = rank ? copied : ready;
-            uint32_t place = 0, step = 0, last[kWgStages];        // last: step + 1, 0: unused
-            for (int s = 0; s < kWgStages; ++s) last[s] = 0;
+            uint32_t place = 0, step = 0, last[kWgPlaces];        // last: step + 1, 0: unused
+            for (int s = 0; s < kWgPlaces; ++s) last[s] = 0;
             bool ok = true;
             for (walk.begin(a, pair); walk.more() && ok; walk.advance(a, pair, 1), ++step) {
-                const uint32_t bar = arrived + 8 * (step % kWgStages);
+                const uint32_t bar = arrived + 8 * (step % kWgRing);
                 for (uint32_t h = 0; h < walk.unit.halves; ++h) {
                     uint32_t before = 0;
 #pragma unroll
-                    for (int s = 0; s < kWgStages; ++s)
+                    for (int s = 0; s < kWgPlaces; ++s)
                         if (s == (int)place) {
                             before = last[s];
                             last[s] = step + 1;
@@ -490,13 +496,13 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                         tma_load_2d(tiles + place * kWgOperand + p * kWgPanel, &map,
                                     (int)(walk.unit.n0 + h * kWgTile + rank * kWgHalf + 64 * p),
                                     (int)walk.token(), bar);
-                    place = place + 1 == kWgStages ? 0 : place + 1;
+                    place = place + 1 == kWgPlaces ? 0 : place + 1;
                 }
             }
             // the copies in flight land before the block may end
             const long long begin = clock64();
-            for (uint32_t i = step < kWgStages ? 0 : step - kWgStages; i < step; ++i)
-                while (!mbar_try(arrived + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
+            for (uint32_t i = step < kWgRing ? 0 : step - kWgRing; i < step; ++i)
+                while (!mbar_try(arrived + 8 * (i % kWgRing), (i / kWgRing) & 1) &&
                        clock64() - begin < 4000000000ll) {}
         }
     } else if (warp == kWgCodeWarp) {
@@ -505,7 +511,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             WgWalk walk;
             uint32_t step = 0;
             for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1), ++step) {
-                const uint32_t slot = step % kWgSlots, bar = coded + 8 * (step % kWgStages);
+                const uint32_t slot = step % kWgSlots, bar = coded + 8 * (step % kWgRing);
                 if (step >= kWgSlots && !wg_wait_step(taken, step - kWgSlots, gave_up)) break;
                 const uint64_t column = walk.unit.k0 + rank * kWgHalf;
                 mbar_expect(bar, kWgCodeBytes + kWgScaleBytes);
@@ -516,8 +522,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                           bar);
             }
             const long long begin = clock64();
-            for (uint32_t i = step < kWgStages ? 0 : step - kWgStages; i < step; ++i)
-                while (!mbar_try(coded + 8 * (i % kWgStages), (i / kWgStages) & 1) &&
+            for (uint32_t i = step < kWgRing ? 0 : step - kWgRing; i < step; ++i)
+                while (!mbar_try(coded + 8 * (i % kWgRing), (i / kWgRing) & 1) &&
                        clock64() - begin < 4000000000ll) {}
         }
     } else if (warp == kWgMmaWarp) {
@@ -544,17 +550,17 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                     const uint64_t right = operand + (kWgDecoded + slot * kWgOperand) / 16;
                     slot = slot + 1 == kWgSlots ? 0 : slot + 1;
                     const uint32_t done = empty + 8 * stage;
-                    stage = stage + 1 == kWgStages ? 0 : stage + 1;
+                    stage = stage + 1 == kWgRing ? 0 : stage + 1;
                     parity ^= stage == 0;
                     uint64_t left = operand + place * (kWgOperand / 16);
-                    place = place + 1 == kWgStages ? 0 : place + 1;
+                    place = place + 1 == kWgPlaces ? 0 : place + 1;
 #pragma unroll
                     for (int i = 0; i < kWgStep / 16; ++i)   // 16 tokens: two groups of lines
                         mma_pair(to, left + 128 * i, right + 128 * i, shape, s > 0 || i > 0,
                                  elected);
                     if (twice) {
                         left = operand + place * (kWgOperand / 16);
-                        place = place + 1 == kWgStages ? 0 : place + 1;
+                        place = place + 1 == kWgPlaces ? 0 : place + 1;
 #pragma unroll
                         for (int i = 0; i < kWgStep / 16; ++i)
                             mma_pair(to + kWgTile, left + 128 * i, right + 128 * i, shape,
@@ -591,7 +597,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         const uint32_t chunk = i0 & 15, token0 = i0 >> 4;          // tokens token0 + 8 j
         WgWalk walk;
         walk.begin(a, pair);
-        WgRing ring = {0, 1};
+        uint32_t step = 0;
         uint4 v[8];
         if (walk.more()) {
 #pragma unroll
@@ -601,9 +607,9 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         }
         while (walk.more()) {
             walk.advance(a, pair, 1);
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(empty + 8 * ring.stage, ring.parity, gave_up)))
-                break;
-            const uint32_t dst = tiles + ring.stage * kWgOperand + (chunk >> 3) * kWgPanel;
+            const bool free = step < kWgPlaces || wg_wait_step(empty, step - kWgPlaces, gave_up);
+            if (!__all_sync(0xFFFFFFFFu, free)) break;
+            const uint32_t dst = tiles + step % kWgPlaces * kWgOperand + (chunk >> 3) * kWgPanel;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t token = token0 + 8 * j;
@@ -615,8 +621,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             }
             fence_async_proxy();
             __syncwarp();
-            if (lane == 0) mbar_arrive_at(ready + 8 * ring.stage, 0);
-            ring.advance(1);
+            if (lane == 0) mbar_arrive_at(ready + 8 * (step % kWgRing), 0);
+            ++step;
         }
     }
     // the pair stays until both blocks are done with each other's barriers and with TMEM

@@ -94,13 +94,14 @@ struct Inject {
     int hold_rank = -1;                  // from its `hold_after`-th read of TMEM on, the first four
     int hold_after = 0;                  // warps of this block stand still until `hold_until`
     long long hold_until = 0;
+    int late = 0;                        // one copy in so many arrives when nothing else can happen
 };
 
 struct World {
     std::vector<std::unique_ptr<Block>> blocks;          // of the running cluster
     std::vector<std::unique_ptr<Thread>> threads;
     std::unordered_map<uint32_t, Barrier> bars;
-    std::vector<std::function<void()>> copies;
+    std::vector<std::function<void()>> copies, late;
     std::deque<std::function<void()>> tensor;            // in order
     std::vector<float> tmem;                             // [rank][lane][column]
     Counter cluster;
@@ -238,6 +239,12 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
             idle = 0;
             continue;
         }
+        if (!W.late.empty()) {           // one of those that come late
+            const size_t i = rng() % W.late.size();
+            W.copies.push_back(std::move(W.late[i]));
+            W.late.erase(W.late.begin() + i);
+            continue;
+        }
         // (a thread that has tried once goes on to wait)
         bool again = false;
         for (auto& t : W.threads) again |= runnable(*t);
@@ -252,7 +259,7 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
         if (W.clock > kWaitLimit) W.ran_out = true;
         ++W.lapses;
     }
-    if (!W.copies.empty()) fail("a block ended with copies in flight");
+    if (!W.copies.empty() || !W.late.empty()) fail("a block ended with copies in flight");
     if (!W.tensor.empty()) fail("a block ended with matrix instructions in flight");
     any_ran_out |= W.ran_out;
     for (auto& blk : W.blocks) {
@@ -370,7 +377,10 @@ inline void bar_check(Barrier& b) {
 }
 inline void bar_arrive(uint32_t a) {
     Barrier& b = bar_at(a);
-    if (!b.pending) fail("more arrivals than a barrier expects");
+    if (!b.pending) {
+        fprintf(stderr, "barrier %x, phase %u, %lld bytes to come\n", a, b.phase, (long long)b.tx);
+        fail("more arrivals than a barrier expects");
+    }
     --b.pending;
     bar_check(b);
 }
@@ -382,7 +392,8 @@ inline void bar_tx(uint32_t a, int64_t bytes) {
 inline bool bar_done(uint32_t a, uint32_t parity) { return (bar_at(a).phase & 1) != parity; }
 
 inline void async_copy(uint32_t dst, std::vector<uint8_t> data, uint32_t bar) {
-    W.copies.push_back([=] {
+    auto& list = inject.late && rng() % inject.late == 0 ? W.late : W.copies;
+    list.push_back([=] {
         memcpy(memory(dst), data.data(), data.size());
         bar_tx(bar, -(int64_t)data.size());
     });

@@ -27,8 +27,9 @@ int main(int argc, char** argv) {
         const std::string a = argv[i];
         const std::string name = a.substr(0, a.find('='));
         const long long v = atoll(a.c_str() + a.find('=') + 1);
-        injected = true;
-        if (name == "drop_rank") model::inject.drop_rank = (int)v;
+        injected |= name != "late";
+        if (name == "late") model::inject.late = (int)v;
+        else if (name == "drop_rank") model::inject.drop_rank = (int)v;
         else if (name == "drop_nth") model::inject.drop_nth = (int)v;
         else if (name == "hold_rank") model::inject.hold_rank = (int)v;
         else if (name == "hold_after") model::inject.hold_after = (int)v;

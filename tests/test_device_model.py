@@ -72,6 +72,16 @@ def test_a_wait_that_runs_out_leaves_nan_and_no_partial_sums(weight_grad, rank, 
     run(weight_grad, 192, 256, 1024, "whole", "f32", 1, 0, seed, *args)
 
 
+@pytest.mark.parametrize("seed", range(1, 5))
+@pytest.mark.parametrize("case", [(700, 256, 1024, "whole", "f32", 1, 0),
+                                  (700, 1024, 300, "whole", "f32", 1, 0),
+                                  (700, 256, 520, "any", "f32", 1, 0)],
+                         ids=["single", "double", "loads"])
+def test_copies_that_arrive_late_are_waited_for(weight_grad, case, seed):
+    # one copy in sixteen arrives only when nothing else can happen, long after those behind it
+    run(weight_grad, *case, seed, "late=16")
+
+
 @pytest.mark.parametrize("old,new", [
     ("step < kWgSlots || wg_wait_step(empty, step - kWgSlots, gave_up)", "true"),
     ("if (before) ok = wg_wait_step(empty, before - 1, gave_up);", "")])
