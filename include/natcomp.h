@@ -507,8 +507,10 @@ nc_status nc_act8_layer_norm_backward(const void* dy, int dtype, size_t rows, si
  * dy: bfloat16, rows x n.  dw: n x k, dw_dtype NC_DTYPE_F32 or NC_DTYPE_BF16.  db: fp32[n], may be
  * NULL.  accumulate != 0: both are added to what they hold.  The product runs in bfloat16 (the
  * decoded values are exact in it; other types of dy are refused for that reason) with binary32
- * accumulation on the tensor cores, which truncate: the relative error grows with the rows, about
- * 1e-5 at 16384.  workspace: nc_act8_weight_grad_workspace_bytes(rows, n, k).
+ * accumulation on the tensor cores, which truncate: the relative error grows with the rows to about
+ * 3e-6 at 8192 (binary32 dw) or 7e-6 at 16384 (bfloat16 dw, rounded by 2e-3 anyway), and no further:
+ * longer sums are made of chains of that many rows, added up in binary32 (where a chain's sum below
+ * 2^-126 may become 0).  workspace: nc_act8_weight_grad_workspace_bytes(rows, n, k).
  * rows, n, k < 2^31 and n * k below about 2^40, else NC_ERR_TOO_LARGE. */
 size_t nc_act8_weight_grad_workspace_bytes(size_t rows, size_t n, size_t k);
 nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy,

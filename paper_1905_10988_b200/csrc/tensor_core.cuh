@@ -140,6 +140,14 @@ __device__ __forceinline__ void shared_store16(uint32_t at, uint32_t a, uint32_t
                  : "memory");
 }
 
+// four neighbouring sums in global memory, 16-byte aligned, added to in place (rounded to nearest; sums
+// below 2^-126 may become 0)
+__device__ __forceinline__ void global_add4(float4* p, float a, float b, float c, float d) {
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a), "f"(b),
+                 "f"(c), "f"(d)
+                 : "memory");
+}
+
 // ordinary stores to shared memory become visible to tensor copies and tensor-core reads
 __device__ __forceinline__ void fence_async_proxy() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -22,6 +22,8 @@
 //   - sixteen warps decode, in four groups that take every fourth step;
 //   - one thread of the pair's first block issues the matrix instructions; TMEM holds two tiles, so
 //     four more warps write one out while the next is computed.
+// A sum over many tokens is made of chains: the accumulator goes to memory after each and is added up
+// there (kWgChainF32 below).
 // The tiles are dealt out evenly to the chip's 74 pairs, double ones while there are rounds of
 // them, then single ones.  What is left over, fewer tiles than pairs, is split along the tokens,
 // and a second kernel adds its binary32 parts in order.
@@ -61,6 +63,17 @@ constexpr uint32_t kWgRows = 32 * 9 * 4;             // a writer warp's rows in 
 constexpr uint32_t kWgSmem = kWgBars + 512 + 2 * kWgTile * 4 + kWgWriters * kWgRows + 1024;
 constexpr int kWgPairs = 74;             // pairs of blocks that the chip holds at a time
 constexpr int kWgMinSteps = 4;           // of a part
+// Most steps that an accumulator adds up before its sums go to memory and are added up there, by the
+// type of dW.  The tensor cores cut off what does not fit 24 bits, always towards 0, so the relative
+// error grows with the length of a chain: in the norm of a binary32 dW 4.6e-7 after 2048 tokens, 1.1e-6
+// after 4096, 2.9e-6 after 8192, 7e-6 after 16384, 4.4e-5 after 65536 (a product in binary32: 5e-7 and
+// 1.5e-6 at the last two), and a sum of chains keeps that of one.  Emptying both tiles of TMEM takes 15
+// to 20 us, in which the pair's tensor cores stand still.  binary32, 16384 x 4096 x 4096: 415 us as one
+// chain, 435 in chains of 8192 tokens, 457 of 4096, 495 of 2048.  Where bfloat16 rounds the result by
+// 1.7e-3 the cut is below a hundredth of that up to 16384.
+constexpr uint32_t kWgChainF32 = 128;
+constexpr uint32_t kWgChainBf16 = 256;
+constexpr uint32_t kWgTileFours = kWgTile / 4 * kWgTile;     // groups of four values of a tile
 
 struct WgArgs {
     const __nv_bfloat16* dy;
@@ -82,6 +95,8 @@ struct WgArgs {
     uint32_t tiles;                      // single ones after that
     uint32_t whole, splits;              // those from `whole` on are computed in `splits` parts
     float* parts;                        // [tile - whole][part][k / 4][256 n][4]
+    uint32_t chain;                      // steps of a chain at most
+    float* runs;                         // [pair][half][k / 4][256 n][4]: sums of a tile's chains
 };
 
 __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) {
@@ -90,9 +105,11 @@ __device__ __forceinline__ float wg_param(const void* p, int dtype, uint64_t i) 
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// the u-th piece of work of a pair: the steps of a double tile, of a single one, or a part of them
+// the u-th piece of work of a pair: a chain of the steps of a double tile, of a single one, or of a
+// part of one
 struct WgUnit {
     uint32_t tile, part, first, steps;   // steps == 0: no more work
+    uint32_t chain, chains;              // of the tile or the part
     uint32_t halves;                     // tiles of 256 n
     uint64_t n0, k0;
 };
@@ -111,30 +128,41 @@ __device__ __forceinline__ void wg_single(const WgArgs& a, uint32_t i, uint64_t&
     }
 }
 
+template <bool CHAINS>
 __device__ __forceinline__ WgUnit wg_unit(const WgArgs& a, uint32_t pair, uint32_t u) {
     const uint32_t all = (uint32_t)((a.rows + kWgStep - 1) / kWgStep);
     const uint32_t pairs = gridDim.x >> 1, rounds = a.whole / pairs;
     WgUnit w = {};
     w.halves = 1;
-    if (u < a.rounds) {
-        const uint32_t m = a.tiles_n / 2, d = u * pairs + pair;
-        w.halves = 2;
-        w.steps = all;
-        w.n0 = (uint64_t)(d % m) * (2 * kWgTile);
-        w.k0 = (uint64_t)(d / m) * kWgTile;
-        return w;
-    }
-    u -= a.rounds;
-    if (u < rounds) {
-        w.tile = u * pairs + pair;
-        w.steps = all;
-    } else if (u == rounds && pair < (a.tiles - a.whole) * a.splits) {
+    w.chains = CHAINS ? (all + a.chain - 1) / a.chain : 1;
+    uint32_t steps = all, piece = CHAINS ? u / w.chains : u;
+    if (piece < a.rounds + rounds) {
+        w.chain = CHAINS ? u % w.chains : 0;
+    } else {                             // the last piece: a part of a tile
+        if (pair >= (a.tiles - a.whole) * a.splits) return w;
         w.tile = a.whole + pair / a.splits;
         w.part = pair % a.splits;
         w.first = (uint32_t)((uint64_t)all * w.part / a.splits);
-        w.steps = (uint32_t)((uint64_t)all * (w.part + 1) / a.splits) - w.first;
+        steps = (uint32_t)((uint64_t)all * (w.part + 1) / a.splits) - w.first;
+        w.chain = u - (a.rounds + rounds) * w.chains;
+        if (CHAINS) w.chains = (steps + a.chain - 1) / a.chain;
+        if (w.chain >= w.chains) return w;
     }
-    if (w.steps) wg_single(a, w.tile, w.n0, w.k0);
+    if (piece < a.rounds) {
+        const uint32_t m = a.tiles_n / 2, d = piece * pairs + pair;
+        w.halves = 2;
+        w.n0 = (uint64_t)(d % m) * (2 * kWgTile);
+        w.k0 = (uint64_t)(d / m) * kWgTile;
+    } else {
+        if (piece < a.rounds + rounds) w.tile = (piece - a.rounds) * pairs + pair;
+        wg_single(a, w.tile, w.n0, w.k0);
+    }
+    w.steps = steps;
+    if (CHAINS) {
+        const uint32_t begin = (uint32_t)((uint64_t)steps * w.chain / w.chains);
+        w.first += begin;
+        w.steps = (uint32_t)((uint64_t)steps * (w.chain + 1) / w.chains) - begin;
+    }
     return w;
 }
 
@@ -160,20 +188,20 @@ struct WgTurns {
 };
 
 // a place in a pair's sequence of steps
-struct WgWalk {
+template <bool CHAINS> struct WgWalk {
     WgUnit unit;
     uint32_t u, step;
     __device__ __forceinline__ void begin(const WgArgs& a, uint32_t pair) {
         u = 0;
         step = 0;
-        unit = wg_unit(a, pair, 0);
+        unit = wg_unit<CHAINS>(a, pair, 0);
     }
     __device__ __forceinline__ bool more() const { return unit.steps != 0; }
     __device__ __forceinline__ void advance(const WgArgs& a, uint32_t pair, uint32_t by) {
         step += by;
         while (unit.steps != 0 && step >= unit.steps) {
             step -= unit.steps;
-            unit = wg_unit(a, pair, ++u);
+            unit = wg_unit<CHAINS>(a, pair, ++u);
         }
     }
     __device__ __forceinline__ uint64_t token() const {
@@ -301,13 +329,38 @@ __device__ __forceinline__ void wg_store_rows(const WgArgs& a, uint64_t n0, uint
     }
 }
 
+// a chain's sums of a warp's 32 rows, to memory or on top of what stands there
+__device__ __forceinline__ void wg_empty(float4* sums, uint32_t from, bool ok, bool first) {
+#pragma unroll 1
+    for (int c = 0; c < kWgTile; c += 32) {
+        uint32_t r[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tmem_load8(from + c + 8 * j, r[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tmem_wait8(r[j]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)              // NaN: a wait ran out, no result
+                v[i] = ok ? __uint_as_float(r[j / 2][4 * (j & 1) + i]) : __uint_as_float(0x7FC00000u);
+            float4* to = sums + (c / 4 + j) * kWgTile;
+            if (first)
+                *to = make_float4(v[0], v[1], v[2], v[3]);
+            else
+                global_add4(to, v[0], v[1], v[2], v[3]);
+        }
+    }
+}
+
 // waits until the barrier of step number `step` among `bars` is over
 __device__ __forceinline__ bool wg_wait_step(uint32_t bars, uint32_t step,
                                              volatile uint32_t* gave_up) {
     return mbar_wait(bars + 8 * (step % kWgRing), (step / kWgRing) & 1, gave_up);
 }
 
-template <bool COPY>
+// CHAINS: a tile's steps are more than one chain
+template <bool COPY, bool CHAINS>
 __global__ void __cluster_dims__(2, 1, 1)
 __launch_bounds__(32 * (kWgLoadWarp + (COPY ? 0 : kWgLoaders)), 1)
 wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUtensorMap map,
@@ -367,7 +420,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         const uint32_t place = kWgDecoded + (odd ? kWgPanel : 0u) + token * 128;
         const uint32_t chunk = (2 * (eighth & 3) + odd) ^ (token & 7);
         uint32_t total = 0, u = 0;
-        for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) total += w.steps;
+        for (WgUnit w = wg_unit<CHAINS>(a, pair, 0); w.steps; w = wg_unit<CHAINS>(a, pair, ++u)) total += w.steps;
         for (uint32_t step = group; step < total; step += kWgGroups) {
             const uint32_t stage = step % kWgRing, slot = step % kWgSlots;
             bool ok = wg_wait_step(coded, step, gave_up);
@@ -413,10 +466,11 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         uint32_t* rows = reinterpret_cast<uint32_t*>(affine + 2 * kWgTile) + warp * (kWgRows / 4);
         uint32_t u = 0;
         WgTurns turns;
-        for (WgUnit w = wg_unit(a, pair, 0); w.steps; w = wg_unit(a, pair, ++u)) {
+        for (WgUnit w = wg_unit<CHAINS>(a, pair, 0); w.steps; w = wg_unit<CHAINS>(a, pair, ++u)) {
             const uint64_t k0 = w.k0;
             const bool part = w.halves == 1 && w.tile >= a.whole && a.splits > 1;
-            if (!part) {
+            const bool last = !part && (!CHAINS || w.chain + 1 == w.chains);      // dW is written
+            if (last) {
                 asm volatile("bar.sync 1, %0;" ::"r"(32 * kWgWriters) : "memory");
                 for (int i = threadIdx.x; i < kWgTile; i += 32 * kWgWriters) {
                     const bool in = k0 + i < a.k;
@@ -430,39 +484,52 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             for (uint32_t h = 0; h < w.halves; ++h) {
                 const uint32_t b = turns.of(w, h);
                 const uint64_t n = w.n0 + h * kWgTile + rank * kWgHalf + 32 * warp + lane;
-                const float add = !part && a.beta && n < a.n ? a.db[n] : 0.0f;
+                const float add = last && a.beta && n < a.n ? a.db[n] : 0.0f;
                 bool ok = mbar_wait(full + 8 * b, turns.parity(b), gave_up);
                 ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
                 tc_fence_after();
                 const uint32_t from = tmem + b * kWgTile + ((uint32_t)(32 * warp) << 16);
-                float4* parts = reinterpret_cast<float4*>(a.parts) +
-                                ((uint64_t)(w.tile - a.whole) * a.splits + w.part) *
-                                    (kWgTile / 4 * kWgTile) +
-                                rank * kWgHalf + 32 * warp + lane;
-                // (a loop of few instructions: in a short call they are all fetched for the first time)
-                const int end = part || k0 + kWgTile <= a.k ? kWgTile : (int)((a.k - k0 + 7) & ~7ull);
-                uint32_t next[8];
-                tmem_load8(from, next);
+                // four columns of all rows follow each other
+                float4* sums = (part ? reinterpret_cast<float4*>(a.parts) +
+                                           ((uint64_t)(w.tile - a.whole) * a.splits + w.part) * kWgTileFours
+                                     : reinterpret_cast<float4*>(a.runs) +
+                                           (uint64_t)(2 * pair + h) * kWgTileFours) +
+                               rank * kWgHalf + 32 * warp + lane;
+                if (CHAINS && !last) {
+                    wg_empty(sums, from, ok, w.chain == 0);
+                } else {
+                    // (a loop of few instructions: in a short call they are all fetched for the first
+                    // time)
+                    const int end = part || k0 + kWgTile <= a.k ? kWgTile : (int)((a.k - k0 + 7) & ~7ull);
+                    uint32_t next[8];
+                    tmem_load8(from, next);
 #pragma unroll 1
-                for (int c = 0; c < end; c += 8) {
-                    float v[8];
-                    tmem_wait8(next);
+                    for (int c = 0; c < end; c += 8) {
+                        float v[8];
+                        float4* to = sums + c / 4 * kWgTile;
+                        tmem_wait8(next);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)      // NaN: a wait ran out, no result
-                        v[i] = ok ? __uint_as_float(next[i]) : __uint_as_float(0x7FC00000u);
-                    if (c + 8 < end) tmem_load8(from + c + 8, next);
-                    if (part) {      // four columns of all rows follow each other
-                        parts[c / 4 * kWgTile] = make_float4(v[0], v[1], v[2], v[3]);
-                        parts[(c / 4 + 1) * kWgTile] = make_float4(v[4], v[5], v[6], v[7]);
-                        continue;
+                        for (int i = 0; i < 8; ++i)      // NaN: a wait ran out, no result
+                            v[i] = ok ? __uint_as_float(next[i]) : __uint_as_float(0x7FC00000u);
+                        if (CHAINS && w.chain > 0) {     // on top of the chains before
+                            const float4 lo = __ldcg(to), hi = __ldcg(to + kWgTile);
+                            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+                            v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+                        }
+                        if (c + 8 < end) tmem_load8(from + c + 8, next);
+                        if (!CHAINS && part) {
+                            to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                            to[kWgTile] = make_float4(v[4], v[5], v[6], v[7]);
+                            continue;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            v[i] = fmaf(v[i], affine[c + i], add * affine[kWgTile + c + i]);
+                        if (!a.vector || k0 + c + 8 > a.k)
+                            wg_store_rows(a, n - lane, k0 + c, v, rows);
+                        else if (n < a.n)
+                            wg_store8(a, n, k0 + c, v);
                     }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        v[i] = fmaf(v[i], affine[c + i], add * affine[kWgTile + c + i]);
-                    if (!a.vector || k0 + c + 8 > a.k)
-                        wg_store_rows(a, n - lane, k0 + c, v, rows);
-                    else if (n < a.n)
-                        wg_store8(a, n, k0 + c, v);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -474,7 +541,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         // ---- copies of the dY tiles: two panels of 64 n each.  A place of their ring is free when
         // the step that used it last is done.
         if (COPY && lane == 0) {
-            WgWalk walk;
+            WgWalk<CHAINS> walk;
             const uint32_t arrived = rank ? copied : ready;
             uint32_t place = 0, step = 0, last[kWgPlaces];        // last: step + 1, 0: unused
             for (int s = 0; s < kWgPlaces; ++s) last[s] = 0;
@@ -508,7 +575,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
     } else if (warp == kWgCodeWarp) {
         // ---- copies of the codes and of their scales
         if (lane == 0) {
-            WgWalk walk;
+            WgWalk<CHAINS> walk;
             uint32_t step = 0;
             for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1), ++step) {
                 const uint32_t slot = step % kWgSlots, bar = coded + 8 * (step % kWgRing);
@@ -535,7 +602,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
             bool ok = true, here = false;            // here: the next step was seen to be ready
             uint32_t u = 0, place = 0, slot = 0, stage = 0, parity = 0;
             WgTurns turns;
-            for (WgUnit w = wg_unit(a, pair, 0); w.steps && ok; w = wg_unit(a, pair, ++u)) {
+            for (WgUnit w = wg_unit<CHAINS>(a, pair, 0); w.steps && ok; w = wg_unit<CHAINS>(a, pair, ++u)) {
                 for (uint32_t h = 0; h < w.halves && ok; ++h) {
                     const uint32_t b = turns.of(w, h);
                     ok = mbar_wait(drained + 8 * b, turns.parity(b) ^ 1, gave_up);
@@ -584,7 +651,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         } else if (COPY && lane == 0) {
             // ---- the other block: pass on that its dY tiles have arrived
             WgRing ring = {0, 0};
-            WgWalk walk;
+            WgWalk<CHAINS> walk;
             for (walk.begin(a, pair); walk.more(); walk.advance(a, pair, 1)) {
                 if (!mbar_wait(copied + 8 * ring.stage, ring.parity, gave_up)) break;
                 mbar_arrive_at(ready + 8 * ring.stage, 0);
@@ -595,7 +662,7 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
         // ---- plain loads of the dY tile, a step ahead: 16 lanes cover the 128 n of a token
         const int i0 = threadIdx.x - 32 * kWgLoadWarp;
         const uint32_t chunk = i0 & 15, token0 = i0 >> 4;          // tokens token0 + 8 j
-        WgWalk walk;
+        WgWalk<CHAINS> walk;
         walk.begin(a, pair);
         uint32_t step = 0;
         uint4 v[8];
@@ -900,7 +967,8 @@ struct WgPlan {
     int sum_blocks;
     uint64_t ldc;                        // row stride of the aligned copy of dY
     uint64_t token_pitch;                // tokens of a column of laid out scales
-    size_t sum_offset, fresh_offset, scale_offset, copy_offset, bytes;
+    uint64_t steps;
+    size_t runs_offset, sum_offset, fresh_offset, scale_offset, copy_offset, bytes;
 };
 
 // `doubles`: double tiles may be used
@@ -911,6 +979,7 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     p.rounds = doubles ? p.tiles_n / 2 * p.tiles_k / kWgPairs : 0;
     p.tiles = p.tiles_n * p.tiles_k - 2 * kWgPairs * p.rounds;
     const uint64_t steps = (rows + kWgStep - 1) / kWgStep, left = p.tiles % kWgPairs;
+    p.steps = steps;
     uint64_t splits = left ? kWgPairs / left : 1;
     if (splits > steps / kWgMinSteps) splits = steps / kWgMinSteps;
     p.whole = p.tiles - left;
@@ -923,7 +992,10 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     if (n % 8 == 0 && rows <= 256) blocks = 1;       // no kernel to join ranges
     if (blocks > kWgSumBlocks) blocks = kWgSumBlocks;
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
-    p.sum_offset = p.splits > 1 ? left * p.splits * kWgTile * kWgTile * 4 : 0;
+    p.runs_offset = p.splits > 1 ? left * p.splits * kWgTileFours * 16 : 0;
+    // (the type of dW, and with it the chains, are the call's)
+    const bool runs = steps > kWgChainF32 && (p.tiles_n * p.tiles_k >= kWgPairs || p.splits == 1);
+    p.sum_offset = p.runs_offset + (runs ? 2 * kWgPairs * (size_t)kWgTileFours * 16 : 0);
     p.fresh_offset = p.sum_offset + round_up16(p.sum_blocks * n * 4);
     p.scale_offset = p.fresh_offset + round_up16(n * 4);
     p.token_pitch = steps * kWgStep;
@@ -967,6 +1039,8 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         return NC_ERR_ALIGN;
     const bool aligned = row_access(dy, lddy, 2, rows) != kRowElement;
     const bool copied = !aligned && n % 8 != 0;          // through a copy that is
+    const bool f32 = dw_dtype == NC_DTYPE_F32;
+    const uint32_t chain = f32 ? kWgChainF32 : kWgChainBf16;
     const WgPlan p = wg_plan(rows, n, k, rows && (aligned || copied));
     if (rows && workspace_bytes < p.bytes) return NC_ERR_WORKSPACE;
 
@@ -1015,7 +1089,7 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     a.token_pitch = p.token_pitch;
     a.gamma = rows ? gamma : nullptr;        // no tokens: 0, not 0 * gamma
     a.beta = with_beta ? beta : nullptr;
-    a.param_dtype = param_dtype; a.dw = dw; a.dw_f32 = dw_dtype == NC_DTYPE_F32; a.lddw = lddw;
+    a.param_dtype = param_dtype; a.dw = dw; a.dw_f32 = f32; a.lddw = lddw;
     a.db = fresh; a.accumulate = accumulate;
     a.vector = row_access(dw, lddw, wbytes, n) != kRowElement;
     a.tiles_n = (uint32_t)p.tiles_n;
@@ -1025,6 +1099,8 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
     a.whole = rows ? (uint32_t)p.whole : 0;
     a.splits = rows ? p.splits : 0;
     a.parts = reinterpret_cast<float*>(ws);
+    a.chain = chain;
+    a.runs = reinterpret_cast<float*>(ws + p.runs_offset);
     if (rows) {
         const bool copy = aligned || copied;             // by tensor copies
         CUtensorMap map = {}, code_map = {};
@@ -1033,9 +1109,12 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
         if (!make_tensor_map(&code_map, codes, false, rows, act8_pitch(k), act8_pitch(k), 128,
                              kWgStep))
             return NC_ERR_CUDA;
-        auto kernel = copy ? wg_product_kernel<true> : wg_product_kernel<false>;
-        static bool allowed[2][64];
-        if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[copy])) return NC_ERR_CUDA;
+        const bool chains = p.steps > chain;
+        auto kernel = copy ? (chains ? wg_product_kernel<true, true> : wg_product_kernel<true, false>)
+                           : (chains ? wg_product_kernel<false, true> : wg_product_kernel<false, false>);
+        static bool allowed[4][64];
+        if (!allow_dynamic_smem((const void*)kernel, kWgSmem, allowed[2 * chains + copy]))
+            return NC_ERR_CUDA;
         const uint64_t pairs = p.whole || p.rounds ? kWgPairs : (p.tiles - p.whole) * p.splits;
         launch_overlapping(kernel, dim3((unsigned)(2 * pairs)),
                            dim3(32 * (kWgLoadWarp + (copy ? 0 : kWgLoaders))), kWgSmem, stream, a,

@@ -557,6 +557,10 @@ inline void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t ba
     if (rank == model::inject.drop_rank && nth == model::inject.drop_nth) return;
     model::async_copy(dst, d, bar);
 }
+inline void global_add4(float4* p, float a, float b, float c, float d) {
+    if ((uintptr_t)p % 16) model::fail("addition that is not aligned");
+    p->x += a; p->y += b; p->z += c; p->w += d;
+}
 inline void fence_async_proxy() {}
 inline void shared_store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     if (at % 16) model::fail("store that is not aligned");

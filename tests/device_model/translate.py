@@ -124,9 +124,10 @@ def _clean(text):
     return _shared(text)
 
 
-def translate(sources, pairs=None, change=None):
-    """The text of the C++ file: the sources of csrc with their entry points.  pairs: how many pairs of blocks the weight gradient takes the chip to hold.  change: a function
-    of (file, text), for a test that wants to see another text fail."""
+def translate(sources, constants=None, change=None):
+    """The text of the C++ file: the sources of csrc with their entry points.  constants: other values
+    of integer constants, by name.  change: a function of (file, text), for a test that wants to see
+    another text fail."""
     change = change or (lambda name, text: text)
     common = _without(change("common.cuh", _read("common.cuh")), ["launch_overlapping"], True)
     common = re.sub(r"#ifdef NC_BOUNDS.*?#else", "#if 1", common, flags=re.S)
@@ -151,7 +152,7 @@ static inline void st_bytes32(void* p, const Bytes32& r, bool wide);
     for name in sources:
         parts.append(change(name, _read(name)))
     text = "\n".join(_clean(p) for p in parts)
-    if pairs:
-        text, n = re.subn(r"(constexpr int kWgPairs = )\d+;", r"\g<1>%d;" % pairs, text)
-        assert n == 1
+    for name, value in (constants or {}).items():
+        text, n = re.subn(r"(constexpr \w+ %s = )\d+;" % name, r"\g<1>%d;" % value, text)
+        assert n == 1, name
     return '#include "model.hpp"\n' + text

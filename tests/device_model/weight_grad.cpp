@@ -36,8 +36,10 @@ int main(int argc, char** argv) {
         else if (name == "hold_until") model::inject.hold_until = v;
         else return 2;
     }
-    model::cluster_of[(const void*)wg_product_kernel<true>] = 2;
-    model::cluster_of[(const void*)wg_product_kernel<false>] = 2;
+    model::cluster_of[(const void*)wg_product_kernel<true, true>] = 2;
+    model::cluster_of[(const void*)wg_product_kernel<true, false>] = 2;
+    model::cluster_of[(const void*)wg_product_kernel<false, true>] = 2;
+    model::cluster_of[(const void*)wg_product_kernel<false, false>] = 2;
     std::mt19937 g(7);
     std::normal_distribution<float> normal;
     const size_t ld = lay == "gap" ? (n + 7) / 8 * 8 + 8 : lay == "any" ? n + 3 : n;

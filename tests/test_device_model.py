@@ -19,12 +19,12 @@ import translate  # noqa: E402
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no C++ compiler")
 
 
-def build(folder, name, pairs=2, change=None):
+def build(folder, name, constants=None, change=None):
     source, program = str(folder / (name + ".cpp")), str(folder / name)
     with open(os.path.join(MODEL, name + ".cpp")) as f:
         main = f.read()
     with open(source, "w") as f:
-        f.write(translate.translate([name + "_kernels.cu"], pairs, change) + main)
+        f.write(translate.translate([name + "_kernels.cu"], constants, change) + main)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     subprocess.run(["g++", "-std=c++20", "-O1", "-g1", "-w", "-ffp-contract=off", "-fsanitize=address",
                     "-I" + MODEL, "-I" + os.path.join(translate.ROOT, "include"),
@@ -41,7 +41,13 @@ def run(program, *args):
 
 @pytest.fixture(scope="module")
 def weight_grad(tmp_path_factory):
-    return build(tmp_path_factory.mktemp("model"), "weight_grad")
+    return build(tmp_path_factory.mktemp("model"), "weight_grad", dict(kWgPairs=2))
+
+
+@pytest.fixture(scope="module")
+def short_chains(tmp_path_factory):
+    return build(tmp_path_factory.mktemp("chains"), "weight_grad",
+                 dict(kWgPairs=2, kWgChainF32=2, kWgChainBf16=3))
 
 
 # rows, n, k, layout of dY, type of dW, affine, accumulate: less than a step and a ragged one; single
@@ -58,6 +64,26 @@ CASES = [(1, 1, 1, "whole", "f32", 0, 0), (70, 40, 33, "whole", "f32", 1, 0),
 @pytest.mark.parametrize("case", CASES, ids=["-".join(map(str, c)) for c in CASES])
 def test_values_and_bounds(weight_grad, case):
     run(weight_grad, *case, 1)
+
+
+# a tile's steps in several chains: single and double tiles, split ones with several chains a part, a
+# ragged last step, more tiles than one a pair, dY by plain loads and through the copy
+CHAINS = [(500, 256, 1024, "whole", "f32", 1, 1), (450, 1024, 500, "whole", "bf16", 1, 0),
+          (700, 1280, 300, "whole", "f32", 0, 0), (700, 1280, 300, "gap", "bf16", 0, 1),
+          (1500, 256, 256, "whole", "f32", 1, 0), (330, 600, 530, "any", "f32", 1, 0),
+          (330, 601, 530, "any", "bf16", 1, 1), (190, 256, 768, "whole", "f32", 0, 0)]
+
+
+@pytest.mark.parametrize("case", CHAINS, ids=["-".join(map(str, c)) for c in CHAINS])
+def test_sums_of_several_chains(short_chains, case):
+    run(short_chains, *case, 1)
+
+
+@pytest.mark.parametrize("rank", [0, 1])
+@pytest.mark.parametrize("nth", [0, 3, 7, 12])
+def test_a_wait_that_runs_out_in_any_chain_leaves_nan(short_chains, rank, nth):
+    run(short_chains, 500, 256, 1024, "whole", "f32", 1, 0, 1, "drop_rank=%d" % rank,
+        "drop_nth=%d" % nth)
 
 
 @pytest.mark.parametrize("seed", [1, 2])
@@ -89,6 +115,6 @@ def test_the_model_sees_a_wait_that_is_missing(tmp_path, old, new):
     def without(name, text):
         assert name != "weight_grad_kernels.cu" or text.count(old) == 1
         return text.replace(old, new)
-    program = build(tmp_path, "weight_grad", change=without)
+    program = build(tmp_path, "weight_grad", dict(kWgPairs=2), without)
     with pytest.raises(AssertionError):
         run(program, 700, 300, 300, "whole", "f32", 1, 0, 1)

@@ -256,3 +256,38 @@ def test_gpu_no_tokens_give_zero_whatever_the_parameters_are(accumulate):
     nc.nc_act8_weight_grad(None, 0, 3, 3, None, None, 40, gamma, beta, F, dw, F, 40, db, accumulate,
                            None, 0)
     assert bool((dw == (2 if accumulate else 0)).all()) and bool((db == (4 if accumulate else 0)).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("wkind,tokens", [("f32", 8192), ("bf16", 16384)])
+def test_gpu_error_does_not_grow_with_the_number_of_tokens(wkind, tokens):
+    # An accumulator cuts off at most an ulp, 2^-23 of its value, each time 16 tokens are added, and is
+    # emptied after `tokens` at most.  The sums of terms of either sign grow like the square root of
+    # their number, so a chain of m additions loses at most 2^-23 * sum of sqrt(s / m) = 2/3 m 2^-23 of
+    # its value, and the sum of chains as much of theirs; rounding adds u for every chain and the
+    # result's own rounding, which is as often up as down.
+    t, n, k = 1 << 18, 2560, 2048                     # more tiles than pairs: whole ones and split ones
+    g = torch.Generator(device="cuda").manual_seed(3)
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    dy = torch.randn(t, n, generator=g, device="cuda", dtype=torch.bfloat16)
+    x = torch.randn(t, k, generator=g, device="cuda", dtype=torch.bfloat16)
+    codes = torch.empty(nc.nc_act8_code_bytes(t, k), **u8)
+    scales = torch.empty(nc.nc_act8_scale_bytes(t, k), **u8)
+    B = nc.DTYPE_BF16
+    nc.nc_act8_compress(x, B, t, k, k, nc.ROUND_NEAREST, 0, 0, codes, scales)
+    nc.nc_act8_decompress(codes, scales, t, k, x, B, k)            # exact
+    size = nc.nc_act8_weight_grad_workspace_bytes(t, n, k)
+    ws = torch.empty(size, **u8)
+    dw = torch.empty(n, k, device="cuda", dtype=TYPES[wkind][1])
+    nc.nc_act8_weight_grad(dy, t, n, n, codes, scales, k, None, None, nc.DTYPE_F32, dw,
+                           TYPES[wkind][0], k, None, False, ws, size)
+    want = torch.zeros(n, k, dtype=torch.float64, device="cuda")
+    for i in range(0, t, 16384):
+        want += dy[i:i + 16384].double().t() @ x[i:i + 16384].double()
+    err = dw.double() - want
+    bound = 2 / 3 * (tokens / 16) * 2.0 ** -23 + (t / tokens + 2) * U
+    if wkind == "f32":
+        assert float(err.norm() / want.norm()) <= bound
+    # towards 0 by so much of the value; rounding to bfloat16 averages out over the entries
+    toward = float((err * want.sign()).sum() / want.abs().sum())
+    assert abs(toward) <= bound + 4 * ROUND[wkind] / (n * k) ** 0.5
