@@ -133,6 +133,11 @@ struct LnPlace {
     }
 };
 
+// whether a wait of the block has run out of time
+__device__ __forceinline__ bool ln_gave_up(const uint32_t* word) {
+    return *static_cast<const volatile uint32_t*>(word) != 0;
+}
+
 // Two numbers of every warp of a row for all of them.  A row has up to 8 warps, or up to 64 in a
 // cluster; slots without a warp stay 0.  Two rows use two sets in turn, so that a slot is written
 // again only after the readers of the row before have passed the row in between.
@@ -140,14 +145,21 @@ struct LnPlace {
 // One block: a barrier of the group's threads.  Cluster: asynchronous stores to all its blocks, of
 // which every block's own barrier counts the bytes; a cluster-wide barrier would wait for the loads
 // and stores of global memory in flight as well.
+//
+// A wait that runs out of time sets the block's word, which ends its other waits at once.  A later wait
+// on the same barrier could not tell the phase that never came from its own, so after that nothing
+// that the block takes from another passes for a result, and it sends nothing more: whoever does not
+// wait for the others may not write to their slots.  Their waits run out in turn.
 template <int CLUSTER>
 struct LnExchange {
     static constexpr int kSlots = CLUSTER > 1 ? 8 * CLUSTER : 8;      // of a row
     float2* set;                         // of even rows; the other one lies `other` further on
     uint32_t other, bars, bytes;
-    // `slots`: [2][kSlots * groups], `words`: two barriers; all threads of the cluster call
-    __device__ __forceinline__ void begin(float2* slots, uint64_t* words,
+    // `slots`: [2][kSlots * groups], `words`: two barriers, `word`: the block's;
+    // all threads of the cluster call
+    __device__ __forceinline__ void begin(float2* slots, uint64_t* words, uint32_t* word,
                                           const LnPlace<CLUSTER>& p) {
+        if (threadIdx.x == 0) *word = 0;
         const int all = kSlots * p.groups;
         for (int i = threadIdx.x; i < 2 * all; i += blockDim.x) slots[i] = make_float2(0.0f, 0.0f);
         set = slots + kSlots * p.group;
@@ -165,23 +177,19 @@ struct LnExchange {
         if (CLUSTER > 1) cluster_sync();
     }
     // row number `turn` of the group (0, 1, 2, ...)
+    // lost: whether a wait of the block has run out of time; then, what it returns is no result
     __device__ __forceinline__ const float2* send(float2 mine, uint32_t turn,
-                                                  const LnPlace<CLUSTER>& p) {
+                                                  const LnPlace<CLUSTER>& p, uint32_t* word,
+                                                  bool& lost) {
         float2* slots = set + (turn & 1 ? other : 0u);
         if constexpr (CLUSTER > 1) {
             const uint32_t bar = bars + 8 * (turn & 1);
-            if (p.lane < CLUSTER)
+            if (p.lane < CLUSTER && !lost)
                 st_async_pair(smem_u32(&slots[p.rank * p.warps + p.warp]), bar, p.lane, mine);
-            const long long begin = clock64();
-            bool done = mbar_try(bar, (turn >> 1) & 1);
-            while (!done && clock64() - begin < 4000000000ll) done = mbar_try(bar, (turn >> 1) & 1);
-            if (!done) {             // given up: the row must not pass for a result
-                const float nan = __uint_as_float(0x7FC00000u);
-                slots[p.lane & (kSlots - 1)] = make_float2(nan, nan);
-            }
+            lost |= !mbar_wait(bar, (turn >> 1) & 1, word);
             // armed for the row after next: nothing of it arrives before this block has sent
             // its part of the next row
-            if (threadIdx.x == 0) mbar_expect(bar, bytes);
+            if (threadIdx.x == 0 && !lost) mbar_expect(bar, bytes);
         } else {
             if (p.lane == 0) slots[p.warp] = mine;
             asm volatile("bar.sync %0, %1;" ::"r"(p.group + 1), "r"(p.G) : "memory");
@@ -190,12 +198,13 @@ struct LnExchange {
     }
     // f(slot) summed over the row's slots, the same in every lane
     template <typename F>
-    __device__ __forceinline__ float sum(const float2* slots, int lane, F f) const {
+    __device__ __forceinline__ float sum(const float2* slots, int lane, bool lost, F f) const {
         constexpr int kLanes = kSlots < 32 ? kSlots : 32;
         float s = f(slots, lane & (kLanes - 1));
         if (kSlots > 32) s += f(slots, lane + 32);
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        if (CLUSTER > 1 && lost) s = __uint_as_float(0x7FC00000u);
         return s;
     }
 };
@@ -240,6 +249,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         scratches[MODE == kSpread ? kLnThreads / 32 : 1][MODE == kSpread ? kSpreadWords<T> : 4];
     uint32_t* scratch = scratches[MODE == kSpread ? threadIdx.x >> 5 : 0];
     __shared__ uint64_t bars[2];
+    __shared__ uint32_t gave_up;
     extern __shared__ float4 tables[];   // gamma, beta
     const LnPlace<CLUSTER> p(threads, a.cols);
     const int row_warps = CLUSTER * p.warps;
@@ -262,7 +272,7 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         counts[w] = make_float2(n, n > 0.0f ? 1.0f / n : 0.0f);
     }
     LnExchange<CLUSTER> others;
-    others.begin(slots, bars, p);
+    others.begin(slots, bars, &gave_up, p);
     const bool whole = MODE == kRegular || 16u * p.tid + 15 < p.cols;
     const float inverse_n = counts[p.rank * p.warps + p.warp].y;
 
@@ -295,10 +305,11 @@ ln_forward_kernel(const __grid_constant__ LnForward a, const int threads,
         of_pair(q, square, odd);
         square = warp_sum(square + odd);
         if (row_warps > 1) {
-            const float2* got = others.send(make_float2(sum, square), turn, p);
-            mean = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; }) *
+            bool lost = CLUSTER > 1 && ln_gave_up(&gave_up);
+            const float2* got = others.send(make_float2(sum, square), turn, p, &gave_up, lost);
+            mean = others.sum(got, p.lane, lost, [](const float2* s, int w) { return s[w].x; }) *
                    inverse_cols;
-            square = others.sum(got, p.lane, [&](const float2* s, int w) {
+            square = others.sum(got, p.lane, lost, [&](const float2* s, int w) {
                 const float d = fmaf(s[w].x, counts[w].y, -mean);
                 return fmaf(counts[w].x * d, d, s[w].y);
             });
@@ -394,6 +405,7 @@ ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads
                           const __grid_constant__ PhiloxKeys keys) {
     __shared__ float2 slots[2 * 8 * 8];
     __shared__ uint64_t bars[2];
+    __shared__ uint32_t gave_up;
     extern __shared__ float4 tables[];   // gamma, beta of the first and of the second half
     const LnPlace<1> p(threads, a.cols);
     const int G = p.G;
@@ -415,7 +427,7 @@ ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads
                               a.params.dtype, G, origin, a.cols - origin, 0.0f);
     }
     LnExchange<1> others;
-    others.begin(slots, bars, p);
+    others.begin(slots, bars, &gave_up, p);
 
     uint32_t turn = 0;
     for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
@@ -442,10 +454,11 @@ ln_forward_regular_kernel(const __grid_constant__ LnForward a, const int threads
         of_pair(q, square, odd);
         square = warp_sum(square + odd);
         if (p.warps > 1) {
-            const float2* got = others.send(make_float2(sum, square), turn, p);
-            mean = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; }) *
+            bool lost = false;
+            const float2* got = others.send(make_float2(sum, square), turn, p, &gave_up, lost);
+            mean = others.sum(got, p.lane, lost, [](const float2* s, int w) { return s[w].x; }) *
                    inverse_cols;
-            square = others.sum(got, p.lane, [&](const float2* s, int w) {
+            square = others.sum(got, p.lane, lost, [&](const float2* s, int w) {
                 const float d = fmaf(s[w].x, 1.0f / 1024.0f, -mean);
                 return w < p.warps ? fmaf(1024.0f * d, d, s[w].y) : 0.0f;
             });
@@ -616,6 +629,7 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
         scratches[MODE == kSpread ? kLnThreads / 32 : 1][MODE == kSpread ? kSpreadWords<T> : 4];
     uint32_t* scratch = scratches[MODE == kSpread ? threadIdx.x >> 5 : 0];
     __shared__ uint64_t bars[2], ringbars[MODE == kRegular ? 8 : 1][3];
+    __shared__ uint32_t gave_up, fetches[MODE == kRegular ? 8 : 1];
     extern __shared__ float4 table[];    // gamma; several groups: their sums; the ring
     const LnPlace<CLUSTER> p(threads, a.cols);
     float* columns = reinterpret_cast<float*>(table + 4 * p.G);
@@ -674,13 +688,14 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     if (kRing && p.tid == 0) {
         for (int s = 0; s < Stage::kStages; ++s) mbar_init(arrived + 8 * s, 1);
         mbar_init_fence();
+        fetches[p.group] = 0;
         for (int s = 0; s < Stage::kStages; ++s)
             if (p.first + s * p.step < a.rows) fetch(p.first + s * p.step, s);
     }
     f32x2 dgamma[8], dbeta[8];
     ln_table(table, a.params.gamma, a.params.has_gamma, a.params.dtype, p.G, p.origin, p.cols, 1.0f);
     LnExchange<CLUSTER> others;
-    others.begin(slots, bars, p);
+    others.begin(slots, bars, &gave_up, p);
     const bool whole = MODE == kRegular || 16u * p.tid + 15 < p.cols;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dgamma[i] = dbeta[i] = 0;
@@ -688,15 +703,11 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     uint32_t turn = 0, stage = 0, parity = 0;
     for (uint64_t row = p.first; row < a.rows; row += p.step, ++turn) {
         f32x2 g[8], xh[8];
-        float rstd = next.rstd;
+        const float rstd = next.rstd;
         const float mean = SAVED8 ? 0.0f : next.mean;
         const uint8_t* here = ring + stage * Stage::bytes(p.G);
         if constexpr (kRing) {
-            const long long begin = clock64();
-            bool done = mbar_try(arrived + 8 * stage, parity);
-            while (!done && clock64() - begin < 4000000000ll)
-                done = mbar_try(arrived + 8 * stage, parity);
-            if (!done) rstd = __uint_as_float(0x7FC00000u);   // must not pass for a result
+            mbar_wait(arrived + 8 * stage, parity, &gave_up);        // what comes of it: `lost` below
             next.dy = ld_shared16<T>(here + Stage::kValues * p.tid);
             if constexpr (SAVED8) {
                 next.codes =
@@ -739,14 +750,17 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             s2 = fma2(g[i], xh[i], s2);
         }
         float m1, m2, odd;
+        bool lost = kRing && ln_gave_up(&gave_up);
         of_pair(s1, m1, odd);
+        if (kRing && lost) odd = __uint_as_float(0x7FC00000u);       // the row must not pass for a result
         m1 = warp_sum(m1 + odd);
         of_pair(s2, m2, odd);
         m2 = warp_sum(m2 + odd);
         if (row_warps > 1) {
-            const float2* got = others.send(make_float2(m1, m2), turn, p);
-            m1 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].x; });
-            m2 = others.sum(got, p.lane, [](const float2* s, int w) { return s[w].y; });
+            if (!kRing && CLUSTER > 1) lost = ln_gave_up(&gave_up);
+            const float2* got = others.send(make_float2(m1, m2), turn, p, &gave_up, lost);
+            m1 = others.sum(got, p.lane, lost, [](const float2* s, int w) { return s[w].x; });
+            m2 = others.sum(got, p.lane, lost, [](const float2* s, int w) { return s[w].y; });
         } else if (kRing) {
             __syncwarp();
         }
@@ -754,7 +768,12 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
             // the whole group has come by, so it is done with the stage of the row before
             const uint32_t before = stage ? stage - 1 : Stage::kStages - 1;
             const uint64_t ahead = row + (Stage::kStages - 1) * p.step;
-            if (p.tid == 0 && turn > 0 && ahead < a.rows) fetch(ahead, before);
+            if (p.tid == 0 && turn > 0 && ahead < a.rows) {
+                if (!lost)
+                    fetch(ahead, before);
+                else if (!fetches[p.group])
+                    fetches[p.group] = turn + Stage::kStages - 1;    // so many before
+            }
             if constexpr (RES) late = ld_shared16<T>(here + Stage::dres(p.G) + Stage::kValues * p.tid);
             if (++stage == Stage::kStages) {
                 stage = 0;
@@ -780,11 +799,23 @@ ln_backward_kernel(const __grid_constant__ LnBackward a, const int threads) {
     }
 
     let_next_begin();
+    // the copies in flight land before the block may end
+    if (kRing && p.tid == 0 && ln_gave_up(&gave_up)) {
+        const long long begin = clock64();
+        const uint32_t n = fetches[p.group] ? fetches[p.group] : turn;
+        for (uint32_t i = n < Stage::kStages ? 0 : n - Stage::kStages; i < n; ++i)
+            while (!mbar_try(arrived + 8 * (i % Stage::kStages), (i / Stage::kStages) & 1) &&
+                   clock64() - begin < 4000000000ll) {}
+    }
     float dg[16], db[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         of_pair(dgamma[i], dg[2 * i], dg[2 * i + 1]);
         of_pair(dbeta[i], db[2 * i], db[2 * i + 1]);
+    }
+    if (kRing && ln_gave_up(&gave_up)) {         // sums of values that may not have come
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dg[i] = db[i] = __uint_as_float(0x7FC00000u);
     }
     float* out = a.parts + (uint64_t)(blockIdx.x / CLUSTER) * 2 * a.parts_pitch + p.origin;
     float* out2 = out + a.parts_pitch;

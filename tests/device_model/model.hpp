@@ -16,7 +16,6 @@
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
-#include <ucontext.h>
 
 #include <algorithm>
 #include <deque>
@@ -24,6 +23,7 @@
 #include <map>
 #include <memory>
 #include <random>
+#include <string>
 #include <tuple>
 #include <unordered_map>
 #include <vector>
@@ -40,7 +40,34 @@ struct CUtensorMap_st {
 };
 typedef CUtensorMap_st CUtensorMap;
 
-extern "C" const char* __asan_default_options() { return "detect_leaks=0"; }
+#if !defined(__x86_64__)
+#error "fibers are switched in x86-64 assembly"
+#endif
+
+// saves the caller's registers on its stack and its stack in *from, and goes on where `to` was saved
+extern "C" void model_switch(void** from, void* to);
+asm(R"(
+.text
+.globl model_switch
+model_switch:
+    push %rbp
+    push %rbx
+    push %r12
+    push %r13
+    push %r14
+    push %r15
+    mov %rsp, (%rdi)
+    mov %rsi, %rsp
+    pop %r15
+    pop %r14
+    pop %r13
+    pop %r12
+    pop %rbx
+    pop %rbp
+    ret
+)");
+
+extern "C" const char* __asan_default_options() { return "detect_leaks=0:detect_stack_use_after_return=0"; }
 
 namespace model {
 
@@ -62,7 +89,7 @@ struct Counter {
     uint32_t count = 0, gen = 0;
 };
 struct Thread {
-    ucontext_t ctx;
+    void* saved;                         // its stack where it stands still
     char* stack;
     void* fake = nullptr;
     Block* block;
@@ -90,7 +117,7 @@ struct Barrier {
 
 // what a test asks for
 struct Inject {
-    int drop_rank = -1, drop_nth = -1;   // this block's nth untiled copy never arrives
+    int drop_rank = -1, drop_nth = -1;   // this block's nth untiled copy or remote store never arrives
     int hold_rank = -1;                  // from its `hold_after`-th read of TMEM on, the first four
     int hold_after = 0;                  // warps of this block stand still until `hold_until`
     long long hold_until = 0;
@@ -115,11 +142,12 @@ inline Inject inject;
 inline std::mt19937 rng(1);
 inline Thread* cur = nullptr;
 inline dim3 grid, block_dim;
-inline ucontext_t home;
+inline void* home;
 inline const void* home_bottom;
 inline size_t home_size;
 inline std::function<void()> body;
 inline bool any_ran_out = false;
+inline long long longest = 0;             // clock at the end of a cluster
 inline std::map<const void*, int> cluster_of;
 inline size_t launches = 0;
 inline int sms = 148;
@@ -128,7 +156,7 @@ inline int sms = 148;
 inline void to_home() {
     Thread* t = cur;
     __sanitizer_start_switch_fiber(t->done ? nullptr : &t->fake, home_bottom, home_size);
-    swapcontext(&t->ctx, &home);
+    model_switch(&t->saved, home);
     __sanitizer_finish_switch_fiber(t->fake, nullptr, nullptr);
 }
 inline void entry() {
@@ -141,7 +169,7 @@ inline void resume(Thread* t) {
     cur = t;
     void* fake = nullptr;
     __sanitizer_start_switch_fiber(&fake, t->stack, kStackBytes);
-    swapcontext(&home, &t->ctx);
+    model_switch(&home, t->saved);
     __sanitizer_finish_switch_fiber(fake, nullptr, nullptr);
     cur = nullptr;
 }
@@ -206,17 +234,20 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
             t->stack = stacks[(size_t)r * n + i];
             t->block = W.blocks[r].get();
             t->index = i;
-            getcontext(&t->ctx);
-            t->ctx.uc_stack.ss_sp = t->stack;
-            t->ctx.uc_stack.ss_size = kStackBytes;
-            t->ctx.uc_link = nullptr;
-            makecontext(&t->ctx, entry, 0);
+            // a first switch pops six registers and returns to entry()
+            void** top = (void**)(((uintptr_t)t->stack + kStackBytes) & ~(uintptr_t)15) - 8;
+            __asan_unpoison_memory_region(t->stack, kStackBytes);
+            for (int k = 0; k < 6; ++k) top[k] = nullptr;
+            top[6] = (void*)&entry;
+            top[7] = nullptr;
+            t->saved = top;
             W.threads.push_back(std::move(t));
         }
     size_t left = W.threads.size();
     std::vector<uint32_t> order(W.threads.size() / 32);
     for (size_t i = 0; i < order.size(); ++i) order[i] = (uint32_t)i;
     int idle = 0;
+    bool looked = false;
     while (left) {
         std::shuffle(order.begin(), order.end(), rng);
         bool moved = false;
@@ -237,6 +268,7 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
         W.clock += 100;
         if (moved) {
             idle = 0;
+            looked = false;
             continue;
         }
         if (!W.late.empty()) {           // one of those that come late
@@ -249,6 +281,12 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
         bool again = false;
         for (auto& t : W.threads) again |= runnable(*t);
         if (again) continue;
+        // a waiting thread looks at other things than its barrier now and then
+        looked = !looked;
+        if (looked) {
+            ++W.lapses;
+            continue;
+        }
         // nothing but time can end a wait: it passes until the first of them runs out
         long long next = 0;
         for (auto& t : W.threads)
@@ -262,6 +300,7 @@ inline void run_cluster(uint32_t first, int size, dim3 g, dim3 b, size_t smem) {
     if (!W.copies.empty() || !W.late.empty()) fail("a block ended with copies in flight");
     if (!W.tensor.empty()) fail("a block ended with matrix instructions in flight");
     any_ran_out |= W.ran_out;
+    longest = std::max(longest, W.clock);
     for (auto& blk : W.blocks) {
         if (blk->dynamic + (blk->statics - kStatic) > kShared) fail("too much shared memory");
         __asan_unpoison_memory_region(blk->arena, kArena);
@@ -391,6 +430,10 @@ inline void bar_tx(uint32_t a, int64_t bytes) {
 }
 inline bool bar_done(uint32_t a, uint32_t parity) { return (bar_at(a).phase & 1) != parity; }
 
+inline bool dropped() {
+    const int rank = (int)cur->block->rank;
+    return W.bulk[rank]++ == inject.drop_nth && rank == inject.drop_rank;
+}
 inline void async_copy(uint32_t dst, std::vector<uint8_t> data, uint32_t bar) {
     auto& list = inject.late && rng() % inject.late == 0 ? W.late : W.copies;
     list.push_back([=] {
@@ -515,6 +558,7 @@ inline void mbar_arrive_at(uint32_t bar, uint32_t rank) { model::bar_arrive(mode
 inline void st_async_pair(uint32_t dst, uint32_t bar, uint32_t rank, float2 v) {
     std::vector<uint8_t> d(8);
     memcpy(d.data(), &v, 8);
+    if (model::dropped()) return;
     model::async_copy(model::mapped(dst, rank), d, model::mapped(bar, rank));
 }
 inline bool mbar_test(uint32_t bar, uint32_t parity) { return model::bar_done(bar, parity); }
@@ -551,10 +595,8 @@ inline void tma_load_2d(uint32_t dst, const CUtensorMap* m, int x, int y, uint32
 }
 inline void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     if (dst % 16 || (uintptr_t)src % 16 || bytes % 16) model::fail("bulk copy that is not aligned");
-    const int rank = (int)model::cur->block->rank;
-    const int nth = model::W.bulk[rank]++;
     std::vector<uint8_t> d((const uint8_t*)src, (const uint8_t*)src + bytes);
-    if (rank == model::inject.drop_rank && nth == model::inject.drop_nth) return;
+    if (model::dropped()) return;
     model::async_copy(dst, d, bar);
 }
 inline void global_add4(float4* p, float a, float b, float c, float d) {
@@ -656,3 +698,38 @@ inline cudaError_t launch_overlapping(K kernel, dim3 g, dim3 b, size_t smem, cud
 }
 
 }  // namespace natcomp
+
+// ---- for the programs
+struct Held {                            // memory whose ends the sanitizer checks, at an offset
+    std::unique_ptr<uint8_t[]> raw;
+    uint8_t* p;
+    Held(size_t bytes, size_t offset = 0) : raw(new uint8_t[bytes + offset + 64]) {
+        uintptr_t a = ((uintptr_t)raw.get() + 63) & ~(uintptr_t)63;
+        p = (uint8_t*)a + offset;
+        const uintptr_t end = (uintptr_t)raw.get() + bytes + offset + 64;
+        memset(raw.get(), 0xFF, bytes + offset + 64);
+        if (end > a + offset + bytes) __asan_poison_memory_region(p + bytes, end - (a + offset + bytes));
+    }
+    ~Held() { __asan_unpoison_memory_region(raw.get(), 1); }
+};
+
+// name=value arguments from `first` on; whether one of them makes a wait run out
+inline bool injected(int argc, char** argv, int first) {
+    bool ran_out = false;
+    for (int i = first; i < argc; ++i) {
+        const std::string a = argv[i], name = a.substr(0, a.find('='));
+        const long long v = atoll(a.c_str() + a.find('=') + 1);
+        if (name == "late") {
+            model::inject.late = (int)v;
+            continue;
+        }
+        ran_out = true;
+        if (name == "drop_rank") model::inject.drop_rank = (int)v;
+        else if (name == "drop_nth") model::inject.drop_nth = (int)v;
+        else if (name == "hold_rank") model::inject.hold_rank = (int)v;
+        else if (name == "hold_after") model::inject.hold_after = (int)v;
+        else if (name == "hold_until") model::inject.hold_until = v;
+        else model::fail("argument");
+    }
+    return ran_out;
+}

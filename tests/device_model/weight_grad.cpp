@@ -3,39 +3,13 @@
 // name=value pairs for what a test injects.  Prints "ok ..." or what is wrong.
 using namespace natcomp;
 
-struct Held {                            // memory whose ends the sanitizer checks, at an offset
-    std::unique_ptr<uint8_t[]> raw;
-    uint8_t* p;
-    Held(size_t bytes, size_t offset = 0) : raw(new uint8_t[bytes + offset + 64]) {
-        uintptr_t a = ((uintptr_t)raw.get() + 63) & ~(uintptr_t)63;
-        p = (uint8_t*)a + offset;
-        const uintptr_t end = (uintptr_t)raw.get() + bytes + offset + 64;
-        memset(raw.get(), 0xFF, bytes + offset + 64);
-        if (end > a + offset + bytes) __asan_poison_memory_region(p + bytes, end - (a + offset + bytes));
-    }
-    ~Held() { __asan_unpoison_memory_region(raw.get(), 1); }
-};
-
 int main(int argc, char** argv) {
     if (argc < 9) return 2;
     const size_t t = atol(argv[1]), n = atol(argv[2]), k = atol(argv[3]);
     const std::string lay = argv[4], kind = argv[5];
     const bool affine = atoi(argv[6]), acc = atoi(argv[7]);
     model::rng.seed(atoi(argv[8]));
-    bool injected = false;
-    for (int i = 9; i < argc; ++i) {
-        const std::string a = argv[i];
-        const std::string name = a.substr(0, a.find('='));
-        const long long v = atoll(a.c_str() + a.find('=') + 1);
-        injected |= name != "late";
-        if (name == "late") model::inject.late = (int)v;
-        else if (name == "drop_rank") model::inject.drop_rank = (int)v;
-        else if (name == "drop_nth") model::inject.drop_nth = (int)v;
-        else if (name == "hold_rank") model::inject.hold_rank = (int)v;
-        else if (name == "hold_after") model::inject.hold_after = (int)v;
-        else if (name == "hold_until") model::inject.hold_until = v;
-        else return 2;
-    }
+    const bool injected = ::injected(argc, argv, 9);
     model::cluster_of[(const void*)wg_product_kernel<true, true>] = 2;
     model::cluster_of[(const void*)wg_product_kernel<true, false>] = 2;
     model::cluster_of[(const void*)wg_product_kernel<false, true>] = 2;

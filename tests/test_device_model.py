@@ -1,9 +1,12 @@
-"""The weight gradient's kernels thread by thread on the host (tests/device_model): their schedule with
-few pairs of blocks, the bounds of every access, and waits that run out of time.  The values are
+"""The kernels of the layer norm and of the weight gradient thread by thread on the host
+(tests/device_model): their schedules on a small chip, the bounds of every access, and waits that run out
+of time.  The values are
 compared with a product in 64 bits; the address sanitizer checks global and shared memory; copies and
 matrix instructions take effect late and in changing order; a wait that nothing ends, a barrier that
 gets too many arrivals or a copy in flight at a block's end is an error."""
+import concurrent.futures
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -19,12 +22,12 @@ import translate  # noqa: E402
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no C++ compiler")
 
 
-def build(folder, name, constants=None, change=None):
+def build(folder, name, constants=None, change=None, define=""):
     source, program = str(folder / (name + ".cpp")), str(folder / name)
     with open(os.path.join(MODEL, name + ".cpp")) as f:
         main = f.read()
     with open(source, "w") as f:
-        f.write(translate.translate([name + "_kernels.cu"], constants, change) + main)
+        f.write(translate.translate([name + "_kernels.cu"], constants, change) + define + main)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     subprocess.run(["g++", "-std=c++20", "-O1", "-g1", "-w", "-ffp-contract=off", "-fsanitize=address",
                     "-I" + MODEL, "-I" + os.path.join(translate.ROOT, "include"),
@@ -118,3 +121,69 @@ def test_the_model_sees_a_wait_that_is_missing(tmp_path, old, new):
     program = build(tmp_path, "weight_grad", dict(kWgPairs=2), without)
     with pytest.raises(AssertionError):
         run(program, 700, 300, 300, "whole", "f32", 1, 0, 1)
+
+
+# ---- layer norm ------------------------------------------------------------------------------
+
+TYPES = {"f32": "float", "bf16": "__nv_bfloat16"}
+
+
+@pytest.fixture(scope="module")
+def layer_norm(tmp_path_factory):
+    """{type: program}; a program has the kernels of one type, so that two compilers share the work"""
+    folders = {kind: tmp_path_factory.mktemp("norm" + kind) for kind in TYPES}
+
+    def one(kind):
+        def only(name, text):
+            if name == "layer_norm_kernels.cu":
+                for other in {"float", "__nv_bfloat16", "__half"} - {TYPES[kind]}:
+                    text, n = re.subn(r"return ln_(forward|backward)_launch<%s>\([^;]*;" % other,
+                                      "return NC_ERR_UNSUPPORTED;", text)
+                    assert n == 2
+            return text
+        return build(folders[kind], "layer_norm", None, only,
+                     "typedef %s T;\n" % TYPES[kind])
+    with concurrent.futures.ThreadPoolExecutor(2) as pool:
+        return dict(zip(TYPES, pool.map(one, TYPES)))
+
+
+# a warp, several groups a block, a whole block, clusters of 2, 4 and 8 with and without a block that
+# has no columns; one row, and many an owner
+ROWS = [(1, 1), (3, 5), (40, 512), (20, 513), (30, 1024), (6, 1001), (7, 2000), (5, 4099), (9, 8192),
+        (2, 16385), (3, 17000), (2, 32768)]
+
+
+@pytest.mark.parametrize("layout,kind", [("whole", "f32"), ("whole", "bf16"), ("gap", "bf16"),
+                                         ("any", "f32"), ("any", "bf16")])
+@pytest.mark.parametrize("rows,cols", ROWS)
+def test_norm_values_and_bounds(layer_norm, rows, cols, layout, kind):
+    sms = 8 if cols > 8192 else 2
+    p = layer_norm[kind]
+    run(p, "forward", rows, cols, layout, "none", 0, 0, 0, sms, 1)
+    run(p, "forward", rows, cols, layout, "random" if kind == "f32" else "nearest", 1, 0, 0, sms, 1)
+    run(p, "backward", rows, cols, layout, "none", 1, 1, 0, sms, 1, "late=5")
+    run(p, "backward", rows, cols, layout, "nearest", 0, 0, 1, sms, 2, "late=9")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_norm_of_regular_rows_in_a_kernel_of_their_own(layer_norm, kind):
+    for cols in (1024, 2048):
+        run(layer_norm[kind], "forward", 512, cols, "whole", "nearest", 1, 0, 0, 2, 1)
+
+
+# the ring of bulk copies (a group of a warp, of a block, a cluster of two) and the exchange of a cluster
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nth", [0, 5, 9, 22])
+@pytest.mark.parametrize("case", [("backward", 200, 512, "whole", "nearest", 1, 1, 0, 2),
+                                  ("backward", 60, 2048, "whole", "none", 1, 0, 0, 2),
+                                  ("backward", 40, 8192, "whole", "nearest", 1, 1, 0, 4),
+                                  ("backward", 30, 5000, "any", "nearest", 1, 1, 0, 4),
+                                  ("forward", 60, 5000, "gap", "random", 1, 0, 0, 4)],
+                         ids=lambda c: "-".join(map(str, c)))
+def test_norm_wait_that_runs_out_leaves_nan_and_ends(layer_norm, case, nth, kind):
+    # everything that the missing values reach is NaN, nothing else is wrong, and the waits behind the
+    # first that ran out of time do not each take as long again
+    for rank in range(2 if case[2] > 4096 else 1):
+        said = run(layer_norm[kind], *case, 1, "drop_rank=%d" % rank, "drop_nth=%d" % nth)
+        limits = int(re.search(r"at most (\d+) limits", said).group(1))
+        assert limits <= 3, said
