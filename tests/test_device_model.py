@@ -1,6 +1,6 @@
-"""The kernels of the layer norm and of the weight gradient thread by thread on the host
-(tests/device_model): their schedules on a small chip, the bounds of every access, and waits that run out
-of time.  The values are
+"""The kernels of the 8-bit checkpoints, the layer norm and the weight gradient thread by thread on the
+host (tests/device_model): their schedules on a small chip, the bounds of every access, and waits that
+run out of time.  The values are
 compared with a product in 64 bits; the address sanitizer checks global and shared memory; copies and
 matrix instructions take effect late and in changing order; a wait that nothing ends, a barrier that
 gets too many arrivals or a copy in flight at a block's end is an error."""
@@ -187,3 +187,19 @@ def test_norm_wait_that_runs_out_leaves_nan_and_ends(layer_norm, case, nth, kind
         said = run(layer_norm[kind], *case, 1, "drop_rank=%d" % rank, "drop_nth=%d" % nth)
         limits = int(re.search(r"at most (\d+) limits", said).group(1))
         assert limits <= 3, said
+
+
+# ---- checkpoints -----------------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def act8(tmp_path_factory):
+    folder = {kind: tmp_path_factory.mktemp("act8" + kind) for kind in TYPES}
+    return {kind: build(folder[kind], "act8", define="typedef %s T;\n" % TYPES[kind]) for kind in TYPES}
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("layout", ["whole", "gap", "any"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 5), (2, 32), (7, 96), (5, 513), (4, 1001), (3, 2048)])
+def test_checkpoint_codes_and_bounds(act8, rows, cols, layout, kind):
+    for random in (0, 1):
+        run(act8[kind], rows, cols, layout, random, 1)

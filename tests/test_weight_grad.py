@@ -291,3 +291,57 @@ def test_gpu_error_does_not_grow_with_the_number_of_tokens(wkind, tokens):
     # towards 0 by so much of the value; rounding to bfloat16 averages out over the entries
     toward = float((err * want.sign()).sum() / want.abs().sum())
     assert abs(toward) <= bound + 4 * ROUND[wkind] / (n * k) ** 0.5
+
+
+# ---- the schedule that large layers take -------------------------------------------------------
+
+PAIRS, TILE, STEP = 74, 256, 64
+
+
+def plan(t, n, k):
+    """rounds of double tiles, rounds of whole single ones, tiles left over and their parts, where dY
+    comes by tensor copies"""
+    tn, tk, steps = -(-n // TILE), -(-k // TILE), -(-t // STEP)
+    doubles = tn // 2 * tk // PAIRS
+    tiles = tn * tk - 2 * PAIRS * doubles
+    left = tiles % PAIRS
+    splits = max(1, min(PAIRS // left if left else 1, steps // 4))
+    return doubles, tiles // PAIRS, left, splits
+
+
+# (what the shape is for, tokens, n, k, layout of dY, affine, type of dW, accumulate)
+LARGE = [("single tiles one after another", 130, 4096, 2048, "whole", "f32", "f32", True),
+         ("double, single and split ones", 600, 4096, 4096, "whole", "bf16", "bf16", True),
+         ("the same through the aligned copy", 600, 4095, 4096, "whole", "f16", "f32", False),
+         ("the same with gaps, a ragged last step", 577, 4000, 4090, "gap", "f32", "f32", True)]
+
+
+def test_large_shapes_take_the_paths_that_they_are_for():
+    # (doubles, rounds of whole ones, left over, parts)
+    assert [plan(*c[1:4]) for c in LARGE] == [(0, 1, 54, 1), (1, 1, 34, 2), (1, 1, 34, 2), (1, 1, 34, 2)]
+    assert LARGE[2][2] % 8 and not LARGE[3][2] % 8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", LARGE, ids=[c[0] for c in LARGE])
+def test_gpu_schedule_of_large_layers(case):
+    _, t, n, k, layout, affine, wkind, accumulate = case
+    got, want, tol, gotb, wantb, tolb = run(t, n, k, affine, wkind, accumulate, layout, "whole")
+    assert np.all(np.abs(got - want) <= tol), np.abs(got - want).max()
+    assert np.all(np.abs(gotb - wantb) <= tolb)
+
+
+@pytest.mark.gpu
+def test_gpu_every_scale_byte_at_its_own_magnitude():
+    # a block of 32 columns has one scale byte in every row, so that each byte is seen in results of its
+    # own size; products below 2^-126 may be taken for 0
+    count, t = 231, 48
+
+    def scales_of(codes, scales):
+        scales[:, :] = 9 + np.arange(count, dtype=np.uint8)
+
+    got, want, tol, _, _, _ = run(t, 16, 32 * count, None, "f32", False, "whole", "whole",
+                                  special=scales_of)
+    assert np.all(np.abs(got - want) <= tol + t * 2.0 ** -126)
+    # and the tolerance tells a byte from its neighbours
+    assert np.all(np.median(np.abs(want) / (tol + t * 2.0 ** -126), axis=0) > 100)
