@@ -7,8 +7,10 @@
 //
 // By its bytes bound by memory: every row is read once and stays in registers between its statistics
 // and its outputs.  What is left above that is the latency of a row's two reductions with the 16 warps
-// an SM that the registers allow (bfloat16 16384 x 4096: forward with checkpoint 63 us, 5.3 TB/s;
-// backward from the checkpoint with a residual gradient 85 us, 5.5 TB/s; a copy reaches 6.55 TB/s).
+// an SM that the registers allow (bfloat16 16384 x 4096: forward with checkpoint 62 us, 5.4 TB/s;
+// backward from the checkpoint with a residual gradient 86 us, 5.5 TB/s; a copy reaches 6.55 TB/s).
+// (8 warps an SM backward for binary32 rows of 2048 and 4096 columns from the saved input with a residual
+// gradient, whose ring leaves room for one block: 16384 x 4096 242 us, 4.4 TB/s.)
 // A warp (up to 512 columns) or more of a block own a row, 16 values a thread.  The backward kernel
 // is persistent: a thread keeps the sums of its own columns over all its rows in registers and reads
 // a row ahead, the blocks' sums go to the workspace once, and a second kernel adds them in a fixed
