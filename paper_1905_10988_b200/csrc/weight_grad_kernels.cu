@@ -994,7 +994,8 @@ static WgPlan wg_plan(uint64_t rows, uint64_t n, uint64_t k, bool doubles) {
     p.sum_blocks = (int)(blocks < 1 ? 1 : blocks);
     p.runs_offset = p.splits > 1 ? left * p.splits * kWgTileFours * 16 : 0;
     // (the type of dW, and with it the chains, are the call's)
-    const bool runs = steps > kWgChainF32 && (p.tiles_n * p.tiles_k >= kWgPairs || p.splits == 1);
+    const uint32_t least_chain = kWgChainF32 < kWgChainBf16 ? kWgChainF32 : kWgChainBf16;
+    const bool runs = steps > least_chain && (p.tiles_n * p.tiles_k >= kWgPairs || p.splits == 1);
     p.sum_offset = p.runs_offset + (runs ? 2 * kWgPairs * (size_t)kWgTileFours * 16 : 0);
     p.fresh_offset = p.sum_offset + round_up16(p.sum_blocks * n * 4);
     p.scale_offset = p.fresh_offset + round_up16(n * 4);
