@@ -533,7 +533,8 @@ wg_product_kernel(const __grid_constant__ WgArgs a, const __grid_constant__ CUte
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_at(drained + 8 * b, 0);
+                // (a tile that was not waited for was not read: the other block may still be reading it)
+                if (lane == 0 && ok) mbar_arrive_at(drained + 8 * b, 0);
             }
             turns.done(w);
         }

@@ -101,6 +101,15 @@ def test_a_wait_that_runs_out_leaves_nan_and_no_partial_sums(weight_grad, rank, 
     run(weight_grad, 192, 256, 1024, "whole", "f32", 1, 0, seed, *args)
 
 
+@pytest.mark.parametrize("rank", [0, 1])
+@pytest.mark.parametrize("case", [(700, 256, 1536, "whole", "bf16", 1, 0),
+                                  (192, 1024, 1024, "whole", "f32", 0, 1)], ids=["single", "double"])
+def test_a_block_that_stands_still_loses_no_tile_to_the_next(weight_grad, case, rank):
+    # one block's writers read TMEM for longer than the other waits: what the other gives up must not
+    # count as read, or the next tile is computed over the one that is still being read
+    run(weight_grad, *case, 1, "hold_rank=%d" % rank, "hold_after=50", "hold_until=5000000000")
+
+
 @pytest.mark.parametrize("seed", range(1, 5))
 @pytest.mark.parametrize("case", [(700, 256, 1024, "whole", "f32", 1, 0),
                                   (700, 1024, 300, "whole", "f32", 1, 0),
