@@ -8,8 +8,8 @@
 //
 // bfloat16 16384 x 4096: nearest 33 us (6.2 TB/s), read back 31 us (6.6 TB/s, a copy's rate), random
 // rounding 43 us: 221 instructions for a warp's 512 values, integer pipe and issue slots at 64 % each,
-// memory at 47 %, because a thread's loads, generator block and stores follow each other.  binary32 4097 x 1001 there and back: 14 us, of two
-// launches, issue-bound.
+// memory at 47 %, because a thread's loads, generator block and stores follow each other.  binary32
+// 4097 x 1001 there and back: 14 us, of two launches, issue-bound.
 #include "act8_common.cuh"
 
 namespace natcomp {

@@ -6,6 +6,7 @@ matrix instructions take effect late and in changing order; a wait that nothing 
 gets too many arrivals or a copy in flight at a block's end is an error."""
 import concurrent.futures
 import os
+import random
 import re
 import shutil
 import subprocess
@@ -212,3 +213,45 @@ def act8(tmp_path_factory):
 def test_checkpoint_codes_and_bounds(act8, rows, cols, layout, kind):
     for random in (0, 1):
         run(act8[kind], rows, cols, layout, random, 1)
+
+
+# ---- sizes, layouts and late or missing copies at random ---------------------------------------
+
+def side(r, most, step):
+    return r.choice([r.randint(1, most), step * r.randint(1, most // step), r.randint(1, 200)])
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_weight_grad_at_random(weight_grad, short_chains, seed):
+    r = random.Random(seed)
+    program = [weight_grad, short_chains][seed % 2]
+    n, k, t = side(r, 900, 256), side(r, 700, 256), side(r, 700, 64)
+    run(program, t, n, k, r.choice(["whole", "gap", "any"]), r.choice(["f32", "bf16"]),
+        r.randint(0, 1), r.randint(0, 1), seed, "late=%d" % r.choice([3, 8, 20]))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_weight_grad_that_waits_in_vain_at_random(weight_grad, short_chains, seed):
+    # (four steps of the first tile at least have copies of scales in both blocks)
+    r = random.Random(100 + seed)
+    program = [weight_grad, short_chains][seed % 2]
+    n, k, t = side(r, 900, 256), side(r, 700, 256), r.randint(256, 700)
+    args = ["drop_rank=%d" % r.randint(0, 1), "drop_nth=0"]
+    if r.random() < 0.6:
+        args += ["hold_rank=%d" % r.randint(0, 1), "hold_after=%d" % r.choice([0, 50, 5000]),
+                 "hold_until=%d" % r.choice([1000000000, 3900000000, 5000000000])]
+    run(program, t, n, k, r.choice(["whole", "gap"]), r.choice(["f32", "bf16"]), r.randint(0, 1), 0,
+        seed, *args)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_norm_at_random(layer_norm, seed):
+    r = random.Random(200 + seed)
+    cols = r.choice([r.randint(1, 600), r.randint(1, 5000), 512 * r.randint(1, 16),
+                     r.randint(4097, 20000)])
+    rows = r.randint(1, max(1, min(80, 200000 // cols)))
+    op = r.choice(["forward", "backward"])
+    kept = r.choice(["none", "nearest"] + (["random"] if op == "forward" else []))
+    run(layer_norm[r.choice(list(TYPES))], op, rows, cols, r.choice(["whole", "gap", "any"]), kept,
+        r.randint(0, 1), r.randint(0, 1), r.randint(0, 1), 8 if cols > 4096 else r.randint(1, 3), seed,
+        "late=%d" % r.choice([2, 5, 20]))
