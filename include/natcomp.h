@@ -519,6 +519,83 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
                               int dw_dtype, size_t lddw, float* db, int accumulate,
                               void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
+/* ---- the two ends of a language model's training step, and the update behind the exchange ----------
+ * (no counterpart in the paper)
+ * tokens and targets: int32 or int64 (token_bytes, target_bytes 4 or 8) on their own boundaries.
+ * Matrices, types, alignment and overlap as in the section above; workspace is 32-byte aligned and of
+ * the size its helper names (0: the sizes are refused).  No call holds state, synchronises or
+ * allocates; two calls that may run at the same time need a workspace each, captured ones too.  Every
+ * result is the same from run to run on one device. */
+
+/* out[t] = scale * table[token[t]], rounded once.  table: dtype, vocabulary x cols.  out: out_dtype, rows
+ * x cols.  A token below 0 (padding) gives a row of 0, one beyond the vocabulary a row of NaN.
+ * rows, cols, vocabulary < 2^31, else NC_ERR_TOO_LARGE. */
+nc_status nc_embedding_forward(const void* tokens, int token_bytes, size_t rows, const void* table,
+                               int dtype, size_t vocabulary, size_t cols, size_t ldt, float scale,
+                               void* out, int out_dtype, size_t ldo, cudaStream_t stream);
+
+/* dtable[v] = scale * sum of dy[t] over the t with token[t] = v, in binary32 and rounded once.  Every
+ * row of dtable is written, rows without a token with 0; accumulate != 0: the sums are added to what
+ * dtable holds, and only rows with a token are touched.  Tokens outside the vocabulary count for
+ * nothing and their rows of dy are not read.  dy: dtype, rows x cols.  dtable: dtable_dtype.
+ * rows, vocabulary < 2^31, cols < 2^24 - 256, else NC_ERR_TOO_LARGE. */
+size_t nc_embedding_backward_workspace_bytes(size_t rows, size_t vocabulary, size_t cols);
+nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows, const void* dy,
+                                int dtype, size_t cols, size_t lddy, float scale, size_t vocabulary,
+                                void* dtable, int dtable_dtype, size_t lddt, int accumulate,
+                                void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Softmax cross entropy of the linear layer z[t][v] = scale * x[t] . table[v], whose logits are not
+ * kept:   lse[t] = log sum over v of exp z[t][v],   loss[t] = lse[t] - z[t][target[t]]
+ * x: rows x width, table: vocabulary x width, both dtype (NC_DTYPE_BF16 or NC_DTYPE_F16; others are
+ * refused).  loss, lse: fp32[rows].  0 < scale < 2e38.  A row with a target below 0 does not count: its
+ * loss and lse are 0, its x is not read and it costs nothing.  A target beyond the vocabulary gives a
+ * loss of NaN.  Products in 16 bits with binary32 accumulation, everything behind them in binary32.
+ *
+ * backward, with the forward call's lse:
+ *   dz[t][v] = exp(z - lse[t]) * (dloss[t] + dlse[t]) - (v == target[t] ? dloss[t] : 0)
+ *   dx = scale * dz table,   dtable = scale * dz^T x   (added to what dtable holds if accumulate != 0)
+ * dloss, dlse: fp32[rows], the gradients of the two results; dlse may be NULL.  dx: dtype; dtable:
+ * dtable_dtype, NC_DTYPE_F32 or dtype.  Either may be NULL and is not computed then.  Rows that do not
+ * count get dx of 0 and count for nothing, whatever x, dloss and dlse hold there; a target beyond the
+ * vocabulary makes the row's dx and all of dtable NaN.  dz is rounded to dtype (relative to the largest
+ * coefficient of any row, so that in binary16 nothing of weight vanishes): that is half a step of 16
+ * bits for each term of both sums, also where dtable is binary32.  The vocabulary is worked through in
+ * pieces whose dz takes 256 MB, or rows * 2048 values where that is more.
+ * rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256 than 2^31 (2^24 of dx),
+ * else NC_ERR_TOO_LARGE.  width or vocabulary of 0: NC_ERR_INVALID. */
+size_t nc_linear_cross_entropy_forward_workspace_bytes(size_t rows, size_t width, size_t vocabulary);
+nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows, size_t width,
+                                          size_t ldx, const void* table, size_t vocabulary, size_t ldt,
+                                          const void* targets, int target_bytes, float scale,
+                                          float* loss, float* lse, void* workspace,
+                                          size_t workspace_bytes, cudaStream_t stream);
+size_t nc_linear_cross_entropy_backward_workspace_bytes(size_t rows, size_t width, size_t vocabulary);
+nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows, size_t width,
+                                           size_t ldx, const void* table, size_t vocabulary,
+                                           size_t ldt, const void* targets, int target_bytes,
+                                           float scale, const float* lse, const float* dloss,
+                                           const float* dlse, void* dx, size_t lddx, void* dtable,
+                                           int dtable_dtype, size_t lddt, int accumulate,
+                                           void* workspace, size_t workspace_bytes,
+                                           cudaStream_t stream);
+
+/* Orthogonalised update of `batch` matrices of rows x cols by Newton-Schulz products:
+ *   X = G / (|G| + eps),  then `steps` times  X <- a X + (b A + c A A) X  with A = X X^T,  out = scale X
+ * |G|: the Frobenius norm.  A matrix with more rows than columns is treated as its transpose is.
+ * coefficients: host memory, a, b, c of every step, read before the call returns.  G: dtype, matrix i
+ * from element i * distance on; out: out_dtype, from element i * out_distance on (both ignored for one
+ * matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that holds an inf or
+ * a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits: the result is
+ * off by 1 to 2 thousandths of its norm with the five steps of (3.4445, -4.7750, 2.0315), also where
+ * out is binary32.  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, else
+ * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written. */
+size_t nc_orthogonalize_workspace_bytes(size_t batch, size_t rows, size_t cols);
+nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, size_t cols,
+                           size_t ldg, size_t distance, const float* coefficients, int steps, float eps,
+                           float scale, void* out, int out_dtype, size_t ldo, size_t out_distance,
+                           void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
 /* ---- debug build (no counterpart in the paper) ------------------------------------------------
  * `python paper_1905_10988_b200/build.py --bounds` builds libnatcomp_bounds.so with -DNC_BOUNDS:
  * the same entry points, but every global store of the C_nat and D_nat kernels (nc_compress*,

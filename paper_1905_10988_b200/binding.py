@@ -47,7 +47,11 @@ EXPORTS = (
     "nc_debug_bounds_selftest", "nc_act8_code_bytes", "nc_act8_scale_bytes", "nc_act8_compress",
     "nc_act8_decompress", "nc_layer_norm_forward", "nc_layer_norm_workspace_bytes",
     "nc_layer_norm_backward", "nc_act8_layer_norm_backward",
-    "nc_act8_weight_grad_workspace_bytes", "nc_act8_weight_grad",
+    "nc_act8_weight_grad_workspace_bytes", "nc_act8_weight_grad", "nc_embedding_forward",
+    "nc_embedding_backward_workspace_bytes", "nc_embedding_backward",
+    "nc_linear_cross_entropy_forward_workspace_bytes", "nc_linear_cross_entropy_forward",
+    "nc_linear_cross_entropy_backward_workspace_bytes", "nc_linear_cross_entropy_backward",
+    "nc_orthogonalize_workspace_bytes", "nc_orthogonalize",
 )
 
 
@@ -684,3 +688,96 @@ def nc_act8_weight_grad(dy, rows, n, lddy, codes, scales, k, gamma, beta, param_
                                 _ptr(gamma), _ptr(beta), param_dtype, _ptr(dw), dw_dtype, lddw,
                                 _ptr(db), int(accumulate), _ptr(workspace), workspace_bytes,
                                 _stream(stream)))
+
+
+# ---- the two ends of a language model's training step, and the update behind the exchange -------
+_nc_embedding_forward = _sig("nc_embedding_forward", C.c_int, _vp, C.c_int, _sz, _vp, C.c_int, _sz,
+                             _sz, _sz, C.c_float, _vp, C.c_int, _sz, _vp)
+_nc_embedding_backward_workspace_bytes = _sig("nc_embedding_backward_workspace_bytes", _sz, _sz,
+                                              _sz, _sz)
+_nc_embedding_backward = _sig("nc_embedding_backward", C.c_int, _vp, C.c_int, _sz, _vp, C.c_int,
+                              _sz, _sz, C.c_float, _sz, _vp, C.c_int, _sz, C.c_int, _vp, _sz, _vp)
+_nc_linear_cross_entropy_forward_workspace_bytes = _sig(
+    "nc_linear_cross_entropy_forward_workspace_bytes", _sz, _sz, _sz, _sz)
+_nc_linear_cross_entropy_forward = _sig("nc_linear_cross_entropy_forward", C.c_int, _vp, C.c_int,
+                                        _sz, _sz, _sz, _vp, _sz, _sz, _vp, C.c_int, C.c_float,
+                                        _vp, _vp, _vp, _sz, _vp)
+_nc_linear_cross_entropy_backward_workspace_bytes = _sig(
+    "nc_linear_cross_entropy_backward_workspace_bytes", _sz, _sz, _sz, _sz)
+_nc_linear_cross_entropy_backward = _sig("nc_linear_cross_entropy_backward", C.c_int, _vp, C.c_int,
+                                         _sz, _sz, _sz, _vp, _sz, _sz, _vp, C.c_int, C.c_float,
+                                         _vp, _vp, _vp, _vp, _sz, _vp, C.c_int, _sz, C.c_int, _vp,
+                                         _sz, _vp)
+_nc_orthogonalize_workspace_bytes = _sig("nc_orthogonalize_workspace_bytes", _sz, _sz, _sz, _sz)
+_nc_orthogonalize = _sig("nc_orthogonalize", C.c_int, _vp, C.c_int, _sz, _sz, _sz, _sz, _sz,
+                         C.POINTER(C.c_float), C.c_int, C.c_float, C.c_float, _vp, C.c_int, _sz,
+                         _sz, _vp, _sz, _vp)
+
+
+def nc_embedding_forward(tokens, token_bytes, rows, table, dtype, vocabulary, cols, ldt, scale, out,
+                         out_dtype, ldo, stream=None) -> None:
+    _check("nc_embedding_forward",
+           _nc_embedding_forward(_ptr(tokens), token_bytes, rows, _ptr(table), dtype, vocabulary,
+                                 cols, ldt, scale, _ptr(out), out_dtype, ldo, _stream(stream)))
+
+
+def nc_embedding_backward_workspace_bytes(rows: int, vocabulary: int, cols: int) -> int:
+    return int(_nc_embedding_backward_workspace_bytes(rows, vocabulary, cols))
+
+
+def nc_embedding_backward(tokens, token_bytes, rows, dy, dtype, cols, lddy, scale, vocabulary,
+                          dtable, dtable_dtype, lddt, accumulate, workspace, workspace_bytes,
+                          stream=None) -> None:
+    _check("nc_embedding_backward",
+           _nc_embedding_backward(_ptr(tokens), token_bytes, rows, _ptr(dy), dtype, cols, lddy,
+                                  scale, vocabulary, _ptr(dtable), dtable_dtype, lddt,
+                                  int(accumulate), _ptr(workspace), workspace_bytes,
+                                  _stream(stream)))
+
+
+def nc_linear_cross_entropy_forward_workspace_bytes(rows: int, width: int, vocabulary: int) -> int:
+    return int(_nc_linear_cross_entropy_forward_workspace_bytes(rows, width, vocabulary))
+
+
+def nc_linear_cross_entropy_forward(x, dtype, rows, width, ldx, table, vocabulary, ldt, targets,
+                                    target_bytes, scale, loss, lse, workspace, workspace_bytes,
+                                    stream=None) -> None:
+    _check("nc_linear_cross_entropy_forward",
+           _nc_linear_cross_entropy_forward(_ptr(x), dtype, rows, width, ldx, _ptr(table),
+                                            vocabulary, ldt, _ptr(targets), target_bytes, scale,
+                                            _ptr(loss), _ptr(lse), _ptr(workspace),
+                                            workspace_bytes, _stream(stream)))
+
+
+def nc_linear_cross_entropy_backward_workspace_bytes(rows: int, width: int, vocabulary: int) -> int:
+    return int(_nc_linear_cross_entropy_backward_workspace_bytes(rows, width, vocabulary))
+
+
+def nc_linear_cross_entropy_backward(x, dtype, rows, width, ldx, table, vocabulary, ldt, targets,
+                                     target_bytes, scale, lse, dloss, dlse, dx, lddx, dtable,
+                                     dtable_dtype, lddt, accumulate, workspace, workspace_bytes,
+                                     stream=None) -> None:
+    """dlse, dx and dtable may be None."""
+    _check("nc_linear_cross_entropy_backward",
+           _nc_linear_cross_entropy_backward(_ptr(x), dtype, rows, width, ldx, _ptr(table),
+                                             vocabulary, ldt, _ptr(targets), target_bytes, scale,
+                                             _ptr(lse), _ptr(dloss), _ptr(dlse), _ptr(dx), lddx,
+                                             _ptr(dtable), dtable_dtype, lddt, int(accumulate),
+                                             _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def nc_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    return int(_nc_orthogonalize_workspace_bytes(batch, rows, cols))
+
+
+def nc_orthogonalize(g, dtype, batch, rows, cols, ldg, distance, coefficients, steps, eps, scale,
+                     out, out_dtype, ldo, out_distance, workspace, workspace_bytes,
+                     stream=None) -> None:
+    """coefficients: 3 * steps numbers."""
+    if len(coefficients) != 3 * steps:
+        raise ValueError("%d coefficients for %d steps" % (len(coefficients), steps))
+    _check("nc_orthogonalize",
+           _nc_orthogonalize(_ptr(g), dtype, batch, rows, cols, ldg, distance,
+                             (C.c_float * len(coefficients))(*coefficients), steps, eps, scale,
+                             _ptr(out), out_dtype, ldo, out_distance, _ptr(workspace),
+                             workspace_bytes, _stream(stream)))

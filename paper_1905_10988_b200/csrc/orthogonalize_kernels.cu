@@ -1,0 +1,426 @@
+// Orthogonalised update of a weight matrix by Newton-Schulz products, for sm_100a:
+//
+//   X <- G / (|G| + eps),  then `steps` times  X <- a X + (b A + c A A) X,  A = X X^T,  out = scale X
+//
+// (|G| the Frobenius norm; of a matrix with more rows than columns A = X^T X and the polynomial is
+// applied from the right).  Each step applies the odd polynomial a s + b s^3 + c s^5 to the singular
+// values and leaves the singular vectors alone.
+//
+// The three products of a step run on the tensor cores.  A and b A + c A A are symmetric: only the tiles
+// on and above the diagonal are computed, and the products that read them take the others from their
+// mirror images, so a step of a square matrix costs four thirds of a product less.  Nothing is
+// transposed: either layout is an operand as it lies in memory.
+//
+// Numbers: operands are binary16, not bfloat16.  All of them are bounded (singular values near 1), so
+// range is no concern and the three bits more are: with bfloat16 the result is off by 1 to 2 % of its
+// norm, with binary16 by 0.1 to 0.2 %, as much as rounding it to bfloat16 costs.  X is kept in 22 bits,
+// as two binary16 values; the term a X takes both, the products the first.  With one value alone the
+// rounding of each step would grow like the smallest singular values do (a^steps, several hundred
+// times), and a gradient of low rank would come out wrong by 4 %.  X is scaled by the power of two near
+// the root of its longer side, which brings its entries to about 1, A and the polynomial by 2^8: away
+// from binary16's subnormal numbers.
+#include "product.cuh"
+
+namespace natcomp {
+
+constexpr float kOrthoGramScale = 256.0f;
+constexpr float kOrthoLow = 2048.0f;                 // of the second of X's two values
+constexpr int kOrthoNormBlocks = 128;                // per matrix at most
+
+// ---- the norm, and the first X ---------------------------------------------------------------
+
+struct OrthoInput {
+    const void* g;
+    int dtype;
+    uint64_t rows, cols, ldg, distance;
+    bool vector;                         // rows may be read 16 bytes at a time
+    double* parts;                       // [matrix][block]
+    int blocks;
+    double eps, scale;
+    __half *high, *low;
+    uint64_t pitch;
+};
+
+// eight values of a row, those beyond it 0
+template <typename T>
+__device__ __forceinline__ void ortho_load8(const OrthoInput& in, const T* row, uint64_t c,
+                                            float (&v)[8]) {
+    if (in.vector && c + 8 <= in.cols) {
+        uint32_t w[2 * sizeof(T)];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
+            w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unpack2<T>(w[i], v[2 * i], v[2 * i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < in.cols ? to_f32<T>(row[c + i]) : 0.0f;
+    }
+}
+
+// Sums of squares, in binary64: neither overflows nor vanishes for any binary32 input.
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__ OrthoInput in) {
+    __shared__ double sums[8];
+    after_previous();
+    let_next_begin();
+    const T* g = static_cast<const T*>(in.g) + blockIdx.y * in.distance;
+    const uint64_t across = (in.cols + 7) / 8, all = in.rows * across;
+    double s = 0.0;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)in.blocks * 256) {
+        const uint64_t r = i / across;
+        float v[8];
+        ortho_load8<T>(in, g + r * in.ldg, (i - r * across) * 8, v);
+        double t = 0.0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t = fma((double)v[k], (double)v[k], t);
+        s += t;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) s += sums[w];
+        in.parts[(uint64_t)blockIdx.y * in.blocks + blockIdx.x] = s;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ OrthoInput in) {
+    after_previous();
+    let_next_begin();
+    double sum = 0.0;
+    for (int i = threadIdx.x & 31; i < in.blocks; i += 32)
+        sum += __ldcg(in.parts + (uint64_t)blockIdx.y * in.blocks + i);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    const double by = sum == 0.0 ? 0.0 : in.scale / (sqrt(sum) + in.eps);
+    const bool narrow = by > 1e-37 && by < 1e37;
+    const float by32 = (float)by;
+    const T* g = static_cast<const T*>(in.g) + blockIdx.y * in.distance;
+    const uint64_t across = in.pitch / 8, all = in.rows * across;
+    const uint64_t base = (uint64_t)blockIdx.y * in.rows * in.pitch;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t r = i / across, c = (i - r * across) * 8;
+        float v[8];
+        ortho_load8<T>(in, g + r * in.ldg, c, v);
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = narrow ? v[k] * by32 : (float)((double)v[k] * by);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a, b;
+            h[k] = pack2<__half>(v[2 * k], v[2 * k + 1]);
+            unpack2<__half>(h[k], a, b);
+            l[k] = pack2<__half>((v[2 * k] - a) * kOrthoLow, (v[2 * k + 1] - b) * kOrthoLow);
+        }
+        const uint64_t at = base + r * in.pitch + c;
+        *reinterpret_cast<uint4*>(in.high + at) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(in.low + at) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+// ---- products --------------------------------------------------------------------------------
+
+// the u-th tile on or above the diagonal of one of several square matrices of `side` tiles
+__device__ __forceinline__ ProductUnit ortho_upper(uint32_t u, uint32_t side) {
+    ProductUnit w = {};
+    const uint32_t each = side * (side + 1) / 2;
+    w.z = (int)(u / each);
+    u -= (uint32_t)w.z * each;
+    uint32_t row = 0;
+    while (u >= side - row) {
+        u -= side - row;
+        ++row;
+    }
+    w.m = (int)(row * kProductTile);
+    w.n = (int)((row + u) * kProductTile);
+    return w;
+}
+
+// 16 values of a row of binary16 as they lie in a workspace
+__device__ __forceinline__ void ortho_load16(const __half* p, float (&v)[16]) {
+    const Bytes32 raw = ld_wide(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) unpack2<__half>(raw.v[i], v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void ortho_store16(__half* p, const float (&v)[16]) {
+    Bytes32 raw;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw.v[i] = pack2<__half>(v[2 * i], v[2 * i + 1]);
+    st_wide(p, raw);
+}
+
+// POLYNOMIAL: b A + c A A from A, else A from X
+template <bool POLYNOMIAL> struct OrthoSquare {
+    CUtensorMap left, right;
+    ProductSide left_side, right_side;
+    bool bf16;
+    uint32_t side, tiles, batch, steps;
+    uint64_t pitch;
+    const __half* gram;                  // POLYNOMIAL
+    __half* out;
+    float b, c;                          // c: of the product; b: of A
+
+    __device__ __forceinline__ uint32_t begin(bool) { return tiles * (tiles + 1) / 2 * batch; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+        ProductUnit w = ortho_upper(u, tiles);
+        w.steps = (int)steps;
+        return w;
+    }
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+        const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
+        const uint64_t at = ((uint64_t)w.z * side + row) * pitch + col;
+#pragma unroll 1
+        for (int k = 0; k < kProductHalf && col + k < side; k += 32) {
+            uint32_t v[32];
+            r.load(k, v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (row >= side || col + k + 16 * h >= side) continue;
+                float o[16], old[16];
+                if (POLYNOMIAL) ortho_load16(gram + at + k + 16 * h, old);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    o[i] = c * __uint_as_float(v[16 * h + i]);
+                    if (POLYNOMIAL) o[i] = fmaf(b, old[i], o[i]);
+                }
+                ortho_store16(out + at + k + 16 * h, o);
+            }
+        }
+    }
+};
+
+struct OrthoStep {
+    CUtensorMap left, right;
+    ProductSide left_side, right_side;
+    bool bf16;
+    uint32_t rows, cols, tiles_m, tiles_n, batch, steps;
+    uint64_t pitch;
+    float a;
+    const __half* high;
+    __half *low, *next;
+    void* out;                           // of the last step, else nullptr
+    uint64_t ldo, out_distance;
+    float scale;
+    ProductTarget target;
+
+    __device__ __forceinline__ uint32_t begin(bool) { return tiles_m * tiles_n * batch; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+        ProductUnit w = {};
+        const uint32_t each = tiles_m * tiles_n, z = u / each;
+        product_tile(u - z * each, tiles_m, tiles_n, w.m, w.n);
+        w.z = (int)z;
+        w.steps = (int)steps;
+        return w;
+    }
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+        const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
+        const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
+        const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
+        char* to = nullptr;
+        if (out && row < rows)
+            to = static_cast<char*>(out) + bytes * (w.z * out_distance + row * ldo + col);
+#pragma unroll 1
+        for (int k = 0; k < kProductHalf && col + k < cols; k += 32) {
+            uint32_t v[32];
+            r.load(k, v);
+            float o[32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (row >= rows || col + k + 16 * h >= cols) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[16 * h + i] = 0.0f;
+                    continue;
+                }
+                float x[16], y[16];
+                ortho_load16(high + at + k + 16 * h, x);
+                ortho_load16(low + at + k + 16 * h, y);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = fmaf(y[i], 1.0f / kOrthoLow, x[i]);
+                    x[i] = fmaf(a, x[i], __uint_as_float(v[16 * h + i]) * (1.0f / kOrthoGramScale));
+                    o[16 * h + i] = scale * x[i];
+                }
+                if (!out) {
+                    Bytes32 first, second;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float p, q;
+                        first.v[i] = pack2<__half>(x[2 * i], x[2 * i + 1]);
+                        unpack2<__half>(first.v[i], p, q);
+                        second.v[i] = pack2<__half>((x[2 * i] - p) * kOrthoLow,
+                                                    (x[2 * i + 1] - q) * kOrthoLow);
+                    }
+                    st_wide(next + at + k + 16 * h, first);
+                    st_wide(low + at + k + 16 * h, second);
+                }
+            }
+            if (out)
+                product_store(target, to ? to + bytes * k : nullptr, (int)(cols - col) - k, o, r);
+        }
+    }
+};
+
+struct OrthoPlan {
+    uint64_t side, pitch, side_pitch;
+    int blocks;
+    size_t parts, high[2], low, gram, poly, bytes;
+};
+
+static size_t ortho_place(size_t& at, size_t bytes) {
+    const size_t here = at;
+    at = (at + bytes + 255) & ~(size_t)255;
+    return here;
+}
+
+static bool ortho_fits(size_t batch, size_t rows, size_t cols) {
+    const size_t most = (size_t)1 << 20;
+    if (rows > most || cols > most || batch > 65535) return false;
+    const uint64_t tiles = ((rows + 255) / 256) * ((cols + 255) / 256);
+    return tiles * (batch ? batch : 1) < ((uint64_t)1 << 31) && batch * rows < ((uint64_t)1 << 31);
+}
+
+static OrthoPlan ortho_plan(uint64_t batch, uint64_t rows, uint64_t cols) {
+    OrthoPlan p = {};
+    p.side = rows < cols ? rows : cols;
+    p.pitch = (cols + 15) / 16 * 16;
+    p.side_pitch = (p.side + 15) / 16 * 16;
+    const uint64_t blocks = (rows * ((cols + 7) / 8) + 1023) / 1024;     // four groups of eight a thread
+    p.blocks = (int)(blocks < 1 ? 1 : blocks > kOrthoNormBlocks ? kOrthoNormBlocks : blocks);
+    size_t at = 0;
+    p.parts = ortho_place(at, 8 * batch * p.blocks);
+    for (int i = 0; i < 2; ++i) p.high[i] = ortho_place(at, 2 * batch * rows * p.pitch);
+    p.low = ortho_place(at, 2 * batch * rows * p.pitch);
+    p.gram = ortho_place(at, 2 * batch * p.side * p.side_pitch);
+    p.poly = ortho_place(at, 2 * batch * p.side * p.side_pitch);
+    p.bytes = at;
+    return p;
+}
+
+template <typename T>
+static void ortho_start(const OrthoInput& in, unsigned batch, cudaStream_t stream) {
+    launch_overlapping(ortho_norm_kernel<T>, dim3(in.blocks, batch), dim3(256), 0, stream, in);
+    const uint64_t blocks = (in.rows * (in.pitch / 8) + 255) / 256;
+    launch_overlapping(ortho_start_kernel<T>, dim3((unsigned)(blocks < 1184 ? blocks : 1184), batch),
+                       dim3(256), 0, stream, in);
+}
+
+}  // namespace natcomp
+
+using namespace natcomp;
+
+extern "C" {
+
+size_t nc_orthogonalize_workspace_bytes(size_t batch, size_t rows, size_t cols) {
+    return ortho_fits(batch, rows, cols) ? ortho_plan(batch, rows, cols).bytes : 0;
+}
+
+nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, size_t cols,
+                           size_t ldg, size_t distance, const float* coefficients, int steps, float eps,
+                           float scale, void* out, int out_dtype, size_t ldo, size_t out_distance,
+                           void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    const int bytes = act8_type_bytes(dtype), out_bytes = act8_type_bytes(out_dtype);
+    if (!bytes || !out_bytes) return NC_ERR_UNSUPPORTED;
+    if (steps < 0 || (steps && !coefficients) || !(eps >= 0.0f)) return NC_ERR_INVALID;
+    if (batch == 0 || rows == 0 || cols == 0) return NC_OK;
+    if (!g || !out || !workspace || ldg < cols || ldo < cols) return NC_ERR_INVALID;
+    if (!ortho_fits(batch, rows, cols)) return NC_ERR_TOO_LARGE;
+    if (batch > 1 && (distance < (rows - 1) * ldg + cols || out_distance < (rows - 1) * ldo + cols))
+        return NC_ERR_INVALID;
+    if (!element_aligned(g, bytes) || !element_aligned(out, out_bytes) || !aligned32(workspace))
+        return NC_ERR_ALIGN;
+    const OrthoPlan p = ortho_plan(batch, rows, cols);
+    if (workspace_bytes < p.bytes) return NC_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    __half* high[2] = {reinterpret_cast<__half*>(ws + p.high[0]),
+                       reinterpret_cast<__half*>(ws + p.high[1])};
+    __half* low = reinterpret_cast<__half*>(ws + p.low);
+    __half* gram = reinterpret_cast<__half*>(ws + p.gram);
+    __half* poly = reinterpret_cast<__half*>(ws + p.poly);
+    const uint64_t longer = rows > cols ? rows : cols;
+    const bool tall = rows > cols;
+    int exponent = 0;                    // 2^exponent about the root of the longer side
+    while (((uint64_t)1 << (2 * (exponent + 1))) <= longer) ++exponent;
+    const float up = (float)(1 << exponent);
+
+    OrthoInput in = {};
+    in.g = g; in.dtype = dtype; in.rows = rows; in.cols = cols; in.ldg = ldg;
+    in.distance = batch > 1 ? distance : 0;
+    in.vector = row_access(g, ldg, bytes, rows) != kRowElement &&
+                (batch == 1 || distance * bytes % 16 == 0);
+    in.parts = reinterpret_cast<double*>(ws + p.parts); in.blocks = p.blocks;
+    in.eps = eps; in.scale = up; in.high = high[0]; in.low = low; in.pitch = p.pitch;
+    if (dtype == NC_DTYPE_F32) ortho_start<float>(in, (unsigned)batch, stream);
+    else if (dtype == NC_DTYPE_BF16) ortho_start<__nv_bfloat16>(in, (unsigned)batch, stream);
+    else ortho_start<__half>(in, (unsigned)batch, stream);
+
+    const uint64_t side_distance = p.side * p.side_pitch;
+    const uint32_t tiles = (uint32_t)((p.side + 255) / 256);
+    CUtensorMap x_map[2], gram_map, poly_map;
+    for (int i = 0; i < 2; ++i)
+        if (!make_box_map(&x_map[i], high[i], false, batch, rows, cols, p.pitch, rows * p.pitch))
+            return NC_ERR_CUDA;
+    if (!make_box_map(&gram_map, gram, false, batch, p.side, p.side, p.side_pitch, side_distance) ||
+        !make_box_map(&poly_map, poly, false, batch, p.side, p.side, p.side_pitch, side_distance))
+        return NC_ERR_CUDA;
+    OrthoSquare<false> s = {};
+    s.left_side.lines = s.right_side.lines = tall;
+    s.side = (uint32_t)p.side; s.tiles = tiles; s.batch = (uint32_t)batch; s.pitch = p.side_pitch;
+    s.steps = (uint32_t)((longer + kProductStep - 1) / kProductStep);
+    s.out = gram; s.c = kOrthoGramScale / (up * up);
+    OrthoSquare<true> q = {};
+    q.left = q.right = gram_map;
+    q.left_side.symmetric = q.right_side.symmetric = true;
+    q.side = s.side; q.tiles = tiles; q.batch = s.batch; q.pitch = p.side_pitch;
+    q.steps = (uint32_t)((p.side + kProductStep - 1) / kProductStep);
+    q.gram = gram; q.out = poly;
+    OrthoStep t = {};
+    (tall ? t.right_side : t.left_side).symmetric = true;
+    if (!tall) t.right_side.lines = true;
+    t.rows = (uint32_t)rows; t.cols = (uint32_t)cols; t.batch = (uint32_t)batch;
+    t.tiles_m = (uint32_t)((rows + 255) / 256); t.tiles_n = (uint32_t)((cols + 255) / 256);
+    t.pitch = p.pitch; t.low = low;
+    t.ldo = ldo; t.out_distance = batch > 1 ? out_distance : 0; t.scale = scale / up;
+    t.target.dtype = out_dtype;
+    t.target.access = row_access(out, ldo, out_bytes, rows);
+    if (batch > 1) {                     // every matrix starts where the first one might
+        const size_t apart = out_distance * out_bytes;
+        if (apart % 16) t.target.access = kRowElement;
+        else if (apart % 32 && t.target.access == kRowWide) t.target.access = kRow16;
+    }
+    const uint64_t upper = (uint64_t)tiles * (tiles + 1) / 2 * batch;
+    const uint64_t whole = (uint64_t)t.tiles_m * t.tiles_n * batch;
+    const int rounds = steps ? steps : 1;
+    for (int i = 0; i < rounds; ++i) {
+        nc_status st = NC_OK;
+        if (steps) {
+            s.left = s.right = x_map[i & 1];
+            st = product_launch(s, upper, stream);
+            if (st != NC_OK) return st;
+            q.b = coefficients[3 * i + 1];
+            q.c = coefficients[3 * i + 2] / kOrthoGramScale;
+            st = product_launch(q, upper, stream);
+            if (st != NC_OK) return st;
+        }
+        t.left = tall ? x_map[i & 1] : poly_map;
+        t.right = tall ? poly_map : x_map[i & 1];
+        t.a = steps ? coefficients[3 * i] : 1.0f;
+        t.steps = steps ? q.steps : 0;   // no steps: the normalised matrix
+        t.high = high[i & 1]; t.next = high[(i + 1) & 1];
+        t.out = i + 1 == rounds ? out : nullptr;
+        st = product_launch(t, whole, stream);
+        if (st != NC_OK) return st;
+    }
+    return launch_status();
+}
+
+}  // extern "C"
