@@ -208,69 +208,80 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
 
 // ---- forward ---------------------------------------------------------------------------------
 
-struct CeLogits {
+// The tensor cores cut off what an accumulator of 24 bits cannot hold, always towards 0, so all logits of
+// a long sum are too small: by 5e-7 of their size after 1024 products, 9e-7 after 2048, twice that after
+// 4096, and the loss with them.  CHAINS: longer sums are read out every 1024 products and added up in
+// registers (128 of a thread's), rounded to nearest, while the next ones are computed; the error stays
+// that of 1024.
+constexpr uint32_t kCeChain = 16;                    // steps
+
+template <bool CHAINS> struct CeLogits {
     CUtensorMap left, right;             // gathered rows, piece of the table
     ProductSide left_side, right_side;
     bool bf16;
     CeRows rows;
     uint32_t columns, tiles_n;           // of the piece
     uint32_t first;                      // its first vocabulary entry
-    uint32_t steps;
+    uint32_t steps, parts_of;            // parts_of: chains of a sum
     float unit;                          // scale * log2 e
     float scale;
     float2* parts;                       // [tile of the vocabulary][pitch of the rows]: maximum, sum
     uint64_t part_pitch;
     uint32_t count;
 
+    static constexpr int kColumns = CHAINS ? 16 : 32;        // at a time
+    struct State {
+        float sums[CHAINS ? kProductHalf : 1];
+    };
     __device__ __forceinline__ uint32_t begin(bool) {
         count = __ldcg(rows.count);
         return (count + kProductTile - 1) / kProductTile * tiles_n;
     }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    __device__ __forceinline__ uint32_t chains() const { return CHAINS ? parts_of : 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t chain) const {
         ProductUnit w = {};
         product_tile(u, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
         w.steps = (int)steps;
+        if (CHAINS) {
+            const uint32_t from = steps * chain / parts_of;
+            w.k = (int)from * kProductStep;
+            w.steps = (int)(steps * (chain + 1) / parts_of - from);
+            w.part = chain;
+        }
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
+        if (CHAINS && w.part + 1 < parts_of) {
+#pragma unroll
+            for (int c = 0; c < kProductHalf; c += kColumns) {
+                uint32_t v[kColumns];
+                r.load(c, v);
+#pragma unroll
+                for (int i = 0; i < kColumns; ++i)
+                    s.sums[c + i] = w.part ? s.sums[c + i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+            }
+            return;
+        }
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint32_t target = row < count ? __ldcg(rows.target + row) : kCeNone;
-        const float lowest = __uint_as_float(0xFF800000u);
-        float top = lowest, sum = 0.0f;
-#pragma unroll 1
-        for (int c = 0; c < kProductHalf && col + c < columns; c += 32) {
-            uint32_t v[32];
+        const uint32_t at = target - first - col;            // of the target among these columns
+        const bool near = target != kCeNone && target >= first + col && at < (uint32_t)kProductHalf;
+        float top = __uint_as_float(0xFF800000u), sum = 0.0f;
+#pragma unroll (CHAINS ? kProductHalf / kColumns : 1)
+        for (int c = 0; c < kProductHalf; c += kColumns) {
+            if (col + c >= columns) break;
+            uint32_t v[kColumns];
             r.load(c, v);
-            if (col + c + 32 > columns) {
+            if (CHAINS) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (col + c + i >= columns) v[i] = 0xFF800000u;
+                for (int i = 0; i < kColumns; ++i)
+                    v[i] = __float_as_uint(s.sums[c + i] + __uint_as_float(v[i]));
             }
-            float m[4] = {top, lowest, lowest, lowest};
-#pragma unroll
-            for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(v[i]));
-            const float next = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-            const float from = next == lowest ? 0.0f : next;     // nothing but -inf so far
-            const float shift = -from * unit;
-            float s[4] = {sum * exp2_approx((top - from) * unit), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                s[i & 3] += exp2_approx(fmaf(__uint_as_float(v[i]), unit, shift));
-            sum = (s[0] + s[1]) + (s[2] + s[3]);
-            top = next;
-        }
-        // the target's logit, where it is among these columns
-        const uint32_t at = target - first - col;
-        uint32_t mask = __ballot_sync(0xFFFFFFFFu, target != kCeNone && target >= first + col &&
-                                                       at < (uint32_t)kProductHalf);
-        while (mask) {
-            const int who = __ffs(mask) - 1;
-            mask &= mask - 1;
-            const uint32_t c = __shfl_sync(0xFFFFFFFFu, at, who);
-            const uint32_t v = r.nothing ? 0u : tmem_load1(r.tmem + c);
-            if (r.lane == who) rows.hit[row] = r.ok ? scale * __uint_as_float(v) : __uint_as_float(0x7FC00000u);
+            take(v, col + c, row, near && at >= (uint32_t)c && at < (uint32_t)c + kColumns, at - c, top,
+                 sum);
         }
         // the two halves of the columns
+        const float lowest = __uint_as_float(0xFF800000u);
         float2* other = reinterpret_cast<float2*>(r.exchange) + r.lane;
         if (r.half) *other = make_float2(top, sum);
         product_pair_barrier(r);
@@ -283,6 +294,35 @@ struct CeLogits {
                     make_float2(next, sum);
         }
         product_pair_barrier(r);
+    }
+    // neighbouring logits of a row, from vocabulary entry first + col on; here: the target is the `at`-th of them
+    __device__ __forceinline__ void take(uint32_t (&v)[kColumns], uint32_t col, uint32_t row, bool here,
+                                         uint32_t at, float& top, float& sum) const {
+        const float lowest = __uint_as_float(0xFF800000u);
+        if (col + kColumns > columns) {
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i)
+                if (col + i >= columns) v[i] = 0xFF800000u;
+        }
+        if (here) {
+            uint32_t hit = 0;
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i)
+                if (at == (uint32_t)i) hit = v[i];
+            rows.hit[row] = scale * __uint_as_float(hit);
+        }
+        float m[4] = {top, lowest, lowest, lowest};
+#pragma unroll
+        for (int i = 0; i < kColumns; ++i) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(v[i]));
+        const float next = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        const float from = next == lowest ? 0.0f : next;     // nothing but -inf so far
+        const float shift = -from * unit;
+        float s[4] = {sum * exp2_approx((top - from) * unit), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < kColumns; ++i)
+            s[i & 3] += exp2_approx(fmaf(__uint_as_float(v[i]), unit, shift));
+        sum = (s[0] + s[1]) + (s[2] + s[3]);
+        top = next;
     }
 };
 
@@ -365,13 +405,15 @@ template <typename T> struct CeDz {
         }
         return (count + kProductTile - 1) / kProductTile * tiles_n;
     }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    typedef ProductNothing State;
+    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
         product_tile(u, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
         w.steps = (int)steps;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const bool counts = row < count;
         const uint32_t target = counts ? __ldcg(rows.target + row) : 0u;
@@ -380,34 +422,29 @@ template <typename T> struct CeDz {
         float all = counts ? __ldcg(rows.both + row) * inverse : 0.0f;
         if (target == kCeNone) all = __uint_as_float(0x7FC00000u);
         const uint32_t keep = counts ? 0xFFFFFFFFu : 0u;
+        const uint32_t at = target - first - col;            // of the target among these columns
+        const bool near = counts && target != kCeNone && target >= first + col &&
+                          at < (uint32_t)kProductHalf;
         T* to = dz + (uint64_t)row * pitch + col;
 #pragma unroll 1
         for (int c = 0; c < kProductHalf; c += 32) {
             uint32_t v[32];
             r.load(c, v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                v[i] = __float_as_uint(all * exp2_approx(fmaf(__uint_as_float(v[i]), unit, shift)));
+            if (near && at >= (uint32_t)c && at < (uint32_t)c + 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)     // (a sum, not a store: v stays in registers)
+                    v[i] = __float_as_uint(__uint_as_float(v[i]) - (at - c == (uint32_t)i ? hot : 0.0f));
+            }
             Bytes32 o[2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float a = all * exp2_approx(fmaf(__uint_as_float(v[2 * i]), unit, shift));
-                const float b = all * exp2_approx(fmaf(__uint_as_float(v[2 * i + 1]), unit, shift));
-                o[i >> 3].v[i & 7] = pack2<T>(a, b) & keep;
-            }
+            for (int i = 0; i < 16; ++i)
+                o[i >> 3].v[i & 7] =
+                    pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) & keep;
             st_wide(to + c, o[0]);
             st_wide(to + c + 16, o[1]);
-        }
-        const uint32_t at = target - first - col;
-        uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts && target != kCeNone &&
-                                                       target >= first + col &&
-                                                       at < (uint32_t)kProductHalf);
-        while (mask) {
-            const int who = __ffs(mask) - 1;
-            mask &= mask - 1;
-            const uint32_t c = __shfl_sync(0xFFFFFFFFu, at, who);
-            const uint32_t v = r.nothing ? 0u : tmem_load1(r.tmem + c);
-            if (r.lane == who) {
-                const float p = exp2_approx(fmaf(__uint_as_float(v), unit, shift));
-                to[c] = from_f32<T>(r.ok ? fmaf(all, p, -hot) : __uint_as_float(0x7FC00000u));
-            }
         }
     }
 };
@@ -438,7 +475,9 @@ struct CeDx {
         factor = reads_out ? ce_factor(rows, scale, bf16) : 0.0f;
         return (count + kProductTile - 1) / kProductTile * tiles_n * splits;
     }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    typedef ProductNothing State;
+    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
         w.part = u % splits;
         product_tile(u / splits, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
@@ -447,7 +486,7 @@ struct CeDx {
         w.steps = (int)((uint32_t)((uint64_t)steps * (w.part + 1) / splits) - from);
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         float* sum = sums + w.part * split_distance + (uint64_t)row * pitch + col;
         char* to = nullptr;
@@ -524,13 +563,15 @@ struct CeDtable {
         factor = reads_out ? ce_factor(rows, scale, bf16) : 0.0f;
         return tiles_m * tiles_n;
     }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    typedef ProductNothing State;
+    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
         product_tile(u, tiles_m, tiles_n, w.m, w.n);
         w.steps = (int)((count + kProductStep - 1) / kProductStep);
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         void* to = row < entries ? product_at(dtable, target.dtype, (uint64_t)row * ldt + col) : nullptr;
         const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
@@ -778,16 +819,20 @@ nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows,
         const uint64_t count = vocabulary - first < step ? vocabulary - first : step;
         uint64_t stride = 0;
         const void* piece = t.piece(first, count, stride);
-        CeLogits a = {};
-        if (!make_box_map(&a.left, to.x, bf16, 1, p.rows_pitch, width, p.pitch, 0) ||
-            !make_box_map(&a.right, piece, bf16, 1, count, width, stride, 0))
+        const uint32_t steps = (uint32_t)((width + kProductStep - 1) / kProductStep);
+        CUtensorMap x_map, table_map;
+        if (!make_box_map(&x_map, to.x, bf16, 1, p.rows_pitch, width, p.pitch, 0) ||
+            !make_box_map(&table_map, piece, bf16, 1, count, width, stride, 0))
             return NC_ERR_CUDA;
-        a.bf16 = bf16; a.rows = to; a.columns = (uint32_t)count;
-        a.tiles_n = (uint32_t)((count + 255) / 256); a.first = (uint32_t)first;
-        a.steps = (uint32_t)((width + kProductStep - 1) / kProductStep);
-        a.unit = scale * kLog2E; a.scale = scale;
-        a.parts = reinterpret_cast<float2*>(ws + p.parts); a.part_pitch = p.rows_pitch;
-        const nc_status st = product_launch(a, p.rows_pitch / 256 * a.tiles_n, stream);
+        const auto launch = [&](auto a) {
+            a.left = x_map; a.right = table_map; a.bf16 = bf16; a.rows = to;
+            a.columns = (uint32_t)count; a.tiles_n = (uint32_t)((count + 255) / 256);
+            a.first = (uint32_t)first; a.steps = steps; a.parts_of = (steps + kCeChain - 1) / kCeChain;
+            a.unit = scale * kLog2E; a.scale = scale;
+            a.parts = reinterpret_cast<float2*>(ws + p.parts); a.part_pitch = p.rows_pitch;
+            return product_launch(a, p.rows_pitch / 256 * a.tiles_n, stream);
+        };
+        const nc_status st = steps > kCeChain ? launch(CeLogits<true>{}) : launch(CeLogits<false>{});
         if (st != NC_OK) return st;
     }
     const uint64_t blocks = (rows + 31) / 32;

@@ -16,7 +16,9 @@
 // norm, with binary16 by 0.1 to 0.2 %, as much as rounding it to bfloat16 costs.  X is kept in 22 bits,
 // as two binary16 values; the term a X takes both, the products the first.  With one value alone the
 // rounding of each step would grow like the smallest singular values do (a^steps, several hundred
-// times), and a gradient of low rank would come out wrong by 4 %.  X is scaled by the power of two near
+// times), and a gradient of low rank would come out wrong by 4 %.  The diagonal of the polynomial, which
+// is most of it once the singular values are near 1, stays in binary32 and outside the product (off by
+// 1.7e-3 of the norm instead of 2.4e-3 for random 256 x 512).  X is scaled by the power of two near
 // the root of its longer side, which brings its entries to about 1, A and the polynomial by 2^8: away
 // from binary16's subnormal numbers.
 #include "product.cuh"
@@ -168,15 +170,18 @@ template <bool POLYNOMIAL> struct OrthoSquare {
     uint64_t pitch;
     const __half* gram;                  // POLYNOMIAL
     __half* out;
+    float* diagonal;                     // POLYNOMIAL: [matrix][pitch]; out has 0 there
     float b, c;                          // c: of the product; b: of A
 
     __device__ __forceinline__ uint32_t begin(bool) { return tiles * (tiles + 1) / 2 * batch; }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    typedef ProductNothing State;
+    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = ortho_upper(u, tiles);
         w.steps = (int)steps;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint64_t at = ((uint64_t)w.z * side + row) * pitch + col;
 #pragma unroll 1
@@ -193,6 +198,14 @@ template <bool POLYNOMIAL> struct OrthoSquare {
                     o[i] = c * __uint_as_float(v[16 * h + i]);
                     if (POLYNOMIAL) o[i] = fmaf(b, old[i], o[i]);
                 }
+                if (POLYNOMIAL && row - (col + k + 16 * h) < 16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (row == col + k + 16 * h + i) {
+                            diagonal[w.z * pitch + row] = o[i] * (1.0f / kOrthoGramScale);
+                            o[i] = 0.0f;
+                        }
+                }
                 ortho_store16(out + at + k + 16 * h, o);
             }
         }
@@ -206,6 +219,9 @@ struct OrthoStep {
     uint32_t rows, cols, tiles_m, tiles_n, batch, steps;
     uint64_t pitch;
     float a;
+    const float* diagonal;               // of the polynomial: by rows, or, tall, by columns
+    uint64_t diagonal_pitch;
+    bool tall;
     const __half* high;
     __half *low, *next;
     void* out;                           // of the last step, else nullptr
@@ -214,7 +230,9 @@ struct OrthoStep {
     ProductTarget target;
 
     __device__ __forceinline__ uint32_t begin(bool) { return tiles_m * tiles_n * batch; }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u) const {
+    typedef ProductNothing State;
+    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
         const uint32_t each = tiles_m * tiles_n, z = u / each;
         product_tile(u - z * each, tiles_m, tiles_n, w.m, w.n);
@@ -222,13 +240,15 @@ struct OrthoStep {
         w.steps = (int)steps;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
         const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
         char* to = nullptr;
         if (out && row < rows)
             to = static_cast<char*>(out) + bytes * (w.z * out_distance + row * ldo + col);
+        const float* d = diagonal + w.z * diagonal_pitch;
+        const float of_row = steps && !tall && row < rows ? __ldcg(d + row) : 0.0f;
 #pragma unroll 1
         for (int k = 0; k < kProductHalf && col + k < cols; k += 32) {
             uint32_t v[32];
@@ -241,13 +261,21 @@ struct OrthoStep {
                     for (int i = 0; i < 16; ++i) o[16 * h + i] = 0.0f;
                     continue;
                 }
-                float x[16], y[16];
+                float x[16], y[16], f[16];
                 ortho_load16(high + at + k + 16 * h, x);
                 ortho_load16(low + at + k + 16 * h, y);
 #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float4 q = make_float4(of_row, of_row, of_row, of_row);
+                    if (steps && tall) q = __ldcg(reinterpret_cast<const float4*>(d + col + k + 16 * h) + i);
+                    f[4 * i] = q.x; f[4 * i + 1] = q.y; f[4 * i + 2] = q.z; f[4 * i + 3] = q.w;
+                }
+#pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    x[i] = fmaf(y[i], 1.0f / kOrthoLow, x[i]);
-                    x[i] = fmaf(a, x[i], __uint_as_float(v[16 * h + i]) * (1.0f / kOrthoGramScale));
+                    const float all = fmaf(y[i], 1.0f / kOrthoLow, x[i]);
+                    const float product =
+                        fmaf(f[i], x[i], __uint_as_float(v[16 * h + i]) * (1.0f / kOrthoGramScale));
+                    x[i] = fmaf(a, all, product);
                     o[16 * h + i] = scale * x[i];
                 }
                 if (!out) {
@@ -273,7 +301,7 @@ struct OrthoStep {
 struct OrthoPlan {
     uint64_t side, pitch, side_pitch;
     int blocks;
-    size_t parts, high[2], low, gram, poly, bytes;
+    size_t parts, high[2], low, gram, poly, diagonal, bytes;
 };
 
 static size_t ortho_place(size_t& at, size_t bytes) {
@@ -302,6 +330,7 @@ static OrthoPlan ortho_plan(uint64_t batch, uint64_t rows, uint64_t cols) {
     p.low = ortho_place(at, 2 * batch * rows * p.pitch);
     p.gram = ortho_place(at, 2 * batch * p.side * p.side_pitch);
     p.poly = ortho_place(at, 2 * batch * p.side * p.side_pitch);
+    p.diagonal = ortho_place(at, 4 * batch * p.side_pitch);
     p.bytes = at;
     return p;
 }
@@ -346,6 +375,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     __half* low = reinterpret_cast<__half*>(ws + p.low);
     __half* gram = reinterpret_cast<__half*>(ws + p.gram);
     __half* poly = reinterpret_cast<__half*>(ws + p.poly);
+    float* diagonal = reinterpret_cast<float*>(ws + p.diagonal);
     const uint64_t longer = rows > cols ? rows : cols;
     const bool tall = rows > cols;
     int exponent = 0;                    // 2^exponent about the root of the longer side
@@ -382,13 +412,14 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     q.left_side.symmetric = q.right_side.symmetric = true;
     q.side = s.side; q.tiles = tiles; q.batch = s.batch; q.pitch = p.side_pitch;
     q.steps = (uint32_t)((p.side + kProductStep - 1) / kProductStep);
-    q.gram = gram; q.out = poly;
+    q.gram = gram; q.out = poly; q.diagonal = diagonal;
     OrthoStep t = {};
     (tall ? t.right_side : t.left_side).symmetric = true;
     if (!tall) t.right_side.lines = true;
     t.rows = (uint32_t)rows; t.cols = (uint32_t)cols; t.batch = (uint32_t)batch;
     t.tiles_m = (uint32_t)((rows + 255) / 256); t.tiles_n = (uint32_t)((cols + 255) / 256);
-    t.pitch = p.pitch; t.low = low;
+    t.pitch = p.pitch; t.low = low; t.tall = tall;
+    t.diagonal = diagonal; t.diagonal_pitch = p.side_pitch;
     t.ldo = ldo; t.out_distance = batch > 1 ? out_distance : 0; t.scale = scale / up;
     t.target.dtype = out_dtype;
     t.target.access = row_access(out, ldo, out_bytes, rows);

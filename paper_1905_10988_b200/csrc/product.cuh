@@ -81,17 +81,6 @@ __device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
                    "+r"(r[30]), "+r"(r[31])::"memory");
 }
 
-// one column of the warp's 32 lanes
-__device__ __forceinline__ uint32_t tmem_load1(uint32_t tmem) {
-    uint32_t r;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\t"
-                 "tcgen05.wait::ld.sync.aligned;"
-                 : "=r"(r)
-                 : "r"(tmem)
-                 : "memory");
-    return r;
-}
-
 // operands of one type; lines: the contraction index runs over the lines of shared memory, else along
 // them
 __host__ __device__ constexpr uint32_t mma_shape_of(uint32_t m, uint32_t n, bool bf16, bool a_lines,
@@ -168,6 +157,18 @@ struct ProductSide {
     }
 };
 
+// the next chain of a unit, or the first of the pair's next unit
+template <typename Job>
+__device__ __forceinline__ void product_next(const Job& job, uint32_t& u, uint32_t& chain,
+                                             uint32_t pairs) {
+    if (++chain >= job.chains()) {
+        chain = 0;
+        u += pairs;
+    }
+}
+
+struct ProductNothing {};
+
 // what a thread that reads a tile out has: one row, 128 of the columns
 struct ProductRead {
     uint32_t tmem;                       // of the warp's lanes and of its first column
@@ -176,18 +177,29 @@ struct ProductRead {
     bool ok, nothing;                    // !ok: a wait ran out, no result;  nothing: no steps
     float* rows;                         // the warp's own 32 x 33 words of shared memory
     float* exchange;                     // 32 x 33 words that the two warps of a quarter share
-    __device__ __forceinline__ void load(int c, uint32_t (&r)[32]) const {
+    template <int N> __device__ __forceinline__ void load(int c, uint32_t (&r)[N]) const {
         if (nothing) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = 0u;
+            for (int i = 0; i < N; ++i) r[i] = 0u;
         } else {
             __syncwarp();
-            tmem_load32(tmem + c, r);
-            tmem_wait32(r);
+            if constexpr (N == 32) {
+                tmem_load32(tmem + c, r);
+                tmem_wait32(r);
+            } else {
+                static_assert(N == 16, "");
+                uint32_t a[2][8];
+                tmem_load8(tmem + c, a[0]);
+                tmem_load8(tmem + c + 8, a[1]);
+                tmem_wait8(a[0]);
+                tmem_wait8(a[1]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r[i] = a[i >> 3][i & 7];
+            }
         }
         if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = 0x7FC00000u;
+            for (int i = 0; i < N; ++i) r[i] = 0x7FC00000u;
         }
     }
 };
@@ -281,8 +293,10 @@ __device__ __forceinline__ void* product_at(void* p, int dtype, uint64_t i) {
 //   CUtensorMap left, right;  ProductSide left_side, right_side;  bool bf16;
 //   uint32_t begin(bool reads_out)    the number of units, for every thread once (may read what earlier
 //                                     kernels wrote); reads_out: of the warps that read tiles out
-//   ProductUnit unit_of(uint32_t u) const
-//   void store(const ProductUnit&, const ProductRead&)      all 256 threads that read tiles out
+//   uint32_t chains() const           parts that the sum of a unit is read out in, one after the other
+//   ProductUnit unit_of(uint32_t u, uint32_t chain) const
+//   struct State                      what a thread keeps from one chain to the next
+//   void store(const ProductUnit&, const ProductRead&, State&)      all 256 threads that read tiles out
 //
 // A wait that runs out leaves NaN: the first block's issuing thread tells both blocks before it lets
 // the tile count as complete.
@@ -337,15 +351,16 @@ product_kernel(const __grid_constant__ Job given) {
         r.exchange =
             reinterpret_cast<float*>(base + kProductBars + 256) + r.quarter * (kProductRows / 4);
         uint32_t turn = 0;
-        for (uint32_t u = pair; u < units; u += pairs, ++turn) {
-            const ProductUnit w = job.unit_of(u);
+        typename Job::State state;
+        for (uint32_t u = pair, chain = 0; u < units; product_next(job, u, chain, pairs), ++turn) {
+            const ProductUnit w = job.unit_of(u, chain);
             const uint32_t b = turn & 1;
             const bool ok = mbar_wait(full + 8 * b, (turn >> 1) & 1, gave_up);
             r.ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
             r.nothing = w.steps == 0;
             tc_fence_after();
             r.tmem = tmem + b * kProductTile + r.column + ((uint32_t)(32 * r.quarter) << 16);
-            job.store(w, r);
+            job.store(w, r, state);
             tc_fence_before();
             __syncwarp();
             // (a tile that was not waited for was not read: the other block may still be reading it)
@@ -355,8 +370,8 @@ product_kernel(const __grid_constant__ Job given) {
         if (lane == 0) {
             uint32_t step = 0, stage = 0, parity = 0;
             bool ok = true;
-            for (uint32_t u = pair; u < units && ok; u += pairs) {
-                const ProductUnit w = job.unit_of(u);
+            for (uint32_t u = pair, chain = 0; u < units && ok; product_next(job, u, chain, pairs)) {
+                const ProductUnit w = job.unit_of(u, chain);
                 const int m = w.m + (int)rank * kProductHalf, n = w.n + (int)rank * kProductHalf;
                 for (int s = 0; s < w.steps; ++s, ++step) {
                     if (step >= kProductStages) ok = mbar_wait(empty + 8 * stage, parity ^ 1, gave_up);
@@ -390,8 +405,9 @@ product_kernel(const __grid_constant__ Job given) {
         const uint32_t plain = mma_shape_of(kProductTile, kProductTile, job.bf16, false, false);
         bool ok = true;
         uint32_t stage = 0, parity = 0, turn = 0;
-        for (uint32_t u = pair; u < units && ok; u += pairs, ++turn) {
-            const ProductUnit w = job.unit_of(u);
+        for (uint32_t u = pair, chain = 0; u < units && ok;
+             product_next(job, u, chain, pairs), ++turn) {
+            const ProductUnit w = job.unit_of(u, chain);
             const uint32_t b = turn & 1, to = tmem + b * kProductTile;
             ok = mbar_wait(drained + 8 * b, ((turn >> 1) & 1) ^ 1, gave_up);
             for (int s = 0; s < w.steps; ++s) {

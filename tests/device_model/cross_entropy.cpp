@@ -21,7 +21,8 @@ int main(int argc, char** argv) {
     const bool acc = atoi(argv[8]), with_dlse = atoi(argv[9]);
     model::rng.seed(atoi(argv[10]));
     const bool injected = ::injected(argc, argv, 11);
-    model::cluster_of[(const void*)product_kernel<CeLogits>] = 2;
+    model::cluster_of[(const void*)product_kernel<CeLogits<false>>] = 2;
+    model::cluster_of[(const void*)product_kernel<CeLogits<true>>] = 2;
     model::cluster_of[(const void*)product_kernel<CeDz<__nv_bfloat16>>] = 2;
     model::cluster_of[(const void*)product_kernel<CeDz<__half>>] = 2;
     model::cluster_of[(const void*)product_kernel<CeDx>] = 2;

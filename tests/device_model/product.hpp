@@ -1,5 +1,5 @@
 // What product.cuh and the kernels on it call beyond model.hpp: pairs' copies of boxes, reads of TMEM by
-// 32 columns and by one, matrix instructions of both types and layouts, votes and atomics.  (Spliced
+// 32 columns, matrix instructions of both types and layouts, votes and atomics.  (Spliced
 // into the translated text after act8_common.cuh and tensor_core.cuh: no includes.)
 
 inline int __ffs(uint32_t v) { return __builtin_ffs((int)v); }
@@ -65,19 +65,6 @@ inline void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
     for (int i = 0; i < 4; ++i) tmem_load8(at + 8 * i, reinterpret_cast<uint32_t(&)[8]>(r[8 * i]));
 }
 inline void tmem_wait32(uint32_t (&)[32]) {}
-inline uint32_t tmem_load1(uint32_t at) {
-    // (as a warp: all lanes name the same column)
-    const uint64_t* s = model::exchange(at);
-    for (int i = 0; i < 32; ++i)
-        if (s[i] != at) model::fail("lanes that read different columns");
-    const uint32_t rank = model::cur->block->rank, lanes = at >> 16, column = at & 0xFFFF;
-    const uint32_t warp = model::cur->index >> 5, lane = model::cur->index & 31;
-    if (lanes != 32 * (warp & 3) || column >= 512) model::fail("TMEM that a warp cannot read");
-    uint32_t v;
-    memcpy(&v, &model::W.tmem[(rank * 128 + lanes + lane) * 512 + column], 4);
-    return v;
-}
-
 inline float exp2_approx(float x) { return exp2f(x); }
 inline Bytes32 ld_wide(const void* p) {
     if ((uintptr_t)p % 32) model::fail("load that is not aligned");

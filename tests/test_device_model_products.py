@@ -67,7 +67,7 @@ def cross_entropy(tmp_path_factory):
 @pytest.fixture(scope="module")
 def small_pieces(tmp_path_factory):
     return build(tmp_path_factory.mktemp("ce_pieces"), "cross_entropy",
-                 dict(kProductPairs=2, kCeLeastPiece=256, kCeCopyPiece=256, kCeGatherBlocks=3),
+                 dict(kProductPairs=2, kCeLeastPiece=256, kCeCopyPiece=256, kCeGatherBlocks=3, kCeChain=2),
                  [("1ull << 27", "1ull << 8")])
 
 
