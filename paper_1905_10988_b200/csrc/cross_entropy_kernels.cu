@@ -78,11 +78,13 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     const uint64_t first = (uint64_t)blockIdx.x * g.per_block;
     const uint64_t last = min(first + g.per_block, g.rows);
     uint32_t before = 0, all = 0, top = 0;
-#pragma unroll 4
+    // (every block begins at another place, or all of them ask the same parts of L2 at a time)
+#pragma unroll 8
     for (uint64_t i = threadIdx.x; i < g.rows; i += 256) {
-        const uint32_t counts = ce_target(g, i) >= 0;
+        const uint64_t at = i + first < g.rows ? i + first : i + first - g.rows;
+        const uint32_t counts = ce_target(g, at) >= 0;
         all += counts;
-        before += i < first ? counts : 0;
+        before += at < first ? counts : 0;
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {

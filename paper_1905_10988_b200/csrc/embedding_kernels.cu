@@ -6,14 +6,16 @@
 //
 // Backward, the tokens are sorted with their places, so that equal ones are neighbours in the order
 // of their places, and each row of the gradient is one sum in that order: no atomics, the same bits
-// from run to run.  Three kernels:
+// from run to run.  Rows that no token names are cleared by blocks of their own, each of which scans the
+// tokens for those of its rows, so that every row is written once.  Three kernels:
 //   - one cluster of up to eight blocks sorts (radix sort from the low digit, two digits up to a
-//     vocabulary of a million), while all other blocks clear the rows of the gradient that no token
-//     of the batch names: each scans the tokens for those of its own rows.  So the sort, which a few
-//     blocks do, costs nothing where the gradient is large, and every row is written once;
-//   - segments of the sorted tokens are added up, a thread eight columns; runs of equal tokens that end
-//     inside their segment are finished there, the others leave binary32 sums behind;
-//   - those are joined in order.
+//     vocabulary of a million), while all other blocks clear as many rows as that takes time for;
+//   - segments of the sorted tokens are added up, a thread eight columns; runs of equal tokens that are
+//     not cut between segments are finished there, the others leave binary32 sums behind; other blocks
+//     clear rows meanwhile;
+//   - those sums are joined in order, and the rest of the rows is cleared.
+// Up to 512 tokens there is one kernel: a block for each token, of which the first of equal ones finds
+// the others by a scan and adds them up.
 // What bounds it: HBM, by the gradient that is written and the rows that are read.
 #include "act8_common.cuh"
 #include "tensor_core.cuh"
@@ -31,6 +33,15 @@ constexpr int kClearBytes = 16384;       // of shared memory for the rows' flags
 constexpr int kSumThreads = 128;
 constexpr int kSumColumns = 8 * kSumThreads;
 constexpr int kMaxSegment = 32;          // sorted tokens of a block
+// Tokens that are not sorted at most.  Into 8192 x 768 binary32, 512 tokens take 9 us instead of 33; into
+// 65536 x 4096 bfloat16, 512 take 96 us and 1024 115, sorted 102.
+constexpr int kDirect = 512;
+constexpr int kDirectThreads = 512;
+// What is cleared beside the sort and the joins: so many bytes a microsecond of them.
+constexpr uint64_t kClearRate = 2000000;
+constexpr uint64_t kClearBlock = 96 << 10;    // bytes that a block clears beside the sums
+constexpr uint64_t kJoinTime = 0;        // us
+constexpr int kJoinShort = 12;           // cuts of a run that one warp joins
 
 struct EmbedTokens {
     const void* p;
@@ -47,29 +58,54 @@ struct EmbedTokens {
     }
 };
 
-// eight values of a row: neighbours from c on, or, spread, every 32nd from c on
+// eight values of a row, neighbours from c on or, spread, every 32nd from c on, as they lie in memory, and
+// to binary32
+template <typename T> struct EmbedRaw {
+    uint32_t w[2 * sizeof(T)];
+};
+
 template <typename T>
-__device__ __forceinline__ void embed_load8(const T* row, uint64_t c, uint64_t cols, bool vector,
-                                            float (&v)[8]) {
+__device__ __forceinline__ EmbedRaw<T> embed_load_raw(const T* row, uint64_t c, uint64_t cols, bool vector) {
+    EmbedRaw<T> r;
     if (vector && c + 8 <= cols) {
-        uint32_t w[2 * sizeof(T)];
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
             const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
-            w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
-        }
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) unpack2<T>(w[i], v[2 * i], v[2 * i + 1]);
+            r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
         }
     } else {
         const int step = vector ? 1 : 32;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i * step < cols ? to_f32<T>(row[c + i * step]) : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const bool in = c + i * step < cols;
+            if constexpr (sizeof(T) == 4) {
+                r.w[i] = in ? __ldg(reinterpret_cast<const uint32_t*>(row) + c + i * step) : 0u;
+            } else {
+                const uint32_t h =
+                    in ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + i * step) : 0u;
+                if (i & 1) r.w[i >> 1] |= h << 16; else r.w[i >> 1] = h;
+            }
+        }
     }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void embed_unpack(const EmbedRaw<T>& r, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2<T>(r.w[i], v[2 * i], v[2 * i + 1]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void embed_load8(const T* row, uint64_t c, uint64_t cols, bool vector,
+                                            float (&v)[8]) {
+    const EmbedRaw<T> r = embed_load_raw<T>(row, c, cols, vector);
+    embed_unpack<T>(r, v);
 }
 
 template <typename T>
@@ -141,97 +177,204 @@ embed_forward_kernel(const __grid_constant__ EmbedTokens tokens, const T* __rest
 
 // ---- backward: sorted tokens, and the rows without any ------------------------------------------
 
+struct EmbedClear {
+    EmbedTokens tokens;
+    char* dtable;
+    uint64_t row_bytes, row_distance;
+    uint64_t begin, end;                 // rows
+};
+
 struct EmbedSort {
     EmbedTokens tokens;
     int blocks;                          // of the cluster that sorts
     int passes, bits;                    // digits, and bits of one
-    uint32_t *keys[2], *places[2];       // the sorted ones end up in [0]
+    uint2* items[2];                     // key, place; the sorted ones end up in [0]
     uint32_t* counts;                    // [block][digits]
-    uint32_t* valid;                     // [block]: tokens of its part that are in the vocabulary
-    char* dtable;                        // rows without a token are cleared, nullptr: not
-    uint64_t row_bytes, row_distance;
-    bool vector;
+    uint32_t* valid;                     // tokens in the vocabulary: [block]: of its part, then all
+    EmbedClear clear;
 };
 
-// Clears rows that no token names.  A block takes every gridDim-th range of rows whose flags fit.
-__device__ __forceinline__ void embed_clear(const EmbedSort& s, uint32_t* flags, uint32_t block,
-                                            uint32_t blocks) {
-    const uint64_t v = s.tokens.vocabulary;
-    uint64_t range = (v + blocks - 1) / blocks;
-    if (range > 8 * kClearBytes) range = 8 * kClearBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (uint64_t first = block * range; first < v; first += blocks * range) {
-        const uint64_t rows = min(range, v - first);
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) flags[i] = 0;
-        __syncthreads();
-#pragma unroll 8
-        for (uint64_t i = threadIdx.x; i < s.tokens.count; i += kSortThreads) {
-            const uint64_t k = (uint64_t)s.tokens.key(i) - first;
-            if (k < rows) atomicOr(flags + (k >> 5), 1u << (k & 31));
-        }
-        __syncthreads();
-        for (uint64_t r = warp; r < rows; r += kSortWarps) {
-            if (flags[r >> 5] >> (r & 31) & 1) continue;
-            char* p = s.dtable + (first + r) * s.row_distance;
-            if (s.vector) {
-                const uint64_t n = s.row_bytes / 16;
+// zeros from p on, `bytes` of them (both even)
+__device__ __forceinline__ void embed_zero(char* p, uint64_t bytes, int lane) {
+    const uint64_t head = min((uint64_t)(-(uintptr_t)p & 15), bytes), n = (bytes - head) / 16;
+    if (2 * lane < head) reinterpret_cast<unsigned short*>(p)[lane] = 0;
+    uint4* q = reinterpret_cast<uint4*>(p + head);
 #pragma unroll 4
-                for (uint64_t i = lane; i < n; i += 32)
-                    reinterpret_cast<uint4*>(p)[i] = make_uint4(0u, 0u, 0u, 0u);
-                for (uint64_t i = 8 * n + lane; i < s.row_bytes / 2; i += 32)
-                    reinterpret_cast<unsigned short*>(p)[i] = 0;
-            } else {
-                for (uint64_t i = lane; i < s.row_bytes / 2; i += 32)
-                    reinterpret_cast<unsigned short*>(p)[i] = 0;
+    for (uint64_t i = lane; i < n; i += 32) q[i] = make_uint4(0u, 0u, 0u, 0u);
+    const uint64_t at = head + 16 * n + 2 * lane;
+    if (at < bytes) *reinterpret_cast<unsigned short*>(p + at) = 0;
+}
+
+// the first of n sorted items whose key is not below `key`: all threads of the block look at as many places at a
+// time
+__device__ __forceinline__ uint32_t embed_find(const uint2* items, uint32_t n, uint32_t key) {
+    uint32_t low = 0, high = n;          // it is in [low, high]
+    while (low < high) {
+        const uint32_t step = (high - low + blockDim.x - 1) / blockDim.x;
+        const uint64_t at = low + (uint64_t)threadIdx.x * step;
+        const int below = __syncthreads_count(at < high && __ldcg(&items[at].x) < key);
+        if (below == 0) return low;      // (those below are the first threads')
+        const uint64_t next = low + (uint64_t)below * step;
+        low = low + (below - 1) * step + 1;
+        high = (uint32_t)min(next, (uint64_t)high);
+    }
+    return low;
+}
+
+// Clears the rows from `begin` to `end` that no token names: block `block` of `blocks` takes every so
+// many-th range of rows, whose flags fit into its memory.  items: the n sorted ones, or nullptr where they
+// are not there yet and all tokens are looked at instead.
+__device__ __forceinline__ void embed_clear(const EmbedClear& s, uint32_t* flags, uint32_t block,
+                                            uint32_t blocks, const uint2* items, uint32_t n) {
+    if (s.begin >= s.end) return;
+    uint64_t range = (s.end - s.begin + blocks - 1) / blocks;
+    if (range > 8 * kClearBytes) range = 8 * kClearBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (uint64_t first = s.begin + block * range; first < s.end; first += blocks * range) {
+        const uint64_t rows = min(range, s.end - first);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) flags[i] = 0;
+        __syncthreads();
+        if (items) {
+            for (uint32_t i = embed_find(items, n, (uint32_t)first) + threadIdx.x; i < n; i += blockDim.x) {
+                const uint64_t k = (uint64_t)__ldcg(&items[i].x) - first;
+                if (k >= rows) break;
+                atomicOr(flags + (k >> 5), 1u << (k & 31));
+            }
+        } else {
+            // (every block begins at another place, or all of them ask the same parts of L2 at a time)
+            const uint64_t n = s.tokens.count, turn = n * block / blocks;
+#pragma unroll 8
+            for (uint64_t i = threadIdx.x; i < n; i += blockDim.x) {
+                const uint64_t at = i + turn < n ? i + turn : i + turn - n;
+                const uint64_t k = (uint64_t)s.tokens.key(at) - first;
+                if (k < rows) atomicOr(flags + (k >> 5), 1u << (k & 31));
             }
         }
+        __syncthreads();
+        for (uint64_t r = warp; r < rows; r += warps)
+            if (!(flags[r >> 5] >> (r & 31) & 1))
+                embed_zero(s.dtable + (first + r) * s.row_distance, s.row_bytes, lane);
     }
 }
 
+// One digit of a chunk of items: a warp's are neighbours, 32 for each round.  Afterwards rank[k] is that
+// of the thread's k-th item among its warp's with the same digit, ranks[warp][digit] how many the warps
+// before have, and the result, of thread `digit`, how many there are in the chunk.
+__device__ __forceinline__ uint32_t embed_rank(const EmbedSort& s, const uint2* items, int pass, int rounds,
+                                               uint64_t chunk, uint64_t last, uint16_t* ranks,
+                                               uint2 (&item)[kSortEach], uint32_t (&rank)[kSortEach]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, shift = pass * s.bits;
+    const uint32_t digits = 1u << s.bits, below = (1u << lane) - 1;
+    for (uint32_t i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads)
+        reinterpret_cast<uint32_t*>(ranks)[i] = 0;
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+        if (k >= rounds) break;
+        const uint64_t i = chunk + (warp * rounds + k) * 32 + lane;
+        item[k] = i >= last ? make_uint2(0xFFFFFFFFu, 0u)
+                  : pass    ? __ldcg(items + i)
+                            : make_uint2(s.tokens.key(i), (uint32_t)i);
+    }
+    __syncthreads();
+    uint16_t* mine = ranks + warp * digits;
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+        if (k >= rounds) break;
+        const bool in = chunk + (warp * rounds + k) * 32 + lane < last;
+        const uint32_t d = item[k].x >> shift & (digits - 1);
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, in ? d : digits);
+        const uint32_t old = in ? mine[d] : 0;
+        rank[k] = old + __popc(same & below);
+        __syncwarp();
+        if (in && (same & below) == 0) mine[d] = (uint16_t)(old + __popc(same));
+        __syncwarp();
+    }
+    __syncthreads();
+    uint32_t sum = 0;
+    if (threadIdx.x < digits) {
+#pragma unroll 8
+        for (int w = 0; w < kSortWarps; ++w) {
+            const uint32_t c = ranks[w * digits + threadIdx.x];
+            ranks[w * digits + threadIdx.x] = (uint16_t)sum;
+            sum += c;
+        }
+    }
+    return sum;
+}
+
 __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __grid_constant__ EmbedSort s) {
-    // of every warp, how many of its items have a digit; then where they go
-    extern __shared__ uint16_t ranks[];
+    extern __shared__ uint16_t ranks[];          // [warp][digit]
     __shared__ uint32_t base[1 << kSortMaxBits];
     __shared__ uint32_t sums[kSortWarps];
     after_previous();
     let_next_begin();
     if ((int)blockIdx.x >= s.blocks) {
-        embed_clear(s, reinterpret_cast<uint32_t*>(ranks), blockIdx.x - s.blocks,
-                    gridDim.x - s.blocks);
+        embed_clear(s.clear, reinterpret_cast<uint32_t*>(ranks), blockIdx.x - s.blocks,
+                    gridDim.x - s.blocks, nullptr, 0);
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t digits = 1u << s.bits, below = (1u << lane) - 1;
+    const uint32_t digits = 1u << s.bits;
     const uint64_t n = s.tokens.count;
     const uint64_t first = n * blockIdx.x / s.blocks, last = n * (blockIdx.x + 1) / s.blocks;
+    // of a warp in a chunk: 32 items each
+    const int rounds = (int)min((last - first + kSortThreads - 1) / kSortThreads, (uint64_t)kSortEach);
+    const bool single = last - first <= (uint64_t)kSortChunk;        // one chunk: read once a pass
+    uint2 item[kSortEach];
+    uint32_t rank[kSortEach];
     uint32_t valid = 0;
     for (int pass = 0; pass < s.passes; ++pass) {
         // from buffer (passes - pass) & 1 to the other one
-        const uint32_t* keys = s.keys[(s.passes - pass) & 1];
-        const uint32_t* places = s.places[(s.passes - pass) & 1];
-        uint32_t* keys_to = s.keys[(s.passes - pass - 1) & 1];
-        uint32_t* places_to = s.places[(s.passes - pass - 1) & 1];
+        const uint2* items = s.items[(s.passes - pass) & 1];
+        uint2* to = s.items[(s.passes - pass - 1) & 1];
         const int shift = pass * s.bits;
-        for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) base[d] = 0;
-        __syncthreads();
-        for (uint64_t i = first + threadIdx.x; i < last; i += kSortThreads) {
-            const uint32_t key = pass ? __ldcg(keys + i) : s.tokens.key(i);
-            if (pass == 0) valid += key < s.tokens.vocabulary;
-            atomicAdd(base + (key >> shift & (digits - 1)), 1u);
+        // how many items of the block have each digit, by thread
+        uint32_t mine = 0;
+        if (single) {
+            mine = embed_rank(s, items, pass, rounds, first, last, ranks, item, rank);
+            if (pass == 0)
+#pragma unroll
+                for (int k = 0; k < kSortEach; ++k)      // (none: a key beyond all)
+                    if (k < rounds) valid += item[k].x < s.tokens.vocabulary;
+        } else {
+            for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) base[d] = 0;
+            __syncthreads();
+            for (uint64_t i = first + threadIdx.x; i < last; i += kSortThreads) {
+                const uint32_t k = pass ? __ldcg(&items[i].x) : s.tokens.key(i);
+                if (pass == 0) valid += k < s.tokens.vocabulary;
+                atomicAdd(base + (k >> shift & (digits - 1)), 1u);
+            }
+            __syncthreads();
+            if (threadIdx.x < digits) mine = base[threadIdx.x];
         }
-        __syncthreads();
-        for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads)
-            s.counts[blockIdx.x * digits + d] = base[d];
+        if (threadIdx.x < digits) s.counts[blockIdx.x * digits + threadIdx.x] = mine;
+        if (pass == 0) {
+#pragma unroll
+            for (int d = 16; d; d >>= 1) valid += __shfl_xor_sync(0xFFFFFFFFu, valid, d);
+            if (lane == 0) sums[warp] = valid;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int w = 1; w < kSortWarps; ++w) valid += sums[w];
+                s.valid[blockIdx.x] = valid;
+            }
+        }
         cluster_sync();
-        // a thread a digit: the items of lower digits, and of this one in the blocks before
+        if (pass == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
+            valid = 0;
+            for (int b = 0; b < s.blocks; ++b) valid += __ldcg(s.valid + b);
+            s.valid[kSortMaxBlocks] = valid;
+        }
+        // the items of lower digits, and of this one in the blocks before
         uint32_t before = 0, all = 0;
-        if (threadIdx.x < digits)
-            for (int b = 0; b < s.blocks; ++b) {
-                const uint32_t c = __ldcg(s.counts + b * digits + threadIdx.x);
+        if (threadIdx.x < digits) {
+#pragma unroll
+            for (int b = 0; b < kSortMaxBlocks; ++b) {
+                const uint32_t c = b < s.blocks ? __ldcg(s.counts + b * digits + threadIdx.x) : 0;
                 before += b < (int)blockIdx.x ? c : 0;
                 all += c;
             }
+        }
         uint32_t up = all;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -240,75 +383,38 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
         }
         if (lane == 31) sums[warp] = up;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) before += sums[w];
-        __syncthreads();
-        if (threadIdx.x < digits) base[threadIdx.x] = before + up - all;
-        for (uint64_t chunk = first; chunk < last; chunk += kSortChunk) {
-            // a warp's items are 256 neighbours, 32 at a time
-            for (uint32_t i = threadIdx.x; i < kSortWarps * digits / 2; i += kSortThreads)
-                reinterpret_cast<uint32_t*>(ranks)[i] = 0;
-            __syncthreads();
-            uint32_t key[kSortEach], place[kSortEach], rank[kSortEach];
+        uint32_t lower = lane < warp ? sums[lane] : 0;
 #pragma unroll
-            for (int k = 0; k < kSortEach; ++k) {
-                const uint64_t i = chunk + (warp * kSortEach + k) * 32 + lane;
-                key[k] = i >= last ? 0xFFFFFFFFu : pass ? __ldcg(keys + i) : s.tokens.key(i);
-                place[k] = i >= last ? 0 : pass ? __ldcg(places + i) : (uint32_t)i;
-            }
-            uint16_t* mine = ranks + warp * digits;
-#pragma unroll
-            for (int k = 0; k < kSortEach; ++k) {
-                const uint64_t i = chunk + (warp * kSortEach + k) * 32 + lane;
-                const uint32_t d = key[k] >> shift & (digits - 1);
-                const uint32_t same = __match_any_sync(0xFFFFFFFFu, i >= last ? digits : d);
-                const uint32_t old = i >= last ? 0 : mine[d];
-                rank[k] = old + __popc(same & below);
-                __syncwarp();
-                if (i < last && (same & below) == 0) mine[d] = (uint16_t)(old + __popc(same));
-                __syncwarp();
-            }
-            __syncthreads();
-            if (threadIdx.x < digits) {
-                uint32_t sum = 0;
-                for (int w = 0; w < kSortWarps; ++w) {
-                    const uint32_t c = ranks[w * digits + threadIdx.x];
-                    ranks[w * digits + threadIdx.x] = (uint16_t)sum;
-                    sum += c;
-                }
-                before = sum;
+        for (int d = 16; d; d >>= 1) lower += __shfl_xor_sync(0xFFFFFFFFu, lower, d);
+        if (threadIdx.x < digits) base[threadIdx.x] = before + lower + up - all;
+        for (uint64_t chunk = first; chunk < last; chunk += rounds * kSortThreads) {
+            if (!single) {
+                __syncthreads();
+                mine = embed_rank(s, items, pass, rounds, chunk, last, ranks, item, rank);
             }
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kSortEach; ++k) {
-                const uint64_t i = chunk + (warp * kSortEach + k) * 32 + lane;
-                if (i < last) {
-                    const uint32_t d = key[k] >> shift & (digits - 1);
-                    const uint32_t to = base[d] + mine[d] + rank[k];
-                    keys_to[to] = key[k];
-                    places_to[to] = place[k];
+                if (k >= rounds) break;
+                if (chunk + (warp * rounds + k) * 32 + lane < last) {
+                    const uint32_t d = item[k].x >> shift & (digits - 1);
+                    to[base[d] + ranks[warp * digits + d] + rank[k]] = item[k];
                 }
             }
-            __syncthreads();
-            if (threadIdx.x < digits) base[threadIdx.x] += before;
-            __syncthreads();
+            if (!single) {
+                __syncthreads();
+                if (threadIdx.x < digits) base[threadIdx.x] += mine;
+            }
         }
         cluster_sync();
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) valid += __shfl_xor_sync(0xFFFFFFFFu, valid, d);
-    if (lane == 0) sums[warp] = valid;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kSortWarps; ++w) valid += sums[w];
-        s.valid[blockIdx.x] = valid;
     }
 }
 
 // ---- backward: sums --------------------------------------------------------------------------
 
 struct EmbedSum {
-    const uint32_t *keys, *places, *valid;
-    int blocks;                          // words of valid
+    const uint2* items;
+    const uint32_t* valid;
     uint32_t segment;                    // sorted tokens of one
     const void* dy;
     uint64_t cols, lddy;
@@ -319,56 +425,123 @@ struct EmbedSum {
     bool add;
     float* parts;                        // [segment][2][pitch]: of the run that began before the
     uint64_t pitch;                      // segment, of the one that goes on behind it
+    uint32_t segments;
+    uint32_t across;                     // threads that take eight columns each of a block's 1024
+    EmbedClear clear[2];                 // beside the sums, and beside the joins
 };
 
+// tokens in the vocabulary.  One thread of a block asks: asked by every warp of a few thousand blocks, the
+// one place in L2 that has it held the joins up by 10 us.
 __device__ __forceinline__ uint32_t embed_valid(const EmbedSum& s) {
-    uint32_t n = 0;
-    for (int b = 0; b < s.blocks; ++b) n += __ldcg(s.valid + b);
+    __shared__ uint32_t n;
+    if (threadIdx.x == 0) n = __ldcg(s.valid);
+    __syncthreads();
     return n;
 }
 
-template <typename T, typename O>
+// Segment g has the sorted tokens from about g * segment on.  A run of equal ones across that place is
+// left to the segment before, where it ends within `segment` tokens; longer ones are cut there.
+__device__ __forceinline__ bool embed_cut(const EmbedSum& s, uint32_t g, uint32_t n) {
+    const uint64_t p = (uint64_t)g * s.segment;
+    if (g == 0 || p + s.segment >= n) return false;
+    const uint32_t a = __ldcg(&s.items[p - 1].x), b = __ldcg(&s.items[p].x),
+                   c = __ldcg(&s.items[p + s.segment].x);
+    return (a == b) & (b == c);          // (three loads at a time)
+}
+
+// Blocks that clear lie evenly between those that work: `number` of this one among its kind
+__device__ __forceinline__ bool embed_clears(uint32_t works, uint32_t& number) {
+    const uint32_t clears = gridDim.x - works;
+    const uint32_t before = (uint32_t)((uint64_t)blockIdx.x * clears / gridDim.x);
+    const bool clear = (uint64_t)(blockIdx.x + 1) * clears / gridDim.x > before;
+    number = clear ? before : blockIdx.x - before;
+    return clear;
+}
+
+template <typename T, typename O, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_constant__ EmbedSum s) {
-    __shared__ uint32_t keys[kMaxSegment + 2], places[kMaxSegment];
+    // of a block's groups of threads, each with a segment of its own: key and place of up to twice as many
+    // tokens, and the keys of the ones before and behind
+    __shared__ uint32_t keys[4][2 * kMaxSegment + 2], places[4][2 * kMaxSegment];
+    __shared__ uint32_t flags[kClearBytes / 4];
     after_previous();
     let_next_begin();
-    const uint32_t n = embed_valid(s), first = blockIdx.x * s.segment;
-    if (first >= n) return;
-    const uint32_t count = min(s.segment, n - first);
-    // keys[i + 1] is that of the i-th token; before and behind: of the neighbours, or no token's
-    for (uint32_t i = threadIdx.x; i < count + 2; i += kSumThreads)
-        keys[i] = first + i == 0 || first + i > n ? 0xFFFFFFFFu : __ldcg(s.keys + first + i - 1);
-    for (uint32_t i = threadIdx.x; i < count; i += kSumThreads) places[i] = __ldcg(s.places + first + i);
+    const uint32_t n = embed_valid(s), groups = kSumThreads / s.across;
+    uint32_t number;
+    const uint32_t works = (s.segments + groups - 1) / groups;
+    if (embed_clears(works, number)) {
+        embed_clear(s.clear[0], flags, number * gridDim.y + blockIdx.y,
+                    (gridDim.x - works) * gridDim.y, s.items, n);
+        return;
+    }
+    const uint32_t group = threadIdx.x / s.across, x = threadIdx.x - group * s.across;
+    const uint32_t g = number * groups + group, first = g * s.segment;
+    const bool any = group < groups && g < s.segments && first < n;
+    uint32_t* key = keys[group & 3];
+    uint32_t* place = places[group & 3];
+    if (any)
+        for (uint32_t i = x; i < 2 * s.segment + 2; i += s.across) {
+            const uint32_t at = first + i - 1;           // key[i] is that of token `at`
+            const bool in = first + i > 0 && at < n;
+            const uint2 item = in ? __ldcg(s.items + at) : make_uint2(0xFFFFFFFFu, 0u);
+            key[i] = item.x;
+            if (i > 0 && i <= 2 * s.segment) place[i - 1] = item.y;
+        }
     __syncthreads();
+    if (!any) return;
+    // from `at` tokens on, the first that begins a run, within a segment's length, or else `at`
+    const auto border = [&](uint32_t at) {
+        if (first + at >= n || first + at == 0) return min(at, n - first);
+        for (uint32_t i = 0; i <= s.segment; ++i)
+            if (key[at + i] != key[at + i + 1]) return at + i;
+        return at;
+    };
+    const uint32_t begin = border(0), end = border(s.segment);
+    if (begin >= end) return;
     const uint64_t c = (uint64_t)blockIdx.y * kSumColumns +
-                       (s.vector ? 8 * threadIdx.x : 256 * (threadIdx.x >> 5) + (threadIdx.x & 31));
+                       (s.vector ? 8 * x : 256 * (x >> 5) + (x & 31));
     if (c >= s.cols) return;
     const T* dy = static_cast<const T*>(s.dy);
     float sum[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
-    bool began = keys[1] != keys[0];     // the run began in this segment
-    for (uint32_t i = 0; i < count; i += 4) {
-        float v[4][8];                   // four rows in flight
+    bool began = key[begin] != key[begin + 1];           // the run began in this segment
+    // rows at a time: as many as leave room for other blocks
+    constexpr int kFlight = 16 / sizeof(T) / (ADD ? 2 : 1);
+    for (uint32_t i = begin; i < end; i += kFlight) {
+        EmbedRaw<T> raw[kFlight];
+        EmbedRaw<O> old[ADD ? kFlight : 1];              // the rows that the sums are added to
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (i + j < count)
-                embed_load8<T>(dy + (uint64_t)places[i + j] * s.lddy, c, s.cols, s.vector, v[j]);
+        for (int j = 0; j < kFlight; ++j)
+            if (i + j < end) {
+                raw[j] = embed_load_raw<T>(dy + (uint64_t)place[i + j] * s.lddy, c, s.cols, s.vector);
+                if (ADD && key[i + j + 1] != key[i + j + 2])
+                    old[j] = embed_load_raw<O>(
+                        static_cast<const O*>(s.dtable) + (uint64_t)key[i + j + 1] * s.ldt, c, s.cols,
+                        s.vector);
+            }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (i + j >= count) break;
+        for (int j = 0; j < kFlight; ++j) {
+            if (i + j >= end) break;
+            float v[8];
+            embed_unpack<T>(raw[j], v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += v[j][k];
-            const bool ends = keys[i + j + 1] != keys[i + j + 2];
-            if (!ends && i + j + 1 < count) continue;
+            for (int k = 0; k < 8; ++k) sum[k] += v[k];
+            const bool ends = key[i + j + 1] != key[i + j + 2];
+            if (!ends && i + j + 1 < end) continue;
             if (began && ends) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum[k] *= s.scale;
-                embed_store8<O>(static_cast<O*>(s.dtable) + (uint64_t)keys[i + j + 1] * s.ldt, c, s.cols,
-                                s.vector, s.add, sum);
+                if (ADD) {
+                    embed_unpack<O>(old[j], v);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[k] += v[k];
+                }
+                embed_store8<O>(static_cast<O*>(s.dtable) + (uint64_t)key[i + j + 1] * s.ldt, c, s.cols,
+                                s.vector, false, sum);
             } else {
-                embed_store8<float>(s.parts + (2ull * blockIdx.x + (began ? 1 : 0)) * s.pitch, c, s.cols,
-                                    s.vector, false, sum);
+                embed_store8<float>(s.parts + (2ull * g + (began ? 1 : 0)) * s.pitch, c, s.cols, s.vector,
+                                    false, sum);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
@@ -377,93 +550,236 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     }
 }
 
-// The runs that go on behind their segment: a block takes 256 columns and every gridDim-th group of 32
-// segments; eight warps add up the parts of a run in turns, and their sums are added in order.
+// The runs that were cut.  A block takes 256 columns and eight segments; a warp joins the run whose first
+// cut is at the beginning of its segment, in the order of the segments.  Runs with more than 12 cuts are
+// left to all eight warps, which take a run's parts in turns and add up their sums in order.
 template <typename O>
 __global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedSum s) {
     __shared__ float sums[8][256];
-    __shared__ uint32_t ends[8];
+    __shared__ uint32_t ends[8];         // of each of those runs: the segment after its last cut
+    __shared__ uint32_t flags[kClearBytes / 4];
     after_previous();
     let_next_begin();
-    const uint32_t n = embed_valid(s), segments = (n + s.segment - 1) / s.segment;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t n = embed_valid(s), segments = (n + s.segment - 1) / s.segment;
+    uint32_t number;
+    const uint32_t works = (s.segments + 7) / 8;
+    if (embed_clears(works, number)) {
+        embed_clear(s.clear[1], flags, number * gridDim.y + blockIdx.y,
+                    (gridDim.x - works) * gridDim.y, s.items, n);
+        return;
+    }
     const uint64_t c = (uint64_t)blockIdx.y * 256 + 8 * lane;
-    for (uint32_t group = blockIdx.x * 32; group < segments; group += gridDim.x * 32) {
-        // (every warp finds out for itself which of the 32 a run begins in that goes on)
-        const uint32_t g = group + lane, end = (g + 1) * s.segment;
-        bool open = false;
-        if (end < n) {
-            const uint32_t k = __ldcg(s.keys + end - 1);
-            open = k == __ldcg(s.keys + end) &&
-                   (g == 0 || __ldcg(s.keys + g * s.segment - 1) != k);
+    const uint32_t group = number * 8;
+    if (group >= segments) return;
+    // (every warp finds out for itself which of the eight a run is cut at for the first time)
+    const uint32_t g = group + (lane & 7);
+    const bool cut = embed_cut(s, g, n), before = embed_cut(s, g ? g - 1 : 0, n);
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, cut && !before) & 0xFFu;
+    if (!mask) return;
+    if (mask >> warp & 1) {
+        const uint32_t from = group + warp;
+        uint32_t to = segments;          // the segment behind the last cut is the first that is not cut
+        for (uint32_t at = from + 1; at < segments && to == segments; at += 32) {
+            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, !embed_cut(s, at + lane, n));
+            if (hit) to = min(at + __ffs(hit) - 1, segments);
         }
-        uint32_t mask = __ballot_sync(0xFFFFFFFFu, open);
-        while (mask) {
-            const uint32_t from = group + __ffs(mask) - 1;
-            mask &= mask - 1;
-            const uint32_t k = __ldcg(s.keys + (from + 1) * s.segment - 1);
-            // the segment that the run ends in
-            uint32_t to = segments;
-            for (uint32_t at = from + 1; at < segments && to == segments; at += 256) {
-                const uint32_t i = at + threadIdx.x;
-                const bool over = i < segments &&
-                                  ((i + 1) * (uint64_t)s.segment >= n ||
-                                   __ldcg(s.keys + (i + 1) * s.segment) != k);
-                const uint32_t hit = __ballot_sync(0xFFFFFFFFu, over);
-                __syncthreads();
-                if (lane == 0) ends[warp] = hit ? at + 32 * warp + __ffs(hit) - 1 : segments;
-                __syncthreads();
-                for (int w = 7; w >= 0; --w)
-                    if (ends[w] < segments) to = ends[w];
-            }
+        if (lane == 0) ends[warp] = to;
+        if (to - from <= kJoinShort && c < s.cols) {
+            const uint32_t k = __ldcg(&s.items[(uint64_t)from * s.segment].x);
             float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-            if (c < s.cols) {
+            const float4* p = reinterpret_cast<const float4*>(s.parts + (2ull * from - 1) * s.pitch + c);
+            *reinterpret_cast<float4*>(v) = __ldcg(p);
+            *reinterpret_cast<float4*>(v + 4) = __ldcg(p + 1);
 #pragma unroll 4
-                for (uint32_t i = from + warp; i <= to; i += 8) {
-                    const float* p = s.parts + (2ull * i + (i == from ? 1 : 0)) * s.pitch + c;
-                    const float4 a = __ldcg(reinterpret_cast<const float4*>(p));
-                    const float4 b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
-                    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-                    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-                }
+            for (uint32_t i = from; i < to; ++i) {
+                const float4* q = reinterpret_cast<const float4*>(s.parts + 2ull * i * s.pitch + c);
+                const float4 a = __ldcg(q), b = __ldcg(q + 1);
+                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+                v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
             }
-            __syncthreads();
+            // (values of neighbouring columns, also where rows are at any element)
+            O* row = static_cast<O*>(s.dtable) + (uint64_t)k * s.ldt;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[warp][8 * lane + i] = v[i];
-            __syncthreads();
-            const uint64_t col = (uint64_t)blockIdx.y * 256 + threadIdx.x;
-            if (col < s.cols) {
-                float all = sums[0][threadIdx.x];
+            for (int i = 0; i < 8; ++i) v[i] *= s.scale;
+            if (s.vector) {
+                embed_store8<O>(row, c, s.cols, true, s.add, v);
+            } else {
 #pragma unroll
-                for (int w = 1; w < 8; ++w) all += sums[w][threadIdx.x];
-                all *= s.scale;
-                O* p = static_cast<O*>(s.dtable) + (uint64_t)k * s.ldt + col;
-                *p = from_f32<O>(s.add ? to_f32<O>(*p) + all : all);
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < s.cols)
+                        row[c + i] = from_f32<O>(s.add ? to_f32<O>(row[c + i]) + v[i] : v[i]);
             }
         }
+    }
+    __syncthreads();
+    for (uint32_t m = mask; m; m &= m - 1) {
+        const uint32_t which = __ffs(m) - 1, from = group + which, to = ends[which];
+        if (to - from <= kJoinShort) continue;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (c < s.cols) {
+            // (the part before the first cut is the second one of the segment before)
+#pragma unroll 4
+            for (uint32_t i = from + warp; i <= to; i += 8) {
+                const float* p = s.parts + (i == from ? 2ull * from - 1 : 2ull * (i - 1)) * s.pitch + c;
+                const float4 a = __ldcg(reinterpret_cast<const float4*>(p));
+                const float4 b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+                v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[warp][8 * lane + i] = v[i];
+        __syncthreads();
+        const uint64_t col = (uint64_t)blockIdx.y * 256 + threadIdx.x;
+        if (col < s.cols) {
+            float all = sums[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) all += sums[w][threadIdx.x];
+            all *= s.scale;
+            const uint32_t k = __ldcg(&s.items[(uint64_t)from * s.segment].x);
+            O* p = static_cast<O*>(s.dtable) + (uint64_t)k * s.ldt + col;
+            *p = from_f32<O>(s.add ? to_f32<O>(*p) + all : all);
+        }
+    }
+}
+
+// ---- backward: few tokens ----------------------------------------------------------------------
+
+struct EmbedDirect {
+    EmbedTokens tokens;
+    const void* dy;
+    uint64_t cols, lddy;
+    bool vector;
+    float scale;
+    void* dtable;
+    uint64_t ldt;
+    bool add;
+    uint32_t across;                     // threads that take eight columns each of a block's 1024
+    EmbedClear clear;
+};
+
+// Blocks of the first tokens.count: the token of the block's number, if it is the first of its kind.
+// Threads beyond `across` take other rows of the sum in turns.
+template <typename T, typename O>
+__global__ void __launch_bounds__(kDirectThreads) embed_direct_kernel(const __grid_constant__ EmbedDirect s) {
+    __shared__ uint32_t flags[kClearBytes / 4];
+    __shared__ uint32_t counts[kDirectThreads / 32];
+    after_previous();
+    let_next_begin();
+    const uint32_t n = (uint32_t)s.tokens.count;
+    if (blockIdx.x >= n) {
+        embed_clear(s.clear, flags, (blockIdx.x - n) * gridDim.y + blockIdx.y,
+                    (gridDim.x - n) * gridDim.y, nullptr, 0);
+        return;
+    }
+    // places of the tokens like this one, in order, and the sums of the rows' groups in passing
+    static_assert(kDirect + 8 * kSumThreads <= kClearBytes / 4, "");
+    uint32_t* places = flags;
+    float* sums = reinterpret_cast<float*>(flags + kDirect);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t mine = s.tokens.key(blockIdx.x);
+    if (mine >= s.tokens.vocabulary) return;
+    uint32_t found[kDirect / kDirectThreads];
+    bool before = false;
+#pragma unroll
+    for (int k = 0; k < kDirect / kDirectThreads; ++k) {
+        const uint32_t i = k * kDirectThreads + threadIdx.x;
+        const bool same = i < n && s.tokens.key(i) == mine;
+        before |= same && i < blockIdx.x;
+        found[k] = __ballot_sync(0xFFFFFFFFu, same);
+    }
+    if (__syncthreads_or(before)) return;
+    uint32_t count = 0;
+#pragma unroll
+    for (int k = 0; k < kDirect / kDirectThreads; ++k) {
+        __syncthreads();
+        if (lane == 0) counts[warp] = __popc(found[k]);
+        __syncthreads();
+        uint32_t at = count;
+        for (int w = 0; w < kDirectThreads / 32; ++w) {
+            if (w < warp) at += counts[w];
+            count += counts[w];
+        }
+        if (found[k] >> lane & 1)
+            places[at + __popc(found[k] & ((1u << lane) - 1))] = k * kDirectThreads + threadIdx.x;
+    }
+    __syncthreads();
+    const uint32_t groups = kDirectThreads / s.across, group = threadIdx.x / s.across;
+    const uint32_t x = threadIdx.x - group * s.across;
+    const uint64_t base = (uint64_t)blockIdx.y * kSumColumns;
+    const uint64_t c = base + (s.vector ? 8 * x : 256 * (x >> 5) + (x & 31));
+    const T* dy = static_cast<const T*>(s.dy);
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+    if (group < groups && c < s.cols) {
+        for (uint32_t i = group; i < count; i += 4 * groups) {
+            EmbedRaw<T> raw[4];          // four rows in flight
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j * groups < count)
+                    raw[j] = embed_load_raw<T>(dy + (uint64_t)places[i + j * groups] * s.lddy, c, s.cols,
+                                               s.vector);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i + j * groups >= count) break;
+                float v[8];
+                embed_unpack<T>(raw[j], v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] += v[k];
+            }
+        }
+    }
+    // the groups' sums in order (none but the first has any where there are fewer rows)
+    const uint32_t used = min(groups, count);
+    for (uint32_t g = 1; g < used; ++g) {
+        __syncthreads();
+        if (group == g)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sums[k * s.across + x] = sum[k];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += sums[k * s.across + x];
+    }
+    if (group == 0 && c < s.cols) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] *= s.scale;
+        embed_store8<O>(static_cast<O*>(s.dtable) + (uint64_t)mine * s.ldt, c, s.cols, s.vector, s.add,
+                        sum);
     }
 }
 
 struct EmbedPlan {
     int sorters, passes, bits;
-    uint32_t segment, segments;
+    uint32_t segment, segments, across;
     uint64_t pitch;
-    size_t keys[2], places[2], counts, valid, parts, bytes;
+    size_t items[2], counts, valid, parts, bytes;
 };
+
+// threads that share a slab of columns: whole warps, because spread columns need them
+static uint32_t embed_across(uint64_t cols) {
+    const uint64_t eights = (cols + 7) / 8;
+    return eights >= kSumThreads ? kSumThreads : (uint32_t)(eights + 31) / 32 * 32;
+}
 
 static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
     EmbedPlan p = {};
     p.sorters = 1;
-    while (p.sorters < kSortMaxBlocks && (uint64_t)p.sorters * kSortChunk < rows) p.sorters *= 2;
+    while (p.sorters < kSortMaxBlocks && (uint64_t)p.sorters * 2 * kSortThreads <= rows) p.sorters *= 2;
     int bits = 1;                        // of the keys 0 .. vocabulary
     while (vocabulary >> bits) ++bits;
     p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
     p.bits = (bits + p.passes - 1) / p.passes;
     const uint64_t slabs = (cols + kSumColumns - 1) / kSumColumns;
+    p.across = embed_across(cols);
+    const uint64_t groups = kSumThreads / p.across;
     p.segment = kMaxSegment;             // shorter ones where the chip would stand idle
-    while (p.segment > 8 && (rows + p.segment - 1) / p.segment * slabs < 8 * 148) p.segment /= 2;
+    while (p.segment > 8 && (rows / p.segment + 1) * slabs / groups < 8 * 148) p.segment /= 2;
     p.segments = (uint32_t)((rows + p.segment - 1) / p.segment);
     p.pitch = (cols + 7) / 8 * 8;
     size_t at = 0;
@@ -472,12 +788,9 @@ static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
         at = (at + bytes + 255) & ~(size_t)255;
         return here;
     };
-    for (int i = 0; i < 2; ++i) {
-        p.keys[i] = place(4 * rows);
-        p.places[i] = place(4 * rows);
-    }
+    for (int i = 0; i < 2; ++i) p.items[i] = place(8 * rows);
     p.counts = place((size_t)4 * kSortMaxBlocks << kSortMaxBits);
-    p.valid = place(4 * kSortMaxBlocks);
+    p.valid = place(4 * (kSortMaxBlocks + 1));
     p.parts = place(8 * (size_t)p.segments * p.pitch);
     p.bytes = at;
     return p;
@@ -486,10 +799,30 @@ static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
 template <typename T, typename O>
 static void embed_sums(const EmbedSum& s, uint32_t segments, cudaStream_t stream) {
     const unsigned slabs = (unsigned)((s.cols + kSumColumns - 1) / kSumColumns);
-    launch_overlapping(embed_sum_kernel<T, O>, dim3(segments, slabs), dim3(kSumThreads), 0, stream, s);
-    const uint32_t groups = (segments + 31) / 32;
-    launch_overlapping(embed_join_kernel<O>, dim3(groups, (unsigned)((s.cols + 255) / 256)), dim3(256),
-                       0, stream, s);
+    const unsigned columns = (unsigned)((s.cols + 255) / 256);
+    // blocks that clear take about as long as those that add up
+    const uint32_t groups = kSumThreads / s.across;
+    const auto clears = [](const EmbedClear& c, unsigned down) {
+        if (c.begin >= c.end) return 0u;
+        const uint64_t n = (c.end - c.begin) * c.row_bytes / kClearBlock / down + 1;
+        return (unsigned)(n < 65536 ? n : 65536);
+    };
+    const unsigned first = clears(s.clear[0], slabs), second = clears(s.clear[1], columns);
+    launch_overlapping(s.add ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>,
+                       dim3((segments + groups - 1) / groups + first, slabs), dim3(kSumThreads), 0, stream,
+                       s);
+    launch_overlapping(embed_join_kernel<O>, dim3((segments + 7) / 8 + second, columns), dim3(256), 0,
+                       stream, s);
+}
+
+template <typename T, typename O>
+static void embed_direct(const EmbedDirect& s, cudaStream_t stream) {
+    const unsigned slabs = (unsigned)((s.cols + kSumColumns - 1) / kSumColumns);
+    const unsigned clear = s.clear.begin < s.clear.end ? (4 * 148 + slabs - 1) / slabs : 0;
+    const unsigned blocks = (unsigned)s.tokens.count + clear;
+    if (blocks)
+        launch_overlapping(embed_direct_kernel<T, O>, dim3(blocks, slabs), dim3(kDirectThreads), 0,
+                           stream, s);
 }
 
 template <typename T, typename O>
@@ -568,23 +901,39 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     const EmbedPlan p = embed_plan(rows, vocabulary, cols);
     if (workspace_bytes < p.bytes) return NC_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
-    EmbedSort s = {};
-    s.tokens = {tokens, token_bytes, rows, vocabulary};
-    s.blocks = p.sorters; s.passes = rows ? p.passes : 0; s.bits = p.bits;
-    for (int i = 0; i < 2; ++i) {
-        s.keys[i] = reinterpret_cast<uint32_t*>(ws + p.keys[i]);
-        s.places[i] = reinterpret_cast<uint32_t*>(ws + p.places[i]);
+    const bool vector = row_access(dtable, lddt, tb, vocabulary) != kRowElement &&
+                        row_access(dy, lddy, yb, rows) != kRowElement;
+    EmbedClear clear = {};
+    clear.tokens = {tokens, token_bytes, rows, vocabulary};
+    clear.dtable = static_cast<char*>(dtable);
+    clear.row_bytes = cols * tb; clear.row_distance = lddt * tb;
+    clear.end = accumulate ? 0 : vocabulary;
+    if (rows <= kDirect) {
+        EmbedDirect d = {};
+        d.tokens = clear.tokens; d.dy = dy; d.cols = cols; d.lddy = lddy; d.vector = vector;
+        d.scale = scale; d.dtable = dtable; d.ldt = lddt; d.add = accumulate != 0; d.clear = clear;
+        d.across = p.across;
+        NC_EMBED_TYPES(dtype, dtable_dtype, embed_direct, d, stream);
+        return launch_status();
     }
+    EmbedSort s = {};
+    s.tokens = clear.tokens;
+    s.blocks = p.sorters; s.passes = p.passes; s.bits = p.bits;
+    for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint2*>(ws + p.items[i]);
     s.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
     s.valid = reinterpret_cast<uint32_t*>(ws + p.valid);
-    if (!accumulate) s.dtable = static_cast<char*>(dtable);
-    s.row_bytes = cols * tb; s.row_distance = lddt * tb;
-    s.vector = row_access(dtable, lddt, tb, vocabulary) != kRowElement;
+    // as many rows as are cleared while the sort runs (8 us a digit and 2 for every 1024 tokens of a
+    // block), and while the joins do, which leave the memory idle as well
+    s.clear = clear;
+    const uint64_t sort_us = p.passes * (8 + 2 * (rows / (p.sorters * (uint64_t)kSortThreads)));
+    const uint64_t beside = sort_us * kClearRate / clear.row_bytes;
+    const uint64_t later = kJoinTime * kClearRate / clear.row_bytes;
+    if (beside < clear.end) s.clear.end = beside;
     // one block on every SM, in whole clusters; no others than the sorting ones where nothing is cleared
-    const int sms = device_sm_count(), clusters = s.dtable ? sms / p.sorters : 1;
-    const int grid = (clusters < 2 ? (s.dtable ? 2 : 1) : clusters) * p.sorters;
-    const int flags = kSortWarps * 2 << p.bits;
-    const int smem = flags > kClearBytes ? flags : kClearBytes;
+    const int clusters = s.clear.end ? device_sm_count() / p.sorters : 1;
+    const int grid = (s.clear.end && clusters < 2 ? 2 : clusters) * p.sorters;
+    const int ranks = kSortWarps * 2 << p.bits;
+    const int smem = ranks > kClearBytes ? ranks : kClearBytes;
     static bool allowed[64];
     if (!allow_dynamic_smem((const void*)embed_sort_kernel, kSortWarps * 2 << kSortMaxBits, allowed))
         return NC_ERR_CUDA;
@@ -602,13 +951,15 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     cudaLaunchKernelEx(&cfg, embed_sort_kernel, s);
-    if (rows == 0) return launch_status();
     EmbedSum e = {};
-    e.keys = s.keys[0]; e.places = s.places[0]; e.valid = s.valid; e.blocks = p.sorters;
-    e.segment = p.segment; e.dy = dy; e.cols = cols; e.lddy = lddy;
-    e.vector = row_access(dy, lddy, yb, rows) != kRowElement && s.vector;
-    e.scale = scale; e.dtable = dtable; e.ldt = lddt; e.add = accumulate != 0;
+    e.items = s.items[0]; e.valid = s.valid + kSortMaxBlocks; e.across = p.across;
+    e.segment = p.segment; e.segments = p.segments; e.dy = dy; e.cols = cols; e.lddy = lddy;
+    e.vector = vector; e.scale = scale; e.dtable = dtable; e.ldt = lddt; e.add = accumulate != 0;
     e.parts = reinterpret_cast<float*>(ws + p.parts); e.pitch = p.pitch;
+    e.clear[0] = e.clear[1] = clear;
+    e.clear[0].begin = s.clear.end;
+    e.clear[1].begin = clear.end > s.clear.end + later ? clear.end - later : s.clear.end;
+    e.clear[0].end = e.clear[1].begin;
     NC_EMBED_TYPES(dtype, dtable_dtype, embed_sums, e, p.segments, stream);
     return launch_status();
 }

@@ -16,6 +16,28 @@ inline uint32_t __match_any_sync(uint32_t, uint32_t v) {
     for (int i = 0; i < 32; ++i) mask |= (uint32_t)(s[i] == v) << i;
     return mask;
 }
+inline int __syncthreads_or(int p) {
+    static int any;                      // (blocks of a cluster come here one by one)
+    __syncthreads();
+    any = 0;
+    __syncthreads();
+    any |= p;
+    __syncthreads();
+    const int r = any;
+    __syncthreads();
+    return r;
+}
+inline int __syncthreads_count(int p) {
+    static int sum;
+    __syncthreads();
+    sum = 0;
+    __syncthreads();
+    sum += p != 0;
+    __syncthreads();
+    const int r = sum;
+    __syncthreads();
+    return r;
+}
 inline uint32_t atomicAdd(uint32_t* p, uint32_t v) {
     const uint32_t old = *p;
     *p += v;

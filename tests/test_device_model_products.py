@@ -147,3 +147,21 @@ EMBEDDING = [(1, 1, 1, "f32", "f32", "whole", "one", 8, 0), (0, 7, 9, "bf16", "f
 @pytest.mark.parametrize("case", EMBEDDING, ids=["-".join(map(str, c)) for c in EMBEDDING])
 def test_embedding(embedding, case):
     run(embedding, *case, 1)
+
+
+@pytest.fixture(scope="module")
+def sorted_embedding(tmp_path_factory):
+    # clears some of the rows beside the sort and some later, and
+    # takes runs of more than three segments for long ones
+    return build(tmp_path_factory.mktemp("embed_sorted"), "embedding",
+                 dict(kJoinShort=3, kClearRate=2000))
+
+
+SORTED = [(600, 50, 20, "f16", "f16", "whole", "few", 8, 0), (900, 1200, 9, "f32", "bf16", "any", "one", 4, 0),
+          (700, 3000, 12, "bf16", "f32", "whole", "many", 8, 0), (520, 40, 1100, "bf16", "f32", "any", "few", 8, 1),
+          (513, 20, 12, "f16", "f32", "whole", "none", 8, 0), (4500, 300, 3, "f32", "f32", "any", "many", 8, 1)]
+
+
+@pytest.mark.parametrize("case", SORTED, ids=["-".join(map(str, c)) for c in SORTED])
+def test_embedding_sorted(sorted_embedding, case):
+    run(sorted_embedding, *case, 1)
