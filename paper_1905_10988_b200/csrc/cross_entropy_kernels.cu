@@ -223,11 +223,12 @@ template <bool CHAINS> struct CeLogits {
     bool bf16;
     CeRows rows;
     uint32_t columns, tiles_n;           // of the piece
+    uint32_t split;                      // pieces that every tile comes in
     uint32_t first;                      // its first vocabulary entry
     uint32_t steps, parts_of;            // parts_of: chains of a sum
     float unit;                          // scale * log2 e
     float scale;
-    float2* parts;                       // [tile of the vocabulary][pitch of the rows]: maximum, sum
+    float2* parts;                       // [piece of the vocabulary][pitch of the rows]: maximum, sum
     uint64_t part_pitch;
     uint32_t count;
 
@@ -237,12 +238,15 @@ template <bool CHAINS> struct CeLogits {
     };
     __device__ __forceinline__ uint32_t begin(bool) {
         count = __ldcg(rows.count);
-        return (count + kProductTile - 1) / kProductTile * tiles_n;
+        return (count + kProductTile - 1) / kProductTile * tiles_n * split;
     }
     __device__ __forceinline__ uint32_t chains() const { return CHAINS ? parts_of : 1; }
+    __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t chain) const {
         ProductUnit w = {};
-        product_tile(u, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        product_tile(u / split, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        w.width = kProductTile / (int)split;
+        w.n += (int)(u % split) * w.width;
         w.steps = (int)steps;
         if (CHAINS) {
             const uint32_t from = steps * chain / parts_of;
@@ -256,6 +260,7 @@ template <bool CHAINS> struct CeLogits {
         if (CHAINS && w.part + 1 < parts_of) {
 #pragma unroll
             for (int c = 0; c < kProductHalf; c += kColumns) {
+                if (c >= r.columns) break;
                 uint32_t v[kColumns];
                 r.load(c, v);
 #pragma unroll
@@ -267,11 +272,11 @@ template <bool CHAINS> struct CeLogits {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint32_t target = row < count ? __ldcg(rows.target + row) : kCeNone;
         const uint32_t at = target - first - col;            // of the target among these columns
-        const bool near = target != kCeNone && target >= first + col && at < (uint32_t)kProductHalf;
+        const bool near = target != kCeNone && target >= first + col && at < (uint32_t)r.columns;
         float top = __uint_as_float(0xFF800000u), sum = 0.0f;
 #pragma unroll (CHAINS ? kProductHalf / kColumns : 1)
         for (int c = 0; c < kProductHalf; c += kColumns) {
-            if (col + c >= columns) break;
+            if (c >= r.columns || col + c >= columns) break;
             uint32_t v[kColumns];
             r.load(c, v);
             if (CHAINS) {
@@ -292,7 +297,7 @@ template <bool CHAINS> struct CeLogits {
             const float next = fmaxf(top, o.x), from = next == lowest ? 0.0f : next;
             sum = sum * exp2_approx((top - from) * unit) + o.y * exp2_approx((o.x - from) * unit);
             if (row < count)
-                parts[(uint64_t)((first + (uint32_t)w.n) / kProductTile) * part_pitch + row] =
+                parts[(uint64_t)((first + (uint32_t)w.n) / (uint32_t)w.width) * part_pitch + row] =
                     make_float2(next, sum);
         }
         product_pair_barrier(r);
@@ -393,6 +398,7 @@ template <typename T> struct CeDz {
     uint64_t pitch;
     int blocks;                          // of the gathering kernel
     uint32_t count;
+    ProductSplit split;
     float inverse;
 
     __device__ __forceinline__ uint32_t begin(bool reads_out) {
@@ -405,13 +411,19 @@ template <typename T> struct CeDz {
             if (blockIdx.x == 0 && threadIdx.x == 0) rows.count[1] = top;
             inverse = ce_headroom<T>() / ce_largest(top);
         }
-        return (count + kProductTile - 1) / kProductTile * tiles_n;
+        const uint32_t tiles = (count + kProductTile - 1) / kProductTile * tiles_n;
+        split = product_split(tiles);
+        return split.units(tiles);
     }
     typedef ProductNothing State;
     __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
-        product_tile(u, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        int column;
+        const uint32_t t = split.tile(u, column, w.width);
+        product_tile(t, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        w.n += column;
         w.steps = (int)steps;
         return w;
     }
@@ -426,10 +438,10 @@ template <typename T> struct CeDz {
         const uint32_t keep = counts ? 0xFFFFFFFFu : 0u;
         const uint32_t at = target - first - col;            // of the target among these columns
         const bool near = counts && target != kCeNone && target >= first + col &&
-                          at < (uint32_t)kProductHalf;
+                          at < (uint32_t)r.columns;
         T* to = dz + (uint64_t)row * pitch + col;
 #pragma unroll 1
-        for (int c = 0; c < kProductHalf; c += 32) {
+        for (int c = 0; c < r.columns; c += 32) {
             uint32_t v[32];
             r.load(c, v);
 #pragma unroll
@@ -452,8 +464,8 @@ template <typename T> struct CeDz {
 };
 
 // what the products over dz are multiplied by
-__device__ __forceinline__ float ce_factor(const CeRows& rows, float scale, bool bf16) {
-    return ce_largest(__ldcg(rows.count + 1)) * (bf16 ? scale : scale * (1.0f / 16384.0f));
+__device__ __forceinline__ float ce_factor(uint32_t largest, float scale, bool bf16) {
+    return ce_largest(largest) * (bf16 ? scale : scale * (1.0f / 16384.0f));
 }
 
 struct CeDx {
@@ -470,19 +482,26 @@ struct CeDx {
     uint64_t lddx;
     ProductTarget target;
     uint32_t count;
+    ProductSplit split;
     float factor;
 
     __device__ __forceinline__ uint32_t begin(bool reads_out) {
         count = __ldcg(rows.count);
-        factor = reads_out ? ce_factor(rows, scale, bf16) : 0.0f;
-        return (count + kProductTile - 1) / kProductTile * tiles_n * splits;
+        factor = reads_out ? ce_factor(__ldcg(rows.count + 1), scale, bf16) : 0.0f;
+        const uint32_t tiles = (count + kProductTile - 1) / kProductTile * tiles_n * splits;
+        split = product_split(tiles);
+        return split.units(tiles);
     }
     typedef ProductNothing State;
     __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
-        w.part = u % splits;
-        product_tile(u / splits, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        int column;
+        const uint32_t t = split.tile(u, column, w.width);
+        w.part = t % splits;
+        product_tile(t / splits, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
+        w.n += column;
         const uint32_t from = (uint32_t)((uint64_t)steps * w.part / splits);
         w.k = (int)from * kProductStep;
         w.steps = (int)((uint32_t)((uint64_t)steps * (w.part + 1) / splits) - from);
@@ -495,7 +514,7 @@ struct CeDx {
         if (ends && splits == 1 && row < count)
             to = static_cast<char*>(dx) + 2 * ((uint64_t)__ldcg(rows.origin + row) * lddx + col);
 #pragma unroll 1
-        for (int c = 0; c < kProductHalf && col + c < width; c += 32) {
+        for (int c = 0; c < r.columns && col + c < width; c += 32) {
             uint32_t v[32];
             r.load(c, v);
             if (!begins) {
@@ -534,8 +553,11 @@ ce_join_dx_kernel(const CeRows rows, const float* __restrict__ sums, const uint6
                   T* __restrict__ dx, const uint64_t lddx, const uint32_t width) {
     after_previous();
     let_next_begin();
-    const uint32_t count = __ldcg(rows.count);
-    const float factor = ce_factor(rows, scale, bf16);
+    __shared__ uint32_t word[2];         // (one thread asks for the block)
+    if (threadIdx.x < 2) word[threadIdx.x] = __ldcg(rows.count + threadIdx.x);
+    __syncthreads();
+    const uint32_t count = word[0];
+    const float factor = ce_factor(word[1], scale, bf16);
     const uint32_t col = blockIdx.x * 256 + threadIdx.x;
     if (col >= width) return;
     for (uint32_t row = blockIdx.y; row < count; row += gridDim.y) {
@@ -558,18 +580,23 @@ struct CeDtable {
     uint64_t ldt;
     ProductTarget target;
     uint32_t count;
+    ProductSplit split;
     float factor;
 
     __device__ __forceinline__ uint32_t begin(bool reads_out) {
         count = __ldcg(rows.count);
-        factor = reads_out ? ce_factor(rows, scale, bf16) : 0.0f;
-        return tiles_m * tiles_n;
+        factor = reads_out ? ce_factor(__ldcg(rows.count + 1), scale, bf16) : 0.0f;
+        split = product_split(tiles_m * tiles_n);
+        return split.units(tiles_m * tiles_n);
     }
     typedef ProductNothing State;
     __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
-        product_tile(u, tiles_m, tiles_n, w.m, w.n);
+        int column;
+        product_tile(split.tile(u, column, w.width), tiles_m, tiles_n, w.m, w.n);
+        w.n += column;
         w.steps = (int)((count + kProductStep - 1) / kProductStep);
         return w;
     }
@@ -578,7 +605,7 @@ struct CeDtable {
         void* to = row < entries ? product_at(dtable, target.dtype, (uint64_t)row * ldt + col) : nullptr;
         const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
 #pragma unroll 1
-        for (int c = 0; c < kProductHalf && col + c < width; c += 32) {
+        for (int c = 0; c < r.columns && col + c < width; c += 32) {
             uint32_t v[32];
             r.load(c, v);
             float o[32];
@@ -596,6 +623,7 @@ struct CeDtable {
 struct CePlan {
     uint64_t rows_pitch, pitch, vocabulary_pitch, piece;
     uint32_t splits;                     // of dx
+    uint32_t pieces;                     // that every tile of the forward pass comes in
     int blocks;
     uint32_t per_block;
     size_t count, origin, target, lse, dloss, both, hit, most, x, copy, parts, dz, sums, bytes;
@@ -626,9 +654,9 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
         if (p.piece < kCeLeastPiece) p.piece = kCeLeastPiece;
     }
     if (p.piece > p.vocabulary_pitch) p.piece = p.vocabulary_pitch;
-    // (at least 16 rows a block: with fewer the counting outweighs the copies)
+    // (a row for every warp at least: with fewer the counting outweighs the copies)
     p.per_block = (uint32_t)((rows + kCeGatherBlocks - 1) / kCeGatherBlocks);
-    if (p.per_block < 16) p.per_block = 16;
+    if (p.per_block < 8) p.per_block = 8;
     p.blocks = (int)((rows + p.per_block - 1) / p.per_block);
     // fewer tiles of dx than pairs: the sum over the vocabulary is split, eight steps a part at least
     const uint64_t tiles = p.rows_pitch / kProductTile * ((width + kProductTile - 1) / kProductTile);
@@ -652,7 +680,10 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
             p.sums = ce_place(at, 4 * p.splits * p.rows_pitch * ((width + 31) / 32 * 32));
     } else {
         p.hit = ce_place(at, 4 * p.rows_pitch);
-        p.parts = ce_place(at, 8 * p.rows_pitch * (p.vocabulary_pitch / 256));
+        // (a few tiles in pieces: the rule is that of product_split, but for all of them)
+        const uint64_t all = p.rows_pitch / 256 * (p.vocabulary_pitch / 256);
+        p.pieces = all < kProductPairs ? product_split((uint32_t)all).parts : 1;
+        p.parts = ce_place(at, 8 * p.rows_pitch * (p.vocabulary_pitch / 256 * p.pieces));
     }
     p.bytes = at;
     return p;
@@ -718,7 +749,7 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
         a.tiles_n = (uint32_t)(dz_pitch / 256); a.first = (uint32_t)first;
         a.steps = (uint32_t)((width + kProductStep - 1) / kProductStep);
         a.unit = scale * kLog2E; a.dz = dz; a.pitch = dz_pitch; a.blocks = p.blocks;
-        nc_status st = product_launch(a, tiles_t * a.tiles_n, stream);
+        nc_status st = product_launch(a, 4 * tiles_t * a.tiles_n, stream);
         if (st != NC_OK) return st;
         if (dx) {
             CeDx b = {};
@@ -730,7 +761,7 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
             b.split_distance = p.rows_pitch * sums_pitch; b.dx = dx; b.lddx = lddx;
             b.target.dtype = bf16 ? NC_DTYPE_BF16 : NC_DTYPE_F16;
             b.target.access = row_access(dx, lddx, 2, most_rows);
-            st = product_launch(b, tiles_t * tiles_n * p.splits, stream);
+            st = product_launch(b, 4 * tiles_t * tiles_n * p.splits, stream);
             if (st != NC_OK) return st;
         }
         if (dtable) {
@@ -742,7 +773,7 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
             c.dtable = static_cast<char*>(dtable) + first * lddt * bytes; c.ldt = lddt;
             c.target.dtype = dtable_dtype; c.target.add = accumulate;
             c.target.access = row_access(dtable, lddt, bytes, vocabulary);
-            st = product_launch(c, (uint64_t)c.tiles_m * tiles_n, stream);
+            st = product_launch(c, 4 * (uint64_t)c.tiles_m * tiles_n, stream);
             if (st != NC_OK) return st;
         }
     }
@@ -832,7 +863,8 @@ nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows,
             a.first = (uint32_t)first; a.steps = steps; a.parts_of = (steps + kCeChain - 1) / kCeChain;
             a.unit = scale * kLog2E; a.scale = scale;
             a.parts = reinterpret_cast<float2*>(ws + p.parts); a.part_pitch = p.rows_pitch;
-            return product_launch(a, p.rows_pitch / 256 * a.tiles_n, stream);
+            a.split = p.pieces;
+            return product_launch(a, p.rows_pitch / 256 * a.tiles_n * a.split, stream);
         };
         const nc_status st = steps > kCeChain ? launch(CeLogits<true>{}) : launch(CeLogits<false>{});
         if (st != NC_OK) return st;
@@ -840,7 +872,7 @@ nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows,
     const uint64_t blocks = (rows + 31) / 32;
     launch_overlapping(ce_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0,
                        stream, to, reinterpret_cast<const float2*>(ws + p.parts), p.rows_pitch,
-                       (uint32_t)(p.vocabulary_pitch / 256), scale, loss, lse);
+                       (uint32_t)((vocabulary + 256 / p.pieces - 1) / (256 / p.pieces)), scale, loss, lse);
     return launch_status();
 }
 

@@ -27,7 +27,7 @@ namespace natcomp {
 
 constexpr float kOrthoGramScale = 256.0f;
 constexpr float kOrthoLow = 2048.0f;                 // of the second of X's two values
-constexpr int kOrthoNormBlocks = 128;                // per matrix at most
+constexpr int kOrthoNormBlocks = 592;                // per matrix at most
 
 // ---- the norm, and the first X ---------------------------------------------------------------
 
@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__
     const T* g = static_cast<const T*>(in.g) + blockIdx.y * in.distance;
     const uint64_t across = (in.cols + 7) / 8, all = in.rows * across;
     double s = 0.0;
+#pragma unroll 4
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)in.blocks * 256) {
         const uint64_t r = i / across;
         float v[8];
@@ -99,11 +100,18 @@ template <typename T>
 __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant__ OrthoInput in) {
     after_previous();
     let_next_begin();
-    double sum = 0.0;
-    for (int i = threadIdx.x & 31; i < in.blocks; i += 32)
-        sum += __ldcg(in.parts + (uint64_t)blockIdx.y * in.blocks + i);
+    __shared__ double sums;
+    if (threadIdx.x < 32) {
+        double s = 0.0;
+#pragma unroll 8
+        for (int i = threadIdx.x; i < in.blocks; i += 32)
+            s += __ldcg(in.parts + (uint64_t)blockIdx.y * in.blocks + i);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        if (threadIdx.x == 0) sums = s;
+    }
+    __syncthreads();
+    const double sum = sums;
     const double by = sum == 0.0 ? 0.0 : in.scale / (sqrt(sum) + in.eps);
     const bool narrow = by > 1e-37 && by < 1e37;
     const float by32 = (float)by;
@@ -149,8 +157,7 @@ __device__ __forceinline__ ProductUnit ortho_upper(uint32_t u, uint32_t side) {
 }
 
 // 16 values of a row of binary16 as they lie in a workspace
-__device__ __forceinline__ void ortho_load16(const __half* p, float (&v)[16]) {
-    const Bytes32 raw = ld_wide(p);
+__device__ __forceinline__ void ortho_unpack16(const Bytes32& raw, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) unpack2<__half>(raw.v[i], v[2 * i], v[2 * i + 1]);
 }
@@ -167,32 +174,53 @@ template <bool POLYNOMIAL> struct OrthoSquare {
     ProductSide left_side, right_side;
     bool bf16;
     uint32_t side, tiles, batch, steps;
+    ProductSplit split;
     uint64_t pitch;
     const __half* gram;                  // POLYNOMIAL
     __half* out;
     float* diagonal;                     // POLYNOMIAL: [matrix][pitch]; out has 0 there
     float b, c;                          // c: of the product; b: of A
 
-    __device__ __forceinline__ uint32_t begin(bool) { return tiles * (tiles + 1) / 2 * batch; }
-    typedef ProductNothing State;
+    struct State {
+        Bytes32 old[2];                  // 32 values of A, a chunk ahead
+    };
     __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ uint32_t begin(bool) {
+        return split.units(tiles * (tiles + 1) / 2 * batch);
+    }
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
-        ProductUnit w = ortho_upper(u, tiles);
+        int column, width;
+        ProductUnit w = ortho_upper(split.tile(u, column, width), tiles);
+        w.n += column;
+        w.width = width;
         w.steps = (int)steps;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
+    __device__ __forceinline__ void load(const ProductUnit& w, const ProductRead& r, int k, State& s) const {
+        const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column) + k;
+        if (!POLYNOMIAL || row >= side || k >= r.columns) return;
+        const __half* p = gram + ((uint64_t)w.z * side + row) * pitch + col;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (col + 16 * h < side) s.old[h] = ld_wide(p + 16 * h);
+    }
+    __device__ __forceinline__ void ahead(const ProductUnit& w, const ProductRead& r, State& s) const {
+        load(w, r, 0, s);
+    }
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint64_t at = ((uint64_t)w.z * side + row) * pitch + col;
 #pragma unroll 1
-        for (int k = 0; k < kProductHalf && col + k < side; k += 32) {
+        for (int k = 0; k < r.columns && col + k < side; k += 32) {
+            const State now = s;
+            load(w, r, k + 32, s);
             uint32_t v[32];
             r.load(k, v);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (row >= side || col + k + 16 * h >= side) continue;
                 float o[16], old[16];
-                if (POLYNOMIAL) ortho_load16(gram + at + k + 16 * h, old);
+                if (POLYNOMIAL) ortho_unpack16(now.old[h], old);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     o[i] = c * __uint_as_float(v[16 * h + i]);
@@ -217,6 +245,7 @@ struct OrthoStep {
     ProductSide left_side, right_side;
     bool bf16;
     uint32_t rows, cols, tiles_m, tiles_n, batch, steps;
+    ProductSplit split;
     uint64_t pitch;
     float a;
     const float* diagonal;               // of the polynomial: by rows, or, tall, by columns
@@ -229,18 +258,41 @@ struct OrthoStep {
     float scale;
     ProductTarget target;
 
-    __device__ __forceinline__ uint32_t begin(bool) { return tiles_m * tiles_n * batch; }
-    typedef ProductNothing State;
+    struct State {
+        Bytes32 high[2], low[2];         // 32 values of X, a chunk ahead
+        float of_column;                 // the lane's diagonal value, tall
+    };
     __device__ __forceinline__ uint32_t chains() const { return 1; }
+    __device__ __forceinline__ uint32_t begin(bool) { return split.units(tiles_m * tiles_n * batch); }
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         ProductUnit w = {};
-        const uint32_t each = tiles_m * tiles_n, z = u / each;
-        product_tile(u - z * each, tiles_m, tiles_n, w.m, w.n);
+        int column;
+        const uint32_t t = split.tile(u, column, w.width);
+        const uint32_t each = tiles_m * tiles_n, z = t / each;
+        product_tile(t - z * each, tiles_m, tiles_n, w.m, w.n);
+        w.n += column;
         w.z = (int)z;
         w.steps = (int)steps;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
+    __device__ __forceinline__ void load(const ProductUnit& w, const ProductRead& r, int k, State& s) const {
+        const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column) + k;
+        if (k >= r.columns) return;
+        if (steps && tall && col + r.lane < cols)
+            s.of_column = __ldcg(diagonal + w.z * diagonal_pitch + col + r.lane);
+        if (row >= rows) return;
+        const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (col + 16 * h < cols) {
+                s.high[h] = ld_wide(high + at + 16 * h);
+                s.low[h] = ld_wide(low + at + 16 * h);
+            }
+    }
+    __device__ __forceinline__ void ahead(const ProductUnit& w, const ProductRead& r, State& s) const {
+        load(w, r, 0, s);
+    }
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
         const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
@@ -250,7 +302,14 @@ struct OrthoStep {
         const float* d = diagonal + w.z * diagonal_pitch;
         const float of_row = steps && !tall && row < rows ? __ldcg(d + row) : 0.0f;
 #pragma unroll 1
-        for (int k = 0; k < kProductHalf && col + k < cols; k += 32) {
+        for (int k = 0; k < r.columns && col + k < cols; k += 32) {
+            const State now = s;
+            load(w, r, k + 32, s);
+            if (steps && tall) {         // the diagonal of the columns, a lane's each, for all lanes
+                __syncwarp();
+                r.rows[r.lane] = now.of_column;
+                __syncwarp();
+            }
             uint32_t v[32];
             r.load(k, v);
             float o[32];
@@ -262,14 +321,10 @@ struct OrthoStep {
                     continue;
                 }
                 float x[16], y[16], f[16];
-                ortho_load16(high + at + k + 16 * h, x);
-                ortho_load16(low + at + k + 16 * h, y);
+                ortho_unpack16(now.high[h], x);
+                ortho_unpack16(now.low[h], y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float4 q = make_float4(of_row, of_row, of_row, of_row);
-                    if (steps && tall) q = __ldcg(reinterpret_cast<const float4*>(d + col + k + 16 * h) + i);
-                    f[4 * i] = q.x; f[4 * i + 1] = q.y; f[4 * i + 2] = q.z; f[4 * i + 3] = q.w;
-                }
+                for (int i = 0; i < 16; ++i) f[i] = steps && tall ? r.rows[16 * h + i] : of_row;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float all = fmaf(y[i], 1.0f / kOrthoLow, x[i]);
@@ -430,16 +485,18 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     }
     const uint64_t upper = (uint64_t)tiles * (tiles + 1) / 2 * batch;
     const uint64_t whole = (uint64_t)t.tiles_m * t.tiles_n * batch;
+    s.split = q.split = product_split((uint32_t)upper);
+    t.split = product_split((uint32_t)whole);
     const int rounds = steps ? steps : 1;
     for (int i = 0; i < rounds; ++i) {
         nc_status st = NC_OK;
         if (steps) {
             s.left = s.right = x_map[i & 1];
-            st = product_launch(s, upper, stream);
+            st = product_launch(s, s.split.units((uint32_t)upper), stream);
             if (st != NC_OK) return st;
             q.b = coefficients[3 * i + 1];
             q.c = coefficients[3 * i + 2] / kOrthoGramScale;
-            st = product_launch(q, upper, stream);
+            st = product_launch(q, q.split.units((uint32_t)upper), stream);
             if (st != NC_OK) return st;
         }
         t.left = tall ? x_map[i & 1] : poly_map;
@@ -448,7 +505,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
         t.steps = steps ? q.steps : 0;   // no steps: the normalised matrix
         t.high = high[i & 1]; t.next = high[(i + 1) & 1];
         t.out = i + 1 == rounds ? out : nullptr;
-        st = product_launch(t, whole, stream);
+        st = product_launch(t, t.split.units((uint32_t)whole), stream);
         if (st != NC_OK) return st;
     }
     return launch_status();

@@ -8,7 +8,8 @@
 // which the matrix instruction takes as it is, so nothing is ever transposed.
 //
 // A pair of blocks (cta_group::2) computes tiles of 256 x 256 one after another, block r of it the
-// rows from 128 r on; it brings 128 rows of either operand for every step of 64 k.  One thread of each
+// rows from 128 r on; it brings 128 rows of either operand for every step of 64 k.  Tiles that do not fill
+// a round of the chip's pairs are cut along n into two or four (product_split).  One thread of each
 // block copies boxes of 64 x 64 into a ring of six stages of 32 KB, one thread of the pair's first
 // block issues the matrix instructions, and eight warps read the finished tile out of TMEM, which
 // holds two, while the next one is computed.  Both blocks' copies are counted by the first block's
@@ -146,8 +147,37 @@ inline bool make_box_map(CUtensorMap* map, const void* p, bool bf16, uint64_t co
 struct ProductUnit {
     int m, n, z;                         // z: which of several matrices
     int k, steps;                        // from k on, in steps of 64
+    int width;                           // n values: 256, 128 or 64
     uint32_t part;                       // of the job's own
 };
+
+// Tiles from `whole` on come in `parts` pieces of 256 / parts columns each.  A round of tiles that leaves
+// half of the pairs idle takes half the time in halves, although the left operand is read once more:
+// 4096 x 4096 x 4096, 256 tiles for 74 pairs, XXX.
+struct ProductSplit {
+    uint32_t whole, parts;
+    __host__ __device__ __forceinline__ uint32_t units(uint32_t tiles) const {
+        return whole + (tiles - whole) * parts;
+    }
+    // the tile of unit u; its first column in the tile and their number
+    __device__ __forceinline__ uint32_t tile(uint32_t u, int& column, int& width) const {
+        column = 0;
+        width = kProductTile;
+        if (u < whole) return u;
+        const uint32_t t = (u - whole) / parts;
+        width = kProductTile / (int)parts;
+        column = (int)(u - whole - t * parts) * width;
+        return whole + t;
+    }
+};
+
+__host__ __device__ __forceinline__ ProductSplit product_split(uint32_t tiles) {
+    const uint32_t rest = tiles % kProductPairs;
+    ProductSplit s = {tiles - rest, 1};
+    if (rest * 4 <= kProductPairs) s.parts = 4;
+    else if (rest * 2 <= kProductPairs) s.parts = 2;
+    return s;
+}
 
 struct ProductSide {
     bool lines;                          // k runs over the lines of memory
@@ -169,10 +199,10 @@ __device__ __forceinline__ void product_next(const Job& job, uint32_t& u, uint32
 
 struct ProductNothing {};
 
-// what a thread that reads a tile out has: one row, 128 of the columns
+// what a thread that reads a tile out has: one row, half of the columns
 struct ProductRead {
     uint32_t tmem;                       // of the warp's lanes and of its first column
-    int row, column;                     // in the tile: of the thread, of its first value
+    int row, column, columns;            // in the unit: of the thread, of its first value; their number
     int lane, quarter, half;             // quarter: of the block's rows, half: of the columns
     bool ok, nothing;                    // !ok: a wait ran out, no result;  nothing: no steps
     float* rows;                         // the warp's own 32 x 33 words of shared memory
@@ -296,6 +326,8 @@ __device__ __forceinline__ void* product_at(void* p, int dtype, uint64_t i) {
 //   uint32_t chains() const           parts that the sum of a unit is read out in, one after the other
 //   ProductUnit unit_of(uint32_t u, uint32_t chain) const
 //   struct State                      what a thread keeps from one chain to the next
+//   void ahead(const ProductUnit&, const ProductRead&, State&)      loads that store() needs, while the
+//                                     product is computed
 //   void store(const ProductUnit&, const ProductRead&, State&)      all 256 threads that read tiles out
 //
 // A wait that runs out leaves NaN: the first block's issuing thread tells both blocks before it lets
@@ -346,7 +378,6 @@ product_kernel(const __grid_constant__ Job given) {
         r.quarter = warp & 3;
         r.half = warp >> 2;
         r.row = (int)rank * kProductHalf + 32 * r.quarter + lane;
-        r.column = 128 * r.half;
         r.rows = reinterpret_cast<float*>(base + kProductBars + 256) + warp * (kProductRows / 4);
         r.exchange =
             reinterpret_cast<float*>(base + kProductBars + 256) + r.quarter * (kProductRows / 4);
@@ -355,6 +386,9 @@ product_kernel(const __grid_constant__ Job given) {
         for (uint32_t u = pair, chain = 0; u < units; product_next(job, u, chain, pairs), ++turn) {
             const ProductUnit w = job.unit_of(u, chain);
             const uint32_t b = turn & 1;
+            r.columns = w.width / 2;
+            r.column = r.columns * r.half;
+            job.ahead(w, r, state);
             const bool ok = mbar_wait(full + 8 * b, (turn >> 1) & 1, gave_up);
             r.ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
             r.nothing = w.steps == 0;
@@ -372,19 +406,21 @@ product_kernel(const __grid_constant__ Job given) {
             bool ok = true;
             for (uint32_t u = pair, chain = 0; u < units && ok; product_next(job, u, chain, pairs)) {
                 const ProductUnit w = job.unit_of(u, chain);
-                const int m = w.m + (int)rank * kProductHalf, n = w.n + (int)rank * kProductHalf;
+                const int m = w.m + (int)rank * kProductHalf, n = w.n + (int)rank * (w.width / 2);
+                const bool second = w.width == kProductTile;     // a second box of the right operand
                 for (int s = 0; s < w.steps; ++s, ++step) {
                     if (step >= kProductStages) ok = mbar_wait(empty + 8 * stage, parity ^ 1, gave_up);
                     if (!ok) break;
                     const int k = w.k + s * kProductStep;
                     const uint32_t bar = filled + 8 * stage, to = stages + stage * kProductStage;
-                    if (rank == 0) mbar_expect(bar, 2 * kProductStage);
+                    if (rank == 0) mbar_expect(bar, 2 * (kProductStage - (second ? 0 : kProductBox)));
                     const bool a = job.left_side.by_lines(m, k), b = job.right_side.by_lines(n, k);
                     for (int h = 0; h < 2; ++h) {
                         tma_load_pair(to + h * kProductBox, &given.left, a ? m + 64 * h : k,
                                       a ? k : m + 64 * h, w.z, bar);
-                        tma_load_pair(to + kProductOperand + h * kProductBox, &given.right,
-                                      b ? n + 64 * h : k, b ? k : n + 64 * h, w.z, bar);
+                        if (h == 0 || second)
+                            tma_load_pair(to + kProductOperand + h * kProductBox, &given.right,
+                                          b ? n + 64 * h : k, b ? k : n + 64 * h, w.z, bar);
                     }
                     stage = stage + 1 == kProductStages ? 0 : stage + 1;
                     parity ^= stage == 0;
@@ -402,13 +438,13 @@ product_kernel(const __grid_constant__ Job given) {
         // ---- matrix instructions: the whole warp, of which one thread issues
         const bool elected = elect_one();
         const uint64_t operand = mma_operand(stages, kProductBox);     // + bytes / 16: further on
-        const uint32_t plain = mma_shape_of(kProductTile, kProductTile, job.bf16, false, false);
         bool ok = true;
         uint32_t stage = 0, parity = 0, turn = 0;
         for (uint32_t u = pair, chain = 0; u < units && ok;
              product_next(job, u, chain, pairs), ++turn) {
             const ProductUnit w = job.unit_of(u, chain);
             const uint32_t b = turn & 1, to = tmem + b * kProductTile;
+            const uint32_t plain = mma_shape_of(kProductTile, w.width, job.bf16, false, false);
             ok = mbar_wait(drained + 8 * b, ((turn >> 1) & 1) ^ 1, gave_up);
             for (int s = 0; s < w.steps; ++s) {
                 if (ok) ok = mbar_wait(filled + 8 * stage, parity, gave_up);

@@ -98,7 +98,7 @@ inline void st_wide(void* p, const Bytes32& r) {
 }
 
 inline constexpr uint32_t mma_shape_of(uint32_t m, uint32_t n, bool bf16, bool a_lines, bool b_lines) {
-    return (uint32_t)bf16 | (uint32_t)a_lines << 15 | (uint32_t)b_lines << 16 | m << 17 | n << 24 << 1;
+    return (uint32_t)bf16 | (n >> 6) << 1 | (uint32_t)a_lines << 15 | (uint32_t)b_lines << 16 | (m >> 8) << 17;
 }
 
 inline float model_value_of(uint16_t h, bool bf16) {
@@ -108,11 +108,12 @@ inline float model_value_of(uint16_t h, bool bf16) {
     return __half2float(v);
 }
 
-// 256 x 256 x 16 of a pair: block r holds rows and columns from 128 r on.  An operand's address is that of
+// 256 x n x 16 of a pair: block r holds the rows from 128 r on and the columns from n / 2 r on.  An operand's address is that of
 // its first value of the 16 k: by lines, panels of 64 values and a line for each k; else rows of 128 bytes
 inline void product_mma(uint32_t to, uint64_t a, uint64_t b, uint32_t shape, bool add, bool elected) {
     if (!elected) return;
-    if (to % 256 || to >= 512) model::fail("matrix instruction");
+    const int n = (int)(shape >> 1 & 7) * 64;
+    if (to % 256 || to >= 512 || (n != 256 && n != 128 && n != 64)) model::fail("matrix instruction");
     model::W.tensor.push_back([=] {
         static float left[256][16], right[16][256];
         const bool bf16 = shape & 1;
@@ -129,13 +130,13 @@ inline void product_mma(uint32_t to, uint64_t a, uint64_t b, uint32_t shape, boo
             for (int k = 0; k < 16; ++k)
                 for (int i = 0; i < 128; ++i) {
                     left[128 * r + i][k] = read(a, shape >> 15 & 1, r, k, i);
-                    right[k][128 * r + i] = read(b, shape >> 16 & 1, r, k, i);
+                    if (i < n / 2) right[k][n / 2 * r + i] = read(b, shape >> 16 & 1, r, k, i);
                 }
         for (int m = 0; m < 256; ++m) {
             float* d = &model::W.tmem[(m / 128 * 128 + m % 128) * 512 + to];
-            if (!add) memset(d, 0, 256 * 4);
+            if (!add) memset(d, 0, n * 4);
             for (int k = 0; k < 16; ++k)
-                for (int n = 0; n < 256; ++n) d[n] += left[m][k] * right[k][n];
+                for (int c = 0; c < n; ++c) d[c] += left[m][k] * right[k][c];
         }
     });
 }

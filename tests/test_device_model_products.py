@@ -67,7 +67,7 @@ def cross_entropy(tmp_path_factory):
 @pytest.fixture(scope="module")
 def small_pieces(tmp_path_factory):
     return build(tmp_path_factory.mktemp("ce_pieces"), "cross_entropy",
-                 dict(kProductPairs=2, kCeLeastPiece=256, kCeCopyPiece=256, kCeGatherBlocks=3, kCeChain=2),
+                 dict(kProductPairs=4, kCeLeastPiece=256, kCeCopyPiece=256, kCeGatherBlocks=3, kCeChain=2),
                  [("1ull << 27", "1ull << 8")])
 
 
@@ -105,7 +105,7 @@ def test_cross_entropy_wait_that_runs_out_leaves_nan(cross_entropy, rank, nth):
 
 @pytest.fixture(scope="module")
 def orthogonalize(tmp_path_factory):
-    return build(tmp_path_factory.mktemp("ortho"), "orthogonalize", dict(kProductPairs=2))
+    return build(tmp_path_factory.mktemp("ortho"), "orthogonalize", dict(kProductPairs=4))
 
 
 ORTHOGONALIZE = [(1, 1, 1, "f32", "f32", "whole", 2), (2, 40, 24, "bf16", "f16", "any", 2),
