@@ -217,10 +217,8 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
 // that of 1024.
 constexpr uint32_t kCeChain = 16;                    // steps
 
-template <bool CHAINS> struct CeLogits {
-    CUtensorMap left, right;             // gathered rows, piece of the table
-    ProductSide left_side, right_side;
-    bool bf16;
+template <bool CHAINS> struct CeLogits : ProductOnce {
+    // left, right: gathered rows, piece of the table
     CeRows rows;
     uint32_t columns, tiles_n;           // of the piece
     uint32_t split;                      // pieces that every tile comes in
@@ -236,7 +234,7 @@ template <bool CHAINS> struct CeLogits {
     struct State {
         float sums[CHAINS ? kProductHalf : 1];
     };
-    __device__ __forceinline__ uint32_t begin(bool) {
+    __device__ __forceinline__ uint32_t begin(uint32_t, bool) {
         count = __ldcg(rows.count);
         return (count + kProductTile - 1) / kProductTile * tiles_n * split;
     }
@@ -387,10 +385,8 @@ template <typename T> __device__ __forceinline__ constexpr float ce_headroom() {
     return sizeof(T) && std::is_same<T, __half>::value ? 16384.0f : 1.0f;
 }
 
-template <typename T> struct CeDz {
-    CUtensorMap left, right;             // gathered rows, piece of the table
-    ProductSide left_side, right_side;
-    bool bf16;
+template <typename T> struct CeDz : ProductOnce {
+    // left, right: gathered rows, piece of the table
     CeRows rows;
     uint32_t tiles_n, first, steps;
     float unit;
@@ -401,7 +397,7 @@ template <typename T> struct CeDz {
     ProductSplit split;
     float inverse;
 
-    __device__ __forceinline__ uint32_t begin(bool reads_out) {
+    __device__ __forceinline__ uint32_t begin(uint32_t, bool reads_out) {
         count = __ldcg(rows.count);
         if (reads_out) {
             uint32_t top = 0;
@@ -468,10 +464,8 @@ __device__ __forceinline__ float ce_factor(uint32_t largest, float scale, bool b
     return ce_largest(largest) * (bf16 ? scale : scale * (1.0f / 16384.0f));
 }
 
-struct CeDx {
-    CUtensorMap left, right;             // dz, piece of the table
-    ProductSide left_side, right_side;
-    bool bf16;
+struct CeDx : ProductOnce {
+    // left, right: dz, piece of the table
     CeRows rows;
     uint32_t width, tiles_n, steps, splits;
     float scale;
@@ -485,7 +479,7 @@ struct CeDx {
     ProductSplit split;
     float factor;
 
-    __device__ __forceinline__ uint32_t begin(bool reads_out) {
+    __device__ __forceinline__ uint32_t begin(uint32_t, bool reads_out) {
         count = __ldcg(rows.count);
         factor = reads_out ? ce_factor(__ldcg(rows.count + 1), scale, bf16) : 0.0f;
         const uint32_t tiles = (count + kProductTile - 1) / kProductTile * tiles_n * splits;
@@ -510,9 +504,10 @@ struct CeDx {
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         float* sum = sums + w.part * split_distance + (uint64_t)row * pitch + col;
-        char* to = nullptr;
+        ProductRows to = {};
+        to.anywhere = true;              // rows go back to where they were gathered from
         if (ends && splits == 1 && row < count)
-            to = static_cast<char*>(dx) + 2 * ((uint64_t)__ldcg(rows.origin + row) * lddx + col);
+            to.own = static_cast<char*>(dx) + 2 * ((uint64_t)__ldcg(rows.origin + row) * lddx + col);
 #pragma unroll 1
         for (int c = 0; c < r.columns && col + c < width; c += 32) {
             uint32_t v[32];
@@ -539,7 +534,7 @@ struct CeDx {
                 float o[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = factor * __uint_as_float(v[i]);
-                product_store(target, to ? to + 2 * c : nullptr, (int)(width - col) - c, o, r);
+                product_store(target, to, c, (int)(width - col) - c, o, r);
             }
         }
     }
@@ -569,10 +564,8 @@ ce_join_dx_kernel(const CeRows rows, const float* __restrict__ sums, const uint6
     }
 }
 
-struct CeDtable {
-    CUtensorMap left, right;             // dz, gathered rows
-    ProductSide left_side, right_side;
-    bool bf16;
+struct CeDtable : ProductOnce {
+    // left, right: dz, gathered rows
     CeRows rows;
     uint32_t entries, width, tiles_m, tiles_n;
     float scale;
@@ -583,7 +576,7 @@ struct CeDtable {
     ProductSplit split;
     float factor;
 
-    __device__ __forceinline__ uint32_t begin(bool reads_out) {
+    __device__ __forceinline__ uint32_t begin(uint32_t, bool reads_out) {
         count = __ldcg(rows.count);
         factor = reads_out ? ce_factor(__ldcg(rows.count + 1), scale, bf16) : 0.0f;
         split = product_split(tiles_m * tiles_n);
@@ -602,8 +595,8 @@ struct CeDtable {
     }
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
-        void* to = row < entries ? product_at(dtable, target.dtype, (uint64_t)row * ldt + col) : nullptr;
-        const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
+        const ProductRows to =
+            product_rows(dtable, target.dtype, ldt, row - r.lane, entries, col, r.lane);
 #pragma unroll 1
         for (int c = 0; c < r.columns && col + c < width; c += 32) {
             uint32_t v[32];
@@ -612,8 +605,7 @@ struct CeDtable {
 #pragma unroll
             for (int i = 0; i < 32; ++i)         // (no row counts: 0, whatever the factor)
                 o[i] = count ? factor * __uint_as_float(v[i]) : 0.0f;
-            product_store(target, to ? static_cast<char*>(to) + bytes * c : nullptr,
-                          (int)(width - col) - c, o, r);
+            product_store(target, to, c, (int)(width - col) - c, o, r);
         }
     }
 };

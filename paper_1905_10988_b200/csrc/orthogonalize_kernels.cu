@@ -26,6 +26,8 @@
 namespace natcomp {
 
 constexpr float kOrthoGramScale = 256.0f;
+constexpr int kOrthoSteps = 16;                      // of one launch
+constexpr int kOrthoLaunches = 64;
 constexpr float kOrthoLow = 2048.0f;                 // of the second of X's two values
 constexpr int kOrthoNormBlocks = 592;                // per matrix at most
 
@@ -41,6 +43,8 @@ struct OrthoInput {
     double eps, scale;
     __half *high, *low;
     uint64_t pitch;
+    uint32_t* arrived;                   // a word for each launch of the products, cleared here
+    int launches;
 };
 
 // eight values of a row, those beyond it 0
@@ -101,6 +105,8 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
     after_previous();
     let_next_begin();
     __shared__ double sums;
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < in.launches; i += 256) in.arrived[i] = 0;
     if (threadIdx.x < 32) {
         double s = 0.0;
 #pragma unroll 8
@@ -168,48 +174,116 @@ __device__ __forceinline__ void ortho_store16(__half* p, const float (&v)[16]) {
     st_wide(p, raw);
 }
 
-// POLYNOMIAL: b A + c A A from A, else A from X
-template <bool POLYNOMIAL> struct OrthoSquare {
-    CUtensorMap left, right;
+// Every step has three phases: A from X, b A + c A A from A, the next X.
+struct OrthoJob {
+    static constexpr bool kPhased = true;
+    CUtensorMap x_map[2], gram_map, poly_map;
+    bool bf16;                           // no
+    bool tall;
+    uint32_t phases;                     // three of every step, or, no steps, one
+    uint32_t* arrived;
+    uint32_t rows, cols, side, batch;
+    uint32_t tiles, tiles_m, tiles_n;    // of a side, of X
+    uint64_t pitch, side_pitch;          // row strides of X, and of A and the polynomial
+    __half *high[2], *low;
+    __half *gram, *poly;
+    float* diagonal;                     // of the polynomial: [matrix][side_pitch]; poly has 0 there
+    float of_step[3 * kOrthoSteps];      // a, b, c of the launch's steps
+    float gram_scale;
+    uint32_t turn;                       // which of the two X the first step reads
+    void* out;                           // of the last step, nullptr: another launch follows
+    uint64_t ldo, out_distance;
+    float scale;
+    ProductTarget target;
+    // of the phase
     ProductSide left_side, right_side;
-    bool bf16;
-    uint32_t side, tiles, batch, steps;
     ProductSplit split;
-    uint64_t pitch;
-    const __half* gram;                  // POLYNOMIAL
-    __half* out;
-    float* diagonal;                     // POLYNOMIAL: [matrix][pitch]; out has 0 there
-    float b, c;                          // c: of the product; b: of A
+    uint32_t kind, step, from, count;    // kind: 0, 1, 2, or 3 for no steps; from: which of the two X is read
+    float a, b, c;
 
     struct State {
-        Bytes32 old[2];                  // 32 values of A, a chunk ahead
+        Bytes32 first[2], second[2];     // 32 values of A, or of X's two, a chunk ahead
+        float of_column;                 // the lane's diagonal value, tall
     };
+    const OrthoJob* self;                // as the kernel was given it: arrays indexed there need no copy
+    __device__ __forceinline__ void given_as(const OrthoJob* job) { self = job; }
+    __device__ __forceinline__ const CUtensorMap* left_map() const {
+        return kind == 1 ? &self->gram_map : kind == 2 && !tall ? &self->poly_map : &self->x_map[from];
+    }
+    __device__ __forceinline__ const CUtensorMap* right_map() const {
+        return kind == 1 ? &self->gram_map : kind == 2 && tall ? &self->poly_map : &self->x_map[from];
+    }
     __device__ __forceinline__ uint32_t chains() const { return 1; }
-    __device__ __forceinline__ uint32_t begin(bool) {
-        return split.units(tiles * (tiles + 1) / 2 * batch);
+    __device__ __forceinline__ uint32_t begin(uint32_t phase, bool) {
+        step = phase / 3;
+        kind = phases == 1 ? 3 : phase - 3 * step;
+        from = (turn + step) & 1;
+        a = kind == 3 ? 1.0f : self->of_step[3 * step];
+        b = self->of_step[3 * step + 1];
+        c = kind == 0 ? gram_scale : self->of_step[3 * step + 2] * (1.0f / kOrthoGramScale);
+        left_side.symmetric = kind == 1 || (kind == 2 && !tall);
+        right_side.symmetric = kind == 1 || (kind == 2 && tall);
+        left_side.lines = kind == 0 && tall;
+        right_side.lines = kind == 0 ? tall : kind == 2 && !tall;
+        const uint32_t longer = tall ? rows : cols;
+        count = kind == 3 ? 0 : ((kind == 0 ? longer : side) + kProductStep - 1) / kProductStep;
+        const uint32_t all = (kind < 2 ? tiles * (tiles + 1) / 2 : tiles_m * tiles_n) * batch;
+        split = product_split(all);
+        return split.units(all);
     }
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         int column, width;
-        ProductUnit w = ortho_upper(split.tile(u, column, width), tiles);
+        const uint32_t t = split.tile(u, column, width);
+        ProductUnit w = {};
+        if (kind < 2) {
+            w = ortho_upper(t, tiles);
+        } else {
+            const uint32_t each = tiles_m * tiles_n, z = t / each;
+            product_tile(t - z * each, tiles_m, tiles_n, w.m, w.n);
+            w.z = (int)z;
+        }
         w.n += column;
         w.width = width;
-        w.steps = (int)steps;
+        w.steps = (int)count;
         return w;
     }
     __device__ __forceinline__ void load(const ProductUnit& w, const ProductRead& r, int k, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column) + k;
-        if (!POLYNOMIAL || row >= side || k >= r.columns) return;
-        const __half* p = gram + ((uint64_t)w.z * side + row) * pitch + col;
+        if (kind == 0 || k >= r.columns) return;
+        if (kind == 1) {
+            if (row >= side) return;
+            const __half* p = gram + ((uint64_t)w.z * side + row) * side_pitch + col;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (col + 16 * h < side) s.first[h] = ld_wide(p + 16 * h);
+            return;
+        }
+        if (kind == 2 && tall && col + r.lane < cols)
+            s.of_column = __ldcg(diagonal + w.z * side_pitch + col + r.lane);
+        if (row >= rows) return;
+        const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
+        const __half* p = self->high[from];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (col + 16 * h < side) s.old[h] = ld_wide(p + 16 * h);
+            if (col + 16 * h < cols) {
+                s.first[h] = ld_wide(p + at + 16 * h);
+                s.second[h] = ld_wide(low + at + 16 * h);
+            }
     }
     __device__ __forceinline__ void ahead(const ProductUnit& w, const ProductRead& r, State& s) const {
         load(w, r, 0, s);
     }
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
+        if (kind < 2)
+            store_square(w, r, s);
+        else
+            store_step(w, r, s);
+    }
+    // A, or b A + c A A without its diagonal
+    __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
-        const uint64_t at = ((uint64_t)w.z * side + row) * pitch + col;
+        const bool polynomial = kind == 1;
+        __half* to = (polynomial ? poly : gram) + ((uint64_t)w.z * side + row) * side_pitch + col;
 #pragma unroll 1
         for (int k = 0; k < r.columns && col + k < side; k += 32) {
             const State now = s;
@@ -219,93 +293,46 @@ template <bool POLYNOMIAL> struct OrthoSquare {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (row >= side || col + k + 16 * h >= side) continue;
-                float o[16], old[16];
-                if (POLYNOMIAL) ortho_unpack16(now.old[h], old);
+                float o[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    o[i] = c * __uint_as_float(v[16 * h + i]);
-                    if (POLYNOMIAL) o[i] = fmaf(b, old[i], o[i]);
-                }
-                if (POLYNOMIAL && row - (col + k + 16 * h) < 16) {
+                for (int i = 0; i < 16; ++i) o[i] = c * __uint_as_float(v[16 * h + i]);
+                if (polynomial) {
+                    float old[16];
+                    ortho_unpack16(now.first[h], old);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (row == col + k + 16 * h + i) {
-                            diagonal[w.z * pitch + row] = o[i] * (1.0f / kOrthoGramScale);
-                            o[i] = 0.0f;
-                        }
+                    for (int i = 0; i < 16; ++i) o[i] = fmaf(b, old[i], o[i]);
+                    if (row - (col + k + 16 * h) < 16) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (row == col + k + 16 * h + i) {
+                                diagonal[w.z * side_pitch + row] = o[i] * (1.0f / kOrthoGramScale);
+                                o[i] = 0.0f;
+                            }
+                    }
                 }
-                ortho_store16(out + at + k + 16 * h, o);
+                ortho_store16(to + k + 16 * h, o);
             }
         }
     }
-};
-
-struct OrthoStep {
-    CUtensorMap left, right;
-    ProductSide left_side, right_side;
-    bool bf16;
-    uint32_t rows, cols, tiles_m, tiles_n, batch, steps;
-    ProductSplit split;
-    uint64_t pitch;
-    float a;
-    const float* diagonal;               // of the polynomial: by rows, or, tall, by columns
-    uint64_t diagonal_pitch;
-    bool tall;
-    const __half* high;
-    __half *low, *next;
-    void* out;                           // of the last step, else nullptr
-    uint64_t ldo, out_distance;
-    float scale;
-    ProductTarget target;
-
-    struct State {
-        Bytes32 high[2], low[2];         // 32 values of X, a chunk ahead
-        float of_column;                 // the lane's diagonal value, tall
-    };
-    __device__ __forceinline__ uint32_t chains() const { return 1; }
-    __device__ __forceinline__ uint32_t begin(bool) { return split.units(tiles_m * tiles_n * batch); }
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
-        ProductUnit w = {};
-        int column;
-        const uint32_t t = split.tile(u, column, w.width);
-        const uint32_t each = tiles_m * tiles_n, z = t / each;
-        product_tile(t - z * each, tiles_m, tiles_n, w.m, w.n);
-        w.n += column;
-        w.z = (int)z;
-        w.steps = (int)steps;
-        return w;
-    }
-    __device__ __forceinline__ void load(const ProductUnit& w, const ProductRead& r, int k, State& s) const {
-        const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column) + k;
-        if (k >= r.columns) return;
-        if (steps && tall && col + r.lane < cols)
-            s.of_column = __ldcg(diagonal + w.z * diagonal_pitch + col + r.lane);
-        if (row >= rows) return;
-        const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (col + 16 * h < cols) {
-                s.high[h] = ld_wide(high + at + 16 * h);
-                s.low[h] = ld_wide(low + at + 16 * h);
-            }
-    }
-    __device__ __forceinline__ void ahead(const ProductUnit& w, const ProductRead& r, State& s) const {
-        load(w, r, 0, s);
-    }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
+    // a X + diagonal * X + the product, or, no steps, X
+    __device__ __forceinline__ void store_step(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint64_t at = ((uint64_t)w.z * rows + row) * pitch + col;
-        const int bytes = target.dtype == NC_DTYPE_F32 ? 4 : 2;
-        char* to = nullptr;
-        if (out && row < rows)
-            to = static_cast<char*>(out) + bytes * (w.z * out_distance + row * ldo + col);
-        const float* d = diagonal + w.z * diagonal_pitch;
-        const float of_row = steps && !tall && row < rows ? __ldcg(d + row) : 0.0f;
+        const bool last = out && (kind == 3 || 3 * step + 3 == phases);
+        ProductRows to = {};
+        if (last)
+            to = product_rows(static_cast<char*>(out) + (target.dtype == NC_DTYPE_F32 ? 4 : 2) *
+                                                            (w.z * out_distance),
+                              target.dtype, ldo, row - r.lane, rows, col, r.lane);
+        const bool by_column = kind == 2 && tall;
+        const float of_row =
+            kind == 2 && !tall && row < rows ? __ldcg(diagonal + w.z * side_pitch + row) : 0.0f;
+        __half* next = self->high[from ^ 1];
 #pragma unroll 1
         for (int k = 0; k < r.columns && col + k < cols; k += 32) {
             const State now = s;
             load(w, r, k + 32, s);
-            if (steps && tall) {         // the diagonal of the columns, a lane's each, for all lanes
+            if (by_column) {             // the diagonal of the columns, a lane's each, for all lanes
                 __syncwarp();
                 r.rows[r.lane] = now.of_column;
                 __syncwarp();
@@ -320,20 +347,18 @@ struct OrthoStep {
                     for (int i = 0; i < 16; ++i) o[16 * h + i] = 0.0f;
                     continue;
                 }
-                float x[16], y[16], f[16];
-                ortho_unpack16(now.high[h], x);
-                ortho_unpack16(now.low[h], y);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] = steps && tall ? r.rows[16 * h + i] : of_row;
+                float x[16], y[16];
+                ortho_unpack16(now.first[h], x);
+                ortho_unpack16(now.second[h], y);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float all = fmaf(y[i], 1.0f / kOrthoLow, x[i]);
-                    const float product =
-                        fmaf(f[i], x[i], __uint_as_float(v[16 * h + i]) * (1.0f / kOrthoGramScale));
+                    const float product = fmaf(by_column ? r.rows[16 * h + i] : of_row, x[i],
+                                               __uint_as_float(v[16 * h + i]) * (1.0f / kOrthoGramScale));
                     x[i] = fmaf(a, all, product);
                     o[16 * h + i] = scale * x[i];
                 }
-                if (!out) {
+                if (!last) {
                     Bytes32 first, second;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -347,8 +372,8 @@ struct OrthoStep {
                     st_wide(low + at + k + 16 * h, second);
                 }
             }
-            if (out)
-                product_store(target, to ? to + bytes * k : nullptr, (int)(cols - col) - k, o, r);
+            if (last)
+                product_store(target, to, k, (int)(cols - col) - k, o, r);
         }
     }
 };
@@ -356,7 +381,7 @@ struct OrthoStep {
 struct OrthoPlan {
     uint64_t side, pitch, side_pitch;
     int blocks;
-    size_t parts, high[2], low, gram, poly, diagonal, bytes;
+    size_t parts, high[2], low, gram, poly, diagonal, arrived, bytes;
 };
 
 static size_t ortho_place(size_t& at, size_t bytes) {
@@ -386,6 +411,7 @@ static OrthoPlan ortho_plan(uint64_t batch, uint64_t rows, uint64_t cols) {
     p.gram = ortho_place(at, 2 * batch * p.side * p.side_pitch);
     p.poly = ortho_place(at, 2 * batch * p.side * p.side_pitch);
     p.diagonal = ortho_place(at, 4 * batch * p.side_pitch);
+    p.arrived = ortho_place(at, 4 * kOrthoLaunches);
     p.bytes = at;
     return p;
 }
@@ -417,7 +443,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     if (steps < 0 || (steps && !coefficients) || !(eps >= 0.0f)) return NC_ERR_INVALID;
     if (batch == 0 || rows == 0 || cols == 0) return NC_OK;
     if (!g || !out || !workspace || ldg < cols || ldo < cols) return NC_ERR_INVALID;
-    if (!ortho_fits(batch, rows, cols)) return NC_ERR_TOO_LARGE;
+    if (!ortho_fits(batch, rows, cols) || steps > kOrthoSteps * kOrthoLaunches) return NC_ERR_TOO_LARGE;
     if (batch > 1 && (distance < (rows - 1) * ldg + cols || out_distance < (rows - 1) * ldo + cols))
         return NC_ERR_INVALID;
     if (!element_aligned(g, bytes) || !element_aligned(out, out_bytes) || !aligned32(workspace))
@@ -444,37 +470,26 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
                 (batch == 1 || distance * bytes % 16 == 0);
     in.parts = reinterpret_cast<double*>(ws + p.parts); in.blocks = p.blocks;
     in.eps = eps; in.scale = up; in.high = high[0]; in.low = low; in.pitch = p.pitch;
+    in.arrived = reinterpret_cast<uint32_t*>(ws + p.arrived);
+    in.launches = (steps + kOrthoSteps - 1) / kOrthoSteps;
     if (dtype == NC_DTYPE_F32) ortho_start<float>(in, (unsigned)batch, stream);
     else if (dtype == NC_DTYPE_BF16) ortho_start<__nv_bfloat16>(in, (unsigned)batch, stream);
     else ortho_start<__half>(in, (unsigned)batch, stream);
 
+    OrthoJob t = {};
     const uint64_t side_distance = p.side * p.side_pitch;
-    const uint32_t tiles = (uint32_t)((p.side + 255) / 256);
-    CUtensorMap x_map[2], gram_map, poly_map;
     for (int i = 0; i < 2; ++i)
-        if (!make_box_map(&x_map[i], high[i], false, batch, rows, cols, p.pitch, rows * p.pitch))
+        if (!make_box_map(&t.x_map[i], high[i], false, batch, rows, cols, p.pitch, rows * p.pitch))
             return NC_ERR_CUDA;
-    if (!make_box_map(&gram_map, gram, false, batch, p.side, p.side, p.side_pitch, side_distance) ||
-        !make_box_map(&poly_map, poly, false, batch, p.side, p.side, p.side_pitch, side_distance))
+    if (!make_box_map(&t.gram_map, gram, false, batch, p.side, p.side, p.side_pitch, side_distance) ||
+        !make_box_map(&t.poly_map, poly, false, batch, p.side, p.side, p.side_pitch, side_distance))
         return NC_ERR_CUDA;
-    OrthoSquare<false> s = {};
-    s.left_side.lines = s.right_side.lines = tall;
-    s.side = (uint32_t)p.side; s.tiles = tiles; s.batch = (uint32_t)batch; s.pitch = p.side_pitch;
-    s.steps = (uint32_t)((longer + kProductStep - 1) / kProductStep);
-    s.out = gram; s.c = kOrthoGramScale / (up * up);
-    OrthoSquare<true> q = {};
-    q.left = q.right = gram_map;
-    q.left_side.symmetric = q.right_side.symmetric = true;
-    q.side = s.side; q.tiles = tiles; q.batch = s.batch; q.pitch = p.side_pitch;
-    q.steps = (uint32_t)((p.side + kProductStep - 1) / kProductStep);
-    q.gram = gram; q.out = poly; q.diagonal = diagonal;
-    OrthoStep t = {};
-    (tall ? t.right_side : t.left_side).symmetric = true;
-    if (!tall) t.right_side.lines = true;
-    t.rows = (uint32_t)rows; t.cols = (uint32_t)cols; t.batch = (uint32_t)batch;
+    t.tall = tall; t.rows = (uint32_t)rows; t.cols = (uint32_t)cols; t.side = (uint32_t)p.side;
+    t.batch = (uint32_t)batch; t.tiles = (uint32_t)((p.side + 255) / 256);
     t.tiles_m = (uint32_t)((rows + 255) / 256); t.tiles_n = (uint32_t)((cols + 255) / 256);
-    t.pitch = p.pitch; t.low = low; t.tall = tall;
-    t.diagonal = diagonal; t.diagonal_pitch = p.side_pitch;
+    t.pitch = p.pitch; t.side_pitch = p.side_pitch;
+    t.high[0] = high[0]; t.high[1] = high[1]; t.low = low; t.gram = gram; t.poly = poly;
+    t.diagonal = diagonal; t.gram_scale = kOrthoGramScale / (up * up);
     t.ldo = ldo; t.out_distance = batch > 1 ? out_distance : 0; t.scale = scale / up;
     t.target.dtype = out_dtype;
     t.target.access = row_access(out, ldo, out_bytes, rows);
@@ -483,29 +498,16 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
         if (apart % 16) t.target.access = kRowElement;
         else if (apart % 32 && t.target.access == kRowWide) t.target.access = kRow16;
     }
-    const uint64_t upper = (uint64_t)tiles * (tiles + 1) / 2 * batch;
+    const uint64_t squares = (uint64_t)t.tiles * (t.tiles + 1) / 2 * batch;
     const uint64_t whole = (uint64_t)t.tiles_m * t.tiles_n * batch;
-    s.split = q.split = product_split((uint32_t)upper);
-    t.split = product_split((uint32_t)whole);
-    const int rounds = steps ? steps : 1;
-    for (int i = 0; i < rounds; ++i) {
-        nc_status st = NC_OK;
-        if (steps) {
-            s.left = s.right = x_map[i & 1];
-            st = product_launch(s, s.split.units((uint32_t)upper), stream);
-            if (st != NC_OK) return st;
-            q.b = coefficients[3 * i + 1];
-            q.c = coefficients[3 * i + 2] / kOrthoGramScale;
-            st = product_launch(q, q.split.units((uint32_t)upper), stream);
-            if (st != NC_OK) return st;
-        }
-        t.left = tall ? x_map[i & 1] : poly_map;
-        t.right = tall ? poly_map : x_map[i & 1];
-        t.a = steps ? coefficients[3 * i] : 1.0f;
-        t.steps = steps ? q.steps : 0;   // no steps: the normalised matrix
-        t.high = high[i & 1]; t.next = high[(i + 1) & 1];
-        t.out = i + 1 == rounds ? out : nullptr;
-        st = product_launch(t, t.split.units((uint32_t)whole), stream);
+    for (int i = 0; i == 0 || i < steps; i += kOrthoSteps) {
+        const int n = steps - i < kOrthoSteps ? steps - i : kOrthoSteps;
+        t.phases = n ? 3 * n : 1;
+        for (int k = 0; k < 3 * n; ++k) t.of_step[k] = coefficients[3 * i + k];
+        t.turn = i & 1;
+        t.out = i + n == steps ? out : nullptr;
+        t.arrived = in.arrived + i / kOrthoSteps;
+        const nc_status st = product_launch(t, 4 * (squares > whole ? squares : whole), stream);
         if (st != NC_OK) return st;
     }
     return launch_status();

@@ -15,6 +15,10 @@
 // holds two, while the next one is computed.  Both blocks' copies are counted by the first block's
 // barrier, so the issuing thread waits once a step.
 //
+// A job may have several phases, each of which reads what the one before has written: the blocks wait
+// for each other between them (a cooperative launch), which takes a third of the time that a launch
+// does.
+//
 // What a caller brings is a Job: maps and layout of the operands, the units of work, and store(), which
 // gets the accumulators of a row of the tile, 32 columns at a time.
 #pragma once
@@ -114,6 +118,53 @@ __device__ __forceinline__ void st_wide(void* p, const Bytes32& r) {
                  : "memory");
 }
 
+// what this thread has written to global memory is visible to the tensor copies of whoever sees what it
+// does next; and what it has seen to its own
+__device__ __forceinline__ void fence_global_copies() {
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+}
+
+__device__ __forceinline__ void grid_arrive(uint32_t* counter) {
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+}
+
+__device__ __forceinline__ uint32_t grid_arrived(const uint32_t* counter) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+    return v;
+}
+
+// Waits until `target` blocks have arrived; gives up after about two seconds, or where its block has.
+__device__ __forceinline__ bool grid_wait(const uint32_t* counter, uint32_t target,
+                                          volatile uint32_t* gave_up) {
+    const long long begin = clock64();
+    while (grid_arrived(counter) < target) {
+        if (*gave_up) return false;
+        if (clock64() - begin > 4000000000ll) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// Launches `kernel`, whose blocks wait for each other, so that all of them run at the same time.
+template <typename Kernel, typename... Args>
+inline cudaError_t launch_together(Kernel kernel, dim3 grid, dim3 block, size_t smem,
+                                   cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // map of `count` row-major matrices of 16-bit values for boxes of 64 x 64 with 128-byte swizzle; what
 // lies beyond a matrix reads as 0
 inline bool make_box_map(CUtensorMap* map, const void* p, bool bf16, uint64_t count, uint64_t rows,
@@ -199,6 +250,23 @@ __device__ __forceinline__ void product_next(const Job& job, uint32_t& u, uint32
 
 struct ProductNothing {};
 
+// a job of one phase
+struct ProductOnce {
+    static constexpr bool kPhased = false;
+    CUtensorMap left, right;
+    ProductSide left_side, right_side;
+    bool bf16;
+    uint32_t phases;
+    uint32_t* arrived;
+    const CUtensorMap *left_given, *right_given;
+    template <typename Job> __device__ __forceinline__ void given_as(const Job* job) {
+        left_given = &job->left;
+        right_given = &job->right;
+    }
+    __device__ __forceinline__ const CUtensorMap* left_map() const { return left_given; }
+    __device__ __forceinline__ const CUtensorMap* right_map() const { return right_given; }
+};
+
 // what a thread that reads a tile out has: one row, half of the columns
 struct ProductRead {
     uint32_t tmem;                       // of the warp's lanes and of its first column
@@ -239,6 +307,10 @@ __device__ __forceinline__ void product_pair_barrier(const ProductRead& r) {
     asm volatile("bar.sync %0, %1;" ::"r"(1 + r.quarter), "r"(64) : "memory");
 }
 
+__device__ __forceinline__ void product_writers_barrier() {
+    asm volatile("bar.sync %0, %1;" ::"r"(5), "r"(32 * kProductWriters) : "memory");
+}
+
 // tile number u of tiles_m x tiles_n, so that tiles computed at the same time share operands
 __device__ __forceinline__ void product_tile(uint32_t u, uint32_t tiles_m, uint32_t tiles_n, int& m,
                                              int& n) {
@@ -257,12 +329,35 @@ struct ProductTarget {
     RowAccess access;
 };
 
+// The rows of a warp: where its lane's own one goes, nullptr: nowhere; and, unless they lie anywhere, where
+// the first one goes, how far apart they are in elements, and how many there are.
+struct ProductRows {
+    void *own, *first;
+    uint64_t step;
+    int count;
+    bool anywhere;
+};
+
+// Rows of a matrix at p, of which `rows` are there: those of the thread's warp, whose first is `row0`.
+__device__ __forceinline__ ProductRows product_rows(void* p, int dtype, uint64_t ld, uint32_t row0,
+                                                    uint32_t rows, uint64_t col, int lane) {
+    const int bytes = dtype == NC_DTYPE_F32 ? 4 : 2;
+    ProductRows r;
+    r.count = row0 < rows ? (int)min(rows - row0, 32u) : 0;
+    r.first = static_cast<char*>(p) + bytes * (row0 * ld + col);
+    r.own = lane < r.count ? static_cast<char*>(r.first) + bytes * (lane * ld) : nullptr;
+    r.step = ld;
+    r.anywhere = false;
+    return r;
+}
+
 template <typename T>
-__device__ __forceinline__ void product_store_typed(const ProductTarget& t, T* row, int cols,
-                                                    float (&v)[32], const ProductRead& r) {
+__device__ __forceinline__ void product_store_typed(const ProductTarget& t, const ProductRows& to, int c,
+                                                    int cols, float (&v)[32], const ProductRead& r) {
     // a row whose 32 values are there and on 16-byte boundaries is written by its thread
     if (t.access != kRowElement && cols >= 32) {
-        if (!row) return;
+        if (!to.own) return;
+        T* row = static_cast<T*>(to.own) + c;
         const bool wide = t.access == kRowWide;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -292,37 +387,58 @@ __device__ __forceinline__ void product_store_typed(const ProductTarget& t, T* r
 #pragma unroll
     for (int i = 0; i < 32; ++i) r.rows[33 * r.lane + i] = v[i];
     __syncwarp();
+    const bool in = r.lane < cols;
+    if (!to.anywhere) {
+        T* p = static_cast<T*>(to.first) + c + r.lane;
+#pragma unroll 1
+        for (int at = 0; at < to.count; at += 8, p += 8 * to.step) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = r.rows[33 * (at + i) + r.lane];
+            if (t.add) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (in && at + i < to.count) x[i] += to_f32<T>(p[i * to.step]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (in && at + i < to.count) p[i * to.step] = from_f32<T>(x[i]);
+        }
+        return;
+    }
 #pragma unroll 4
     for (int i = 0; i < 32; ++i) {
-        T* p = reinterpret_cast<T*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)row, i));
+        T* p = reinterpret_cast<T*>(
+            __shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)to.own, i));
         const float x = r.rows[33 * i + r.lane];
-        if (p && r.lane < cols) p[r.lane] = from_f32<T>(t.add ? to_f32<T>(p[r.lane]) + x : x);
+        if (p && in) p[c + r.lane] = from_f32<T>(t.add ? to_f32<T>(p[c + r.lane]) + x : x);
     }
 }
 
-// 32 values of the thread's row, of which the first `cols` are there.  row: where the first one goes,
-// nullptr: nowhere.  All lanes of a warp come here with the same cols.
-__device__ __forceinline__ void product_store(const ProductTarget& t, void* row, int cols,
-                                              float (&v)[32], const ProductRead& r) {
+// 32 values of the thread's row, from column c of its part on, of which the first `cols` are there.  All
+// lanes of a warp come here with the same c and cols.
+__device__ __forceinline__ void product_store(const ProductTarget& t, const ProductRows& to, int c,
+                                              int cols, float (&v)[32], const ProductRead& r) {
     if (cols <= 0) return;
     if (t.dtype == NC_DTYPE_F32)
-        product_store_typed<float>(t, static_cast<float*>(row), cols, v, r);
+        product_store_typed<float>(t, to, c, cols, v, r);
     else if (t.dtype == NC_DTYPE_BF16)
-        product_store_typed<__nv_bfloat16>(t, static_cast<__nv_bfloat16*>(row), cols, v, r);
+        product_store_typed<__nv_bfloat16>(t, to, c, cols, v, r);
     else
-        product_store_typed<__half>(t, static_cast<__half*>(row), cols, v, r);
-}
-
-__device__ __forceinline__ void* product_at(void* p, int dtype, uint64_t i) {
-    return static_cast<char*>(p) + (dtype == NC_DTYPE_F32 ? 4 : 2) * i;
+        product_store_typed<__half>(t, to, c, cols, v, r);
 }
 
 // ---- the kernel ------------------------------------------------------------------------------
 //
 // Job:
-//   CUtensorMap left, right;  ProductSide left_side, right_side;  bool bf16;
-//   uint32_t begin(bool reads_out)    the number of units, for every thread once (may read what earlier
-//                                     kernels wrote); reads_out: of the warps that read tiles out
+//   ProductSide left_side, right_side;  bool bf16;
+//   static bool kPhased;  uint32_t phases;  uint32_t* arrived       phased: their number, and a word that
+//                                     is 0 at the beginning
+//   void given_as(const Job*)         the job as the kernel was given it (maps must be used where they are)
+//   const CUtensorMap* left_map(), right_map()
+//   uint32_t begin(uint32_t phase, bool reads_out)   the number of units, for every thread at the beginning
+//                                     of each phase (may read what earlier kernels wrote); reads_out: of
+//                                     the warps that read tiles out
 //   uint32_t chains() const           parts that the sum of a unit is read out in, one after the other
 //   ProductUnit unit_of(uint32_t u, uint32_t chain) const
 //   struct State                      what a thread keeps from one chain to the next
@@ -370,7 +486,8 @@ product_kernel(const __grid_constant__ Job given) {
     let_next_begin();
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, words[0], 0);
     Job job = given;
-    const uint32_t units = job.begin(warp < kProductWriters);
+    job.given_as(&given);
+    const uint32_t phases = Job::kPhased ? job.phases : 1;
 
     if (warp < kProductWriters) {
         ProductRead r;
@@ -383,6 +500,12 @@ product_kernel(const __grid_constant__ Job given) {
             reinterpret_cast<float*>(base + kProductBars + 256) + r.quarter * (kProductRows / 4);
         uint32_t turn = 0;
         typename Job::State state;
+        for (uint32_t phase = 0; phase < phases; ++phase) {
+        if (Job::kPhased && phase) {     // every block is done with the phase before
+            if (threadIdx.x == 0) grid_wait(job.arrived, phase * gridDim.x, gave_up);
+            product_writers_barrier();
+        }
+        const uint32_t units = job.begin(phase, true);
         for (uint32_t u = pair, chain = 0; u < units; product_next(job, u, chain, pairs), ++turn) {
             const ProductUnit w = job.unit_of(u, chain);
             const uint32_t b = turn & 1;
@@ -400,10 +523,24 @@ product_kernel(const __grid_constant__ Job given) {
             // (a tile that was not waited for was not read: the other block may still be reading it)
             if (lane == 0 && r.ok) mbar_arrive_at(drained + 8 * b, 0);
         }
+        if (Job::kPhased && phase + 1 < phases) {
+            fence_global_copies();
+            __threadfence();
+            product_writers_barrier();
+            if (threadIdx.x == 0) grid_arrive(job.arrived);
+        }
+        }
     } else if (warp == kProductCopyWarp) {
         if (lane == 0) {
             uint32_t step = 0, stage = 0, parity = 0;
             bool ok = true;
+            for (uint32_t phase = 0; phase < phases && ok; ++phase) {
+            if (Job::kPhased && phase) {
+                ok = grid_wait(job.arrived, phase * gridDim.x, gave_up);
+                fence_global_copies();
+            }
+            const uint32_t units = job.begin(phase, false);
+            const CUtensorMap *left = job.left_map(), *right = job.right_map();
             for (uint32_t u = pair, chain = 0; u < units && ok; product_next(job, u, chain, pairs)) {
                 const ProductUnit w = job.unit_of(u, chain);
                 const int m = w.m + (int)rank * kProductHalf, n = w.n + (int)rank * (w.width / 2);
@@ -416,15 +553,16 @@ product_kernel(const __grid_constant__ Job given) {
                     if (rank == 0) mbar_expect(bar, 2 * (kProductStage - (second ? 0 : kProductBox)));
                     const bool a = job.left_side.by_lines(m, k), b = job.right_side.by_lines(n, k);
                     for (int h = 0; h < 2; ++h) {
-                        tma_load_pair(to + h * kProductBox, &given.left, a ? m + 64 * h : k,
+                        tma_load_pair(to + h * kProductBox, left, a ? m + 64 * h : k,
                                       a ? k : m + 64 * h, w.z, bar);
                         if (h == 0 || second)
-                            tma_load_pair(to + kProductOperand + h * kProductBox, &given.right,
+                            tma_load_pair(to + kProductOperand + h * kProductBox, right,
                                           b ? n + 64 * h : k, b ? k : n + 64 * h, w.z, bar);
                     }
                     stage = stage + 1 == kProductStages ? 0 : stage + 1;
                     parity ^= stage == 0;
                 }
+            }
             }
             // both blocks' copies in flight land before the pair ends
             if (rank == 0) {
@@ -440,6 +578,8 @@ product_kernel(const __grid_constant__ Job given) {
         const uint64_t operand = mma_operand(stages, kProductBox);     // + bytes / 16: further on
         bool ok = true;
         uint32_t stage = 0, parity = 0, turn = 0;
+        for (uint32_t phase = 0; phase < phases && ok; ++phase) {
+        const uint32_t units = job.begin(phase, false);
         for (uint32_t u = pair, chain = 0; u < units && ok;
              product_next(job, u, chain, pairs), ++turn) {
             const ProductUnit w = job.unit_of(u, chain);
@@ -476,6 +616,7 @@ product_kernel(const __grid_constant__ Job given) {
             __syncwarp();
             mma_commit_pair(full + 8 * b, elected);
         }
+        }
     }
     // the pair stays until both blocks are done with each other's barriers and with TMEM
     __syncwarp();
@@ -485,16 +626,22 @@ product_kernel(const __grid_constant__ Job given) {
     if (warp == kProductMmaWarp) tmem_free_pair(tmem, 2 * kProductTile);
 }
 
-// most: an upper bound of the units
+// most: an upper bound of the units of a phase
 template <typename Job>
 inline nc_status product_launch(const Job& job, uint64_t most, cudaStream_t stream) {
     static bool allowed[64];
     if (!allow_dynamic_smem((const void*)product_kernel<Job>, kProductSmem, allowed))
         return NC_ERR_CUDA;
     const unsigned pairs = (unsigned)(most < kProductPairs ? (most ? most : 1) : kProductPairs);
-    launch_overlapping(product_kernel<Job>, dim3(2 * pairs), dim3(kProductThreads), kProductSmem,
-                       stream, job);
-    return NC_OK;
+    if (!Job::kPhased) {
+        launch_overlapping(product_kernel<Job>, dim3(2 * pairs), dim3(kProductThreads), kProductSmem,
+                           stream, job);
+        return NC_OK;
+    }
+    return launch_together(product_kernel<Job>, dim3(2 * pairs), dim3(kProductThreads), kProductSmem,
+                           stream, job) == cudaSuccess
+               ? NC_OK
+               : NC_ERR_CUDA;
 }
 
 }  // namespace natcomp

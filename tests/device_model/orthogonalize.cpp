@@ -32,9 +32,7 @@ int main(int argc, char** argv) {
     const bool any = std::string(argv[6]) == "any";
     model::rng.seed(atoi(argv[8]));
     const bool injected = ::injected(argc, argv, 9);
-    model::cluster_of[(const void*)product_kernel<OrthoSquare<false>>] = 2;
-    model::cluster_of[(const void*)product_kernel<OrthoSquare<true>>] = 2;
-    model::cluster_of[(const void*)product_kernel<OrthoStep>] = 2;
+    model::cluster_of[(const void*)product_kernel<OrthoJob>] = 2;
     const int ib = in == NC_DTYPE_F32 ? 4 : 2, ob = out == NC_DTYPE_F32 ? 4 : 2;
     const size_t ld = any ? cols + 3 : cols, off = any ? 1 : 0, apart = rows * ld + (any ? 5 : 0);
     const size_t all = (batch - 1) * apart + (rows - 1) * ld + cols;

@@ -87,6 +87,28 @@ inline void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
     for (int i = 0; i < 4; ++i) tmem_load8(at + 8 * i, reinterpret_cast<uint32_t(&)[8]>(r[8 * i]));
 }
 inline void tmem_wait32(uint32_t (&)[32]) {}
+inline void __threadfence() {}
+inline void fence_global_copies() {}
+inline void grid_arrive(uint32_t* counter) { ++*counter; }
+inline bool grid_wait(const uint32_t* counter, uint32_t target, volatile uint32_t* gave_up) {
+    const long long end = model::W.clock + model::kWaitLimit;
+    while (*counter < target) {
+        if (*gave_up) return false;
+        if (model::W.clock > end) {
+            *gave_up = 1;
+            return false;
+        }
+        model::cur->until = end + 201;
+        model::wait_on(counter, *counter, true);
+    }
+    return true;
+}
+template <typename K, typename... A>
+inline cudaError_t launch_together(K kernel, dim3 g, dim3 b, size_t smem, cudaStream_t, const A&... a) {
+    if ((int)g.x != model::declared_cluster(kernel))
+        model::fail("blocks that wait for each other: one cluster at a time runs here");
+    return model::launch_kernel(kernel, g, b, smem, model::declared_cluster(kernel), a...);
+}
 inline float exp2_approx(float x) { return exp2f(x); }
 inline Bytes32 ld_wide(const void* p) {
     if ((uintptr_t)p % 32) model::fail("load that is not aligned");
