@@ -28,6 +28,7 @@ namespace natcomp {
 constexpr float kOrthoGramScale = 256.0f;
 constexpr int kOrthoSteps = 16;                      // of one launch
 constexpr int kOrthoLaunches = 64;
+constexpr uint64_t kOrthoLong = 24;                  // steps of a sum that is worth splitting
 constexpr float kOrthoLow = 2048.0f;                 // of the second of X's two values
 constexpr int kOrthoNormBlocks = 592;                // per matrix at most
 
@@ -43,8 +44,8 @@ struct OrthoInput {
     double eps, scale;
     __half *high, *low;
     uint64_t pitch;
-    uint32_t* arrived;                   // a word for each launch of the products, cleared here
-    int launches;
+    uint32_t* arrived;                   // words that the products count in, cleared here
+    int words;
 };
 
 // eight values of a row, those beyond it 0
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
     let_next_begin();
     __shared__ double sums;
     if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int i = threadIdx.x; i < in.launches; i += 256) in.arrived[i] = 0;
+        for (int i = threadIdx.x; i < in.words; i += 256) in.arrived[i] = 0;
     if (threadIdx.x < 32) {
         double s = 0.0;
 #pragma unroll 8
@@ -190,6 +191,9 @@ struct OrthoJob {
     float* diagonal;                     // of the polynomial: [matrix][side_pitch]; poly has 0 there
     float of_step[3 * kOrthoSteps];      // a, b, c of the launch's steps
     float gram_scale;
+    uint32_t splits;                     // of the long sums of A
+    float4* parts;                       // [unit][split][column / 4][256 rows]
+    uint32_t* tickets;                   // [unit][half of the rows]: 0 at the beginning
     uint32_t turn;                       // which of the two X the first step reads
     void* out;                           // of the last step, nullptr: another launch follows
     uint64_t ldo, out_distance;
@@ -229,11 +233,12 @@ struct OrthoJob {
         count = kind == 3 ? 0 : ((kind == 0 ? longer : side) + kProductStep - 1) / kProductStep;
         const uint32_t all = (kind < 2 ? tiles * (tiles + 1) / 2 : tiles_m * tiles_n) * batch;
         split = product_split(all);
-        return split.units(all);
+        return split.units(all) * (kind == 0 ? splits : 1);
     }
     __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
         int column, width;
-        const uint32_t t = split.tile(u, column, width);
+        const uint32_t number = u, by = kind == 0 ? splits : 1;
+        const uint32_t t = split.tile(u / by, column, width);
         ProductUnit w = {};
         if (kind < 2) {
             w = ortho_upper(t, tiles);
@@ -244,7 +249,10 @@ struct OrthoJob {
         }
         w.n += column;
         w.width = width;
-        w.steps = (int)count;
+        w.part = number;
+        const uint32_t i = number % by, first = count * i / by;
+        w.k = (int)first * kProductStep;
+        w.steps = (int)(count * (i + 1) / by - first);
         return w;
     }
     __device__ __forceinline__ void load(const ProductUnit& w, const ProductRead& r, int k, State& s) const {
@@ -274,13 +282,43 @@ struct OrthoJob {
         load(w, r, 0, s);
     }
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
-        if (kind < 2)
-            store_square(w, r, s);
+        if (kind == 0 && splits > 1) {
+            if (store_part(w, r)) store_square<true>(w, r, s);
+        } else if (kind < 2)
+            store_square<false>(w, r, s);
         else
             store_step(w, r, s);
     }
-    // A, or b A + c A A without its diagonal
-    __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
+    __device__ __forceinline__ float4* part(const ProductUnit& w, const ProductRead& r, uint32_t number) const {
+        return parts + ((uint64_t)number * (w.width / 4) + r.column / 4) * kProductTile + r.row;
+    }
+    // A part of a sum, to memory.  Whether all parts of the block's rows are there now: the block that
+    // brings the last one adds them up, in their order.
+    __device__ __forceinline__ bool store_part(const ProductUnit& w, const ProductRead& r) const {
+        float4* to = part(w, r, w.part);
+#pragma unroll 1
+        for (int k = 0; k < r.columns; k += 32) {
+            uint32_t v[32];
+            r.load(k, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                to[(k / 4 + i) * kProductTile] =
+                    make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+        }
+        __threadfence();
+        product_writers_barrier();
+        if (threadIdx.x == 0) {
+            const uint32_t before = atomicAdd(tickets + 2 * (w.part / splits) + r.row / kProductHalf, 1u);
+            *r.word = (before + 1) % splits == 0;        // (every step of the launch comes round)
+        }
+        product_writers_barrier();
+        const bool last = *reinterpret_cast<volatile uint32_t*>(r.word) != 0;
+        __threadfence();
+        return last;
+    }
+    // A, or b A + c A A without its diagonal.  PARTS: the sums lie in parts.
+    template <bool PARTS> __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const bool polynomial = kind == 1;
         __half* to = (polynomial ? poly : gram) + ((uint64_t)w.z * side + row) * side_pitch + col;
@@ -289,7 +327,30 @@ struct OrthoJob {
             const State now = s;
             load(w, r, k + 32, s);
             uint32_t v[32];
-            r.load(k, v);
+            if (PARTS) {
+                float4 all[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) all[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                const float4* p = part(w, r, w.part / splits * splits) + k / 4 * kProductTile;
+#pragma unroll 2
+                for (uint32_t j = 0; j < splits; ++j) {
+                    const float4* q = p + (uint64_t)j * (w.width / 4) * kProductTile;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 x = __ldcg(q + i * kProductTile);
+                        all[i].x += x.x; all[i].y += x.y; all[i].z += x.z; all[i].w += x.w;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[4 * i] = __float_as_uint(all[i].x);
+                    v[4 * i + 1] = __float_as_uint(all[i].y);
+                    v[4 * i + 2] = __float_as_uint(all[i].z);
+                    v[4 * i + 3] = __float_as_uint(all[i].w);
+                }
+            } else {
+                r.load(k, v);
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (row >= side || col + k + 16 * h >= side) continue;
@@ -381,7 +442,8 @@ struct OrthoJob {
 struct OrthoPlan {
     uint64_t side, pitch, side_pitch;
     int blocks;
-    size_t parts, high[2], low, gram, poly, diagonal, arrived, bytes;
+    size_t parts, high[2], low, gram, poly, diagonal, arrived, sums, bytes;
+    uint32_t splits;
 };
 
 static size_t ortho_place(size_t& at, size_t bytes) {
@@ -411,7 +473,18 @@ static OrthoPlan ortho_plan(uint64_t batch, uint64_t rows, uint64_t cols) {
     p.gram = ortho_place(at, 2 * batch * p.side * p.side_pitch);
     p.poly = ortho_place(at, 2 * batch * p.side * p.side_pitch);
     p.diagonal = ortho_place(at, 4 * batch * p.side_pitch);
-    p.arrived = ortho_place(at, 4 * kOrthoLaunches);
+    p.arrived = ortho_place(at, 4 * (kOrthoLaunches + 2 * kProductPairs));
+    // Long sums of A by few tiles are split over the idle pairs, four steps a part at least.
+    const uint64_t tiles = (p.side + 255) / 256, squares = tiles * (tiles + 1) / 2 * batch;
+    const uint64_t steps = ((rows < cols ? cols : rows) + kProductStep - 1) / kProductStep;
+    p.splits = 1;
+    if (squares < kProductPairs && steps >= kOrthoLong) {
+        const ProductSplit s = product_split((uint32_t)squares);
+        const uint64_t units = s.units((uint32_t)squares), most = kProductPairs / units;
+        p.splits = (uint32_t)(most < steps / 4 ? most : steps / 4);
+        if (p.splits > 1)
+            p.sums = ortho_place(at, 4 * units * p.splits * kProductTile * (kProductTile / s.parts));
+    }
     p.bytes = at;
     return p;
 }
@@ -471,7 +544,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     in.parts = reinterpret_cast<double*>(ws + p.parts); in.blocks = p.blocks;
     in.eps = eps; in.scale = up; in.high = high[0]; in.low = low; in.pitch = p.pitch;
     in.arrived = reinterpret_cast<uint32_t*>(ws + p.arrived);
-    in.launches = (steps + kOrthoSteps - 1) / kOrthoSteps;
+    in.words = kOrthoLaunches + 2 * kProductPairs;
     if (dtype == NC_DTYPE_F32) ortho_start<float>(in, (unsigned)batch, stream);
     else if (dtype == NC_DTYPE_BF16) ortho_start<__nv_bfloat16>(in, (unsigned)batch, stream);
     else ortho_start<__half>(in, (unsigned)batch, stream);
@@ -490,6 +563,8 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     t.pitch = p.pitch; t.side_pitch = p.side_pitch;
     t.high[0] = high[0]; t.high[1] = high[1]; t.low = low; t.gram = gram; t.poly = poly;
     t.diagonal = diagonal; t.gram_scale = kOrthoGramScale / (up * up);
+    t.splits = p.splits; t.parts = reinterpret_cast<float4*>(ws + p.sums);
+    t.tickets = in.arrived + kOrthoLaunches;
     t.ldo = ldo; t.out_distance = batch > 1 ? out_distance : 0; t.scale = scale / up;
     t.target.dtype = out_dtype;
     t.target.access = row_access(out, ldo, out_bytes, rows);
@@ -507,7 +582,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
         t.turn = i & 1;
         t.out = i + n == steps ? out : nullptr;
         t.arrived = in.arrived + i / kOrthoSteps;
-        const nc_status st = product_launch(t, 4 * (squares > whole ? squares : whole), stream);
+        const nc_status st = product_launch(t, 4 * (squares > whole ? squares : whole) * p.splits, stream);
         if (st != NC_OK) return st;
     }
     return launch_status();

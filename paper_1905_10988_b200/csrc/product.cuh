@@ -225,6 +225,7 @@ struct ProductSplit {
 __host__ __device__ __forceinline__ ProductSplit product_split(uint32_t tiles) {
     const uint32_t rest = tiles % kProductPairs;
     ProductSplit s = {tiles - rest, 1};
+    if (rest == 0) return s;
     if (rest * 4 <= kProductPairs) s.parts = 4;
     else if (rest * 2 <= kProductPairs) s.parts = 2;
     return s;
@@ -275,6 +276,7 @@ struct ProductRead {
     bool ok, nothing;                    // !ok: a wait ran out, no result;  nothing: no steps
     float* rows;                         // the warp's own 32 x 33 words of shared memory
     float* exchange;                     // 32 x 33 words that the two warps of a quarter share
+    uint32_t* word;                      // one that all threads that read tiles out share
     template <int N> __device__ __forceinline__ void load(int c, uint32_t (&r)[N]) const {
         if (nothing) {
 #pragma unroll
@@ -498,6 +500,7 @@ product_kernel(const __grid_constant__ Job given) {
         r.rows = reinterpret_cast<float*>(base + kProductBars + 256) + warp * (kProductRows / 4);
         r.exchange =
             reinterpret_cast<float*>(base + kProductBars + 256) + r.quarter * (kProductRows / 4);
+        r.word = words + 2;
         uint32_t turn = 0;
         typename Job::State state;
         for (uint32_t phase = 0; phase < phases; ++phase) {

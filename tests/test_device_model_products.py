@@ -118,6 +118,19 @@ def test_orthogonalize(orthogonalize, case):
     run(orthogonalize, *case, 1)
 
 
+@pytest.fixture(scope="module")
+def split_sums(tmp_path_factory):
+    # sums of A of more than eight steps in two or more parts, although there is one pair only
+    return build(tmp_path_factory.mktemp("ortho_split"), "orthogonalize", dict(kProductPairs=1, kOrthoLong=8),
+                 [("most = kProductPairs / units", "most = 3"), ("squares < kProductPairs && ", "")])
+
+
+@pytest.mark.parametrize("case", [(1, 40, 700, "f32", "f32", "whole", 2), (1, 600, 33, "f32", "bf16", "any", 2)],
+                         ids=["wide", "tall"])
+def test_orthogonalize_with_split_sums(split_sums, case):
+    run(split_sums, *case, 1)
+
+
 def test_orthogonalize_with_late_copies(orthogonalize):
     run(orthogonalize, 1, 260, 300, "f32", "f32", "whole", 1, 2, "late=8")
 
