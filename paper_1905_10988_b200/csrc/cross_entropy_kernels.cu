@@ -79,12 +79,14 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     const uint64_t last = min(first + g.per_block, g.rows);
     uint32_t before = 0, all = 0, top = 0;
     // (every block begins at another place, or all of them ask the same parts of L2 at a time)
-#pragma unroll 8
-    for (uint64_t i = threadIdx.x; i < g.rows; i += 256) {
-        const uint64_t at = i + first < g.rows ? i + first : i + first - g.rows;
-        const uint32_t counts = ce_target(g, at) >= 0;
-        all += counts;
-        before += at < first ? counts : 0;
+    for (uint64_t i = threadIdx.x; i < g.rows; i += 8 * 256) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint64_t to = i + j * 256, at = to + first < g.rows ? to + first : to + first - g.rows;
+            const uint32_t counts = to < g.rows && ce_target(g, at) >= 0;
+            all += counts;
+            before += at < first ? counts : 0;
+        }
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {

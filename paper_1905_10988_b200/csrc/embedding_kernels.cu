@@ -13,7 +13,7 @@
 //   - segments of the sorted tokens are added up, a thread eight columns; runs of equal tokens that are
 //     not cut between segments are finished there, the others leave binary32 sums behind; other blocks
 //     clear rows meanwhile;
-//   - those sums are joined in order, and the rest of the rows is cleared.
+//   - those sums are joined in order.
 // Up to 512 tokens there is one kernel: a block for each token, of which the first of equal ones finds
 // the others by a scan and adds them up.
 // What bounds it: HBM, by the gradient that is written and the rows that are read.
@@ -37,10 +37,10 @@ constexpr int kMaxSegment = 32;          // sorted tokens of a block
 // 65536 x 4096 bfloat16, 512 take 96 us and 1024 115, sorted 102.
 constexpr int kDirect = 512;
 constexpr int kDirectThreads = 512;
-// What is cleared beside the sort and the joins: so many bytes a microsecond of them.
-constexpr uint64_t kClearRate = 2000000;
+// What is cleared beside the sort.  The blocks that do have scanned the tokens 7 to 8 us before the sort ends
+// (4096 tokens: after 4 of 11 us, 16384: after 7 of 15) and clear about 9 MB a microsecond.
+constexpr uint64_t kClearBeside = 64 << 20;
 constexpr uint64_t kClearBlock = 96 << 10;    // bytes that a block clears beside the sums
-constexpr uint64_t kJoinTime = 0;        // us
 constexpr int kJoinShort = 12;           // cuts of a run that one warp joins
 
 struct EmbedTokens {
@@ -190,7 +190,7 @@ struct EmbedSort {
     int passes, bits;                    // digits, and bits of one
     uint2* items[2];                     // key, place; the sorted ones end up in [0]
     uint32_t* counts;                    // [block][digits]
-    uint32_t* valid;                     // tokens in the vocabulary: [block]: of its part, then all
+    uint32_t* valid;                     // tokens in the vocabulary
     EmbedClear clear;
 };
 
@@ -243,12 +243,19 @@ __device__ __forceinline__ void embed_clear(const EmbedClear& s, uint32_t* flags
             }
         } else {
             // (every block begins at another place, or all of them ask the same parts of L2 at a time)
-            const uint64_t n = s.tokens.count, turn = n * block / blocks;
-#pragma unroll 8
-            for (uint64_t i = threadIdx.x; i < n; i += blockDim.x) {
-                const uint64_t at = i + turn < n ? i + turn : i + turn - n;
-                const uint64_t k = (uint64_t)s.tokens.key(at) - first;
-                if (k < rows) atomicOr(flags + (k >> 5), 1u << (k & 31));
+            const uint32_t n = (uint32_t)s.tokens.count, turn = (uint32_t)((uint64_t)n * block / blocks);
+            for (uint32_t i = threadIdx.x; i < n; i += 4 * blockDim.x) {
+                uint32_t key[4];         // (all loads before the first use)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t to = i + j * blockDim.x, at = to < n - turn ? to + turn : to - (n - turn);
+                    key[j] = to < n ? s.tokens.key(at) : 0xFFFFFFFFu;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t k = key[j] - (uint32_t)first;
+                    if (k < (uint32_t)rows) atomicOr(flags + (k >> 5), 1u << (k & 31));
+                }
             }
         }
         __syncthreads();
@@ -258,9 +265,21 @@ __device__ __forceinline__ void embed_clear(const EmbedClear& s, uint32_t* flags
     }
 }
 
+// two words to the same place in block `rank` of the cluster
+__device__ __forceinline__ void shared_store_pair_at(uint32_t at, uint32_t rank, uint2 v) {
+    asm volatile("{\n\t"
+                 ".reg .b32 remote;\n\t"
+                 "mapa.shared::cluster.u32 remote, %0, %1;\n\t"
+                 "st.shared::cluster.v2.u32 [remote], {%2, %3};\n\t"
+                 "}" ::"r"(at), "r"(rank), "r"(v.x), "r"(v.y)
+                 : "memory");
+}
+
 // One digit of a chunk of items: a warp's are neighbours, 32 for each round.  Afterwards rank[k] is that
 // of the thread's k-th item among its warp's with the same digit, ranks[warp][digit] how many the warps
-// before have, and the result, of thread `digit`, how many there are in the chunk.
+// before have, and the result, of thread `digit`, how many there are in the chunk.  ON_CHIP: items are
+// those of the chunk, in shared memory.
+template <bool ON_CHIP>
 __device__ __forceinline__ uint32_t embed_rank(const EmbedSort& s, const uint2* items, int pass, int rounds,
                                                uint64_t chunk, uint64_t last, uint16_t* ranks,
                                                uint2 (&item)[kSortEach], uint32_t (&rank)[kSortEach]) {
@@ -271,10 +290,12 @@ __device__ __forceinline__ uint32_t embed_rank(const EmbedSort& s, const uint2* 
 #pragma unroll
     for (int k = 0; k < kSortEach; ++k) {
         if (k >= rounds) break;
-        const uint64_t i = chunk + (warp * rounds + k) * 32 + lane;
-        item[k] = i >= last ? make_uint2(0xFFFFFFFFu, 0u)
-                  : pass    ? __ldcg(items + i)
-                            : make_uint2(s.tokens.key(i), (uint32_t)i);
+        const uint32_t at = (warp * rounds + k) * 32 + lane;
+        const uint64_t i = chunk + at;
+        item[k] = i >= last    ? make_uint2(0xFFFFFFFFu, 0u)
+                  : pass == 0  ? make_uint2(s.tokens.key(i), (uint32_t)i)
+                  : ON_CHIP    ? items[at]
+                               : __ldcg(items + i);
     }
     __syncthreads();
     uint16_t* mine = ranks + warp * digits;
@@ -283,7 +304,13 @@ __device__ __forceinline__ uint32_t embed_rank(const EmbedSort& s, const uint2* 
         if (k >= rounds) break;
         const bool in = chunk + (warp * rounds + k) * 32 + lane < last;
         const uint32_t d = item[k].x >> shift & (digits - 1);
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, in ? d : digits);
+        // lanes with the same digit: a vote for each bit (the instruction that finds equal values takes
+        // about 118 cycles of an SM with this many different ones, the votes a tenth)
+        uint32_t same = __ballot_sync(0xFFFFFFFFu, in);
+        for (int b = 0; b < s.bits; ++b) {
+            const uint32_t ones = __ballot_sync(0xFFFFFFFFu, d >> b & 1);
+            same &= d >> b & 1 ? ones : ~ones;
+        }
         const uint32_t old = in ? mine[d] : 0;
         rank[k] = old + __popc(same & below);
         __syncwarp();
@@ -303,40 +330,53 @@ __device__ __forceinline__ uint32_t embed_rank(const EmbedSort& s, const uint2* 
     return sum;
 }
 
+// ON_CHIP: a block's items are one chunk.  Between the passes they are held by the cluster's shared
+// memory, block b the places from b * each on, and so are the counts: nothing goes through L2, which the
+// blocks that clear keep busy.  (16384 tokens of 65536: XXX us instead of 19.)
+template <bool ON_CHIP>
 __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __grid_constant__ EmbedSort s) {
-    extern __shared__ uint16_t ranks[];          // [warp][digit]
+    // [warp][digit]; ON_CHIP, behind it, of every block how many items have each digit, and the items
+    extern __shared__ uint16_t ranks[];
     __shared__ uint32_t base[1 << kSortMaxBits];
     __shared__ uint32_t sums[kSortWarps];
+    __shared__ uint32_t valids[kSortMaxBlocks];      // of the first block
+    const bool clears = (int)blockIdx.x >= s.blocks;
+    if (!clears) cluster_sync();         // all of its blocks run
     after_previous();
     let_next_begin();
-    if ((int)blockIdx.x >= s.blocks) {
+    if (clears) {
         embed_clear(s.clear, reinterpret_cast<uint32_t*>(ranks), blockIdx.x - s.blocks,
                     gridDim.x - s.blocks, nullptr, 0);
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t digits = 1u << s.bits;
+    const uint32_t digits = 1u << s.bits, number = blockIdx.x;
+    uint32_t* counts = reinterpret_cast<uint32_t*>(ranks + kSortWarps * digits);
+    uint2* here = reinterpret_cast<uint2*>(counts + s.blocks * digits);
     const uint64_t n = s.tokens.count;
-    const uint64_t first = n * blockIdx.x / s.blocks, last = n * (blockIdx.x + 1) / s.blocks;
+    const uint32_t each = (uint32_t)((n + s.blocks - 1) / s.blocks);
+    const uint64_t first = min((uint64_t)number * each, n), last = min(first + each, n);
     // of a warp in a chunk: 32 items each
-    const int rounds = (int)min((last - first + kSortThreads - 1) / kSortThreads, (uint64_t)kSortEach);
-    const bool single = last - first <= (uint64_t)kSortChunk;        // one chunk: read once a pass
+    const int rounds = min((int)((each + kSortThreads - 1) / kSortThreads), kSortEach);
     uint2 item[kSortEach];
     uint32_t rank[kSortEach];
     uint32_t valid = 0;
     for (int pass = 0; pass < s.passes; ++pass) {
-        // from buffer (passes - pass) & 1 to the other one
-        const uint2* items = s.items[(s.passes - pass) & 1];
-        uint2* to = s.items[(s.passes - pass - 1) & 1];
+        // from buffer (passes - pass) & 1 to the other one, or through the blocks' own
+        const uint2* items = ON_CHIP ? here : s.items[(s.passes - pass) & 1];
+        uint2* to = s.items[ON_CHIP ? 0 : (s.passes - pass - 1) & 1];
         const int shift = pass * s.bits;
         // how many items of the block have each digit, by thread
         uint32_t mine = 0;
-        if (single) {
-            mine = embed_rank(s, items, pass, rounds, first, last, ranks, item, rank);
+        if (ON_CHIP) {
+            mine = embed_rank<true>(s, items, pass, rounds, first, last, ranks, item, rank);
             if (pass == 0)
 #pragma unroll
                 for (int k = 0; k < kSortEach; ++k)      // (none: a key beyond all)
                     if (k < rounds) valid += item[k].x < s.tokens.vocabulary;
+            if (threadIdx.x < digits)
+                for (int b = 0; b < s.blocks; ++b)
+                    shared_store_at(smem_u32(counts + number * digits + threadIdx.x), b, mine);
         } else {
             for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) base[d] = 0;
             __syncthreads();
@@ -346,9 +386,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
                 atomicAdd(base + (k >> shift & (digits - 1)), 1u);
             }
             __syncthreads();
-            if (threadIdx.x < digits) mine = base[threadIdx.x];
+            if (threadIdx.x < digits) s.counts[number * digits + threadIdx.x] = base[threadIdx.x];
         }
-        if (threadIdx.x < digits) s.counts[blockIdx.x * digits + threadIdx.x] = mine;
         if (pass == 0) {
 #pragma unroll
             for (int d = 16; d; d >>= 1) valid += __shfl_xor_sync(0xFFFFFFFFu, valid, d);
@@ -356,22 +395,25 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
             __syncthreads();
             if (threadIdx.x == 0) {
                 for (int w = 1; w < kSortWarps; ++w) valid += sums[w];
-                s.valid[blockIdx.x] = valid;
+                shared_store_at(smem_u32(valids + number), 0, valid);
             }
         }
         cluster_sync();
-        if (pass == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
+        if (pass == 0 && number == 0 && threadIdx.x == 0) {
             valid = 0;
-            for (int b = 0; b < s.blocks; ++b) valid += __ldcg(s.valid + b);
-            s.valid[kSortMaxBlocks] = valid;
+            for (int b = 0; b < s.blocks; ++b) valid += valids[b];
+            *s.valid = valid;
         }
         // the items of lower digits, and of this one in the blocks before
         uint32_t before = 0, all = 0;
         if (threadIdx.x < digits) {
 #pragma unroll
             for (int b = 0; b < kSortMaxBlocks; ++b) {
-                const uint32_t c = b < s.blocks ? __ldcg(s.counts + b * digits + threadIdx.x) : 0;
-                before += b < (int)blockIdx.x ? c : 0;
+                uint32_t c = 0;
+                if (b < s.blocks)
+                    c = ON_CHIP ? counts[b * digits + threadIdx.x]
+                                : __ldcg(s.counts + b * digits + threadIdx.x);
+                before += b < (int)number ? c : 0;
                 all += c;
             }
         }
@@ -387,10 +429,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
 #pragma unroll
         for (int d = 16; d; d >>= 1) lower += __shfl_xor_sync(0xFFFFFFFFu, lower, d);
         if (threadIdx.x < digits) base[threadIdx.x] = before + lower + up - all;
-        for (uint64_t chunk = first; chunk < last; chunk += rounds * kSortThreads) {
-            if (!single) {
+        for (uint64_t chunk = first; ON_CHIP || chunk < last; chunk += rounds * kSortThreads) {
+            if (!ON_CHIP) {
                 __syncthreads();
-                mine = embed_rank(s, items, pass, rounds, chunk, last, ranks, item, rank);
+                mine = embed_rank<false>(s, items, pass, rounds, chunk, last, ranks, item, rank);
             }
             __syncthreads();
 #pragma unroll
@@ -398,15 +440,21 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
                 if (k >= rounds) break;
                 if (chunk + (warp * rounds + k) * 32 + lane < last) {
                     const uint32_t d = item[k].x >> shift & (digits - 1);
-                    to[base[d] + ranks[warp * digits + d] + rank[k]] = item[k];
+                    const uint32_t at = base[d] + ranks[warp * digits + d] + rank[k];
+                    if (ON_CHIP && pass + 1 < s.passes) {
+                        const uint32_t owner = at / each;
+                        shared_store_pair_at(smem_u32(here + (at - owner * each)), owner, item[k]);
+                    } else {
+                        to[at] = item[k];
+                    }
                 }
             }
-            if (!single) {
-                __syncthreads();
-                if (threadIdx.x < digits) base[threadIdx.x] += mine;
-            }
+            if (ON_CHIP) break;
+            __syncthreads();
+            if (threadIdx.x < digits) base[threadIdx.x] += mine;
         }
-        cluster_sync();
+        // (the last pass of the chip leaves nothing that a block of the cluster reads)
+        if (!ON_CHIP || pass + 1 < s.passes) cluster_sync();
     }
 }
 
@@ -427,7 +475,7 @@ struct EmbedSum {
     uint64_t pitch;                      // segment, of the one that goes on behind it
     uint32_t segments;
     uint32_t across;                     // threads that take eight columns each of a block's 1024
-    EmbedClear clear[2];                 // beside the sums, and beside the joins
+    EmbedClear clear;
 };
 
 // tokens in the vocabulary.  One thread of a block asks: asked by every warp of a few thousand blocks, the
@@ -470,7 +518,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     uint32_t number;
     const uint32_t works = (s.segments + groups - 1) / groups;
     if (embed_clears(works, number)) {
-        embed_clear(s.clear[0], flags, number * gridDim.y + blockIdx.y,
+        embed_clear(s.clear, flags, number * gridDim.y + blockIdx.y,
                     (gridDim.x - works) * gridDim.y, s.items, n);
         return;
     }
@@ -557,20 +605,12 @@ template <typename O>
 __global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedSum s) {
     __shared__ float sums[8][256];
     __shared__ uint32_t ends[8];         // of each of those runs: the segment after its last cut
-    __shared__ uint32_t flags[kClearBytes / 4];
     after_previous();
     let_next_begin();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t n = embed_valid(s), segments = (n + s.segment - 1) / s.segment;
-    uint32_t number;
-    const uint32_t works = (s.segments + 7) / 8;
-    if (embed_clears(works, number)) {
-        embed_clear(s.clear[1], flags, number * gridDim.y + blockIdx.y,
-                    (gridDim.x - works) * gridDim.y, s.items, n);
-        return;
-    }
     const uint64_t c = (uint64_t)blockIdx.y * 256 + 8 * lane;
-    const uint32_t group = number * 8;
+    const uint32_t group = blockIdx.x * 8;
     if (group >= segments) return;
     // (every warp finds out for itself which of the eight a run is cut at for the first time)
     const uint32_t g = group + (lane & 7);
@@ -790,7 +830,7 @@ static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
     };
     for (int i = 0; i < 2; ++i) p.items[i] = place(8 * rows);
     p.counts = place((size_t)4 * kSortMaxBlocks << kSortMaxBits);
-    p.valid = place(4 * (kSortMaxBlocks + 1));
+    p.valid = place(4);
     p.parts = place(8 * (size_t)p.segments * p.pitch);
     p.bytes = at;
     return p;
@@ -807,11 +847,11 @@ static void embed_sums(const EmbedSum& s, uint32_t segments, cudaStream_t stream
         const uint64_t n = (c.end - c.begin) * c.row_bytes / kClearBlock / down + 1;
         return (unsigned)(n < 65536 ? n : 65536);
     };
-    const unsigned first = clears(s.clear[0], slabs), second = clears(s.clear[1], columns);
+    const unsigned clear = clears(s.clear, slabs);
     launch_overlapping(s.add ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>,
-                       dim3((segments + groups - 1) / groups + first, slabs), dim3(kSumThreads), 0, stream,
+                       dim3((segments + groups - 1) / groups + clear, slabs), dim3(kSumThreads), 0, stream,
                        s);
-    launch_overlapping(embed_join_kernel<O>, dim3((segments + 7) / 8 + second, columns), dim3(256), 0,
+    launch_overlapping(embed_join_kernel<O>, dim3((segments + 7) / 8, columns), dim3(256), 0,
                        stream, s);
 }
 
@@ -922,21 +962,23 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint2*>(ws + p.items[i]);
     s.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
     s.valid = reinterpret_cast<uint32_t*>(ws + p.valid);
-    // as many rows as are cleared while the sort runs (8 us a digit and 2 for every 1024 tokens of a
-    // block), and while the joins do, which leave the memory idle as well
+    // as many rows as are cleared while the sort runs
     s.clear = clear;
-    const uint64_t sort_us = p.passes * (8 + 2 * (rows / (p.sorters * (uint64_t)kSortThreads)));
-    const uint64_t beside = sort_us * kClearRate / clear.row_bytes;
-    const uint64_t later = kJoinTime * kClearRate / clear.row_bytes;
+    const uint64_t beside = kClearBeside / clear.row_bytes;
     if (beside < clear.end) s.clear.end = beside;
-    // one block on every SM, in whole clusters; no others than the sorting ones where nothing is cleared
-    const int clusters = s.clear.end ? device_sm_count() / p.sorters : 1;
+    // a block on most SMs, in clusters (16 of 8 blocks run at a time: the chip's parts hold two each); none
+    // but the sorting ones where nothing is cleared
+    const int clusters = s.clear.end ? device_sm_count() * 7 / 8 / p.sorters : 1;
     const int grid = (s.clear.end && clusters < 2 ? 2 : clusters) * p.sorters;
-    const int ranks = kSortWarps * 2 << p.bits;
-    const int smem = ranks > kClearBytes ? ranks : kClearBytes;
-    static bool allowed[64];
-    if (!allow_dynamic_smem((const void*)embed_sort_kernel, kSortWarps * 2 << kSortMaxBits, allowed))
-        return NC_ERR_CUDA;
+    const bool on_chip = (rows + p.sorters - 1) / p.sorters <= (uint64_t)kSortChunk;
+    int smem = kSortWarps * 2 << p.bits;
+    if (on_chip) smem += (p.sorters * 4 << p.bits) + (int)((rows + p.sorters - 1) / p.sorters) * 8;
+    if (smem < kClearBytes) smem = kClearBytes;
+    auto kernel = on_chip ? embed_sort_kernel<true> : embed_sort_kernel<false>;
+    constexpr int kMost = (kSortWarps * 2 << kSortMaxBits) + (kSortMaxBlocks * 4 << kSortMaxBits) +
+                          kSortChunk * 8;
+    static bool allowed[2][64];
+    if (!allow_dynamic_smem((const void*)kernel, kMost, allowed[on_chip])) return NC_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kSortThreads);
@@ -950,16 +992,14 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaLaunchKernelEx(&cfg, embed_sort_kernel, s);
+    cudaLaunchKernelEx(&cfg, kernel, s);
     EmbedSum e = {};
-    e.items = s.items[0]; e.valid = s.valid + kSortMaxBlocks; e.across = p.across;
+    e.items = s.items[0]; e.valid = s.valid; e.across = p.across;
     e.segment = p.segment; e.segments = p.segments; e.dy = dy; e.cols = cols; e.lddy = lddy;
     e.vector = vector; e.scale = scale; e.dtable = dtable; e.ldt = lddt; e.add = accumulate != 0;
     e.parts = reinterpret_cast<float*>(ws + p.parts); e.pitch = p.pitch;
-    e.clear[0] = e.clear[1] = clear;
-    e.clear[0].begin = s.clear.end;
-    e.clear[1].begin = clear.end > s.clear.end + later ? clear.end - later : s.clear.end;
-    e.clear[0].end = e.clear[1].begin;
+    e.clear = clear;
+    e.clear.begin = s.clear.end;
     NC_EMBED_TYPES(dtype, dtable_dtype, embed_sums, e, p.segments, stream);
     return launch_status();
 }

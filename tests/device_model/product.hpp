@@ -87,6 +87,10 @@ inline void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
     for (int i = 0; i < 4; ++i) tmem_load8(at + 8 * i, reinterpret_cast<uint32_t(&)[8]>(r[8 * i]));
 }
 inline void tmem_wait32(uint32_t (&)[32]) {}
+inline void shared_store_pair_at(uint32_t at, uint32_t rank, uint2 v) {
+    if (at % 8) model::fail("store that is not aligned");
+    memcpy(model::memory(model::mapped(at, rank)), &v, 8);
+}
 inline void __threadfence() {}
 inline void fence_global_copies() {}
 inline void grid_arrive(uint32_t* counter) { ++*counter; }

@@ -31,6 +31,8 @@ def build(folder, name, constants=None, replace=()):
             for b, e in reversed(cut):
                 text = text[:b] + text[e:]
             text = model + text.replace("mma_pair(", "product_mma(")
+        if file == "embedding_kernels.cu":
+            text = translate._without(text, ["shared_store_pair_at"])
         for old, new in replace:
             if file == name + "_kernels.cu":
                 assert text.count(old) == 1, old
@@ -167,12 +169,27 @@ def sorted_embedding(tmp_path_factory):
     # clears some of the rows beside the sort and some later, and
     # takes runs of more than three segments for long ones
     return build(tmp_path_factory.mktemp("embed_sorted"), "embedding",
-                 dict(kJoinShort=3, kClearRate=2000))
+                 dict(kJoinShort=3),
+                 [("kClearBeside = 64 << 20", "kClearBeside = 8 << 10")])
 
 
 SORTED = [(600, 50, 20, "f16", "f16", "whole", "few", 8, 0), (900, 1200, 9, "f32", "bf16", "any", "one", 4, 0),
           (700, 3000, 12, "bf16", "f32", "whole", "many", 8, 0), (520, 40, 1100, "bf16", "f32", "any", "few", 8, 1),
-          (513, 20, 12, "f16", "f32", "whole", "none", 8, 0), (4500, 300, 3, "f32", "f32", "any", "many", 8, 1)]
+          (513, 20, 12, "f16", "f32", "whole", "none", 8, 0), (4500, 300, 3, "f32", "f32", "any", "many", 8, 1),
+          (9000, 70000, 2, "f32", "f32", "whole", "many", 8, 0)]
+
+
+@pytest.fixture(scope="module")
+def chunked_embedding(tmp_path_factory):
+    # sorts in chunks through memory what would fit the chip
+    return build(tmp_path_factory.mktemp("embed_chunks"), "embedding", dict(kSortMaxBlocks=2),
+                 [("<= (uint64_t)kSortChunk;", "<= 0;"), ("min((int)((each + kSortThreads - 1) / kSortThreads), kSortEach)", "2")])
+
+
+@pytest.mark.parametrize("case", [(700, 50, 20, "f16", "f16", "whole", "few", 8, 0),
+                                  (9001, 3000, 3, "f32", "f32", "whole", "many", 4, 1)], ids=["one", "two"])
+def test_embedding_sorted_in_chunks(chunked_embedding, case):
+    run(chunked_embedding, *case, 1)
 
 
 @pytest.mark.parametrize("case", SORTED, ids=["-".join(map(str, c)) for c in SORTED])
