@@ -66,6 +66,19 @@ __device__ __forceinline__ int64_t ce_target(const CeGather& g, uint64_t i) {
 // bits of a coefficient's magnitude: ordered as the magnitudes are, NaN above all
 __device__ __forceinline__ uint32_t ce_magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// a row at any element to one on 16-byte boundaries, eight values a lane; what lies behind it becomes 0
+__device__ __forceinline__ void ce_copy_row(const unsigned short* from, uint64_t width, uint4* to, int lane) {
+    const uint32_t eights = (uint32_t)((width + 7) / 8);
+#pragma unroll 2
+    for (uint32_t c = lane; c < eights; c += 32) {
+        uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (8 * c + i < width) v[i >> 1] |= (uint32_t)__ldg(from + 8 * c + i) << (16 * (i & 1));
+        to[c] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+
 // Every block counts the rows before its own, and all of them, for itself: a few reads of the targets
 // out of L2 instead of a pass that finds the places first.
 __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ CeGather g) {
@@ -104,7 +117,7 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
         all += sums[w][1];
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) g.to.count[0] = all;
-    const uint32_t words = (uint32_t)((g.width + 1) / 2), eights = (uint32_t)(g.to.pitch / 8);
+    const uint32_t eights = (uint32_t)(g.to.pitch / 8);
     for (uint64_t chunk = first; chunk < last; chunk += 256) {
         // places of up to 256 rows
         const uint64_t i = chunk + threadIdx.x;
@@ -161,13 +174,7 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
                 for (uint32_t c = lane; c < g.width / 8; c += 32)
                     out[c] = __ldg(reinterpret_cast<const uint4*>(from) + c);
             } else {
-                uint32_t* pairs = reinterpret_cast<uint32_t*>(out);
-#pragma unroll 4
-                for (uint32_t c = lane; c < words; c += 32) {
-                    uint32_t v = __ldg(from + 2 * c);
-                    if (2 * c + 1 < g.width) v |= (uint32_t)__ldg(from + 2 * c + 1) << 16;
-                    pairs[c] = v;
-                }
+                ce_copy_row(from, g.width, out, lane);
             }
         }
     }
@@ -195,19 +202,9 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
                const uint64_t ld, unsigned short* __restrict__ to, const uint64_t pitch) {
     after_previous();
     let_next_begin();
-    const int lane = threadIdx.x & 31;
-    const uint32_t words = (uint32_t)((width + 1) / 2);
     for (uint64_t r = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows;
-         r += (uint64_t)gridDim.x * 8) {
-        const unsigned short* p = from + r * ld;
-        uint32_t* out = reinterpret_cast<uint32_t*>(to + r * pitch);
-#pragma unroll 4
-        for (uint32_t c = lane; c < words; c += 32) {
-            uint32_t v = __ldg(p + 2 * c);
-            if (2 * c + 1 < width) v |= (uint32_t)__ldg(p + 2 * c + 1) << 16;
-            out[c] = v;
-        }
-    }
+         r += (uint64_t)gridDim.x * 8)
+        ce_copy_row(from + r * ld, width, reinterpret_cast<uint4*>(to + r * pitch), threadIdx.x & 31);
 }
 
 // ---- forward ---------------------------------------------------------------------------------

@@ -966,9 +966,11 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     s.clear = clear;
     const uint64_t beside = kClearBeside / clear.row_bytes;
     if (beside < clear.end) s.clear.end = beside;
-    // a block on most SMs, in clusters (16 of 8 blocks run at a time: the chip's parts hold two each); none
-    // but the sorting ones where nothing is cleared
-    const int clusters = s.clear.end ? device_sm_count() * 7 / 8 / p.sorters : 1;
+    // a block on most SMs, in clusters: not all SMs, because the chip's parts do not hold whole numbers of
+    // clusters, and one that waits for another to end is late (18 clusters of 8 blocks: the last ended
+    // after 25 us, the others after 13); none but the sorting one where nothing is cleared
+    const int sms = device_sm_count(), fit = p.sorters > 1 ? sms * 3 / 4 / p.sorters : sms;
+    const int clusters = s.clear.end ? fit : 1;
     const int grid = (s.clear.end && clusters < 2 ? 2 : clusters) * p.sorters;
     const bool on_chip = (rows + p.sorters - 1) / p.sorters <= (uint64_t)kSortChunk;
     int smem = kSortWarps * 2 << p.bits;

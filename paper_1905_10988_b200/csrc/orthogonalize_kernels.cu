@@ -211,6 +211,12 @@ struct OrthoJob {
     };
     const OrthoJob* self;                // as the kernel was given it: arrays indexed there need no copy
     __device__ __forceinline__ void given_as(const OrthoJob* job) { self = job; }
+    __device__ __forceinline__ void prefetch() const {
+        prefetch_map(&x_map[0]);
+        prefetch_map(&x_map[1]);
+        prefetch_map(&gram_map);
+        prefetch_map(&poly_map);
+    }
     __device__ __forceinline__ const CUtensorMap* left_map() const {
         return kind == 1 ? &self->gram_map : kind == 2 && !tall ? &self->poly_map : &self->x_map[from];
     }

@@ -118,6 +118,11 @@ __device__ __forceinline__ void st_wide(void* p, const Bytes32& r) {
                  : "memory");
 }
 
+// brings a map to where tensor copies look it up
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
 // what this thread has written to global memory is visible to the tensor copies of whoever sees what it
 // does next; and what it has seen to its own
 __device__ __forceinline__ void fence_global_copies() {
@@ -263,6 +268,10 @@ struct ProductOnce {
     template <typename Job> __device__ __forceinline__ void given_as(const Job* job) {
         left_given = &job->left;
         right_given = &job->right;
+    }
+    __device__ __forceinline__ void prefetch() const {
+        prefetch_map(&left);
+        prefetch_map(&right);
     }
     __device__ __forceinline__ const CUtensorMap* left_map() const { return left_given; }
     __device__ __forceinline__ const CUtensorMap* right_map() const { return right_given; }
@@ -436,6 +445,7 @@ __device__ __forceinline__ void product_store(const ProductTarget& t, const Prod
 //   ProductSide left_side, right_side;  bool bf16;
 //   static bool kPhased;  uint32_t phases;  uint32_t* arrived       phased: their number, and a word that
 //                                     is 0 at the beginning
+//   void prefetch() const             of its maps
 //   void given_as(const Job*)         the job as the kernel was given it (maps must be used where they are)
 //   const CUtensorMap* left_map(), right_map()
 //   uint32_t begin(uint32_t phase, bool reads_out)   the number of units, for every thread at the beginning
@@ -469,6 +479,7 @@ product_kernel(const __grid_constant__ Job given) {
     const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (warp == kProductMmaWarp) tmem_alloc_pair(smem_u32(words), 2 * kProductTile);
+    if (threadIdx.x == 32 * kProductCopyWarp) given.prefetch();
     if (threadIdx.x == 0) {
         words[1] = 0;
         for (int s = 0; s < kProductStages; ++s) {

@@ -92,6 +92,7 @@ inline void shared_store_pair_at(uint32_t at, uint32_t rank, uint2 v) {
     memcpy(model::memory(model::mapped(at, rank)), &v, 8);
 }
 inline void __threadfence() {}
+inline void prefetch_map(const CUtensorMap*) {}
 inline void fence_global_copies() {}
 inline void grid_arrive(uint32_t* counter) { ++*counter; }
 inline bool grid_wait(const uint32_t* counter, uint32_t target, volatile uint32_t* gave_up) {
