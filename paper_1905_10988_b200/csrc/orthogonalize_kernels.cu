@@ -289,7 +289,8 @@ struct OrthoJob {
     }
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
         if (kind == 0 && splits > 1) {
-            if (store_part(w, r)) store_square<true>(w, r, s);
+            uint32_t* ticket = tickets + 2 * (w.part / splits) + r.row / kProductHalf;
+            if (product_part(r, part(w, r, w.part), ticket, splits)) store_square<true>(w, r, s);
         } else if (kind < 2)
             store_square<false>(w, r, s);
         else
@@ -297,31 +298,6 @@ struct OrthoJob {
     }
     __device__ __forceinline__ float4* part(const ProductUnit& w, const ProductRead& r, uint32_t number) const {
         return parts + ((uint64_t)number * (w.width / 4) + r.column / 4) * kProductTile + r.row;
-    }
-    // A part of a sum, to memory.  Whether all parts of the block's rows are there now: the block that
-    // brings the last one adds them up, in their order.
-    __device__ __forceinline__ bool store_part(const ProductUnit& w, const ProductRead& r) const {
-        float4* to = part(w, r, w.part);
-#pragma unroll 1
-        for (int k = 0; k < r.columns; k += 32) {
-            uint32_t v[32];
-            r.load(k, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                to[(k / 4 + i) * kProductTile] =
-                    make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
-                                __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-        }
-        __threadfence();
-        product_writers_barrier();
-        if (threadIdx.x == 0) {
-            const uint32_t before = atomicAdd(tickets + 2 * (w.part / splits) + r.row / kProductHalf, 1u);
-            *r.word = (before + 1) % splits == 0;        // (every step of the launch comes round)
-        }
-        product_writers_barrier();
-        const bool last = *reinterpret_cast<volatile uint32_t*>(r.word) != 0;
-        __threadfence();
-        return last;
     }
     // A, or b A + c A A without its diagonal.  PARTS: the sums lie in parts.
     template <bool PARTS> __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
@@ -334,26 +310,8 @@ struct OrthoJob {
             load(w, r, k + 32, s);
             uint32_t v[32];
             if (PARTS) {
-                float4 all[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) all[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                const float4* p = part(w, r, w.part / splits * splits) + k / 4 * kProductTile;
-#pragma unroll 2
-                for (uint32_t j = 0; j < splits; ++j) {
-                    const float4* q = p + (uint64_t)j * (w.width / 4) * kProductTile;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 x = __ldcg(q + i * kProductTile);
-                        all[i].x += x.x; all[i].y += x.y; all[i].z += x.z; all[i].w += x.w;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[4 * i] = __float_as_uint(all[i].x);
-                    v[4 * i + 1] = __float_as_uint(all[i].y);
-                    v[4 * i + 2] = __float_as_uint(all[i].z);
-                    v[4 * i + 3] = __float_as_uint(all[i].w);
-                }
+                product_sum(part(w, r, w.part / splits * splits) + k / 4 * kProductTile,
+                            (uint64_t)(w.width / 4) * kProductTile, splits, v);
             } else {
                 r.load(k, v);
             }

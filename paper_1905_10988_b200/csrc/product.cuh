@@ -439,6 +439,58 @@ __device__ __forceinline__ void product_store(const ProductTarget& t, const Prod
         product_store_typed<__half>(t, to, c, cols, v, r);
 }
 
+// ---- sums in parts ---------------------------------------------------------------------------
+// A part of a unit's sums lies in memory as [column / 4][256 rows] groups of four columns.
+
+// The part of all threads that read the unit out, to memory (`to`: where the thread's first four columns
+// go).  Whether all `splits` parts of the block's rows are there now: the block that brings the last one
+// adds them up, in their order.  ticket: of the unit and of the block's half of the rows, 0 at first.
+__device__ __forceinline__ bool product_part(const ProductRead& r, float4* to, uint32_t* ticket,
+                                             uint32_t splits) {
+#pragma unroll 1
+    for (int c = 0; c < r.columns; c += 32) {
+        uint32_t v[32];
+        r.load(c, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            to[(c / 4 + i) * kProductTile] =
+                make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                            __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+    }
+    product_writers_barrier();
+    if (threadIdx.x == 0) {
+        __threadfence();                 // (covers what all of the block's threads wrote before)
+        const uint32_t before = atomicAdd(ticket, 1u);
+        *r.word = (before + 1) % splits == 0;            // (the same ticket may serve several times)
+        __threadfence();
+    }
+    product_writers_barrier();
+    return *reinterpret_cast<volatile uint32_t*>(r.word) != 0;
+}
+
+// 32 columns of the parts' sum; `distance`: from one part to the next, in groups
+__device__ __forceinline__ void product_sum(const float4* p, uint64_t distance, uint32_t splits,
+                                            uint32_t (&v)[32]) {
+    float4 all[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+    for (uint32_t j = 0; j < splits; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 x = __ldcg(p + j * distance + i * kProductTile);
+            all[i].x += x.x; all[i].y += x.y; all[i].z += x.z; all[i].w += x.w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[4 * i] = __float_as_uint(all[i].x);
+        v[4 * i + 1] = __float_as_uint(all[i].y);
+        v[4 * i + 2] = __float_as_uint(all[i].z);
+        v[4 * i + 3] = __float_as_uint(all[i].w);
+    }
+}
+
 // ---- the kernel ------------------------------------------------------------------------------
 //
 // Job:
@@ -539,8 +591,7 @@ product_kernel(const __grid_constant__ Job given) {
         }
         if (Job::kPhased && phase + 1 < phases) {
             fence_global_copies();
-            __threadfence();
-            product_writers_barrier();
+            product_writers_barrier();   // (the release of one thread behind it covers what all wrote)
             if (threadIdx.x == 0) grid_arrive(job.arrived);
         }
         }
