@@ -63,8 +63,12 @@ __device__ __forceinline__ int64_t ce_target(const CeGather& g, uint64_t i) {
                                : (int64_t)__ldg(static_cast<const int*>(g.targets) + i);
 }
 
-// bits of a coefficient's magnitude: ordered as the magnitudes are, NaN above all
-__device__ __forceinline__ uint32_t ce_magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// bits of a coefficient's magnitude, ordered as the magnitudes are; 0 for one that is not finite: it makes
+// its own row what it is, whatever the rows are divided by
+__device__ __forceinline__ uint32_t ce_magnitude(float v) {
+    const uint32_t bits = __float_as_uint(v) & 0x7FFFFFFFu;
+    return bits < 0x7F800000u ? bits : 0u;
+}
 
 // a row at any element to one on 16-byte boundaries, eight values a lane; what lies behind it becomes 0
 __device__ __forceinline__ void ce_copy_row(const unsigned short* from, uint64_t width, uint4* to, int lane) {
@@ -373,11 +377,9 @@ ce_join_kernel(const CeRows rows, const float2* __restrict__ parts, const uint64
 
 // ---- backward --------------------------------------------------------------------------------
 
-// the largest coefficient of any row, 1 where it is not finite, and never so small that its inverse
-// is not finite
+// the largest coefficient of any row, never so small that its inverse is not finite
 __device__ __forceinline__ float ce_largest(uint32_t bits) {
-    const float v = __uint_as_float(bits);
-    return bits >= 0x7F800000u ? 1.0f : fmaxf(v, 1e-33f);
+    return fmaxf(__uint_as_float(bits), 1e-33f);
 }
 // dz / largest in binary16 is at most this much
 template <typename T> __device__ __forceinline__ constexpr float ce_headroom() {

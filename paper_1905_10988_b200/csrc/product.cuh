@@ -417,12 +417,22 @@ __device__ __forceinline__ void product_store_typed(const ProductTarget& t, cons
         }
         return;
     }
-#pragma unroll 4
-    for (int i = 0; i < 32; ++i) {
-        T* p = reinterpret_cast<T*>(
-            __shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)to.own, i));
-        const float x = r.rows[33 * i + r.lane];
-        if (p && in) p[c + r.lane] = from_f32<T>(t.add ? to_f32<T>(p[c + r.lane]) + x : x);
+#pragma unroll 1
+    for (int at = 0; at < 32; at += 8) {
+        T* p[8];
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = reinterpret_cast<T*>(
+                __shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)to.own, at + i));
+            x[i] = r.rows[33 * (at + i) + r.lane];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!p[i] || !in) continue;
+            p[i] += c + r.lane;
+            *p[i] = from_f32<T>(t.add ? to_f32<T>(*p[i]) + x[i] : x[i]);
+        }
     }
 }
 

@@ -282,6 +282,27 @@ def test_targets_beyond_the_vocabulary_are_nan_and_no_gradient_of_zero_is():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_gradient_that_is_not_finite_leaves_the_other_rows_alone(kind, bad):
+    c = Case(40, 64, 300, kind, without=0.0)
+    _, lse = c.forward()
+    size = nc.nc_linear_cross_entropy_backward_workspace_bytes(40, 64, 300)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    dloss, got = torch.full((40,), 20.0, device="cuda"), []
+    for i in range(2):
+        dx = torch.empty(40, 64, dtype=TYPES[kind], device="cuda")
+        nc.nc_linear_cross_entropy_backward(c.x.view, CODES[kind], 40, 64, c.x.ld, c.w.view, 300, c.w.ld,
+                                            c.target, 8, c.scale, lse, dloss, None, dx, 64, None, CODES[kind],
+                                            64, False, ws, size)
+        got.append(dx)
+        dloss[3] = bad
+    keep = torch.arange(40, device="cuda") != 3
+    assert bool(got[0].isfinite().all()) and torch.equal(got[0][keep], got[1][keep])
+    assert not bool(got[1][3].isfinite().any())
+
+
+@pytest.mark.gpu
 def test_infinities_reach_their_own_rows_only():
     c = Case(50, 64, 300, "f16", without=0.0)
     c.x.view[4, 5] = float("inf")
