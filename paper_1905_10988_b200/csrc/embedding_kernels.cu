@@ -157,22 +157,24 @@ embed_forward_kernel(const __grid_constant__ EmbedTokens tokens, const T* __rest
     const float fill = token < 0 ? 0.0f : __uint_as_float(0x7FC00000u);
     const T* row = table + (in ? (uint64_t)token * ldt : 0);
     O* to = out + t * ldo;
-    float v[4][8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint64_t c = base + 256 * i + (vector ? 8 * lane : lane);
-        if (in) {
-            embed_load8<T>(row, c, cols, vector, v[i]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[i][k] *= scale;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[i][k] = fill;
-        }
-    }
+    EmbedRaw<T> raw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        embed_store8<O>(to, base + 256 * i + (vector ? 8 * lane : lane), cols, vector, false, v[i]);
+        if (in)
+            raw[i] = embed_load_raw<T>(row, base + 256 * i + (vector ? 8 * lane : lane), cols, vector);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+        if (in) {
+            embed_unpack<T>(raw[i], v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= scale;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = fill;
+        }
+        embed_store8<O>(to, base + 256 * i + (vector ? 8 * lane : lane), cols, vector, false, v);
+    }
 }
 
 // ---- backward: sorted tokens, and the rows without any ------------------------------------------
