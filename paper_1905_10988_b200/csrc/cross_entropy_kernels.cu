@@ -19,14 +19,17 @@
 // just under 1, where 16 bits are finest relative to the value, and keeps binary16 (with another
 // 2^14) clear of its subnormal numbers: a p of 2^-28 is still a normal one.
 //
-// What bounds it: the tensor cores.  2, 6 operations for every row, column and vocabulary entry.
+// What bounds it: the tensor cores and the power cap.  2 operations forward and 6 backward for every row,
+// column and vocabulary entry.  8192 x 4096 x 65536 backward: 10.4 ms back to back, 1.26 PFLOP/s (9.1 for
+// one call on a cool chip).
 #include "product.cuh"
 
 namespace natcomp {
 
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr uint32_t kCeNone = 0xFFFFFFFFu;            // a target beyond the vocabulary: the row is NaN
-constexpr uint64_t kCeDzValues = 1ull << 27;         // of a piece of dz: 256 MB
+// Of a piece of dz: 256 MB.  8192 x 2048 x 65536 backward: 5.01 ms; pieces of 64 MB 5.36, of 1 GB 5.05.
+constexpr uint64_t kCeDzValues = 1ull << 27;
 constexpr uint64_t kCeLeastPiece = 2048;             // vocabulary entries of a piece
 constexpr uint64_t kCeCopyPiece = 8192;              // of the forward pass, where the table is copied
 constexpr int kCeGatherBlocks = 592;
@@ -217,7 +220,7 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
 // a long sum are too small: by 5e-7 of their size after 1024 products, 9e-7 after 2048, twice that after
 // 4096, and the loss with them.  CHAINS: longer sums are read out every 1024 products and added up in
 // registers (128 of a thread's), rounded to nearest, while the next ones are computed; the error stays
-// that of 1024.
+// that of 1024.  6144 x 2048 x 65536: 1161 us, 1123 as one sum.
 constexpr uint32_t kCeChain = 16;                    // steps
 
 template <bool CHAINS> struct CeLogits : ProductOnce {
@@ -651,7 +654,8 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
     p.per_block = (uint32_t)((rows + kCeGatherBlocks - 1) / kCeGatherBlocks);
     if (p.per_block < 8) p.per_block = 8;
     p.blocks = (int)((rows + p.per_block - 1) / p.per_block);
-    // fewer tiles of dx than pairs: the sum over the vocabulary is split, eight steps a part at least
+    // Fewer tiles of dx than pairs: the sum over the vocabulary is split, eight steps a part at least, and a
+    // kernel adds up the parts.  515 x 1001 x 8193: 69 us instead of 95, 200 x 512 x 32768: 55 instead of 191.
     const uint64_t tiles = p.rows_pitch / kProductTile * ((width + kProductTile - 1) / kProductTile);
     const uint64_t steps = (p.piece + kProductStep - 1) / kProductStep;
     uint64_t splits = tiles ? kProductPairs / tiles : 1;

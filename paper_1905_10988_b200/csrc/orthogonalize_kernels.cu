@@ -21,6 +21,10 @@
 // 1.7e-3 of the norm instead of 2.4e-3 for random 256 x 512).  X is scaled by the power of two near
 // the root of its longer side, which brings its entries to about 1, A and the polynomial by 2^8: away
 // from binary16's subnormal numbers.
+//
+// All steps are one cooperative launch: a phase costs 3.7 us at least (64 x 64) and 90 us for 4096 x 4096,
+// where the power cap bounds it (1.1 ms for five steps, 1.3 back to back; 1.2 PFLOP/s counting half of the
+// symmetric products).
 #include "product.cuh"
 
 namespace natcomp {
@@ -28,7 +32,9 @@ namespace natcomp {
 constexpr float kOrthoGramScale = 256.0f;
 constexpr int kOrthoSteps = 16;                      // of one launch
 constexpr int kOrthoLaunches = 64;
-constexpr uint64_t kOrthoLong = 24;                  // steps of a sum that is worth splitting
+// Steps of a sum that is worth splitting.  Updates of five steps, whole and split: 512 x 1024 121 and 124 us,
+// 512 x 1536 133 and 130, 512 x 2048 148 and 133, 128 x 2048 125 and 111.
+constexpr uint64_t kOrthoLong = 24;
 constexpr float kOrthoLow = 2048.0f;                 // of the second of X's two values
 constexpr int kOrthoNormBlocks = 592;                // per matrix at most
 
