@@ -562,7 +562,8 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
  * coefficient of any row, so that in binary16 nothing of weight vanishes): that is half a step of 16
  * bits for each term of both sums, also where dtable is binary32.  The vocabulary is worked through in
  * pieces whose dz takes 256 MB, or rows * 2048 values where that is more.
- * rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256 than 2^31 (2^24 of dx),
+ * The forward workspace holds the rows that count once more, 8 bytes for every row and 256 entries, and
+ * a piece of the table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256 than 2^31 (2^24 of dx),
  * else NC_ERR_TOO_LARGE.  width or vocabulary of 0: NC_ERR_INVALID. */
 size_t nc_linear_cross_entropy_forward_workspace_bytes(size_t rows, size_t width, size_t vocabulary);
 nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows, size_t width,
@@ -588,8 +589,9 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
  * matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that holds an inf or
  * a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits: the result is
  * off by 1 to 2 thousandths of its norm with the five steps of (3.4445, -4.7750, 2.0315), also where
- * out is binary32.  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, else
- * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written. */
+ * out is binary32.  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, steps <= 1024, else
+ * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written.  The blocks of the products wait for one
+ * another (a cooperative launch): where other work holds some of the SMs, the call waits for it. */
 size_t nc_orthogonalize_workspace_bytes(size_t batch, size_t rows, size_t cols);
 nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, size_t cols,
                            size_t ldg, size_t distance, const float* coefficients, int steps, float eps,

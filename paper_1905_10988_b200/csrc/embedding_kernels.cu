@@ -66,13 +66,15 @@ template <typename T> struct EmbedRaw {
     uint32_t w[2 * sizeof(T)];
 };
 
-template <typename T>
+// (OWN: of a row that this thread writes later, so not through the cache for what no one writes)
+template <typename T, bool OWN = false>
 __device__ __forceinline__ EmbedRaw<T> embed_load_raw(const T* row, uint64_t c, uint64_t cols, bool vector) {
     EmbedRaw<T> r;
     if (vector && c + 8 <= cols) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
+            const uint4* p = reinterpret_cast<const uint4*>(row + c) + i;
+            const uint4 q = OWN ? __ldcg(p) : __ldg(p);
             r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
         }
     } else {
@@ -81,10 +83,11 @@ __device__ __forceinline__ EmbedRaw<T> embed_load_raw(const T* row, uint64_t c, 
         for (int i = 0; i < 8; ++i) {
             const bool in = c + i * step < cols;
             if constexpr (sizeof(T) == 4) {
-                r.w[i] = in ? __ldg(reinterpret_cast<const uint32_t*>(row) + c + i * step) : 0u;
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + c + i * step;
+                r.w[i] = !in ? 0u : OWN ? __ldcg(p) : __ldg(p);
             } else {
-                const uint32_t h =
-                    in ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + i * step) : 0u;
+                const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + c + i * step;
+                const uint32_t h = !in ? 0u : OWN ? __ldcg(p) : __ldg(p);
                 if (i & 1) r.w[i >> 1] |= h << 16; else r.w[i >> 1] = h;
             }
         }
@@ -104,20 +107,13 @@ __device__ __forceinline__ void embed_unpack(const EmbedRaw<T>& r, float (&v)[8]
 }
 
 template <typename T>
-__device__ __forceinline__ void embed_load8(const T* row, uint64_t c, uint64_t cols, bool vector,
-                                            float (&v)[8]) {
-    const EmbedRaw<T> r = embed_load_raw<T>(row, c, cols, vector);
-    embed_unpack<T>(r, v);
-}
-
-template <typename T>
 __device__ __forceinline__ void embed_store8(T* row, uint64_t c, uint64_t cols, bool vector, bool add,
                                              float (&v)[8]) {
     if (vector && c + 8 <= cols) {
         uint4* p = reinterpret_cast<uint4*>(row + c);
         if (add) {
             float old[8];
-            embed_load8<T>(row, c, cols, true, old);
+            embed_unpack<T>(embed_load_raw<T, true>(row, c, cols, true), old);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += old[i];
         }
@@ -569,7 +565,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
             if (i + j < end) {
                 raw[j] = embed_load_raw<T>(dy + (uint64_t)place[i + j] * s.lddy, c, s.cols, s.vector);
                 if (ADD && key[i + j + 1] != key[i + j + 2])
-                    old[j] = embed_load_raw<O>(
+                    old[j] = embed_load_raw<O, true>(
                         static_cast<const O*>(s.dtable) + (uint64_t)key[i + j + 1] * s.ldt, c, s.cols,
                         s.vector);
             }

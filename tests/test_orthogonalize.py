@@ -59,6 +59,7 @@ def test_refusals_need_no_gpu():
     for kw in (dict(rows=(1 << 20) + 1), dict(cols=1 << 21, ldg=1 << 21, ldo=1 << 21), dict(batch=65536)):
         assert status(lambda: f(**kw)) == "NC_ERR_TOO_LARGE", kw
     assert status(lambda: f(size=100)) == "NC_ERR_WORKSPACE"
+    assert status(lambda: f(co=MUON * 1025, steps=1025)) == "NC_ERR_TOO_LARGE"
     for kw in (dict(batch=0), dict(rows=0), dict(cols=0)):
         assert status(lambda: f(**kw)) == "NC_OK", kw
     with pytest.raises(ValueError):
@@ -123,6 +124,9 @@ def test_other_coefficients_and_no_steps():
     cubic = [(1.5, -0.5, 0.0)] * 9                     # converges to the orthogonal factor
     given, got = run(x, coefficients=cubic)
     assert off(got, plain(given, cubic, 1e-7, 1.0)) <= 8 * 2.0 ** -11
+    many = [(1.0, -1e-3 * i, 1e-4) for i in range(35)]  # more than one launch takes, an odd number of X
+    given, got = run(x, coefficients=many)
+    assert off(got, plain(given, [tuple(float(np.float32(v)) for v in c) for c in many], 1e-7, 1.0)) <= 8 * 2.0 ** -11
     given, got = run(x, coefficients=(), scale=3.0)
     # X is kept in two binary16 values, 22 bits
     assert off(got, plain(given, [], 1e-7, 3.0)) <= 2.0 ** -20
