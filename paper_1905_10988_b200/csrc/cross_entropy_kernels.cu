@@ -31,7 +31,9 @@ constexpr uint32_t kCeNone = 0xFFFFFFFFu;            // a target beyond the voca
 // Of a piece of dz: 256 MB.  8192 x 2048 x 65536 backward: 5.01 ms; pieces of 64 MB 5.36, of 1 GB 5.05.
 constexpr uint64_t kCeDzValues = 1ull << 27;
 constexpr uint64_t kCeLeastPiece = 2048;             // vocabulary entries of a piece
-constexpr uint64_t kCeCopyPiece = 8192;              // of the forward pass, where the table is copied
+// Of a piece of the table that the forward pass copies: 64 MB, 8192 entries of width 4096.  (64 x 101 x 71851
+// took 92 us in pieces of 8192 entries, whatever the width.)
+constexpr uint64_t kCeCopyValues = 1ull << 25;
 constexpr int kCeGatherBlocks = 592;
 
 // the rows that count, side by side
@@ -644,7 +646,8 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
     p.rows_pitch = (rows + 255) / 256 * 256;
     p.pitch = (width + 15) / 16 * 16;
     p.vocabulary_pitch = (vocabulary + 255) / 256 * 256;
-    p.piece = kCeCopyPiece;
+    p.piece = kCeCopyValues / (p.pitch ? p.pitch : 1) / 256 * 256;
+    if (p.piece < kCeLeastPiece) p.piece = kCeLeastPiece;
     if (backward) {
         p.piece = p.rows_pitch ? kCeDzValues / p.rows_pitch / 256 * 256 : 0;
         if (p.piece < kCeLeastPiece) p.piece = kCeLeastPiece;

@@ -69,8 +69,8 @@ def cross_entropy(tmp_path_factory):
 @pytest.fixture(scope="module")
 def small_pieces(tmp_path_factory):
     return build(tmp_path_factory.mktemp("ce_pieces"), "cross_entropy",
-                 dict(kProductPairs=4, kCeLeastPiece=256, kCeCopyPiece=256, kCeGatherBlocks=3, kCeChain=2),
-                 [("1ull << 27", "1ull << 8")])
+                 dict(kProductPairs=4, kCeLeastPiece=256, kCeGatherBlocks=3, kCeChain=2),
+                 [("1ull << 27", "1ull << 8"), ("1ull << 25", "1ull << 8")])
 
 
 CROSS_ENTROPY = [(1, 1, 1, "bf16", "whole", 0, "same", 0, 0), (5, 40, 33, "f16", "any", 0, "f32", 1, 1),
