@@ -17,6 +17,8 @@
 // Up to 512 tokens there is one kernel: a block for each token, of which the first of equal ones finds
 // the others by a scan and adds them up.
 // What bounds it: HBM, by the gradient that is written and the rows that are read.
+#include <type_traits>
+
 #include "act8_common.cuh"
 #include "tensor_core.cuh"
 
@@ -78,19 +80,23 @@ __device__ __forceinline__ EmbedRaw<T> embed_load_raw(const T* row, uint64_t c, 
             r.w[4 * i] = q.x; r.w[4 * i + 1] = q.y; r.w[4 * i + 2] = q.z; r.w[4 * i + 3] = q.w;
         }
     } else {
+        typedef typename std::conditional<sizeof(T) == 4, uint32_t, unsigned short>::type Word;
         const int step = vector ? 1 : 32;
+        const Word* p = reinterpret_cast<const Word*>(row) + c;
+        uint32_t w[8];
+        if (c + 7 * step < cols) {       // (all of them: loads without a question each)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool in = c + i * step < cols;
-            if constexpr (sizeof(T) == 4) {
-                const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + c + i * step;
-                r.w[i] = !in ? 0u : OWN ? __ldcg(p) : __ldg(p);
-            } else {
-                const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + c + i * step;
-                const uint32_t h = !in ? 0u : OWN ? __ldcg(p) : __ldg(p);
-                if (i & 1) r.w[i >> 1] |= h << 16; else r.w[i >> 1] = h;
+            for (int i = 0; i < 8; ++i) w[i] = OWN ? __ldcg(p + i * step) : __ldg(p + i * step);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = 0u;
+                if (c + i * step < cols) w[i] = OWN ? __ldcg(p + i * step) : __ldg(p + i * step);
             }
         }
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i)
+            r.w[i] = sizeof(T) == 4 ? w[i & 7] : w[2 * i & 7] | w[(2 * i + 1) & 7] << 16;
     }
     return r;
 }
@@ -128,12 +134,16 @@ __device__ __forceinline__ void embed_store8(T* row, uint64_t c, uint64_t cols, 
         }
     } else {
         const int step = vector ? 1 : 32;
+        T* p = row + c;
+        if (!add && c + 7 * step < cols) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i * step] = from_f32<T>(v[i]);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i * step < cols) {
-                T* p = row + c + i * step;
-                *p = from_f32<T>(add ? to_f32<T>(*p) + v[i] : v[i]);
-            }
+            if (c + i * step < cols)
+                p[i * step] = from_f32<T>(add ? to_f32<T>(p[i * step]) + v[i] : v[i]);
     }
 }
 
@@ -972,7 +982,8 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     // a block on most SMs, in clusters: not all SMs, because the chip's parts do not hold whole numbers of
     // clusters, and one that waits for another to end is late (18 clusters of 8 blocks: the last ended
     // after 25 us, the others after 13); none but the sorting one where nothing is cleared
-    const int sms = device_sm_count(), fit = p.sorters > 1 ? sms * 3 / 4 / p.sorters : sms;
+    const int sms = device_sm_count();
+    const int fit = p.sorters == 1 ? sms : (p.sorters < kSortMaxBlocks ? sms * 7 / 8 : sms * 3 / 4) / p.sorters;
     const int clusters = s.clear.end ? fit : 1;
     const int grid = (s.clear.end && clusters < 2 ? 2 : clusters) * p.sorters;
     const bool on_chip = (rows + p.sorters - 1) / p.sorters <= (uint64_t)kSortChunk;
