@@ -60,6 +60,10 @@ struct CeGather {
     void* dx;                            // of the backward pass, or nullptr
     uint64_t lddx;
     uint32_t per_block;
+    int blocks;                          // that gather; those behind them copy a piece of the table:
+    const unsigned short* piece;
+    uint64_t piece_rows, ldt;
+    unsigned short* piece_to;
     CeRows to;
 };
 
@@ -97,6 +101,13 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     after_previous();
     let_next_begin();
+    if ((int)blockIdx.x >= g.blocks) {
+        for (uint64_t r = (uint64_t)(blockIdx.x - g.blocks) * 8 + warp; r < g.piece_rows;
+             r += (uint64_t)(gridDim.x - g.blocks) * 8)
+            ce_copy_row(g.piece + r * g.ldt, g.width,
+                        reinterpret_cast<uint4*>(g.piece_to + r * g.to.pitch), lane);
+        return;
+    }
     const uint64_t first = (uint64_t)blockIdx.x * g.per_block;
     const uint64_t last = min(first + g.per_block, g.rows);
     uint32_t before = 0, all = 0, top = 0;
@@ -189,7 +200,7 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     }
     // the last step of the products over the rows reads up to 63 rows more: 0, not what stood there
     const uint64_t end = ((uint64_t)all + 63) & ~(uint64_t)63;
-    for (uint64_t r = all + blockIdx.x; r < end; r += gridDim.x) {
+    for (uint64_t r = all + blockIdx.x; r < end; r += g.blocks) {
         uint4* out = reinterpret_cast<uint4*>(static_cast<unsigned short*>(g.to.x) + r * g.to.pitch);
         for (uint32_t c = threadIdx.x; c < eights; c += 256) out[c] = make_uint4(0u, 0u, 0u, 0u);
     }
@@ -704,22 +715,26 @@ static CeRows ce_rows(const CePlan& p, char* ws) {
     return r;
 }
 
-// the piece of the table from entry `first` on as tensor copies may read it; it is copied where they
-// may not
+// The piece of the table from entry `first` on as tensor copies may read it.  It is copied where they may
+// not: the first one beside the gathering of the rows (515 x 1001 x 8193 backward: 66 us instead of 73).
 struct CeTable {
     const unsigned short* p;
     uint64_t vocabulary, width, ld, pitch;
     bool copied;
     unsigned short* copy;
     cudaStream_t stream;
+    static unsigned blocks(uint64_t rows) {
+        const uint64_t n = (rows + 7) / 8;
+        return (unsigned)(n < 1184 ? n : 1184);
+    }
     const void* piece(uint64_t first, uint64_t count, uint64_t& stride) const {
         if (!copied) {
             stride = vocabulary > 1 ? ld : pitch;
             return p + first * ld;
         }
-        const uint64_t blocks = (count + 7) / 8;
-        launch_overlapping(ce_copy_kernel, dim3((unsigned)(blocks < 1184 ? blocks : 1184)), dim3(256),
-                           0, stream, p + first * ld, count, width, ld, copy, pitch);
+        if (first)
+            launch_overlapping(ce_copy_kernel, dim3(blocks(count)), dim3(256), 0, stream, p + first * ld,
+                               count, width, ld, copy, pitch);
         stride = pitch;
         return copy;
     }
@@ -803,9 +818,16 @@ static nc_status ce_check(const void* x, int dtype, size_t rows, size_t width, s
     return NC_OK;
 }
 
-static void ce_gather(CeGather& g, const CePlan& p, cudaStream_t stream) {
+static void ce_gather(CeGather& g, const CePlan& p, const CeTable& t, uint64_t piece) {
     g.per_block = p.per_block;
-    launch_overlapping(ce_gather_kernel, dim3((unsigned)p.blocks), dim3(256), 0, stream, g);
+    g.blocks = p.blocks;
+    unsigned more = 0;
+    if (t.copied) {
+        g.piece = t.p; g.ldt = t.ld; g.piece_to = t.copy;
+        g.piece_rows = piece < t.vocabulary ? piece : t.vocabulary;
+        more = CeTable::blocks(g.piece_rows);
+    }
+    launch_overlapping(ce_gather_kernel, dim3((unsigned)p.blocks + more), dim3(256), 0, t.stream, g);
 }
 
 }  // namespace natcomp
@@ -843,10 +865,10 @@ nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows,
     g.aligned = row_access(x, ldx, 2, rows) != kRowElement;
     g.targets = targets; g.target_bytes = target_bytes; g.vocabulary = vocabulary;
     g.loss_out = loss; g.lse_out = lse; g.to = to;
-    ce_gather(g, p, stream);
     const bool copied = row_access(table, ldt, 2, vocabulary) == kRowElement;
     const CeTable t = {static_cast<const unsigned short*>(table), vocabulary, width, ldt, p.pitch,
                        copied, reinterpret_cast<unsigned short*>(ws + p.copy), stream};
+    ce_gather(g, p, t, p.piece);
     const uint64_t step = copied ? p.piece : vocabulary;
     for (uint64_t first = 0; first < vocabulary; first += step) {
         const uint64_t count = vocabulary - first < step ? vocabulary - first : step;
@@ -913,10 +935,10 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
     g.aligned = row_access(x, ldx, 2, rows) != kRowElement;
     g.targets = targets; g.target_bytes = target_bytes; g.vocabulary = vocabulary;
     g.lse = lse; g.dloss = dloss; g.dlse = dlse; g.dx = dx; g.lddx = lddx; g.to = to;
-    ce_gather(g, p, stream);
     const bool copied = row_access(table, ldt, 2, vocabulary) == kRowElement;
     const CeTable t = {static_cast<const unsigned short*>(table), vocabulary, width, ldt, p.pitch,
                        copied, reinterpret_cast<unsigned short*>(ws + p.copy), stream};
+    ce_gather(g, p, t, p.piece);
     if (bf16)
         return ce_backward(p, to, t, bf16, scale, ws, static_cast<__nv_bfloat16*>(dx), lddx, dtable,
                            dtable_dtype, lddt, accumulate != 0, rows, stream);

@@ -15,7 +15,7 @@ import torch
 import paper_1905_10988_b200 as nc
 from operator_util import CODES, HALF, TYPES, Placed, address, status, workspace
 
-MUON = (3.4445, -4.7750, 2.0315)
+QUINTIC = (3.4445, -4.7750, 2.0315)
 
 
 def plain(g, coefficients, eps, scale):
@@ -36,15 +36,15 @@ def test_the_formula_is_the_polynomial_of_the_singular_values():
         u, s, v = torch.linalg.svd(x, full_matrices=False)
         s = s / x.norm()
         for _ in range(5):
-            s = MUON[0] * s + MUON[1] * s ** 3 + MUON[2] * s ** 5
-        assert float((plain(x, [MUON] * 5, 0.0, 1.0) - u @ torch.diag(s) @ v).norm()) < 1e-12
+            s = QUINTIC[0] * s + QUINTIC[1] * s ** 3 + QUINTIC[2] * s ** 5
+        assert float((plain(x, [QUINTIC] * 5, 0.0, 1.0) - u @ torch.diag(s) @ v).norm()) < 1e-12
         assert 0.3 < float(s.min()) and float(s.max()) < 1.3
 
 
 def test_refusals_need_no_gpu():
     keep, A = address()
 
-    def f(g=A, dtype=nc.DTYPE_F32, batch=1, rows=8, cols=8, ldg=8, dist=64, co=MUON, steps=1, eps=1e-7, out=A,
+    def f(g=A, dtype=nc.DTYPE_F32, batch=1, rows=8, cols=8, ldg=8, dist=64, co=QUINTIC, steps=1, eps=1e-7, out=A,
           ot=nc.DTYPE_BF16, ldo=8, od=64, ws=A, size=1 << 20):
         return nc.nc_orthogonalize(g, dtype, batch, rows, cols, ldg, dist, co, steps, eps, 1.0, out, ot, ldo,
                                    od, ws, size, stream=0)
@@ -59,7 +59,7 @@ def test_refusals_need_no_gpu():
     for kw in (dict(rows=(1 << 20) + 1), dict(cols=1 << 21, ldg=1 << 21, ldo=1 << 21), dict(batch=65536)):
         assert status(lambda: f(**kw)) == "NC_ERR_TOO_LARGE", kw
     assert status(lambda: f(size=100)) == "NC_ERR_WORKSPACE"
-    assert status(lambda: f(co=MUON * 1025, steps=1025)) == "NC_ERR_TOO_LARGE"
+    assert status(lambda: f(co=QUINTIC * 1025, steps=1025)) == "NC_ERR_TOO_LARGE"
     for kw in (dict(batch=0), dict(rows=0), dict(cols=0)):
         assert status(lambda: f(**kw)) == "NC_OK", kw
     with pytest.raises(ValueError):
@@ -67,7 +67,7 @@ def test_refusals_need_no_gpu():
     assert nc.nc_orthogonalize_workspace_bytes(1, 1 << 21, 8) == 0
 
 
-def run(x, out="f32", coefficients=(MUON,) * 5, eps=1e-7, scale=1.0, layout="whole", kind="f32"):
+def run(x, out="f32", coefficients=(QUINTIC,) * 5, eps=1e-7, scale=1.0, layout="whole", kind="f32"):
     batch, rows, cols = x.shape
     g, o = Placed(x.shape, kind, layout, x), Placed(x.shape, out, layout)
     size = nc.nc_orthogonalize_workspace_bytes(batch, rows, cols)
@@ -97,7 +97,7 @@ def test_update(batch, rows, cols):
                               ("f32", "f32", "any"), ("f32", "f16", "gap")):
         x = 1e-3 * torch.randn(batch, rows, cols, generator=g, device="cuda")
         given, got = run(x, out, layout=layout, kind=kind, scale=1.5)
-        want = plain(given, [tuple(float(np.float32(v)) for v in MUON)] * 5, 1e-7, 1.5)
+        want = plain(given, [tuple(float(np.float32(v)) for v in QUINTIC)] * 5, 1e-7, 1.5)
         assert off(got, want) <= 8 * 2.0 ** -11 + HALF[out], (kind, out, layout)
 
 
@@ -106,7 +106,7 @@ def test_update(batch, rows, cols):
 def test_any_size_of_the_gradient(size):
     x = size * torch.randn(1, 60, 90, device="cuda")
     given, got = run(x, eps=0.0)
-    assert off(got, plain(given, [MUON] * 5, 0.0, 1.0)) <= 8 * 2.0 ** -11
+    assert off(got, plain(given, [QUINTIC] * 5, 0.0, 1.0)) <= 8 * 2.0 ** -11
 
 
 @pytest.mark.gpu
@@ -115,7 +115,7 @@ def test_low_rank_gradients():
     for rows, cols in ((500, 700), (700, 500)):
         x = torch.randn(1, rows, 8, generator=g, device="cuda") @ torch.randn(1, 8, cols, generator=g, device="cuda")
         given, got = run(x)
-        assert off(got, plain(given, [MUON] * 5, 1e-7, 1.0)) <= 8 * 2.0 ** -11
+        assert off(got, plain(given, [QUINTIC] * 5, 1e-7, 1.0)) <= 8 * 2.0 ** -11
 
 
 @pytest.mark.gpu
@@ -151,7 +151,7 @@ def test_the_same_bits_captured_and_on_two_streams():
     m = 300 * 600
 
     def call(out, ws):
-        nc.nc_orthogonalize(x, nc.DTYPE_F32, 2, 300, 600, 600, m, MUON * 5, 5, 1e-7, 1.0, out, nc.DTYPE_BF16,
+        nc.nc_orthogonalize(x, nc.DTYPE_F32, 2, 300, 600, 600, m, QUINTIC * 5, 5, 1e-7, 1.0, out, nc.DTYPE_BF16,
                             600, m, ws, size)
 
     sets = [(torch.empty(2, 300, 600, dtype=torch.bfloat16, device="cuda"),
