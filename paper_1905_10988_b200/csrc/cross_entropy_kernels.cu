@@ -14,7 +14,7 @@
 // first, side by side.  So a NaN in a row that does not count reaches nothing, a batch that is half
 // padding costs half, and rows of any alignment become ones that tensor copies take.
 //
-// dz is divided by the largest coefficient of any row before it is rounded to 16 bits and the products
+// dz is divided by about the largest coefficient of any row before it is rounded to 16 bits and the products
 // are multiplied by it again.  That puts the entries of the targets, 1 - p times their coefficient,
 // just under 1, where 16 bits are finest relative to the value, and keeps binary16 (with another
 // 2^14) clear of its subnormal numbers: a p of 2^-28 is still a normal one.
@@ -43,7 +43,8 @@ struct CeRows {
     uint32_t* target;                    // kCeNone: beyond the vocabulary
     float *lse, *dloss, *both;           // both: dloss + dlse
     float* hit;                          // logit of the target (forward)
-    uint32_t* most;                      // largest coefficient's bits of each gathering block
+    uint2* most;                         // of each gathering block, bits of the largest dloss and of the
+                                         // largest of the others
     void* x;                             // pitch values a row
     uint64_t pitch;
 };
@@ -97,7 +98,7 @@ __device__ __forceinline__ void ce_copy_row(const unsigned short* from, uint64_t
 __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ CeGather g) {
     __shared__ uint32_t sums[8][2];
     __shared__ uint32_t place[256];
-    __shared__ uint32_t most[8];
+    __shared__ uint2 most[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     after_previous();
     let_next_begin();
@@ -110,7 +111,8 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     }
     const uint64_t first = (uint64_t)blockIdx.x * g.per_block;
     const uint64_t last = min(first + g.per_block, g.rows);
-    uint32_t before = 0, all = 0, top = 0;
+    uint32_t before = 0, all = 0;
+    uint2 top = make_uint2(0u, 0u);      // of dloss, of the others
     // (every block begins at another place, or all of them ask the same parts of L2 at a time)
     for (uint64_t i = threadIdx.x; i < g.rows; i += 8 * 256) {
 #pragma unroll
@@ -167,7 +169,8 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
                 g.to.lse[at] = g.lse[i];
                 g.to.dloss[at] = dl;
                 g.to.both[at] = both;
-                top = max(top, max(ce_magnitude(dl), max(ce_magnitude(ds), ce_magnitude(both))));
+                top.x = max(top.x, ce_magnitude(dl));
+                top.y = max(top.y, max(ce_magnitude(ds), ce_magnitude(both)));
             } else {
                 g.to.hit[at] = __uint_as_float(0x7FC00000u);
             }
@@ -206,11 +209,17 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const __grid_constant__ 
     }
     if (g.dloss) {
 #pragma unroll
-        for (int d = 16; d; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        for (int d = 16; d; d >>= 1) {
+            top.x = max(top.x, __shfl_xor_sync(0xFFFFFFFFu, top.x, d));
+            top.y = max(top.y, __shfl_xor_sync(0xFFFFFFFFu, top.y, d));
+        }
         if (lane == 0) most[warp] = top;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < 8; ++w) top = max(top, most[w]);
+            for (int w = 1; w < 8; ++w) {
+                top.x = max(top.x, most[w].x);
+                top.y = max(top.y, most[w].y);
+            }
             g.to.most[blockIdx.x] = top;
         }
     }
@@ -393,11 +402,18 @@ ce_join_kernel(const CeRows rows, const float2* __restrict__ parts, const uint64
 
 // ---- backward --------------------------------------------------------------------------------
 
+// What the rows are divided by: the largest dloss, unless the other coefficients reach more than twice as
+// far.  (With the same dloss for all rows the entries of targets of small p become -1, which is exact, also
+// where a small dlse makes p's coefficient a little larger.)
+__device__ __forceinline__ uint32_t ce_chosen(uint32_t hot, uint32_t others) {
+    return __uint_as_float(others) > 2.0f * __uint_as_float(hot) ? others : hot;
+}
+
 // the largest coefficient of any row, never so small that its inverse is not finite
 __device__ __forceinline__ float ce_largest(uint32_t bits) {
     return fmaxf(__uint_as_float(bits), 1e-33f);
 }
-// dz / largest in binary16 is at most this much
+// dz / largest in binary16 is at most twice this much
 template <typename T> __device__ __forceinline__ constexpr float ce_headroom() {
     return sizeof(T) && std::is_same<T, __half>::value ? 16384.0f : 1.0f;
 }
@@ -417,10 +433,18 @@ template <typename T> struct CeDz : ProductOnce {
     __device__ __forceinline__ uint32_t begin(uint32_t, bool reads_out) {
         count = __ldcg(rows.count);
         if (reads_out) {
-            uint32_t top = 0;
-            for (int i = threadIdx.x & 31; i < blocks; i += 32) top = max(top, __ldcg(rows.most + i));
+            uint32_t hot = 0, others = 0;
+            for (int i = threadIdx.x & 31; i < blocks; i += 32) {
+                const uint2 m = __ldcg(rows.most + i);
+                hot = max(hot, m.x);
+                others = max(others, m.y);
+            }
 #pragma unroll
-            for (int d = 16; d; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            for (int d = 16; d; d >>= 1) {
+                hot = max(hot, __shfl_xor_sync(0xFFFFFFFFu, hot, d));
+                others = max(others, __shfl_xor_sync(0xFFFFFFFFu, others, d));
+            }
+            const uint32_t top = ce_chosen(hot, others);
             if (blockIdx.x == 0 && threadIdx.x == 0) rows.count[1] = top;
             inverse = ce_headroom<T>() / ce_largest(top);
         }
@@ -685,7 +709,7 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
         p.lse = ce_place(at, 4 * p.rows_pitch);
         p.dloss = ce_place(at, 4 * p.rows_pitch);
         p.both = ce_place(at, 4 * p.rows_pitch);
-        p.most = ce_place(at, 4 * (size_t)(p.blocks + 1));
+        p.most = ce_place(at, 8 * (size_t)(p.blocks + 1));
         p.dz = ce_place(at, 2 * p.rows_pitch * p.piece);
         if (p.splits > 1 || p.piece < p.vocabulary_pitch)
             p.sums = ce_place(at, 4 * p.splits * p.rows_pitch * ((width + 31) / 32 * 32));
@@ -709,7 +733,7 @@ static CeRows ce_rows(const CePlan& p, char* ws) {
     r.dloss = reinterpret_cast<float*>(ws + p.dloss);
     r.both = reinterpret_cast<float*>(ws + p.both);
     r.hit = reinterpret_cast<float*>(ws + p.hit);
-    r.most = reinterpret_cast<uint32_t*>(ws + p.most);
+    r.most = reinterpret_cast<uint2*>(ws + p.most);
     r.x = ws + p.x;
     r.pitch = p.pitch;
     return r;
