@@ -563,8 +563,8 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
  * bits for each term of both sums, also where dtable is binary32.  The vocabulary is worked through in
  * pieces whose dz takes 256 MB, or rows * 2048 values where that is more.
  * The forward workspace holds the rows that count once more, 8 bytes for every row and 256 entries, and
- * a piece of the table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256 than 2^31 (2^24 of dx),
- * else NC_ERR_TOO_LARGE.  width or vocabulary of 0: NC_ERR_INVALID. */
+ * a piece of the table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256
+ * than 2^31 (2^24 of dx), else NC_ERR_TOO_LARGE.  width or vocabulary of 0: NC_ERR_INVALID. */
 size_t nc_linear_cross_entropy_forward_workspace_bytes(size_t rows, size_t width, size_t vocabulary);
 nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows, size_t width,
                                           size_t ldx, const void* table, size_t vocabulary, size_t ldt,

@@ -306,7 +306,8 @@ struct OrthoJob {
         return parts + ((uint64_t)number * (w.width / 4) + r.column / 4) * kProductTile + r.row;
     }
     // A, or b A + c A A without its diagonal.  PARTS: the sums lie in parts.
-    template <bool PARTS> __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
+    template <bool PARTS>
+    __device__ __forceinline__ void store_square(const ProductUnit& w, const ProductRead& r, State& s) const {
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const bool polynomial = kind == 1;
         __half* to = (polynomial ? poly : gram) + ((uint64_t)w.z * side + row) * side_pitch + col;

@@ -7,9 +7,9 @@
 // and above the diagonal exist: a block below it is read from its mirror image with the other layout,
 // which the matrix instruction takes as it is, so nothing is ever transposed.
 //
-// What bounds it: at full clock the path from L2 to an SM (a step of 512 cycles brings 32 KB, 64 bytes a
-// cycle) with the tensor pipe active 87 to 91 % of the cycles for 4096 and more k; over a longer time the power
-// cap.  8192 x 16384 x 4096: 720 to 750 us a product, 1.47 to 1.53 PFLOP/s.
+// What bounds it: at full clock the path from L2 to an SM (a step of 512 cycles brings 32 KB, 64 bytes
+// a cycle), with the tensor pipe active 87 to 91 % of the cycles for 4096 and more k; over a longer time
+// the power cap.  8192 x 16384 x 4096: 720 to 750 us a product, 1.47 to 1.53 PFLOP/s.
 //
 // A pair of blocks (cta_group::2) computes tiles of 256 x 256 one after another, block r of it the
 // rows from 128 r on; it brings 128 rows of either operand for every step of 64 k.  Tiles that do not fill
@@ -192,7 +192,8 @@ inline bool make_box_map(CUtensorMap* map, const void* p, bool bf16, uint64_t co
             return false;
         encode = (Encode)f;
     }
-    const cuuint64_t dims[3] = {cols, rows, count}, strides[2] = {2 * ld, 2 * (count > 1 ? distance : rows * ld)};
+    const cuuint64_t dims[3] = {cols, rows, count};
+    const cuuint64_t strides[2] = {2 * ld, 2 * (count > 1 ? distance : rows * ld)};
     const cuuint32_t box[3] = {64, 64, 1}, steps[3] = {1, 1, 1};
     return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                   const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -213,8 +214,8 @@ struct ProductUnit {
 
 // Tiles from `whole` on come in `parts` pieces of 256 / parts columns each.  A round of tiles that leaves
 // half of the pairs idle takes about half the time in halves, although the left operand is read once more.
-// Updates of five steps: 512 x 512 157 us instead of 225, 1024 x 1024 217 instead of 270, 4096 x 4096 (256 tiles
-// for 74 pairs) 1321 instead of 1406.
+// Updates of five steps: 512 x 512 157 us instead of 225, 1024 x 1024 217 instead of 270, 4096 x 4096
+// (256 tiles for 74 pairs) 1321 instead of 1406.
 struct ProductSplit {
     uint32_t whole, parts;
     __host__ __device__ __forceinline__ uint32_t units(uint32_t tiles) const {
@@ -582,67 +583,70 @@ product_kernel(const __grid_constant__ Job given) {
         uint32_t turn = 0;
         typename Job::State state;
         for (uint32_t phase = 0; phase < phases; ++phase) {
-        if (Job::kPhased && phase) {     // every block is done with the phase before
-            if (threadIdx.x == 0) grid_wait(job.arrived, phase * gridDim.x, gave_up);
-            product_writers_barrier();
-        }
-        const uint32_t units = job.begin(phase, true);
-        for (uint32_t u = pair, chain = 0; u < units; product_next(job, u, chain, pairs), ++turn) {
-            const ProductUnit w = job.unit_of(u, chain);
-            const uint32_t b = turn & 1;
-            r.columns = w.width / 2;
-            r.column = r.columns * r.half;
-            job.ahead(w, r, state);
-            const bool ok = mbar_wait(full + 8 * b, (turn >> 1) & 1, gave_up);
-            r.ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
-            r.nothing = w.steps == 0;
-            tc_fence_after();
-            r.tmem = tmem + b * kProductTile + r.column + ((uint32_t)(32 * r.quarter) << 16);
-            job.store(w, r, state);
-            tc_fence_before();
-            __syncwarp();
-            // (a tile that was not waited for was not read: the other block may still be reading it)
-            if (lane == 0 && r.ok) mbar_arrive_at(drained + 8 * b, 0);
-        }
-        if (Job::kPhased && phase + 1 < phases) {
-            fence_global_copies();
-            product_writers_barrier();   // (the release of one thread behind it covers what all wrote)
-            if (threadIdx.x == 0) grid_arrive(job.arrived);
-        }
+            if (Job::kPhased && phase) {     // every block is done with the phase before
+                if (threadIdx.x == 0) grid_wait(job.arrived, phase * gridDim.x, gave_up);
+                product_writers_barrier();
+            }
+            const uint32_t units = job.begin(phase, true);
+            for (uint32_t u = pair, chain = 0; u < units; product_next(job, u, chain, pairs), ++turn) {
+                const ProductUnit w = job.unit_of(u, chain);
+                const uint32_t b = turn & 1;
+                r.columns = w.width / 2;
+                r.column = r.columns * r.half;
+                job.ahead(w, r, state);
+                const bool ok = mbar_wait(full + 8 * b, (turn >> 1) & 1, gave_up);
+                r.ok = __all_sync(0xFFFFFFFFu, ok && !*gave_up);
+                r.nothing = w.steps == 0;
+                tc_fence_after();
+                r.tmem = tmem + b * kProductTile + r.column + ((uint32_t)(32 * r.quarter) << 16);
+                job.store(w, r, state);
+                tc_fence_before();
+                __syncwarp();
+                // (a tile that was not waited for was not read: the other block may still be reading it)
+                if (lane == 0 && r.ok) mbar_arrive_at(drained + 8 * b, 0);
+            }
+            if (Job::kPhased && phase + 1 < phases) {
+                fence_global_copies();
+                product_writers_barrier();       // (one thread's release behind it covers what all wrote)
+                if (threadIdx.x == 0) grid_arrive(job.arrived);
+            }
         }
     } else if (warp == kProductCopyWarp) {
         if (lane == 0) {
             uint32_t step = 0, stage = 0, parity = 0;
             bool ok = true;
             for (uint32_t phase = 0; phase < phases && ok; ++phase) {
-            if (Job::kPhased && phase) {
-                ok = grid_wait(job.arrived, phase * gridDim.x, gave_up);
-                fence_global_copies();
-            }
-            const uint32_t units = job.begin(phase, false);
-            const CUtensorMap *left = job.left_map(), *right = job.right_map();
-            for (uint32_t u = pair, chain = 0; u < units && ok; product_next(job, u, chain, pairs)) {
-                const ProductUnit w = job.unit_of(u, chain);
-                const int m = w.m + (int)rank * kProductHalf, n = w.n + (int)rank * (w.width / 2);
-                const bool second = w.width == kProductTile;     // a second box of the right operand
-                for (int s = 0; s < w.steps; ++s, ++step) {
-                    if (step >= kProductStages) ok = mbar_wait(empty + 8 * stage, parity ^ 1, gave_up);
-                    if (!ok) break;
-                    const int k = w.k + s * kProductStep;
-                    const uint32_t bar = filled + 8 * stage, to = stages + stage * kProductStage;
-                    if (rank == 0) mbar_expect(bar, 2 * (kProductStage - (second ? 0 : kProductBox)));
-                    const bool a = job.left_side.by_lines(m, k), b = job.right_side.by_lines(n, k);
-                    for (int h = 0; h < 2; ++h) {
-                        tma_load_pair(to + h * kProductBox, left, a ? m + 64 * h : k,
-                                      a ? k : m + 64 * h, w.z, bar);
-                        if (h == 0 || second)
-                            tma_load_pair(to + kProductOperand + h * kProductBox, right,
-                                          b ? n + 64 * h : k, b ? k : n + 64 * h, w.z, bar);
-                    }
-                    stage = stage + 1 == kProductStages ? 0 : stage + 1;
-                    parity ^= stage == 0;
+                if (Job::kPhased && phase) {
+                    ok = grid_wait(job.arrived, phase * gridDim.x, gave_up);
+                    fence_global_copies();
                 }
-            }
+                const uint32_t units = job.begin(phase, false);
+                const CUtensorMap *left = job.left_map(), *right = job.right_map();
+                for (uint32_t u = pair, chain = 0; u < units && ok; product_next(job, u, chain, pairs)) {
+                    const ProductUnit w = job.unit_of(u, chain);
+                    const int m = w.m + (int)rank * kProductHalf;
+                    const int n = w.n + (int)rank * (w.width / 2);
+                    const bool second = w.width == kProductTile;     // box of the right operand
+                    for (int s = 0; s < w.steps; ++s, ++step) {
+                        if (step >= kProductStages) ok = mbar_wait(empty + 8 * stage, parity ^ 1, gave_up);
+                        if (!ok) break;
+                        const int k = w.k + s * kProductStep;
+                        const uint32_t bar = filled + 8 * stage, to = stages + stage * kProductStage;
+                        if (rank == 0)
+                            mbar_expect(bar, 2 * (kProductStage - (second ? 0 : kProductBox)));
+                        const bool a = job.left_side.by_lines(m, k);
+                        const bool b = job.right_side.by_lines(n, k);
+                        for (int h = 0; h < 2; ++h) {
+                            tma_load_pair(to + h * kProductBox, left, a ? m + 64 * h : k,
+                                          a ? k : m + 64 * h, w.z, bar);
+                            if (h == 0 || second)
+                                tma_load_pair(to + kProductOperand + h * kProductBox, right,
+                                              b ? n + 64 * h : k, b ? k : n + 64 * h, w.z, bar);
+                        }
+                        stage = stage + 1 == kProductStages ? 0 : stage + 1;
+                        parity ^= stage == 0;
+                    }
+                }
             }
             // both blocks' copies in flight land before the pair ends
             if (rank == 0) {
@@ -659,43 +663,44 @@ product_kernel(const __grid_constant__ Job given) {
         bool ok = true;
         uint32_t stage = 0, parity = 0, turn = 0;
         for (uint32_t phase = 0; phase < phases && ok; ++phase) {
-        const uint32_t units = job.begin(phase, false);
-        for (uint32_t u = pair, chain = 0; u < units && ok;
-             product_next(job, u, chain, pairs), ++turn) {
-            const ProductUnit w = job.unit_of(u, chain);
-            const uint32_t b = turn & 1, to = tmem + b * kProductTile;
-            const uint32_t plain = mma_shape_of(kProductTile, w.width, job.bf16, false, false);
-            ok = mbar_wait(drained + 8 * b, ((turn >> 1) & 1) ^ 1, gave_up);
-            for (int s = 0; s < w.steps; ++s) {
-                if (ok) ok = mbar_wait(filled + 8 * stage, parity, gave_up);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                const int k = w.k + s * kProductStep;
-                const bool a = job.left_side.by_lines(w.m, k), c = job.right_side.by_lines(w.n, k);
-                const uint32_t shape = plain | (uint32_t)a << 15 | (uint32_t)c << 16;
-                // 16 k further on: 16 lines, or 32 bytes of each line
-                const uint32_t da = a ? 128 : 2, dc = c ? 128 : 2;
-                const uint64_t left = operand + stage * (kProductStage / 16);
-                const uint64_t right = left + kProductOperand / 16;
+            const uint32_t units = job.begin(phase, false);
+            for (uint32_t u = pair, chain = 0; u < units && ok;
+                 product_next(job, u, chain, pairs), ++turn) {
+                const ProductUnit w = job.unit_of(u, chain);
+                const uint32_t b = turn & 1, to = tmem + b * kProductTile;
+                const uint32_t plain = mma_shape_of(kProductTile, w.width, job.bf16, false, false);
+                ok = mbar_wait(drained + 8 * b, ((turn >> 1) & 1) ^ 1, gave_up);
+                for (int s = 0; s < w.steps; ++s) {
+                    if (ok) ok = mbar_wait(filled + 8 * stage, parity, gave_up);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int k = w.k + s * kProductStep;
+                    const bool a = job.left_side.by_lines(w.m, k);
+                    const bool c = job.right_side.by_lines(w.n, k);
+                    const uint32_t shape = plain | (uint32_t)a << 15 | (uint32_t)c << 16;
+                    // 16 k further on: 16 lines, or 32 bytes of each line
+                    const uint32_t da = a ? 128 : 2, dc = c ? 128 : 2;
+                    const uint64_t left = operand + stage * (kProductStage / 16);
+                    const uint64_t right = left + kProductOperand / 16;
 #pragma unroll
-                for (int i = 0; i < kProductStep / 16; ++i)
-                    mma_pair(to, left + i * da, right + i * dc, shape, s > 0 || i > 0, elected);
-                mma_commit_pair(empty + 8 * stage, elected);
-                stage = stage + 1 == kProductStages ? 0 : stage + 1;
-                parity ^= stage == 0;
+                    for (int i = 0; i < kProductStep / 16; ++i)
+                        mma_pair(to, left + i * da, right + i * dc, shape, s > 0 || i > 0, elected);
+                    mma_commit_pair(empty + 8 * stage, elected);
+                    stage = stage + 1 == kProductStages ? 0 : stage + 1;
+                    parity ^= stage == 0;
+                }
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                // given up: both blocks know before their writers hear that the tile is complete, for what
+                // stands in TMEM is the sum of some of the steps
+                if (!ok && elected) {
+                    shared_store_at(smem_u32(words + 1), 0, 1);
+                    shared_store_at(smem_u32(words + 1), 1, 1);
+                    fence_cluster();
+                }
+                __syncwarp();
+                mma_commit_pair(full + 8 * b, elected);
             }
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            // given up: both blocks know before their writers hear that the tile is complete, for what
-            // stands in TMEM is the sum of some of the steps
-            if (!ok && elected) {
-                shared_store_at(smem_u32(words + 1), 0, 1);
-                shared_store_at(smem_u32(words + 1), 1, 1);
-                fence_cluster();
-            }
-            __syncwarp();
-            mma_commit_pair(full + 8 * b, elected);
-        }
         }
     }
     // the pair stays until both blocks are done with each other's barriers and with TMEM
