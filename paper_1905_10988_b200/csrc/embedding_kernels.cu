@@ -42,7 +42,9 @@ constexpr int kDirectThreads = 512;
 // What is cleared beside the sort.  The blocks that do have scanned the tokens 7 to 8 us before the sort ends
 // (4096 tokens: after 4 of 11 us, 16384: after 7 of 15) and clear about 9 MB a microsecond.
 constexpr uint64_t kClearBeside = 64 << 20;
-constexpr uint64_t kClearBlock = 96 << 10;    // bytes that a block clears beside the sums
+// Bytes that a block clears beside the sums.  16384 x 4096 into 65536 rows, 4096 x 2048 into 32768, 8191 x 1001
+// into 32001: 140, 40, 52 us; 24 KB 144, 41, 55; 400 KB 140, 49, 57.
+constexpr uint64_t kClearBlock = 96 << 10;
 // Cuts of a run that one warp joins.  30000 x 768 binary32 of one token: 179 us; left to one warp whatever the
 // number 252, all runs by eight warps 196.
 constexpr int kJoinShort = 12;
@@ -508,15 +510,6 @@ __device__ __forceinline__ bool embed_cut(const EmbedSum& s, uint32_t g, uint32_
     return (a == b) & (b == c);          // (three loads at a time)
 }
 
-// Blocks that clear lie evenly between those that work: `number` of this one among its kind
-__device__ __forceinline__ bool embed_clears(uint32_t works, uint32_t& number) {
-    const uint32_t clears = gridDim.x - works;
-    const uint32_t before = (uint32_t)((uint64_t)blockIdx.x * clears / gridDim.x);
-    const bool clear = (uint64_t)(blockIdx.x + 1) * clears / gridDim.x > before;
-    number = clear ? before : blockIdx.x - before;
-    return clear;
-}
-
 template <typename T, typename O, bool ADD>
 __global__ void __launch_bounds__(kSumThreads, ADD ? 5 : 8) embed_sum_kernel(const __grid_constant__ EmbedSum s) {
     // of a block's groups of threads, each with a segment of its own: key and place of up to twice as many
@@ -526,10 +519,9 @@ __global__ void __launch_bounds__(kSumThreads, ADD ? 5 : 8) embed_sum_kernel(con
     after_previous();
     let_next_begin();
     const uint32_t n = embed_valid(s), groups = kSumThreads / s.across;
-    uint32_t number;
-    const uint32_t works = (s.segments + groups - 1) / groups;
-    if (embed_clears(works, number)) {
-        embed_clear(s.clear, flags, number * gridDim.y + blockIdx.y,
+    const uint32_t works = (s.segments + groups - 1) / groups, number = blockIdx.x;
+    if (number >= works) {               // (last: evenly between the others they took 1 to 3 us longer)
+        embed_clear(s.clear, flags, (number - works) * gridDim.y + blockIdx.y,
                     (gridDim.x - works) * gridDim.y, s.items, n);
         return;
     }
