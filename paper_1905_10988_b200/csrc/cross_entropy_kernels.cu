@@ -289,9 +289,9 @@ template <bool CHAINS> struct CeLogits : ProductOnce {
         w.n += (int)(u % split) * w.width;
         w.steps = (int)steps;
         if (CHAINS) {
-            const uint32_t from = steps * chain / parts_of;
+            const uint32_t from = (uint32_t)((uint64_t)steps * chain / parts_of);
             w.k = (int)from * kProductStep;
-            w.steps = (int)(steps * (chain + 1) / parts_of - from);
+            w.steps = (int)((uint32_t)((uint64_t)steps * (chain + 1) / parts_of) - from);
             w.part = chain;
         }
         return w;

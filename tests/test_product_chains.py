@@ -1,0 +1,88 @@
+"""How the sums of a product are cut into chains: on the host, the jobs' own text."""
+import os
+import re
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+MODEL = os.path.join(HERE, "device_model")
+sys.path.insert(0, MODEL)
+
+import translate  # noqa: E402
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="no C++ compiler")
+
+MAIN = r"""
+using namespace natcomp;
+
+// the chains of a unit follow each other from the first step to the last, none is empty or longer than
+// most, and every one begins where its columns of k do
+template <typename Job> static int check(const Job& job, uint32_t steps, uint32_t chains, uint32_t most) {
+    int64_t at = 0;
+    for (uint32_t c = 0; c < chains; ++c) {
+        const ProductUnit w = job.unit_of(0, c);
+        if (w.steps <= 0 || w.steps > (int)most || w.k != at * kProductStep || w.part != c) {
+            printf("chain %u of %u: k %d, steps %d, part %u; should begin at step %lld\n", c, chains, w.k,
+                   w.steps, w.part, (long long)at);
+            return 1;
+        }
+        at += w.steps;
+    }
+    if (at != steps) { printf("%lld of %u steps\n", (long long)at, steps); return 1; }
+    return 0;
+}
+
+int main(int argc, char** argv) {
+    const std::string name = argv[1];
+    const uint32_t steps = (uint32_t)atoll(argv[2]);
+    int bad = 2;
+    if (name == "logits") {
+        CeLogits<true> a = {};
+        a.steps = steps; a.parts_of = (steps + kCeChain - 1) / kCeChain;
+        a.tiles_n = 1; a.split = 1; a.count = 1;
+        bad = check(a, steps, a.chains(), kCeChain);
+    }
+    if (!bad) printf("ok\n");
+    return bad;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    with open(os.path.join(MODEL, "product.hpp")) as f:
+        model = f.read()
+
+    def change(file, text):
+        if file != "product.cuh":
+            return text
+        text = translate._without(text, ["make_box_map", "mma_shape_of", "launch_together", "grid_wait"])
+        cut = [(b, e) for b, e, n, body in translate._functions(text)
+               if re.search(r"\basm\b", body) and n not in ("product_pair_barrier", "product_writers_barrier")]
+        for b, e in reversed(cut):
+            text = text[:b] + text[e:]
+        return model + text.replace("mma_pair(", "product_mma(")
+
+    folder = tmp_path_factory.mktemp("chains")
+    source, out = str(folder / "chains.cpp"), str(folder / "chains")
+    with open(source, "w") as f:
+        f.write(translate.translate(["product.cuh", "cross_entropy_kernels.cu"], None, change) + MAIN)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.run(["g++", "-std=c++20", "-O1", "-w", "-ffp-contract=off", "-fsanitize=address", "-I" + MODEL,
+                    "-I" + os.path.join(translate.ROOT, "include"), "-I" + os.path.join(cuda, "include"),
+                    "-o", out, source], check=True)
+    return out
+
+
+def chains(program, *args):
+    got = subprocess.run([program] + [str(a) for a in args], capture_output=True, text=True, timeout=120)
+    assert got.returncode == 0 and got.stdout.startswith("ok"), got.stdout + got.stderr[-2000:]
+
+
+# 2^18 steps are a width of 2^24; the widest layer has 2^25 - 4
+@pytest.mark.parametrize("steps", [17, 33, 1000, (1 << 18) - 1, 1 << 18, (1 << 18) + 1, 1 << 19, (1 << 25) - 4])
+def test_the_logits_chains_cover_every_step_once(program, steps):
+    chains(program, "logits", steps)
