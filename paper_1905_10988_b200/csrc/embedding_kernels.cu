@@ -806,10 +806,11 @@ struct EmbedPlan {
     size_t items[2], counts, valid, parts, bytes;
 };
 
-// threads that share a slab of columns: whole warps, because spread columns need them
+// threads that share a slab of columns: whole warps, because spread columns need them; one at least, also
+// where there are no columns
 static uint32_t embed_across(uint64_t cols) {
     const uint64_t eights = (cols + 7) / 8;
-    return eights >= kSumThreads ? kSumThreads : (uint32_t)(eights + 31) / 32 * 32;
+    return eights >= kSumThreads ? kSumThreads : eights ? (uint32_t)(eights + 31) / 32 * 32 : 32;
 }
 
 static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
