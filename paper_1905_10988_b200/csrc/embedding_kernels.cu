@@ -813,6 +813,12 @@ static uint32_t embed_across(uint64_t cols) {
     return eights >= kSumThreads ? kSumThreads : eights ? (uint32_t)(eights + 31) / 32 * 32 : 32;
 }
 
+// (columns: a grid has 65535 blocks of 256 in its second dimension)
+static bool embed_fits(size_t rows, size_t vocabulary, size_t cols) {
+    const size_t most = (size_t)1 << 31;
+    return rows < most && vocabulary < most && cols < (size_t)256 * 65535;
+}
+
 static EmbedPlan embed_plan(uint64_t rows, uint64_t vocabulary, uint64_t cols) {
     EmbedPlan p = {};
     p.sorters = 1;
@@ -927,9 +933,7 @@ nc_status nc_embedding_forward(const void* tokens, int token_bytes, size_t rows,
 }
 
 size_t nc_embedding_backward_workspace_bytes(size_t rows, size_t vocabulary, size_t cols) {
-    const size_t most = (size_t)1 << 31;
-    if (rows >= most || cols >= most || vocabulary >= most) return 0;
-    return embed_plan(rows, vocabulary, cols).bytes;
+    return embed_fits(rows, vocabulary, cols) ? embed_plan(rows, vocabulary, cols).bytes : 0;
 }
 
 nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows, const void* dy,
@@ -941,8 +945,7 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
     if (vocabulary == 0 || cols == 0) return NC_OK;
     if (!dtable || lddt < cols || !workspace) return NC_ERR_INVALID;
     if (rows && (!tokens || !dy || lddy < cols)) return NC_ERR_INVALID;
-    const size_t most = (size_t)1 << 31;
-    if (rows >= most || cols >= (size_t)256 * 65535 || vocabulary >= most) return NC_ERR_TOO_LARGE;
+    if (!embed_fits(rows, vocabulary, cols)) return NC_ERR_TOO_LARGE;
     if (!element_aligned(tokens, token_bytes) || !element_aligned(dy, yb) ||
         !element_aligned(dtable, tb) || !aligned16(workspace))
         return NC_ERR_ALIGN;
