@@ -125,7 +125,10 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(const __grid_constant_
     }
     __syncthreads();
     const double sum = sums;
-    const double by = sum == 0.0 ? 0.0 : in.scale / (sqrt(sum) + in.eps);
+    // (of an inf: NaN for all values, not 0 for those that are finite)
+    const double by = sum == 0.0      ? 0.0
+                      : isfinite(sum) ? in.scale / (sqrt(sum) + in.eps)
+                                      : (double)__uint_as_float(0x7FC00000u);
     const bool narrow = by > 1e-37 && by < 1e37;
     const float by32 = (float)by;
     const T* g = static_cast<const T*>(in.g) + blockIdx.y * in.distance;
