@@ -256,8 +256,14 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
 // a long sum are too small: by 5e-7 of their size after 1024 products, 9e-7 after 2048, twice that after
 // 4096, and the loss with them.  CHAINS: longer sums are read out every 1024 products and added up in
 // registers (128 of a thread's), rounded to nearest, while the next ones are computed; the error stays
-// that of 1024.  6144 x 2048 x 65536: 1161 us, 1123 as one sum.
+// that of 1024.  6144 x 2048 x 65536: 1161 us, 1123 as one sum.  (Figures of bfloat16.  A product of binary16
+// has more bits than the accumulator has below the sum's first, so something of each is cut off too: 7e-6 after
+// 1024 products of one sign.)
 constexpr uint32_t kCeChain = 16;                    // steps
+// The backward pass makes its logits as the forward pass does, chain by chain, so that they are the same bits
+// as those in lse.  As one sum of 4096 products they were 1.8e-6 of their size smaller, and the entry of a
+// target with 1 - p = 1e-4 and a logit of 25 was off by a half.  8192 x 4096 x 65536: 10.72 ms, 10.46 as one sum.
+constexpr uint32_t kCeDzChain = 16;
 
 template <bool CHAINS> struct CeLogits : ProductOnce {
     // left, right: gathered rows, piece of the table
@@ -288,26 +294,16 @@ template <bool CHAINS> struct CeLogits : ProductOnce {
         w.width = kProductTile / (int)split;
         w.n += (int)(u % split) * w.width;
         w.steps = (int)steps;
-        if (CHAINS) {
-            const uint32_t from = (uint32_t)((uint64_t)steps * chain / parts_of);
-            w.k = (int)from * kProductStep;
-            w.steps = (int)((uint32_t)((uint64_t)steps * (chain + 1) / parts_of) - from);
-            w.part = chain;
-        }
+        if (CHAINS) product_chain(w, chain, parts_of);
+        w.part = chain;
         return w;
     }
     __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
-        if (CHAINS && w.part + 1 < parts_of) {
-#pragma unroll
-            for (int c = 0; c < kProductHalf; c += kColumns) {
-                if (c >= r.columns) break;
-                uint32_t v[kColumns];
-                r.load(c, v);
-#pragma unroll
-                for (int i = 0; i < kColumns; ++i)
-                    s.sums[c + i] = w.part ? s.sums[c + i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+        if constexpr (CHAINS) {
+            if (w.part + 1 < parts_of) {
+                product_keep(r, w.part == 0, s.sums);
+                return;
             }
-            return;
         }
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const uint32_t target = row < count ? __ldcg(rows.target + row) : kCeNone;
@@ -432,10 +428,10 @@ template <typename T> __device__ __forceinline__ constexpr float ce_headroom() {
     return sizeof(T) && std::is_same<T, __half>::value ? 16384.0f : 1.0f;
 }
 
-template <typename T> struct CeDz : ProductOnce {
+template <typename T, bool CHAINS> struct CeDzJob : ProductOnce {
     // left, right: gathered rows, piece of the table
     CeRows rows;
-    uint32_t tiles_n, first, steps;
+    uint32_t tiles_n, first, steps, parts_of;            // parts_of: chains of a sum
     float unit;
     T* dz;                               // [row][pitch]
     uint64_t pitch;
@@ -466,19 +462,29 @@ template <typename T> struct CeDz : ProductOnce {
         split = product_split(tiles);
         return split.units(tiles);
     }
-    typedef ProductNothing State;
-    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    struct State {
+        float sums[CHAINS ? kProductHalf : 1];           // of the chains before
+    };
+    __device__ __forceinline__ uint32_t chains() const { return CHAINS ? parts_of : 1; }
     __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t chain) const {
         ProductUnit w = {};
         int column;
         const uint32_t t = split.tile(u, column, w.width);
         product_tile(t, (count + kProductTile - 1) / kProductTile, tiles_n, w.m, w.n);
         w.n += column;
         w.steps = (int)steps;
+        if (CHAINS) product_chain(w, chain, parts_of);
+        w.part = chain;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
+        if constexpr (CHAINS) {
+            if (w.part + 1 < parts_of) {
+                product_keep(r, w.part == 0, s.sums);
+                return;
+            }
+        }
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const bool counts = row < count;
         const uint32_t target = counts ? __ldcg(rows.target + row) : 0u;
@@ -491,28 +497,46 @@ template <typename T> struct CeDz : ProductOnce {
         const bool near = counts && target != kCeNone && target >= first + col &&
                           at < (uint32_t)r.columns;
         T* to = dz + (uint64_t)row * pitch + col;
-#pragma unroll 1
-        for (int c = 0; c < r.columns; c += 32) {
-            uint32_t v[32];
-            r.load(c, v);
+        const auto put = [&](auto& v, int c) {
+            constexpr int N = CHAINS ? 16 : 32;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < N; ++i)
                 v[i] = __float_as_uint(all * exp2_approx(fmaf(__uint_as_float(v[i]), unit, shift)));
-            if (near && at >= (uint32_t)c && at < (uint32_t)c + 32) {
+            if (near && at >= (uint32_t)c && at < (uint32_t)c + N) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)     // (a sum, not a store: v stays in registers)
+                for (int i = 0; i < N; ++i)      // (a sum, not a store: v stays in registers)
                     v[i] = __float_as_uint(__uint_as_float(v[i]) - (at - c == (uint32_t)i ? hot : 0.0f));
             }
-            Bytes32 o[2];
+            Bytes32 o[N / 16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < N / 2; ++i)
                 o[i >> 3].v[i & 7] =
                     pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])) & keep;
-            st_wide(to + c, o[0]);
-            st_wide(to + c + 16, o[1]);
+#pragma unroll
+            for (int i = 0; i < N / 16; ++i) st_wide(to + c + 16 * i, o[i]);
+        };
+        if constexpr (CHAINS) {
+#pragma unroll
+            for (int c = 0; c < kProductHalf; c += 16) {
+                if (c >= r.columns) break;
+                uint32_t v[16];
+                r.load(c, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    v[i] = __float_as_uint(s.sums[c + i] + __uint_as_float(v[i]));
+                put(v, c);
+            }
+        } else {
+#pragma unroll 1
+            for (int c = 0; c < r.columns; c += 32) {
+                uint32_t v[32];
+                r.load(c, v);
+                put(v, c);
+            }
         }
     }
 };
+template <typename T> using CeDz = CeDzJob<T, false>;
 
 // what the products over dz are multiplied by
 __device__ __forceinline__ float ce_factor(uint32_t largest, float scale, bool bf16) {
@@ -797,12 +821,16 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
             !make_box_map(&table_map, piece, bf16, 1, count, width, stride, 0) ||
             !make_box_map(&dz_map, dz, bf16, 1, p.rows_pitch, count, dz_pitch, 0))
             return NC_ERR_CUDA;
-        CeDz<T> a = {};
-        a.left = x_map; a.right = table_map; a.bf16 = bf16; a.rows = rows;
-        a.tiles_n = (uint32_t)(dz_pitch / 256); a.first = (uint32_t)first;
-        a.steps = (uint32_t)((width + kProductStep - 1) / kProductStep);
-        a.unit = scale * kLog2E; a.dz = dz; a.pitch = dz_pitch; a.blocks = p.blocks;
-        nc_status st = product_launch(a, 4 * tiles_t * a.tiles_n, stream);
+        const auto launch_dz = [&](auto a) {
+            a.left = x_map; a.right = table_map; a.bf16 = bf16; a.rows = rows;
+            a.tiles_n = (uint32_t)(dz_pitch / 256); a.first = (uint32_t)first;
+            a.steps = (uint32_t)((width + kProductStep - 1) / kProductStep);
+            a.parts_of = (a.steps + kCeDzChain - 1) / kCeDzChain;
+            a.unit = scale * kLog2E; a.dz = dz; a.pitch = dz_pitch; a.blocks = p.blocks;
+            return product_launch(a, 4 * tiles_t * a.tiles_n, stream);
+        };
+        nc_status st = width > (uint64_t)kCeDzChain * kProductStep ? launch_dz(CeDzJob<T, true>{})
+                                                                   : launch_dz(CeDz<T>{});
         if (st != NC_OK) return st;
         if (dx) {
             CeDx b = {};

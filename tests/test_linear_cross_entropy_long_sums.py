@@ -1,0 +1,53 @@
+"""Cross entropy gradients whose logits or table gradients are long sums.
+
+The tensor cores cut off what an accumulator cannot hold, always towards 0.  With bfloat16 a sum of 1024
+products of one sign is too small by 5e-7 of its size, one of 8192 by 4e-6; twice that is allowed here.  A
+product of binary16 has 22 bits instead of 16, so that of each of them something is cut off too: with u = 2^-24
+the unit of a sum in [1, 2) is 2 u, and of 1024 products each loses at most that of a partial sum which is half
+the final one on the average: at most 1024 u = 6e-5 of the sum.  A cut of 25 or 26 bits, which the 16 products
+of an instruction are added with, makes it a quarter to a half of that; allowed is what the tests of shorter sums
+allow, 4 u for each 16 products, 1.6e-5 for 1024.  Longer sums are chains of that many products, added up in binary32 (u for each),
+so that nothing grows with the length.  The cases have terms of one sign, for which the cut-off adds up."""
+import pytest
+import torch
+
+from operator_util import U
+from test_linear_cross_entropy import Case, check_backward, check_forward
+
+
+class Confident(Case):
+    """Rows along their target's entry of the table: 1 - p of a target between about 1e-3 and 1e-5, logits of
+    25 and more, sums of which no term is negative."""
+
+    def __init__(self, rows, width, vocabulary, kind, out=None):
+        super().__init__(rows, width, vocabulary, kind, without=0.1, scale=1.0)
+        g = self.generator
+        w = 1 + torch.randn(vocabulary, width, generator=g, device="cuda")
+        self.w.view.copy_(w)
+        w = self.w.view.double()
+        size = 25 + 8 * torch.rand(rows, 1, generator=g, device="cuda")
+        x = w[self.target.clamp(min=0)]
+        x = size * x / x.square().sum(1, keepdim=True)
+        x[self.target < 0] = float("nan")
+        self.x.view.copy_(x)
+
+    def exact(self):
+        loss, lse, z, off, counts, x, w = super().exact()
+        # in place of the bound for one sum of any length: that of chains of 1024
+        chain = 1e-6 if self.kind == "bf16" else (1024 / 16 + 4) * 4 * U
+        off = (chain + (self.width / 1024 + 2) * U) * (x.abs() @ w.abs().t())
+        return loss, lse, z, off, counts, x, w
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("width", [1024, 1025, 2048, 4096, 8192, 16384])
+def test_confident_rows_of_a_wide_layer(width, kind):
+    c = Confident(200, width, 300, kind)
+    _, lse, z, _, counts, _, _ = c.exact()
+    p = torch.exp(z - lse[:, None]).gather(1, c.target.clamp(min=0)[:, None])[counts]
+    assert 1e-6 < float((1 - p).min()) and float((1 - p).max()) < 1e-2
+    check_forward(c)
+    check_backward(c, "f32", False, False, size_of_dloss=1.0)
+    check_backward(c, kind, True, True, size_of_dloss=1.0)
+

@@ -45,14 +45,19 @@ int main(int argc, char** argv) {
         a.tiles_n = 1; a.split = 1; a.count = 1;
         bad = check(a, steps, a.chains(), kCeChain);
     }
+    if (name == "dz") {
+        CeDzJob<__half, true> a = {};
+        a.steps = steps; a.parts_of = (steps + kCeDzChain - 1) / kCeDzChain;
+        a.tiles_n = 1; a.count = 1; a.split = {1, 1};
+        bad = check(a, steps, a.chains(), kCeDzChain);
+    }
     if (!bad) printf("ok\n");
     return bad;
 }
 """
 
 
-@pytest.fixture(scope="module")
-def program(tmp_path_factory):
+def build(folder, main, constants=None):
     with open(os.path.join(MODEL, "product.hpp")) as f:
         model = f.read()
 
@@ -66,15 +71,31 @@ def program(tmp_path_factory):
             text = text[:b] + text[e:]
         return model + text.replace("mma_pair(", "product_mma(")
 
-    folder = tmp_path_factory.mktemp("chains")
     source, out = str(folder / "chains.cpp"), str(folder / "chains")
     with open(source, "w") as f:
-        f.write(translate.translate(["product.cuh", "cross_entropy_kernels.cu"], None, change) + MAIN)
+        f.write(translate.translate(["product.cuh", "cross_entropy_kernels.cu"], constants, change) + main)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     subprocess.run(["g++", "-std=c++20", "-O1", "-w", "-ffp-contract=off", "-fsanitize=address", "-I" + MODEL,
                     "-I" + os.path.join(translate.ROOT, "include"), "-I" + os.path.join(cuda, "include"),
                     "-o", out, source], check=True)
     return out
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    return build(tmp_path_factory.mktemp("chains"), MAIN)
+
+
+@pytest.fixture(scope="module")
+def short_chains(tmp_path_factory):
+    """The program of the cross entropy's tests with chains of two steps in the backward pass, one pair."""
+    with open(os.path.join(MODEL, "cross_entropy.cpp")) as f:
+        main = f.read()
+    kernels = ["CeDzJob<__nv_bfloat16, true>", "CeDzJob<__half, true>"]
+    more = "".join("    model::cluster_of[(const void*)product_kernel<%s>] = 2;\n" % k for k in kernels)
+    at = main.index("    const int dtype = ")
+    return build(tmp_path_factory.mktemp("short_chains"), main[:at] + more + main[at:],
+                 dict(kProductPairs=2, kCeChain=2, kCeDzChain=2))
 
 
 def chains(program, *args):
@@ -86,3 +107,15 @@ def chains(program, *args):
 @pytest.mark.parametrize("steps", [17, 33, 1000, (1 << 18) - 1, 1 << 18, (1 << 18) + 1, 1 << 19, (1 << 25) - 4])
 def test_the_logits_chains_cover_every_step_once(program, steps):
     chains(program, "logits", steps)
+
+
+@pytest.mark.parametrize("steps", [17, 64, 65, (1 << 18) + 1, 1 << 19, (1 << 25) - 4])
+def test_the_chains_of_the_recomputed_logits_cover_every_step_once(program, steps):
+    chains(program, "dz", steps)
+
+
+@pytest.mark.parametrize("args", [(300, 136, 257, "f16", "whole", 2, "same", 0, 0), (130, 300, 520, "bf16", "any", 5, "f32", 1, 1),
+                                  (20, 700, 40, "f16", "whole", 0, "f32", 0, 0), (5, 128, 300, "bf16", "whole", 0, "same", 0, 1)],
+                         ids=str)
+def test_gradients_of_logits_in_chains(short_chains, args):
+    chains(short_chains, *args, 1)
