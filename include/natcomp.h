@@ -560,7 +560,10 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
  * count get dx of 0 and count for nothing, whatever x, dloss and dlse hold there; a target beyond the
  * vocabulary makes the row's dx and all of dtable NaN.  dz is rounded to dtype (relative to the largest
  * coefficient of any row, so that in binary16 nothing of weight vanishes): that is half a step of 16
- * bits for each term of both sums, also where dtable is binary32.  The vocabulary is worked through in
+ * bits for each term of both sums, also where dtable is binary32.  The tensor cores cut sums off: a sum
+ * of terms of one sign is too small by 5e-7 of its size after 1024 of them (7e-6 in binary16).  Logits and
+ * dtable are sums of no more than 1024 terms and 8192 rows (2048 in binary16), added up in binary32, and
+ * no further off; a sum of dx is one over a piece of the vocabulary.  The vocabulary is worked through in
  * pieces whose dz takes 256 MB, or rows * 2048 values where that is more.
  * The forward workspace holds the rows that count once more, 8 bytes for every row and 256 entries, and
  * a piece of the table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256

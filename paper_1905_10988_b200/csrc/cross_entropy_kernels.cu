@@ -264,6 +264,10 @@ constexpr uint32_t kCeChain = 16;                    // steps
 // as those in lse.  As one sum of 4096 products they were 1.8e-6 of their size smaller, and the entry of a
 // target with 1 - p = 1e-4 and a logit of 25 was off by a half.  8192 x 4096 x 65536: 10.72 ms, 10.46 as one sum.
 constexpr uint32_t kCeDzChain = 16;
+// dtable, a sum over the rows: chains of 8192 rows, 4e-6 of it, and in binary16 of 2048, 1.3e-5.  (One sum of
+// 131072 rows was 6e-5 and, in binary16, 5e-4 too small.)  dx is rounded to 16 bits and stays one sum a piece.
+constexpr uint32_t kCeLongChain = 128;
+constexpr uint32_t kCeLongChainF16 = 32;
 
 template <bool CHAINS> struct CeLogits : ProductOnce {
     // left, right: gathered rows, piece of the table
@@ -643,36 +647,47 @@ ce_join_dx_kernel(const CeRows rows, const float* __restrict__ sums, const uint6
     }
 }
 
-struct CeDtable : ProductOnce {
+template <bool CHAINS> struct CeDtableJob : ProductOnce {
     // left, right: dz, gathered rows
     CeRows rows;
-    uint32_t entries, width, tiles_m, tiles_n;
+    uint32_t entries, width, tiles_m, tiles_n, chain_steps;
     float scale;
     void* dtable;                        // of the piece
     uint64_t ldt;
     ProductTarget target;
-    uint32_t count;
+    uint32_t count, parts_of;            // parts_of: chains of a sum
     ProductSplit split;
     float factor;
 
     __device__ __forceinline__ uint32_t begin(uint32_t, bool reads_out) {
         count = __ldcg(rows.count);
+        parts_of = max(1u, ((count + kProductStep - 1) / kProductStep + chain_steps - 1) / chain_steps);
         factor = reads_out ? ce_factor(__ldcg(rows.count + 1), scale, bf16) : 0.0f;
         split = product_split(tiles_m * tiles_n);
         return split.units(tiles_m * tiles_n);
     }
-    typedef ProductNothing State;
-    __device__ __forceinline__ uint32_t chains() const { return 1; }
+    struct State {
+        float sums[CHAINS ? kProductHalf : 1];           // of the chains before
+    };
+    __device__ __forceinline__ uint32_t chains() const { return CHAINS ? parts_of : 1; }
     __device__ __forceinline__ void ahead(const ProductUnit&, const ProductRead&, State&) const {}
-    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t) const {
+    __device__ __forceinline__ ProductUnit unit_of(uint32_t u, uint32_t chain) const {
         ProductUnit w = {};
         int column;
         product_tile(split.tile(u, column, w.width), tiles_m, tiles_n, w.m, w.n);
         w.n += column;
         w.steps = (int)((count + kProductStep - 1) / kProductStep);
+        if (CHAINS) product_chain(w, chain, parts_of);
+        w.part = chain;
         return w;
     }
-    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State&) const {
+    __device__ __forceinline__ void store(const ProductUnit& w, const ProductRead& r, State& s) const {
+        if constexpr (CHAINS) {
+            if (w.part + 1 < parts_of) {
+                product_keep(r, w.part == 0, s.sums);
+                return;
+            }
+        }
         const uint32_t row = (uint32_t)(w.m + r.row), col = (uint32_t)(w.n + r.column);
         const ProductRows to =
             product_rows(dtable, target.dtype, ldt, row - r.lane, entries, col, r.lane);
@@ -680,6 +695,9 @@ struct CeDtable : ProductOnce {
         for (int c = 0; c < r.columns && col + c < width; c += 32) {
             uint32_t v[32];
             r.load(c, v);
+            if constexpr (CHAINS) {              // (few rows may count)
+                if (parts_of > 1) product_join(s.sums, c, v);
+            }
             float o[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i)         // (no row counts: 0, whatever the factor)
@@ -688,6 +706,7 @@ struct CeDtable : ProductOnce {
         }
     }
 };
+typedef CeDtableJob<false> CeDtable;
 
 // ---- plans -----------------------------------------------------------------------------------
 
@@ -811,6 +830,7 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
     const uint64_t sums_pitch = (width + 31) / 32 * 32, tiles_n = (width + 255) / 256;
     const uint64_t tiles_t = p.rows_pitch / 256;
     T* dz = reinterpret_cast<T*>(ws + p.dz);
+    const uint32_t chain = bf16 ? kCeLongChain : kCeLongChainF16;
     for (uint64_t first = 0; first < vocabulary; first += p.piece) {
         const uint64_t count = vocabulary - first < p.piece ? vocabulary - first : p.piece;
         const uint64_t dz_pitch = (count + 255) / 256 * 256;
@@ -832,6 +852,17 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
         nc_status st = width > (uint64_t)kCeDzChain * kProductStep ? launch_dz(CeDzJob<T, true>{})
                                                                    : launch_dz(CeDz<T>{});
         if (st != NC_OK) return st;
+        const auto launch_dtable = [&](auto c) {
+            c.left = dz_map; c.right = x_map; c.left_side.lines = c.right_side.lines = true;
+            c.bf16 = bf16; c.rows = rows; c.entries = (uint32_t)count; c.width = (uint32_t)width;
+            c.tiles_m = (uint32_t)(dz_pitch / 256); c.tiles_n = (uint32_t)tiles_n; c.scale = scale;
+            c.chain_steps = chain;
+            const int bytes = act8_type_bytes(dtable_dtype);
+            c.dtable = static_cast<char*>(dtable) + first * lddt * bytes; c.ldt = lddt;
+            c.target.dtype = dtable_dtype; c.target.add = accumulate;
+            c.target.access = row_access(dtable, lddt, bytes, vocabulary);
+            return product_launch(c, 4 * (uint64_t)c.tiles_m * tiles_n, stream);
+        };
         if (dx) {
             CeDx b = {};
             b.left = dz_map; b.right = table_map; b.right_side.lines = true; b.bf16 = bf16;
@@ -846,15 +877,8 @@ static nc_status ce_backward(const CePlan& p, const CeRows& rows, const CeTable&
             if (st != NC_OK) return st;
         }
         if (dtable) {
-            CeDtable c = {};
-            c.left = dz_map; c.right = x_map; c.left_side.lines = c.right_side.lines = true;
-            c.bf16 = bf16; c.rows = rows; c.entries = (uint32_t)count; c.width = (uint32_t)width;
-            c.tiles_m = (uint32_t)(dz_pitch / 256); c.tiles_n = (uint32_t)tiles_n; c.scale = scale;
-            const int bytes = act8_type_bytes(dtable_dtype);
-            c.dtable = static_cast<char*>(dtable) + first * lddt * bytes; c.ldt = lddt;
-            c.target.dtype = dtable_dtype; c.target.add = accumulate;
-            c.target.access = row_access(dtable, lddt, bytes, vocabulary);
-            st = product_launch(c, 4 * (uint64_t)c.tiles_m * tiles_n, stream);
+            st = most_rows > (uint64_t)chain * kProductStep ? launch_dtable(CeDtableJob<true>{})
+                                                            : launch_dtable(CeDtable{});
             if (st != NC_OK) return st;
         }
     }

@@ -487,6 +487,15 @@ __device__ __forceinline__ void product_keep(const ProductRead& r, bool first, f
     }
 }
 
+// 32 of the sums of the chains before, those of the thread's columns from c on (0, 32, 64 or 96), added to v.
+__device__ __forceinline__ void product_join(const float (&sums)[kProductHalf], int c, uint32_t (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {       // (selects: an index would put the sums into memory)
+        const float low = c & 32 ? sums[32 + i] : sums[i], high = c & 32 ? sums[96 + i] : sums[64 + i];
+        v[i] = __float_as_uint((c & 64 ? high : low) + __uint_as_float(v[i]));
+    }
+}
+
 // ---- sums in parts ---------------------------------------------------------------------------
 // A part of a unit's sums lies in memory as [column / 4][256 rows] groups of four columns.
 

@@ -11,7 +11,8 @@ so that nothing grows with the length.  The cases have terms of one sign, for wh
 import pytest
 import torch
 
-from operator_util import U
+import paper_1905_10988_b200 as nc
+from operator_util import CODES, TYPES, U
 from test_linear_cross_entropy import Case, check_backward, check_forward
 
 
@@ -51,3 +52,26 @@ def test_confident_rows_of_a_wide_layer(width, kind):
     check_backward(c, "f32", False, False, size_of_dloss=1.0)
     check_backward(c, kind, True, True, size_of_dloss=1.0)
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,every", [(8192, 1), (8193, 1), (50000, 2), (131072, 1), (60000, 100)])
+def test_table_gradients_of_many_rows(rows, every, kind):
+    # all logits 0: p = 2^-8, exact in 16 bits, and dtable is 2^-8 times the sum of the rows of x
+    width, vocabulary = 72, 256
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (0.5 + torch.rand(rows, width, generator=g, device="cuda")).to(TYPES[kind])
+    table = torch.zeros(vocabulary, width, dtype=TYPES[kind], device="cuda")
+    target = torch.full((rows,), -1, device="cuda")
+    target[::every] = 0                   # the rows that count
+    lse = torch.full((rows,), float(torch.tensor(256.0, dtype=torch.float64).log()), device="cuda")
+    zero, one = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    for accumulate in (False, True):
+        dtable = torch.full((vocabulary, width), 3.0, device="cuda")
+        size = nc.nc_linear_cross_entropy_backward_workspace_bytes(rows, width, vocabulary)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        nc.nc_linear_cross_entropy_backward(x, CODES[kind], rows, width, width, table, vocabulary, width, target, 8,
+                                            1.0, lse, zero, one, None, width, dtable, nc.DTYPE_F32, width,
+                                            accumulate, ws, size)
+        want = x.double()[target >= 0].sum(0) / 256 + (3.0 if accumulate else 0.0)
+        off = float(((dtable.double() - want).abs() / want).max())
+        assert off <= 8e-6 + (rows / 8192 + 4) * U, off

@@ -51,6 +51,13 @@ int main(int argc, char** argv) {
         a.tiles_n = 1; a.count = 1; a.split = {1, 1};
         bad = check(a, steps, a.chains(), kCeDzChain);
     }
+    if (name == "dtable") {
+        CeDtableJob<true> a = {};
+        a.count = 64 * steps - 5; a.chain_steps = kCeLongChainF16;
+        a.parts_of = (steps + kCeLongChainF16 - 1) / kCeLongChainF16;
+        a.tiles_m = a.tiles_n = 1; a.split = {1, 1};
+        bad = check(a, steps, a.chains(), kCeLongChainF16);
+    }
     if (!bad) printf("ok\n");
     return bad;
 }
@@ -91,11 +98,11 @@ def short_chains(tmp_path_factory):
     """The program of the cross entropy's tests with chains of two steps in the backward pass, one pair."""
     with open(os.path.join(MODEL, "cross_entropy.cpp")) as f:
         main = f.read()
-    kernels = ["CeDzJob<__nv_bfloat16, true>", "CeDzJob<__half, true>"]
+    kernels = ["CeDzJob<__nv_bfloat16, true>", "CeDzJob<__half, true>", "CeDtableJob<true>"]
     more = "".join("    model::cluster_of[(const void*)product_kernel<%s>] = 2;\n" % k for k in kernels)
     at = main.index("    const int dtype = ")
     return build(tmp_path_factory.mktemp("short_chains"), main[:at] + more + main[at:],
-                 dict(kProductPairs=2, kCeChain=2, kCeDzChain=2))
+                 dict(kProductPairs=2, kCeChain=2, kCeDzChain=2, kCeLongChain=2, kCeLongChainF16=1))
 
 
 def chains(program, *args):
@@ -114,8 +121,20 @@ def test_the_chains_of_the_recomputed_logits_cover_every_step_once(program, step
     chains(program, "dz", steps)
 
 
+@pytest.mark.parametrize("steps", [33, 128, 1000, (1 << 20) + 1, (1 << 25) - 4])
+def test_the_table_gradients_chains_cover_every_step_once(program, steps):
+    chains(program, "dtable", steps)
+
+
 @pytest.mark.parametrize("args", [(300, 136, 257, "f16", "whole", 2, "same", 0, 0), (130, 300, 520, "bf16", "any", 5, "f32", 1, 1),
-                                  (20, 700, 40, "f16", "whole", 0, "f32", 0, 0), (5, 128, 300, "bf16", "whole", 0, "same", 0, 1)],
+                                  (20, 700, 40, "f16", "whole", 0, "f32", 0, 0), (5, 128, 300, "bf16", "whole", 0, "same", 0, 1),
+                                  (400, 40, 300, "f16", "any", 0, "f32", 1, 0), (500, 24, 260, "bf16", "whole", 1, "same", 0, 0)],
                          ids=str)
-def test_gradients_of_logits_in_chains(short_chains, args):
+def test_gradients_of_sums_in_chains(short_chains, args):
     chains(short_chains, *args, 1)
+
+
+@pytest.mark.parametrize("rank", [0, 1])
+@pytest.mark.parametrize("nth", [3, 9, 17])
+def test_a_wait_that_runs_out_in_a_chain_leaves_nan(short_chains, rank, nth):
+    chains(short_chains, 300, 300, 260, "f16", "whole", 0, "f32", 0, 0, 1, "drop_rank=%d" % rank, "drop_nth=%d" % nth)
