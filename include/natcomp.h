@@ -587,7 +587,10 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
 /* Orthogonalised update of `batch` matrices of rows x cols by Newton-Schulz products:
  *   X = G / (|G| + eps),  then `steps` times  X <- a X + (b A + c A A) X  with A = X X^T,  out = scale X
  * |G|: the Frobenius norm.  A matrix with more rows than columns is treated as its transpose is.
- * coefficients: host memory, a, b, c of every step, read before the call returns.  G: dtype, matrix i
+ * coefficients: host memory, a, b, c of every step, read before the call returns.  Refused
+ * (NC_ERR_INVALID) are those that could overflow what is held in binary16: with s up to the largest
+ * singular value that X can have before a step (1 before the first), s^2 and |b s^2 + c s^4| must not
+ * pass 240.  The usual ones stay below 6.  G: dtype, matrix i
  * from element i * distance on; out: out_dtype, from element i * out_distance on (both ignored for one
  * matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that holds an inf or
  * a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits: the result is

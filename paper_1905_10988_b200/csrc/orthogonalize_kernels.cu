@@ -433,6 +433,30 @@ static bool ortho_fits(size_t batch, size_t rows, size_t cols) {
     return tiles * (batch ? batch : 1) < ((uint64_t)1 << 31) && batch * rows < ((uint64_t)1 << 31);
 }
 
+// Whether nothing that is held in binary16 overflows, whatever the matrix: A, whose entries are at most s^2 for
+// the largest singular value s of X, and the polynomial's, at most |b s^2 + c s^4| for one of them, both times
+// 256.  The singular values are at most 1 before the first step, and at most the largest of |a s + b s^3 + c s^5|
+// after one.  (240: 6 % below what overflows, for the roundings.  Beyond it inf met 0 and all became NaN.)
+static bool ortho_bounded(const float* coefficients, int steps) {
+    double top = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        const double a = coefficients[3 * i], b = coefficients[3 * i + 1], c = coefficients[3 * i + 2];
+        const double square = top * top;
+        const auto poly = [&](double u) { return fabs(b * u + c * u * u); };
+        const auto next = [&](double u) { return fabs(sqrt(u) * (a + b * u + c * u * u)); };
+        if (!(square <= 240.0 && poly(square) <= 240.0)) return false;
+        const double middle = -b / (2.0 * c);            // where the slope of b u + c u u is 0
+        if (middle > 0.0 && middle < square && !(poly(middle) <= 240.0)) return false;
+        // the slope of the step is 0 where a + 3 b u + 5 c u u is; with c = 0, or nearly so, at -a / 3 b
+        top = next(square);
+        const double root = sqrt(9.0 * b * b - 20.0 * a * c), q = -0.5 * (3.0 * b + (b < 0.0 ? -root : root));
+        const double at[2] = {q / (5.0 * c), a / q};
+        for (double u : at)
+            if (u > 0.0 && u < square && next(u) > top) top = next(u);
+    }
+    return true;
+}
+
 static OrthoPlan ortho_plan(uint64_t batch, uint64_t rows, uint64_t cols) {
     OrthoPlan p = {};
     p.side = rows < cols ? rows : cols;
@@ -491,6 +515,7 @@ nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, 
     if (batch == 0 || rows == 0 || cols == 0) return NC_OK;
     if (!g || !out || !workspace || ldg < cols || ldo < cols) return NC_ERR_INVALID;
     if (!ortho_fits(batch, rows, cols) || steps > kOrthoSteps * kOrthoLaunches) return NC_ERR_TOO_LARGE;
+    if (!ortho_bounded(coefficients, steps)) return NC_ERR_INVALID;
     if (batch > 1 && (distance < (rows - 1) * ldg + cols || out_distance < (rows - 1) * ldo + cols))
         return NC_ERR_INVALID;
     if (!element_aligned(g, bytes) || !element_aligned(out, out_bytes) || !aligned32(workspace))
