@@ -107,12 +107,7 @@ class TokenModel:
         if self.ids is None:
             raise RuntimeError("no forward pass has kept activations for this one")
         t, w, v, bf16, f32 = self.tokens, self.width, self.vocabulary, nc.DTYPE_BF16, nc.DTYPE_F32
-        if gradient.dtype != torch.float32 or tuple(gradient.shape) != (self.gradient_size,):
-            raise ValueError("gradient is %s %s, not a torch.float32 vector of %d entries"
-                             % (gradient.dtype, tuple(gradient.shape), self.gradient_size))
-        if gradient.stride(0) != 1:
-            raise ValueError("gradient has a stride of %d" % gradient.stride(0))
-        _on_device("gradient", gradient, self.lse.device)
+        self._check_gradient(gradient)
         for begin, end in self.gaps:
             gradient[begin:end].zero_()
         piece = {name: gradient[at:at + n] for name, (at, n) in self.slices.items()}
@@ -130,10 +125,19 @@ class TokenModel:
         nc.nc_embedding_backward(self.ids, self.ids.element_size(), t, dx, bf16, w, w, self.scale, v,
                                  piece["table"], f32, w, True, self.workspace, self.ws_bytes)
 
+    def _check_gradient(self, gradient) -> None:
+        if gradient.dtype != torch.float32 or tuple(gradient.shape) != (self.gradient_size,):
+            raise ValueError("gradient is %s %s, not a torch.float32 vector of %d entries"
+                             % (gradient.dtype, tuple(gradient.shape), self.gradient_size))
+        if gradient.stride(0) != 1:
+            raise ValueError("gradient has a stride of %d" % gradient.stride(0))
+        _on_device("gradient", gradient, self.lse.device)
+
     def apply(self, gradient, rate: float, matrix_rate: float) -> None:
-        """One step along the (aggregated) gradient: the blocks' matrices by matrix_rate times their
-        orthogonalised gradients, which have singular values near 1 whatever the gradient's size, the
-        rest by rate times the gradient."""
+        """One step along the (aggregated) gradient, an fp32 vector of gradient_size entries: the blocks'
+        matrices by matrix_rate times their orthogonalised gradients, which have singular values near 1
+        whatever the gradient's size, the rest by rate times the gradient."""
+        self._check_gradient(gradient)
         for b, (at, n) in zip(self.blocks, self.block_slices):
             for name, (begin, size) in b.slices.items():
                 p, g = getattr(b, name), gradient[at + begin:at + begin + size]
