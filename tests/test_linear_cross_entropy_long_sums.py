@@ -75,3 +75,11 @@ def test_table_gradients_of_many_rows(rows, every, kind):
         want = x.double()[target >= 0].sum(0) / 256 + (3.0 if accumulate else 0.0)
         off = float(((dtable.double() - want).abs() / want).max())
         assert off <= 8e-6 + (rows / 8192 + 4) * U, off
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,width,vocabulary", [(87, 200, 513), (300, 1001, 2049), (1000, 520, 4000), (130, 2100, 300)])
+def test_forward_of_rows_with_gaps_that_count(rows, width, vocabulary, kind):
+    for without, tb in ((0.0, 8), (0.3, 4)):
+        check_forward(Case(rows, width, vocabulary, kind, "gap", without=without, target_bytes=tb))

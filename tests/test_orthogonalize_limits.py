@@ -83,3 +83,15 @@ def test_coefficients_are_judged_by_the_values_that_they_reach():
         assert answer(co) == ("NC_ERR_WORKSPACE" if worst <= 240 else "NC_ERR_INVALID"), (co, worst)
         taken += worst <= 240
     assert 30 < taken < 270
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,rows,cols", [(1, 2300, 2300), (5, 777, 1001), (40, 300, 290), (1, 2600, 4100)])
+def test_more_tiles_than_pairs_of_blocks(batch, rows, cols):
+    # a pair computes several tiles of a phase, whole ones and the narrow ones of the last round
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(batch, rows, cols, generator=g, device="cuda")
+    for out, layout in (("f32", "any"), ("bf16", "whole")):
+        given, got = run(x, out, layout=layout)
+        exact = [tuple(float(np.float32(v)) for v in QUINTIC)] * 5
+        assert off(got, plain(given, exact, 1e-7, 1.0)) <= 8 * 2.0 ** -11 + HALF[out]
