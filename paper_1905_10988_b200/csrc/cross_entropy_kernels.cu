@@ -250,6 +250,16 @@ ce_copy_kernel(const unsigned short* __restrict__ from, const uint64_t rows, con
                  (uint64_t)gridDim.x * 256);
 }
 
+// rows of zeros, a warp each
+template <typename T>
+__global__ void __launch_bounds__(256)
+ce_clear_kernel(T* __restrict__ p, const uint64_t rows, const uint64_t width, const uint64_t ld) {
+    after_previous();
+    let_next_begin();
+    for (uint64_t r = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (uint64_t)gridDim.x * 8)
+        for (uint64_t c = threadIdx.x & 31; c < width; c += 32) p[r * ld + c] = from_f32<T>(0.0f);
+}
+
 // ---- forward ---------------------------------------------------------------------------------
 
 // The tensor cores cut off what an accumulator of 24 bits cannot hold, always towards 0, so all logits of
@@ -1013,11 +1023,15 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
     const bool bf16 = dtype == NC_DTYPE_BF16;
     const CeRows to = ce_rows(p, ws);
     if (rows == 0) {
-        if (dtable && !accumulate &&
-            cudaMemset2DAsync(dtable, lddt * act8_type_bytes(dtable_dtype), 0,
-                              width * act8_type_bytes(dtable_dtype), vocabulary,
-                              stream) != cudaSuccess)
-            return NC_ERR_CUDA;
+        if (dtable && !accumulate) {
+            const unsigned blocks = (unsigned)(vocabulary < 8 * 1184 ? (vocabulary + 7) / 8 : 1184);
+            if (dtable_dtype == NC_DTYPE_F32)
+                launch_overlapping(ce_clear_kernel<float>, dim3(blocks), dim3(256), 0, stream,
+                                   static_cast<float*>(dtable), vocabulary, width, lddt);
+            else                         // (zeros of either 16-bit type are the same)
+                launch_overlapping(ce_clear_kernel<__half>, dim3(blocks), dim3(256), 0, stream,
+                                   static_cast<__half*>(dtable), vocabulary, width, lddt);
+        }
         return launch_status();
     }
     CeGather g = {};

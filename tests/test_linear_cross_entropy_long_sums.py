@@ -8,11 +8,15 @@ the final one on the average: at most 1024 u = 6e-5 of the sum.  A cut of 25 or 
 of an instruction are added with, makes it a quarter to a half of that; allowed is what the tests of shorter sums
 allow, 4 u for each 16 products, 1.6e-5 for 1024.  Longer sums are chains of that many products, added up in binary32 (u for each),
 so that nothing grows with the length.  The cases have terms of one sign, for which the cut-off adds up."""
+import glob
+import os
+import re
+
 import pytest
 import torch
 
 import paper_1905_10988_b200 as nc
-from operator_util import CODES, TYPES, U
+from operator_util import CODES, TYPES, U, Placed, workspace
 from test_linear_cross_entropy import Case, check_backward, check_forward
 
 
@@ -83,3 +87,29 @@ def test_table_gradients_of_many_rows(rows, every, kind):
 def test_forward_of_rows_with_gaps_that_count(rows, width, vocabulary, kind):
     for without, tb in ((0.0, 8), (0.3, 4)):
         check_forward(Case(rows, width, vocabulary, kind, "gap", without=without, target_bytes=tb))
+
+
+# ---- no rows -------------------------------------------------------------------------------
+
+def test_calls_enqueue_kernels_only():
+    # memory is set and copied by kernels of the library's own, but for nc_copy_* and the debug build's record
+    for path in glob.glob(os.path.join(os.path.dirname(nc.LIB_PATH), "csrc", "*_kernels.cu")):
+        with open(path) as f:
+            found = re.findall(r"\bcudaMem(?:set|cpy)\w*", f.read())
+        assert not found, (os.path.basename(path), found)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["whole", "gap", "any"])
+@pytest.mark.parametrize("kind,out", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+def test_no_rows_clear_the_table_gradient_or_leave_it(kind, out, layout):
+    for vocabulary, width in ((1, 1), (700, 33), (3, 5000), (9000, 8)):
+        size = nc.nc_linear_cross_entropy_backward_workspace_bytes(0, width, vocabulary)
+        memory, ws = workspace(size)
+        table = torch.zeros(vocabulary, width, dtype=TYPES[kind], device="cuda")
+        for accumulate in (False, True):
+            d = Placed((vocabulary, width), out, layout)
+            nc.nc_linear_cross_entropy_backward(None, CODES[kind], 0, width, width, table, vocabulary, width, None, 8,
+                                                1.0, None, None, None, table, width, d.view, CODES[out], d.ld,
+                                                accumulate, ws, size)
+            assert bool((d.view == (-77.0 if accumulate else 0.0)).all()) and d.untouched()
