@@ -525,7 +525,9 @@ nc_status nc_act8_weight_grad(const void* dy, size_t rows, size_t n, size_t lddy
  * Matrices, types, alignment and overlap as in the section above; workspace is 32-byte aligned and of
  * the size its helper names (0: the sizes are refused).  No call holds state, synchronises or
  * allocates; two calls that may run at the same time need a workspace each, captured ones too.  Every
- * result is the same from run to run on one device. */
+ * result is the same from run to run on one device.  A wait inside a kernel (of the products, for copies
+ * and for other blocks) ends after 4e9 cycles, about two seconds, which a device takes that another
+ * process holds meanwhile; what was waited for is NaN then, and the status, which came before, NC_OK. */
 
 /* out[t] = scale * table[token[t]], rounded once.  table: dtype, vocabulary x cols.  out: out_dtype, rows
  * x cols.  A token below 0 (padding) gives a row of 0, one beyond the vocabulary a row of NaN.
@@ -595,9 +597,11 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
  * matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that holds an inf or
  * a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits: the result is
  * off by 1 to 2 thousandths of its norm with the five steps of (3.4445, -4.7750, 2.0315), also where
- * out is binary32.  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, steps <= 1024, else
- * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written.  The blocks of the products wait for one
- * another (a cooperative launch): where other work holds some of the SMs, the call waits for it. */
+ * out is binary32 (2.4 with a side of 2^20).  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, steps <= 1024, else
+ * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written.  Of several matrices each begins behind
+ * the one before: distance >= (rows - 1) * ldg + cols and out_distance likewise, else NC_ERR_INVALID.
+ * The blocks of the products wait for one another (a cooperative launch): where other work holds some of
+ * the SMs, the kernel begins when that has ended. */
 size_t nc_orthogonalize_workspace_bytes(size_t batch, size_t rows, size_t cols);
 nc_status nc_orthogonalize(const void* g, int dtype, size_t batch, size_t rows, size_t cols,
                            size_t ldg, size_t distance, const float* coefficients, int steps, float eps,

@@ -656,7 +656,9 @@ product_kernel(const __grid_constant__ Job given) {
             if (Job::kPhased && phase + 1 < phases) {
                 fence_global_copies();
                 product_writers_barrier();       // (one thread's release behind it covers what all wrote)
-                if (threadIdx.x == 0) grid_arrive(job.arrived);
+                // (given up: others must not take this block's phases for done, or those of a block that is
+                // late for it; they give up too)
+                if (threadIdx.x == 0 && !*gave_up) grid_arrive(job.arrived);
             }
         }
     } else if (warp == kProductCopyWarp) {

@@ -64,7 +64,7 @@ int main(int argc, char** argv) {
 """
 
 
-def build(folder, main, constants=None):
+def build(folder, main, constants=None, name="cross_entropy"):
     with open(os.path.join(MODEL, "product.hpp")) as f:
         model = f.read()
 
@@ -80,7 +80,7 @@ def build(folder, main, constants=None):
 
     source, out = str(folder / "chains.cpp"), str(folder / "chains")
     with open(source, "w") as f:
-        f.write(translate.translate(["product.cuh", "cross_entropy_kernels.cu"], constants, change) + main)
+        f.write(translate.translate(["product.cuh", name + "_kernels.cu"], constants, change) + main)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     subprocess.run(["g++", "-std=c++20", "-O1", "-w", "-ffp-contract=off", "-fsanitize=address", "-I" + MODEL,
                     "-I" + os.path.join(translate.ROOT, "include"), "-I" + os.path.join(cuda, "include"),
