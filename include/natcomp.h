@@ -568,7 +568,9 @@ nc_status nc_embedding_backward(const void* tokens, int token_bytes, size_t rows
  * no further off; a sum of dx is one over a piece of the vocabulary.  The vocabulary is worked through in
  * pieces whose dz takes 256 MB, or rows * 2048 values where that is more.
  * The forward workspace holds the rows that count once more, 8 bytes for every row and 256 entries, and
- * a piece of the table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256
+ * a piece of the table (64 MB, or 2048 entries).  The backward workspace holds the rows, a piece of dz and
+ * as many entries of the table, for tables that tensor copies cannot read as they lie (rows off 16-byte
+ * boundaries): few rows of a large vocabulary make that the whole table.  rows, width, vocabulary < 2^31 - 256, and together no more tiles of 256 x 256
  * than 2^31 (2^24 of dx), else NC_ERR_TOO_LARGE.  width or vocabulary of 0: NC_ERR_INVALID. */
 size_t nc_linear_cross_entropy_forward_workspace_bytes(size_t rows, size_t width, size_t vocabulary);
 nc_status nc_linear_cross_entropy_forward(const void* x, int dtype, size_t rows, size_t width,
@@ -592,13 +594,13 @@ nc_status nc_linear_cross_entropy_backward(const void* x, int dtype, size_t rows
  * coefficients: host memory, a, b, c of every step, read before the call returns.  Refused
  * (NC_ERR_INVALID) are those that could overflow what is held in binary16: with s up to the largest
  * singular value that X can have before a step (1 before the first), s^2 and |b s^2 + c s^4| must not
- * pass 240.  The usual ones stay below 6.  G: dtype, matrix i
- * from element i * distance on; out: out_dtype, from element i * out_distance on (both ignored for one
- * matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that holds an inf or
- * a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits: the result is
- * off by 1 to 2 thousandths of its norm with the five steps of (3.4445, -4.7750, 2.0315), also where
- * out is binary32 (2.4 with a side of 2^20).  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31, steps <= 1024, else
- * NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written.  Of several matrices each begins behind
+ * pass 240.  (Five steps of (3.4445, -4.7750, 2.0315) reach 2.9.)
+ * G: dtype, matrix i from element i * distance on; out: out_dtype, from element i * out_distance on (both
+ * ignored for one matrix).  steps == 0: the normalised matrix.  A matrix of zeros gives zeros; one that
+ * holds an inf or a NaN gives NaN.  Products in binary16 with binary32 accumulation, X kept in 22 bits:
+ * the result is off by 1 to 2 thousandths of its norm with those five steps, also where out is binary32
+ * (2.4 with a side of 2^20).  eps >= 0.  rows, cols <= 2^20, batch <= 65535, batch * rows < 2^31,
+ * steps <= 1024, else NC_ERR_TOO_LARGE; batch, rows or cols of 0: nothing is written.  Of several matrices each begins behind
  * the one before: distance >= (rows - 1) * ldg + cols and out_distance likewise, else NC_ERR_INVALID.
  * The blocks of the products wait for one another (a cooperative launch): where other work holds some of
  * the SMs, the kernel begins when that has ended. */

@@ -20,15 +20,14 @@
 // 2^14) clear of its subnormal numbers: a p of 2^-28 is still a normal one.
 //
 // What bounds it: the tensor cores and the power cap.  2 operations forward and 6 backward for every row,
-// column and vocabulary entry.  8192 x 4096 x 65536 backward: 10.4 ms back to back, 1.26 PFLOP/s (9.1 for
-// one call on a cool chip).
+// column and vocabulary entry.  8192 x 4096 x 65536 backward: 10.6 ms back to back, 1.24 PFLOP/s.
 #include "product.cuh"
 
 namespace natcomp {
 
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr uint32_t kCeNone = 0xFFFFFFFFu;            // a target beyond the vocabulary: the row is NaN
-// Of a piece of dz: 256 MB.  8192 x 2048 x 65536 backward: 5.01 ms; pieces of 64 MB 5.36, of 1 GB 5.05.
+// Of a piece of dz: 256 MB.  8192 x 2048 x 65536 backward: 5.41 ms; pieces of 64 MB 5.71, of 1 GB 5.37.
 constexpr uint64_t kCeDzValues = 1ull << 27;
 constexpr uint64_t kCeLeastPiece = 2048;             // vocabulary entries of a piece
 // Of a piece of the table that the forward pass copies: 64 MB, 8192 entries of width 4096.  (64 x 101 x 71851
@@ -272,10 +271,11 @@ ce_clear_kernel(T* __restrict__ p, const uint64_t rows, const uint64_t width, co
 constexpr uint32_t kCeChain = 16;                    // steps
 // The backward pass makes its logits as the forward pass does, chain by chain, so that they are the same bits
 // as those in lse.  As one sum of 4096 products they were 1.8e-6 of their size smaller, and the entry of a
-// target with 1 - p = 1e-4 and a logit of 25 was off by a half.  8192 x 4096 x 65536: 10.72 ms, 10.46 as one sum.
+// target with 1 - p = 1e-4 and a logit of 25 was off by a half.  8192 x 4096 x 65536: 10.61 ms, 10.44 as one sum.
 constexpr uint32_t kCeDzChain = 16;
 // dtable, a sum over the rows: chains of 8192 rows, 4e-6 of it, and in binary16 of 2048, 1.3e-5.  (One sum of
-// 131072 rows was 6e-5 and, in binary16, 5e-4 too small.)  dx is rounded to 16 bits and stays one sum a piece.
+// 131072 rows was 6e-5 and, in binary16, 5e-4 too small; 16384 x 1024 x 65536 into binary32 5.87 ms, 5.82 as one
+// sum, 16384 x 1024 x 32768 binary16 3.26 and 3.09.)  dx is rounded to 16 bits and stays one sum a piece.
 constexpr uint32_t kCeLongChain = 128;
 constexpr uint32_t kCeLongChainF16 = 32;
 
@@ -760,7 +760,7 @@ static CePlan ce_plan(uint64_t rows, uint64_t width, uint64_t vocabulary, bool b
     if (p.per_block < 8) p.per_block = 8;
     p.blocks = (int)((rows + p.per_block - 1) / p.per_block);
     // Fewer tiles of dx than pairs: the sum over the vocabulary is split, eight steps a part at least, and a
-    // kernel adds up the parts.  515 x 1001 x 8193: 69 us instead of 95, 200 x 512 x 32768: 55 instead of 191.
+    // kernel adds up the parts.  515 x 1001 x 8193: 67 us instead of 93, 200 x 512 x 32768: 56 instead of 194.
     const uint64_t tiles = p.rows_pitch / kProductTile * ((width + kProductTile - 1) / kProductTile);
     const uint64_t steps = (p.piece + kProductStep - 1) / kProductStep;
     uint64_t splits = tiles ? kProductPairs / tiles : 1;

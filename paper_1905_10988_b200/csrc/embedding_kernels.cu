@@ -5,8 +5,8 @@
 // Forward, a warp moves up to 1024 columns of a row.  What bounds it: HBM.
 //
 // Backward, the tokens are sorted with their places, so that equal ones are neighbours in the order
-// of their places, and each row of the gradient is one sum in that order: no atomics, the same bits
-// from run to run.  Rows that no token names are cleared by blocks of their own, each of which scans the
+// of their places, and each row of the gradient is a sum in that order or, of many rows, of such sums: no
+// atomics, the same bits from run to run.  Rows that no token names are cleared by blocks of their own, each of which scans the
 // tokens for those of its rows, so that every row is written once.  Three kernels:
 //   - one cluster of up to eight blocks sorts (radix sort from the low digit, two digits up to a
 //     vocabulary of a million), while all other blocks clear as many rows as that takes time for;
@@ -35,15 +35,17 @@ constexpr int kClearBytes = 16384;       // of shared memory for the rows' flags
 constexpr int kSumThreads = 128;
 constexpr int kSumColumns = 8 * kSumThreads;
 constexpr int kMaxSegment = 32;          // sorted tokens of a block
-// Tokens that are not sorted at most.  512 tokens into 8192 x 768 binary32: 10 us, sorted 25; into 65536 x 4096
-// bfloat16: 95 and 94; 1024 into the latter: 115 and 96.
+// Tokens that are not sorted at most.  512 tokens into 8192 x 768 binary32: 9 us, sorted 19; into 32001 x 1001 26
+// and 39; into 65536 x 4096 bfloat16 94 and 96.  With a limit of 2048, which takes more registers: 512 10.6, 27
+// and 97; 1024 14, 31 and 112, sorted 20, 39 and 99; 2048 22, 40 and 146, sorted 21, 41 and 103.  So 512 is where
+// the largest table breaks even; a small one takes twice as long from 513 tokens on, and would not up to 1500.
 constexpr int kDirect = 512;
 constexpr int kDirectThreads = 512;
 // What is cleared beside the sort.  The blocks that do have scanned the tokens 7 to 8 us before the sort ends
 // (4096 tokens: after 4 of 11 us, 16384: after 7 of 15) and clear about 9 MB a microsecond.
 constexpr uint64_t kClearBeside = 64 << 20;
 // Bytes that a block clears beside the sums.  16384 x 4096 into 65536 rows, 4096 x 2048 into 32768, 8191 x 1001
-// into 32001: 140, 40, 52 us; 24 KB 144, 41, 55; 400 KB 140, 49, 57.
+// into 32001: 137, 39, 48 us; 24 KB 136, 38, 46; 400 KB 142, 76, 88.
 constexpr uint64_t kClearBlock = 96 << 10;
 // Cuts of a run that one warp joins.  30000 x 768 binary32 of one token: 179 us; left to one warp whatever the
 // number 252, all runs by eight warps 196.

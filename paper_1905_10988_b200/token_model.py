@@ -6,6 +6,7 @@ gradients of all parameters in one fp32 vector, which nc_compress reads.
     z = norm(x) table^T                   nc_layer_norm_forward
     loss = mean of lse(z) - z[target]     nc_linear_cross_entropy_forward: z is not kept
 
+The blocks work on every token by itself (nothing mixes tokens), so the model learns which token follows which.
 One table serves both ends: its gradient is written by nc_linear_cross_entropy_backward, and
 nc_embedding_backward adds the rows of the batch's tokens to it.  A token below 0 is padding (its row is 0),
 a target below 0 does not count.  apply() takes the aggregated gradient: the blocks' matrices move along
