@@ -113,3 +113,39 @@ def test_no_rows_clear_the_table_gradient_or_leave_it(kind, out, layout):
                                                 1.0, None, None, None, table, width, d.view, CODES[out], d.ld,
                                                 accumulate, ws, size)
             assert bool((d.view == (-77.0 if accumulate else 0.0)).all()) and d.untouched()
+
+
+# ---- more of the shapes that sums in chains come in ------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,vocabulary,kind,out,layout", [
+    (5000, 40, 700, "f16", "f16", "any"),            # dtable in chains, added to what is there
+    (2500, 1100, 20000, "f16", "f32", "whole"),      # both sums in chains, several tiles for every pair
+    (9000, 1300, 3000, "bf16", "bf16", "gap"),
+    (20000, 100, 8000, "bf16", "f32", "any"),        # the vocabulary in two pieces
+])
+def test_gradients_of_sums_in_chains(rows, width, vocabulary, kind, out, layout):
+    check_backward(Case(rows, width, vocabulary, kind, layout, without=0.2), out, True, True)
+
+
+@pytest.mark.gpu
+def test_a_layer_wider_than_the_steps_of_all_chains_in_32_bits():
+    width = 1 << 24
+    size = nc.nc_linear_cross_entropy_forward_workspace_bytes(1, width, 3)
+    if torch.cuda.mem_get_info()[0] < size + (2 << 30):
+        pytest.skip("not enough free memory")
+    # whole multiples of 2^-20 of which every sum is exact; the last chain of 1024 has none, the one before many
+    x = torch.ones(1, width, dtype=torch.bfloat16, device="cuda")
+    x[0, -1024:] = 0
+    x[0, -2048:-1024] = 8
+    table = torch.empty(3, width, dtype=torch.bfloat16, device="cuda")
+    for v in range(3):
+        table[v] = (v + 1) * 2.0 ** -20
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    loss, lse = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    nc.nc_linear_cross_entropy_forward(x, nc.DTYPE_BF16, 1, width, width, table, 3, width,
+                                       torch.zeros(1, dtype=torch.long, device="cuda"), 8, 1.0, loss, lse, ws, size)
+    z = torch.tensor([(v + 1) * 2.0 ** -20 * (width - 2048 + 8 * 1024) for v in range(3)], dtype=torch.float64)
+    want = float(torch.logsumexp(z, 0))
+    # a chain more or less is 2^-10; exponentials and the logarithm 8 u of 48
+    assert abs(float(lse) - want) <= 8 * U * 48 + 8 * U and abs(float(loss) - (want - float(z[0]))) <= 16 * U * 48
